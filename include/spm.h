@@ -435,6 +435,96 @@ int spm_ffn_noalloc(const spm_model_cfg* cfg, const void* blobs, int n_blobs, co
                     const float* w, int count, const float* x_norm, float* h_inout, void* stream,
                     int wait_and_check);
 
+/* ---- attention block: rotary positions and a key/value cache held in 4 bits ------------------------
+ * What stands before the router in a layer (the synthetic configurations omit it): queries, keys and values get their head norm
+ * and rotation, keys and values are cut to the 4-bit format of the experts as they enter a paged cache, and new rows attend to
+ * what the cache holds of their sequence. These calls need no context: they use no memory but their arguments, allocate nothing,
+ * enqueue on `stream` (a cudaStream_t of the current device) and return; spm_last_error(NULL) has the message of a refusal. They
+ * may be captured into CUDA graphs. All sizes that change from step to step (lengths, row starts, page numbers, positions) are
+ * read on the device, so a captured call serves every later step of the same batch shape.
+ *
+ * Cache: `pages` is [n_pages][n_kv_heads][page_size / 16] blocks; a block holds 16 tokens of one head in 18 * head_dim bytes:
+ *     key codes [head_dim/32][16 tokens][16 bytes], value codes alike, key scales fp16 [16 tokens][head_dim/32], value scales alike.
+ * Byte b of a group's 16 holds element 2b in its low half and 2b + 1 in its high half; element = scale * (code - 8). A group of 32 is
+ * written as scale = fp16(-m / 8), m its element of largest magnitude (the lowest of equals; the scale is kept within fp16's finite
+ * range), code = min(15, rint(x / scale) + 8) with x / scale taken as x times the fp32 reciprocal; a group whose scale is 0 gets codes 8.
+ *
+ * Batch: sequence s holds lengths[s] tokens, its new rows included, in pages page_table[s][0], [1], ... Its new rows are the rows
+ * row_start[s] .. row_start[s+1] - 1 of the row arrays; the last of n rows stands at position lengths[s] - 1, the first at lengths[s] - n.
+ * Rows from row_start[n_seq] on (a padded batch) are neither read nor written. A row before position 0 (more rows than tokens) is not
+ * written to the cache; read and attended, it gives zeros. Tokens beyond table_stride * page_size, and tokens of a page number outside
+ * 0 .. n_pages - 1, do not exist: they are not written, read as zeros, and attention passes over them; a status bit records it. A page
+ * that a call writes to belongs to one place of one sequence; pages that are only read may be shared. */
+#define SPM_KV_MAX_SEQS 1024
+#define SPM_KV_MAX_AXES 4
+#define SPM_KV_BAD_PAGE  1   /* a page number outside the pool               */
+#define SPM_KV_TOO_LONG  2   /* a length beyond its row of the page table    */
+#define SPM_KV_NONFINITE 4   /* a NaN or infinity was cut to 4 bits: NaN became 0, infinity the largest value that a scale allows */
+
+typedef struct {
+    void*    pages;         /* dev, 16-byte aligned, spm_kv_cache_bytes() long                                  */
+    int32_t* status;        /* dev: one word that SPM_KV_* bits are or-ed into; NULL: not recorded              */
+    int32_t  n_pages;
+    int32_t  page_size;     /* tokens, a multiple of 16, at most 65536                                          */
+    int32_t  n_kv_heads;
+    int32_t  head_dim;      /* 64, 128 or 256                                                                   */
+} spm_kv_cache;
+
+typedef struct {
+    const int32_t* page_table;    /* dev [n_seq][table_stride]                                                  */
+    const int32_t* lengths;       /* dev [n_seq]                                                                */
+    const int32_t* row_start;     /* dev [n_seq + 1], not falling; NULL: row s is the one new row of sequence s */
+    int32_t n_seq;                /* 0 .. SPM_KV_MAX_SEQS                                                       */
+    int32_t table_stride;         /* page numbers a sequence                                                    */
+    int32_t n_rows;               /* rows of the row arrays                                                     */
+    int32_t max_rows;             /* about how many new rows the longest prompt has (0: n_rows / n_seq): chooses between
+                                     kernels for few and for many rows; results hold for any value              */
+} spm_kv_batch;
+
+/* Rows of heads: element e of head h of row i is p[i * row_stride + h * head_stride + e] (strides in elements). p and both strides in
+ * bytes are multiples of 16. */
+typedef struct { void* p; int64_t row_stride, head_stride; } spm_rows;
+
+/* Norm and rotation of a head: x * rsqrt(mean(x^2) + eps) * gamma (gamma NULL: no norm), then pair i = 0 .. rot_dim/2 - 1 is turned by
+ * the angle positions[axis_of[i]][row] * inv_freq[i]. Angles and the norm's sum are taken in 64 bits (far positions; and a last bit more
+ * or less may cut a value into another 4-bit code). */
+typedef struct {
+    const float*   inv_freq;      /* dev [rot_dim / 2]                                                           */
+    const uint8_t* axis_of;       /* dev [rot_dim / 2], each below n_axes (larger ones count as the last axis); NULL: axis 0 */
+    const float*   q_gamma;       /* dev [head_dim] or NULL                                                      */
+    const float*   k_gamma;
+    int32_t n_axes;               /* 1 .. SPM_KV_MAX_AXES                                                        */
+    int32_t rot_dim;              /* leading elements that turn: a multiple of head_dim / 16, at most head_dim; 0: none */
+    int32_t neighbours;           /* 0: pair i is elements (i, i + rot_dim/2); 1: elements (2i, 2i + 1)          */
+    float   eps;
+} spm_rope;
+
+int spm_kv_cache_bytes(const spm_kv_cache* kv, size_t* bytes);      /* of `pages`, from the other fields */
+
+/* y = norm and rotation (q_gamma) of x: n_rows rows of n_heads heads. positions dev [n_axes][pos_stride]. y may be x itself (same
+ * strides); it may not overlap it otherwise. dtype: SPM_DTYPE_FP32 or SPM_DTYPE_BF16, of x and y. */
+int spm_rotate_heads(const spm_rope* rope, const int32_t* positions, int64_t pos_stride, const spm_rows* x, const spm_rows* y,
+                     int n_rows, int n_heads, int head_dim, int dtype, void* stream);
+
+/* The batch's new rows of k and v go into the cache (k normed with k_gamma and rotated first), and q_out = norm and rotation of q
+ * (n_q_heads heads; q NULL: none). rope NULL: neither norm nor rotation, and q must be NULL. */
+int spm_kv_write(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
+                 const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* k, const spm_rows* v, int dtype, void* stream);
+
+/* The cache's rows at the positions of the batch's new rows (all of a sequence's tokens, where it has as many rows as tokens). k_out or
+ * v_out may be NULL. */
+int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* k_out, const spm_rows* v_out, int dtype, void* stream);
+
+/* out = softmax(scale * q K^T) V for each new row and each of its n_q_heads heads (a multiple of n_kv_heads: query head h reads cache head
+ * h / (n_q_heads / n_kv_heads)), over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's
+ * statistics and all sums are fp32; bf16 calls round probabilities (and many-row calls the cache's values) once to 16 bits for the tensor
+ * cores. Results do not depend on the order in which CTAs run.
+ * workspace: dev, 16-byte aligned, at least spm_kv_attend_workspace() bytes; what it held before does not matter, and calls that may run
+ * at the same time need one each. */
+int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, int n_q_heads, int dtype, size_t* bytes);
+int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_q_heads, const spm_rows* out, float scale,
+                  int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Pinned host memory for the expert store (thin wrappers over cudaHostAlloc / cudaFreeHost). */
 int spm_host_alloc(size_t bytes, void** out);
 int spm_host_free(void* p);

@@ -18,6 +18,7 @@ SPM_OK = 0
 ERR_NAMES = {-1: "SPM_ERR_INVALID_ARG", -2: "SPM_ERR_CONFIG", -3: "SPM_ERR_CUDA", -4: "SPM_ERR_TIMEOUT",
              -5: "SPM_ERR_NOT_RESIDENT", -6: "SPM_ERR_STATE", -7: "SPM_ERR_NUMERIC"}
 DTYPE_FP32, DTYPE_BF16, DTYPE_Q4 = 0, 1, 2
+KV_BAD_PAGE, KV_TOO_LONG, KV_NONFINITE, KV_MAX_SEQS = 1, 2, 4, 1024
 POLICY_ADAPTER, POLICY_ON_DEMAND, POLICY_HINT_TRACE, POLICY_PRED0, POLICY_NAIVE = 0, 1, 2, 3, 4
 POLICIES = {"adapter": 0, "on_demand": 1, "hint_trace": 2, "pred0": 3, "naive": 4}
 EVENT_NAMES = {1: "HIT", 2: "HIT_PREFETCHED", 3: "MISS", 4: "EVICT", 5: "EVICT_WASTED", 6: "PREFETCH",
@@ -60,6 +61,24 @@ class Stats(C.Structure):
         d = {k: getattr(self, k) for k, _ in self._fields_}
         d["recall_at"] = list(d["recall_at"])
         return d
+
+
+class KvCache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("status", C.c_void_p)] + [(k, C.c_int32) for k in ("n_pages", "page_size", "n_kv_heads", "head_dim")]
+
+
+class KvBatch(C.Structure):
+    _fields_ = ([(k, C.c_void_p) for k in ("page_table", "lengths", "row_start")]
+                + [(k, C.c_int32) for k in ("n_seq", "table_stride", "n_rows", "max_rows")])
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = ([(k, C.c_void_p) for k in ("inv_freq", "axis_of", "q_gamma", "k_gamma")]
+                + [(k, C.c_int32) for k in ("n_axes", "rot_dim", "neighbours")] + [("eps", C.c_float)])
 
 
 # symbol -> argument types (all return int except spm_last_error)
@@ -107,6 +126,14 @@ _SIG = {
     "spm_get_slot_table": [_P, C.c_int, _P],
     "spm_synchronize": [_P],
     "spm_ffn_noalloc": [C.POINTER(ModelCfg), _P, C.c_int, _P, _P, C.c_int, _P, _P, _P, C.c_int],
+    "spm_kv_cache_bytes": [C.POINTER(KvCache), C.POINTER(C.c_size_t)],
+    "spm_rotate_heads": [C.POINTER(Rope), _P, C.c_int64, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_int, C.c_int, C.c_int, _P],
+    "spm_kv_write": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rope), _P, C.c_int64, C.POINTER(Rows), C.POINTER(Rows), C.c_int,
+                     C.POINTER(Rows), C.POINTER(Rows), C.c_int, _P],
+    "spm_kv_read": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rows), C.POINTER(Rows), C.c_int, _P],
+    "spm_kv_attend_workspace": [C.POINTER(KvCache), C.POINTER(KvBatch), C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "spm_kv_attend": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rows), C.c_int, C.POINTER(Rows), C.c_float, C.c_int, _P,
+                      C.c_size_t, _P],
     "spm_host_alloc": [C.c_size_t, C.POINTER(_P)],
     "spm_host_free": [_P],
     "spm_sim_create": [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(_P)],
@@ -443,6 +470,35 @@ def spm_plan_grouped_chunks(n_units, n_dt, grid):
     count = C.c_size_t()
     _check(load().spm_plan_grouped_chunks(n_units, n_dt, grid, _ptr(chunks), cap, C.byref(count)))
     return chunks[:count.value]
+
+
+# (structs come in and go out as they are; a struct that is None is a null pointer)
+def spm_kv_cache_bytes(kv: KvCache) -> int:
+    out = C.c_size_t()
+    _check(load().spm_kv_cache_bytes(C.byref(kv), C.byref(out)))
+    return out.value
+
+
+def spm_rotate_heads(rope, positions, pos_stride, x, y, n_rows, n_heads, head_dim, dtype, stream=None):
+    _check(load().spm_rotate_heads(rope, positions, pos_stride, x, y, n_rows, n_heads, head_dim, dtype, stream))
+
+
+def spm_kv_write(kv, batch, rope, positions, pos_stride, q, q_out, n_q_heads, k, v, dtype, stream=None):
+    _check(load().spm_kv_write(kv, batch, rope, positions, pos_stride, q, q_out, n_q_heads, k, v, dtype, stream))
+
+
+def spm_kv_read(kv, batch, k_out, v_out, dtype, stream=None):
+    _check(load().spm_kv_read(kv, batch, k_out, v_out, dtype, stream))
+
+
+def spm_kv_attend_workspace(kv, batch, n_q_heads, dtype) -> int:
+    out = C.c_size_t()
+    _check(load().spm_kv_attend_workspace(kv, batch, n_q_heads, dtype, C.byref(out)))
+    return out.value
+
+
+def spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
+    _check(load().spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream))
 
 
 def spm_host_alloc(nbytes: int) -> int:

@@ -1,0 +1,214 @@
+// The entry points of the attention block: checks of arguments, launches.
+#include <cstdint>
+#include <string>
+#include <type_traits>
+
+#include <cuda_runtime.h>
+
+#include "kv_attend.cuh"
+#include "kv_write.cuh"
+
+namespace spm {
+void set_thread_error(const std::string& msg);   // defined next to spm_last_error
+}
+
+using namespace spm;
+
+namespace {
+
+int fail(const char* call, int code, const std::string& msg) {
+    set_thread_error(std::string(call) + ": " + msg);
+    return code;
+}
+int launched(const char* call) {
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
+}
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+int check_dtype(const char* call, int dtype) {
+    return dtype == SPM_DTYPE_FP32 || dtype == SPM_DTYPE_BF16 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "rows are fp32 or bf16");
+}
+int check_head_dim(const char* call, int hd) {
+    return hd == 64 || hd == 128 || hd == 256 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(hd) + " not supported: 64, 128 or 256");
+}
+int check_cache_shape(const char* call, const spm_kv_cache* kv) {
+    if (!kv) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_head_dim(call, kv->head_dim)) return rc;
+    if (kv->page_size < kKvBlock || kv->page_size % kKvBlock || kv->page_size > 65536)
+        return fail(call, SPM_ERR_CONFIG, "page_size " + std::to_string(kv->page_size) + " is not a multiple of 16 up to 65536");
+    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return fail(call, SPM_ERR_CONFIG, "n_kv_heads outside 1..1024");
+    if (kv->n_pages < 0) return fail(call, SPM_ERR_INVALID_ARG, "n_pages is negative");
+    return SPM_OK;
+}
+int check_cache(const char* call, const spm_kv_cache* kv) {
+    if (int rc = check_cache_shape(call, kv)) return rc;
+    if (!kv->pages && kv->n_pages > 0) return fail(call, SPM_ERR_INVALID_ARG, "pages is null");
+    if (!aligned(kv->pages, 16) || !aligned(kv->status, 4)) return fail(call, SPM_ERR_INVALID_ARG, "pages must be 16-byte aligned, status 4-byte aligned");
+    return SPM_OK;
+}
+int check_batch(const char* call, const spm_kv_cache* kv, const spm_kv_batch* b) {
+    if (!b) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (b->n_seq < 0 || b->n_seq > SPM_KV_MAX_SEQS) return fail(call, SPM_ERR_INVALID_ARG, "n_seq " + std::to_string(b->n_seq) + " outside 0.." + std::to_string(SPM_KV_MAX_SEQS));
+    if (b->n_rows < 0 || b->max_rows < 0 || b->table_stride < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
+    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX) return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 1 tokens");
+    if (b->n_seq > 0 && (!b->lengths || (!b->page_table && b->table_stride > 0))) return fail(call, SPM_ERR_INVALID_ARG, "page_table or lengths is null");
+    if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_start, 4)) return fail(call, SPM_ERR_INVALID_ARG, "page_table, lengths and row_start must be 4-byte aligned");
+    if (!b->row_start && b->n_rows < b->n_seq) return fail(call, SPM_ERR_INVALID_ARG, "fewer rows than sequences, and no row_start");
+    return SPM_OK;
+}
+int check_rows(const char* call, const char* name, const spm_rows* r, int dtype) {
+    const long long e = dtype == SPM_DTYPE_BF16 ? 2 : 4;
+    if (!r || !r->p) return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + " is null");
+    if (!aligned(r->p, 16) || r->row_stride * e % 16 || r->head_stride * e % 16)
+        return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + ": rows of heads must start on 16-byte boundaries");
+    return SPM_OK;
+}
+int check_rope(const char* call, const spm_rope* r, const int32_t* positions, int64_t pos_stride, int n_rows, int hd) {
+    if (!r) return fail(call, SPM_ERR_INVALID_ARG, "rope is null");
+    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % (hd / 16)) return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of head_dim / 16 up to head_dim");
+    if (r->n_axes < 1 || r->n_axes > SPM_KV_MAX_AXES) return fail(call, SPM_ERR_INVALID_ARG, "n_axes outside 1.." + std::to_string(SPM_KV_MAX_AXES));
+    if (r->rot_dim > 0 && (!r->inv_freq || !positions)) return fail(call, SPM_ERR_INVALID_ARG, "inv_freq or positions is null");
+    if (r->rot_dim > 0 && r->n_axes > 1 && pos_stride < n_rows) return fail(call, SPM_ERR_INVALID_ARG, "pos_stride is less than the rows");
+    if (!aligned(r->inv_freq, 4) || !aligned(positions, 4) || !aligned(r->q_gamma, 16) || !aligned(r->k_gamma, 16))
+        return fail(call, SPM_ERR_INVALID_ARG, "gammas must be 16-byte aligned, inv_freq and positions 4-byte aligned");
+    return SPM_OK;
+}
+
+KvPool pool_of(const spm_kv_cache* kv) { return {static_cast<unsigned char*>(kv->pages), kv->status, kv->n_pages, kv->page_size, kv->n_kv_heads}; }
+KvBatch batch_of(const spm_kv_batch* b) { return {b->page_table, b->lengths, b->row_start, b->n_seq, b->table_stride, b->n_rows}; }
+HeadRows rows_of(const spm_rows* r) { return {r->p, r->row_stride, r->head_stride}; }
+RopeArgs rope_of(const spm_rope* r, const int32_t* positions, int64_t pos_stride) {
+    return {r->inv_freq, r->axis_of, r->q_gamma, r->k_gamma, positions, pos_stride, r->n_axes, r->rot_dim, r->neighbours, r->eps};
+}
+
+// calls f with a null pointer of the row type and the head size as a constant
+template <typename F>
+void by_type(int dtype, int hd, F f) {
+    auto size = [&](auto* t) {
+        if (hd == 64) f(t, std::integral_constant<int, 64>{});
+        else if (hd == 128) f(t, std::integral_constant<int, 128>{});
+        else f(t, std::integral_constant<int, 256>{});
+    };
+    if (dtype == SPM_DTYPE_BF16) size(static_cast<__nv_bfloat16*>(nullptr));
+    else size(static_cast<float*>(nullptr));
+}
+
+int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaStream_t st) {
+    const int heads = 2 * a.kv_heads + a.q_heads;
+    if (a.n_rows == 0 || heads == 0) return SPM_OK;
+    // a few rows: a head a warp, for latency; many: a block goes through all heads of its row, whose angles it takes once
+    const int chunks = (heads + kKvWarps - 1) / kKvWarps;
+    const dim3 grid(a.n_rows, static_cast<long long>(a.n_rows) * chunks <= 592 ? chunks : 1);
+    by_type(dtype, hd, [&](auto* t, auto size) {
+        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a);
+    });
+    return launched(call);
+}
+
+}  // namespace
+
+extern "C" {
+
+int spm_kv_cache_bytes(const spm_kv_cache* kv, size_t* bytes) {
+    if (!bytes) return fail("spm_kv_cache_bytes", SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_cache_shape("spm_kv_cache_bytes", kv)) return rc;
+    *bytes = size_t(kv->n_pages) * kv->n_kv_heads * (kv->page_size / kKvBlock) * kv_block_bytes(kv->head_dim);
+    return SPM_OK;
+}
+
+int spm_rotate_heads(const spm_rope* rope, const int32_t* positions, int64_t pos_stride, const spm_rows* x, const spm_rows* y,
+                     int n_rows, int n_heads, int head_dim, int dtype, void* stream) {
+    const char* call = "spm_rotate_heads";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_head_dim(call, head_dim)) return rc;
+    if (n_rows < 0 || n_heads < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
+    if (n_rows == 0 || n_heads == 0) return SPM_OK;
+    if (int rc = check_rope(call, rope, positions, pos_stride, n_rows, head_dim)) return rc;
+    if (int rc = check_rows(call, "x", x, dtype)) return rc;
+    if (int rc = check_rows(call, "y", y, dtype)) return rc;
+    WriteArgs a{};
+    a.kv.page_size = kKvBlock;
+    a.batch.n_seq = -1;
+    a.rope = rope_of(rope, positions, pos_stride);
+    a.q = rows_of(x); a.q_out = rows_of(y);
+    a.q_heads = n_heads; a.n_rows = n_rows;
+    return launch_write(call, a, head_dim, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int spm_kv_write(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
+                 const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* k, const spm_rows* v, int dtype, void* stream) {
+    const char* call = "spm_kv_write";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (n_q_heads < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
+    if (q && !rope) return fail(call, SPM_ERR_INVALID_ARG, "q without rope: there is nothing to do to it");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    if (rope)
+        if (int rc = check_rope(call, rope, positions, pos_stride, batch->n_rows, kv->head_dim)) return rc;
+    if (int rc = check_rows(call, "k", k, dtype)) return rc;
+    if (int rc = check_rows(call, "v", v, dtype)) return rc;
+    if (q) {
+        if (int rc = check_rows(call, "q", q, dtype)) return rc;
+        if (int rc = check_rows(call, "q_out", q_out, dtype)) return rc;
+    }
+    WriteArgs a{};
+    a.kv = pool_of(kv);
+    a.batch = batch_of(batch);
+    if (rope) a.rope = rope_of(rope, positions, pos_stride);
+    if (q) { a.q = rows_of(q); a.q_out = rows_of(q_out); a.q_heads = n_q_heads; }
+    a.k = rows_of(k); a.v = rows_of(v);
+    a.kv_heads = kv->n_kv_heads; a.n_rows = batch->n_rows;
+    return launch_write(call, a, kv->head_dim, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* k_out, const spm_rows* v_out, int dtype, void* stream) {
+    const char* call = "spm_kv_read";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (!k_out && !v_out) return fail(call, SPM_ERR_INVALID_ARG, "neither k_out nor v_out");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    ReadArgs a{};
+    a.kv = pool_of(kv);
+    a.batch = batch_of(batch);
+    if (k_out) { if (int rc = check_rows(call, "k_out", k_out, dtype)) return rc; a.k = rows_of(k_out); }
+    if (v_out) { if (int rc = check_rows(call, "v_out", v_out, dtype)) return rc; a.v = rows_of(v_out); }
+    const unsigned grid = unsigned((static_cast<long long>(batch->n_rows) + kKvWarps - 1) / kKvWarps);
+    by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
+        kv_read_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    });
+    return launched(call);
+}
+
+int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, int n_q_heads, int dtype, size_t* bytes) {
+    const char* call = "spm_kv_attend_workspace";
+    if (!bytes) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_cache_shape(call, kv)) return rc;
+    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
+    *bytes = 0;
+    return SPM_OK;
+}
+
+int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_q_heads, const spm_rows* out, float scale,
+                  int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* call = "spm_kv_attend";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    if (int rc = check_rows(call, "q", q, dtype)) return rc;
+    if (int rc = check_rows(call, "out", out, dtype)) return rc;
+    AttendArgs a{pool_of(kv), batch_of(batch), rows_of(q), rows_of(out), n_q_heads, scale};
+    by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
+        kv_attend_kernel<std::remove_pointer_t<decltype(t)>, size.value>
+            <<<dim3(batch->n_rows, n_q_heads), kKvWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    });
+    return launched(call);
+}
+
+}  // extern "C"

@@ -1,0 +1,188 @@
+"""The cache side of an attention block, on torch tensors: rotary positions, a key/value cache held in 4 bits, attention over it.
+
+Marshals to spm_rotate_heads, spm_kv_write, spm_kv_read and spm_kv_attend (include/spm.h says what they compute and how a page is
+laid out). Everything is enqueued on the current stream of the tensors' device and may be captured into a CUDA graph; lengths, row
+starts, page numbers and positions are read on the device. Outputs and workspaces come from torch's allocator, a call's own each.
+"""
+from __future__ import annotations
+
+import contextlib
+
+import torch
+
+from . import binding as B
+
+DTYPES = {torch.float32: B.DTYPE_FP32, torch.bfloat16: B.DTYPE_BF16}
+BLOCK = 16                      # tokens of a block
+_HERE = contextlib.nullcontext()
+
+
+def _need(ok, message):
+    if not ok:
+        raise ValueError(message)
+
+
+def _on(device):
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _vector(x, dtype, device, what, n=None):
+    _need(x.dtype is dtype and x.dim() == 1 and x.is_contiguous() and x.device == device, f"{what}: a contiguous {dtype} vector on {device}")
+    _need(n is None or x.numel() == n, f"{what}: {n} elements")
+    return x.data_ptr()
+
+
+def _rows(x, heads, hd, dtype, device, what):
+    """spm_rows of a tensor [rows, heads, hd] whose heads are contiguous."""
+    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != hd:
+        raise ValueError(f"{what}: shape [rows, {heads}, {hd}], not {list(x.shape)}")
+    if x.dtype is not dtype or x.device != device:
+        raise ValueError(f"{what}: {dtype} on {device}, not {x.dtype} on {x.device}")
+    row, head, one = x.stride()
+    if one != 1:
+        raise ValueError(f"{what}: the elements of a head must be contiguous")
+    return B.Rows(x.data_ptr(), row, head)
+
+
+def _dtype(x, what):
+    _need(x.is_cuda, f"{what}: a CUDA tensor (there is no CPU implementation of this path)")
+    _need(x.dtype in DTYPES, f"{what}: fp32 or bf16, not {x.dtype}")
+    return DTYPES[x.dtype]
+
+
+class Rope:
+    """How heads are normed and turned. inv_freq [rot_dim / 2] fp32; axis_of [rot_dim / 2] uint8: which of the position's axes turns a
+    pair (None: the first); gammas [head_dim] fp32 or None (no norm); neighbours: pairs (2i, 2i + 1) instead of (i, i + rot_dim / 2)."""
+
+    def __init__(self, inv_freq, axis_of=None, q_gamma=None, k_gamma=None, eps=1e-6, neighbours=False):
+        _need(inv_freq.is_cuda, "inv_freq: a CUDA tensor")
+        self.device = inv_freq.device
+        self._keep = (inv_freq, axis_of, q_gamma, k_gamma)
+        half = inv_freq.numel()
+        self.gamma_sizes = tuple(None if g is None else g.numel() for g in (q_gamma, k_gamma))
+        fields = (_vector(inv_freq, torch.float32, self.device, "inv_freq"),
+                  None if axis_of is None else _vector(axis_of, torch.uint8, self.device, "axis_of", half),
+                  None if q_gamma is None else _vector(q_gamma, torch.float32, self.device, "q_gamma"),
+                  None if k_gamma is None else _vector(k_gamma, torch.float32, self.device, "k_gamma"))
+        self._by_axes = {n: B.Rope(*fields, n, 2 * half, int(neighbours), eps) for n in range(1, 5)}
+
+    def _with(self, positions, n_rows, hd, which):
+        """(struct, positions' address, axis stride) of a call with positions [n_axes, rows] or [rows]."""
+        _need(positions is not None, "positions are needed to turn heads")
+        _need(positions.dtype is torch.int32 and positions.device == self.device, f"positions: int32 on {self.device}")
+        for i in which:
+            _need(self.gamma_sizes[i] in (None, hd), f"gammas: {hd} elements")
+        p = positions if positions.dim() == 2 else positions[None]
+        _need(p.dim() == 2 and p.shape[1] == n_rows and 1 <= p.shape[0] <= 4, f"positions: [1..4 axes, {n_rows}], not {list(positions.shape)}")
+        _need(p.stride(1) == 1 or n_rows <= 1, "positions: the rows of an axis must be contiguous")
+        return self._by_axes[p.shape[0]], p.data_ptr(), p.stride(0) if p.shape[0] > 1 else n_rows
+
+
+class KVBatch:
+    """New rows of several sequences. page_table [n_seq, pages] int32; lengths [n_seq] int32: tokens each sequence holds, its new rows
+    included; row_start [n_seq + 1] int32: where a sequence's rows begin (None: one row each); n_rows: rows of the row tensors (None:
+    n_seq); max_rows: about how many rows the longest prompt has (0: their mean), which chooses between kernels and nothing else."""
+
+    def __init__(self, page_table, lengths, row_start=None, n_rows=None, max_rows=0):
+        _need(page_table.is_cuda and page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
+              "page_table: a contiguous int32 CUDA tensor [n_seq, pages]")
+        self.device = page_table.device
+        n = page_table.shape[0]
+        _need(row_start is not None or n_rows is None or n_rows >= n, "n_rows is less than the sequences, and there is no row_start")
+        self.n_rows = n if n_rows is None else n_rows
+        self._keep = (page_table, lengths, row_start)
+        self.c = B.KvBatch(page_table.data_ptr(), _vector(lengths, torch.int32, self.device, "lengths", n),
+                           None if row_start is None else _vector(row_start, torch.int32, self.device, "row_start", n + 1),
+                           n, page_table.shape[1], self.n_rows, max_rows)
+
+
+class KVCache:
+    """A pool of pages [n_pages, kv_heads, page_size / 16, 18 * head_dim] uint8. status: an int32 tensor of one element that SPM_KV_* bits are
+    or-ed into (bad page numbers, lengths beyond the table, numbers that are not finite), or None."""
+
+    def __init__(self, pages, status=None):
+        _need(pages.is_cuda and pages.dtype is torch.uint8 and pages.dim() == 4 and pages.is_contiguous() and pages.shape[3] % 18 == 0,
+              "pages: a contiguous uint8 CUDA tensor [n_pages, kv_heads, page_size / 16, 18 * head_dim]")
+        self.device, self.pages, self.status = pages.device, pages, status
+        self.kv_heads, self.page_size, self.head_dim = pages.shape[1], pages.shape[2] * BLOCK, pages.shape[3] // 18
+        self.c = B.KvCache(pages.data_ptr(), None if status is None else _vector(status, torch.int32, self.device, "status", 1),
+                           pages.shape[0], self.page_size, self.kv_heads, self.head_dim)
+        self._workspace = {}        # bytes that a call of a batch's shape asks for
+        B.spm_kv_cache_bytes(self.c)
+
+    @classmethod
+    def empty(cls, n_pages, page_size, kv_heads, head_dim, device="cuda", status=None):
+        _need(page_size % BLOCK == 0 and page_size > 0, "page_size: a multiple of 16")
+        return cls(torch.zeros(n_pages, kv_heads, page_size // BLOCK, 18 * head_dim, dtype=torch.uint8, device=device), status)
+
+    def _stream(self, batch):
+        _need(batch.device == self.device, "the batch is on another device than the cache")
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def write(self, batch, k, v, q=None, positions=None, rope=None, q_out=None):
+        """k, v [rows, kv_heads, head_dim] of the batch's new rows go into the cache, k normed and turned by `rope`; returns q [rows, q_heads,
+        head_dim] normed and turned (None without q)."""
+        dt, hd, n = _dtype(k, "k"), self.head_dim, batch.n_rows
+        ck, cv = _rows(k, self.kv_heads, hd, k.dtype, self.device, "k"), _rows(v, self.kv_heads, hd, k.dtype, self.device, "v")
+        _need(k.shape[0] == n and v.shape[0] == n, f"k, v: {n} rows")
+        cq = co = cr = pos = None
+        stride = heads = 0
+        if rope is not None:
+            cr, pos, stride = rope._with(positions, n, hd, (0, 1) if q is not None else (1,))
+        if q is not None:
+            _need(rope is not None, "q without rope: there is nothing to do to it")
+            heads = q.shape[1] if q.dim() == 3 else 0
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            cq, co = _rows(q, heads, hd, k.dtype, self.device, "q"), _rows(q_out, heads, hd, k.dtype, self.device, "q_out")
+            _need(q.shape[0] == n and q_out.shape[0] == n, f"q: {n} rows")
+        with _on(self.device):
+            B.spm_kv_write(self.c, batch.c, cr, pos, stride, cq, co, heads, ck, cv, dt, self._stream(batch))
+        return q_out
+
+    def read(self, batch, dtype=torch.bfloat16, k_out=None, v_out=None):
+        """The cache's keys and values at the positions of the batch's new rows: two tensors [rows, kv_heads, head_dim]."""
+        shape = (batch.n_rows, self.kv_heads, self.head_dim)
+        k_out, v_out = (torch.empty(shape, dtype=dtype, device=self.device) if x is None else x for x in (k_out, v_out))
+        dt = _dtype(k_out, "k_out")
+        ck, cv = (_rows(x, self.kv_heads, self.head_dim, k_out.dtype, self.device, "k_out, v_out") for x in (k_out, v_out))
+        _need(k_out.shape[0] == batch.n_rows and v_out.shape[0] == batch.n_rows, f"k_out, v_out: {batch.n_rows} rows")
+        with _on(self.device):
+            B.spm_kv_read(self.c, batch.c, ck, cv, dt, self._stream(batch))
+        return k_out, v_out
+
+    def attend(self, batch, q, scale=None, out=None):
+        """softmax(scale q K^T) V of q [rows, q_heads, head_dim], each row over its sequence's tokens up to its own position. scale None:
+        head_dim ** -0.5."""
+        dt, hd = _dtype(q, "q"), self.head_dim
+        heads = q.shape[1] if q.dim() == 3 else 0
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        cq, co = _rows(q, heads, hd, q.dtype, self.device, "q"), _rows(out, heads, hd, q.dtype, self.device, "out")
+        _need(q.shape[0] == batch.n_rows and out.shape[0] == batch.n_rows, f"q, out: {batch.n_rows} rows")
+        b = batch.c
+        key = (b.n_seq, b.table_stride, b.n_rows, b.max_rows, heads, dt)
+        with _on(self.device):
+            stream = self._stream(batch)
+            size = self._workspace.get(key)
+            if size is None:
+                size = self._workspace[key] = B.spm_kv_attend_workspace(self.c, b, heads, dt)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
+            B.spm_kv_attend(self.c, b, cq, heads, co, hd ** -0.5 if scale is None else scale, dt,
+                            work.data_ptr() if size else None, size, stream)
+        return out
+
+
+def rotate_heads(x, positions, rope, out=None):
+    """Norm (rope's q_gamma) and rotation of x [rows, heads, head_dim] by positions [axes, rows]."""
+    dt = _dtype(x, "x")
+    _need(x.dim() == 3 and x.device == rope.device, "x: [rows, heads, head_dim] on the device of the rope")
+    n, heads, hd = x.shape
+    c, pos, stride = rope._with(positions, n, hd, (0,))
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    cx, cy = _rows(x, heads, hd, x.dtype, x.device, "x"), _rows(out, heads, hd, x.dtype, x.device, "out")
+    _need(out.shape[0] == n, f"out: {n} rows")
+    with _on(x.device):
+        B.spm_rotate_heads(c, pos, stride, cx, cy, n, heads, hd, dt, torch.cuda.current_stream(x.device).cuda_stream)
+    return out
