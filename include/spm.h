@@ -460,6 +460,7 @@ int spm_ffn_noalloc(const spm_model_cfg* cfg, const void* blobs, int n_blobs, co
 #define SPM_KV_BAD_PAGE  1   /* a page number outside the pool               */
 #define SPM_KV_TOO_LONG  2   /* a length beyond its row of the page table    */
 #define SPM_KV_NONFINITE 4   /* a NaN or infinity was cut to 4 bits: NaN became 0, infinity the largest value that a scale allows */
+#define SPM_KV_TIMEOUT   8   /* a copy inside a kernel did not land within 2 s; the call's results are void */
 
 typedef struct {
     void*    pages;         /* dev, 16-byte aligned, spm_kv_cache_bytes() long                                  */

@@ -18,7 +18,7 @@ SPM_OK = 0
 ERR_NAMES = {-1: "SPM_ERR_INVALID_ARG", -2: "SPM_ERR_CONFIG", -3: "SPM_ERR_CUDA", -4: "SPM_ERR_TIMEOUT",
              -5: "SPM_ERR_NOT_RESIDENT", -6: "SPM_ERR_STATE", -7: "SPM_ERR_NUMERIC"}
 DTYPE_FP32, DTYPE_BF16, DTYPE_Q4 = 0, 1, 2
-KV_BAD_PAGE, KV_TOO_LONG, KV_NONFINITE, KV_MAX_SEQS = 1, 2, 4, 1024
+KV_BAD_PAGE, KV_TOO_LONG, KV_NONFINITE, KV_TIMEOUT, KV_MAX_SEQS = 1, 2, 4, 8, 1024
 POLICY_ADAPTER, POLICY_ON_DEMAND, POLICY_HINT_TRACE, POLICY_PRED0, POLICY_NAIVE = 0, 1, 2, 3, 4
 POLICIES = {"adapter": 0, "on_demand": 1, "hint_trace": 2, "pred0": 3, "naive": 4}
 EVENT_NAMES = {1: "HIT", 2: "HIT_PREFETCHED", 3: "MISS", 4: "EVICT", 5: "EVICT_WASTED", 6: "PREFETCH",

@@ -1,8 +1,20 @@
-// Attention of new rows over the 4-bit cache.
+// Attention of new rows over the 4-bit cache, for a few rows a sequence (and for many fp32 ones).
+//
+// For a cache head, the new rows' query heads that read it are columns: column x is head x % group of row x / group, and eight columns are
+// the N of an m16n8k16. Keys are its A operand (16 tokens by 16 elements) straight from their nibbles: the codes less 8 are exact in
+// bf16, the scale of a group is put on the sum of the group's 32 products. Values are the A operand of the second product, transposed by
+// ldmatrix (32 elements by 16 tokens); their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32
+// queries are split into three bf16 parts and probabilities into two.
+//
+// All (sequence, columns, head) items together are a line of tiles of 32 tokens that is cut evenly between CTAs, and a CTA's piece
+// evenly between its warps, whatever the lengths are: a warp walks its tiles with the running maximum and sum of each column, fed by its
+// own ring of bulk copies. Where a cut falls into an item the parts meet in shared memory (cuts between warps) or, for cuts between
+// CTAs, in the workspace, where kv_attend_join_kernel adds them in order.
 #pragma once
 
-#include "kv_write.cuh"
+#include "kv_cache.cuh"
 #include "ptx.cuh"
+#include "q4_mma.cuh"
 
 namespace spm {
 
@@ -10,64 +22,553 @@ struct AttendArgs {
     KvPool kv;
     KvBatch batch;
     HeadRows q, out;
-    int q_heads;
+    int group;                  // query heads a cache head
+    int min_tiles;              // of a CTA, before another one starts
     float scale;
+    float* parts;               // [2 * CTAs][part floats]
+    int* joins;                 // [CTAs][4]: CTAs that share the item that begins in this one and goes on behind it (0: none), sequence, columns, head
 };
 
-// A block takes a row and a head, a warp every eighth token: softmax by its running maximum and sum
-template <typename T, int HD>
-__global__ void __launch_bounds__(kKvWarps * 32) kv_attend_kernel(const AttendArgs a) {
-    constexpr int E = HD / 32;
-    __shared__ float part[kKvWarps][HD + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x, head = blockIdx.y;
-    const RowAt r = kv_row_at(a.batch, row);
-    if (r.seq >= a.batch.n_seq) return;
-    const int kv_head = head / (a.q_heads / a.kv.heads);
-    float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
-    load_row<E>(static_cast<const T*>(a.q.p) + row * a.q.row + head * a.q.head + lane * E, q);
-    const int g = lane * E / 32, in = lane * E % 32;
-    const long long cap = static_cast<long long>(a.batch.stride) * a.kv.page_size;
-    if (r.pos >= cap && threadIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-    const int n = int(min(static_cast<long long>(r.pos) + 1, cap));
-    for (int t = warp; t < n; t += kKvWarps) {
-        const long long block = kv_block_at<HD>(a.kv, a.batch, r.seq, t, kv_head);
-        if (block < 0) { if (lane == 0) kv_note(a.kv, SPM_KV_BAD_PAGE); continue; }
-        const unsigned char* at = a.kv.pages + block;
-        const int tok = t % kKvBlock;
-        float x[2][E];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const unsigned char* c = at + p * kv_v_codes(HD) + (g * kKvBlock + tok) * 16 + in / 2;
-            const float d = __half2float(*reinterpret_cast<const __half*>(at + kv_k_scales(HD) + p * HD + (tok * (HD / 32) + g) * 2));
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[p][e] = (float(c[e / 2] >> (4 * (e % 2)) & 15) - 8.f) * d;
+constexpr int kAtTile = 32;     // tokens
+constexpr int kAtMaxCtas = 148;
+constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
+
+template <int HD, int NT>
+struct AtShape {
+    static constexpr int cols = 8 * NT;
+    static constexpr int tile_bytes = kAtTile / kKvBlock * kv_block_bytes(HD);
+    static constexpr int part_floats = cols * (HD + 2);      // sums, then maxima, then sums of probabilities
+    static constexpr int part_bytes = (part_floats * 4 + 15) / 16 * 16;
+    // warps and stages of a warp's ring: what registers (the sums of HD x cols numbers, the queries) and shared memory leave
+    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : (HD == 256 ? 8 : 12);
+    static constexpr int stages = HD == 64 ? 4 : HD == 256 ? 2 : NT == 4 ? 4 : 3;
+    static constexpr int ring_bytes = stages * tile_bytes;
+    static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
+    static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8 + 64) + (n_seq + 1) * 4; }
+    static_assert(warps * (ring_bytes + part_bytes + stages * 8 + 64) + (SPM_KV_MAX_SEQS + 1) * 4 <= 232448, "227 KB");
+};
+
+// A walk along the line of tiles. nk: tokens that the last of the item's columns sees, nt: tiles (one at least, so that rows that see
+// nothing are written too).
+template <int COLS>
+struct Walk {
+    int seq, ct, head, t, nt, first, n, len, nk;
+
+    __device__ __forceinline__ void load(const AttendArgs& a) {
+        len = a.batch.lengths[seq];
+        first = seq; n = 1;
+        if (a.batch.row_start) {
+            first = a.batch.row_start[seq];
+            n = min(a.batch.row_start[seq + 1] - first, a.batch.n_rows);
         }
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s += q[e] * x[0][e];
-        s = warp_sum(s) * a.scale;
-        const float top = fmaxf(m, s), keep = __expf(m - top), p = __expf(s - top);
-        l = l * keep + p;
-        m = top;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * keep + p * x[1][e];
     }
+    __device__ __forceinline__ int blocks(const AttendArgs& a) const { return n > 0 ? (n * a.group + COLS - 1) / COLS : 0; }
+    __device__ __forceinline__ void columns(const AttendArgs& a) {
+        const int last = min(n - 1, ((ct + 1) * COLS - 1) / a.group);
+        nk = max(0, min(len - n + last + 1, a.batch.stride * a.kv.page_size));
+        nt = max(1, (nk + kAtTile - 1) / kAtTile);
+    }
+    __device__ __forceinline__ int tiles_of_sequence(const AttendArgs& a) {
+        int sum = 0;
+        const int m = blocks(a);
+        for (ct = 0; ct < m; ++ct) { columns(a); sum += nt; }
+        return sum * a.kv.heads;
+    }
+    __device__ __forceinline__ void seek(const AttendArgs& a, const int* before, int x) {
+        int lo = 0, hi = a.batch.n_seq;          // before[lo] <= x < before[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (before[mid] <= x) lo = mid; else hi = mid;
+        }
+        seq = lo;
+        load(a);
+        int rest = x - before[lo];
+        for (ct = 0;; ++ct) {
+            columns(a);
+            if (rest < nt * a.kv.heads) break;
+            rest -= nt * a.kv.heads;
+        }
+        head = rest / nt;
+        t = rest - head * nt;
+    }
+    __device__ __forceinline__ void next(const AttendArgs& a) {
+        if (++t < nt) return;
+        t = 0;
+        if (++head < a.kv.heads) return;
+        head = 0;
+        if (++ct >= blocks(a)) {
+            ct = 0;
+            do {
+                if (++seq >= a.batch.n_seq) return;
+                load(a);
+            } while (n <= 0);
+        }
+        columns(a);
+    }
+};
+
+// Where a column's result goes: its row, -1 where the item has no such column
+template <int COLS>
+__device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int n, int ct, int col, int& g) {
+    const int x = ct * COLS + col, i = x / a.group;
+    g = x - i * a.group;
+    return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
+}
+
+struct PartMeta { int id, seq, ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// HD / 32 scales of a token
+template <int G>
+__device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
+    uint32_t w[G / 2];
+    if constexpr (G == 2) w[0] = lds32(addr);
+    else if constexpr (G == 4) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
+    else { const uint4 v = lds128(addr); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
 #pragma unroll
-    for (int e = 0; e < E; ++e) part[warp][lane * E + e] = o[e];
-    if (lane == 0) { part[warp][HD] = m; part[warp][HD + 1] = l; }
+    for (int i = 0; i < G / 2; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        s[2 * i] = f.x; s[2 * i + 1] = f.y;
+    }
+}
+
+// One column's group of queries as the B operand: pairs (i, i + 4) of the eight elements 8 c .. 8 c + 7
+__device__ __forceinline__ void query_words(const __nv_bfloat16* p, uint32_t (&w)[1][4]) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0][0] = __byte_perm(v.x, v.z, 0x5410); w[0][1] = __byte_perm(v.x, v.z, 0x7632);
+    w[0][2] = __byte_perm(v.y, v.w, 0x5410); w[0][3] = __byte_perm(v.y, v.w, 0x7632);
+}
+__device__ __forceinline__ void query_words(const float* p, uint32_t (&w)[3][4]) {
+    float x[8];
+    load_row<8>(p, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Split3 s = split3(x[i], x[i + 4]);
+        w[0][i] = s.part[0]; w[1][i] = s.part[1]; w[2][i] = s.part[2];
+    }
+}
+
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kernel(const AttendArgs a) {
+    using S = AtShape<HD, NT>;
+    constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
+    constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 2 : 1;        // parts of a query, of a probability
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+    unsigned char* ring = smem + warp * S::ring_bytes;
+    float* own_part = reinterpret_cast<float*>(smem + W * S::ring_bytes + warp * S::part_bytes);
+    unsigned char* rest = smem + W * (S::ring_bytes + S::part_bytes);
+    const uint32_t bars = smem_u32(rest) + warp * STAGES * 8;
+    int* before = reinterpret_cast<int*>(rest + W * (STAGES * 8 + 64));
+    __shared__ PartMeta meta[2 * W];
+    __shared__ int warp_sum_of[W];
+
+    if (lane == 0) {
+        for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1);
+        fence_barrier_init();
+        meta[2 * warp].id = meta[2 * warp + 1].id = -1;
+    }
+    // ---- the line of tiles: tiles before each sequence ----
+    const int n_seq = a.batch.n_seq;
+    const int each = (n_seq + W * 32 - 1) / (W * 32);
+    int mine = 0;
+    Walk<COLS> use;
+    for (int i = 0; i < each; ++i) {
+        const int s = tid * each + i;
+        if (s >= n_seq) break;
+        use.seq = s;
+        use.load(a);
+        const int k = use.tiles_of_sequence(a);
+        if (use.n > 0 && use.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+        before[s] = mine;
+        mine += k;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) warp_sum_of[warp] = upto;
     __syncthreads();
-    for (int d = threadIdx.x * 8; d < HD; d += blockDim.x * 8) {
-        float top = -INFINITY, sum = 0.f, y[8] = {};
-        for (int w = 0; w < kKvWarps; ++w) top = fmaxf(top, part[w][HD]);
-        if (top > -INFINITY)
-            for (int w = 0; w < kKvWarps; ++w) {
-                const float f = __expf(part[w][HD] - top);
-                sum += part[w][HD + 1] * f;
-                for (int e = 0; e < 8; ++e) y[e] += part[w][d + e] * f;
-            }
-        for (int e = 0; e < 8; ++e) y[e] = sum > 0.f ? y[e] / sum : 0.f;
-        store_row<8>(static_cast<T*>(a.out.p) + row * a.out.row + head * a.out.head + d, y);
+    int all = 0, off = upto - mine;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < warp) off += warp_sum_of[w];
+        all += warp_sum_of[w];
     }
+    for (int i = 0; i < each; ++i)
+        if (tid * each + i < n_seq) before[tid * each + i] += off;
+    if (tid == 0) before[n_seq] = all;
+    __syncthreads();
+    grid_dep_launch();
+
+    const int ctas = max(1, min(int(gridDim.x), (all + a.min_tiles - 1) / a.min_tiles)), cta = blockIdx.x;
+    const int cta_lo = cta < ctas ? int(static_cast<long long>(all) * cta / ctas) : all;
+    const int cta_hi = cta < ctas ? int(static_cast<long long>(all) * (cta + 1) / ctas) : all;
+    const int lo = cta_lo + int(static_cast<long long>(cta_hi - cta_lo) * warp / W);
+    const int hi = cta_lo + int(static_cast<long long>(cta_hi - cta_lo) * (warp + 1) / W);
+    const int count = hi - lo;
+
+    float m[NT][2], l[NT][2], y[NT][G][2][4];
+    uint32_t qf[NT][QP][G][4];
+    if (count > 0) {
+        // ---- copies: lanes 0 and 1 take a block each; page numbers are looked up a tile ahead of their use ----
+        Walk<COLS> ahead;
+        ahead.seek(a, before, lo);
+        use = ahead;
+        const int per_page = a.kv.page_size / kKvBlock;
+        const uint32_t ring_at = smem_u32(ring);
+        uint32_t present = 0;                    // two bits a stage: which blocks are there
+        int issued = 0, page = -1, in_page = 0, ahead_head = 0;
+        bool wanted = false;
+        auto look_up = [&] {                     // for the tile `ahead`, which moves on
+            const int block = ahead.t * 2 + lane;
+            wanted = lane < 2 && block * kKvBlock < ahead.nk;
+            const int slot = block / per_page;
+            in_page = block - slot * per_page;
+            ahead_head = ahead.head;
+            page = wanted ? a.batch.table[size_t(ahead.seq) * a.batch.stride + slot] : -1;
+        };
+        auto issue = [&](int stage) {
+            const bool ok = wanted && page >= 0 && page < a.kv.n_pages;
+            if (wanted && !ok) kv_note(a.kv, SPM_KV_BAD_PAGE);
+            const long long at = ((static_cast<long long>(page) * a.kv.heads + ahead_head) * per_page + in_page) * BB;
+            const uint32_t have = __ballot_sync(0xffffffffu, ok);
+            const long long at0 = __shfl_sync(0xffffffffu, at, 0), at1 = __shfl_sync(0xffffffffu, at, 1);
+            const bool both = have == 3 && at1 == at0 + BB;
+            const uint32_t bar = bars + 8 * stage, dst = ring_at + stage * S::tile_bytes;
+            if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * BB);
+            __syncwarp();
+            if (ok && !(both && lane == 1)) bulk_g2s_plain(dst + lane * BB, a.kv.pages + at, both ? 2 * BB : BB, bar);
+            present = (present & ~(3u << (2 * stage))) | have << (2 * stage);
+            ++issued;
+            if (issued < count) { ahead.next(a); look_up(); }
+        };
+        look_up();
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i)
+            if (i < count) issue(i);
+
+        const float f = a.scale * (kQ4ExactUnscale * 1.4426950408889634f);
+        int began = use.t;                       // the item's tile with which this warp's part of it begins
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int i = 0; i < count; ++i) {
+            if (i == 0 || use.t == 0) {          // an item begins
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    int g;
+                    const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
+                    const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
+#pragma unroll
+                    for (int k = 0; k < G; ++k) {
+                        uint32_t w[QP][4] = {};
+                        if (row >= 0) query_words(p + 32 * k, w);
+#pragma unroll
+                        for (int q = 0; q < QP; ++q)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) qf[nt][q][k][j] = w[q][j];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) y[nt][k][0][j] = y[nt][k][1][j] = 0.f;
+                    }
+                    m[nt][0] = m[nt][1] = -INFINITY;
+                    l[nt][0] = l[nt][1] = 0.f;
+                }
+                began = use.t;
+            }
+            if (!mbar_wait_bounded(bars + 8 * stage, phase, kAtWaitNs)) {       // give up, but not with copies in flight
+                if (lane == 0) kv_note(a.kv, SPM_KV_TIMEOUT);
+                for (int j = i; j < issued; ++j) mbar_wait_bounded(bars + 8 * (j % STAGES), j / STAGES & 1, kAtWaitNs);
+                break;
+            }
+            const uint32_t at = ring_at + stage * S::tile_bytes, have = present >> (2 * stage) & 3;
+            // ---- scores: tokens r, r + 8 of each block for columns 2 c, 2 c + 1 ----
+            float s[NT][2][4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t block = at + b * BB;
+                float s0[G], s1[G];
+                token_scales<G>(block + kv_k_scales(HD) + r * (2 * G), s0);
+                token_scales<G>(block + kv_k_scales(HD) + (r + 8) * (2 * G), s1);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[nt][b][j] = 0.f;
+#pragma unroll
+                for (int k = 0; k < G; k += 2) {
+                    const uint4 w = ldsm4(block + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float d[4];
+                            mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
+                            mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[nt][0][k + h][2], qf[nt][0][k + h][3]);
+#pragma unroll
+                            for (int q = 1; q < QP; ++q) {
+                                mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][q][k + h][0], qf[nt][q][k + h][1]);
+                                mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[nt][q][k + h][2], qf[nt][q][k + h][3]);
+                            }
+                            s[nt][b][0] += s0[k + h] * d[0]; s[nt][b][1] += s0[k + h] * d[1];
+                            s[nt][b][2] += s1[k + h] * d[2]; s[nt][b][3] += s1[k + h] * d[3];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[nt][b][j] *= f;
+            }
+            // ---- tokens that are not there, or behind a column's row ----
+            const int row0 = use.ct * COLS / a.group;
+            const bool whole = have == 3 && (use.t + 1) * kAtTile <= min(use.nk, use.len - use.n + row0 + 1);
+            if (!whole) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int i2 = (use.ct * COLS + 8 * nt + 2 * c + e) / a.group;
+                        const int sees = min(use.nk, use.len - use.n + i2 + 1) - use.t * kAtTile;      // tokens of this tile
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                if (!(have >> b & 1) || 16 * b + 8 * j + r >= sees) s[nt][b][2 * j + e] = -INFINITY;
+                    }
+            }
+            // ---- running maximum: moved only where a score is above it by enough (2^6) to matter ----
+            bool raise = false;
+            float top[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float v = fmaxf(fmaxf(s[nt][0][e], s[nt][0][2 + e]), fmaxf(s[nt][1][e], s[nt][1][2 + e]));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+                    top[nt][e] = v;
+                    raise |= v > m[nt][e] + 6.f || (m[nt][e] == -INFINITY && v > -INFINITY);
+                }
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float to = fmaxf(m[nt][e], top[nt][e]), by = to == -INFINITY ? 1.f : ex2(m[nt][e] - to);
+                        m[nt][e] = to;
+                        l[nt][e] *= by;
+#pragma unroll
+                        for (int k = 0; k < G; ++k) { y[nt][k][0][e] *= by; y[nt][k][0][2 + e] *= by; y[nt][k][1][e] *= by; y[nt][k][1][2 + e] *= by; }
+                    }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float base = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const float p = ex2(s[nt][b][2 * j + e] - base);
+                            s[nt][b][2 * j + e] = p;
+                            l[nt][e] += p;
+                        }
+                }
+            // ---- y += V^T p, the values' scales on p ----
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t block = at + b * BB;
+                float s0[G], s1[G];
+                token_scales<G>(block + kv_v_scales(HD) + r * (2 * G), s0);
+                token_scales<G>(block + kv_v_scales(HD) + (r + 8) * (2 * G), s1);
+                if (!whole) {                    // what has never been written may be anything
+#pragma unroll
+                    for (int k = 0; k < G; ++k) {
+                        if (!(have >> b & 1) || use.t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
+                        if (!(have >> b & 1) || use.t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < G; k += 2) {
+                    const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float p0 = s[nt][b][0] * s0[k + h], p1 = s[nt][b][1] * s0[k + h], p2 = s[nt][b][2] * s1[k + h], p3 = s[nt][b][3] * s1[k + h];
+#pragma unroll
+                            for (int q = 0; q < PP; ++q) {
+                                const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3);
+                                if (q + 1 < PP) {
+                                    float x0, x1;
+                                    two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
+                                    two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
+                                }
+                                const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
+                                mma_k16(y[nt][k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                                mma_k16(y[nt][k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (i + STAGES < count) issue(stage);
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
+
+            // ---- the item ends, or the warp's piece ----
+            const bool ends = use.t + 1 == use.nt;
+            if (ends || i + 1 == count) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float v = l[nt][e];
+                        v += __shfl_xor_sync(0xffffffffu, v, 4);
+                        v += __shfl_xor_sync(0xffffffffu, v, 8);
+                        v += __shfl_xor_sync(0xffffffffu, v, 16);
+                        l[nt][e] = v;
+                    }
+                if (ends && began == 0) {        // all of it is this warp's
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            int g;
+                            const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + 2 * c + e, g);
+                            if (row < 0) continue;
+                            const float by = l[nt][e] > 0.f ? kQ4ExactUnscale / l[nt][e] : 0.f;
+                            T* p = static_cast<T*>(a.out.p) + row * a.out.row + (use.head * a.group + g) * a.out.head + 4 * r;
+#pragma unroll
+                            for (int k = 0; k < G; ++k) {
+                                float o[4] = {y[nt][k][0][e] * by, y[nt][k][0][2 + e] * by, y[nt][k][1][e] * by, y[nt][k][1][2 + e] * by};
+                                store_row<4>(p + 32 * k, o);
+                            }
+                        }
+                } else {
+                    // an item that ends here began in another warp: the warp's first part. One that goes on is its last part, and the ring is free
+                    float* part = ends ? own_part : reinterpret_cast<float*>(ring);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int col = 8 * nt + 2 * c + e;
+#pragma unroll
+                            for (int k = 0; k < G; ++k)
+                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], y[nt][k][0][2 + e], y[nt][k][1][e], y[nt][k][1][2 + e]);
+                            if (r == 0) { part[COLS * HD + col] = m[nt][e]; part[COLS * HD + COLS + col] = l[nt][e]; }
+                        }
+                    if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - use.t, use.seq, use.ct, use.head, began, use.t + 1, use.nt, use.first, use.n};
+                }
+            }
+            use.next(a);
+        }
+    }
+    __syncthreads();
+
+    // ---- parts of one item in this CTA meet: they stand one after another ----
+    int joined = 0;                              // of the item that goes on behind this CTA
+    PartMeta open{};
+    for (int i = 0; i < 2 * W;) {
+        const PartMeta first = meta[i];
+        if (first.id < 0) { ++i; continue; }
+        int end = i, to = first.to;
+        for (int j = i; j < 2 * W && (meta[j].id < 0 || meta[j].id == first.id); ++j)
+            if (meta[j].id >= 0) { end = j; to = meta[j].to; }
+        const bool done = first.from == 0 && to == first.nt;
+        const int slot = first.from > 0 ? 0 : 1;
+        if (!done && slot == 1) {                // CTA of the item's last tile
+            const long long last = first.id + first.nt - 1;
+            joined = int(((last + 1) * ctas - 1) / all) - cta + 1;
+            open = first;
+        }
+        float* out_part = a.parts + (size_t(cta) * 2 + slot) * S::part_floats;
+        for (int x = tid; x < COLS * (HD / 4); x += W * 32) {
+            const int col = x / (HD / 4), d = x % (HD / 4) * 4;
+            float top = -INFINITY;
+            for (int j = i; j <= end; ++j) {
+                if (meta[j].id < 0) continue;
+                const float* p = reinterpret_cast<const float*>(j & 1 ? smem + (j / 2) * S::ring_bytes : smem + W * S::ring_bytes + (j / 2) * S::part_bytes);
+                top = fmaxf(top, p[COLS * HD + col]);
+            }
+            float sum = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int j = i; j <= end; ++j) {
+                if (meta[j].id < 0) continue;
+                const float* p = reinterpret_cast<const float*>(j & 1 ? smem + (j / 2) * S::ring_bytes : smem + W * S::ring_bytes + (j / 2) * S::part_bytes);
+                const float by = top == -INFINITY ? 0.f : ex2(p[COLS * HD + col] - top);
+                const float4 v = *reinterpret_cast<const float4*>(p + col * HD + d);
+                sum += by * p[COLS * HD + COLS + col];
+                o.x += by * v.x; o.y += by * v.y; o.z += by * v.z; o.w += by * v.w;
+            }
+            if (done) {
+                int g;
+                const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
+                const float by = sum > 0.f ? kQ4ExactUnscale / sum : 0.f;
+                float res[4] = {o.x * by, o.y * by, o.z * by, o.w * by};
+                if (row >= 0) store_row<4>(static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + d, res);
+            } else {
+                *reinterpret_cast<float4*>(out_part + col * HD + d) = o;
+                if (d == 0) { out_part[COLS * HD + col] = top; out_part[COLS * HD + COLS + col] = sum; }
+            }
+        }
+        i = end + 1;
+    }
+    if (tid == 0) *reinterpret_cast<int4*>(a.joins + 4 * cta) = make_int4(joined, open.seq, open.ct, open.head);
+}
+
+// Adds the parts of items that were cut between CTAs: block (x, column) takes the item that begins in CTA x and goes on behind it.
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(HD) kv_attend_join_kernel(const AttendArgs a) {
+    constexpr int COLS = AtShape<HD, NT>::cols, FLOATS = AtShape<HD, NT>::part_floats;
+    __shared__ float by[kAtMaxCtas], red[HD / 32];
+    grid_dep_wait();
+    const int cta = blockIdx.x, col = blockIdx.y, tid = threadIdx.x;
+    const int4 join = *reinterpret_cast<const int4*>(a.joins + 4 * cta);
+    if (join.x == 0) return;
+    Walk<COLS> w;
+    w.seq = join.y;
+    w.load(a);
+    int g;
+    const int row = row_of_column<COLS>(a, w.first, w.n, join.z, col, g);
+    if (row < 0) return;
+    // part 0 is the second slot of its CTA, the others are the first slots of theirs
+    const float* part = a.parts + size_t(cta) * 2 * FLOATS;
+    auto at = [&](int j) { return part + size_t(j == 0 ? 1 : 2 * j) * FLOATS; };
+    float top = -INFINITY;
+    for (int j = tid; j < join.x; j += HD) top = fmaxf(top, at(j)[COLS * HD + col]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if ((tid & 31) == 0) red[tid / 32] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) top = fmaxf(top, red[i]);
+    for (int j = tid; j < join.x; j += HD) by[j] = top == -INFINITY ? 0.f : ex2(at(j)[COLS * HD + col] - top);
+    __syncthreads();
+    float sum = 0.f, o = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < join.x; ++j) {
+        sum += by[j] * at(j)[COLS * HD + COLS + col];
+        o += by[j] * at(j)[col * HD + tid];
+    }
+    o = sum > 0.f ? o * (kQ4ExactUnscale / sum) : 0.f;
+    T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.w * a.group + g) * a.out.head + tid;
+    if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(o);
+    else *to = o;
 }
 
 }  // namespace spm

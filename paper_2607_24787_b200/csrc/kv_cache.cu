@@ -1,4 +1,6 @@
 // The entry points of the attention block: checks of arguments, launches.
+#include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <string>
 #include <type_traits>
@@ -106,6 +108,56 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
     return launched(call);
 }
 
+// Columns of an item in eights: as few as hold a sequence's new rows, as many as registers allow (fp32 queries take three times those
+// of bf16 ones, sums of wide heads twice those of 128)
+int attend_eights(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
+    const long long rows = !b->row_start ? 1 : b->max_rows ? b->max_rows : (b->n_rows + b->n_seq - 1) / std::max(b->n_seq, 1);
+    const long long cols = rows * (n_q_heads / kv->n_kv_heads);
+    const int most = dtype == SPM_DTYPE_BF16 ? (kv->head_dim == 256 ? 2 : 4) : (kv->head_dim == 256 ? 1 : 2);
+    return cols <= 8 ? 1 : cols <= 16 ? std::min(2, most) : most;
+}
+template <typename F>
+void by_eights(int n, F f) {
+    if (n == 1) f(std::integral_constant<int, 1>{});
+    else if (n == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
+}
+constexpr size_t attend_part_bytes(int hd, int eights) { return size_t(8 * eights) * (hd + 2) * 4; }
+size_t attend_bytes(int hd, int eights) { return kAtMaxCtas * (16 + 2 * attend_part_bytes(hd, eights)); }
+
+constexpr int kMaxDevices = 64;
+// Once a kernel and device: shared memory beyond 48 KB
+template <auto KERNEL>
+cudaError_t allow_smem(int dev, int bytes) {
+    static std::atomic<bool> done[kMaxDevices];
+    if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done[dev].store(true, std::memory_order_release);
+    return e;
+}
+
+template <typename T, int HD, int NT>
+cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st) {
+    using S = AtShape<HD, NT>;
+    cudaError_t e = allow_smem<kv_attend_kernel<T, HD, NT>>(dev, S::smem(SPM_KV_MAX_SEQS));
+    if (e != cudaSuccess) return e;
+    const int ctas = std::min(sms, kAtMaxCtas);
+    kv_attend_kernel<T, HD, NT><<<ctas, S::warps * 32, S::smem(a.batch.n_seq), st>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    // launched ahead of the first kernel's end, which it waits for: its blocks are in place when the parts are
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas, S::cols);
+    cfg.blockDim = dim3(HD);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD, NT>, a);
+}
+
 }  // namespace
 
 extern "C" {
@@ -189,7 +241,7 @@ int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, i
     if (int rc = check_cache_shape(call, kv)) return rc;
     if (int rc = check_batch(call, kv, batch)) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
-    *bytes = 0;
+    *bytes = attend_bytes(kv->head_dim, attend_eights(kv, batch, n_q_heads, dtype));
     return SPM_OK;
 }
 
@@ -203,12 +255,33 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     if (int rc = check_rows(call, "q", q, dtype)) return rc;
     if (int rc = check_rows(call, "out", out, dtype)) return rc;
-    AttendArgs a{pool_of(kv), batch_of(batch), rows_of(q), rows_of(out), n_q_heads, scale};
+    const int eights = attend_eights(kv, batch, n_q_heads, dtype);
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < attend_bytes(kv->head_dim, eights))
+        return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(attend_bytes(kv->head_dim, eights)) + " bytes");
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return fail(call, SPM_ERR_CUDA, cudaGetErrorString(e));
+    if (dev < 0 || dev >= kMaxDevices) return fail(call, SPM_ERR_CONFIG, "device ordinal out of range");
+    AttendArgs a{};
+    a.kv = pool_of(kv);
+    a.batch = batch_of(batch);
+    a.q = rows_of(q); a.out = rows_of(out);
+    a.group = n_q_heads / kv->n_kv_heads;
+    a.scale = scale;
+    a.joins = static_cast<int*>(workspace);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 16);
     by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
-        kv_attend_kernel<std::remove_pointer_t<decltype(t)>, size.value>
-            <<<dim3(batch->n_rows, n_q_heads), kKvWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+        using T = std::remove_pointer_t<decltype(t)>;
+        by_eights(eights, [&](auto n) {
+            constexpr int most = sizeof(T) == 2 ? (size.value == 256 ? 2 : 4) : (size.value == 256 ? 1 : 2);
+            if constexpr (n.value <= most) {
+                a.min_tiles = AtShape<size.value, n.value>::warps;
+                e = launch_attend<T, size.value, n.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
+            }
+        });
     });
-    return launched(call);
+    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
 }
 
 }  // extern "C"
