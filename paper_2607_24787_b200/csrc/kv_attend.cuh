@@ -1,10 +1,15 @@
 // Attention of new rows over the 4-bit cache, for a few rows a sequence (and for many fp32 ones).
 //
 // For a cache head, the new rows' query heads that read it are columns: column x is head x % group of row x / group, and eight columns are
-// the N of an m16n8k16. Keys are its A operand (16 tokens by 16 elements) straight from their nibbles: the codes less 8 are exact in
-// bf16, the scale of a group is put on the sum of the group's 32 products. Values are the A operand of the second product, transposed by
-// ldmatrix (32 elements by 16 tokens); their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32
-// queries are split into three bf16 parts and probabilities into two.
+// the N of an m16n8k16. Keys are its A operand (16 tokens by 16 elements) straight from their nibbles, and the scale of a group is put on
+// the sum of the group's 32 products. Values are the A operand of the second product, transposed by ldmatrix (32 elements by 16 tokens);
+// their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries are split into three bf16
+// parts and probabilities into two.
+// Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
+// bf16 calls of one eight of columns leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is
+// what the group's sum starts with. Values: the probability is scaled up, and one more product with -8 in the codes' place goes into the
+// running sum before theirs, so that what is left to round is a tile's and not the whole context's sum of codes. Other calls subtract the
+// 8 from each code, nine instructions for eight, which the columns then share.
 //
 // All (sequence, columns, head) items together are a line of tiles of 32 tokens that is cut evenly between CTAs, and a CTA's piece
 // evenly between its warps, whatever the lengths are: a warp walks its tiles with the running maximum and sum of each column, fed by its
@@ -23,6 +28,7 @@ struct AttendArgs {
     KvBatch batch;
     HeadRows q, out;
     int group;                  // query heads a cache head
+    int page_shift;             // blocks a page are 1 << page_shift, or -1
     int min_tiles;              // of a CTA, before another one starts
     float scale;
     float* parts;               // [2 * CTAs][part floats]
@@ -33,15 +39,19 @@ constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
 constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
 
-template <int HD, int NT>
+template <typename T, int HD, int NT>
 struct AtShape {
     static constexpr int cols = 8 * NT;
     static constexpr int tile_bytes = kAtTile / kKvBlock * kv_block_bytes(HD);
     static constexpr int part_floats = cols * (HD + 2);      // sums, then maxima, then sums of probabilities
     static constexpr int part_bytes = (part_floats * 4 + 15) / 16 * 16;
     // warps and stages of a warp's ring: what registers (the sums of HD x cols numbers, the queries) and shared memory leave
-    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : (HD == 256 ? 8 : 12);
-    static constexpr int stages = HD == 64 ? 4 : HD == 256 ? 2 : NT == 4 ? 4 : 3;
+    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
+    static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : NT == 4 ? 4 : 3;
+    static constexpr bool raw = sizeof(T) == 2 && NT == 1;              // codes as they are masked out
+    static constexpr float up = raw ? 64.f : 0.f;                       // probabilities are taken to 2^64 then
+    static constexpr float unscale = raw ? 0x1p69f : kQ4ExactUnscale;   // of sums of codes times probabilities
+    static constexpr float odd = raw ? 1.f / 16.f : 1.f;                // of elements 4 r + 1, 4 r + 3, whose codes stand four bits higher
     static constexpr int ring_bytes = stages * tile_bytes;
     static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
     static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8 + 64) + (n_seq + 1) * 4; }
@@ -127,6 +137,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
+// D = A B + {c0, c1, c0, c1}
+__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float (&c)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]));
+}
 // HD / 32 scales of a token
 template <int G>
 __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
@@ -141,26 +156,39 @@ __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
     }
 }
 
-// One column's group of queries as the B operand: pairs (i, i + 4) of the eight elements 8 c .. 8 c + 7
-__device__ __forceinline__ void query_words(const __nv_bfloat16* p, uint32_t (&w)[1][4]) {
+// One column's group of queries as the B operand: pairs (i, i + 4) of the eight elements 8 c .. 8 c + 7. bf16 queries are taken to the
+// nibbles' scale: 2^64 to codes of 2^-133, 2^60 to 16 times those; sums then stand at 2^-69 (queries of 2^63 and more, or below 2^-57,
+// would leave the range of numbers).
+constexpr uint32_t kAtUp64 = 0x5f805f80u, kAtUp60 = 0x5d805d80u;
+constexpr float kAtUp69 = 0x1p69f;
+constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus128 = 0x80808080u;      // -8 and -8 * 16 as codes
+template <bool RAW>
+__device__ __forceinline__ void query_words(const __nv_bfloat16* p, bool flip, uint32_t (&w)[1][4]) {
     const uint4 v = *reinterpret_cast<const uint4*>(p);
-    w[0][0] = __byte_perm(v.x, v.z, 0x5410); w[0][1] = __byte_perm(v.x, v.z, 0x7632);
-    w[0][2] = __byte_perm(v.y, v.w, 0x5410); w[0][3] = __byte_perm(v.y, v.w, 0x7632);
+    const uint32_t sign = flip ? 0x80008000u : 0u;
+    w[0][0] = __byte_perm(v.x, v.z, 0x5410) ^ sign; w[0][1] = __byte_perm(v.x, v.z, 0x7632) ^ sign;
+    w[0][2] = __byte_perm(v.y, v.w, 0x5410) ^ sign; w[0][3] = __byte_perm(v.y, v.w, 0x7632) ^ sign;
+    if constexpr (RAW) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? kAtUp60 : kAtUp64)));
+    }
 }
-__device__ __forceinline__ void query_words(const float* p, uint32_t (&w)[3][4]) {
+template <bool RAW>
+__device__ __forceinline__ void query_words(const float* p, bool flip, uint32_t (&w)[3][4]) {
     float x[8];
     load_row<8>(p, x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const Split3 s = split3(x[i], x[i + 4]);
+        const Split3 s = split3(flip ? -x[i] : x[i], flip ? -x[i + 4] : x[i + 4]);
         w[0][i] = s.part[0]; w[1][i] = s.part[1]; w[2][i] = s.part[2];
     }
 }
 
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kernel(const AttendArgs a) {
-    using S = AtShape<HD, NT>;
+__global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_kernel(const AttendArgs a) {
+    using S = AtShape<T, HD, NT>;
     constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
+    constexpr bool RAW = S::raw;
     constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 2 : 1;        // parts of a query, of a probability
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
@@ -222,70 +250,92 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
     float m[NT][2], l[NT][2], y[NT][G][2][4];
     uint32_t qf[NT][QP][G][4];
     if (count > 0) {
-        // ---- copies: lanes 0 and 1 take a block each; page numbers are looked up a tile ahead of their use ----
+        // ---- copies: lanes 0 and 1 walk ahead and look up a block's page each, a tile before its use. A page of an even number of
+        // blocks holds both ----
         Walk<COLS> ahead;
         ahead.seek(a, before, lo);
         use = ahead;
         const int per_page = a.kv.page_size / kKvBlock;
+        const bool even = per_page % 2 == 0;
+        const long long page_bytes = static_cast<long long>(a.kv.heads) * per_page * BB;
         const uint32_t ring_at = smem_u32(ring);
         uint32_t present = 0;                    // two bits a stage: which blocks are there
-        int issued = 0, page = -1, in_page = 0, ahead_head = 0;
-        bool wanted = false;
-        auto look_up = [&] {                     // for the tile `ahead`, which moves on
+        int issued = 0, page = -1, in_page = 0;
+        auto look_up = [&] {                     // for the tile `ahead`
             const int block = ahead.t * 2 + lane;
-            wanted = lane < 2 && block * kKvBlock < ahead.nk;
-            const int slot = block / per_page;
+            const int slot = a.page_shift >= 0 ? block >> a.page_shift : block / per_page;
             in_page = block - slot * per_page;
-            ahead_head = ahead.head;
-            page = wanted ? a.batch.table[size_t(ahead.seq) * a.batch.stride + slot] : -1;
+            page = block * kKvBlock < ahead.nk ? a.batch.table[size_t(ahead.seq) * a.batch.stride + slot] : -2;       // -2: not wanted
         };
         auto issue = [&](int stage) {
-            const bool ok = wanted && page >= 0 && page < a.kv.n_pages;
-            if (wanted && !ok) kv_note(a.kv, SPM_KV_BAD_PAGE);
-            const long long at = ((static_cast<long long>(page) * a.kv.heads + ahead_head) * per_page + in_page) * BB;
-            const uint32_t have = __ballot_sync(0xffffffffu, ok);
-            const long long at0 = __shfl_sync(0xffffffffu, at, 0), at1 = __shfl_sync(0xffffffffu, at, 1);
-            const bool both = have == 3 && at1 == at0 + BB;
-            const uint32_t bar = bars + 8 * stage, dst = ring_at + stage * S::tile_bytes;
-            if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * BB);
-            __syncwarp();
-            if (ok && !(both && lane == 1)) bulk_g2s_plain(dst + lane * BB, a.kv.pages + at, both ? 2 * BB : BB, bar);
-            present = (present & ~(3u << (2 * stage))) | have << (2 * stage);
+            uint32_t have = 0;
+            if (lane < 2) {
+                const bool ok = page >= 0 && page < a.kv.n_pages;
+                if (!ok && page != -2) kv_note(a.kv, SPM_KV_BAD_PAGE);
+                const unsigned char* from = a.kv.pages + (page * page_bytes + static_cast<long long>(ahead.head * per_page + in_page) * BB);
+                have = __ballot_sync(3u, ok);
+                const uint32_t bar = bars + 8 * stage, dst = ring_at + stage * S::tile_bytes, bytes = __popc(have) * BB;
+                if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+                __syncwarp(3u);
+                if (ok && (lane == 0 || !even)) bulk_g2s_plain(dst + lane * BB, from, even ? bytes : BB, bar);
+                if (issued + 1 < count) { ahead.next(a); look_up(); }
+            }
             ++issued;
-            if (issued < count) { ahead.next(a); look_up(); }
+            present = (present & ~(3u << (2 * stage))) | __shfl_sync(0xffffffffu, have, 0) << (2 * stage);
         };
-        look_up();
+        if (lane < 2) look_up();
 #pragma unroll
         for (int i = 0; i < STAGES; ++i)
             if (i < count) issue(i);
 
-        const float f = a.scale * (kQ4ExactUnscale * 1.4426950408889634f);
-        int began = use.t;                       // the item's tile with which this warp's part of it begins
+        // scores are kept as the products give them; f > 0 takes them to powers of two (a negative scale turns the queries' signs, and
+        // with a scale of 0 a masked score still counts as one)
+        const float f = fmaxf(fabsf(a.scale), 1e-30f) * ((RAW ? kAtUp69 : kQ4ExactUnscale) * 1.4426950408889634f), slack = 6.f / f;
+        const bool flip = a.scale < 0.f;
+        float start[G][2];                       // -8 times the sum of a group's queries, columns 2 c, 2 c + 1
+        int whole_tiles = 0;
+        int began = 0;                           // the item's tile with which this warp's part of it begins
+        auto begin = [&] {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                int g;
+                const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
+                const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
+#pragma unroll
+                for (int k = 0; k < G; ++k) {
+                    uint32_t w[QP][4] = {};
+                    if (row >= 0) query_words<RAW>(p + 32 * k, flip, w);
+#pragma unroll
+                    for (int q = 0; q < QP; ++q)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) qf[nt][q][k][j] = w[q][j];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[nt][k][0][j] = y[nt][k][1][j] = 0.f;
+                    if constexpr (RAW) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float x0, x1;
+                            two_bf16(w[0][j], x0, x1);
+                            sum += (x0 + x1) * (j & 1 ? 16.f : 1.f);
+                        }
+                        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                        sum *= -8.f * 0x1p-133f;       // to where a code's 1 stands
+                        start[k][0] = __shfl_sync(0xffffffffu, sum, 8 * c);
+                        start[k][1] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
+                    }
+                }
+                m[nt][0] = m[nt][1] = -INFINITY;
+                l[nt][0] = l[nt][1] = 0.f;
+            }
+            began = use.t;
+            whole_tiles = min(use.nk, use.len - use.n + use.ct * COLS / a.group + 1) / kAtTile;
+        };
+        begin();
         int stage = 0;
         uint32_t phase = 0;
         for (int i = 0; i < count; ++i) {
-            if (i == 0 || use.t == 0) {          // an item begins
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    int g;
-                    const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
-                    const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
-#pragma unroll
-                    for (int k = 0; k < G; ++k) {
-                        uint32_t w[QP][4] = {};
-                        if (row >= 0) query_words(p + 32 * k, w);
-#pragma unroll
-                        for (int q = 0; q < QP; ++q)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) qf[nt][q][k][j] = w[q][j];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) y[nt][k][0][j] = y[nt][k][1][j] = 0.f;
-                    }
-                    m[nt][0] = m[nt][1] = -INFINITY;
-                    l[nt][0] = l[nt][1] = 0.f;
-                }
-                began = use.t;
-            }
             if (!mbar_wait_bounded(bars + 8 * stage, phase, kAtWaitNs)) {       // give up, but not with copies in flight
                 if (lane == 0) kv_note(a.kv, SPM_KV_TIMEOUT);
                 for (int j = i; j < issued; ++j) mbar_wait_bounded(bars + 8 * (j % STAGES), j / STAGES & 1, kAtWaitNs);
@@ -309,15 +359,15 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                     const uint4 w = ldsm4(block + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
+                        const Nib4 u = RAW ? q4_unpack(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_unpack(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             float d[4];
-                            mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
-                            mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[nt][0][k + h][2], qf[nt][0][k + h][3]);
+                            if constexpr (RAW) mma_k16_from(d, start[k + h], u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
+                            else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
 #pragma unroll
-                            for (int q = 1; q < QP; ++q) {
-                                mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][q][k + h][0], qf[nt][q][k + h][1]);
+                            for (int q = 0; q < QP; ++q) {
+                                if (q > 0) mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][q][k + h][0], qf[nt][q][k + h][1]);
                                 mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[nt][q][k + h][2], qf[nt][q][k + h][3]);
                             }
                             s[nt][b][0] += s0[k + h] * d[0]; s[nt][b][1] += s0[k + h] * d[1];
@@ -325,14 +375,9 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                         }
                     }
                 }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[nt][b][j] *= f;
             }
             // ---- tokens that are not there, or behind a column's row ----
-            const int row0 = use.ct * COLS / a.group;
-            const bool whole = have == 3 && (use.t + 1) * kAtTile <= min(use.nk, use.len - use.n + row0 + 1);
+            const bool whole = have == 3 && use.t < whole_tiles;
             if (!whole) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -347,7 +392,7 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                                 if (!(have >> b & 1) || 16 * b + 8 * j + r >= sees) s[nt][b][2 * j + e] = -INFINITY;
                     }
             }
-            // ---- running maximum: moved only where a score is above it by enough (2^6) to matter ----
+            // ---- running maximum: moved only where a score is above it by a factor of 2^6 ----
             bool raise = false;
             float top[NT][2];
 #pragma unroll
@@ -359,14 +404,14 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
                     top[nt][e] = v;
-                    raise |= v > m[nt][e] + 6.f || (m[nt][e] == -INFINITY && v > -INFINITY);
+                    raise |= v > m[nt][e] + slack;         // (-infinity is not above -infinity)
                 }
             if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float to = fmaxf(m[nt][e], top[nt][e]), by = to == -INFINITY ? 1.f : ex2(m[nt][e] - to);
+                        const float to = fmaxf(m[nt][e], top[nt][e]), by = to == -INFINITY ? 1.f : ex2((m[nt][e] - to) * f);
                         m[nt][e] = to;
                         l[nt][e] *= by;
 #pragma unroll
@@ -377,12 +422,12 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float base = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
+                    const float base = (m[nt][e] == -INFINITY ? 0.f : m[nt][e] * -f) + S::up;
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const float p = ex2(s[nt][b][2 * j + e] - base);
+                            const float p = ex2(fmaf(s[nt][b][2 * j + e], f, base));
                             s[nt][b][2 * j + e] = p;
                             l[nt][e] += p;
                         }
@@ -406,7 +451,7 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                     const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
+                        const Nib4 u = RAW ? q4_unpack(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_unpack(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             float p0 = s[nt][b][0] * s0[k + h], p1 = s[nt][b][1] * s0[k + h], p2 = s[nt][b][2] * s1[k + h], p3 = s[nt][b][3] * s1[k + h];
@@ -419,6 +464,10 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                                     two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
                                 }
                                 const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
+                                if constexpr (RAW) {
+                                    mma_k16(y[nt][k + h][0], kAtMinus8, kAtMinus128, kAtMinus8, kAtMinus128, b0, b1);
+                                    mma_k16(y[nt][k + h][1], kAtMinus8, kAtMinus128, kAtMinus8, kAtMinus128, b0, b1);
+                                }
                                 mma_k16(y[nt][k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
                                 mma_k16(y[nt][k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
                             }
@@ -441,7 +490,7 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                         v += __shfl_xor_sync(0xffffffffu, v, 4);
                         v += __shfl_xor_sync(0xffffffffu, v, 8);
                         v += __shfl_xor_sync(0xffffffffu, v, 16);
-                        l[nt][e] = v;
+                        l[nt][e] = RAW ? v * 0x1p-64f : v;
                     }
                 if (ends && began == 0) {        // all of it is this warp's
 #pragma unroll
@@ -451,11 +500,11 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                             int g;
                             const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + 2 * c + e, g);
                             if (row < 0) continue;
-                            const float by = l[nt][e] > 0.f ? kQ4ExactUnscale / l[nt][e] : 0.f;
+                            const float by = l[nt][e] > 0.f ? S::unscale / l[nt][e] : 0.f, by16 = by * S::odd;
                             T* p = static_cast<T*>(a.out.p) + row * a.out.row + (use.head * a.group + g) * a.out.head + 4 * r;
 #pragma unroll
                             for (int k = 0; k < G; ++k) {
-                                float o[4] = {y[nt][k][0][e] * by, y[nt][k][0][2 + e] * by, y[nt][k][1][e] * by, y[nt][k][1][2 + e] * by};
+                                float o[4] = {y[nt][k][0][e] * by, y[nt][k][0][2 + e] * by16, y[nt][k][1][e] * by, y[nt][k][1][2 + e] * by16};
                                 store_row<4>(p + 32 * k, o);
                             }
                         }
@@ -469,13 +518,14 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
                             const int col = 8 * nt + 2 * c + e;
 #pragma unroll
                             for (int k = 0; k < G; ++k)
-                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], y[nt][k][0][2 + e], y[nt][k][1][e], y[nt][k][1][2 + e]);
-                            if (r == 0) { part[COLS * HD + col] = m[nt][e]; part[COLS * HD + COLS + col] = l[nt][e]; }
+                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], y[nt][k][0][2 + e] * S::odd, y[nt][k][1][e], y[nt][k][1][2 + e] * S::odd);
+                            if (r == 0) { part[COLS * HD + col] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * f; part[COLS * HD + COLS + col] = l[nt][e]; }
                         }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - use.t, use.seq, use.ct, use.head, began, use.t + 1, use.nt, use.first, use.n};
                 }
             }
-            use.next(a);
+            if (!ends) ++use.t;
+            else if (i + 1 < count) { use.next(a); begin(); }
         }
     }
     __syncthreads();
@@ -518,7 +568,7 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
             if (done) {
                 int g;
                 const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
-                const float by = sum > 0.f ? kQ4ExactUnscale / sum : 0.f;
+                const float by = sum > 0.f ? S::unscale / sum : 0.f;
                 float res[4] = {o.x * by, o.y * by, o.z * by, o.w * by};
                 if (row >= 0) store_row<4>(static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + d, res);
             } else {
@@ -534,7 +584,7 @@ __global__ void __launch_bounds__(AtShape<HD, NT>::warps * 32, 1) kv_attend_kern
 // Adds the parts of items that were cut between CTAs: block (x, column) takes the item that begins in CTA x and goes on behind it.
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(HD) kv_attend_join_kernel(const AttendArgs a) {
-    constexpr int COLS = AtShape<HD, NT>::cols, FLOATS = AtShape<HD, NT>::part_floats;
+    constexpr int COLS = AtShape<T, HD, NT>::cols, FLOATS = AtShape<T, HD, NT>::part_floats;
     __shared__ float by[kAtMaxCtas], red[HD / 32];
     grid_dep_wait();
     const int cta = blockIdx.x, col = blockIdx.y, tid = threadIdx.x;
@@ -565,7 +615,7 @@ __global__ void __launch_bounds__(HD) kv_attend_join_kernel(const AttendArgs a) 
         sum += by[j] * at(j)[COLS * HD + COLS + col];
         o += by[j] * at(j)[col * HD + tid];
     }
-    o = sum > 0.f ? o * (kQ4ExactUnscale / sum) : 0.f;
+    o = sum > 0.f ? o * (AtShape<T, HD, NT>::unscale / sum) : 0.f;
     T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.w * a.group + g) * a.out.head + tid;
     if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(o);
     else *to = o;

@@ -138,7 +138,7 @@ cudaError_t allow_smem(int dev, int bytes) {
 
 template <typename T, int HD, int NT>
 cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st) {
-    using S = AtShape<HD, NT>;
+    using S = AtShape<T, HD, NT>;
     cudaError_t e = allow_smem<kv_attend_kernel<T, HD, NT>>(dev, S::smem(SPM_KV_MAX_SEQS));
     if (e != cudaSuccess) return e;
     const int ctas = std::min(sms, kAtMaxCtas);
@@ -268,6 +268,10 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.batch = batch_of(batch);
     a.q = rows_of(q); a.out = rows_of(out);
     a.group = n_q_heads / kv->n_kv_heads;
+    const int per_page = kv->page_size / kKvBlock;
+    a.page_shift = -1;
+    for (int i = 0; i < 16; ++i)
+        if (per_page == 1 << i) a.page_shift = i;
     a.scale = scale;
     a.joins = static_cast<int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 16);
@@ -276,7 +280,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
         by_eights(eights, [&](auto n) {
             constexpr int most = sizeof(T) == 2 ? (size.value == 256 ? 2 : 4) : (size.value == 256 ? 1 : 2);
             if constexpr (n.value <= most) {
-                a.min_tiles = AtShape<size.value, n.value>::warps;
+                a.min_tiles = AtShape<T, size.value, n.value>::warps;
                 e = launch_attend<T, size.value, n.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
             }
         });

@@ -6,15 +6,12 @@ starts, page numbers and positions are read on the device. Outputs and workspace
 """
 from __future__ import annotations
 
-import contextlib
-
 import torch
 
 from . import binding as B
 
 DTYPES = {torch.float32: B.DTYPE_FP32, torch.bfloat16: B.DTYPE_BF16}
 BLOCK = 16                      # tokens of a block
-_HERE = contextlib.nullcontext()
 
 
 def _need(ok, message):
@@ -22,8 +19,17 @@ def _need(ok, message):
         raise ValueError(message)
 
 
-def _on(device):
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _enqueue(device, call, *args):
+    """call(*args, stream) on the current stream of the device, with the device current."""
+    at = device.index
+    stream = torch._C._cuda_getCurrentRawStream(at)       # (torch.cuda.current_stream builds an object, 2 us)
+    if torch._C._cuda_getDevice() == at:
+        rc = call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, stream)
+    if rc:
+        B._check(rc)
 
 
 def _vector(x, dtype, device, what, n=None):
@@ -32,10 +38,10 @@ def _vector(x, dtype, device, what, n=None):
     return x.data_ptr()
 
 
-def _rows(x, heads, hd, dtype, device, what):
-    """spm_rows of a tensor [rows, heads, hd] whose heads are contiguous."""
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != hd:
-        raise ValueError(f"{what}: shape [rows, {heads}, {hd}], not {list(x.shape)}")
+def _rows(x, n, heads, hd, dtype, device, what):
+    """spm_rows of a tensor [n, heads, hd] whose heads are contiguous."""
+    if x.shape != (n, heads, hd):
+        raise ValueError(f"{what}: shape [{n}, {heads}, {hd}], not {list(x.shape)}")
     if x.dtype is not dtype or x.device != device:
         raise ValueError(f"{what}: {dtype} on {device}, not {x.dtype} on {x.device}")
     row, head, one = x.stride()
@@ -45,9 +51,12 @@ def _rows(x, heads, hd, dtype, device, what):
 
 
 def _dtype(x, what):
-    _need(x.is_cuda, f"{what}: a CUDA tensor (there is no CPU implementation of this path)")
-    _need(x.dtype in DTYPES, f"{what}: fp32 or bf16, not {x.dtype}")
-    return DTYPES[x.dtype]
+    if not x.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor (there is no CPU implementation of this path)")
+    dt = DTYPES.get(x.dtype)
+    if dt is None or x.dim() != 3:
+        raise ValueError(f"{what}: fp32 or bf16 [rows, heads, head_dim], not {x.dtype} {list(x.shape)}")
+    return dt
 
 
 class Rope:
@@ -66,16 +75,21 @@ class Rope:
                   None if k_gamma is None else _vector(k_gamma, torch.float32, self.device, "k_gamma"))
         self._by_axes = {n: B.Rope(*fields, n, 2 * half, int(neighbours), eps) for n in range(1, 5)}
 
-    def _with(self, positions, n_rows, hd, which):
-        """(struct, positions' address, axis stride) of a call with positions [n_axes, rows] or [rows]."""
-        _need(positions is not None, "positions are needed to turn heads")
-        _need(positions.dtype is torch.int32 and positions.device == self.device, f"positions: int32 on {self.device}")
-        for i in which:
-            _need(self.gamma_sizes[i] in (None, hd), f"gammas: {hd} elements")
-        p = positions if positions.dim() == 2 else positions[None]
-        _need(p.dim() == 2 and p.shape[1] == n_rows and 1 <= p.shape[0] <= 4, f"positions: [1..4 axes, {n_rows}], not {list(positions.shape)}")
-        _need(p.stride(1) == 1 or n_rows <= 1, "positions: the rows of an axis must be contiguous")
-        return self._by_axes[p.shape[0]], p.data_ptr(), p.stride(0) if p.shape[0] > 1 else n_rows
+    def _with(self, positions, n_rows, hd, q, k):
+        """(struct, positions' address, axis stride) of a call with positions [n_axes, rows] or [rows]; q, k: whose gammas it uses."""
+        if positions is None:
+            raise ValueError("positions are needed to turn heads")
+        if positions.dtype is not torch.int32 or positions.device != self.device:
+            raise ValueError(f"positions: int32 on {self.device}")
+        if q and self.gamma_sizes[0] not in (None, hd) or k and self.gamma_sizes[1] not in (None, hd):
+            raise ValueError(f"gammas: {hd} elements")
+        shape, stride = positions.shape, positions.stride()
+        axes = shape[0] if len(shape) == 2 else 1
+        if not 1 <= len(shape) <= 2 or shape[-1] != n_rows or not 1 <= axes <= 4:
+            raise ValueError(f"positions: [1..4 axes, {n_rows}], not {list(shape)}")
+        if stride[-1] != 1 and n_rows > 1:
+            raise ValueError("positions: the rows of an axis must be contiguous")
+        return self._by_axes[axes], positions.data_ptr(), stride[0] if axes > 1 else n_rows
 
 
 class KVBatch:
@@ -94,6 +108,7 @@ class KVBatch:
         self.c = B.KvBatch(page_table.data_ptr(), _vector(lengths, torch.int32, self.device, "lengths", n),
                            None if row_start is None else _vector(row_start, torch.int32, self.device, "row_start", n + 1),
                            n, page_table.shape[1], self.n_rows, max_rows)
+        self.shape = (n, page_table.shape[1], self.n_rows, max_rows, row_start is None)
 
 
 class KVCache:
@@ -107,6 +122,7 @@ class KVCache:
         self.kv_heads, self.page_size, self.head_dim = pages.shape[1], pages.shape[2] * BLOCK, pages.shape[3] // 18
         self.c = B.KvCache(pages.data_ptr(), None if status is None else _vector(status, torch.int32, self.device, "status", 1),
                            pages.shape[0], self.page_size, self.kv_heads, self.head_dim)
+        self._lib = B.load()
         self._workspace = {}        # bytes that a call of a batch's shape asks for
         B.spm_kv_cache_bytes(self.c)
 
@@ -115,74 +131,73 @@ class KVCache:
         _need(page_size % BLOCK == 0 and page_size > 0, "page_size: a multiple of 16")
         return cls(torch.zeros(n_pages, kv_heads, page_size // BLOCK, 18 * head_dim, dtype=torch.uint8, device=device), status)
 
-    def _stream(self, batch):
-        _need(batch.device == self.device, "the batch is on another device than the cache")
-        return torch.cuda.current_stream(self.device).cuda_stream
+    def _size(self, batch):
+        if batch.device != self.device:
+            raise ValueError("the batch is on another device than the cache")
+        return batch.n_rows, self.kv_heads, self.head_dim
 
     def write(self, batch, k, v, q=None, positions=None, rope=None, q_out=None):
         """k, v [rows, kv_heads, head_dim] of the batch's new rows go into the cache, k normed and turned by `rope`; returns q [rows, q_heads,
         head_dim] normed and turned (None without q)."""
-        dt, hd, n = _dtype(k, "k"), self.head_dim, batch.n_rows
-        ck, cv = _rows(k, self.kv_heads, hd, k.dtype, self.device, "k"), _rows(v, self.kv_heads, hd, k.dtype, self.device, "v")
-        _need(k.shape[0] == n and v.shape[0] == n, f"k, v: {n} rows")
+        n, heads, hd = self._size(batch)
+        dt, dtype, device = _dtype(k, "k"), k.dtype, self.device
+        ck, cv = _rows(k, n, heads, hd, dtype, device, "k"), _rows(v, n, heads, hd, dtype, device, "v")
         cq = co = cr = pos = None
-        stride = heads = 0
+        stride = q_heads = 0
         if rope is not None:
-            cr, pos, stride = rope._with(positions, n, hd, (0, 1) if q is not None else (1,))
+            cr, pos, stride = rope._with(positions, n, hd, q is not None, True)
         if q is not None:
-            _need(rope is not None, "q without rope: there is nothing to do to it")
-            heads = q.shape[1] if q.dim() == 3 else 0
+            if rope is None or q.dim() != 3:
+                raise ValueError("q without rope: there is nothing to do to it" if rope is None else "q: [rows, heads, head_dim]")
+            q_heads = q.shape[1]
+            cq = _rows(q, n, q_heads, hd, dtype, device, "q")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            cq, co = _rows(q, heads, hd, k.dtype, self.device, "q"), _rows(q_out, heads, hd, k.dtype, self.device, "q_out")
-            _need(q.shape[0] == n and q_out.shape[0] == n, f"q: {n} rows")
-        with _on(self.device):
-            B.spm_kv_write(self.c, batch.c, cr, pos, stride, cq, co, heads, ck, cv, dt, self._stream(batch))
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            co = _rows(q_out, n, q_heads, hd, dtype, device, "q_out")
+        _enqueue(device, self._lib.spm_kv_write, self.c, batch.c, cr, pos, stride, cq, co, q_heads, ck, cv, dt)
         return q_out
 
     def read(self, batch, dtype=torch.bfloat16, k_out=None, v_out=None):
         """The cache's keys and values at the positions of the batch's new rows: two tensors [rows, kv_heads, head_dim]."""
-        shape = (batch.n_rows, self.kv_heads, self.head_dim)
-        k_out, v_out = (torch.empty(shape, dtype=dtype, device=self.device) if x is None else x for x in (k_out, v_out))
-        dt = _dtype(k_out, "k_out")
-        ck, cv = (_rows(x, self.kv_heads, self.head_dim, k_out.dtype, self.device, "k_out, v_out") for x in (k_out, v_out))
-        _need(k_out.shape[0] == batch.n_rows and v_out.shape[0] == batch.n_rows, f"k_out, v_out: {batch.n_rows} rows")
-        with _on(self.device):
-            B.spm_kv_read(self.c, batch.c, ck, cv, dt, self._stream(batch))
+        n, heads, hd = size = self._size(batch)
+        if k_out is None:
+            k_out = self.pages.new_empty(size, dtype=dtype)
+        if v_out is None:
+            v_out = torch.empty_like(k_out, memory_format=torch.contiguous_format)
+        dt, dtype = _dtype(k_out, "k_out"), k_out.dtype
+        ck, cv = _rows(k_out, n, heads, hd, dtype, self.device, "k_out"), _rows(v_out, n, heads, hd, dtype, self.device, "v_out")
+        _enqueue(self.device, self._lib.spm_kv_read, self.c, batch.c, ck, cv, dt)
         return k_out, v_out
 
     def attend(self, batch, q, scale=None, out=None):
         """softmax(scale q K^T) V of q [rows, q_heads, head_dim], each row over its sequence's tokens up to its own position. scale None:
         head_dim ** -0.5."""
-        dt, hd = _dtype(q, "q"), self.head_dim
-        heads = q.shape[1] if q.dim() == 3 else 0
+        n, _, hd = self._size(batch)
+        dt, dtype, device = _dtype(q, "q"), q.dtype, self.device
+        heads = q.shape[1]
+        cq = _rows(q, n, heads, hd, dtype, device, "q")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        cq, co = _rows(q, heads, hd, q.dtype, self.device, "q"), _rows(out, heads, hd, q.dtype, self.device, "out")
-        _need(q.shape[0] == batch.n_rows and out.shape[0] == batch.n_rows, f"q, out: {batch.n_rows} rows")
-        b = batch.c
-        key = (b.n_seq, b.table_stride, b.n_rows, b.max_rows, heads, dt)
-        with _on(self.device):
-            stream = self._stream(batch)
-            size = self._workspace.get(key)
-            if size is None:
-                size = self._workspace[key] = B.spm_kv_attend_workspace(self.c, b, heads, dt)
-            work = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
-            B.spm_kv_attend(self.c, b, cq, heads, co, hd ** -0.5 if scale is None else scale, dt,
-                            work.data_ptr() if size else None, size, stream)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        co = _rows(out, n, heads, hd, dtype, device, "out")
+        key = (batch.shape, heads, dt)
+        size = self._workspace.get(key)
+        if size is None:
+            size = self._workspace[key] = B.spm_kv_attend_workspace(self.c, batch.c, heads, dt)
+        work = self.pages.new_empty(size)
+        _enqueue(device, self._lib.spm_kv_attend, self.c, batch.c, cq, heads, co, hd ** -0.5 if scale is None else scale, dt,
+                 work.data_ptr(), size)
         return out
 
 
 def rotate_heads(x, positions, rope, out=None):
     """Norm (rope's q_gamma) and rotation of x [rows, heads, head_dim] by positions [axes, rows]."""
     dt = _dtype(x, "x")
-    _need(x.dim() == 3 and x.device == rope.device, "x: [rows, heads, head_dim] on the device of the rope")
     n, heads, hd = x.shape
-    c, pos, stride = rope._with(positions, n, hd, (0,))
+    device = rope.device
+    c, pos, stride = rope._with(positions, n, hd, True, False)
+    cx = _rows(x, n, heads, hd, x.dtype, device, "x")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    cx, cy = _rows(x, heads, hd, x.dtype, x.device, "x"), _rows(out, heads, hd, x.dtype, x.device, "out")
-    _need(out.shape[0] == n, f"out: {n} rows")
-    with _on(x.device):
-        B.spm_rotate_heads(c, pos, stride, cx, cy, n, heads, hd, dt, torch.cuda.current_stream(x.device).cuda_stream)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    cy = _rows(out, n, heads, hd, x.dtype, device, "out")
+    _enqueue(device, B.load().spm_rotate_heads, c, pos, stride, cx, cy, n, heads, hd, dt)
     return out
