@@ -32,9 +32,13 @@ struct AttendArgs {
     int min_tiles;              // of a CTA, before another one starts
     float scale;
     float* parts;               // [2 * CTAs][part floats]
-    int* joins;                 // [CTAs][4]: CTAs that share the item that begins in this one and goes on behind it (0: none), sequence, columns, head
+    int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns, head, first row, rows
+    int once;                   // every block is read by one warp alone
 };
 
+#ifndef AT_W
+#define AT_W 16
+#endif
 constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
 constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
@@ -46,16 +50,17 @@ struct AtShape {
     static constexpr int part_floats = cols * (HD + 2);      // sums, then maxima, then sums of probabilities
     static constexpr int part_bytes = (part_floats * 4 + 15) / 16 * 16;
     // warps and stages of a warp's ring: what registers (the sums of HD x cols numbers, the queries) and shared memory leave
-    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
+    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : HD == 256 ? 8 : sizeof(T) == 4 ? 12 : AT_W;
     static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : NT == 4 ? 4 : 3;
     static constexpr bool raw = sizeof(T) == 2 && NT == 1;              // codes as they are masked out
     static constexpr float up = raw ? 64.f : 0.f;                       // probabilities are taken to 2^64 then
     static constexpr float unscale = raw ? 0x1p69f : kQ4ExactUnscale;   // of sums of codes times probabilities
-    static constexpr float odd = raw ? 1.f / 16.f : 1.f;                // of elements 4 r + 1, 4 r + 3, whose codes stand four bits higher
+    // a sum of an odd element, beside that of the even one before it
+    __device__ static float odd(float both, float low) { return raw ? (both - low) * (1.f / 16.f) : both; }
     static constexpr int ring_bytes = stages * tile_bytes;
     static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
-    static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8 + 64) + (n_seq + 1) * 4; }
-    static_assert(warps * (ring_bytes + part_bytes + stages * 8 + 64) + (SPM_KV_MAX_SEQS + 1) * 4 <= 232448, "227 KB");
+    static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8) + (n_seq > 64 ? n_seq * 4 : 0); }
+    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 4 + 6 * 1024 <= 232448, "227 KB");
 };
 
 // A walk along the line of tiles. nk: tokens that the last of the item's columns sees, nt: tiles (one at least, so that rows that see
@@ -74,7 +79,7 @@ struct Walk {
     }
     __device__ __forceinline__ int blocks(const AttendArgs& a) const { return n > 0 ? (n * a.group + COLS - 1) / COLS : 0; }
     __device__ __forceinline__ void columns(const AttendArgs& a) {
-        const int last = min(n - 1, ((ct + 1) * COLS - 1) / a.group);
+        const int last = n == 1 ? 0 : min(n - 1, ((ct + 1) * COLS - 1) / a.group);
         nk = max(0, min(len - n + last + 1, a.batch.stride * a.kv.page_size));
         nt = max(1, (nk + kAtTile - 1) / kAtTile);
     }
@@ -84,15 +89,10 @@ struct Walk {
         for (ct = 0; ct < m; ++ct) { columns(a); sum += nt; }
         return sum * a.kv.heads;
     }
-    __device__ __forceinline__ void seek(const AttendArgs& a, const int* before, int x) {
-        int lo = 0, hi = a.batch.n_seq;          // before[lo] <= x < before[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (before[mid] <= x) lo = mid; else hi = mid;
-        }
-        seq = lo;
+    // to tile `rest` of sequence `s`
+    __device__ __forceinline__ void seek(const AttendArgs& a, int s, int rest) {
+        seq = s;
         load(a);
-        int rest = x - before[lo];
         for (ct = 0;; ++ct) {
             columns(a);
             if (rest < nt * a.kv.heads) break;
@@ -120,7 +120,7 @@ struct Walk {
 // Where a column's result goes: its row, -1 where the item has no such column
 template <int COLS>
 __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int n, int ct, int col, int& g) {
-    const int x = ct * COLS + col, i = x / a.group;
+    const int x = ct * COLS + col, i = n == 1 ? (x >= a.group) : x / a.group;
     g = x - i * a.group;
     return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
 }
@@ -137,10 +137,10 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// D = A B + {c0, c1, c0, c1}
-__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float (&c)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]));
+// D = A B + C
+__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 // HD / 32 scales of a token
 template <int G>
@@ -161,25 +161,29 @@ __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
 // would leave the range of numbers).
 constexpr uint32_t kAtUp64 = 0x5f805f80u, kAtUp60 = 0x5d805d80u;
 constexpr float kAtUp69 = 0x1p69f;
-constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus128 = 0x80808080u;      // -8 and -8 * 16 as codes
+// A word's bytes as operands: the low nibble of bytes 0, 2 and both nibbles of them (low + 16 high, also linear), the same of bytes 1, 3:
+// four instructions. Values' elements are rows of the product, so the high nibble's sum is had from the two.
+constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus136 = 0x80888088u;      // -8 and -8 - 16 * 8 as codes
+__device__ __forceinline__ Nib4 q4_bytes(uint32_t w) {
+    const uint32_t even = w & 0x00ff00ffu, odd = __byte_perm(w, 0u, 0x4341);
+    return Nib4{{even & 0x000f000fu, even, odd & 0x000f000fu, odd}};
+}
 template <bool RAW>
-__device__ __forceinline__ void query_words(const __nv_bfloat16* p, bool flip, uint32_t (&w)[1][4]) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t sign = flip ? 0x80008000u : 0u;
-    w[0][0] = __byte_perm(v.x, v.z, 0x5410) ^ sign; w[0][1] = __byte_perm(v.x, v.z, 0x7632) ^ sign;
-    w[0][2] = __byte_perm(v.y, v.w, 0x5410) ^ sign; w[0][3] = __byte_perm(v.y, v.w, 0x7632) ^ sign;
+__device__ __forceinline__ void query_words(uint32_t (&w)[1][4], bool flip) {          // in: eight bf16 numbers as they were loaded
+    const uint32_t x = w[0][0], y = w[0][1], z = w[0][2], u = w[0][3], sign = flip ? 0x80008000u : 0u;
+    w[0][0] = __byte_perm(x, z, 0x5410) ^ sign; w[0][1] = __byte_perm(x, z, 0x7632) ^ sign;
+    w[0][2] = __byte_perm(y, u, 0x5410) ^ sign; w[0][3] = __byte_perm(y, u, 0x7632) ^ sign;
     if constexpr (RAW) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? kAtUp60 : kAtUp64)));
     }
 }
 template <bool RAW>
-__device__ __forceinline__ void query_words(const float* p, bool flip, uint32_t (&w)[3][4]) {
-    float x[8];
-    load_row<8>(p, x);
+__device__ __forceinline__ void query_words(uint32_t (&w)[3][4], bool flip) {          // in: eight fp32 numbers in the first two parts
+    const uint32_t sign = flip ? 0x80000000u : 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const Split3 s = split3(flip ? -x[i] : x[i], flip ? -x[i + 4] : x[i + 4]);
+        const Split3 s = split3(__uint_as_float(w[0][i] ^ sign), __uint_as_float(w[1][i] ^ sign));
         w[0][i] = s.part[0]; w[1][i] = s.part[1]; w[2][i] = s.part[2];
     }
 }
@@ -196,48 +200,65 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     float* own_part = reinterpret_cast<float*>(smem + W * S::ring_bytes + warp * S::part_bytes);
     unsigned char* rest = smem + W * (S::ring_bytes + S::part_bytes);
     const uint32_t bars = smem_u32(rest) + warp * STAGES * 8;
-    int* before = reinterpret_cast<int*>(rest + W * (STAGES * 8 + 64));
+    int* before = reinterpret_cast<int*>(rest + W * STAGES * 8);
     __shared__ PartMeta meta[2 * W];
     __shared__ int warp_sum_of[W];
+    __shared__ float weight[2 * W][COLS], total[2 * W][COLS], highest[2 * W][COLS];
 
     if (lane == 0) {
         for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1);
         fence_barrier_init();
         meta[2 * warp].id = meta[2 * warp + 1].id = -1;
     }
-    // ---- the line of tiles: tiles before each sequence ----
+    __syncwarp();
+    // ---- the line of tiles: how many there are, and before each sequence. Up to 64 sequences are two a lane, in every warp for itself ----
     const int n_seq = a.batch.n_seq;
-    const int each = (n_seq + W * 32 - 1) / (W * 32);
-    int mine = 0;
     Walk<COLS> use;
-    for (int i = 0; i < each; ++i) {
-        const int s = tid * each + i;
-        if (s >= n_seq) break;
+    int all = 0, before0 = 0, before1 = 0;
+    auto count_tiles = [&](int s) {
         use.seq = s;
         use.load(a);
-        const int k = use.tiles_of_sequence(a);
         if (use.n > 0 && use.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-        before[s] = mine;
-        mine += k;
-    }
-    int upto = mine;
+        return use.tiles_of_sequence(a);
+    };
+    if (n_seq <= 64) {
+        const int k0 = 2 * lane < n_seq ? count_tiles(2 * lane) : 0, k1 = 2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0;
+        int upto = k0 + k1;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 31) warp_sum_of[warp] = upto;
-    __syncthreads();
-    int all = 0, off = upto - mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        all = __shfl_sync(0xffffffffu, upto, 31);
+        before0 = upto - k0 - k1;
+        before1 = upto - k1;
+    } else {
+        const int each = (n_seq + W * 32 - 1) / (W * 32);
+        int mine = 0;
+        for (int i = 0; i < each; ++i) {
+            const int s = tid * each + i;
+            if (s >= n_seq) break;
+            before[s] = mine;
+            mine += count_tiles(s);
+        }
+        int upto = mine;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (w < warp) off += warp_sum_of[w];
-        all += warp_sum_of[w];
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) warp_sum_of[warp] = upto;
+        __syncthreads();
+        int off = upto - mine;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) off += warp_sum_of[w];
+            all += warp_sum_of[w];
+        }
+        for (int i = 0; i < each; ++i)
+            if (tid * each + i < n_seq) before[tid * each + i] += off;
+        __syncthreads();
     }
-    for (int i = 0; i < each; ++i)
-        if (tid * each + i < n_seq) before[tid * each + i] += off;
-    if (tid == 0) before[n_seq] = all;
-    __syncthreads();
     grid_dep_launch();
 
     const int ctas = max(1, min(int(gridDim.x), (all + a.min_tiles - 1) / a.min_tiles)), cta = blockIdx.x;
@@ -253,8 +274,37 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
         // ---- copies: lanes 0 and 1 walk ahead and look up a block's page each, a tile before its use. A page of an even number of
         // blocks holds both ----
         Walk<COLS> ahead;
-        ahead.seek(a, before, lo);
+        if (n_seq <= 64) {
+            const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
+            const int b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
+            ahead.seek(a, s, lo - (s & 1 ? b1 : b0));
+        } else {
+            int s = 0, end = n_seq;              // the last sequence with before[s] <= lo
+            while (end - s > 1) {
+                const int mid = (s + end) / 2;
+                if (before[mid] <= lo) s = mid; else end = mid;
+            }
+            ahead.seek(a, s, lo - before[s]);
+        }
         use = ahead;
+        // an item's queries, as they are in memory
+        auto fetch = [&] {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                int g;
+                const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
+                const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
+#pragma unroll
+                for (int k = 0; k < G; ++k)
+#pragma unroll
+                    for (int q = 0; q < (QP + 1) / 2; ++q) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (row >= 0) v = *reinterpret_cast<const uint4*>(p + 32 * k + 4 * q);
+                        qf[nt][q][k][0] = v.x; qf[nt][q][k][1] = v.y; qf[nt][q][k][2] = v.z; qf[nt][q][k][3] = v.w;
+                    }
+            }
+        };
+        fetch();
         const int per_page = a.kv.page_size / kKvBlock;
         const bool even = per_page % 2 == 0;
         const long long page_bytes = static_cast<long long>(a.kv.heads) * per_page * BB;
@@ -277,7 +327,10 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                 const uint32_t bar = bars + 8 * stage, dst = ring_at + stage * S::tile_bytes, bytes = __popc(have) * BB;
                 if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
                 __syncwarp(3u);
-                if (ok && (lane == 0 || !even)) bulk_g2s_plain(dst + lane * BB, from, even ? bytes : BB, bar);
+                if (ok && (lane == 0 || !even)) {        // (what nobody reads again leaves tables, queries and code in L2)
+                    if (a.once) bulk_g2s(dst + lane * BB, from, even ? bytes : BB, bar, policy_evict_first());
+                    else bulk_g2s_plain(dst + lane * BB, from, even ? bytes : BB, bar);
+                }
                 if (issued + 1 < count) { ahead.next(a); look_up(); }
             }
             ++issued;
@@ -292,19 +345,20 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
         // with a scale of 0 a masked score still counts as one)
         const float f = fmaxf(fabsf(a.scale), 1e-30f) * ((RAW ? kAtUp69 : kQ4ExactUnscale) * 1.4426950408889634f), slack = 6.f / f;
         const bool flip = a.scale < 0.f;
-        float start[G][2];                       // -8 times the sum of a group's queries, columns 2 c, 2 c + 1
+        float start[G][4];                       // -8 times the sum of a group's queries, as the product's C
         int whole_tiles = 0;
         int began = 0;                           // the item's tile with which this warp's part of it begins
         auto begin = [&] {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                int g;
-                const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
-                const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
 #pragma unroll
                 for (int k = 0; k < G; ++k) {
-                    uint32_t w[QP][4] = {};
-                    if (row >= 0) query_words<RAW>(p + 32 * k, flip, w);
+                    uint32_t w[QP][4];
+#pragma unroll
+                    for (int q = 0; q < QP; ++q)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[q][j] = qf[nt][q][k][j];
+                    query_words<RAW>(w, flip);
 #pragma unroll
                     for (int q = 0; q < QP; ++q)
 #pragma unroll
@@ -322,8 +376,8 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                         sum *= -8.f * 0x1p-133f;       // to where a code's 1 stands
-                        start[k][0] = __shfl_sync(0xffffffffu, sum, 8 * c);
-                        start[k][1] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
+                        start[k][0] = start[k][2] = __shfl_sync(0xffffffffu, sum, 8 * c);
+                        start[k][1] = start[k][3] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
                     }
                 }
                 m[nt][0] = m[nt][1] = -INFINITY;
@@ -451,7 +505,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                     const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const Nib4 u = RAW ? q4_unpack(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_unpack(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
+                        const Nib4 u = RAW ? q4_bytes(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_bytes(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             float p0 = s[nt][b][0] * s0[k + h], p1 = s[nt][b][1] * s0[k + h], p2 = s[nt][b][2] * s1[k + h], p3 = s[nt][b][3] * s1[k + h];
@@ -465,8 +519,8 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                                 }
                                 const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
                                 if constexpr (RAW) {
-                                    mma_k16(y[nt][k + h][0], kAtMinus8, kAtMinus128, kAtMinus8, kAtMinus128, b0, b1);
-                                    mma_k16(y[nt][k + h][1], kAtMinus8, kAtMinus128, kAtMinus8, kAtMinus128, b0, b1);
+                                    mma_k16(y[nt][k + h][0], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
+                                    mma_k16(y[nt][k + h][1], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
                                 }
                                 mma_k16(y[nt][k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
                                 mma_k16(y[nt][k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
@@ -500,11 +554,12 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                             int g;
                             const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + 2 * c + e, g);
                             if (row < 0) continue;
-                            const float by = l[nt][e] > 0.f ? S::unscale / l[nt][e] : 0.f, by16 = by * S::odd;
+                            const float by = l[nt][e] > 0.f ? S::unscale / l[nt][e] : 0.f;
                             T* p = static_cast<T*>(a.out.p) + row * a.out.row + (use.head * a.group + g) * a.out.head + 4 * r;
 #pragma unroll
                             for (int k = 0; k < G; ++k) {
-                                float o[4] = {y[nt][k][0][e] * by, y[nt][k][0][2 + e] * by16, y[nt][k][1][e] * by, y[nt][k][1][2 + e] * by16};
+                                float o[4] = {y[nt][k][0][e] * by, S::odd(y[nt][k][0][2 + e], y[nt][k][0][e]) * by,
+                                              y[nt][k][1][e] * by, S::odd(y[nt][k][1][2 + e], y[nt][k][1][e]) * by};
                                 store_row<4>(p + 32 * k, o);
                             }
                         }
@@ -518,105 +573,147 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                             const int col = 8 * nt + 2 * c + e;
 #pragma unroll
                             for (int k = 0; k < G; ++k)
-                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], y[nt][k][0][2 + e] * S::odd, y[nt][k][1][e], y[nt][k][1][2 + e] * S::odd);
+                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], S::odd(y[nt][k][0][2 + e], y[nt][k][0][e]),
+                                                                                                           y[nt][k][1][e], S::odd(y[nt][k][1][2 + e], y[nt][k][1][e]));
                             if (r == 0) { part[COLS * HD + col] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * f; part[COLS * HD + COLS + col] = l[nt][e]; }
                         }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - use.t, use.seq, use.ct, use.head, began, use.t + 1, use.nt, use.first, use.n};
                 }
             }
             if (!ends) ++use.t;
-            else if (i + 1 < count) { use.next(a); begin(); }
+            else if (i + 1 < count) { use.next(a); fetch(); begin(); }
         }
     }
     __syncthreads();
 
-    // ---- parts of one item in this CTA meet: they stand one after another ----
-    int joined = 0;                              // of the item that goes on behind this CTA
-    PartMeta open{};
-    for (int i = 0; i < 2 * W;) {
-        const PartMeta first = meta[i];
-        if (first.id < 0) { ++i; continue; }
-        int end = i, to = first.to;
-        for (int j = i; j < 2 * W && (meta[j].id < 0 || meta[j].id == first.id); ++j)
-            if (meta[j].id >= 0) { end = j; to = meta[j].to; }
-        const bool done = first.from == 0 && to == first.nt;
-        const int slot = first.from > 0 ? 0 : 1;
-        if (!done && slot == 1) {                // CTA of the item's last tile
-            const long long last = first.id + first.nt - 1;
-            joined = int(((last + 1) * ctas - 1) / all) - cta + 1;
-            open = first;
-        }
-        float* out_part = a.parts + (size_t(cta) * 2 + slot) * S::part_floats;
-        for (int x = tid; x < COLS * (HD / 4); x += W * 32) {
-            const int col = x / (HD / 4), d = x % (HD / 4) * 4;
-            float top = -INFINITY;
-            for (int j = i; j <= end; ++j) {
-                if (meta[j].id < 0) continue;
-                const float* p = reinterpret_cast<const float*>(j & 1 ? smem + (j / 2) * S::ring_bytes : smem + W * S::ring_bytes + (j / 2) * S::part_bytes);
-                top = fmaxf(top, p[COLS * HD + col]);
-            }
-            float sum = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int j = i; j <= end; ++j) {
-                if (meta[j].id < 0) continue;
-                const float* p = reinterpret_cast<const float*>(j & 1 ? smem + (j / 2) * S::ring_bytes : smem + W * S::ring_bytes + (j / 2) * S::part_bytes);
-                const float by = top == -INFINITY ? 0.f : ex2(p[COLS * HD + col] - top);
-                const float4 v = *reinterpret_cast<const float4*>(p + col * HD + d);
-                sum += by * p[COLS * HD + COLS + col];
-                o.x += by * v.x; o.y += by * v.y; o.z += by * v.z; o.w += by * v.w;
-            }
-            if (done) {
-                int g;
-                const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
-                const float by = sum > 0.f ? S::unscale / sum : 0.f;
-                float res[4] = {o.x * by, o.y * by, o.z * by, o.w * by};
-                if (row >= 0) store_row<4>(static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + d, res);
-            } else {
-                *reinterpret_cast<float4*>(out_part + col * HD + d) = o;
-                if (d == 0) { out_part[COLS * HD + col] = top; out_part[COLS * HD + COLS + col] = sum; }
+    // ---- parts of one item in this CTA meet: they stand one after another. Every warp sees which parts belong together (lane j: part j);
+    // first a warp takes a column of an item for the parts' weights, then threads take sums ----
+    const int id = lane < 2 * W ? meta[lane].id : -1;
+    const uint32_t used = __ballot_sync(0xffffffffu, id >= 0), mates = __match_any_sync(0xffffffffu, id) & used;
+    const uint32_t leaders = __ballot_sync(0xffffffffu, id >= 0 && (mates & ((1u << lane) - 1)) == 0);
+    auto part_of = [&](int j) { return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes); };
+    {
+        int n = 0;
+        for (uint32_t left = leaders; left; left &= left - 1, ++n) {
+            const uint32_t group = __shfl_sync(0xffffffffu, mates, __ffs(left) - 1);
+            for (int col = (warp + W - n * COLS % W) % W; col < COLS; col += W) {
+                const bool in = group >> lane & 1;
+                const float v = in ? part_of(lane)[COLS * HD + col] : -INFINITY;
+                float top = v;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float by = top == -INFINITY ? 0.f : ex2(v - top);
+                const float sum = warp_sum(in ? by * part_of(lane)[COLS * HD + COLS + col] : 0.f);
+                if (in) weight[lane][col] = by;
+                if (lane == 0) { total[n][col] = sum; highest[n][col] = top; }
             }
         }
-        i = end + 1;
     }
-    if (tid == 0) *reinterpret_cast<int4*>(a.joins + 4 * cta) = make_int4(joined, open.seq, open.ct, open.head);
+    __syncthreads();
+    int4 join0 = make_int4(0, 0, 0, 0);
+    int join1 = 0;
+    {
+        int n = 0;
+        for (uint32_t left = leaders; left; left &= left - 1, ++n) {
+            const uint32_t group = __shfl_sync(0xffffffffu, mates, __ffs(left) - 1);
+            const PartMeta first = meta[__ffs(group) - 1];
+            const int to = meta[31 - __clz(group)].to;
+            const bool done = first.from == 0 && to == first.nt;
+            const int slot = first.from > 0 ? 0 : 1;
+            if (!done && slot == 1) {            // up to the CTA of the item's last tile
+                const long long last = first.id + first.nt - 1;
+                join0 = make_int4(int(((last + 1) * ctas - 1) / all) - cta + 1, first.ct, first.head, first.first);
+                join1 = first.n;
+            }
+            float* out_part = a.parts + (size_t(cta) * 2 + slot) * S::part_floats;
+            for (int x = tid; x < COLS * (HD / 2); x += W * 32) {
+                const int col = x / (HD / 2), d = x % (HD / 2) * 2;
+                float2 o = make_float2(0.f, 0.f);
+#pragma unroll 4
+                for (int j = __ffs(group) - 1; j <= 31 - __clz(group); ++j) {
+                    if (!(group >> j & 1)) continue;
+                    const float by = weight[j][col];
+                    const float2 v = *reinterpret_cast<const float2*>(part_of(j) + col * HD + d);
+                    o.x += by * v.x; o.y += by * v.y;
+                }
+                if (done) {
+                    int g;
+                    const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
+                    const float by = total[n][col] > 0.f ? S::unscale / total[n][col] : 0.f;
+                    float res[2] = {o.x * by, o.y * by};
+                    if (row >= 0) store_row<2>(static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + d, res);
+                } else {
+                    *reinterpret_cast<float2*>(out_part + col * HD + d) = o;
+                    if (d == 0) { out_part[COLS * HD + col] = highest[n][col]; out_part[COLS * HD + COLS + col] = total[n][col]; }
+                }
+            }
+        }
+    }
+    if (tid == 0) {
+        *reinterpret_cast<int4*>(a.joins + 8 * cta) = join0;
+        a.joins[8 * cta + 4] = join1;
+    }
 }
 
-// Adds the parts of items that were cut between CTAs: block (x, column) takes the item that begins in CTA x and goes on behind it.
+// Adds the parts of items that were cut between CTAs: block (x, column) takes the item that begins in CTA x and goes on behind it. Its
+// 256 threads take the parts in turn by HD-wide groups, eight parts at a time with their loads ahead of their use.
+constexpr int kAtJoinThreads = 256;
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(HD) kv_attend_join_kernel(const AttendArgs a) {
-    constexpr int COLS = AtShape<T, HD, NT>::cols, FLOATS = AtShape<T, HD, NT>::part_floats;
-    __shared__ float by[kAtMaxCtas], red[HD / 32];
+__global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const AttendArgs a) {
+    using S = AtShape<T, HD, NT>;
+    constexpr int COLS = S::cols, FLOATS = S::part_floats, SETS = kAtJoinThreads / HD;
+    __shared__ float tops[SETS], sums[SETS], rows[SETS][HD];
     grid_dep_wait();
-    const int cta = blockIdx.x, col = blockIdx.y, tid = threadIdx.x;
-    const int4 join = *reinterpret_cast<const int4*>(a.joins + 4 * cta);
+    const int cta = blockIdx.x, col = blockIdx.y, d = threadIdx.x % HD, set = threadIdx.x / HD;
+    const int4 join = *reinterpret_cast<const int4*>(a.joins + 8 * cta);
+    const int n = a.joins[8 * cta + 4];
     if (join.x == 0) return;
-    Walk<COLS> w;
-    w.seq = join.y;
-    w.load(a);
     int g;
-    const int row = row_of_column<COLS>(a, w.first, w.n, join.z, col, g);
+    const int row = row_of_column<COLS>(a, join.w, n, join.y, col, g);
     if (row < 0) return;
     // part 0 is the second slot of its CTA, the others are the first slots of theirs
     const float* part = a.parts + size_t(cta) * 2 * FLOATS;
-    auto at = [&](int j) { return part + size_t(j == 0 ? 1 : 2 * j) * FLOATS; };
-    float top = -INFINITY;
-    for (int j = tid; j < join.x; j += HD) top = fmaxf(top, at(j)[COLS * HD + col]);
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+    for (int j0 = set; j0 < join.x; j0 += 8 * SETS) {
+        float m[8], l[8], y[8];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((tid & 31) == 0) red[tid / 32] = top;
-    __syncthreads();
+        for (int i = 0; i < 8; ++i) {
+            const int j = j0 + i * SETS;
+            const float* p = part + size_t(j == 0 ? 1 : 2 * j) * FLOATS;
+            m[i] = j < join.x ? p[COLS * HD + col] : -INFINITY;
+            l[i] = j < join.x ? p[COLS * HD + COLS + col] : 0.f;
+            y[i] = j < join.x ? p[col * HD + d] : 0.f;
+        }
+        float to = top;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) top = fmaxf(top, red[i]);
-    for (int j = tid; j < join.x; j += HD) by[j] = top == -INFINITY ? 0.f : ex2(at(j)[COLS * HD + col] - top);
-    __syncthreads();
-    float sum = 0.f, o = 0.f;
-#pragma unroll 8
-    for (int j = 0; j < join.x; ++j) {
-        sum += by[j] * at(j)[COLS * HD + COLS + col];
-        o += by[j] * at(j)[col * HD + tid];
+        for (int i = 0; i < 8; ++i) to = fmaxf(to, m[i]);
+        if (to == -INFINITY) continue;
+        const float keep = ex2(top - to);
+        sum *= keep; o *= keep; top = to;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float by = ex2(m[i] - to);
+            sum += by * l[i]; o += by * y[i];
+        }
     }
-    o = sum > 0.f ? o * (AtShape<T, HD, NT>::unscale / sum) : 0.f;
-    T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.w * a.group + g) * a.out.head + tid;
+    if constexpr (SETS > 1) {
+        rows[set][d] = o;
+        if (d == 0) { tops[set] = top; sums[set] = sum; }
+        __syncthreads();
+        if (set > 0) return;
+        float to = top;
+#pragma unroll
+        for (int i = 1; i < SETS; ++i) to = fmaxf(to, tops[i]);
+        o = sum = 0.f;
+        if (to > -INFINITY)
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) {
+                const float by = ex2(tops[i] - to);
+                sum += by * sums[i]; o += by * rows[i][d];
+            }
+    }
+    o = sum > 0.f ? o * (S::unscale / sum) : 0.f;
+    T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.z * a.group + g) * a.out.head + d;
     if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(o);
     else *to = o;
 }

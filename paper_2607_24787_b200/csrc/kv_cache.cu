@@ -123,7 +123,7 @@ void by_eights(int n, F f) {
     else f(std::integral_constant<int, 4>{});
 }
 constexpr size_t attend_part_bytes(int hd, int eights) { return size_t(8 * eights) * (hd + 2) * 4; }
-size_t attend_bytes(int hd, int eights) { return kAtMaxCtas * (16 + 2 * attend_part_bytes(hd, eights)); }
+size_t attend_bytes(int hd, int eights) { return kAtMaxCtas * (32 + 2 * attend_part_bytes(hd, eights)); }
 
 constexpr int kMaxDevices = 64;
 // Once a kernel and device: shared memory beyond 48 KB
@@ -148,7 +148,7 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     // launched ahead of the first kernel's end, which it waits for: its blocks are in place when the parts are
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(ctas, S::cols);
-    cfg.blockDim = dim3(HD);
+    cfg.blockDim = dim3(kAtJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -272,9 +272,11 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.page_shift = -1;
     for (int i = 0; i < 16; ++i)
         if (per_page == 1 << i) a.page_shift = i;
+    // (a guess where max_rows is one: it only says what to keep in L2)
+    a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8 * eights);
     a.scale = scale;
     a.joins = static_cast<int*>(workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 16);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
     by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
         by_eights(eights, [&](auto n) {

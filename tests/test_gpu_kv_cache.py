@@ -280,6 +280,19 @@ def test_attend(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     assert c.status.item() == 0
 
 
+@pytest.mark.parametrize("n_seq", [64, 65, 300, 1024])
+@pytest.mark.parametrize("rows", ["one", "ragged"])
+def test_many_sequences(kv, n_seq, rows):
+    """Sequences are found by a warp for itself up to 64 of them, by the block beyond; some have no rows, some no tokens."""
+    g = torch.Generator().manual_seed(n_seq)
+    new = [1] * n_seq if rows == "one" else torch.randint(0, 3, (n_seq,), generator=g).tolist()
+    lengths = torch.randint(0, 45, (n_seq,), generator=g).tolist()
+    lengths[n_seq // 2] = 400
+    c = Case(kv, 20, lengths, new, 1, 64, 16, BF16, 2, fill=True)
+    check_attend(c, 4)
+    assert c.status.item() == 0
+
+
 def test_one_row_a_sequence_without_row_start(kv):
     c = Case(kv, 9, [20, 0, 57], [1, 1, 1], 2, 128, 16, BF16, fill=True)
     q = c.randn(3, 8, 128)
