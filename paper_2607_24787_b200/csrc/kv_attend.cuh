@@ -60,7 +60,7 @@ struct AtShape {
     static constexpr int ring_bytes = stages * tile_bytes;
     static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
     static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8) + (n_seq > 64 ? n_seq * 4 : 0); }
-    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 4 + 6 * 1024 <= 232448, "227 KB");
+    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 4 + 10 * 1024 <= 232448, "227 KB");
 };
 
 // A walk along the line of tiles. nk: tokens that the last of the item's columns sees, nt: tiles (one at least, so that rows that see
@@ -125,7 +125,7 @@ __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int
     return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
 }
 
-struct PartMeta { int id, seq, ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
+struct PartMeta { int id, ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -138,9 +138,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     return r;
 }
 // D = A B + C
-__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float4& c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c.x), "f"(c.y), "f"(c.z), "f"(c.w));
 }
 // HD / 32 scales of a token
 template <int G>
@@ -202,6 +202,8 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     const uint32_t bars = smem_u32(rest) + warp * STAGES * 8;
     int* before = reinterpret_cast<int*>(rest + W * STAGES * 8);
     __shared__ PartMeta meta[2 * W];
+    __shared__ Walk<COLS> copied[W], used[W];      // the items that a warp's copies and its sums are at
+    __shared__ float4 starts[RAW ? W : 1][G][4];   // -8 times the sum of a group's queries, as the product's C for columns 2 c, 2 c + 1
     __shared__ int warp_sum_of[W];
     __shared__ float weight[2 * W][COLS], total[2 * W][COLS], highest[2 * W][COLS];
 
@@ -213,13 +215,13 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     __syncwarp();
     // ---- the line of tiles: how many there are, and before each sequence. Up to 64 sequences are two a lane, in every warp for itself ----
     const int n_seq = a.batch.n_seq;
-    Walk<COLS> use;
     int all = 0, before0 = 0, before1 = 0;
     auto count_tiles = [&](int s) {
-        use.seq = s;
-        use.load(a);
-        if (use.n > 0 && use.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-        return use.tiles_of_sequence(a);
+        Walk<COLS> w;
+        w.seq = s;
+        w.load(a);
+        if (w.n > 0 && w.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+        return w.tiles_of_sequence(a);
     };
     if (n_seq <= 64) {
         const int k0 = 2 * lane < n_seq ? count_tiles(2 * lane) : 0, k1 = 2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0;
@@ -271,22 +273,25 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     float m[NT][2], l[NT][2], y[NT][G][2][4];
     uint32_t qf[NT][QP][G][4];
     if (count > 0) {
-        // ---- copies: lanes 0 and 1 walk ahead and look up a block's page each, a tile before its use. A page of an even number of
-        // blocks holds both ----
-        Walk<COLS> ahead;
-        if (n_seq <= 64) {
-            const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
-            const int b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
-            ahead.seek(a, s, lo - (s & 1 ? b1 : b0));
-        } else {
-            int s = 0, end = n_seq;              // the last sequence with before[s] <= lo
-            while (end - s > 1) {
-                const int mid = (s + end) / 2;
-                if (before[mid] <= lo) s = mid; else end = mid;
+        {
+            Walk<COLS> at;
+            if (n_seq <= 64) {
+                const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
+                const int b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
+                at.seek(a, s, lo - (s & 1 ? b1 : b0));
+            } else {
+                int s = 0, end = n_seq;          // the last sequence with before[s] <= lo
+                while (end - s > 1) {
+                    const int mid = (s + end) / 2;
+                    if (before[mid] <= lo) s = mid; else end = mid;
+                }
+                at.seek(a, s, lo - before[s]);
             }
-            ahead.seek(a, s, lo - before[s]);
+            if (lane == 0) copied[warp] = used[warp] = at;
+            __syncwarp();
         }
-        use = ahead;
+        const Walk<COLS>& use = used[warp];
+        int t = use.t, nt_left = use.nt - t;     // tile of its item, tiles left there
         // an item's queries, as they are in memory
         auto fetch = [&] {
 #pragma unroll
@@ -305,24 +310,32 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             }
         };
         fetch();
+        // ---- copies: lanes 0 and 1 walk ahead and look up a block's page each, a tile before its use. A page of an even number of
+        // blocks holds both ----
         const int per_page = a.kv.page_size / kKvBlock;
         const bool even = per_page % 2 == 0;
         const long long page_bytes = static_cast<long long>(a.kv.heads) * per_page * BB;
         const uint32_t ring_at = smem_u32(ring);
         uint32_t present = 0;                    // two bits a stage: which blocks are there
         int issued = 0, page = -1, in_page = 0;
-        auto look_up = [&] {                     // for the tile `ahead`
-            const int block = ahead.t * 2 + lane;
+        int to_t, to_left, to_nk, to_head;
+        const int* to_table;
+        auto copies_at = [&](const Walk<COLS>& w) {
+            to_t = w.t; to_left = w.nt - w.t; to_nk = w.nk; to_head = w.head * per_page;
+            to_table = a.batch.table + size_t(w.seq) * a.batch.stride;
+        };
+        auto look_up = [&] {
+            const int block = to_t * 2 + lane;
             const int slot = a.page_shift >= 0 ? block >> a.page_shift : block / per_page;
-            in_page = block - slot * per_page;
-            page = block * kKvBlock < ahead.nk ? a.batch.table[size_t(ahead.seq) * a.batch.stride + slot] : -2;       // -2: not wanted
+            in_page = to_head + block - slot * per_page;
+            page = block * kKvBlock < to_nk ? to_table[slot] : -2;       // -2: not wanted
         };
         auto issue = [&](int stage) {
             uint32_t have = 0;
             if (lane < 2) {
                 const bool ok = page >= 0 && page < a.kv.n_pages;
                 if (!ok && page != -2) kv_note(a.kv, SPM_KV_BAD_PAGE);
-                const unsigned char* from = a.kv.pages + (page * page_bytes + static_cast<long long>(ahead.head * per_page + in_page) * BB);
+                const unsigned char* from = a.kv.pages + (page * page_bytes + static_cast<long long>(in_page) * BB);
                 have = __ballot_sync(3u, ok);
                 const uint32_t bar = bars + 8 * stage, dst = ring_at + stage * S::tile_bytes, bytes = __popc(have) * BB;
                 if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
@@ -331,21 +344,32 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                     if (a.once) bulk_g2s(dst + lane * BB, from, even ? bytes : BB, bar, policy_evict_first());
                     else bulk_g2s_plain(dst + lane * BB, from, even ? bytes : BB, bar);
                 }
-                if (issued + 1 < count) { ahead.next(a); look_up(); }
+                if (issued + 1 < count) {
+                    ++to_t;
+                    if (--to_left == 0) {
+                        Walk<COLS> w = copied[warp];
+                        w.t = w.nt - 1;
+                        w.next(a);
+                        __syncwarp(3u);
+                        if (lane == 0) copied[warp] = w;
+                        __syncwarp(3u);
+                        copies_at(w);
+                    }
+                    look_up();
+                }
             }
             ++issued;
             present = (present & ~(3u << (2 * stage))) | __shfl_sync(0xffffffffu, have, 0) << (2 * stage);
         };
+        copies_at(use);
         if (lane < 2) look_up();
 #pragma unroll
         for (int i = 0; i < STAGES; ++i)
             if (i < count) issue(i);
-
         // scores are kept as the products give them; f > 0 takes them to powers of two (a negative scale turns the queries' signs, and
         // with a scale of 0 a masked score still counts as one)
         const float f = fmaxf(fabsf(a.scale), 1e-30f) * ((RAW ? kAtUp69 : kQ4ExactUnscale) * 1.4426950408889634f), slack = 6.f / f;
         const bool flip = a.scale < 0.f;
-        float start[G][4];                       // -8 times the sum of a group's queries, as the product's C
         int whole_tiles = 0;
         int began = 0;                           // the item's tile with which this warp's part of it begins
         auto begin = [&] {
@@ -376,14 +400,17 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                         sum *= -8.f * 0x1p-133f;       // to where a code's 1 stands
-                        start[k][0] = start[k][2] = __shfl_sync(0xffffffffu, sum, 8 * c);
-                        start[k][1] = start[k][3] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
+                        if (c == 0) {
+                            float* to = reinterpret_cast<float*>(&starts[warp][k][r / 2]) + r % 2;
+                            to[0] = to[2] = sum;
+                        }
                     }
                 }
                 m[nt][0] = m[nt][1] = -INFINITY;
                 l[nt][0] = l[nt][1] = 0.f;
             }
-            began = use.t;
+            if constexpr (RAW) __syncwarp();
+            began = t;
             whole_tiles = min(use.nk, use.len - use.n + use.ct * COLS / a.group + 1) / kAtTile;
         };
         begin();
@@ -417,7 +444,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             float d[4];
-                            if constexpr (RAW) mma_k16_from(d, start[k + h], u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
+                            if constexpr (RAW) mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
                             else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
 #pragma unroll
                             for (int q = 0; q < QP; ++q) {
@@ -431,14 +458,14 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                 }
             }
             // ---- tokens that are not there, or behind a column's row ----
-            const bool whole = have == 3 && use.t < whole_tiles;
+            const bool whole = have == 3 && t < whole_tiles;
             if (!whole) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int i2 = (use.ct * COLS + 8 * nt + 2 * c + e) / a.group;
-                        const int sees = min(use.nk, use.len - use.n + i2 + 1) - use.t * kAtTile;      // tokens of this tile
+                        const int sees = min(use.nk, use.len - use.n + i2 + 1) - t * kAtTile;      // tokens of this tile
 #pragma unroll
                         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -496,8 +523,8 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                 if (!whole) {                    // what has never been written may be anything
 #pragma unroll
                     for (int k = 0; k < G; ++k) {
-                        if (!(have >> b & 1) || use.t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
-                        if (!(have >> b & 1) || use.t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
+                        if (!(have >> b & 1) || t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
+                        if (!(have >> b & 1) || t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
                     }
                 }
 #pragma unroll
@@ -534,7 +561,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
 
             // ---- the item ends, or the warp's piece ----
-            const bool ends = use.t + 1 == use.nt;
+            const bool ends = nt_left == 1;
             if (ends || i + 1 == count) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -577,11 +604,22 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                                                                                                            y[nt][k][1][e], S::odd(y[nt][k][1][2 + e], y[nt][k][1][e]));
                             if (r == 0) { part[COLS * HD + col] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * f; part[COLS * HD + COLS + col] = l[nt][e]; }
                         }
-                    if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - use.t, use.seq, use.ct, use.head, began, use.t + 1, use.nt, use.first, use.n};
+                    if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - t, use.ct, use.head, began, t + 1, use.nt, use.first, use.n};
                 }
             }
-            if (!ends) ++use.t;
-            else if (i + 1 < count) { use.next(a); fetch(); begin(); }
+            ++t;
+            if (--nt_left == 0 && i + 1 < count) {
+                Walk<COLS> w = use;
+                w.t = w.nt - 1;
+                w.next(a);
+                __syncwarp();
+                if (lane == 0) used[warp] = w;
+                __syncwarp();
+                t = 0;
+                nt_left = w.nt;
+                fetch();
+                begin();
+            }
         }
     }
     __syncthreads();
@@ -589,7 +627,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     // ---- parts of one item in this CTA meet: they stand one after another. Every warp sees which parts belong together (lane j: part j);
     // first a warp takes a column of an item for the parts' weights, then threads take sums ----
     const int id = lane < 2 * W ? meta[lane].id : -1;
-    const uint32_t used = __ballot_sync(0xffffffffu, id >= 0), mates = __match_any_sync(0xffffffffu, id) & used;
+    const uint32_t mates = __match_any_sync(0xffffffffu, id);
     const uint32_t leaders = __ballot_sync(0xffffffffu, id >= 0 && (mates & ((1u << lane) - 1)) == 0);
     auto part_of = [&](int j) { return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes); };
     {
