@@ -495,7 +495,7 @@ typedef struct {
     const float*   q_gamma;       /* dev [head_dim] or NULL                                                      */
     const float*   k_gamma;
     int32_t n_axes;               /* 1 .. SPM_KV_MAX_AXES                                                        */
-    int32_t rot_dim;              /* leading elements that turn: a multiple of head_dim / 16, at most head_dim; 0: none */
+    int32_t rot_dim;              /* leading elements that turn: a multiple of 16, at most head_dim; 0: none */
     int32_t neighbours;           /* 0: pair i is elements (i, i + rot_dim/2); 1: elements (2i, 2i + 1)          */
     float   eps;
 } spm_rope;

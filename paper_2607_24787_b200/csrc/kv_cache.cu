@@ -68,7 +68,7 @@ int check_rows(const char* call, const char* name, const spm_rows* r, int dtype)
 }
 int check_rope(const char* call, const spm_rope* r, const int32_t* positions, int64_t pos_stride, int n_rows, int hd) {
     if (!r) return fail(call, SPM_ERR_INVALID_ARG, "rope is null");
-    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % (hd / 16)) return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of head_dim / 16 up to head_dim");
+    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % 16) return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of 16 up to head_dim");
     if (r->n_axes < 1 || r->n_axes > SPM_KV_MAX_AXES) return fail(call, SPM_ERR_INVALID_ARG, "n_axes outside 1.." + std::to_string(SPM_KV_MAX_AXES));
     if (r->rot_dim > 0 && (!r->inv_freq || !positions)) return fail(call, SPM_ERR_INVALID_ARG, "inv_freq or positions is null");
     if (r->rot_dim > 0 && r->n_axes > 1 && pos_stride < n_rows) return fail(call, SPM_ERR_INVALID_ARG, "pos_stride is less than the rows");
@@ -99,11 +99,12 @@ void by_type(int dtype, int hd, F f) {
 int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaStream_t st) {
     const int heads = 2 * a.kv_heads + a.q_heads;
     if (a.n_rows == 0 || heads == 0) return SPM_OK;
-    // a few rows: a head a warp, for latency; many: a block goes through all heads of its row, whose angles it takes once
-    const int chunks = (heads + kKvWarps - 1) / kKvWarps;
-    const dim3 grid(a.n_rows, static_cast<long long>(a.n_rows) * chunks <= 592 ? chunks : 1);
+    // many rows: eight a block; few: one, and blocks share its heads (a turn a warp)
+    const int each = a.n_rows >= kKvWriteRows * 592 ? kKvWriteRows : a.n_rows >= 1184 ? 2 : 1;
+    const int at_once = 256 / hd, turns = 2 * ((a.kv_heads + at_once - 1) / at_once) + (a.q_heads + at_once - 1) / at_once, chunks = (turns + kKvWarps - 1) / kKvWarps;
+    const dim3 grid((a.n_rows + each - 1) / each, static_cast<long long>(a.n_rows) * chunks <= 592 ? chunks : 1);
     by_type(dtype, hd, [&](auto* t, auto size) {
-        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a);
+        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a, each);
     });
     return launched(call);
 }
@@ -227,7 +228,8 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
     a.batch = batch_of(batch);
     if (k_out) { if (int rc = check_rows(call, "k_out", k_out, dtype)) return rc; a.k = rows_of(k_out); }
     if (v_out) { if (int rc = check_rows(call, "v_out", v_out, dtype)) return rc; a.v = rows_of(v_out); }
-    const unsigned grid = unsigned((static_cast<long long>(batch->n_rows) + kKvWarps - 1) / kKvWarps);
+    const int each = kKvWarps * 32 / (kv->head_dim / 8);
+    const unsigned grid = unsigned((static_cast<long long>(batch->n_rows) + each - 1) / each);
     by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         kv_read_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
     });

@@ -24,130 +24,203 @@ struct WriteArgs {
     int q_heads, kv_heads, n_rows;
 };
 
-// What a lane turns of a head row: its elements' cosines and sines, and the lane that holds their partners
-template <int E>
-struct Turn {
-    float c[E], s[E];
-    int partner;                       // -1: not turned
-};
+// A lane holds eight consecutive elements of a head, HD / 8 lanes a head, so a warp takes 32 / (HD / 8) heads at once.
+//
+// The norm and the rotation decide between 4-bit codes, so their roundings are spelled out: every product and sum is rounded by itself
+// (nothing is contracted), the norm's sum is taken in 64 bits, and so are the angles.
 
-// x: E elements a lane of one head row. Products and sums are rounded one by one and the norm's sum is taken in 64 bits, so that the
-// 4-bit codes do not depend on how the compiler contracts or on the order of a sum.
-template <int E>
-__device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Turn<E>& t, const float* gamma, int lane, float (&x)[E]) {
-    if (gamma) {
+// 1 / sqrt(v): Newton's step from the fp32 instruction's 22 bits leaves more than 40 (the double division and root take four times the
+// rest of the kernel)
+__device__ __forceinline__ float rsqrt_of(double v) {
+    if (!(v > 1e-30 && v < 1e30)) return float(1. / sqrt(v));
+    const double y = rsqrtf(float(v));
+    return float(fma(0.5 * y, fma(-v * y, y, 1.0), y));
+}
+
+// Cosines and sines of a row's pairs. Lane `sub` of the first halves turns pairs 8 sub .. 8 sub + 7 (with neighbours: pairs 4 sub .. 4 sub + 3),
+// lane sub + rot_dim / 16 their second halves; entry [j][i] holds pairs 8 i + 2 j and 8 i + 2 j + 1, so that lanes read side by side. The
+// second table has the sines' signs turned: a first half is a cos + b (-sin), rounded as a cos - b sin is.
+template <int HD>
+struct Angles { float4 at[2][4][HD / 16]; };
+template <int HD>
+__device__ __forceinline__ void set_angle(Angles<HD>& t, int pair, float c, float s) {
+    const int j = pair % 8 / 2, i = pair / 8, odd = pair & 1;
+    reinterpret_cast<float2*>(&t.at[0][j][i])[odd] = make_float2(c, s);
+    reinterpret_cast<float2*>(&t.at[1][j][i])[odd] = make_float2(c, -s);
+}
+
+// Norm (with gammas g) and rotation of eight elements a lane
+template <int HD>
+__device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Angles<HD>& t, bool norm, const float (&g)[8], int sub, float (&x)[8]) {
+    constexpr int LANES = HD / 8;
+    if (norm) {
         double sum = 0.;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += double(x[e]) * double(x[e]);
+        for (int e = 0; e < 8; ++e) { const double v = x[e]; sum = fma(v, v, sum); }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float inv = float(1. / sqrt(sum / (32 * E) + double(a.eps)));
-        float g[E];
-        load_row<E>(gamma + lane * E, g);
+        for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float inv = rsqrt_of(sum * (1. / HD) + double(a.eps));
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], inv), g[e]);
+        for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], inv), g[e]);
     }
     if (a.rot_dim == 0) return;
     if (a.neighbours) {
-        if (t.partner < 0) return;
+        if (sub * 8 >= a.rot_dim) return;
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            const float p = x[e], q = x[e + 1];
-            x[e] = __fsub_rn(__fmul_rn(p, t.c[e]), __fmul_rn(q, t.s[e]));
-            x[e + 1] = __fadd_rn(__fmul_rn(q, t.c[e]), __fmul_rn(p, t.s[e]));
+        for (int e = 0; e < 8; e += 4) {
+            const float4 v = t.at[0][2 * (sub & 1) + e / 4][sub / 2];
+            const float p0 = x[e], q0 = x[e + 1], p1 = x[e + 2], q1 = x[e + 3];
+            x[e] = __fsub_rn(__fmul_rn(p0, v.x), __fmul_rn(q0, v.y));
+            x[e + 1] = __fadd_rn(__fmul_rn(q0, v.x), __fmul_rn(p0, v.y));
+            x[e + 2] = __fsub_rn(__fmul_rn(p1, v.z), __fmul_rn(q1, v.w));
+            x[e + 3] = __fadd_rn(__fmul_rn(q1, v.z), __fmul_rn(p1, v.w));
         }
         return;
     }
-    const int from = t.partner < 0 ? lane : t.partner;
+    const int half = a.rot_dim / 16;             // lanes of the first halves
+    const bool low = sub < half, in = sub < 2 * half;
+    const int from = (threadIdx.x & 31) + (!in ? 0 : low ? half : -half);
+    float o[8];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float o = __shfl_sync(0xffffffffu, x[e], from);
-        if (t.partner < 0) continue;
-        const float xc = __fmul_rn(x[e], t.c[e]), os = __fmul_rn(o, t.s[e]);
-        x[e] = t.partner > lane ? __fsub_rn(xc, os) : __fadd_rn(xc, os);
+    for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(0xffffffffu, x[e], from);
+    if (!in) return;
+    const float4* at = &t.at[low][0][low ? sub : sub - half];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float4 v = at[e / 2 * (HD / 16)];
+        x[e] = __fadd_rn(__fmul_rn(x[e], v.x), __fmul_rn(o[e], v.y));
+        x[e + 1] = __fadd_rn(__fmul_rn(x[e + 1], v.z), __fmul_rn(o[e + 1], v.w));
     }
 }
 
-// One head row into the cache: `at` is its block, tok its place there, part 0 / 1 keys / values
+// A lane's eight elements into the cache (lanes with `write`): `at` is the head's block and part, tok the row's place there. Four lanes hold
+// a group.
 template <int HD>
-__device__ __forceinline__ void quantise_row(const KvPool& kv, unsigned char* at, int tok, int part, int lane, float (&x)[HD / 32]) {
-    constexpr int E = HD / 32;
+__device__ __forceinline__ void quantise_row(const KvPool& kv, unsigned char* codes_at, unsigned char* scales_at, int tok, bool write, int sub, float (&x)[8]) {
     bool odd = false;
     float m = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < 8; ++e) {
         odd |= !(fabsf(x[e]) < INFINITY);
         if (x[e] != x[e]) x[e] = 0.f;
         if (fabsf(x[e]) > fabsf(m)) m = x[e];
     }
-    if (__any_sync(0xffffffffu, odd) && lane == 0) kv_note(kv, SPM_KV_NONFINITE);
 #pragma unroll
-    for (int o = 1; o < 32 / E; o <<= 1) {
+    for (int o = 1; o < 4; o <<= 1) {
         const float other = __shfl_xor_sync(0xffffffffu, m, o);
-        if (fabsf(other) > fabsf(m) || (fabsf(other) == fabsf(m) && (lane & o))) m = other;
+        if (fabsf(other) > fabsf(m) || (fabsf(other) == fabsf(m) && (sub & o))) m = other;
     }
+    if (!write) return;
+    if (odd) kv_note(kv, SPM_KV_NONFINITE);
     const __half scale = __float2half_rn(fminf(fmaxf(m * -0.125f, -65504.f), 65504.f));
     const float d = __half2float(scale), inv = d == 0.f ? 0.f : __frcp_rn(d);
     uint32_t codes = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < 8; ++e) {
         const float r = fminf(fmaxf(rintf(__fmul_rn(x[e], inv)), -8.f), 7.f);
         codes |= uint32_t(int(r) + 8) << (4 * e);
     }
-    const int g = lane * E / 32, in = lane * E % 32;
-    unsigned char* to = at + part * kv_v_codes(HD) + (g * kKvBlock + tok) * 16 + in / 2;
-    if constexpr (E == 2) *to = (unsigned char)codes;
-    else if constexpr (E == 4) *reinterpret_cast<unsigned short*>(to) = (unsigned short)codes;
-    else *reinterpret_cast<uint32_t*>(to) = codes;
-    if (in == 0) *reinterpret_cast<__half*>(at + kv_k_scales(HD) + part * HD + (tok * (HD / 32) + g) * 2) = scale;
+    const int g = sub / 4;
+    *reinterpret_cast<uint32_t*>(codes_at + (g * kKvBlock + tok) * 16 + sub % 4 * 4) = codes;
+    if (sub % 4 == 0) *reinterpret_cast<__half*>(scales_at + (tok * (HD / 32) + g) * 2) = scale;
 }
 
-// A block takes a row and, of its heads (keys, values, queries), every gridDim.y-th eight; a warp takes a head.
+// Eight elements as they are in memory
+struct Raw8 { uint4 a, b; };
+__device__ __forceinline__ Raw8 raw8(const float* p) { return {reinterpret_cast<const uint4*>(p)[0], reinterpret_cast<const uint4*>(p)[1]}; }
+__device__ __forceinline__ Raw8 raw8(const __nv_bfloat16* p) { return {*reinterpret_cast<const uint4*>(p), make_uint4(0, 0, 0, 0)}; }
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8& r, float (&x)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        two_bf16(r.a.x, x[0], x[1]); two_bf16(r.a.y, x[2], x[3]); two_bf16(r.a.z, x[4], x[5]); two_bf16(r.a.w, x[6], x[7]);
+    } else {
+        x[0] = __uint_as_float(r.a.x); x[1] = __uint_as_float(r.a.y); x[2] = __uint_as_float(r.a.z); x[3] = __uint_as_float(r.a.w);
+        x[4] = __uint_as_float(r.b.x); x[5] = __uint_as_float(r.b.y); x[6] = __uint_as_float(r.b.z); x[7] = __uint_as_float(r.b.w);
+    }
+}
+
+// A block takes up to kKvWriteRows rows: where they are and all of their angles first. Then a warp goes through the rows with a few heads
+// of one kind at a time (a turn), so that what it has of a head stays in registers; a row is loaded while the one before it is worked on.
+// gridDim.y > 1 (few rows): blocks share the turns.
+constexpr int kKvWriteRows = 8;
 template <typename T, int HD>
-__global__ void __launch_bounds__(kKvWarps * 32) kv_write_kernel(const WriteArgs a) {
-    constexpr int E = HD / 32;
-    __shared__ float2 turn[HD / 2];
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long block = -1;
-    int tok = 0;
-    if (a.batch.n_seq >= 0) {
-        const RowAt r = kv_row_at(a.batch, row);
-        if (r.seq >= a.batch.n_seq) return;
-        if (r.pos >= 0 && a.kv_heads) {
-            block = kv_block_at<HD>(a.kv, a.batch, r.seq, r.pos, 0);
-            tok = r.pos % kKvBlock;
-            if (block < 0 && lane == 0) kv_note(a.kv, r.pos / a.kv.page_size >= a.batch.stride ? SPM_KV_TOO_LONG : SPM_KV_BAD_PAGE);
+__global__ void __launch_bounds__(kKvWarps * 32, 4) kv_write_kernel(const WriteArgs a, int rows_each) {
+    constexpr int LANES = HD / 8, HEADS = 32 / LANES;
+    __shared__ Angles<HD> angles[kKvWriteRows];
+    __shared__ long long blocks[kKvWriteRows];   // of the row's head 0 in the cache; -1: nowhere, -2: no sequence's row
+    __shared__ int toks[kKvWriteRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES;
+    const long long row0 = static_cast<long long>(blockIdx.x) * rows_each;
+    const int rows = int(min(static_cast<long long>(rows_each), a.n_rows - row0));
+    // turns: keys, values, queries
+    const int kv_turns = (a.kv_heads + HEADS - 1) / HEADS, turns = 2 * kv_turns + (a.q_heads + HEADS - 1) / HEADS;
+    // a turn's rows are cut in `cuts`, so that all warps have work, and about the same
+    const int cuts = min(rows, max(2, 2 * kKvWarps / turns));
+    int task = blockIdx.y * kKvWarps + warp, kind = 0, head = 0, first = 0, end = 0;
+    const T* src = nullptr;
+    Raw8 raw{};
+    auto take = [&] {
+        const int turn = task / cuts, cut = task - turn * cuts;
+        first = rows * cut / cuts; end = rows * (cut + 1) / cuts;
+        kind = turn < kv_turns ? 0 : turn < 2 * kv_turns ? 1 : 2;
+        head = (turn - kind * kv_turns) * HEADS + lane / LANES;
+        const HeadRows& from = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
+        const bool is = turn < turns && head < (kind == 2 ? a.q_heads : a.kv_heads);
+        src = is ? static_cast<const T*>(from.p) + (row0 + first) * from.row + head * from.head + sub * 8 : nullptr;
+        if (is) raw = raw8(src);
+    };
+    take();
+    if (warp < rows) {
+        long long block = -1;
+        int tok = 0;
+        if (a.batch.n_seq >= 0) {
+            const RowAt r = kv_row_at(a.batch, int(row0) + warp);
+            if (r.seq >= a.batch.n_seq) block = -2;
+            else if (r.pos >= 0) {
+                block = kv_block_at<HD>(a.kv, a.batch, r.seq, r.pos, 0);
+                tok = r.pos % kKvBlock;
+                if (block < 0 && lane == 0) kv_note(a.kv, r.pos / a.kv.page_size >= a.batch.stride ? SPM_KV_TOO_LONG : SPM_KV_BAD_PAGE);
+            }
         }
+        if (lane == 0) { blocks[warp] = block; toks[warp] = tok; }
     }
     const int half = a.rope.rot_dim / 2;
-    for (int i = threadIdx.x; i < half; i += blockDim.x) {
-        const int axis = a.rope.axis_of ? min(int(a.rope.axis_of[i]), a.rope.n_axes - 1) : 0;
+    for (int j = threadIdx.x; j < rows * half; j += blockDim.x) {
+        const int rr = j / half, p = j - rr * half;
+        const int axis = a.rope.axis_of ? min(int(a.rope.axis_of[p]), a.rope.n_axes - 1) : 0;
         double s, c;
-        sincos(double(a.rope.positions[axis * a.rope.pos_stride + row]) * double(a.rope.inv_freq[i]), &s, &c);
-        turn[i] = make_float2(float(c), float(s));
+        sincos(double(a.rope.positions[axis * a.rope.pos_stride + row0 + rr]) * double(a.rope.inv_freq[p]), &s, &c);
+        set_angle(angles[rr], p, float(c), float(s));
     }
     __syncthreads();
-    Turn<E> t;
-    const int lanes = a.rope.rot_dim / E;            // that hold turned elements
-    t.partner = lane >= lanes ? -1 : lane < lanes / 2 ? lane + lanes / 2 : lane - lanes / 2;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int pair = a.rope.neighbours ? (lane * E + e) / 2 : (t.partner < lane ? t.partner : lane) * E + e;
-        const float2 cs = t.partner < 0 ? make_float2(1.f, 0.f) : turn[pair];
-        t.c[e] = cs.x; t.s[e] = cs.y;
-    }
-    const long long head_bytes = static_cast<long long>(a.kv.page_size / kKvBlock) * kv_block_bytes(HD);
-    const int heads = 2 * a.kv_heads + a.q_heads;
-    for (int h = blockIdx.y * kKvWarps + warp; h < heads; h += gridDim.y * kKvWarps) {
-        const int kind = h < a.kv_heads ? 0 : h < 2 * a.kv_heads ? 1 : 2;       // key, value, query
-        const int in = h - kind * a.kv_heads;
-        const HeadRows& src = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
-        if (kind < 2 && block < 0) continue;
-        float x[E];
-        load_row<E>(static_cast<const T*>(src.p) + row * src.row + in * src.head + lane * E, x);
-        if (kind != 1) norm_and_turn<E>(a.rope, t, kind == 0 ? a.rope.k_gamma : a.rope.q_gamma, lane, x);
-        if (kind == 2) store_row<E>(static_cast<T*>(a.q_out.p) + row * a.q_out.row + in * a.q_out.head + lane * E, x);
-        else quantise_row<HD>(a.kv, a.kv.pages + block + in * head_bytes, tok, kind, lane, x);
+    while (task < turns * cuts) {
+        const float* gamma = kind == 0 ? a.rope.k_gamma : kind == 2 ? a.rope.q_gamma : nullptr;
+        float g[8] = {};
+        if (gamma) load_row<8>(gamma + sub * 8, g);
+        const long long step = (kind == 0 ? a.k : kind == 1 ? a.v : a.q).row;
+        if (kind == 2) {
+            T* dst = static_cast<T*>(a.q_out.p) + (row0 + first) * a.q_out.row + head * a.q_out.head + sub * 8;
+            for (int r = first; r < end; ++r) {
+                float x[8];
+                unpack8<T>(raw, x);
+                if (src && r + 1 < end) raw = raw8(src += step);
+                norm_and_turn<HD>(a.rope, angles[r], gamma != nullptr, g, sub, x);
+                if (src && blocks[r] != -2) store_row<8>(dst, x);
+                dst += a.q_out.row;
+            }
+        } else {
+            unsigned char* at = a.kv.pages + head * static_cast<long long>(a.kv.page_size / kKvBlock) * kv_block_bytes(HD);
+            for (int r = first; r < end; ++r) {
+                float x[8];
+                unpack8<T>(raw, x);
+                if (src && r + 1 < end) raw = raw8(src += step);
+                if (kind == 0) norm_and_turn<HD>(a.rope, angles[r], gamma != nullptr, g, sub, x);
+                const long long block = blocks[r];
+                quantise_row<HD>(a.kv, at + block + kind * kv_v_codes(HD), at + block + kv_k_scales(HD) + kind * HD, toks[r], src && block >= 0, sub, x);
+            }
+        }
+        task += gridDim.y * kKvWarps;
+        take();
     }
 }
 
@@ -157,35 +230,58 @@ struct ReadArgs {
     HeadRows k, v;
 };
 
-// A warp takes a row; HD / 8 lanes a head's keys or values, eight elements each
+// A thread takes eight elements of a row, of every head's keys and values, four of them in flight. Neighbouring tokens, whose codes stand
+// side by side, are in one warp.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kKvWarps * 32) kv_read_kernel(const ReadArgs a) {
-    constexpr int LANES = HD / 8;
-    const int lane = threadIdx.x & 31, sub = lane % LANES;
-    const long long row = static_cast<long long>(blockIdx.x) * kKvWarps + (threadIdx.x >> 5);
-    if (row >= a.batch.n_rows) return;
-    const RowAt r = kv_row_at(a.batch, int(row));
-    if (r.seq >= a.batch.n_seq) return;
-    long long block = -1;
-    if (r.pos >= 0) {
-        block = kv_block_at<HD>(a.kv, a.batch, r.seq, r.pos, 0);
-        if (block < 0 && lane == 0) kv_note(a.kv, r.pos / a.kv.page_size >= a.batch.stride ? SPM_KV_TOO_LONG : SPM_KV_BAD_PAGE);
+    constexpr int LANES = HD / 8, ROWS = kKvWarps * 32 / LANES, AHEAD = 4;
+    __shared__ long long blocks[ROWS];           // of the row's head 0; -1: nowhere (zeros), -2: no sequence's row
+    __shared__ int toks[ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long row0 = static_cast<long long>(blockIdx.x) * ROWS;
+    const int rows = int(min(static_cast<long long>(ROWS), a.batch.n_rows - row0));
+    for (int i = warp; i < rows; i += kKvWarps) {
+        const RowAt r = kv_row_at(a.batch, int(row0) + i);
+        long long block = r.seq >= a.batch.n_seq ? -2 : -1;
+        if (block == -1 && r.pos >= 0) {
+            block = kv_block_at<HD>(a.kv, a.batch, r.seq, r.pos, 0);
+            if (block < 0 && lane == 0) kv_note(a.kv, r.pos / a.kv.page_size >= a.batch.stride ? SPM_KV_TOO_LONG : SPM_KV_BAD_PAGE);
+        }
+        if (lane == 0) { blocks[i] = block; toks[i] = r.pos % kKvBlock; }
     }
-    const int tok = r.pos % kKvBlock;
+    __syncthreads();
+    const int sub = threadIdx.x % LANES, rr = threadIdx.x / LANES;
+    if (rr >= rows || blocks[rr] == -2) return;
+    const bool there = blocks[rr] >= 0;
+    const int tok = there ? toks[rr] : 0;
     const long long head_bytes = static_cast<long long>(a.kv.page_size / kKvBlock) * kv_block_bytes(HD);
-    for (int i = lane / LANES; i < 2 * a.kv.heads; i += 32 / LANES) {
-        const int part = i >= a.kv.heads, head = i - part * a.kv.heads;
+    const unsigned char* at = a.kv.pages + (there ? blocks[rr] : 0) + (sub / 4 * kKvBlock + tok) * 16 + sub % 4 * 4;
+    const unsigned char* scales = a.kv.pages + (there ? blocks[rr] : 0) + kv_k_scales(HD) + (tok * (HD / 32) + sub / 4) * 2;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
         const HeadRows& out = part ? a.v : a.k;
         if (!out.p) continue;
-        float x[8] = {};
-        if (block >= 0) {
-            const unsigned char* at = a.kv.pages + block + head * head_bytes;
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(at + part * kv_v_codes(HD) + (sub / 4 * kKvBlock + tok) * 16 + sub % 4 * 4);
-            const float d = __half2float(*reinterpret_cast<const __half*>(at + kv_k_scales(HD) + part * HD + (tok * (HD / 32) + sub / 4) * 2));
+        T* to = static_cast<T*>(out.p) + (row0 + rr) * out.row + sub * 8;
+        for (int h0 = 0; h0 < a.kv.heads; h0 += AHEAD) {
+            uint32_t w[AHEAD];
+            __half d[AHEAD];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float(w >> (4 * e) & 15) - 8.f) * d;
+            for (int u = 0; u < AHEAD; ++u) {
+                if (!there || h0 + u >= a.kv.heads) continue;
+                w[u] = *reinterpret_cast<const uint32_t*>(at + part * kv_v_codes(HD) + (h0 + u) * head_bytes);
+                d[u] = *reinterpret_cast<const __half*>(scales + part * HD + (h0 + u) * head_bytes);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (h0 + u >= a.kv.heads) continue;
+                float x[8] = {};
+                if (there) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = (float(w[u] >> (4 * e) & 15) - 8.f) * __half2float(d[u]);
+                }
+                store_row<8>(to + (h0 + u) * out.head, x);
+            }
         }
-        store_row<8>(static_cast<T*>(out.p) + row * out.row + head * out.head + sub * 8, x);
     }
 }
 

@@ -97,6 +97,35 @@ def test_write_is_exact(kv, lengths, rows, hk, hd, page, dtype, pad):
     assert c.status.item() == 0
 
 
+def test_many_rows(kv):
+    """More rows than one block a row takes: written, read back and turned as in small calls."""
+    c = Case(kv, 17, [2500, 900, 17], [2400, 900, 10], 1, 64, 16, BF16, 3)
+    k, v = c.randn(c.n_rows, 1, 64), c.randn(c.n_rows, 1, 64)
+    rope, plain = rope_of(kv, 64)
+    pos = torch.randint(0, 9000, (3, c.n_rows), generator=c.g, dtype=torch.int32).cuda()
+    c.cache.write(c.batch, k, v)
+    assert np.array_equal(c.pages(), expected_pages(c, k.float().cpu().numpy(), v.float().cpu().numpy()))
+    back = [torch.full((c.n_rows, 1, 64), 4.0, device="cuda") for _ in range(2)]
+    c.cache.read(c.batch, k_out=back[0], v_out=back[1])
+    n = c.row_start[-1]
+    for x, y in ((k, back[0]), (v, back[1])):
+        codes, d = R.quantise(x.float().cpu().numpy())
+        want = (codes.astype(np.float64) - 8) * np.repeat(d.astype(np.float64), 32, axis=-1)
+        assert np.array_equal(y.double().cpu().numpy()[:n], want[:n]) and (y[n:] == 4).all()
+    big = torch.randn(20_001, 3, 64, generator=c.g).cuda()          # and enough for blocks of many rows, in both calls
+    at = torch.randint(0, 9000, (3, 20_001), generator=c.g, dtype=torch.int32)
+    want = plain(big, at, 0)
+    off = np.abs(kv.rotate_heads(big, at.cuda(), rope).double().cpu().numpy() - want)
+    assert (off <= turn_tolerance(want, 64, False, FP32)).all()
+    whole = Case(kv, 18, [19_500, 33], [19_500, 33], 1, 64, 16, BF16, fill=True)
+    got = whole.cache.read(whole.batch, FP32)
+    for i in list(range(0, 19_500, 977)) + [19_499, 19_500, 19_532]:
+        seq, p = (0, i) if i < 19_500 else (1, i - 19_500)
+        page = R.page_of(whole.start, whole.table.numpy(), seq, p, 16)
+        for part in range(2):
+            assert np.array_equal(got[part][i, 0].double().cpu().numpy(), R.get(whole.start, page, 0, p % 16, part))
+
+
 @pytest.mark.parametrize("layout", ["projection", "heads_first", "wide_rows"])
 def test_write_takes_strided_rows(kv, layout):
     c = Case(kv, 4, [40, 9], [11, 3], 2, 128, 16, BF16)
