@@ -58,9 +58,14 @@ def get(pages, page, head, offset, part):
     for g in range(hd // 32):
         raw = block[part * 8 * hd + (g * 16 + tok) * 16:][:16]
         code[32 * g:32 * g + 32:2], code[32 * g + 1:32 * g + 32:2] = raw & 15, raw >> 4
-    at = 16 * hd + part * hd + tok * (hd // 32) * 2
-    scale = np.frombuffer(block[at:at + hd // 16].tobytes(), np.float16).astype(np.float64)
-    return (code - 8) * np.repeat(scale, 32)
+    return (code - 8) * scales(pages, page, head, offset, part)
+
+
+def scales(pages, page, head, offset, part):
+    """The scale of each element of that row, as float64 values [hd]."""
+    hd = pages.shape[3] // 18
+    at = 16 * hd + part * hd + offset % 16 * (hd // 32) * 2
+    return np.repeat(np.frombuffer(pages[page, head, offset // 16][at:at + hd // 16].tobytes(), np.float16).astype(np.float64), 32)
 
 
 def places(lengths, row_start, n_rows):
@@ -81,23 +86,25 @@ def page_of(pages, table, seq, pos, page_size):
 
 
 def context(pages, table, seq, length, page_size, head):
-    """(keys, values [n, hd], which of the first `length` tokens exist)."""
-    k, v, there = [], [], []
+    """(keys, values [n, hd], which of the first `length` tokens exist, 8 |scale| of the values' elements [n, hd])."""
+    k, v, there, wide = [], [], [], []
+    hd = pages.shape[3] // 18
     for t in range(max(0, length)):
         p = page_of(pages, table, seq, t, page_size)
         there.append(p is not None)
         for part, out in ((0, k), (1, v)):
-            out.append(get(pages, p, head, t % page_size, part) if p is not None else np.zeros(pages.shape[3] // 18))
-    hd = pages.shape[3] // 18
-    return np.array(k).reshape(-1, hd), np.array(v).reshape(-1, hd), np.array(there, bool)
+            out.append(get(pages, p, head, t % page_size, part) if p is not None else np.zeros(hd))
+        wide.append(np.zeros(hd) if p is None else 8 * np.abs(scales(pages, p, head, t % page_size, 1)))
+    return np.array(k).reshape(-1, hd), np.array(v).reshape(-1, hd), np.array(there, bool), np.array(wide).reshape(-1, hd)
 
 
 def attend(q, pages, table, lengths, row_start, scale):
-    """q [rows, heads, hd] float64 -> (out, sum of p |v|, largest scale * sum |q k|), each [rows, heads, hd or 1]; rows of no sequence: NaN."""
+    """q [rows, heads, hd] float64 -> (out, sum of p |v|, largest scale * sum |q k|, sum of p times what a value of its group can be), each
+    [rows, heads, hd or 1]; rows of no sequence: NaN."""
     n_rows, heads, hd = q.shape
     kv_heads, page_size = pages.shape[1], pages.shape[2] * 16
     out = np.full(q.shape, np.nan)
-    spread, reach = np.zeros(q.shape), np.zeros((n_rows, heads, 1))
+    spread, reach, span = np.zeros(q.shape), np.zeros((n_rows, heads, 1)), np.zeros(q.shape)
     where = places(lengths, row_start, n_rows)
     kept = {}
     for i, at in enumerate(where):
@@ -108,7 +115,7 @@ def attend(q, pages, table, lengths, row_start, scale):
             c = h // (heads // kv_heads)
             if (seq, c) not in kept:
                 kept[seq, c] = context(pages, table, seq, min(lengths[seq], table.shape[1] * page_size), page_size, c)
-            k, v, there = kept[seq, c]
+            k, v, there, wide = kept[seq, c]
             see = there & (np.arange(len(there)) <= pos)
             if not see.any():
                 out[i, h] = 0
@@ -118,5 +125,6 @@ def attend(q, pages, table, lengths, row_start, scale):
             p /= p.sum()
             out[i, h] = p @ v[see]
             spread[i, h] = p @ np.abs(v[see])
+            span[i, h] = p @ wide[see]
             reach[i, h] = (np.abs(k[see]) @ np.abs(q[i, h])).max() * abs(scale)
-    return out, spread, reach
+    return out, spread, reach, span

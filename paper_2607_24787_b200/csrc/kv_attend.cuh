@@ -6,10 +6,10 @@
 // their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries are split into three bf16
 // parts and probabilities into two.
 // Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
-// bf16 calls of one eight of columns leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is
-// what the group's sum starts with. Values: the probability is scaled up, and one more product with -8 in the codes' place goes into the
-// running sum before theirs, so that what is left to round is a tile's and not the whole context's sum of codes. Other calls subtract the
-// 8 from each code, nine instructions for eight, which the columns then share.
+// bf16 calls leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is what the group's sum starts
+// with. Values: the probability is scaled up, and one more product with -8 in the codes' place goes into the running sum before theirs, so
+// that what is left to round is a tile's and not the whole context's sum of codes. fp32 calls subtract the 8 from each code, nine
+// instructions for eight, and lose nothing to it.
 //
 // All (sequence, columns, head) items together are a line of tiles of 32 tokens that is cut evenly between CTAs, and a CTA's piece
 // evenly between its warps, whatever the lengths are: a warp walks its tiles with the running maximum and sum of each column, fed by its
@@ -36,23 +36,21 @@ struct AttendArgs {
     int once;                   // every block is read by one warp alone
 };
 
-#ifndef AT_W
-#define AT_W 16
-#endif
 constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
+constexpr int kAtFewBlocks = 8; // column blocks of a sequence that a lane counts by itself
 constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
 
-template <typename T, int HD, int NT>
+template <typename T, int HD>
 struct AtShape {
-    static constexpr int cols = 8 * NT;
+    static constexpr int cols = 8;
     static constexpr int tile_bytes = kAtTile / kKvBlock * kv_block_bytes(HD);
     static constexpr int part_floats = cols * (HD + 2);      // sums, then maxima, then sums of probabilities
     static constexpr int part_bytes = (part_floats * 4 + 15) / 16 * 16;
     // warps and stages of a warp's ring: what registers (the sums of HD x cols numbers, the queries) and shared memory leave
-    static constexpr int warps = NT == 4 ? (HD == 64 ? 8 : 6) : NT == 2 ? (HD == 64 ? 12 : HD == 128 ? 8 : 6) : HD == 256 ? 8 : sizeof(T) == 4 ? 12 : AT_W;
-    static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : NT == 4 ? 4 : 3;
-    static constexpr bool raw = sizeof(T) == 2 && NT == 1;              // codes as they are masked out
+    static constexpr int warps = HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
+    static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : 3;
+    static constexpr bool raw = sizeof(T) == 2;              // codes as they are masked out
     static constexpr float up = raw ? 64.f : 0.f;                       // probabilities are taken to 2^64 then
     static constexpr float unscale = raw ? 0x1p69f : kQ4ExactUnscale;   // of sums of codes times probabilities
     // a sum of an odd element, beside that of the even one before it
@@ -83,21 +81,39 @@ struct Walk {
         nk = max(0, min(len - n + last + 1, a.batch.stride * a.kv.page_size));
         nt = max(1, (nk + kAtTile - 1) / kAtTile);
     }
-    __device__ __forceinline__ int tiles_of_sequence(const AttendArgs& a) {
+    // tiles of all heads of column blocks `from`, `from` + `step`, ...
+    __device__ __forceinline__ int tiles_of_sequence(const AttendArgs& a, int from, int step) {
         int sum = 0;
         const int m = blocks(a);
-        for (ct = 0; ct < m; ++ct) { columns(a); sum += nt; }
+        for (ct = from; ct < m; ct += step) { columns(a); sum += nt; }
         return sum * a.kv.heads;
     }
-    // to tile `rest` of sequence `s`
+    // to tile `rest` of sequence `s`, by a warp: lanes look at 32 column blocks at a time
     __device__ __forceinline__ void seek(const AttendArgs& a, int s, int rest) {
+        const int lane = threadIdx.x & 31;
         seq = s;
         load(a);
-        for (ct = 0;; ++ct) {
+        const int m = blocks(a);
+        for (int ct0 = 0; m > 1; ct0 += 32) {
+            ct = ct0 + lane;
             columns(a);
-            if (rest < nt * a.kv.heads) break;
-            rest -= nt * a.kv.heads;
+            const int own = ct < m ? nt * a.kv.heads : 0;
+            int upto = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const int behind = __popc(__ballot_sync(0xffffffffu, upto <= rest));
+            if (behind < 32) {
+                rest -= __shfl_sync(0xffffffffu, upto - own, behind);
+                ct = ct0 + behind;
+                break;
+            }
+            rest -= __shfl_sync(0xffffffffu, upto, 31);
         }
+        if (m <= 1) ct = 0;
+        columns(a);
         head = rest / nt;
         t = rest - head * nt;
     }
@@ -188,9 +204,9 @@ __device__ __forceinline__ void query_words(uint32_t (&w)[3][4], bool flip) {   
     }
 }
 
-template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_kernel(const AttendArgs a) {
-    using S = AtShape<T, HD, NT>;
+template <typename T, int HD>
+__global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kernel(const AttendArgs a) {
+    using S = AtShape<T, HD>;
     constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
     constexpr bool RAW = S::raw;
     constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 2 : 1;        // parts of a query, of a probability
@@ -221,10 +237,23 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
         w.seq = s;
         w.load(a);
         if (w.n > 0 && w.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-        return w.tiles_of_sequence(a);
+        return w.blocks(a) <= kAtFewBlocks ? w.tiles_of_sequence(a, 0, 1) : -1;
+    };
+    // sequences of many column blocks: their lanes' counts come back as -1, and the warp counts together
+    auto count_many = [&](int k, int s) {
+        for (uint32_t left = __ballot_sync(0xffffffffu, k < 0); left; left &= left - 1) {
+            const int owner = __ffs(left) - 1;
+            Walk<COLS> w;
+            w.seq = __shfl_sync(0xffffffffu, s, owner);
+            w.load(a);
+            const int sum = __reduce_add_sync(0xffffffffu, w.tiles_of_sequence(a, lane, 32));
+            if (lane == owner) k = sum;
+        }
+        return k;
     };
     if (n_seq <= 64) {
-        const int k0 = 2 * lane < n_seq ? count_tiles(2 * lane) : 0, k1 = 2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0;
+        const int k0 = count_many(2 * lane < n_seq ? count_tiles(2 * lane) : 0, 2 * lane);
+        const int k1 = count_many(2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0, 2 * lane + 1);
         int upto = k0 + k1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -239,9 +268,9 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
         int mine = 0;
         for (int i = 0; i < each; ++i) {
             const int s = tid * each + i;
-            if (s >= n_seq) break;
-            before[s] = mine;
-            mine += count_tiles(s);
+            const int k = count_many(s < n_seq ? count_tiles(s) : 0, s);
+            if (s < n_seq) before[s] = mine;
+            mine += k;
         }
         int upto = mine;
 #pragma unroll
@@ -270,8 +299,8 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
     const int hi = cta_lo + int(static_cast<long long>(cta_hi - cta_lo) * (warp + 1) / W);
     const int count = hi - lo;
 
-    float m[NT][2], l[NT][2], y[NT][G][2][4];
-    uint32_t qf[NT][QP][G][4];
+    float m[2], l[2], y[G][2][4];
+    uint32_t qf[QP][G][4];
     if (count > 0) {
         {
             Walk<COLS> at;
@@ -291,23 +320,20 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             __syncwarp();
         }
         const Walk<COLS>& use = used[warp];
-        int t = use.t, nt_left = use.nt - t;     // tile of its item, tiles left there
+        int t = use.t, left_there = use.nt - t;     // tile of its item, tiles left there
         // an item's queries, as they are in memory
         auto fetch = [&] {
+            int g;
+            const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, r, g);
+            const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                int g;
-                const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + r, g);
-                const T* p = static_cast<const T*>(a.q.p) + row * a.q.row + (use.head * a.group + g) * a.q.head + 8 * c;
+            for (int k = 0; k < G; ++k)
 #pragma unroll
-                for (int k = 0; k < G; ++k)
-#pragma unroll
-                    for (int q = 0; q < (QP + 1) / 2; ++q) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (row >= 0) v = *reinterpret_cast<const uint4*>(p + 32 * k + 4 * q);
-                        qf[nt][q][k][0] = v.x; qf[nt][q][k][1] = v.y; qf[nt][q][k][2] = v.z; qf[nt][q][k][3] = v.w;
-                    }
-            }
+                for (int q = 0; q < (QP + 1) / 2; ++q) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (row >= 0) v = *reinterpret_cast<const uint4*>(p + 32 * k + 4 * q);
+                    qf[q][k][0] = v.x; qf[q][k][1] = v.y; qf[q][k][2] = v.z; qf[q][k][3] = v.w;
+                }
         };
         fetch();
         // ---- copies: lanes 0 and 1 walk ahead and look up a block's page each, a tile before its use. A page of an even number of
@@ -374,41 +400,38 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
         int began = 0;                           // the item's tile with which this warp's part of it begins
         auto begin = [&] {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int k = 0; k < G; ++k) {
+                uint32_t w[QP][4];
 #pragma unroll
-                for (int k = 0; k < G; ++k) {
-                    uint32_t w[QP][4];
+                for (int q = 0; q < QP; ++q)
 #pragma unroll
-                    for (int q = 0; q < QP; ++q)
+                    for (int j = 0; j < 4; ++j) w[q][j] = qf[q][k][j];
+                query_words<RAW>(w, flip);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[q][j] = qf[nt][q][k][j];
-                    query_words<RAW>(w, flip);
+                for (int q = 0; q < QP; ++q)
 #pragma unroll
-                    for (int q = 0; q < QP; ++q)
+                    for (int j = 0; j < 4; ++j) qf[q][k][j] = w[q][j];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) qf[nt][q][k][j] = w[q][j];
+                for (int j = 0; j < 4; ++j) y[k][0][j] = y[k][1][j] = 0.f;
+                if constexpr (RAW) {
+                    float sum = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) y[nt][k][0][j] = y[nt][k][1][j] = 0.f;
-                    if constexpr (RAW) {
-                        float sum = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float x0, x1;
-                            two_bf16(w[0][j], x0, x1);
-                            sum += (x0 + x1) * (j & 1 ? 16.f : 1.f);
-                        }
-                        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                        sum *= -8.f * 0x1p-133f;       // to where a code's 1 stands
-                        if (c == 0) {
-                            float* to = reinterpret_cast<float*>(&starts[warp][k][r / 2]) + r % 2;
-                            to[0] = to[2] = sum;
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        float x0, x1;
+                        two_bf16(w[0][j], x0, x1);
+                        sum += (x0 + x1) * (j & 1 ? 16.f : 1.f);
+                    }
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                    sum *= -8.f * 0x1p-133f;       // to where a code's 1 stands
+                    if (c == 0) {
+                        float* to = reinterpret_cast<float*>(&starts[warp][k][r / 2]) + r % 2;
+                        to[0] = to[2] = sum;
                     }
                 }
-                m[nt][0] = m[nt][1] = -INFINITY;
-                l[nt][0] = l[nt][1] = 0.f;
             }
+            m[0] = m[1] = -INFINITY;
+            l[0] = l[1] = 0.f;
             if constexpr (RAW) __syncwarp();
             began = t;
             whole_tiles = min(use.nk, use.len - use.n + use.ct * COLS / a.group + 1) / kAtTile;
@@ -424,7 +447,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             }
             const uint32_t at = ring_at + stage * S::tile_bytes, have = present >> (2 * stage) & 3;
             // ---- scores: tokens r, r + 8 of each block for columns 2 c, 2 c + 1 ----
-            float s[NT][2][4];
+            float s[2][4];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const uint32_t block = at + b * BB;
@@ -432,28 +455,23 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                 token_scales<G>(block + kv_k_scales(HD) + r * (2 * G), s0);
                 token_scales<G>(block + kv_k_scales(HD) + (r + 8) * (2 * G), s1);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[nt][b][j] = 0.f;
+                for (int j = 0; j < 4; ++j) s[b][j] = 0.f;
 #pragma unroll
                 for (int k = 0; k < G; k += 2) {
                     const uint4 w = ldsm4(block + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const Nib4 u = RAW ? q4_unpack(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_unpack(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
+                        float d[4];
+                        if constexpr (RAW) mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
+                        else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float d[4];
-                            if constexpr (RAW) mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
-                            else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][0][k + h][0], qf[nt][0][k + h][1]);
-#pragma unroll
-                            for (int q = 0; q < QP; ++q) {
-                                if (q > 0) mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[nt][q][k + h][0], qf[nt][q][k + h][1]);
-                                mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[nt][q][k + h][2], qf[nt][q][k + h][3]);
-                            }
-                            s[nt][b][0] += s0[k + h] * d[0]; s[nt][b][1] += s0[k + h] * d[1];
-                            s[nt][b][2] += s1[k + h] * d[2]; s[nt][b][3] += s1[k + h] * d[3];
+                        for (int q = 0; q < QP; ++q) {
+                            if (q > 0) mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[q][k + h][0], qf[q][k + h][1]);
+                            mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[q][k + h][2], qf[q][k + h][3]);
                         }
+                        s[b][0] += s0[k + h] * d[0]; s[b][1] += s0[k + h] * d[1];
+                        s[b][2] += s1[k + h] * d[2]; s[b][3] += s1[k + h] * d[3];
                     }
                 }
             }
@@ -461,58 +479,50 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             const bool whole = have == 3 && t < whole_tiles;
             if (!whole) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int i2 = (use.ct * COLS + 8 * nt + 2 * c + e) / a.group;
-                        const int sees = min(use.nk, use.len - use.n + i2 + 1) - t * kAtTile;      // tokens of this tile
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                if (!(have >> b & 1) || 16 * b + 8 * j + r >= sees) s[nt][b][2 * j + e] = -INFINITY;
-                    }
-            }
-            // ---- running maximum: moved only where a score is above it by a factor of 2^6 ----
-            bool raise = false;
-            float top[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float v = fmaxf(fmaxf(s[nt][0][e], s[nt][0][2 + e]), fmaxf(s[nt][1][e], s[nt][1][2 + e]));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-                    top[nt][e] = v;
-                    raise |= v > m[nt][e] + slack;         // (-infinity is not above -infinity)
-                }
-            if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float to = fmaxf(m[nt][e], top[nt][e]), by = to == -INFINITY ? 1.f : ex2((m[nt][e] - to) * f);
-                        m[nt][e] = to;
-                        l[nt][e] *= by;
-#pragma unroll
-                        for (int k = 0; k < G; ++k) { y[nt][k][0][e] *= by; y[nt][k][0][2 + e] *= by; y[nt][k][1][e] *= by; y[nt][k][1][2 + e] *= by; }
-                    }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float base = (m[nt][e] == -INFINITY ? 0.f : m[nt][e] * -f) + S::up;
+                    const int i2 = (use.ct * COLS + 2 * c + e) / a.group;
+                    const int sees = min(use.nk, use.len - use.n + i2 + 1) - t * kAtTile;      // tokens of this tile
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float p = ex2(fmaf(s[nt][b][2 * j + e], f, base));
-                            s[nt][b][2 * j + e] = p;
-                            l[nt][e] += p;
-                        }
+                        for (int j = 0; j < 2; ++j)
+                            if (!(have >> b & 1) || 16 * b + 8 * j + r >= sees) s[b][2 * j + e] = -INFINITY;
                 }
+            }
+            // ---- running maximum: moved only where a score is above it by a factor of 2^6 ----
+            bool raise = false;
+            float top[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v = fmaxf(fmaxf(s[0][e], s[0][2 + e]), fmaxf(s[1][e], s[1][2 + e]));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+                top[e] = v;
+                raise |= v > m[e] + slack;         // (-infinity is not above -infinity)
+            }
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f);
+                    m[e] = to;
+                    l[e] *= by;
+#pragma unroll
+                    for (int k = 0; k < G; ++k) { y[k][0][e] *= by; y[k][0][2 + e] *= by; y[k][1][e] *= by; y[k][1][2 + e] *= by; }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f) + S::up;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float p = ex2(fmaf(s[b][2 * j + e], f, base));
+                        s[b][2 * j + e] = p;
+                        l[e] += p;
+                    }
+            }
             // ---- y += V^T p, the values' scales on p ----
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -533,25 +543,22 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const Nib4 u = RAW ? q4_bytes(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_bytes(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
+                        float p0 = s[b][0] * s0[k + h], p1 = s[b][1] * s0[k + h], p2 = s[b][2] * s1[k + h], p3 = s[b][3] * s1[k + h];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float p0 = s[nt][b][0] * s0[k + h], p1 = s[nt][b][1] * s0[k + h], p2 = s[nt][b][2] * s1[k + h], p3 = s[nt][b][3] * s1[k + h];
-#pragma unroll
-                            for (int q = 0; q < PP; ++q) {
-                                const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3);
-                                if (q + 1 < PP) {
-                                    float x0, x1;
-                                    two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
-                                    two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
-                                }
-                                const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
-                                if constexpr (RAW) {
-                                    mma_k16(y[nt][k + h][0], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
-                                    mma_k16(y[nt][k + h][1], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
-                                }
-                                mma_k16(y[nt][k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
-                                mma_k16(y[nt][k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+                        for (int q = 0; q < PP; ++q) {
+                            const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3);
+                            if (q + 1 < PP) {
+                                float x0, x1;
+                                two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
+                                two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
                             }
+                            const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
+                            if constexpr (RAW) {
+                                mma_k16(y[k + h][0], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
+                                mma_k16(y[k + h][1], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
+                            }
+                            mma_k16(y[k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                            mma_k16(y[k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
                         }
                     }
                 }
@@ -561,54 +568,48 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
 
             // ---- the item ends, or the warp's piece ----
-            const bool ends = nt_left == 1;
+            const bool ends = left_there == 1;
             if (ends || i + 1 == count) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float v = l[nt][e];
-                        v += __shfl_xor_sync(0xffffffffu, v, 4);
-                        v += __shfl_xor_sync(0xffffffffu, v, 8);
-                        v += __shfl_xor_sync(0xffffffffu, v, 16);
-                        l[nt][e] = RAW ? v * 0x1p-64f : v;
-                    }
+                for (int e = 0; e < 2; ++e) {
+                    float v = l[e];
+                    v += __shfl_xor_sync(0xffffffffu, v, 4);
+                    v += __shfl_xor_sync(0xffffffffu, v, 8);
+                    v += __shfl_xor_sync(0xffffffffu, v, 16);
+                    l[e] = RAW ? v * 0x1p-64f : v;
+                }
                 if (ends && began == 0) {        // all of it is this warp's
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int e = 0; e < 2; ++e) {
+                        int g;
+                        const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 2 * c + e, g);
+                        if (row < 0) continue;
+                        const float by = l[e] > 0.f ? S::unscale / l[e] : 0.f;
+                        T* p = static_cast<T*>(a.out.p) + row * a.out.row + (use.head * a.group + g) * a.out.head + 4 * r;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            int g;
-                            const int row = row_of_column<COLS>(a, use.first, use.n, use.ct, 8 * nt + 2 * c + e, g);
-                            if (row < 0) continue;
-                            const float by = l[nt][e] > 0.f ? S::unscale / l[nt][e] : 0.f;
-                            T* p = static_cast<T*>(a.out.p) + row * a.out.row + (use.head * a.group + g) * a.out.head + 4 * r;
-#pragma unroll
-                            for (int k = 0; k < G; ++k) {
-                                float o[4] = {y[nt][k][0][e] * by, S::odd(y[nt][k][0][2 + e], y[nt][k][0][e]) * by,
-                                              y[nt][k][1][e] * by, S::odd(y[nt][k][1][2 + e], y[nt][k][1][e]) * by};
-                                store_row<4>(p + 32 * k, o);
-                            }
+                        for (int k = 0; k < G; ++k) {
+                            float o[4] = {y[k][0][e] * by, S::odd(y[k][0][2 + e], y[k][0][e]) * by,
+                                          y[k][1][e] * by, S::odd(y[k][1][2 + e], y[k][1][e]) * by};
+                            store_row<4>(p + 32 * k, o);
                         }
+                    }
                 } else {
                     // an item that ends here began in another warp: the warp's first part. One that goes on is its last part, and the ring is free
                     float* part = ends ? own_part : reinterpret_cast<float*>(ring);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int e = 0; e < 2; ++e) {
+                        const int col = 2 * c + e;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int col = 8 * nt + 2 * c + e;
-#pragma unroll
-                            for (int k = 0; k < G; ++k)
-                                *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[nt][k][0][e], S::odd(y[nt][k][0][2 + e], y[nt][k][0][e]),
-                                                                                                           y[nt][k][1][e], S::odd(y[nt][k][1][2 + e], y[nt][k][1][e]));
-                            if (r == 0) { part[COLS * HD + col] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * f; part[COLS * HD + COLS + col] = l[nt][e]; }
-                        }
+                        for (int k = 0; k < G; ++k)
+                            *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[k][0][e], S::odd(y[k][0][2 + e], y[k][0][e]),
+                                                                                                       y[k][1][e], S::odd(y[k][1][2 + e], y[k][1][e]));
+                        if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f; part[COLS * HD + COLS + col] = l[e]; }
+                    }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - t, use.ct, use.head, began, t + 1, use.nt, use.first, use.n};
                 }
             }
             ++t;
-            if (--nt_left == 0 && i + 1 < count) {
+            if (--left_there == 0 && i + 1 < count) {
                 Walk<COLS> w = use;
                 w.t = w.nt - 1;
                 w.next(a);
@@ -616,7 +617,7 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
                 if (lane == 0) used[warp] = w;
                 __syncwarp();
                 t = 0;
-                nt_left = w.nt;
+                left_there = w.nt;
                 fetch();
                 begin();
             }
@@ -696,9 +697,9 @@ __global__ void __launch_bounds__(AtShape<T, HD, NT>::warps * 32, 1) kv_attend_k
 // Adds the parts of items that were cut between CTAs: block (x, column) takes the item that begins in CTA x and goes on behind it. Its
 // 256 threads take the parts in turn by HD-wide groups, eight parts at a time with their loads ahead of their use.
 constexpr int kAtJoinThreads = 256;
-template <typename T, int HD, int NT>
+template <typename T, int HD>
 __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const AttendArgs a) {
-    using S = AtShape<T, HD, NT>;
+    using S = AtShape<T, HD>;
     constexpr int COLS = S::cols, FLOATS = S::part_floats, SETS = kAtJoinThreads / HD;
     __shared__ float tops[SETS], sums[SETS], rows[SETS][HD];
     grid_dep_wait();

@@ -109,22 +109,7 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
     return launched(call);
 }
 
-// Columns of an item in eights: as few as hold a sequence's new rows, as many as registers allow (fp32 queries take three times those
-// of bf16 ones, sums of wide heads twice those of 128)
-int attend_eights(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
-    const long long rows = !b->row_start ? 1 : b->max_rows ? b->max_rows : (b->n_rows + b->n_seq - 1) / std::max(b->n_seq, 1);
-    const long long cols = rows * (n_q_heads / kv->n_kv_heads);
-    const int most = dtype == SPM_DTYPE_BF16 ? (kv->head_dim == 256 ? 2 : 4) : (kv->head_dim == 256 ? 1 : 2);
-    return cols <= 8 ? 1 : cols <= 16 ? std::min(2, most) : most;
-}
-template <typename F>
-void by_eights(int n, F f) {
-    if (n == 1) f(std::integral_constant<int, 1>{});
-    else if (n == 2) f(std::integral_constant<int, 2>{});
-    else f(std::integral_constant<int, 4>{});
-}
-constexpr size_t attend_part_bytes(int hd, int eights) { return size_t(8 * eights) * (hd + 2) * 4; }
-size_t attend_bytes(int hd, int eights) { return kAtMaxCtas * (32 + 2 * attend_part_bytes(hd, eights)); }
+size_t attend_bytes(int hd) { return kAtMaxCtas * (32 + 2 * size_t(8) * (hd + 2) * 4); }
 
 constexpr int kMaxDevices = 64;
 // Once a kernel and device: shared memory beyond 48 KB
@@ -137,13 +122,13 @@ cudaError_t allow_smem(int dev, int bytes) {
     return e;
 }
 
-template <typename T, int HD, int NT>
+template <typename T, int HD>
 cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st) {
-    using S = AtShape<T, HD, NT>;
-    cudaError_t e = allow_smem<kv_attend_kernel<T, HD, NT>>(dev, S::smem(SPM_KV_MAX_SEQS));
+    using S = AtShape<T, HD>;
+    cudaError_t e = allow_smem<kv_attend_kernel<T, HD>>(dev, S::smem(SPM_KV_MAX_SEQS));
     if (e != cudaSuccess) return e;
     const int ctas = std::min(sms, kAtMaxCtas);
-    kv_attend_kernel<T, HD, NT><<<ctas, S::warps * 32, S::smem(a.batch.n_seq), st>>>(a);
+    kv_attend_kernel<T, HD><<<ctas, S::warps * 32, S::smem(a.batch.n_seq), st>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     // launched ahead of the first kernel's end, which it waits for: its blocks are in place when the parts are
@@ -156,7 +141,7 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD, NT>, a);
+    return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD>, a);
 }
 
 }  // namespace
@@ -243,7 +228,7 @@ int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, i
     if (int rc = check_cache_shape(call, kv)) return rc;
     if (int rc = check_batch(call, kv, batch)) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
-    *bytes = attend_bytes(kv->head_dim, attend_eights(kv, batch, n_q_heads, dtype));
+    *bytes = attend_bytes(kv->head_dim);
     return SPM_OK;
 }
 
@@ -257,9 +242,8 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     if (int rc = check_rows(call, "q", q, dtype)) return rc;
     if (int rc = check_rows(call, "out", out, dtype)) return rc;
-    const int eights = attend_eights(kv, batch, n_q_heads, dtype);
-    if (!workspace || !aligned(workspace, 16) || workspace_bytes < attend_bytes(kv->head_dim, eights))
-        return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(attend_bytes(kv->head_dim, eights)) + " bytes");
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < attend_bytes(kv->head_dim))
+        return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(attend_bytes(kv->head_dim)) + " bytes");
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -275,19 +259,14 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     for (int i = 0; i < 16; ++i)
         if (per_page == 1 << i) a.page_shift = i;
     // (a guess where max_rows is one: it only says what to keep in L2)
-    a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8 * eights);
+    a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8);
     a.scale = scale;
     a.joins = static_cast<int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
     by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
-        by_eights(eights, [&](auto n) {
-            constexpr int most = sizeof(T) == 2 ? (size.value == 256 ? 2 : 4) : (size.value == 256 ? 1 : 2);
-            if constexpr (n.value <= most) {
-                a.min_tiles = AtShape<T, size.value, n.value>::warps;
-                e = launch_attend<T, size.value, n.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
-            }
-        });
+        a.min_tiles = AtShape<T, size.value>::warps;
+        e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
     });
     return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
 }

@@ -259,23 +259,30 @@ def test_read(kv, hd, hk, page, dtype):
 # fp32 calls: products of split operands are short of 2^-17 of a probability times a value, and the sums of a few hundred terms add a
 # rounding each at worst; a score is off by a few roundings of its terms' sum, which moves a probability by as much. bf16 calls round a
 # probability, a value and the result once, and a key once (with many rows), which moves a score by a rounding of its terms' sum.
-def attend_tolerance(want, spread, reach, dtype):
+# On top, for both: products are summed in fp32 with codes of up to 15 (or both nibbles of a byte, up to 255) less 8 (136) times the
+# probability and scale, where an element may be nearly zero. Two products for every 16 tokens and a few joins go into a sum, each leaves
+# at most 2^-23 (a truncated fp32 sum) of the largest: 15 / 8, or 255 / (16 * 8) = 2 times the sum of p 8 |scale|.
+SUMS = 2 * 2 ** -23
+
+
+def attend_tolerance(want, spread, reach, span, dtype, tokens):
+    sums = SUMS * (2 * (tokens + 15) // 16 + 8) * span
     if dtype is FP32:
-        return (2.0 ** -17 + 300 * HALF[FP32] + 2 * 40 * HALF[FP32] * (1 + reach)) * spread + 1e-30
-    return HALF[BF16] * np.abs(want) + (2 * HALF[BF16] + 2 * HALF[BF16] * reach) * spread + 1e-30
+        return (2.0 ** -17 + 300 * HALF[FP32] + 2 * 40 * HALF[FP32] * (1 + reach)) * spread + sums + 1e-30
+    return HALF[BF16] * np.abs(want) + (2 * HALF[BF16] + 2 * HALF[BF16] * reach) * spread + sums + 1e-30
 
 
 def check_attend(c, heads, scale=None, q=None):
     q = c.randn(c.n_rows, heads, c.hd) if q is None else q
     out = torch.full_like(q, 9.0)
     c.cache.attend(c.batch, q, scale, out=out)
-    want, spread, reach = R.attend(q.double().cpu().numpy(), c.start, c.table.numpy(), c.lengths, c.row_start,
+    want, spread, reach, span = R.attend(q.double().cpu().numpy(), c.start, c.table.numpy(), c.lengths, c.row_start,
                                    c.hd ** -0.5 if scale is None else scale)
     got = out.double().cpu().numpy()
     n = c.row_start[-1]
     assert (got[n:] == 9).all()
     off = np.abs(got[:n] - want[:n])
-    tol = attend_tolerance(want, spread, reach, c.dtype)[:n]
+    tol = attend_tolerance(want, spread, reach, span, c.dtype, max(c.lengths))[:n]
     assert (off <= tol).all(), (off.max(), np.unravel_index((off - tol).argmax(), off.shape))
     # the 2-norm is far below what single elements may be off
     norm = np.linalg.norm(want[:n])
@@ -387,8 +394,8 @@ def test_steps_as_a_decoder_takes_them(kv):
         turned = cache.write(batch, k, v, q=q, positions=pos.cuda(), rope=rope)
         out = cache.attend(batch, turned)
         edges = np.cumsum([0] + rows)
-        want, spread, reach = R.attend(plain(q, pos, 0), cache.pages.cpu().numpy(), table.numpy(), lengths.tolist(), edges, hd ** -0.5)
-        assert (np.abs(out.double().cpu().numpy() - want) <= attend_tolerance(want, spread, reach, FP32)).all(), step
+        want, spread, reach, span = R.attend(plain(q, pos, 0), cache.pages.cpu().numpy(), table.numpy(), lengths.tolist(), edges, hd ** -0.5)
+        assert (np.abs(out.double().cpu().numpy() - want) <= attend_tolerance(want, spread, reach, span, FP32, 64)).all(), step
         lengths += 1
 
 
