@@ -77,7 +77,7 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D[tmem] (+)= A[tmem] * B[smem desc]: the A operand (128 rows = lanes, 16 bf16 = 8 columns) comes from tensor memory
-__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t"
         ".reg .pred p;\n\t"
@@ -242,8 +242,8 @@ ffn_grouped_q4_kernel(const __grid_constant__ CUtensorMap nib64, const __grid_co
 #pragma unroll
                         for (int ks = 0; ks < 4; ++ks) {
                             const uint64_t bx = smem_desc_sw128(xb + ks * 32, 16, 1024);
-                            tc_mma_bf16_ts(acc, at + ks * 8, bx, idesc1, (kb | ks) != 0);
-                            tc_mma_bf16_ts(acc + 64, at + 32 + ks * 8, bx, idesc1, (kb | ks) != 0);
+                            tc_mma_f16_ts(acc, at + ks * 8, bx, idesc1, (kb | ks) != 0);
+                            tc_mma_f16_ts(acc + 64, at + 32 + ks * 8, bx, idesc1, (kb | ks) != 0);
                         }
                         tc_commit(smem_u32(tempty + s));
                         tc_commit(smem_u32(xempty + xs));
@@ -271,7 +271,7 @@ ffn_grouped_q4_kernel(const __grid_constant__ CUtensorMap nib64, const __grid_co
                         for (int ks = 0; ks < 8; ++ks) {
                             const uint64_t da = smem_desc_sw128(base + ks * 2048, kGgTileBytes, 1024);
                             const uint64_t db = smem_desc_sw128(act_addr + ks * 2048, kGgActBytes, 1024);
-                            tc_mma_bf16(tmem + 256 + 64 * b, da, db, idesc2, ks != 0);
+                            tc_mma_f16(tmem + 256 + 64 * b, da, db, idesc2, ks != 0);
                         }
                         tc_commit(smem_u32(mempty + s));
                         tc_commit(smem_u32(acc2_full + b));

@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include "kv_attend.cuh"
+#include "kv_prefill.cuh"
 #include "kv_write.cuh"
 
 namespace spm {
@@ -144,6 +145,23 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD>, a);
 }
 
+// Whether a call's rows are enough for the tensor-core kernel
+bool prefill_pays(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
+    if (dtype != SPM_DTYPE_BF16 || kv->head_dim > 128 || !b->row_start) return false;
+    const long long rows = b->max_rows ? b->max_rows : (b->n_rows + b->n_seq - 1) / std::max(b->n_seq, 1);
+    return rows * (n_q_heads / kv->n_kv_heads) >= kPfPays;
+}
+template <int HD>
+cudaError_t launch_prefill(const AttendArgs& a, int dev, cudaStream_t st) {
+    const cudaError_t e = allow_smem<kv_prefill_kernel<HD>>(dev, PfShape<HD>::smem);
+    if (e != cudaSuccess) return e;
+    // as many CTAs as there can be items: full ones of all rows, and one a sequence that is not full
+    const long long items = (static_cast<long long>(a.batch.n_rows) * a.group / kPfCols + a.batch.n_seq) * a.kv.heads;
+    if (items > INT32_MAX) return cudaErrorInvalidValue;
+    kv_prefill_kernel<HD><<<unsigned(items), kPfThreads, PfShape<HD>::smem, st>>>(a);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 extern "C" {
@@ -263,7 +281,9 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.scale = scale;
     a.joins = static_cast<int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
-    by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
+    if (prefill_pays(kv, batch, n_q_heads, dtype))
+        e = kv->head_dim == 64 ? launch_prefill<64>(a, dev, static_cast<cudaStream_t>(stream)) : launch_prefill<128>(a, dev, static_cast<cudaStream_t>(stream));
+    else by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
         a.min_tiles = AtShape<T, size.value>::warps;
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));

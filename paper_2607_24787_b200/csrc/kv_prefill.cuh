@@ -1,0 +1,485 @@
+// Attention of many bf16 rows a sequence (prompts) over the 4-bit cache, on tcgen05.
+//
+// A CTA takes 256 columns (column x: head x % group of row x / group) of one cache head, two M = 128 halves, and walks the tokens in tiles
+// of 128. Four warps bring a tile's codes to fp16 operands in shared memory, once for both halves; one warp issues the products; four
+// warps a half turn scores into probabilities, one row a thread, while the tensor cores are at the other half: S(j) of one half, then
+// P V(j) and S(j + 1) of the other. Scores, probabilities (fp16, in the scores' place, as the A operand of the second product) and sums
+// stay in tensor memory: 2 x 128 + 2 x HD columns.
+//
+// fp16 and not bf16 operands, since a bf16 rounding of probabilities and values would each cost as much as that of the result. Ranges are
+// kept by powers of two, which round nothing: a row's queries are brought to [2^9, 2^10) by its largest, keys of a tile in which one would
+// not fit are taken times 2^-4, a probability times 2^8 (it is at most 2^6 above the running maximum, see below), and values times 2^-E, E from the largest scale so
+// far (a tile whose values would not fit raises E, and the sums so far are scaled down).
+//
+// Probabilities are taken against the running maximum of the tiles before; only where a score is above it by more than 2^6 is the tile
+// done again with the new one and the sums are scaled.
+#pragma once
+
+#include "kv_attend.cuh"
+#include "tc_ops.cuh"
+
+namespace spm {
+
+constexpr int kPfTile = 128;                     // tokens of a tile, rows of a half
+constexpr int kPfCols = 256;
+constexpr int kPfPays = 128;                     // columns of a sequence from which this kernel is taken
+// two halves' softmax warps, operand warps, the issuing warp and three that only make its four whole. Registers a thread: 128 at the launch,
+// of which the last two fours give some to the softmax warps (2 x 176 + 104 + 56 = 4 x 128).
+constexpr int kPfThreads = 16 * 32;
+constexpr int kPfSoftmaxRegs = 176, kPfOperandRegs = 104, kPfIssueRegs = 56;
+static_assert(2 * kPfSoftmaxRegs + kPfOperandRegs + kPfIssueRegs == 4 * 128, "the split is what the launch has");
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int HD>
+struct PfShape {
+    static constexpr int block_bytes = kPfTile * 128;                    // 64 elements of 128 rows
+    static constexpr int op_bytes = HD / 64 * block_bytes;               // one operand tile
+    static constexpr int smem = 6 * op_bytes + 1024;                     // queries of two halves, two stages of keys and values
+};
+
+// A in tensor memory
+__device__ __forceinline__ void pf_mma_ts(uint32_t d, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "}\n"
+        ::"r"(d), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// fp16 x fp16 -> fp32, M = 128
+__host__ __device__ constexpr uint32_t pf_idesc(int n, bool b_mn_major) {
+    return (1u << 4) | (uint32_t(b_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+}
+#define PF_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define PF_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : PF_R8(r, 0), PF_R8(r, 8), PF_R8(r, 16), PF_R8(r, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::PF_W8(r, 0), PF_W8(r, 8), PF_W8(r, 16), PF_W8(r, 24), "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
+__device__ __forceinline__ uint32_t bits_of(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ uint32_t pack_half(float a, float b) { return bits_of(__floats2half2_rn(a, b)); }
+
+// Eight codes of a word as fp16 elements times a scale, in the order (0, 4, 1, 5, 2, 6, 3, 7): 1024 + q (low nibbles of the masked halves)
+// less 1032, 1024 + 16 q over 16 less 72, both exact, then one rounding
+__device__ __forceinline__ uint4 pf_expand(uint32_t w, __half2 s) {
+    const __half2 off = as_half2(0xe408e408u), sixteenth = as_half2(0x2c002c00u), off72 = as_half2(0xd480d480u);       // -1032, 1 / 16, -72
+    const uint32_t h = w >> 8;
+    return make_uint4(bits_of(__hmul2(__hadd2(as_half2((w & 0x000f000fu) | 0x64006400u), off), s)),
+                      bits_of(__hmul2(__hfma2(as_half2((w & 0x00f000f0u) | 0x64006400u), sixteenth, off72), s)),
+                      bits_of(__hmul2(__hadd2(as_half2((h & 0x000f000fu) | 0x64006400u), off), s)),
+                      bits_of(__hmul2(__hfma2(as_half2((h & 0x00f000f0u) | 0x64006400u), sixteenth, off72), s)));
+}
+__device__ __forceinline__ void st_shared16(uint32_t at, const uint4& v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
+__device__ __forceinline__ uint32_t pf_chunk(int row, int ch) { return uint32_t((ch >> 3) * (kPfTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)); }
+
+struct PfShared {
+    unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+    uint32_t tmem;
+    int quit;                                    // a wait has run out: everybody leaves
+    int exps[4];                                 // E of a tile, and whether its keys are times 2^-4 (bit 16)
+    int widest[4];                               // largest scale of a tile's values, and of its keys, as fp16 bits
+    int widest_key[4];
+    uint32_t there[4][4];                        // which tokens of a tile exist
+};
+
+template <int HD>
+__global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendArgs a) {
+    using S = PfShape<HD>;
+    constexpr int G = HD / 32;
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~uintptr_t(1023));
+    const uint32_t base = smem_u32(smem), q_at = base, k_at = base + 2 * S::op_bytes, v_at = base + 4 * S::op_bytes;
+    __shared__ PfShared sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const KvBatch& b = a.batch;
+
+    // ---- which item: sequences one after another, a sequence's last (longest) columns first, heads together ----
+    const int head = blockIdx.x % a.kv.heads;
+    int block = blockIdx.x / a.kv.heads, seq = 0, first = 0, n = 0, blocks = 0;
+    for (int s0 = 0; s0 < b.n_seq; s0 += 32) {   // (every warp for itself)
+        const int s = s0 + lane;
+        int f = s, m = s < b.n_seq ? 1 : 0;
+        if (b.row_start && s < b.n_seq) {
+            f = b.row_start[s];
+            m = min(b.row_start[s + 1] - f, b.n_rows);
+        }
+        const int own = m > 0 ? int((static_cast<long long>(m) * a.group + kPfCols - 1) / kPfCols) : 0;
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const int behind = __popc(__ballot_sync(0xffffffffu, upto <= block));
+        if (behind < 32) {
+            seq = s0 + behind;
+            block -= __shfl_sync(0xffffffffu, upto - own, behind);
+            blocks = __shfl_sync(0xffffffffu, own, behind);
+            first = __shfl_sync(0xffffffffu, f, behind);
+            n = __shfl_sync(0xffffffffu, m, behind);
+            break;
+        }
+        block -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (blocks == 0) return;                     // more CTAs than items
+    const int rb = blocks - 1 - block;
+    const int len = b.lengths[seq];
+    const int cap = b.stride * a.kv.page_size;
+    if (len > cap && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+    // tiles of a half: up to the token that its last row sees
+    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x / a.group) + 1, cap)); };
+    const bool used1 = rb * kPfCols + kPfTile < n * a.group;
+    const int tiles0 = (sees(rb * kPfCols + kPfTile - 1) + kPfTile - 1) / kPfTile;
+    const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kPfTile - 1) / kPfTile : 0;
+    const int tiles = max(tiles0, tiles1);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.k_full[i]), 128); mbar_init(smem_u32(&sh.v_full[i]), 128);
+            mbar_init(smem_u32(&sh.k_empty[i]), 1); mbar_init(smem_u32(&sh.v_empty[i]), 1);
+            mbar_init(smem_u32(&sh.s_full[i]), 1); mbar_init(smem_u32(&sh.p_full[i]), 128); mbar_init(smem_u32(&sh.o_full[i]), 1);
+        }
+        sh.quit = 0;
+        for (int i = 0; i < 4; ++i) sh.widest[i] = sh.widest_key[i] = 0;
+        fence_barrier_init();
+    }
+    if (warp == 12) tmem_alloc(smem_u32(&sh.tmem), 512);
+
+    auto wait = [&](const unsigned long long& bar, int parity) {
+        const uint32_t at = smem_u32(&bar);
+        if (mbar_try_wait(at, parity)) return true;
+        const unsigned long long t0 = global_timer_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 32; ++i)
+                if (mbar_try_wait(at, parity)) return true;
+            if (*reinterpret_cast<volatile int*>(&sh.quit)) return false;
+            if (global_timer_ns() - t0 > kAtWaitNs) {
+                *reinterpret_cast<volatile int*>(&sh.quit) = 1;
+                kv_note(a.kv, SPM_KV_TIMEOUT);
+                return false;
+            }
+        }
+    };
+
+    // ---- queries: a softmax thread brings its row ----
+    const int half = warp >> 2, row_in = tid & 127;             // (softmax warps: 0 - 3, 4 - 7)
+    int row = -1, g = 0, limit = 0;
+    float f = 1.f;
+    if (warp < 8) {
+        const int x = rb * kPfCols + tid, i = x / a.group;
+        g = x - i * a.group;
+        if (i < n && first + i >= 0 && first + i < b.n_rows) row = first + i;
+        limit = sees(x);
+        if (i >= n) limit = 0;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + row * a.q.row + (head * a.group + g) * a.q.head;
+        uint4 v[HD / 8];
+        uint32_t top = 0;                        // largest magnitude, as bf16 bits
+#pragma unroll
+        for (int ch = 0; ch < HD / 8; ++ch) {
+            v[ch] = row >= 0 ? *reinterpret_cast<const uint4*>(src + ch * 8) : make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {v[ch].x, v[ch].y, v[ch].z, v[ch].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, w[j] >> 16 & 0x7fffu));
+        }
+        // to [2^9, 2^10); what is not a number stays as it is
+        const int e = top == 0 || top >= 0x7f80u ? 0 : 9 - (int(top >> 7) - 127);
+        const float up = top < 0x80u ? 0x1p100f : exp2f(float(min(e, 120))), sign = a.scale < 0.f ? -up : up;
+        f = fmaxf(fabsf(a.scale), 1e-30f) * 1.4426950408889634f / up;
+#pragma unroll
+        for (int ch = 0; ch < HD / 8; ++ch) {
+            float q[8];
+            two_bf16(v[ch].x, q[0], q[1]); two_bf16(v[ch].y, q[2], q[3]); two_bf16(v[ch].z, q[4], q[5]); two_bf16(v[ch].w, q[6], q[7]);
+            st_shared16(q_at + half * S::op_bytes + pf_chunk(row_in, ch),
+                        make_uint4(pack_half(q[0] * sign, q[4] * sign), pack_half(q[1] * sign, q[5] * sign), pack_half(q[2] * sign, q[6] * sign), pack_half(q[3] * sign, q[7] * sign)));
+        }
+        fence_proxy_async();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem, t_s = tmem, t_o = tmem + 256;
+    const int own_tiles = half == 0 ? tiles0 : tiles1;
+
+    if (warp < 8) {
+        more_registers<kPfSoftmaxRegs>();
+        // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
+        const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
+        float m = -INFINITY, l = 0.f;
+        int e_now = 0;
+        bool ok = true;
+        for (int j = 0; j < own_tiles && ok; ++j) {
+            if (!(ok = wait(sh.s_full[half], j & 1))) break;
+            tc_fence_after();
+            const int packed = *reinterpret_cast<volatile int*>(&sh.exps[j & 3]), e = int(short(packed & 0xffff));
+            const float ft = packed >> 16 & 1 ? f * 16.f : f;
+            uint32_t there[4];
+            bool whole = (j + 1) * kPfTile <= limit;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                there[i] = *reinterpret_cast<volatile uint32_t*>(&sh.there[j & 3][i]);
+                whole &= there[i] == 0xffffffffu;
+            }
+            whole = __all_sync(0xffffffffu, whole);
+            if (!whole)                          // tokens that this row sees
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int left = limit - j * kPfTile - 32 * i;
+                    if (left < 32) there[i] &= left <= 0 ? 0u : (1u << left) - 1;
+                }
+            uint32_t p[64];
+            float top = -INFINITY, sum;
+            auto probabilities = [&] {
+                const float nb = 8.f - (m == -INFINITY ? 0.f : m);
+                sum = 0.f;
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) {
+                    uint32_t r[32];
+                    tmem_ld32(s_at + 32 * ch, r);
+                    tmem_wait_ld();
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(there[ch] >> i & 1)) r[i] = 0xff800000u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float x0 = __uint_as_float(r[i]), x1 = __uint_as_float(r[i + 1]);
+                        top = fmaxf(top, fmaxf(x0, x1));
+                        const float p0 = ex2(fmaf(x0, ft, nb)), p1 = ex2(fmaf(x1, ft, nb));
+                        sum += p0 + p1;
+                        p[ch * 16 + i / 2] = pack_half(p0, p1);
+                    }
+                }
+            };
+            probabilities();
+            const float peak = top * ft;         // m is kept as a power of two's exponent
+            const bool raise = peak > m + 6.f;
+            if (__any_sync(0xffffffffu, raise || e != e_now)) {
+                const float to = fmaxf(m, peak), by = m == -INFINITY ? 0.f : ex2(m - to);
+                m = to;
+                l *= by;
+                if (j > 0) {                     // (before that the sums hold nothing)
+                    const float scale = by * exp2f(float(e_now - e));
+#pragma unroll 1
+                    for (int ch = 0; ch < HD / 32; ++ch) {
+                        uint32_t r[32];
+                        tmem_ld32(o_at + 32 * ch, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * scale);
+                        tmem_st32(o_at + 32 * ch, r);
+                    }
+                    tmem_wait_st();
+                }
+                e_now = e;
+                probabilities();
+            }
+            l += sum;
+            {
+                uint32_t r[32];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = p[32 * h + i];
+                    tmem_st32(s_at + 32 * h, r);
+                }
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&sh.p_full[half]));
+        }
+        if (own_tiles > 0 && ok) ok = wait(sh.o_full[half], 0);
+        tc_fence_after();
+        if (ok) {
+            // values stand at 2^-E, probabilities and their sum at 2^8
+            const float by = l > 0.f ? exp2f(float(e_now)) / l : 0.f;
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + row * a.out.row + (head * a.group + g) * a.out.head;
+#pragma unroll 1
+            for (int ch = 0; ch < HD / 32; ++ch) {
+                uint32_t r[32];
+                if (own_tiles > 0) {
+                    tmem_ld32(o_at + 32 * ch, r);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = 0u;
+                }
+                if (row < 0) continue;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {                // (0, 4, 1, 5, 2, 6, 3, 7)
+                        y[k] = __uint_as_float(r[i + 2 * k]) * by;
+                        y[k + 4] = __uint_as_float(r[i + 2 * k + 1]) * by;
+                    }
+                    store_row<8>(to + 32 * ch + i, y);
+                }
+            }
+        }
+    } else if (warp < 12) {
+        fewer_registers<kPfOperandRegs>();
+        // ---- operands: a thread takes a token of each tile, its codes a tile ahead ----
+        const int t = tid - 256, w = warp - 8;
+        const int nk = max(sees(rb * kPfCols + kPfTile - 1), used1 ? sees(rb * kPfCols + kPfCols - 1) : 0);
+        uint4 kc[G], vc[G];
+        uint32_t ks[G / 2], vs[G / 2];
+        const unsigned char* at = nullptr;
+        bool exists = false;
+        auto locate = [&](int j) {
+            const int pos = j * kPfTile + t;
+            exists = false;
+            if (pos >= nk) return;
+            const long long block_at = kv_block_at<HD>(a.kv, b, seq, pos, head);
+            if (block_at < 0) { kv_note(a.kv, SPM_KV_BAD_PAGE); return; }
+            exists = true;
+            at = a.kv.pages + block_at + (pos % kKvBlock) * 16;
+        };
+        auto scales = [&](uint32_t (&s)[G / 2], int part) {
+            const unsigned char* p = at - (t % kKvBlock) * 16 + kv_k_scales(HD) + part * HD + (t % kKvBlock) * (2 * G);
+#pragma unroll
+            for (int i = 0; i < G / 2; ++i) s[i] = exists ? *reinterpret_cast<const uint32_t*>(p + 4 * i) : 0u;
+        };
+        auto codes = [&](uint4 (&x)[G], int part) {
+#pragma unroll
+            for (int k = 0; k < G; ++k) x[k] = exists ? *reinterpret_cast<const uint4*>(at + part * kv_v_codes(HD) + k * (kKvBlock * 16)) : make_uint4(0, 0, 0, 0);
+        };
+        auto expand = [&](uint32_t to, const uint4 (&x)[G], const uint32_t (&s)[G / 2], float by) {
+#pragma unroll
+            for (int k = 0; k < G; ++k) {
+                const float2 pair = __half22float2(as_half2(s[k / 2]));
+                const __half2 d = __float2half2_rn((k & 1 ? pair.y : pair.x) * by);
+                const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st_shared16(to + pf_chunk(t, 4 * k + i), pf_expand(word[i], d));
+            }
+        };
+        locate(0);
+        scales(ks, 0); scales(vs, 1);
+        codes(kc, 0); codes(vc, 1);
+        int e = -1000;
+        bool ok = true;                          // (a warp that has given up still comes to the others' barrier)
+        for (int j = 0; j < tiles; ++j) {
+            // the largest magnitude of a value's scale in the tile; E keeps eight times it, times 2^-E, below 2^15
+            uint32_t wide = 0, wide_key = 0;
+#pragma unroll
+            for (int i = 0; i < G / 2; ++i) {
+                wide = max(wide, max(vs[i] & 0x7fffu, vs[i] >> 16 & 0x7fffu));
+                wide_key = max(wide_key, max(ks[i] & 0x7fffu, ks[i] >> 16 & 0x7fffu));
+            }
+            wide = __reduce_max_sync(0xffffffffu, wide);
+            wide_key = __reduce_max_sync(0xffffffffu, wide_key);
+            const uint32_t have = __ballot_sync(0xffffffffu, exists);
+            if (lane == 0) { atomicMax(&sh.widest[j & 3], int(wide)); atomicMax(&sh.widest_key[j & 3], int(wide_key)); sh.there[j & 3][w] = have; }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            {
+                const int widest = *reinterpret_cast<volatile int*>(&sh.widest[j & 3]);
+                const float most = 8.f * __half2float(__ushort_as_half((unsigned short)widest));
+                // (a little room above the first tile, so that E is raised seldom)
+                const int need = most > 0.f && most < 1e9f ? ilogbf(most) + 1 : -1000;
+                if (need - e > 15) e = need - 8;
+            }
+            const int e_use = e == -1000 ? 0 : e;
+            const bool down = *reinterpret_cast<volatile int*>(&sh.widest_key[j & 3]) >= 0x7000;        // a scale of 2^13 or more: keys of 2^16
+            if (t == 0) { sh.exps[j & 3] = (e_use & 0xffff) | int(down) << 16; sh.widest[(j + 2) & 3] = sh.widest_key[(j + 2) & 3] = 0; }
+            const int st = j & 1;
+            if (ok && j >= 2) ok = wait(sh.k_empty[st], (j / 2 - 1) & 1);
+            if (!ok) continue;
+            expand(k_at + st * S::op_bytes, kc, ks, down ? 1.f / 16.f : 1.f);
+            fence_proxy_async();
+            mbar_arrive(smem_u32(&sh.k_full[st]));
+            const bool more = j + 1 < tiles;
+            uint32_t vs_now[G / 2];
+#pragma unroll
+            for (int i = 0; i < G / 2; ++i) vs_now[i] = vs[i];
+            if (more) { locate(j + 1); scales(ks, 0); codes(kc, 0); scales(vs, 1); }
+            if (j >= 2) ok = wait(sh.v_empty[st], (j / 2 - 1) & 1);
+            if (!ok) continue;
+            expand(v_at + st * S::op_bytes, vc, vs_now, exp2f(float(-e_use)));
+            fence_proxy_async();
+            mbar_arrive(smem_u32(&sh.v_full[st]));
+            if (more) codes(vc, 1);
+        }
+    } else {
+        fewer_registers<kPfIssueRegs>();
+        // ---- products ----
+        if (warp == 12) {
+            constexpr uint32_t idesc_s = pf_idesc(kPfTile, false), idesc_o = pf_idesc(HD, true);
+            auto scores = [&](int h, int st) {
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < HD / 16; ++k) {
+                        const uint32_t off = (k / 4) * S::block_bytes + (k % 4) * 32;
+                        tc_mma_f16(t_s + h * 128, smem_desc_sw128(q_at + h * S::op_bytes + off, 16, 1024), smem_desc_sw128(k_at + st * S::op_bytes + off, 16, 1024), idesc_s, k > 0);
+                    }
+                    tc_commit(smem_u32(&sh.s_full[h]));
+                }
+                __syncwarp();
+            };
+            auto sums = [&](int h, int st, bool more) {
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kPfTile / 16; ++k)
+                        pf_mma_ts(t_o + h * HD, t_s + h * 128 + 8 * k, smem_desc_sw128(v_at + st * S::op_bytes + k * 2048, S::block_bytes, 1024), idesc_o, more || k > 0);
+                }
+                __syncwarp();
+            };
+            auto signal = [&](unsigned long long& bar) {
+                if (elect_one()) tc_commit(smem_u32(&bar));
+                __syncwarp();
+            };
+            const int count[2] = {tiles0, tiles1};
+            bool ok = tiles == 0 || wait(sh.k_full[0], 0);
+            tc_fence_after();
+            if (ok && tiles > 0) {
+                for (int h = 0; h < 2; ++h)
+                    if (count[h] > 0) scores(h, 0);
+                signal(sh.k_empty[0]);
+            }
+            for (int j = 0; ok && j < tiles; ++j) {
+                const int st = j & 1, next = (j + 1) & 1;
+                bool keys = false;                   // of the next tile have been waited for
+                if (!(ok = wait(sh.v_full[st], (j / 2) & 1))) break;
+                for (int h = 0; h < 2; ++h) {
+                    if (j < count[h]) {
+                        if (!(ok = wait(sh.p_full[h], j & 1))) break;
+                        tc_fence_after();
+                        sums(h, st, j > 0);
+                        if (j + 1 == count[h]) signal(sh.o_full[h]);
+                    }
+                    if (j + 1 < count[h]) {
+                        if (!keys && !(ok = wait(sh.k_full[next], ((j + 1) / 2) & 1))) break;
+                        keys = true;
+                        tc_fence_after();
+                        scores(h, next);
+                    }
+                }
+                if (!ok) break;
+                signal(sh.v_empty[st]);
+                if (j + 1 < tiles) signal(sh.k_empty[next]);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace spm

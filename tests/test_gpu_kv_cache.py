@@ -316,6 +316,65 @@ def test_attend(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     assert c.status.item() == 0
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("lengths,rows,hq,hk,hd,page,pad", [
+    ([900, 333, 0, 128], [300, 333, 0, 128], 8, 1, 128, 32, 3),
+    ([640], [256], 4, 2, 128, 256, 0),
+    ([257, 700], [257, 90], 8, 2, 64, 16, 5),
+    ([130, 20], [150, 31], 16, 1, 64, 48, 0),          # more rows than tokens
+    ([385], [129], 3, 1, 128, 16, 0),
+])
+def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
+    c = Case(kv, 21, lengths, rows, hk, hd, page, dtype, pad, wide_table=2, fill=True)
+    check_attend(c, hq)
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("rows", [[1, 1], [200, 64]])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_values_and_keys_of_any_size(kv, rows, dtype):
+    """Scales of values grow by ten decades along the context, and then fall; keys are large in one stretch, queries tiny and large."""
+    c = Case(kv, 22, [900, 400], rows, 1, 128, 16, dtype, fill=True)
+    g = torch.Generator().manual_seed(5)
+    pages = torch.from_numpy(c.start)
+    for seq in range(2):
+        for t in range(0, c.lengths[seq], 16):
+            block = pages[c.table[seq, t // 16], 0, 0]
+            at = t / c.lengths[seq]
+            size = 10.0 ** (-6 + 10 * (at / 0.7 if at < 0.7 else (1 - at) / 0.3))
+            block[17 * 128:] = ((torch.rand(64, generator=g) + 0.5) * size).half().view(torch.uint8)
+            key = 9000.0 if 0.4 < at < 0.5 else 0.1
+            block[16 * 128:17 * 128] = ((torch.rand(64, generator=g) - 0.5) * key).half().view(torch.uint8)
+    c.start = pages.numpy().copy()
+    c.cache.pages.copy_(pages)
+    q = c.randn(c.n_rows, 4, 128)
+    for size in (1e-6, 1e-20):
+        check_attend(c, 4, q=(q * size))
+    c.start[:, :, :, 16 * 128:17 * 128] = 0            # keys of 0 and the largest queries
+    c.cache.pages.copy_(torch.from_numpy(c.start))
+    check_attend(c, 4, q=q * 1e15)
+
+
+def test_bad_pages_in_a_prompt(kv):
+    c = Case(kv, 23, [600, 300], [200, 300], 1, 64, 16, BF16, fill=True)
+    c.table[0, 3], c.table[0, 20], c.table[1, 0], c.table[1, 18] = -1, 10 ** 6, -2, c.start.shape[0]
+    c.batch = kv.KVBatch(c.table.cuda(), c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=300)
+    check_attend(c, 4)
+    assert c.status.item() == 1
+    c.status.zero_()
+    c.table = c.table[:, :10].contiguous()             # and contexts beyond the table
+    c.batch = kv.KVBatch(c.table.cuda(), c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=300)
+    check_attend(c, 4)
+    assert c.status.item() == 3
+
+
+@pytest.mark.parametrize("max_rows", [0, 1, 10 ** 6])
+def test_max_rows_is_a_hint(kv, max_rows):
+    c = Case(kv, 24, [150, 33, 90], [150, 1, 30], 2, 128, 16, BF16, fill=True)
+    c.batch = kv.KVBatch(c.batch._keep[0], c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=max_rows)
+    check_attend(c, 8)
+
+
 @pytest.mark.parametrize("n_seq", [64, 65, 300, 1024])
 @pytest.mark.parametrize("rows", ["one", "ragged"])
 def test_many_sequences(kv, n_seq, rows):
