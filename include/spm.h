@@ -526,6 +526,32 @@ int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, i
 int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_q_heads, const spm_rows* out, float scale,
                   int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The attention block of a decode step: before each layer's router,
+ *     x = RMSNorm(h); (q, k, v) = W_qkv x; spm_kv_write (norm, rotation, k and v into the layer's cache); o = spm_kv_attend; h += W_o o
+ * for the step's nb rows, row s being the new token of sequence s. The synthetic configurations omit it (spm_set_attention_stub_us stands
+ * in for its time); a model that has it hands it over once: */
+typedef struct {
+    const spm_kv_cache* caches;     /* HOST [L]: a cache a layer, all of one shape; copied                                        */
+    spm_kv_batch batch;             /* page_table, lengths, n_seq (>= every nb), table_stride; the rest is not read. Before a step
+                                       the caller counts its new token in `lengths` (device memory, read by the step's kernels)   */
+    spm_rope rope;                  /* q_gamma, k_gamma: dev [L][head_dim] or NULL                                               */
+    const int32_t* positions;       /* dev [n_axes][pos_stride]: of the step's rows, set before a step like `lengths`            */
+    int64_t pos_stride;
+    const float* rms_gamma;         /* dev fp32 [L][D]                                                                           */
+    const void* w_qkv;              /* dev [L][(n_q_heads + 2 n_kv_heads) * head_dim][D], bf16 (fp32 models: fp32)               */
+    const void* w_o;                /* dev [L][D][n_q_heads * head_dim]                                                          */
+    int32_t n_q_heads;
+    float scale;                    /* of the scores                                                                             */
+    void* workspace;                /* dev, 16-byte aligned, spm_attention_workspace() bytes                                     */
+    size_t workspace_bytes;
+} spm_attention;
+int spm_attention_workspace(const spm_model_cfg* cfg, const spm_attention* attention, size_t* bytes);
+/* From the next step on every step has this block (attention NULL: none). The structs are copied, what they point to on the device stays
+ * the caller's. Such a step is separate launches (not one kernel) and is replayed from graphs like others. Waits for the compute stream. */
+int spm_set_attention(spm_ctx* ctx, const spm_attention* attention);
+/* The block of one layer by itself, as spm_decode_step runs it: h_inout dev [nb][D]. Asynchronous, on the compute stream. */
+int spm_attention_block(spm_ctx* ctx, int layer, float* h_inout, int nb);
+
 /* Pinned host memory for the expert store (thin wrappers over cudaHostAlloc / cudaFreeHost). */
 int spm_host_alloc(size_t bytes, void** out);
 int spm_host_free(void* p);

@@ -81,6 +81,12 @@ class Rope(C.Structure):
                 + [(k, C.c_int32) for k in ("n_axes", "rot_dim", "neighbours")] + [("eps", C.c_float)])
 
 
+class Attention(C.Structure):
+    _fields_ = [("caches", C.POINTER(KvCache)), ("batch", KvBatch), ("rope", Rope), ("positions", C.c_void_p), ("pos_stride", C.c_int64),
+                ("rms_gamma", C.c_void_p), ("w_qkv", C.c_void_p), ("w_o", C.c_void_p), ("n_q_heads", C.c_int32), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 # symbol -> argument types (all return int except spm_last_error)
 _P = C.c_void_p
 _SIG = {
@@ -126,6 +132,9 @@ _SIG = {
     "spm_get_slot_table": [_P, C.c_int, _P],
     "spm_synchronize": [_P],
     "spm_ffn_noalloc": [C.POINTER(ModelCfg), _P, C.c_int, _P, _P, C.c_int, _P, _P, _P, C.c_int],
+    "spm_attention_workspace": [C.POINTER(ModelCfg), C.POINTER(Attention), C.POINTER(C.c_size_t)],
+    "spm_set_attention": [_P, C.POINTER(Attention)],
+    "spm_attention_block": [_P, C.c_int, _P, C.c_int],
     "spm_kv_cache_bytes": [C.POINTER(KvCache), C.POINTER(C.c_size_t)],
     "spm_rotate_heads": [C.POINTER(Rope), _P, C.c_int64, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_int, C.c_int, C.c_int, _P],
     "spm_kv_write": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rope), _P, C.c_int64, C.POINTER(Rows), C.POINTER(Rows), C.c_int,
@@ -499,6 +508,20 @@ def spm_kv_attend_workspace(kv, batch, n_q_heads, dtype) -> int:
 
 def spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
     _check(load().spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream))
+
+
+def spm_attention_workspace(cfg: ModelCfg, attention: Attention) -> int:
+    out = C.c_size_t()
+    _check(load().spm_attention_workspace(C.byref(cfg), attention, C.byref(out)))
+    return out.value
+
+
+def spm_set_attention(ctx, attention):
+    _check(load().spm_set_attention(ctx, attention), ctx)
+
+
+def spm_attention_block(ctx, layer, h_inout, nb):
+    _check(load().spm_attention_block(ctx, layer, _ptr(h_inout), nb), ctx)
 
 
 def spm_host_alloc(nbytes: int) -> int:

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspm.so")
-SOURCES = ["spm.cu", "ffn_noalloc.cu", "kv_cache.cu"]
+SOURCES = ["spm.cu", "ffn_noalloc.cu", "kv_cache.cu", "attention_block.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC,-O3,-Wall", "--expt-relaxed-constexpr",

@@ -18,6 +18,7 @@
 #include <immintrin.h>
 
 #include "../../include/spm.h"
+#include "attention_block.h"
 #include "ffn_gemv.cuh"
 #include "ffn_gemv_q4.cuh"
 #include "ffn_multi.cuh"
@@ -125,6 +126,8 @@ struct spm_ctx {
     int hint_steps = 0, hint_stride = 0;
     int drop_modulo = 0;
     int stub_us = 0;                          // attention stand-in before each layer's router
+    AttentionBlock attention;                 // the block itself, where the model has it
+    bool between_layers() const { return stub_us > 0 || attention.on; }       // something reads the hidden rows before a router does
     int copy_delay_us = 0;                    // emulated slower storage tier: extra wait after every expert copy
     bool device_wait = false;                 // batch-1 FFN launched at once, waits for its copies on the device
     double prof_window_us = 0, prof_xfer_us = 0;   // what the last spm_profile_window measured (0: never run)
@@ -1161,6 +1164,21 @@ void borda_rank(const int32_t* ids, int nb, int K, int n, std::vector<int32_t>& 
 }
 
 
+// What a step runs before a layer's router: the attention stand-in, the attention block
+int enqueue_between_layers(spm_ctx* c, int layer, float* h, int nb) {
+    if (c->stub_us > 0) {
+        attention_stub_kernel<<<1, 1, 0, c->compute>>>(uint64_t(c->stub_us) * 1000ull);
+        CU(c, cudaGetLastError());
+        c->kernel_launches++;
+    }
+    if (c->attention.on) {
+        std::string why;
+        if (int rc = enqueue_attention(c->attention, c->cfg, layer, h, nb, c->compute, &why)) return fail(c, rc, "%s", why.c_str());
+        c->kernel_launches += kAttentionLaunches;
+    }
+    return SPM_OK;
+}
+
 // The layers of one decode step. With `trace` null the kernels are launched and the routing results
 // awaited layer by layer; with a trace (the mailboxes a host-free step filled) only the host side
 // runs: accounting, slot-table updates, selection — the same calls in the same order.
@@ -1177,11 +1195,7 @@ int step_layers(spm_ctx* c, float* h_out, int nb, Timing* t, const Mailbox* trac
     // the device never waits for that host work. The mailbox words of layer l are read before.
     bool partial_left = false;       // the preceding layer's partial rows are still to be folded into the hidden row
     auto enqueue_router = [&](int l) -> int {
-        if (c->stub_us > 0) {
-            attention_stub_kernel<<<1, 1, 0, c->compute>>>(uint64_t(c->stub_us) * 1000ull);
-            CU(c, cudaGetLastError());
-            c->kernel_launches++;
-        }
+        if (int rc = enqueue_between_layers(c, l, h_out, nb)) return rc;
         RouterRoute fold{c->mb_dev, nullptr, nullptr, false, c->ws_partial, ffn_grid_for(c, nb), nullptr};
         if (int rc = launch_router(c, l, h_out, nullptr, nb, c->ws_x, nullptr, true, predict && l <= L - 2,
                                    partial_left ? &fold : nullptr, false)) return rc;
@@ -1219,7 +1233,7 @@ int step_layers(spm_ctx* c, float* h_out, int nb, Timing* t, const Mailbox* trac
             }
         }
         if (int rc = run_ffn(c, l, c->ws_x, ids.data(), c->ws_w, nb, h_out, t, -1, trace == nullptr,
-                             gemv_path && l + 1 < L && c->stub_us == 0, &partial_left)) return rc;
+                             gemv_path && l + 1 < L && !c->between_layers(), &partial_left)) return rc;
         if (c->policy == SPM_POLICY_NAIVE) borda_rank(ids.data(), nb, K, n, this_rank);
 
         c->prev_order_valid = false;
@@ -1316,16 +1330,12 @@ int enqueue_host_free_layers(spm_ctx* c, int nb, float* h_out, int slot, bool pr
     const int L = m.n_layers, K = m.top_k, n = m.n_experts;
     const int G = ffn_grid_for(c, nb);
     for (int l = 0; l < L; ++l) {
-        if (c->stub_us > 0) {
-            attention_stub_kernel<<<1, 1, 0, c->compute>>>(uint64_t(c->stub_us) * 1000ull);
-            CU(c, cudaGetLastError());
-            c->kernel_launches++;
-        }
+        if (int rc = enqueue_between_layers(c, l, h_out, nb)) return rc;
         short* codes = c->ws_codes + size_t(l) * m.max_batch * SPM_MAX_TOPK;
         // On the GEMV path the routing kernel of layer l + 1 also folds layer l's partial rows into the
         // hidden row, so only the last layer needs the combine kernel.
         const bool use_tc = ffn_path(c, nb) == FfnPath::kGrouped, multi = ffn_path(c, nb) == FfnPath::kMulti;
-        const bool fold = !use_tc && !multi && l > 0 && c->stub_us == 0;
+        const bool fold = !use_tc && !multi && l > 0 && !c->between_layers();
         RankArgs rank{};               // grouped kernels: the plan and gather kernel has a block for the adapter's ranking
         RouterRoute route{c->tr_dev + size_t(slot) * L + l, c->ws_slot_map + size_t(l) * n, codes, true,
                           fold ? c->ws_partial : nullptr, G, use_tc ? &rank : nullptr};
@@ -1391,7 +1401,7 @@ int enqueue_host_free_layers(spm_ctx* c, int nb, float* h_out, int slot, bool pr
             fill(a);
             CU(c, launch_gemv<SPM_MAX_BATCH>(c, a, G, nb, true));
         }
-        if (l == L - 1 || c->stub_us > 0) {
+        if (l == L - 1 || c->between_layers()) {
             unsigned long long* reduce_clock = nullptr;
             if (int rc = take_clock(c, kClkReduce, &reduce_clock)) return rc;
             CU(c, launch_k(ffn_reduce_kernel, dim3((m.hidden + kReduceCols - 1) / kReduceCols, nb), dim3(kReduceCols * kReduceGroups), 0,
@@ -1501,7 +1511,7 @@ int enqueue_resident_step(spm_ctx* c, const float* h_in, float* h_out, int slot,
     const int G = c->num_sms;
     StepArgs a{};
     size_t smem = 0;
-    if (!c->coop || (m.dtype == SPM_DTYPE_FP32 && m.n_layers < 3) || c->timing || c->stub_us > 0 || ffn_grid_for(c, 1) != G ||
+    if (!c->coop || (m.dtype == SPM_DTYPE_FP32 && m.n_layers < 3) || c->timing || c->between_layers() || ffn_grid_for(c, 1) != G ||
         G > kStepMaxCtas || 2 * G > kMaxCtasBatch1 || m.hidden > G * kStepCols || !resident_shape(c, G, &a, &smem)) return SPM_OK;
     predict = predict && m.n_layers > 1;
     if (predict && !aligned16(c->buf.adapter_a)) return fail(c, SPM_ERR_INVALID_ARG, "adapter_a must be 16-byte aligned");
@@ -2057,6 +2067,56 @@ int spm_set_attention_stub_us(spm_ctx* c, int us) {
     c->stub_us = us;
     return SPM_OK;
 }
+int spm_attention_workspace(const spm_model_cfg* cfg, const spm_attention* a, size_t* bytes) {
+    std::string why;
+    if (!cfg || !bytes) return fail(nullptr, SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_cfg(cfg, 32767, nullptr)) return rc;
+    if (int rc = check_attention(*cfg, a, &why)) return fail(nullptr, rc, "%s", why.c_str());
+    *bytes = attention_bytes(*cfg, *a);
+    return SPM_OK;
+}
+
+int spm_set_attention(spm_ctx* c, const spm_attention* a) {
+    if (!c) return SPM_ERR_INVALID_ARG;
+    if (int rc = flush_trace(c)) return rc;
+    AttentionBlock block;
+    if (a) {
+        std::string why;
+        if (int rc = check_attention(c->cfg, a, &why)) return fail(c, rc, "%s", why.c_str());
+        const int hd = a->caches[0].head_dim;
+        if (!a->rms_gamma || !a->w_qkv || !a->w_o || !a->batch.lengths || (!a->batch.page_table && a->batch.table_stride > 0))
+            return fail(c, SPM_ERR_INVALID_ARG, "attention: null argument");
+        if (!aligned16(a->rms_gamma) || !aligned16(a->w_qkv) || !aligned16(a->w_o)) return fail(c, SPM_ERR_INVALID_ARG, "attention: rms_gamma, w_qkv and w_o must be 16-byte aligned");
+        if (a->rope.rot_dim < 0 || a->rope.rot_dim > hd || a->rope.rot_dim % 16 || a->rope.n_axes < 1 || a->rope.n_axes > SPM_KV_MAX_AXES)
+            return fail(c, SPM_ERR_CONFIG, "attention: rot_dim or n_axes unsupported");
+        if (a->rope.rot_dim > 0 && (!a->rope.inv_freq || !a->positions || (a->rope.n_axes > 1 && a->pos_stride < a->batch.n_seq)))
+            return fail(c, SPM_ERR_INVALID_ARG, "attention: inv_freq or positions is null, or pos_stride less than the sequences");
+        if (!aligned16(a->rope.q_gamma) || !aligned16(a->rope.k_gamma)) return fail(c, SPM_ERR_INVALID_ARG, "attention: gammas must be 16-byte aligned");
+        if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < attention_bytes(c->cfg, *a))
+            return fail(c, SPM_ERR_INVALID_ARG, "attention: workspace must be 16-byte aligned and hold %zu bytes", attention_bytes(c->cfg, *a));
+        block.a = *a;
+        block.caches.assign(a->caches, a->caches + c->cfg.n_layers);
+        block.on = true;
+    }
+    CU(c, cudaStreamSynchronize(c->compute));
+    for (auto& g : c->hf_graphs) if (g.exec) cudaGraphExecDestroy(g.exec);       // (captured with what was set before)
+    c->hf_graphs.clear();
+    c->hf_warm = false;
+    c->attention = std::move(block);
+    c->attention.a.caches = c->attention.caches.data();
+    return SPM_OK;
+}
+
+int spm_attention_block(spm_ctx* c, int layer, float* h_inout, int nb) {
+    if (int rc = check_layer(c, layer, nb)) return rc;
+    if (!c->attention.on) return fail(c, SPM_ERR_STATE, "spm_set_attention has not been called");
+    if (!h_inout || !aligned16(h_inout)) return fail(c, SPM_ERR_INVALID_ARG, "h_inout must be 16-byte aligned");
+    std::string why;
+    if (int rc = enqueue_attention(c->attention, c->cfg, layer, h_inout, nb, c->compute, &why)) return fail(c, rc, "%s", why.c_str());
+    c->kernel_launches += kAttentionLaunches;
+    return SPM_OK;
+}
+
 int spm_set_deadline_ms(spm_ctx* c, int ms) {
     if (!c || ms < 1) return SPM_ERR_INVALID_ARG;
     c->deadline_ms = ms;

@@ -75,6 +75,10 @@ class Rope:
                   None if k_gamma is None else _vector(k_gamma, torch.float32, self.device, "k_gamma"))
         self._by_axes = {n: B.Rope(*fields, n, 2 * half, int(neighbours), eps) for n in range(1, 5)}
 
+    def for_axes(self, n):
+        """The spm_rope struct of positions with n axes."""
+        return self._by_axes[n]
+
     def _with(self, positions, n_rows, hd, q, k):
         """(struct, positions' address, axis stride) of a call with positions [n_axes, rows] or [rows]; q, k: whose gammas it uses."""
         if positions is None:

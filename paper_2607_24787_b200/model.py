@@ -141,6 +141,44 @@ class OffloadedMoE:
         B.spm_decode_step_host(self.ctx, h_in_host, h_in_host.shape[0], h_out_host)
         return h_out_host
 
+    # ---- the attention block, for models that have it ----
+    def set_attention(self, caches, page_table, lengths, rope, positions, rms_gamma, w_qkv, w_o, scale=None):
+        """Steps run spm_attention before each router. caches: a kv_cache.KVCache a layer; page_table [n_seq, pages], lengths [n_seq] and
+        positions [axes, n_seq] int32 on the device, which the caller moves on before each step; rope: a kv_cache.Rope whose gammas are
+        [L * head_dim]; rms_gamma [L, D] fp32; w_qkv [L, (q_heads + 2 kv_heads) * head_dim, D], w_o [L, D, q_heads * head_dim]. caches
+        None: no block any more."""
+        if caches is None:
+            B.spm_set_attention(self.ctx, None)
+            self._attention = None
+            return
+        dtype = torch.float32 if self.cfg.dtype == B.DTYPE_FP32 else torch.bfloat16
+        hd, n_q = caches[0].head_dim, w_o.shape[2] // caches[0].head_dim
+        n = (n_q + 2 * caches[0].kv_heads) * hd
+        if len(caches) != self.L:
+            raise ValueError(f"{self.L} caches, one a layer")
+        for name, x, shape, dt in (("w_qkv", w_qkv, (self.L, n, self.D), dtype), ("w_o", w_o, (self.L, self.D, n_q * hd), dtype),
+                                   ("rms_gamma", rms_gamma, (self.L, self.D), torch.float32),
+                                   ("lengths", lengths, (page_table.shape[0],), torch.int32), ("page_table", page_table, tuple(page_table.shape), torch.int32)):
+            if tuple(x.shape) != shape or x.dtype is not dt or x.device != self.device or not x.is_contiguous():
+                raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {self.device}")
+        if any(g not in (None, self.L * hd) for g in rope.gamma_sizes):
+            raise ValueError("the rope's gammas: [L * head_dim]")
+        if positions.dim() != 2 or positions.shape[1] != page_table.shape[0] or positions.dtype is not torch.int32 or not positions.is_contiguous():
+            raise ValueError("positions: a contiguous int32 tensor [axes, n_seq]")
+        shapes = (B.KvCache * self.L)(*[c.c for c in caches])
+        batch = B.KvBatch(page_table.data_ptr(), lengths.data_ptr(), None, page_table.shape[0], page_table.shape[1], page_table.shape[0], 1)
+        a = B.Attention(shapes, batch, rope.for_axes(positions.shape[0]), positions.data_ptr(), positions.shape[1], rms_gamma.data_ptr(),
+                        w_qkv.data_ptr(), w_o.data_ptr(), n_q, hd ** -0.5 if scale is None else scale, None, 0)
+        a.workspace_bytes = B.spm_attention_workspace(self.cfg, a)
+        work = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
+        a.workspace = work.data_ptr()
+        torch.cuda.synchronize(self.device)
+        B.spm_set_attention(self.ctx, a)
+        self._attention = (caches, page_table, lengths, rope, positions, rms_gamma, w_qkv, w_o, work)
+
+    def attention_block(self, layer, h_inout):
+        B.spm_attention_block(self.ctx, layer, h_inout, h_inout.shape[0])
+
     # ---- control / accounting --------------------------------------------
     def set_policy(self, p): B.spm_set_policy(self.ctx, p)
     def set_budget(self, b): B.spm_set_budget(self.ctx, b)

@@ -171,3 +171,29 @@ def test_rotation_keeps_distances():
             return (a * b).sum()
         assert abs(dot((5, 7, 9), (2, 3, 4)) - dot((105, 57, 10), (102, 53, 5))) < 1e-9     # only the axes' differences count
         assert np.isclose((R.rotate(q, np.array([[3], [4], [5]]), inv, axis, neighbours=neighbours) ** 2).sum(), (q ** 2).sum())
+
+
+# ---- the block of a decode step -------------------------------------------------
+def test_attention_blocks_that_are_refused(B):
+    cfg = B.make_cfg(2, 512, 8, 128, 2, 0, 4, B.DTYPE_BF16, max_batch=4)
+
+    def block(kv=None, n=2, **kw):
+        caches = (B.KvCache * n)(*[kv or cache(B)] * n)
+        d = dict(caches=caches, batch=batch(B, row_start=None, n_seq=4, n_rows=4), rope=rope(B), positions=AT, pos_stride=4, rms_gamma=AT, w_qkv=AT,
+                 w_o=AT, n_q_heads=8, scale=0.1, workspace=AT, workspace_bytes=1 << 40)
+        d.update(kw)
+        return B.Attention(**d)
+
+    nb, hd = 4, 128
+    least = 8 * 1024 * 6 + nb * (8 + 4) * hd * 4 + nb * 8 * hd * 4
+    assert B.spm_attention_workspace(cfg, block()) >= least
+    refused(B, INVALID, lambda: B.spm_attention_workspace(cfg, block(caches=None)))
+    refused(B, CONFIG, lambda: B.spm_attention_workspace(cfg, block(n_q_heads=0)))
+    refused(B, CONFIG, lambda: B.spm_attention_workspace(cfg, block(n_q_heads=3)))
+    refused(B, INVALID, lambda: B.spm_attention_workspace(cfg, block(batch=batch(B, n_seq=0))))
+    refused(B, INVALID, lambda: B.spm_attention_workspace(cfg, block(batch=batch(B, lengths=None))))
+    refused(B, INVALID, lambda: B.spm_attention_workspace(cfg, block(kv=cache(B, pages=AT + 8))))
+    refused(B, CONFIG, lambda: B.spm_attention_workspace(cfg, block(kv=cache(B, head_dim=96))))
+    mixed = (B.KvCache * 2)(cache(B), cache(B, page_size=16))
+    refused(B, CONFIG, lambda: B.spm_attention_workspace(cfg, block(caches=mixed)))
+    refused(B, CONFIG, lambda: B.spm_attention_workspace(B.make_cfg(2, 500, 8, 128, 2, 0, 4, B.DTYPE_BF16, max_batch=4), block()))
