@@ -3,8 +3,8 @@
 // For a cache head, the new rows' query heads that read it are columns: column x is head x % group of row x / group, and eight columns are
 // the N of an m16n8k16. Keys are its A operand (16 tokens by 16 elements) straight from their nibbles, and the scale of a group is put on
 // the sum of the group's 32 products. Values are the A operand of the second product, transposed by ldmatrix (32 elements by 16 tokens);
-// their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries are split into three bf16
-// parts and probabilities into two.
+// their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries and scaled probabilities are split
+// into three bf16 parts each.
 // Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
 // bf16 calls leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is what the group's sum starts
 // with. Values: the probability is scaled up, and one more product with -8 in the codes' place goes into the running sum before theirs, so
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     using S = AtShape<T, HD>;
     constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
     constexpr bool RAW = S::raw;
-    constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 2 : 1;        // parts of a query, of a probability
+    constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = QP;        // parts of a query, of a probability
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
     unsigned char* ring = smem + warp * S::ring_bytes;

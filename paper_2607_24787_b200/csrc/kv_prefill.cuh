@@ -11,8 +11,7 @@
 // not fit are taken times 2^-4, a probability times 2^8 (it is at most 2^6 above the running maximum, see below), and values times 2^-E, E from the largest scale so
 // far (a tile whose values would not fit raises E, and the sums so far are scaled down).
 //
-// Probabilities are taken against the running maximum of the tiles before; only where a score is above it by more than 2^6 is the tile
-// done again with the new one and the sums are scaled.
+// A row's maximum is moved, and its sums scaled, only where a score is above it by more than 2^6.
 #pragma once
 
 #include "kv_attend.cuh"
@@ -59,11 +58,33 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
         "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         : PF_R8(r, 0), PF_R8(r, 8), PF_R8(r, 16), PF_R8(r, 24) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16_raw(uint32_t at, uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
-        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-        ::PF_W8(r, 0), PF_W8(r, 8), PF_W8(r, 16), PF_W8(r, 24), "r"(at) : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : PF_R8(r, 0), PF_R8(r, 8) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::PF_W8(r, 0), PF_W8(r, 8), "r"(at) : "memory");
+}
+// two fp32 numbers in one register pair
+__device__ __forceinline__ unsigned long long two_words(uint32_t a, uint32_t b) {
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
+    return v;
+}
+__device__ __forceinline__ unsigned long long two_floats(float a, float b) { return two_words(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ void floats_of(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -93,8 +114,7 @@ struct PfShared {
     uint32_t tmem;
     int quit;                                    // a wait has run out: everybody leaves
     int exps[4];                                 // E of a tile, and whether its keys are times 2^-4 (bit 16)
-    int widest[4];                               // largest scale of a tile's values, and of its keys, as fp16 bits
-    int widest_key[4];
+    int widest[4], widest_key[4];                // an operand warp's largest scale of a tile's values and keys, as fp32 bits
     uint32_t there[4][4];                        // which tokens of a tile exist
 };
 
@@ -156,7 +176,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
             mbar_init(smem_u32(&sh.s_full[i]), 1); mbar_init(smem_u32(&sh.p_full[i]), 128); mbar_init(smem_u32(&sh.o_full[i]), 1);
         }
         sh.quit = 0;
-        for (int i = 0; i < 4; ++i) sh.widest[i] = sh.widest_key[i] = 0;
         fence_barrier_init();
     }
     if (warp == 12) tmem_alloc(smem_u32(&sh.tmem), 512);
@@ -243,63 +262,64 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                     const int left = limit - j * kPfTile - 32 * i;
                     if (left < 32) there[i] &= left <= 0 ? 0u : (1u << left) - 1;
                 }
-            uint32_t p[64];
-            float top = -INFINITY, sum;
-            auto probabilities = [&] {
-                const float nb = 8.f - (m == -INFINITY ? 0.f : m);
-                sum = 0.f;
+            uint32_t r[4][32];
 #pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    uint32_t r[32];
-                    tmem_ld32(s_at + 32 * ch, r);
-                    tmem_wait_ld();
-                    if (!whole) {
+            for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_at + 32 * ch, r[ch]);
+            tmem_wait_ld();
+            if (!whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!(there[ch] >> i & 1)) r[i] = 0xff800000u;
-                    }
+                for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float x0 = __uint_as_float(r[i]), x1 = __uint_as_float(r[i + 1]);
-                        top = fmaxf(top, fmaxf(x0, x1));
-                        const float p0 = ex2(fmaf(x0, ft, nb)), p1 = ex2(fmaf(x1, ft, nb));
-                        sum += p0 + p1;
-                        p[ch * 16 + i / 2] = pack_half(p0, p1);
-                    }
-                }
-            };
-            probabilities();
-            const float peak = top * ft;         // m is kept as a power of two's exponent
-            const bool raise = peak > m + 6.f;
-            if (__any_sync(0xffffffffu, raise || e != e_now)) {
+                    for (int i = 0; i < 32; ++i)
+                        if (!(there[ch] >> i & 1)) r[ch][i] = 0xff800000u;
+            }
+            float tops[4];
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) {
+                tops[ch] = __uint_as_float(r[ch][0]);
+#pragma unroll
+                for (int i = 1; i < 32; ++i) tops[ch] = fmaxf(tops[ch], __uint_as_float(r[ch][i]));
+            }
+            const float peak = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * ft;         // m is kept as a power of two's exponent
+            if (__any_sync(0xffffffffu, peak > m + 6.f || e != e_now)) {
                 const float to = fmaxf(m, peak), by = m == -INFINITY ? 0.f : ex2(m - to);
                 m = to;
                 l *= by;
                 if (j > 0) {                     // (before that the sums hold nothing)
                     const float scale = by * exp2f(float(e_now - e));
 #pragma unroll 1
-                    for (int ch = 0; ch < HD / 32; ++ch) {
-                        uint32_t r[32];
-                        tmem_ld32(o_at + 32 * ch, r);
+                    for (int ch = 0; ch < HD / 16; ++ch) {
+                        uint32_t o[16];
+                        tmem_ld16_raw(o_at + 16 * ch, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * scale);
-                        tmem_st32(o_at + 32 * ch, r);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * scale);
+                        tmem_st16(o_at + 16 * ch, o);
                     }
-                    tmem_wait_st();
                 }
                 e_now = e;
-                probabilities();
             }
-            l += sum;
-            {
-                uint32_t r[32];
+            const float nb = 8.f - (m == -INFINITY ? 0.f : m);
+            const unsigned long long f2 = two_floats(ft, ft), nb2 = two_floats(nb, nb);
+            unsigned long long sum0 = 0, sum1 = 0;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+            for (int ch = 0; ch < 4; ++ch) {
+                uint32_t p[16];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) r[i] = p[32 * h + i];
-                    tmem_st32(s_at + 32 * h, r);
+                for (int i = 0; i < 32; i += 2) {
+                    float x0, x1;
+                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, nb2), x0, x1);
+                    const float p0 = ex2(x0), p1 = ex2(x1);
+                    unsigned long long& sum = i & 2 ? sum1 : sum0;
+                    sum = add2(sum, two_floats(p0, p1));
+                    p[i / 2] = pack_half(p0, p1);
                 }
+                tmem_st16(s_at + 16 * ch, p);
+            }
+            {
+                float x0, x1;
+                floats_of(add2(sum0, sum1), x0, x1);
+                l += x0 + x1;
             }
             tmem_wait_st();
             tc_fence_before();
@@ -339,21 +359,24 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         // ---- operands: a thread takes a token of each tile, its codes a tile ahead ----
         const int t = tid - 256, w = warp - 8;
         const int nk = max(sees(rb * kPfCols + kPfTile - 1), used1 ? sees(rb * kPfCols + kPfCols - 1) : 0);
+        const int per_page = a.kv.page_size / kKvBlock;
+        const int* table = b.table + static_cast<size_t>(seq) * b.stride;
+        const int tok = t % kKvBlock;
         uint4 kc[G], vc[G];
-        uint32_t ks[G / 2], vs[G / 2];
+        uint32_t ks[G / 2], vs[G / 2], ks_then[G / 2], vs_then[G / 2];
+        // where this thread's token of tile j is; its page has been loaded a tile before (-2: there is no such token)
+        auto slot_of = [&](int j) { const int block = (j * kPfTile + t) / kKvBlock; return a.page_shift >= 0 ? block >> a.page_shift : block / per_page; };
+        auto page_of = [&](int j) { return j * kPfTile + t < nk ? table[slot_of(j)] : -2; };
         const unsigned char* at = nullptr;
         bool exists = false;
-        auto locate = [&](int j) {
-            const int pos = j * kPfTile + t;
-            exists = false;
-            if (pos >= nk) return;
-            const long long block_at = kv_block_at<HD>(a.kv, b, seq, pos, head);
-            if (block_at < 0) { kv_note(a.kv, SPM_KV_BAD_PAGE); return; }
-            exists = true;
-            at = a.kv.pages + block_at + (pos % kKvBlock) * 16;
+        auto locate = [&](int j, int page) {
+            exists = page >= 0 && page < a.kv.n_pages;
+            if (!exists && page != -2) kv_note(a.kv, SPM_KV_BAD_PAGE);
+            const int block = (j * kPfTile + t) / kKvBlock - slot_of(j) * per_page;
+            at = a.kv.pages + ((static_cast<long long>(exists ? page : 0) * a.kv.heads + head) * per_page + block) * kv_block_bytes(HD) + tok * 16;
         };
         auto scales = [&](uint32_t (&s)[G / 2], int part) {
-            const unsigned char* p = at - (t % kKvBlock) * 16 + kv_k_scales(HD) + part * HD + (t % kKvBlock) * (2 * G);
+            const unsigned char* p = at + kv_k_scales(HD) + part * HD + tok * (2 * G - 16);
 #pragma unroll
             for (int i = 0; i < G / 2; ++i) s[i] = exists ? *reinterpret_cast<const uint32_t*>(p + 4 * i) : 0u;
         };
@@ -362,60 +385,87 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
             for (int k = 0; k < G; ++k) x[k] = exists ? *reinterpret_cast<const uint4*>(at + part * kv_v_codes(HD) + k * (kKvBlock * 16)) : make_uint4(0, 0, 0, 0);
         };
         auto expand = [&](uint32_t to, const uint4 (&x)[G], const uint32_t (&s)[G / 2], float by) {
+            const uint32_t row_at = to + t * 128 + ((t & 7) << 4);               // (tiles start on 1024 bytes)
 #pragma unroll
             for (int k = 0; k < G; ++k) {
                 const float2 pair = __half22float2(as_half2(s[k / 2]));
                 const __half2 d = __float2half2_rn((k & 1 ? pair.y : pair.x) * by);
                 const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) st_shared16(to + pf_chunk(t, 4 * k + i), pf_expand(word[i], d));
+                for (int i = 0; i < 4; ++i) st_shared16((row_at ^ ((4 * k + i & 7) << 4)) + (k >> 1) * S::block_bytes, pf_expand(word[i], d));
             }
         };
-        locate(0);
-        scales(ks, 0); scales(vs, 1);
-        codes(kc, 0); codes(vc, 1);
-        int e = -1000;
+        auto largest = [&](const uint32_t (&s)[G / 2]) {
+            __half2 m = __habs2(as_half2(s[0]));
+#pragma unroll
+            for (int i = 1; i < G / 2; ++i) m = __hmax2_nan(m, __habs2(as_half2(s[i])));
+            return __half2float(__hmax_nan(__low2half(m), __high2half(m)));
+        };
+        int page = -2;
+        if (tiles > 0) {
+            const int first_page = page_of(0);
+            if (tiles > 1) page = page_of(1);
+            locate(0, first_page);
+            scales(ks, 0); scales(vs, 1);
+            codes(kc, 0); codes(vc, 1);
+        }
+        int e = -1000;                           // E keeps eight times the largest scale of values so far, times 2^-E, below 2^15
+        float v_limit = -1.f, by_v = 1.f;        // the largest scale that E allows, 2^-E
         bool ok = true;                          // (a warp that has given up still comes to the others' barrier)
         for (int j = 0; j < tiles; ++j) {
-            // the largest magnitude of a value's scale in the tile; E keeps eight times it, times 2^-E, below 2^15
-            uint32_t wide = 0, wide_key = 0;
-#pragma unroll
-            for (int i = 0; i < G / 2; ++i) {
-                wide = max(wide, max(vs[i] & 0x7fffu, vs[i] >> 16 & 0x7fffu));
-                wide_key = max(wide_key, max(ks[i] & 0x7fffu, ks[i] >> 16 & 0x7fffu));
-            }
-            wide = __reduce_max_sync(0xffffffffu, wide);
-            wide_key = __reduce_max_sync(0xffffffffu, wide_key);
             const uint32_t have = __ballot_sync(0xffffffffu, exists);
-            if (lane == 0) { atomicMax(&sh.widest[j & 3], int(wide)); atomicMax(&sh.widest_key[j & 3], int(wide_key)); sh.there[j & 3][w] = have; }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
-            {
-                const int widest = *reinterpret_cast<volatile int*>(&sh.widest[j & 3]);
-                const float most = 8.f * __half2float(__ushort_as_half((unsigned short)widest));
-                // (a little room above the first tile, so that E is raised seldom)
-                const int need = most > 0.f && most < 1e9f ? ilogbf(most) + 1 : -1000;
-                if (need - e > 15) e = need - 8;
+            if (lane == 0) sh.there[j & 3][w] = have;
+            const float wide = largest(vs), wide_key = largest(ks);
+            const bool keys_fit = wide_key < 8192.f;                             // eight times it is below 2^16
+            int any;
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                         : "=r"(any) : "r"(int(!(wide <= v_limit) || !keys_fit)) : "memory");
+            bool down = false;
+            if (any) {                           // (seldom, but for the first tile)
+                if (lane == 0) sh.widest[w] = sh.widest_key[w] = 0;
+                __syncwarp();
+                atomicMax(&sh.widest[w], __float_as_int(wide < INFINITY ? wide : 0.f));
+                atomicMax(&sh.widest_key[w], __float_as_int(wide_key));
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                float widest = 0.f, widest_key = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    widest = fmaxf(widest, __int_as_float(*reinterpret_cast<volatile int*>(&sh.widest[i])));
+                    widest_key = fmaxf(widest_key, __int_as_float(*reinterpret_cast<volatile int*>(&sh.widest_key[i])));
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                down = !(widest_key < 8192.f);
+                if (widest > v_limit || e == -1000) {
+                    const int need = widest > 0.f ? ilogbf(widest) + 4 : 0;      // eight times it is below 2^need
+                    e = need - 8;                // (a little room, so that E is raised seldom)
+                    v_limit = exp2f(float(e + 15 - 3)) * 0.999f;
+                    by_v = exp2f(float(-e));
+                }
             }
-            const int e_use = e == -1000 ? 0 : e;
-            const bool down = *reinterpret_cast<volatile int*>(&sh.widest_key[j & 3]) >= 0x7000;        // a scale of 2^13 or more: keys of 2^16
-            if (t == 0) { sh.exps[j & 3] = (e_use & 0xffff) | int(down) << 16; sh.widest[(j + 2) & 3] = sh.widest_key[(j + 2) & 3] = 0; }
+            if (t == 0) sh.exps[j & 3] = (e & 0xffff) | int(down) << 16;
             const int st = j & 1;
             if (ok && j >= 2) ok = wait(sh.k_empty[st], (j / 2 - 1) & 1);
-            if (!ok) continue;
-            expand(k_at + st * S::op_bytes, kc, ks, down ? 1.f / 16.f : 1.f);
-            fence_proxy_async();
-            mbar_arrive(smem_u32(&sh.k_full[st]));
             const bool more = j + 1 < tiles;
-            uint32_t vs_now[G / 2];
+            if (ok) {
+                expand(k_at + st * S::op_bytes, kc, ks, down ? 1.f / 16.f : 1.f);
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&sh.k_full[st]));
+                if (more) {
+                    locate(j + 1, page);
+                    scales(ks_then, 0); scales(vs_then, 1);
+                    codes(kc, 0);
+                }
+                if (j + 2 < tiles) page = page_of(j + 2);
+                if (j >= 2) ok = wait(sh.v_empty[st], (j / 2 - 1) & 1);
+            }
+            if (ok) {
+                expand(v_at + st * S::op_bytes, vc, vs, by_v);
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&sh.v_full[st]));
+                if (more) codes(vc, 1);
+            }
 #pragma unroll
-            for (int i = 0; i < G / 2; ++i) vs_now[i] = vs[i];
-            if (more) { locate(j + 1); scales(ks, 0); codes(kc, 0); scales(vs, 1); }
-            if (j >= 2) ok = wait(sh.v_empty[st], (j / 2 - 1) & 1);
-            if (!ok) continue;
-            expand(v_at + st * S::op_bytes, vc, vs_now, exp2f(float(-e_use)));
-            fence_proxy_async();
-            mbar_arrive(smem_u32(&sh.v_full[st]));
-            if (more) codes(vc, 1);
+            for (int i = 0; i < G / 2; ++i) { ks[i] = ks_then[i]; vs[i] = vs_then[i]; }
         }
     } else {
         fewer_registers<kPfIssueRegs>();
