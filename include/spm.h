@@ -478,8 +478,8 @@ typedef struct {
     int32_t n_seq;                /* 0 .. SPM_KV_MAX_SEQS                                                       */
     int32_t table_stride;         /* page numbers a sequence                                                    */
     int32_t n_rows;               /* rows of the row arrays                                                     */
-    int32_t max_rows;             /* about how many new rows the longest prompt has (0: n_rows / n_seq): chooses between
-                                     kernels for few and for many rows; results hold for any value              */
+    int32_t max_rows;             /* about how many new rows a sequence has at most (0: not known): a hint for what to keep
+                                     in L2; results hold for any value                                          */
 } spm_kv_batch;
 
 /* Rows of heads: element e of head h of row i is p[i * row_stride + h * head_stride + e] (strides in elements). p and both strides in

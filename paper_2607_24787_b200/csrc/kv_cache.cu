@@ -145,11 +145,14 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD>, a);
 }
 
-// Whether a call's rows are enough for the tensor-core kernel
+// Which of the two kernels a call's rows are for. Per token of context the tensor-core kernel takes 17 ns a round of CTAs (an SM does 256
+// columns of a head, and an item's tokens are not shared out), the other 4.3 ps a column of a head on all SMs together, whatever the rows
+// are (measured with 46592 columns of 4 heads: 245 and 1605 us; with 144 columns the rule leaves the other, 27 us). Lengths cancel.
 bool prefill_pays(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
     if (dtype != SPM_DTYPE_BF16 || kv->head_dim > 128 || !b->row_start) return false;
-    const long long rows = b->max_rows ? b->max_rows : (b->n_rows + b->n_seq - 1) / std::max(b->n_seq, 1);
-    return rows * (n_q_heads / kv->n_kv_heads) >= kPfPays;
+    const long long columns = static_cast<long long>(b->n_rows) * (n_q_heads / kv->n_kv_heads), each = (columns + b->n_seq - 1) / b->n_seq;
+    const long long items = (each + kPfCols - 1) / kPfCols * b->n_seq * kv->n_kv_heads;
+    return columns * kv->n_kv_heads > 4000 * ((items + kAtMaxCtas - 1) / kAtMaxCtas);
 }
 template <int HD>
 cudaError_t launch_prefill(const AttendArgs& a, int dev, cudaStream_t st) {

@@ -21,7 +21,6 @@ namespace spm {
 
 constexpr int kPfTile = 128;                     // tokens of a tile, rows of a half
 constexpr int kPfCols = 256;
-constexpr int kPfPays = 128;                     // columns of a sequence from which this kernel is taken
 // two halves' softmax warps, operand warps, the issuing warp and three that only make its four whole. Registers a thread: 128 at the launch,
 // of which the last two fours give some to the softmax warps (2 x 176 + 104 + 56 = 4 x 128).
 constexpr int kPfThreads = 16 * 32;

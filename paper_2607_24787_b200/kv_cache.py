@@ -99,7 +99,7 @@ class Rope:
 class KVBatch:
     """New rows of several sequences. page_table [n_seq, pages] int32; lengths [n_seq] int32: tokens each sequence holds, its new rows
     included; row_start [n_seq + 1] int32: where a sequence's rows begin (None: one row each); n_rows: rows of the row tensors (None:
-    n_seq); max_rows: about how many rows the longest prompt has (0: their mean), which chooses between kernels and nothing else."""
+    n_seq); max_rows: about how many rows a sequence has at most (0: not known), a hint."""
 
     def __init__(self, page_table, lengths, row_start=None, n_rows=None, max_rows=0):
         _need(page_table.is_cuda and page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),

@@ -323,6 +323,12 @@ def test_attend(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     ([257, 700], [257, 90], 8, 2, 64, 16, 5),
     ([130, 20], [150, 31], 16, 1, 64, 48, 0),          # more rows than tokens
     ([385], [129], 3, 1, 128, 16, 0),
+    # enough columns for the tensor cores
+    ([640], [256], 16, 2, 128, 256, 0),
+    ([257, 700, 9], [257, 90, 9], 16, 2, 64, 16, 5),
+    ([130, 20], [150, 31], 32, 1, 64, 48, 0),
+    ([385], [129], 33, 1, 128, 16, 0),
+    ([70] * 9, [60] * 9, 8, 1, 128, 16, 1),
 ])
 def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     c = Case(kv, 21, lengths, rows, hk, hd, page, dtype, pad, wide_table=2, fill=True)
@@ -330,9 +336,9 @@ def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     assert c.status.item() == 0
 
 
-@pytest.mark.parametrize("rows", [[1, 1], [200, 64]])
+@pytest.mark.parametrize("rows,heads", [([1, 1], 4), ([200, 64], 4), ([200, 64], 16)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
-def test_values_and_keys_of_any_size(kv, rows, dtype):
+def test_values_and_keys_of_any_size(kv, rows, heads, dtype):
     """Scales of values grow by ten decades along the context, and then fall; keys are large in one stretch, queries tiny and large."""
     c = Case(kv, 22, [900, 400], rows, 1, 128, 16, dtype, fill=True)
     g = torch.Generator().manual_seed(5)
@@ -347,32 +353,34 @@ def test_values_and_keys_of_any_size(kv, rows, dtype):
             block[16 * 128:17 * 128] = ((torch.rand(64, generator=g) - 0.5) * key).half().view(torch.uint8)
     c.start = pages.numpy().copy()
     c.cache.pages.copy_(pages)
-    q = c.randn(c.n_rows, 4, 128)
+    q = c.randn(c.n_rows, heads, 128)
     for size in (1e-6, 1e-20):
-        check_attend(c, 4, q=(q * size))
+        check_attend(c, heads, q=(q * size))
     c.start[:, :, :, 16 * 128:17 * 128] = 0            # keys of 0 and the largest queries
     c.cache.pages.copy_(torch.from_numpy(c.start))
-    check_attend(c, 4, q=q * 1e15)
+    check_attend(c, heads, q=q * 1e15)
 
 
-def test_bad_pages_in_a_prompt(kv):
+@pytest.mark.parametrize("heads", [4, 12])
+def test_bad_pages_in_a_prompt(kv, heads):
     c = Case(kv, 23, [600, 300], [200, 300], 1, 64, 16, BF16, fill=True)
     c.table[0, 3], c.table[0, 20], c.table[1, 0], c.table[1, 18] = -1, 10 ** 6, -2, c.start.shape[0]
     c.batch = kv.KVBatch(c.table.cuda(), c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=300)
-    check_attend(c, 4)
+    check_attend(c, heads)
     assert c.status.item() == 1
     c.status.zero_()
     c.table = c.table[:, :10].contiguous()             # and contexts beyond the table
     c.batch = kv.KVBatch(c.table.cuda(), c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=300)
-    check_attend(c, 4)
+    check_attend(c, heads)
     assert c.status.item() == 3
 
 
 @pytest.mark.parametrize("max_rows", [0, 1, 10 ** 6])
-def test_max_rows_is_a_hint(kv, max_rows):
+@pytest.mark.parametrize("heads", [8, 24])
+def test_max_rows_is_a_hint(kv, max_rows, heads):
     c = Case(kv, 24, [150, 33, 90], [150, 1, 30], 2, 128, 16, BF16, fill=True)
     c.batch = kv.KVBatch(c.batch._keep[0], c.dev_lengths, c.batch._keep[2], n_rows=c.n_rows, max_rows=max_rows)
-    check_attend(c, 8)
+    check_attend(c, heads)
 
 
 @pytest.mark.parametrize("n_seq", [64, 65, 300, 1024])
@@ -398,13 +406,13 @@ def test_one_row_a_sequence_without_row_start(kv):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
-@pytest.mark.parametrize("rows", [[1, 1], [40, 25]])
-def test_sharp_and_flat_scores(kv, rows, dtype):
+@pytest.mark.parametrize("rows,heads", [([1, 1], 8), ([40, 25], 8), ([260, 100], 16)])
+def test_sharp_and_flat_scores(kv, rows, heads, dtype):
     """One token far above the rest, later than many others; and every score alike."""
     c = Case(kv, 10, [260, 100], rows, 1, 128, 32, dtype, fill=True)
-    check_attend(c, 8, scale=3.0)
-    check_attend(c, 8, scale=0.0)
-    check_attend(c, 8, scale=-0.05)
+    check_attend(c, heads, scale=3.0)
+    check_attend(c, heads, scale=0.0)
+    check_attend(c, heads, scale=-0.05)
 
 
 def test_bad_pages_and_lengths(kv):
