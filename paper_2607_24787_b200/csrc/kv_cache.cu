@@ -100,12 +100,13 @@ void by_type(int dtype, int hd, F f) {
 int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaStream_t st) {
     const int heads = 2 * a.kv_heads + a.q_heads;
     if (a.n_rows == 0 || heads == 0) return SPM_OK;
-    // many rows: eight a block; few: one, and blocks share its heads (a turn a warp)
-    const int each = a.n_rows >= kKvWriteRows * 592 ? kKvWriteRows : a.n_rows >= 1184 ? 2 : 1;
-    const int at_once = 256 / hd, turns = 2 * ((a.kv_heads + at_once - 1) / at_once) + (a.q_heads + at_once - 1) / at_once, chunks = (turns + kKvWarps - 1) / kKvWarps;
-    const dim3 grid((a.n_rows + each - 1) / each, static_cast<long long>(a.n_rows) * chunks <= 592 ? chunks : 1);
+    // a row a warp, or where these are few a row's turns shared out, up to a turn a warp
+    const int at_once = 256 / hd, turns = 2 * ((a.kv_heads + at_once - 1) / at_once) + (a.q_heads + at_once - 1) / at_once;
+    constexpr int kWarps = 592 * kKvWarps;       // that the GPU has room for
+    const int parts = std::max(1, std::min(turns, kWarps / a.n_rows));
+    const unsigned grid = unsigned((static_cast<long long>(a.n_rows) * parts + kKvWarps - 1) / kKvWarps);
     by_type(dtype, hd, [&](auto* t, auto size) {
-        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a, each);
+        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a, parts);
     });
     return launched(call);
 }

@@ -72,6 +72,30 @@ __device__ __forceinline__ RowAt kv_row_at(const KvBatch& b, int row) {
     return r;
 }
 
+// two fp32 numbers in one register pair
+__device__ __forceinline__ unsigned long long two_words(uint32_t a, uint32_t b) {
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
+    return v;
+}
+__device__ __forceinline__ unsigned long long two_floats(float a, float b) { return two_words(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ void floats_of(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+
 // E consecutive elements in 32 bits
 template <int E>
 __device__ __forceinline__ void load_row(const float* p, float (&f)[E]) {

@@ -67,24 +67,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) 
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
         ::PF_W8(r, 0), PF_W8(r, 8), "r"(at) : "memory");
 }
-// two fp32 numbers in one register pair
-__device__ __forceinline__ unsigned long long two_words(uint32_t a, uint32_t b) {
-    unsigned long long v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
-    return v;
-}
-__device__ __forceinline__ unsigned long long two_floats(float a, float b) { return two_words(__float_as_uint(a), __float_as_uint(b)); }
-__device__ __forceinline__ void floats_of(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long v;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
-    return v;
-}
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-    unsigned long long v;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-    return v;
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -229,14 +211,19 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         }
         fence_proxy_async();
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = sh.tmem, t_s = tmem, t_o = tmem + 256;
+    uint32_t tmem = 0, t_s = 0, t_o = 0;
+    auto together = [&] {                        // queries, barriers and tensor memory are there; each role has begun what needs none of them
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        tmem = t_s = sh.tmem;
+        t_o = tmem + 256;
+    };
     const int own_tiles = half == 0 ? tiles0 : tiles1;
 
     if (warp < 8) {
         more_registers<kPfSoftmaxRegs>();
+        together();
         // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
         const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
         float m = -INFINITY, l = 0.f;
@@ -408,6 +395,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
             scales(ks, 0); scales(vs, 1);
             codes(kc, 0); codes(vc, 1);
         }
+        together();
         int e = -1000;                           // E keeps eight times the largest scale of values so far, times 2^-E, below 2^15
         float v_limit = -1.f, by_v = 1.f;        // the largest scale that E allows, 2^-E
         bool ok = true;                          // (a warp that has given up still comes to the others' barrier)
@@ -468,6 +456,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         }
     } else {
         fewer_registers<kPfIssueRegs>();
+        together();
         // ---- products ----
         if (warp == 12) {
             constexpr uint32_t idesc_s = pf_idesc(kPfTile, false), idesc_o = pf_idesc(HD, true);

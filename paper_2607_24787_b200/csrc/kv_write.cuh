@@ -27,7 +27,7 @@ struct WriteArgs {
 // A lane holds eight consecutive elements of a head, HD / 8 lanes a head, so a warp takes 32 / (HD / 8) heads at once.
 //
 // The norm and the rotation decide between 4-bit codes, so their roundings are spelled out: every product and sum is rounded by itself
-// (nothing is contracted), the norm's sum is taken in 64 bits, and so are the angles.
+// (in pairs, nothing is contracted), the norm's sum is taken in 64 bits, and so are the angles.
 
 // 1 / sqrt(v): Newton's step from the fp32 instruction's 22 bits leaves more than 40 (the double division and root take four times the
 // rest of the kernel)
@@ -38,15 +38,20 @@ __device__ __forceinline__ float rsqrt_of(double v) {
 }
 
 // Cosines and sines of a row's pairs. Lane `sub` of the first halves turns pairs 8 sub .. 8 sub + 7 (with neighbours: pairs 4 sub .. 4 sub + 3),
-// lane sub + rot_dim / 16 their second halves; entry [j][i] holds pairs 8 i + 2 j and 8 i + 2 j + 1, so that lanes read side by side. The
+// lane sub + rot_dim / 16 their second halves; entry [j][i] holds the cosines, then the sines, of pairs
+// 8 i + 2 j and 8 i + 2 j + 1, so that lanes read side by side. The
 // second table has the sines' signs turned: a first half is a cos + b (-sin), rounded as a cos - b sin is.
 template <int HD>
 struct Angles { float4 at[2][4][HD / 16]; };
 template <int HD>
 __device__ __forceinline__ void set_angle(Angles<HD>& t, int pair, float c, float s) {
     const int j = pair % 8 / 2, i = pair / 8, odd = pair & 1;
-    reinterpret_cast<float2*>(&t.at[0][j][i])[odd] = make_float2(c, s);
-    reinterpret_cast<float2*>(&t.at[1][j][i])[odd] = make_float2(c, -s);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        float* to = reinterpret_cast<float*>(&t.at[k][j][i]) + odd;
+        to[0] = c;
+        to[2] = k ? -s : s;
+    }
 }
 
 // Norm (with gammas g) and rotation of eight elements a lane
@@ -60,8 +65,9 @@ __device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Angles<HD
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const float inv = rsqrt_of(sum * (1. / HD) + double(a.eps));
+        const unsigned long long inv2 = two_floats(inv, inv);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], inv), g[e]);
+        for (int e = 0; e < 8; e += 2) floats_of(mul2(mul2(two_floats(x[e], x[e + 1]), inv2), two_floats(g[e], g[e + 1])), x[e], x[e + 1]);
     }
     if (a.rot_dim == 0) return;
     if (a.neighbours) {
@@ -70,10 +76,10 @@ __device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Angles<HD
         for (int e = 0; e < 8; e += 4) {
             const float4 v = t.at[0][2 * (sub & 1) + e / 4][sub / 2];
             const float p0 = x[e], q0 = x[e + 1], p1 = x[e + 2], q1 = x[e + 3];
-            x[e] = __fsub_rn(__fmul_rn(p0, v.x), __fmul_rn(q0, v.y));
-            x[e + 1] = __fadd_rn(__fmul_rn(q0, v.x), __fmul_rn(p0, v.y));
-            x[e + 2] = __fsub_rn(__fmul_rn(p1, v.z), __fmul_rn(q1, v.w));
-            x[e + 3] = __fadd_rn(__fmul_rn(q1, v.z), __fmul_rn(p1, v.w));
+            x[e] = __fsub_rn(__fmul_rn(p0, v.x), __fmul_rn(q0, v.z));
+            x[e + 1] = __fadd_rn(__fmul_rn(q0, v.x), __fmul_rn(p0, v.z));
+            x[e + 2] = __fsub_rn(__fmul_rn(p1, v.y), __fmul_rn(q1, v.w));
+            x[e + 3] = __fadd_rn(__fmul_rn(q1, v.y), __fmul_rn(p1, v.w));
         }
         return;
     }
@@ -88,8 +94,7 @@ __device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Angles<HD
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
         const float4 v = at[e / 2 * (HD / 16)];
-        x[e] = __fadd_rn(__fmul_rn(x[e], v.x), __fmul_rn(o[e], v.y));
-        x[e + 1] = __fadd_rn(__fmul_rn(x[e + 1], v.z), __fmul_rn(o[e + 1], v.w));
+        floats_of(add2(mul2(two_floats(x[e], x[e + 1]), two_floats(v.x, v.y)), mul2(two_floats(o[e], o[e + 1]), two_floats(v.z, v.w))), x[e], x[e + 1]);
     }
 }
 
@@ -139,88 +144,71 @@ __device__ __forceinline__ void unpack8(const Raw8& r, float (&x)[8]) {
     }
 }
 
-// A block takes up to kKvWriteRows rows: where they are and all of their angles first. Then a warp goes through the rows with a few heads
-// of one kind at a time (a turn), so that what it has of a head stays in registers; a row is loaded while the one before it is worked on.
-// gridDim.y > 1 (few rows): blocks share the turns.
-constexpr int kKvWriteRows = 8;
+// A warp takes a row, or one of `parts` of its heads: its angles first, then a few heads of one kind at a time (a turn), the next ones loaded
+// meanwhile. Warps share nothing, so that one's angles go along with another's heads.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kKvWarps * 32, 4) kv_write_kernel(const WriteArgs a, int rows_each) {
+__global__ void __launch_bounds__(kKvWarps * 32, 4) kv_write_kernel(const WriteArgs a, int parts) {
     constexpr int LANES = HD / 8, HEADS = 32 / LANES;
-    __shared__ Angles<HD> angles[kKvWriteRows];
-    __shared__ long long blocks[kKvWriteRows];   // of the row's head 0 in the cache; -1: nowhere, -2: no sequence's row
-    __shared__ int toks[kKvWriteRows];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES;
-    const long long row0 = static_cast<long long>(blockIdx.x) * rows_each;
-    const int rows = int(min(static_cast<long long>(rows_each), a.n_rows - row0));
+    __shared__ Angles<HD> angles_of[kKvWarps];
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    Angles<HD>& angles = angles_of[threadIdx.x >> 5];
     // turns: keys, values, queries
     const int kv_turns = (a.kv_heads + HEADS - 1) / HEADS, turns = 2 * kv_turns + (a.q_heads + HEADS - 1) / HEADS;
-    // a turn's rows are cut in `cuts`, so that all warps have work, and about the same
-    const int cuts = min(rows, max(2, 2 * kKvWarps / turns));
-    int task = blockIdx.y * kKvWarps + warp, kind = 0, head = 0, first = 0, end = 0;
-    const T* src = nullptr;
-    Raw8 raw{};
-    auto take = [&] {
-        const int turn = task / cuts, cut = task - turn * cuts;
-        first = rows * cut / cuts; end = rows * (cut + 1) / cuts;
-        kind = turn < kv_turns ? 0 : turn < 2 * kv_turns ? 1 : 2;
-        head = (turn - kind * kv_turns) * HEADS + lane / LANES;
-        const HeadRows& from = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
-        const bool is = turn < turns && head < (kind == 2 ? a.q_heads : a.kv_heads);
-        src = is ? static_cast<const T*>(from.p) + (row0 + first) * from.row + head * from.head + sub * 8 : nullptr;
-        if (is) raw = raw8(src);
-    };
-    take();
-    if (warp < rows) {
-        long long block = -1;
+    const int half = a.rope.rot_dim / 2;
+    float gk[8] = {}, gq[8] = {};
+    if (a.rope.k_gamma && a.kv_heads) load_row<8>(a.rope.k_gamma + sub * 8, gk);
+    if (a.rope.q_gamma && a.q_heads) load_row<8>(a.rope.q_gamma + sub * 8, gq);
+    for (long long task = static_cast<long long>(blockIdx.x) * kKvWarps + (threadIdx.x >> 5); task < static_cast<long long>(a.n_rows) * parts;
+         task += static_cast<long long>(gridDim.x) * kKvWarps) {
+        const int row = int(task / parts), part = int(task - static_cast<long long>(row) * parts);
+        int turn = turns * part / parts;
+        const int end = turns * (part + 1) / parts;
+        int kind = 0, head = 0;
+        bool is = false;
+        Raw8 raw{};
+        auto take = [&] {
+            kind = turn < kv_turns ? 0 : turn < 2 * kv_turns ? 1 : 2;
+            head = (turn - kind * kv_turns) * HEADS + lane / LANES;
+            const HeadRows& from = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
+            is = turn < end && head < (kind == 2 ? a.q_heads : a.kv_heads);
+            if (is) raw = raw8(static_cast<const T*>(from.p) + row * from.row + head * from.head + sub * 8);
+        };
+        take();
+        long long block = -1;                    // of the row's head 0 in the cache; -1: nowhere
         int tok = 0;
         if (a.batch.n_seq >= 0) {
-            const RowAt r = kv_row_at(a.batch, int(row0) + warp);
-            if (r.seq >= a.batch.n_seq) block = -2;
-            else if (r.pos >= 0) {
+            const RowAt r = kv_row_at(a.batch, row);
+            if (r.seq >= a.batch.n_seq) continue;
+            if (r.pos >= 0) {
                 block = kv_block_at<HD>(a.kv, a.batch, r.seq, r.pos, 0);
                 tok = r.pos % kKvBlock;
                 if (block < 0 && lane == 0) kv_note(a.kv, r.pos / a.kv.page_size >= a.batch.stride ? SPM_KV_TOO_LONG : SPM_KV_BAD_PAGE);
             }
         }
-        if (lane == 0) { blocks[warp] = block; toks[warp] = tok; }
-    }
-    const int half = a.rope.rot_dim / 2;
-    for (int j = threadIdx.x; j < rows * half; j += blockDim.x) {
-        const int rr = j / half, p = j - rr * half;
-        const int axis = a.rope.axis_of ? min(int(a.rope.axis_of[p]), a.rope.n_axes - 1) : 0;
-        double s, c;
-        sincos(double(a.rope.positions[axis * a.rope.pos_stride + row0 + rr]) * double(a.rope.inv_freq[p]), &s, &c);
-        set_angle(angles[rr], p, float(c), float(s));
-    }
-    __syncthreads();
-    while (task < turns * cuts) {
-        const float* gamma = kind == 0 ? a.rope.k_gamma : kind == 2 ? a.rope.q_gamma : nullptr;
-        float g[8] = {};
-        if (gamma) load_row<8>(gamma + sub * 8, g);
-        const long long step = (kind == 0 ? a.k : kind == 1 ? a.v : a.q).row;
-        if (kind == 2) {
-            T* dst = static_cast<T*>(a.q_out.p) + (row0 + first) * a.q_out.row + head * a.q_out.head + sub * 8;
-            for (int r = first; r < end; ++r) {
-                float x[8];
-                unpack8<T>(raw, x);
-                if (src && r + 1 < end) raw = raw8(src += step);
-                norm_and_turn<HD>(a.rope, angles[r], gamma != nullptr, g, sub, x);
-                if (src && blocks[r] != -2) store_row<8>(dst, x);
-                dst += a.q_out.row;
-            }
-        } else {
-            unsigned char* at = a.kv.pages + head * static_cast<long long>(a.kv.page_size / kKvBlock) * kv_block_bytes(HD);
-            for (int r = first; r < end; ++r) {
-                float x[8];
-                unpack8<T>(raw, x);
-                if (src && r + 1 < end) raw = raw8(src += step);
-                if (kind == 0) norm_and_turn<HD>(a.rope, angles[r], gamma != nullptr, g, sub, x);
-                const long long block = blocks[r];
-                quantise_row<HD>(a.kv, at + block + kind * kv_v_codes(HD), at + block + kv_k_scales(HD) + kind * HD, toks[r], src && block >= 0, sub, x);
+        __syncwarp();
+        for (int p = lane; p < half; p += 32) {
+            const int axis = a.rope.axis_of ? min(int(a.rope.axis_of[p]), a.rope.n_axes - 1) : 0;
+            double s, c;
+            sincos(double(a.rope.positions[axis * a.rope.pos_stride + row]) * double(a.rope.inv_freq[p]), &s, &c);
+            set_angle(angles, p, float(c), float(s));
+        }
+        __syncwarp();
+        while (turn < end) {
+            float x[8];
+            unpack8<T>(raw, x);
+            const int kind_now = kind, head_now = head;
+            const bool is_now = is;
+            ++turn;
+            take();
+            if (kind_now == 2) {
+                norm_and_turn<HD>(a.rope, angles, a.rope.q_gamma != nullptr, gq, sub, x);
+                if (is_now) store_row<8>(static_cast<T*>(a.q_out.p) + row * a.q_out.row + head_now * a.q_out.head + sub * 8, x);
+            } else {
+                if (kind_now == 0) norm_and_turn<HD>(a.rope, angles, a.rope.k_gamma != nullptr, gk, sub, x);
+                unsigned char* at = a.kv.pages + block + head_now * static_cast<long long>(a.kv.page_size / kKvBlock) * kv_block_bytes(HD);
+                quantise_row<HD>(a.kv, at + kind_now * kv_v_codes(HD), at + kv_k_scales(HD) + kind_now * HD, tok, is_now && block >= 0, sub, x);
             }
         }
-        task += gridDim.y * kKvWarps;
-        take();
     }
 }
 
@@ -233,7 +221,7 @@ struct ReadArgs {
 // A thread takes eight elements of a row, of every head's keys and values, four of them in flight. Neighbouring tokens, whose codes stand
 // side by side, are in one warp.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kKvWarps * 32) kv_read_kernel(const ReadArgs a) {
+__global__ void __launch_bounds__(kKvWarps * 32, 6) kv_read_kernel(const ReadArgs a) {
     constexpr int LANES = HD / 8, ROWS = kKvWarps * 32 / LANES, AHEAD = 4;
     __shared__ long long blocks[ROWS];           // of the row's head 0; -1: nowhere (zeros), -2: no sequence's row
     __shared__ int toks[ROWS];

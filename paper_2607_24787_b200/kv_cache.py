@@ -157,19 +157,25 @@ class KVCache:
             cq = _rows(q, n, q_heads, hd, dtype, device, "q")
             if q_out is None:
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            co = _rows(q_out, n, q_heads, hd, dtype, device, "q_out")
+                co = B.Rows(q_out.data_ptr(), q_heads * hd, hd)
+            else:
+                co = _rows(q_out, n, q_heads, hd, dtype, device, "q_out")
         _enqueue(device, self._lib.spm_kv_write, self.c, batch.c, cr, pos, stride, cq, co, q_heads, ck, cv, dt)
         return q_out
 
     def read(self, batch, dtype=torch.bfloat16, k_out=None, v_out=None):
         """The cache's keys and values at the positions of the batch's new rows: two tensors [rows, kv_heads, head_dim]."""
         n, heads, hd = size = self._size(batch)
-        if k_out is None:
+        if k_out is None and v_out is None:
             k_out = self.pages.new_empty(size, dtype=dtype)
-        if v_out is None:
-            v_out = torch.empty_like(k_out, memory_format=torch.contiguous_format)
-        dt, dtype = _dtype(k_out, "k_out"), k_out.dtype
-        ck, cv = _rows(k_out, n, heads, hd, dtype, self.device, "k_out"), _rows(v_out, n, heads, hd, dtype, self.device, "v_out")
+            v_out = torch.empty_like(k_out)
+            dt = _dtype(k_out, "dtype")
+            ck, cv = B.Rows(k_out.data_ptr(), heads * hd, hd), B.Rows(v_out.data_ptr(), heads * hd, hd)
+        else:
+            have = v_out if k_out is None else k_out
+            k_out, v_out = (torch.empty_like(have, memory_format=torch.contiguous_format) if x is None else x for x in (k_out, v_out))
+            dt, dtype = _dtype(have, "k_out, v_out"), have.dtype
+            ck, cv = _rows(k_out, n, heads, hd, dtype, self.device, "k_out"), _rows(v_out, n, heads, hd, dtype, self.device, "v_out")
         _enqueue(self.device, self._lib.spm_kv_read, self.c, batch.c, ck, cv, dt)
         return k_out, v_out
 
@@ -182,7 +188,9 @@ class KVCache:
         cq = _rows(q, n, heads, hd, dtype, device, "q")
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        co = _rows(out, n, heads, hd, dtype, device, "out")
+            co = B.Rows(out.data_ptr(), heads * hd, hd)
+        else:
+            co = _rows(out, n, heads, hd, dtype, device, "out")
         key = (batch.shape, heads, dt)
         size = self._workspace.get(key)
         if size is None:
@@ -202,6 +210,8 @@ def rotate_heads(x, positions, rope, out=None):
     cx = _rows(x, n, heads, hd, x.dtype, device, "x")
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    cy = _rows(out, n, heads, hd, x.dtype, device, "out")
+        cy = B.Rows(out.data_ptr(), heads * hd, hd)
+    else:
+        cy = _rows(out, n, heads, hd, x.dtype, device, "out")
     _enqueue(device, B.load().spm_rotate_heads, c, pos, stride, cx, cy, n, heads, hd, dt)
     return out
