@@ -518,8 +518,9 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
 
 /* out = softmax(scale * q K^T) V for each new row and each of its n_q_heads heads (a multiple of n_kv_heads: query head h reads cache head
  * h / (n_q_heads / n_kv_heads)), over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's
- * statistics and all sums are fp32; bf16 calls round probabilities (and many-row calls the cache's values) once to 16 bits for the tensor
- * cores. Results do not depend on the order in which CTAs run.
+ * statistics and all sums are fp32. bf16 calls round a probability, times its value's scale, once to bf16, or (calls of many rows) a
+ * probability, a key and a value once each to fp16; fp32 calls round nothing but their sums. bf16 queries are below 2^63 in magnitude.
+ * out may not overlap q. Results do not depend on the order in which CTAs run, and are the same bits for the same call.
  * workspace: dev, 16-byte aligned, at least spm_kv_attend_workspace() bytes; what it held before does not matter, and calls that may run
  * at the same time need one each. */
 int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, int n_q_heads, int dtype, size_t* bytes);
@@ -533,7 +534,8 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
 typedef struct {
     const spm_kv_cache* caches;     /* HOST [L]: a cache a layer, all of one shape; copied                                        */
     spm_kv_batch batch;             /* page_table, lengths, n_seq (>= every nb), table_stride; the rest is not read. Before a step
-                                       the caller counts its new token in `lengths` (device memory, read by the step's kernels)   */
+                                       the caller counts its new token in `lengths`, ahead of the step on the compute stream or
+                                       synchronised with it (device memory, read by the step's kernels)                           */
     spm_rope rope;                  /* q_gamma, k_gamma: dev [L][head_dim] or NULL                                               */
     const int32_t* positions;       /* dev [n_axes][pos_stride]: of the step's rows, set before a step like `lengths`            */
     int64_t pos_stride;

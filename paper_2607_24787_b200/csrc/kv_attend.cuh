@@ -57,8 +57,8 @@ struct AtShape {
     __device__ static float odd(float both, float low) { return raw ? (both - low) * (1.f / 16.f) : both; }
     static constexpr int ring_bytes = stages * tile_bytes;
     static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
-    static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8) + (n_seq > 64 ? n_seq * 4 : 0); }
-    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 4 + 10 * 1024 <= 232448, "227 KB");
+    static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8) + (n_seq > 64 ? n_seq * 8 : 0); }
+    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 8 + (raw ? 9728 : 4608) <= 232448, "227 KB, the last of it for the kernel's own arrays");
 };
 
 // A walk along the line of tiles. nk: tokens that the last of the item's columns sees, nt: tiles (one at least, so that rows that see
@@ -82,14 +82,14 @@ struct Walk {
         nt = max(1, (nk + kAtTile - 1) / kAtTile);
     }
     // tiles of all heads of column blocks `from`, `from` + `step`, ...
-    __device__ __forceinline__ int tiles_of_sequence(const AttendArgs& a, int from, int step) {
-        int sum = 0;
+    __device__ __forceinline__ long long tiles_of_sequence(const AttendArgs& a, int from, int step) {
+        long long sum = 0;
         const int m = blocks(a);
         for (ct = from; ct < m; ct += step) { columns(a); sum += nt; }
         return sum * a.kv.heads;
     }
     // to tile `rest` of sequence `s`, by a warp: lanes look at 32 column blocks at a time
-    __device__ __forceinline__ void seek(const AttendArgs& a, int s, int rest) {
+    __device__ __forceinline__ void seek(const AttendArgs& a, int s, long long rest) {
         const int lane = threadIdx.x & 31;
         seq = s;
         load(a);
@@ -97,11 +97,11 @@ struct Walk {
         for (int ct0 = 0; m > 1; ct0 += 32) {
             ct = ct0 + lane;
             columns(a);
-            const int own = ct < m ? nt * a.kv.heads : 0;
-            int upto = own;
+            const long long own = ct < m ? static_cast<long long>(nt) * a.kv.heads : 0;
+            long long upto = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
                 if (lane >= o) upto += v;
             }
             const int behind = __popc(__ballot_sync(0xffffffffu, upto <= rest));
@@ -114,8 +114,8 @@ struct Walk {
         }
         if (m <= 1) ct = 0;
         columns(a);
-        head = rest / nt;
-        t = rest - head * nt;
+        head = int(rest / nt);
+        t = int(rest - static_cast<long long>(head) * nt);
     }
     __device__ __forceinline__ void next(const AttendArgs& a) {
         if (++t < nt) return;
@@ -141,7 +141,7 @@ __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int
     return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
 }
 
-struct PartMeta { int id, ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
+struct PartMeta { long long id; int ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -216,11 +216,11 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     float* own_part = reinterpret_cast<float*>(smem + W * S::ring_bytes + warp * S::part_bytes);
     unsigned char* rest = smem + W * (S::ring_bytes + S::part_bytes);
     const uint32_t bars = smem_u32(rest) + warp * STAGES * 8;
-    int* before = reinterpret_cast<int*>(rest + W * STAGES * 8);
+    long long* before = reinterpret_cast<long long*>(rest + W * STAGES * 8);      // tiles before each sequence, where there are many of these
     __shared__ PartMeta meta[2 * W];
     __shared__ Walk<COLS> copied[W], used[W];      // the items that a warp's copies and its sums are at
     __shared__ float4 starts[RAW ? W : 1][G][4];   // -8 times the sum of a group's queries, as the product's C for columns 2 c, 2 c + 1
-    __shared__ int warp_sum_of[W];
+    __shared__ long long warp_sum_of[W];
     __shared__ float weight[2 * W][COLS], total[2 * W][COLS], highest[2 * W][COLS];
 
     if (lane == 0) {
@@ -231,33 +231,35 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     __syncwarp();
     // ---- the line of tiles: how many there are, and before each sequence. Up to 64 sequences are two a lane, in every warp for itself ----
     const int n_seq = a.batch.n_seq;
-    int all = 0, before0 = 0, before1 = 0;
+    long long all = 0, before0 = 0, before1 = 0;
     auto count_tiles = [&](int s) {
         Walk<COLS> w;
         w.seq = s;
         w.load(a);
         if (w.n > 0 && w.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-        return w.blocks(a) <= kAtFewBlocks ? w.tiles_of_sequence(a, 0, 1) : -1;
+        return w.blocks(a) <= kAtFewBlocks ? w.tiles_of_sequence(a, 0, 1) : -1ll;
     };
     // sequences of many column blocks: their lanes' counts come back as -1, and the warp counts together
-    auto count_many = [&](int k, int s) {
+    auto count_many = [&](long long k, int s) {
         for (uint32_t left = __ballot_sync(0xffffffffu, k < 0); left; left &= left - 1) {
             const int owner = __ffs(left) - 1;
             Walk<COLS> w;
             w.seq = __shfl_sync(0xffffffffu, s, owner);
             w.load(a);
-            const int sum = __reduce_add_sync(0xffffffffu, w.tiles_of_sequence(a, lane, 32));
+            long long sum = w.tiles_of_sequence(a, lane, 32);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == owner) k = sum;
         }
         return k;
     };
     if (n_seq <= 64) {
-        const int k0 = count_many(2 * lane < n_seq ? count_tiles(2 * lane) : 0, 2 * lane);
-        const int k1 = count_many(2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0, 2 * lane + 1);
-        int upto = k0 + k1;
+        const long long k0 = count_many(2 * lane < n_seq ? count_tiles(2 * lane) : 0ll, 2 * lane);
+        const long long k1 = count_many(2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0ll, 2 * lane + 1);
+        long long upto = k0 + k1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += v;
         }
         all = __shfl_sync(0xffffffffu, upto, 31);
@@ -265,22 +267,22 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         before1 = upto - k1;
     } else {
         const int each = (n_seq + W * 32 - 1) / (W * 32);
-        int mine = 0;
+        long long mine = 0;
         for (int i = 0; i < each; ++i) {
             const int s = tid * each + i;
-            const int k = count_many(s < n_seq ? count_tiles(s) : 0, s);
+            const long long k = count_many(s < n_seq ? count_tiles(s) : 0ll, s);
             if (s < n_seq) before[s] = mine;
             mine += k;
         }
-        int upto = mine;
+        long long upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += v;
         }
         if (lane == 31) warp_sum_of[warp] = upto;
         __syncthreads();
-        int off = upto - mine;
+        long long off = upto - mine;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             if (w < warp) off += warp_sum_of[w];
@@ -292,12 +294,10 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     }
     grid_dep_launch();
 
-    const int ctas = max(1, min(int(gridDim.x), (all + a.min_tiles - 1) / a.min_tiles)), cta = blockIdx.x;
-    const int cta_lo = cta < ctas ? int(static_cast<long long>(all) * cta / ctas) : all;
-    const int cta_hi = cta < ctas ? int(static_cast<long long>(all) * (cta + 1) / ctas) : all;
-    const int lo = cta_lo + int(static_cast<long long>(cta_hi - cta_lo) * warp / W);
-    const int hi = cta_lo + int(static_cast<long long>(cta_hi - cta_lo) * (warp + 1) / W);
-    const int count = hi - lo;
+    const int ctas = all >= static_cast<long long>(gridDim.x) * a.min_tiles ? int(gridDim.x) : max(1, (int(all) + a.min_tiles - 1) / a.min_tiles), cta = blockIdx.x;
+    const long long cta_lo = cta < ctas ? all * cta / ctas : all, cta_hi = cta < ctas ? all * (cta + 1) / ctas : all;
+    const long long lo = cta_lo + (cta_hi - cta_lo) * warp / W;
+    const int count = int(cta_lo + (cta_hi - cta_lo) * (warp + 1) / W - lo);
 
     float m[2], l[2], y[G][2][4];
     uint32_t qf[QP][G][4];
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             Walk<COLS> at;
             if (n_seq <= 64) {
                 const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
-                const int b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
+                const long long b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
                 at.seek(a, s, lo - (s & 1 ? b1 : b0));
             } else {
                 int s = 0, end = n_seq;          // the last sequence with before[s] <= lo
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
 
     // ---- parts of one item in this CTA meet: they stand one after another. Every warp sees which parts belong together (lane j: part j);
     // first a warp takes a column of an item for the parts' weights, then threads take sums ----
-    const int id = lane < 2 * W ? meta[lane].id : -1;
+    const long long id = lane < 2 * W ? meta[lane].id : -1;
     const uint32_t mates = __match_any_sync(0xffffffffu, id);
     const uint32_t leaders = __ballot_sync(0xffffffffu, id >= 0 && (mates & ((1u << lane) - 1)) == 0);
     auto part_of = [&](int j) { return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes); };

@@ -264,6 +264,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     if (int rc = check_rows(call, "q", q, dtype)) return rc;
     if (int rc = check_rows(call, "out", out, dtype)) return rc;
+    if (static_cast<long long>(batch->n_rows) * n_q_heads > INT32_MAX) return fail(call, SPM_ERR_INVALID_ARG, "n_rows * n_q_heads is over 2^31 - 1");
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < attend_bytes(kv->head_dim))
         return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(attend_bytes(kv->head_dim)) + " bytes");
     int dev = 0, sms = 0;

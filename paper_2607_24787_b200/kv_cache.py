@@ -149,6 +149,8 @@ class KVCache:
         cq = co = cr = pos = None
         stride = q_heads = 0
         if rope is not None:
+            if rope.device != device:
+                raise ValueError("the rope is on another device than the cache")
             cr, pos, stride = rope._with(positions, n, hd, q is not None, True)
         if q is not None:
             if rope is None or q.dim() != 3:

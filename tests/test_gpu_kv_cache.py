@@ -547,6 +547,26 @@ def test_refusals(kv):
             pytest.fail(f"call {i} was taken")
 
 
+@pytest.mark.parametrize("rows,heads", [([1, 1], 8), ([300, 270], 16)])
+def test_pages_beyond_32_bits(kv, rows, heads):
+    """A pool of over 4 GB, sequences in its last pages: written, read, attended as in a small one."""
+    small = Case(kv, 25, [300, 270], rows, 2, 128, 64, BF16, fill=True)
+    n, need = 61_000, small.start.shape[0]                  # 61000 pages of 2 * 4 * 2304 bytes and some
+    pages = torch.empty(n * 4, 2, 4, 18 * 128, dtype=torch.uint8, device="cuda")
+    assert pages.numel() > 2 ** 32
+    pages[-need:] = small.cache.pages
+    table = torch.where(small.table >= 0, small.table + (pages.shape[0] - need), small.table).to(torch.int32).cuda()
+    big = kv.KVCache(pages)
+    batch = kv.KVBatch(table, small.dev_lengths, small.batch._keep[2], n_rows=small.n_rows, max_rows=max(rows))
+    k, v = small.randn(small.n_rows, 2, 128), small.randn(small.n_rows, 2, 128)
+    q = small.randn(small.n_rows, heads, 128)
+    for cache, b in ((small.cache, small.batch), (big, batch)):
+        cache.write(b, k, v)
+    assert torch.equal(pages[-need:], small.cache.pages)
+    assert all(torch.equal(x, y) for x, y in zip(big.read(batch), small.cache.read(small.batch)))
+    assert torch.equal(big.attend(batch, q), small.cache.attend(small.batch, q))
+
+
 def test_nothing_to_do(kv):
     c = Case(kv, 16, [20], [0], 2, 128, 16, BF16, pad_rows=2, fill=True)
     q = c.randn(2, 4, 128)

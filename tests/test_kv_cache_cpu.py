@@ -114,6 +114,7 @@ def test_calls_that_are_refused(B):
     need = B.spm_kv_attend_workspace(kv, b, 8, SPM_BF16)
     for at, size in ((None, need), (AT + 8, need), (AT, need - 1), (AT, 0)):
         refused(B, INVALID, lambda: B.spm_kv_attend(kv, b, x, 8, x, 1.0, SPM_BF16, at, size))
+    refused(B, INVALID, lambda: B.spm_kv_attend(kv, batch(B, n_rows=1 << 28), x, 16, x, 1.0, SPM_BF16, AT, 1 << 40))      # 2^32 columns
     for heads in (0, -2, 3):
         refused(B, CONFIG, lambda: B.spm_kv_attend(kv, b, x, heads, x, 1.0, SPM_BF16, AT, 1 << 40))
         refused(B, CONFIG, lambda: B.spm_kv_attend_workspace(kv, b, heads, SPM_BF16))
