@@ -229,6 +229,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         meta[2 * warp].id = meta[2 * warp + 1].id = -1;
     }
     __syncwarp();
+    grid_dep_wait();
+    grid_dep_launch();
     // ---- the line of tiles: how many there are, and before each sequence. Up to 64 sequences are two a lane, in every warp for itself ----
     const int n_seq = a.batch.n_seq;
     long long all = 0, before0 = 0, before1 = 0;
@@ -292,7 +294,6 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             if (tid * each + i < n_seq) before[tid * each + i] += off;
         __syncthreads();
     }
-    grid_dep_launch();
 
     const int ctas = all >= static_cast<long long>(gridDim.x) * a.min_tiles ? int(gridDim.x) : max(1, (int(all) + a.min_tiles - 1) / a.min_tiles), cta = blockIdx.x;
     const long long cta_lo = cta < ctas ? all * cta / ctas : all, cta_hi = cta < ctas ? all * (cta + 1) / ctas : all;
@@ -703,6 +704,7 @@ __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const At
     constexpr int COLS = S::cols, FLOATS = S::part_floats, SETS = kAtJoinThreads / HD;
     __shared__ float tops[SETS], sums[SETS], rows[SETS][HD];
     grid_dep_wait();
+    grid_dep_launch();
     const int cta = blockIdx.x, col = blockIdx.y, d = threadIdx.x % HD, set = threadIdx.x / HD;
     const int4 join = *reinterpret_cast<const int4*>(a.joins + 8 * cta);
     const int n = a.joins[8 * cta + 4];

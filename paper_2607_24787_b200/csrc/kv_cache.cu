@@ -23,10 +23,6 @@ int fail(const char* call, int code, const std::string& msg) {
     set_thread_error(std::string(call) + ": " + msg);
     return code;
 }
-int launched(const char* call) {
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
-}
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 int check_dtype(const char* call, int dtype) {
@@ -97,6 +93,27 @@ void by_type(int dtype, int hd, F f) {
     else size(static_cast<float*>(nullptr));
 }
 
+// Launched so that its CTAs may be in place before the stream's kernel before it has ended: every kernel here waits for that one before it
+// reads or writes anything, and lets its own successor do the same.
+template <typename... A, typename... B>
+cudaError_t launch_early(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const B&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, A(args)...);
+}
+int launched(const char* call, cudaError_t e) {
+    if (e != cudaSuccess) cudaGetLastError();
+    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
+}
+
 int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaStream_t st) {
     const int heads = 2 * a.kv_heads + a.q_heads;
     if (a.n_rows == 0 || heads == 0) return SPM_OK;
@@ -105,10 +122,11 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
     constexpr int kWarps = 592 * kKvWarps;       // that the GPU has room for
     const int parts = std::max(1, std::min(turns, kWarps / a.n_rows));
     const unsigned grid = unsigned((static_cast<long long>(a.n_rows) * parts + kKvWarps - 1) / kKvWarps);
+    cudaError_t e = cudaSuccess;
     by_type(dtype, hd, [&](auto* t, auto size) {
-        kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, st>>>(a, parts);
+        e = launch_early(kv_write_kernel<std::remove_pointer_t<decltype(t)>, size.value>, grid, kKvWarps * 32, 0, st, a, parts);
     });
-    return launched(call);
+    return launched(call, e);
 }
 
 size_t attend_bytes(int hd) { return kAtMaxCtas * (32 + 2 * size_t(8) * (hd + 2) * 4); }
@@ -130,20 +148,8 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     cudaError_t e = allow_smem<kv_attend_kernel<T, HD>>(dev, S::smem(SPM_KV_MAX_SEQS));
     if (e != cudaSuccess) return e;
     const int ctas = std::min(sms, kAtMaxCtas);
-    kv_attend_kernel<T, HD><<<ctas, S::warps * 32, S::smem(a.batch.n_seq), st>>>(a);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    // launched ahead of the first kernel's end, which it waits for: its blocks are in place when the parts are
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(ctas, S::cols);
-    cfg.blockDim = dim3(kAtJoinThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv_attend_join_kernel<T, HD>, a);
+    e = launch_early(kv_attend_kernel<T, HD>, ctas, S::warps * 32, S::smem(a.batch.n_seq), st, a);
+    return e == cudaSuccess ? launch_early(kv_attend_join_kernel<T, HD>, dim3(ctas, S::cols), kAtJoinThreads, 0, st, a) : e;
 }
 
 // Which of the two kernels a call's rows are for. Per token of context the tensor-core kernel takes 17 ns a round of CTAs (an SM does 256
@@ -162,8 +168,7 @@ cudaError_t launch_prefill(const AttendArgs& a, int dev, cudaStream_t st) {
     // as many CTAs as there can be items: full ones of all rows, and one a sequence that is not full
     const long long items = (static_cast<long long>(a.batch.n_rows) * a.group / kPfCols + a.batch.n_seq) * a.kv.heads;
     if (items > INT32_MAX) return cudaErrorInvalidValue;
-    kv_prefill_kernel<HD><<<unsigned(items), kPfThreads, PfShape<HD>::smem, st>>>(a);
-    return cudaGetLastError();
+    return launch_early(kv_prefill_kernel<HD>, unsigned(items), kPfThreads, PfShape<HD>::smem, st, a);
 }
 
 }  // namespace
@@ -237,10 +242,11 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
     if (v_out) { if (int rc = check_rows(call, "v_out", v_out, dtype)) return rc; a.v = rows_of(v_out); }
     const int each = kKvWarps * 32 / (kv->head_dim / 8);
     const unsigned grid = unsigned((static_cast<long long>(batch->n_rows) + each - 1) / each);
+    cudaError_t e = cudaSuccess;
     by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
-        kv_read_kernel<std::remove_pointer_t<decltype(t)>, size.value><<<grid, kKvWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+        e = launch_early(kv_read_kernel<std::remove_pointer_t<decltype(t)>, size.value>, grid, kKvWarps * 32, 0, static_cast<cudaStream_t>(stream), a);
     });
-    return launched(call);
+    return launched(call, e);
 }
 
 int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, int n_q_heads, int dtype, size_t* bytes) {
@@ -293,7 +299,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
         a.min_tiles = AtShape<T, size.value>::warps;
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
     });
-    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
+    return launched(call, e);
 }
 
 }  // extern "C"

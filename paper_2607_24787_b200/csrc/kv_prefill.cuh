@@ -110,6 +110,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvBatch& b = a.batch;
 
+    grid_dep_wait();
+    grid_dep_launch();
     // ---- which item: sequences one after another, a sequence's last (longest) columns first, heads together ----
     const int head = blockIdx.x % a.kv.heads;
     int block = blockIdx.x / a.kv.heads, seq = 0, first = 0, n = 0, blocks = 0;

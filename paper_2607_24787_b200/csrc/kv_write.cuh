@@ -2,6 +2,7 @@
 #pragma once
 
 #include "kv_cache.cuh"
+#include "ptx.cuh"
 
 namespace spm {
 
@@ -152,6 +153,8 @@ __global__ void __launch_bounds__(kKvWarps * 32, 4) kv_write_kernel(const WriteA
     __shared__ Angles<HD> angles_of[kKvWarps];
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     Angles<HD>& angles = angles_of[threadIdx.x >> 5];
+    grid_dep_wait();
+    grid_dep_launch();
     // turns: keys, values, queries
     const int kv_turns = (a.kv_heads + HEADS - 1) / HEADS, turns = 2 * kv_turns + (a.q_heads + HEADS - 1) / HEADS;
     const int half = a.rope.rot_dim / 2;
@@ -227,6 +230,8 @@ __global__ void __launch_bounds__(kKvWarps * 32, 6) kv_read_kernel(const ReadArg
     __shared__ int toks[ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long row0 = static_cast<long long>(blockIdx.x) * ROWS;
+    grid_dep_wait();
+    grid_dep_launch();
     const int rows = int(min(static_cast<long long>(ROWS), a.batch.n_rows - row0));
     for (int i = warp; i < rows; i += kKvWarps) {
         const RowAt r = kv_row_at(a.batch, int(row0) + i);
