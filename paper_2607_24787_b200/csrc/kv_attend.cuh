@@ -29,7 +29,6 @@ struct AttendArgs {
     HeadRows q, out;
     int group;                  // query heads a cache head
     int page_shift;             // blocks a page are 1 << page_shift, or -1
-    int min_tiles;              // of a CTA, before another one starts
     float scale;
     float* parts;               // [2 * CTAs][part floats]
     int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns, head, first row, rows
@@ -38,6 +37,7 @@ struct AttendArgs {
 
 constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
+constexpr int kAtMinTiles = 4;  // of a CTA, before another one starts: a tile a scheduler (16, one a warp: 1025 tokens 11.8 us, 9.7 with 4)
 constexpr int kAtFewBlocks = 8; // column blocks of a sequence that a lane counts by itself
 constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
 
@@ -211,7 +211,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     constexpr bool RAW = S::raw;
     constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = QP;        // parts of a query, of a probability
     extern __shared__ __align__(128) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+    // pieces of a line go round the SM's four schedulers a quarter of the warps apart, so that a CTA of a few tiles uses all four
+    const int tid = threadIdx.x, lane = tid & 31, place = tid >> 5, warp = (place & 3) * (W / 4) + (place >> 2), r = lane >> 2, c = lane & 3;
     unsigned char* ring = smem + warp * S::ring_bytes;
     float* own_part = reinterpret_cast<float*>(smem + W * S::ring_bytes + warp * S::part_bytes);
     unsigned char* rest = smem + W * (S::ring_bytes + S::part_bytes);
@@ -282,12 +283,12 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             const long long v = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += v;
         }
-        if (lane == 31) warp_sum_of[warp] = upto;
+        if (lane == 31) warp_sum_of[place] = upto;
         __syncthreads();
         long long off = upto - mine;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            if (w < warp) off += warp_sum_of[w];
+            if (w < place) off += warp_sum_of[w];
             all += warp_sum_of[w];
         }
         for (int i = 0; i < each; ++i)
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         __syncthreads();
     }
 
-    const int ctas = all >= static_cast<long long>(gridDim.x) * a.min_tiles ? int(gridDim.x) : max(1, (int(all) + a.min_tiles - 1) / a.min_tiles), cta = blockIdx.x;
+    const int ctas = all >= static_cast<long long>(gridDim.x) * kAtMinTiles ? int(gridDim.x) : max(1, (int(all) + kAtMinTiles - 1) / kAtMinTiles), cta = blockIdx.x;
     const long long cta_lo = cta < ctas ? all * cta / ctas : all, cta_hi = cta < ctas ? all * (cta + 1) / ctas : all;
     const long long lo = cta_lo + (cta_hi - cta_lo) * warp / W;
     const int count = int(cta_lo + (cta_hi - cta_lo) * (warp + 1) / W - lo);

@@ -296,7 +296,6 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
         e = kv->head_dim == 64 ? launch_prefill<64>(a, dev, static_cast<cudaStream_t>(stream)) : launch_prefill<128>(a, dev, static_cast<cudaStream_t>(stream));
     else by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
-        a.min_tiles = AtShape<T, size.value>::warps;
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
     });
     return launched(call, e);
