@@ -94,10 +94,17 @@ struct PfShared {
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
     uint32_t tmem;
     int quit;                                    // a wait has run out: everybody leaves
+    int rb, seq, first, n, len;                  // the item: its columns, its sequence's rows and tokens
     int exps[4];                                 // E of a tile, and whether its keys are times 2^-4 (bit 16)
     int widest[4], widest_key[4];                // an operand warp's largest scale of a tile's values and keys, as fp32 bits
     uint32_t there[4][4];                        // which tokens of a tile exist
 };
+
+// 16 bytes to shared memory, or zeros, without a register on the way; then: this thread's have arrived.
+__device__ __forceinline__ void copy16_or_zero(uint32_t at, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 template <int HD>
 __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendArgs a) {
@@ -112,46 +119,57 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 
     grid_dep_wait();
     grid_dep_launch();
-    // ---- which item: sequences one after another, a sequence's last (longest) columns first, heads together ----
-    const int head = blockIdx.x % a.kv.heads;
-    int block = blockIdx.x / a.kv.heads, seq = 0, first = 0, n = 0, blocks = 0;
-    for (int s0 = 0; s0 < b.n_seq; s0 += 32) {   // (every warp for itself)
-        const int s = s0 + lane;
-        int f = s, m = s < b.n_seq ? 1 : 0;
-        if (b.row_start && s < b.n_seq) {
-            f = b.row_start[s];
-            m = min(b.row_start[s + 1] - f, b.n_rows);
-        }
-        const int own = m > 0 ? int((static_cast<long long>(m) * a.group + kPfCols - 1) / kPfCols) : 0;
-        int upto = own;
+    // ---- which item, heads together. Up to 32 sequences: those of the most tokens first, so that what is left at the end is short; more:
+    // one sequence after another, its last (longest) columns first. A warp searches, others prepare what all items need ----
+    const int head = blockIdx.x % a.kv.heads, cap = b.stride * a.kv.page_size;
+    if (warp == 13) {
+        int block = blockIdx.x / a.kv.heads;
+        if (lane == 0) sh.n = 0;
+        for (int s0 = 0; s0 < b.n_seq; s0 += 32) {
+            const int s = s0 + lane;
+            int f = s, m = s < b.n_seq ? 1 : 0;
+            if (b.row_start && s < b.n_seq) {
+                f = b.row_start[s];
+                m = max(0, min(b.row_start[s + 1] - f, b.n_rows));
+            }
+            const int len = s < b.n_seq ? b.lengths[s] : 0, tokens = max(0, min(len, cap));
+            const int own = (m * a.group + kPfCols - 1) / kPfCols;               // (a call's rows times heads fit)
+            auto running = [&](int v) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const int behind = __popc(__ballot_sync(0xffffffffu, upto <= block));
-        if (behind < 32) {
-            seq = s0 + behind;
-            block -= __shfl_sync(0xffffffffu, upto - own, behind);
-            blocks = __shfl_sync(0xffffffffu, own, behind);
-            first = __shfl_sync(0xffffffffu, f, behind);
-            n = __shfl_sync(0xffffffffu, m, behind);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int w = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += w;
+                }
+                return v;
+            };
+            int before = running(own) - own;
+            const int all = __shfl_sync(0xffffffffu, before + own, 31);
+            if (block >= all) { block -= all; continue; }
+            int ours = own, skip = 0;            // of this sequence's items, longest first: `ours` after `skip`
+            if (b.n_seq <= 32) {
+                // items whose first row sees `t` tokens and more
+                auto at_least = [&](int t) {
+                    if (t <= 0) return own;
+                    if (t > tokens) return 0;
+                    return max(0, own - int(unsigned(max(0, min(t - 1 - (len - m), m)) * a.group + kPfCols - 1) / kPfCols));
+                };
+                int low = 0, high = __reduce_max_sync(0xffffffffu, tokens) + 1;  // `low`: the most tokens that more than `block` items have
+                while (high - low > 1) {
+                    const int mid = low + (high - low) / 2;
+                    if (__reduce_add_sync(0xffffffffu, at_least(mid)) > block) low = mid; else high = mid;
+                }
+                skip = at_least(low + 1);
+                ours = at_least(low) - skip;
+                block -= __reduce_add_sync(0xffffffffu, skip);
+                before = running(ours) - ours;
+            }
+            if (before <= block && block < before + ours) {
+                sh.rb = own - 1 - skip - (block - before);
+                sh.seq = s; sh.first = f; sh.n = m; sh.len = len;
+            }
             break;
         }
-        block -= __shfl_sync(0xffffffffu, upto, 31);
     }
-    if (blocks == 0) return;                     // more CTAs than items
-    const int rb = blocks - 1 - block;
-    const int len = b.lengths[seq];
-    const int cap = b.stride * a.kv.page_size;
-    if (len > cap && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
-    // tiles of a half: up to the token that its last row sees
-    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x / a.group) + 1, cap)); };
-    const bool used1 = rb * kPfCols + kPfTile < n * a.group;
-    const int tiles0 = (sees(rb * kPfCols + kPfTile - 1) + kPfTile - 1) / kPfTile;
-    const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kPfTile - 1) / kPfTile : 0;
-    const int tiles = max(tiles0, tiles1);
-
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 128); mbar_init(smem_u32(&sh.v_full[i]), 128);
@@ -162,6 +180,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         fence_barrier_init();
     }
     if (warp == 12) tmem_alloc(smem_u32(&sh.tmem), 512);
+    __syncthreads();
+    const int rb = sh.rb, seq = sh.seq, first = sh.first, n = sh.n, len = sh.len;
+    if (n == 0) {                                // more CTAs than items
+        tc_fence_before();
+        if (warp == 12) tmem_dealloc(sh.tmem, 512);
+        return;
+    }
+    if (len > cap && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+    // tiles of a half: up to the token that its last row sees
+    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x / a.group) + 1, cap)); };
+    const bool used1 = rb * kPfCols + kPfTile < n * a.group;
+    const int tiles0 = (sees(rb * kPfCols + kPfTile - 1) + kPfTile - 1) / kPfTile;
+    const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kPfTile - 1) / kPfTile : 0;
+    const int tiles = max(tiles0, tiles1);
 
     auto wait = [&](const unsigned long long& bar, int parity) {
         const uint32_t at = smem_u32(&bar);
@@ -180,7 +212,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         }
     };
 
-    // ---- queries: a softmax thread brings its row ----
+    // ---- queries: a softmax warp brings its 32 rows, HD / 8 lanes a row; then a lane has a row (swizzled as the operand is: no two lanes
+    // of a quarter meet in a bank) ----
+    constexpr int LANES = HD / 8, AT_ONCE = 32 / LANES;
     const int half = warp >> 2, row_in = tid & 127;             // (softmax warps: 0 - 3, 4 - 7)
     int row = -1, g = 0, limit = 0;
     float f = 1.f;
@@ -190,13 +224,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         if (i < n && first + i >= 0 && first + i < b.n_rows) row = first + i;
         limit = sees(x);
         if (i >= n) limit = 0;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + row * a.q.row + (head * a.group + g) * a.q.head;
-        uint4 v[HD / 8];
-        uint32_t top = 0;                        // largest magnitude, as bf16 bits
-#pragma unroll
-        for (int ch = 0; ch < HD / 8; ++ch) {
-            v[ch] = row >= 0 ? *reinterpret_cast<const uint4*>(src + ch * 8) : make_uint4(0, 0, 0, 0);
-            const uint32_t w[4] = {v[ch].x, v[ch].y, v[ch].z, v[ch].w};
+        const __nv_bfloat16* src = row < 0 ? nullptr : static_cast<const __nv_bfloat16*>(a.q.p) + row * a.q.row + (head * a.group + g) * a.q.head;
+        const uint32_t to = q_at + half * S::op_bytes;
+#pragma unroll 4
+        for (int k = 0; k < LANES; ++k) {
+            const auto* from = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * AT_ONCE + lane / LANES));
+            copy16_or_zero(to + pf_chunk((row_in & ~31) + k * AT_ONCE + lane / LANES, lane % LANES), from ? from + lane % LANES * 8 : static_cast<const __nv_bfloat16*>(a.q.p), from != nullptr);
+        }
+        copies_arrived();
+        __syncwarp();
+        uint32_t top = 0;                        // this lane's row: its largest magnitude, as bf16 bits
+#pragma unroll 4
+        for (int ch = 0; ch < LANES; ++ch) {
+            const uint4 v = lds128(to + pf_chunk(row_in, ch));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, w[j] >> 16 & 0x7fffu));
         }
@@ -204,12 +245,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         const int e = top == 0 || top >= 0x7f80u ? 0 : 9 - (int(top >> 7) - 127);
         const float up = top < 0x80u ? 0x1p100f : exp2f(float(min(e, 120))), sign = a.scale < 0.f ? -up : up;
         f = fmaxf(fabsf(a.scale), 1e-30f) * 1.4426950408889634f / up;
-#pragma unroll
-        for (int ch = 0; ch < HD / 8; ++ch) {
+#pragma unroll 4
+        for (int ch = 0; ch < LANES; ++ch) {
+            const uint32_t at = to + pf_chunk(row_in, ch);
+            const uint4 v = lds128(at);
             float q[8];
-            two_bf16(v[ch].x, q[0], q[1]); two_bf16(v[ch].y, q[2], q[3]); two_bf16(v[ch].z, q[4], q[5]); two_bf16(v[ch].w, q[6], q[7]);
-            st_shared16(q_at + half * S::op_bytes + pf_chunk(row_in, ch),
-                        make_uint4(pack_half(q[0] * sign, q[4] * sign), pack_half(q[1] * sign, q[5] * sign), pack_half(q[2] * sign, q[6] * sign), pack_half(q[3] * sign, q[7] * sign)));
+            two_bf16(v.x, q[0], q[1]); two_bf16(v.y, q[2], q[3]); two_bf16(v.z, q[4], q[5]); two_bf16(v.w, q[6], q[7]);
+            st_shared16(at, make_uint4(pack_half(q[0] * sign, q[4] * sign), pack_half(q[1] * sign, q[5] * sign), pack_half(q[2] * sign, q[6] * sign), pack_half(q[3] * sign, q[7] * sign)));
         }
         fence_proxy_async();
     }
@@ -316,9 +358,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         if (own_tiles > 0 && ok) ok = wait(sh.o_full[half], 0);
         tc_fence_after();
         if (ok) {
-            // values stand at 2^-E, probabilities and their sum at 2^8
+            // values stand at 2^-E, probabilities and their sum at 2^8. The rows go out by way of the half's queries' place, HD / 8 lanes a row
             const float by = l > 0.f ? exp2f(float(e_now)) / l : 0.f;
-            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + row * a.out.row + (head * a.group + g) * a.out.head;
+            const uint32_t rows_at = q_at + half * S::op_bytes + (row_in & ~31) * (HD * 2);
 #pragma unroll 1
             for (int ch = 0; ch < HD / 32; ++ch) {
                 uint32_t r[32];
@@ -329,7 +371,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 #pragma unroll
                     for (int i = 0; i < 32; ++i) r[i] = 0u;
                 }
-                if (row < 0) continue;
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     float y[8];
@@ -338,8 +379,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                         y[k] = __uint_as_float(r[i + 2 * k]) * by;
                         y[k + 4] = __uint_as_float(r[i + 2 * k + 1]) * by;
                     }
-                    store_row<8>(to + 32 * ch + i, y);
+                    st_shared16(rows_at + lane * (HD * 2) + ((ch * 4 + i / 8 ^ lane & LANES - 1) << 4),
+                                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
                 }
+            }
+            __syncwarp();
+            __nv_bfloat16* to = row < 0 ? nullptr : static_cast<__nv_bfloat16*>(a.out.p) + row * a.out.row + (head * a.group + g) * a.out.head;
+#pragma unroll 4
+            for (int k = 0; k < LANES; ++k) {
+                const int i = k * AT_ONCE + lane / LANES;
+                auto* dst = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), i));
+                const uint4 v = lds128(rows_at + i * (HD * 2) + ((lane % LANES ^ i & LANES - 1) << 4));
+                if (dst) *reinterpret_cast<uint4*>(dst + lane % LANES * 8) = v;
             }
         }
     } else if (warp < 12) {
