@@ -7,9 +7,13 @@
 // into three bf16 parts each.
 // Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
 // bf16 calls leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is what the group's sum starts
-// with. Values: the probability is scaled up, and one more product with -8 in the codes' place goes into the running sum before theirs, so
-// that what is left to round is a tile's and not the whole context's sum of codes. fp32 calls subtract the 8 from each code, nine
-// instructions for eight, and lose nothing to it.
+// with. Values: the same words are fp16 subnormals, and probabilities times scales are fp16 numbers, of 11 bits and not bf16's 8: with bf16
+// the result's error was 1.5 times that of its own rounding, now it is 1.02 times that (64 sequences of up to 16001 tokens, 268 MB: 71 us
+// then, 73 now). For their range a group's scales are taken to 2^5 by a power of two that is above all of them so far, kept like the running
+// maximum; a probability and its product with the scale are each rounded to 11 bits while probability times scale is at least 2^-23 of the
+// most, to multiples of 2^-34 of the most below that. One more product with -8 in the codes' place goes into the
+// running sum before theirs, so that what is left to round is a tile's and not the whole context's sum of codes. fp32 calls subtract the 8
+// from each code, nine instructions for eight, and lose nothing to it.
 //
 // All (sequence, columns, head) items together are a line of tiles of 32 tokens that is cut evenly between CTAs, and a CTA's piece
 // evenly between its warps, whatever the lengths are: a warp walks its tiles with the running maximum and sum of each column, fed by its
@@ -51,8 +55,8 @@ struct AtShape {
     static constexpr int warps = HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
     static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : 3;
     static constexpr bool raw = sizeof(T) == 2;              // codes as they are masked out
-    static constexpr float up = raw ? 64.f : 0.f;                       // probabilities are taken to 2^64 then
-    static constexpr float unscale = raw ? 0x1p69f : kQ4ExactUnscale;   // of sums of codes times probabilities
+    static constexpr float up = raw ? 4.f : 0.f;                        // probabilities are taken to 2^4 then, so that none is above 2^10
+    static constexpr float unscale = raw ? 0x1p19f : kQ4ExactUnscale;   // of sums of codes times probabilities
     // a sum of an odd element, beside that of the even one before it
     __device__ static float odd(float both, float low) { return raw ? (both - low) * (1.f / 16.f) : both; }
     static constexpr int ring_bytes = stages * tile_bytes;
@@ -158,13 +162,25 @@ __device__ __forceinline__ void mma_k16_from(float (&d)[4], const float4& c, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c.x), "f"(c.y), "f"(c.z), "f"(c.w));
 }
-// HD / 32 scales of a token
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
+__device__ __forceinline__ uint32_t bits_of(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ uint32_t pack_half(float a, float b) { return bits_of(__floats2half2_rn(a, b)); }
+// D += A B of fp16
+__device__ __forceinline__ void mma_half_k16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// HD / 32 scales of a token, two a word; as numbers
 template <int G>
-__device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
-    uint32_t w[G / 2];
+__device__ __forceinline__ void scale_words(uint32_t addr, uint32_t (&w)[G / 2]) {
     if constexpr (G == 2) w[0] = lds32(addr);
     else if constexpr (G == 4) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
     else { const uint4 v = lds128(addr); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+}
+template <int G>
+__device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
+    uint32_t w[G / 2];
+    scale_words<G>(addr, w);
 #pragma unroll
     for (int i = 0; i < G / 2; ++i) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
@@ -177,6 +193,7 @@ __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
 // would leave the range of numbers).
 constexpr uint32_t kAtUp64 = 0x5f805f80u, kAtUp60 = 0x5d805d80u;
 constexpr float kAtUp69 = 0x1p69f;
+constexpr uint32_t kAtNarrowest = 0x18001800u, kAtWidest = 0x78007800u;     // 2^-9, 2^15
 // A word's bytes as operands: the low nibble of bytes 0, 2 and both nibbles of them (low + 16 high, also linear), the same of bytes 1, 3:
 // four instructions. Values' elements are rows of the product, so the high nibble's sum is had from the two.
 constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus136 = 0x80888088u;      // -8 and -8 - 16 * 8 as codes
@@ -209,7 +226,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     using S = AtShape<T, HD>;
     constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
     constexpr bool RAW = S::raw;
-    constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = QP;        // parts of a query, of a probability
+    constexpr int QP = sizeof(T) == 4 ? 3 : 1;                 // parts of a query
     extern __shared__ __align__(128) unsigned char smem[];
     // pieces of a line go round the SM's four schedulers a quarter of the warps apart, so that a CTA of a few tiles uses all four
     const int tid = threadIdx.x, lane = tid & 31, place = tid >> 5, warp = (place & 3) * (W / 4) + (place >> 2), r = lane >> 2, c = lane & 3;
@@ -302,6 +319,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     const int count = int(cta_lo + (cta_hi - cta_lo) * (warp + 1) / W - lo);
 
     float m[2], l[2], y[G][2][4];
+    uint32_t wide[G / 2];                        // (bf16) a power of two per group that no value's scale so far is above, as fp16, as far as these go
     uint32_t qf[QP][G][4];
     if (count > 0) {
         {
@@ -434,7 +452,11 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             }
             m[0] = m[1] = -INFINITY;
             l[0] = l[1] = 0.f;
-            if constexpr (RAW) __syncwarp();
+            if constexpr (RAW) {
+#pragma unroll
+                for (int k = 0; k < G / 2; ++k) wide[k] = kAtNarrowest;
+                __syncwarp();
+            }
             began = t;
             whole_tiles = min(use.nk, use.len - use.n + use.ct * COLS / a.group + 1) / kAtTile;
         };
@@ -503,7 +525,41 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 top[e] = v;
                 raise |= v > m[e] + slack;         // (-infinity is not above -infinity)
             }
+            // ---- bf16: the values' scales, and whether one is above its group's power of two (what has never been written may be anything) ----
+            uint32_t vs[2][2][G / 2], widest[G / 2];
+            if constexpr (RAW) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        scale_words<G>(at + b * BB + kv_v_scales(HD) + (8 * j + r) * (2 * G), vs[b][j]);
+                        if (!whole && (!(have >> b & 1) || t * kAtTile + 16 * b + 8 * j + r >= use.nk))
+#pragma unroll
+                            for (int k = 0; k < G / 2; ++k) vs[b][j][k] = 0;
+                    }
+#pragma unroll
+                for (int k = 0; k < G / 2; ++k) {
+                    auto of = [&](int b, int j) { return __habs2(as_half2(vs[b][j][k])); };
+                    widest[k] = bits_of(__hmax2(__hmax2(__hmax2(of(0, 0), of(0, 1)), __hmax2(of(1, 0), of(1, 1))), as_half2(wide[k])));
+                    raise |= widest[k] != wide[k];
+                }
+            }
             if (__any_sync(0xffffffffu, raise)) {
+                if constexpr (RAW) {
+#pragma unroll
+                    for (int k = 0; k < G / 2; ++k) {
+                        uint32_t w = widest[k];
+                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 4));
+                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 8));
+                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 16));
+                        w = __vminu2(w, kAtWidest) + 0x03ff03ffu & 0x7c007c00u;
+                        const float2 was = __half22float2(as_half2(wide[k])), is = __half22float2(as_half2(w));
+                        const float by0 = was.x / is.x, by1 = was.y / is.y;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { y[2 * k][0][j] *= by0; y[2 * k][1][j] *= by0; y[2 * k + 1][0][j] *= by1; y[2 * k + 1][1][j] *= by1; }
+                        wide[k] = w;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f);
@@ -529,38 +585,61 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const uint32_t block = at + b * BB;
-                float s0[G], s1[G];
-                token_scales<G>(block + kv_v_scales(HD) + r * (2 * G), s0);
-                token_scales<G>(block + kv_v_scales(HD) + (r + 8) * (2 * G), s1);
-                if (!whole) {                    // what has never been written may be anything
+                if constexpr (RAW) {
+                    const __half2 p0 = as_half2(pack_half(s[b][0], s[b][1])), p1 = as_half2(pack_half(s[b][2], s[b][3]));
 #pragma unroll
-                    for (int k = 0; k < G; ++k) {
-                        if (!(have >> b & 1) || t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
-                        if (!(have >> b & 1) || t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
+                    for (int k = 0; k < G; k += 2) {
+                        const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
+                        const __half2 down = as_half2(0x8c008c00u - wide[k / 2]);          // 2^5 / wide
+                        const __half2 s0 = __hmul2(as_half2(vs[b][0][k / 2]), down), s1 = __hmul2(as_half2(vs[b][1][k / 2]), down);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const Nib4 u = q4_bytes(h ? w.z : w.x), v = q4_bytes(h ? w.w : w.y);
+                            const uint32_t b0 = transpose8(bits_of(__hmul2(p0, h ? __high2half2(s0) : __low2half2(s0))));
+                            const uint32_t b1 = transpose8(bits_of(__hmul2(p1, h ? __high2half2(s1) : __low2half2(s1))));
+                            mma_half_k16(y[k + h][0], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
+                            mma_half_k16(y[k + h][1], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
+                            mma_half_k16(y[k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                            mma_half_k16(y[k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+                        }
                     }
-                }
+                } else {
+                    float s0[G], s1[G];
+                    token_scales<G>(block + kv_v_scales(HD) + r * (2 * G), s0);
+                    token_scales<G>(block + kv_v_scales(HD) + (r + 8) * (2 * G), s1);
+                    if (!whole) {
 #pragma unroll
-                for (int k = 0; k < G; k += 2) {
-                    const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
+                        for (int k = 0; k < G; ++k) {
+                            if (!(have >> b & 1) || t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
+                            if (!(have >> b & 1) || t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
+                        }
+                    }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const Nib4 u = RAW ? q4_bytes(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_bytes(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
-                        float p0 = s[b][0] * s0[k + h], p1 = s[b][1] * s0[k + h], p2 = s[b][2] * s1[k + h], p3 = s[b][3] * s1[k + h];
+                    for (int k = 0; k < G; k += 2) {
+                        const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
-                        for (int q = 0; q < PP; ++q) {
-                            const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3);
-                            if (q + 1 < PP) {
-                                float x0, x1;
-                                two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
-                                two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
+                        for (int h = 0; h < 2; ++h) {
+                            const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
+                            float p0 = s[b][0] * s0[k + h], p1 = s[b][1] * s0[k + h], p2 = s[b][2] * s1[k + h], p3 = s[b][3] * s1[k + h];
+                            float d[2][4];       // (a product cuts its sum off where it does not round it: the running sum is added outside of it)
+#pragma unroll
+                            for (int q = 0; q < 3; ++q) {
+                                const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3), b0 = transpose8(lo2), b1 = transpose8(hi2);
+                                if (q < 2) {
+                                    float x0, x1;
+                                    two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
+                                    two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
+                                }
+                                if (q == 0) {
+                                    mma_k16_first(d[0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                                    mma_k16_first(d[1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+                                } else {
+                                    mma_k16(d[0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                                    mma_k16(d[1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+                                }
                             }
-                            const uint32_t b0 = transpose8(lo2), b1 = transpose8(hi2);
-                            if constexpr (RAW) {
-                                mma_k16(y[k + h][0], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
-                                mma_k16(y[k + h][1], kAtMinus8, kAtMinus136, kAtMinus8, kAtMinus136, b0, b1);
-                            }
-                            mma_k16(y[k + h][0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
-                            mma_k16(y[k + h][1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) { y[k + h][0][j] += d[0][j]; y[k + h][1][j] += d[1][j]; }
                         }
                     }
                 }
@@ -578,7 +657,15 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                     v += __shfl_xor_sync(0xffffffffu, v, 4);
                     v += __shfl_xor_sync(0xffffffffu, v, 8);
                     v += __shfl_xor_sync(0xffffffffu, v, 16);
-                    l[e] = RAW ? v * 0x1p-64f : v;
+                    l[e] = v;
+                }
+                if constexpr (RAW) {
+#pragma unroll
+                    for (int k = 0; k < G / 2; ++k) {
+                        const float2 by = __half22float2(as_half2(wide[k]));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { y[2 * k][0][j] *= by.x; y[2 * k][1][j] *= by.x; y[2 * k + 1][0][j] *= by.y; y[2 * k + 1][1][j] *= by.y; }
+                    }
                 }
                 if (ends && began == 0) {        // all of it is this warp's
 #pragma unroll

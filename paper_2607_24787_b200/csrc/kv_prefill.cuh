@@ -70,9 +70,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) 
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
-__device__ __forceinline__ uint32_t bits_of(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
-__device__ __forceinline__ uint32_t pack_half(float a, float b) { return bits_of(__floats2half2_rn(a, b)); }
 
 // Eight codes of a word as fp16 elements times a scale, in the order (0, 4, 1, 5, 2, 6, 3, 7): 1024 + q (low nibbles of the masked halves)
 // less 1032, 1024 + 16 q over 16 less 72, both exact, then one rounding

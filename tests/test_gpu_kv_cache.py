@@ -361,6 +361,24 @@ def test_values_and_keys_of_any_size(kv, rows, heads, dtype):
     check_attend(c, heads, q=q * 1e15)
 
 
+@pytest.mark.parametrize("rows,heads", [([4], 4), ([200], 16)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_small_values_beside_large_ones_that_a_row_does_not_see(kv, rows, heads, dtype):
+    """The last three tokens' values are 2^13 times the others': rows before them hold what the others give, as exactly as without them."""
+    c = Case(kv, 24, [325], rows, 1, 128, 16, dtype, fill=True)
+    g = torch.Generator().manual_seed(6)
+    pages = torch.from_numpy(c.start)
+    for t in range(0, 325, 16):
+        block = pages[c.table[0, t // 16], 0, 0]
+        size = torch.full((16, 4), 0.0625)
+        size[max(0, 322 - t):] = 512.0
+        block[17 * 128:] = ((torch.rand(16, 4, generator=g) + 0.5) * size).half().view(torch.uint8).flatten()
+        block[16 * 128:17 * 128] = ((torch.rand(64, generator=g) - 0.5) * 0.1).half().view(torch.uint8)
+    c.start = pages.numpy().copy()
+    c.cache.pages.copy_(pages)
+    check_attend(c, heads)
+
+
 @pytest.mark.parametrize("heads", [4, 12])
 def test_bad_pages_in_a_prompt(kv, heads):
     c = Case(kv, 23, [600, 300], [200, 300], 1, 64, 16, BF16, fill=True)
