@@ -71,7 +71,7 @@ template <int COLS>
 struct Walk {
     int seq, ct, head, t, nt, first, n, len, nk;
 
-    __device__ __forceinline__ void load(const AttendArgs& a) {
+    __device__ __forceinline__ void load(const AttendArgs& a) {      // of `seq`
         len = a.batch.lengths[seq];
         first = seq; n = 1;
         if (a.batch.row_start) {
@@ -92,11 +92,9 @@ struct Walk {
         for (ct = from; ct < m; ct += step) { columns(a); sum += nt; }
         return sum * a.kv.heads;
     }
-    // to tile `rest` of sequence `s`, by a warp: lanes look at 32 column blocks at a time
-    __device__ __forceinline__ void seek(const AttendArgs& a, int s, long long rest) {
+    // to tile `rest` of the sequence, by a warp: lanes look at 32 column blocks at a time
+    __device__ __forceinline__ void seek(const AttendArgs& a, long long rest) {
         const int lane = threadIdx.x & 31;
-        seq = s;
-        load(a);
         const int m = blocks(a);
         for (int ct0 = 0; m > 1; ct0 += 32) {
             ct = ct0 + lane;
@@ -239,7 +237,6 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     __shared__ Walk<COLS> copied[W], used[W];      // the items that a warp's copies and its sums are at
     __shared__ float4 starts[RAW ? W : 1][G][4];   // -8 times the sum of a group's queries, as the product's C for columns 2 c, 2 c + 1
     __shared__ long long warp_sum_of[W];
-    __shared__ float weight[2 * W][COLS], total[2 * W][COLS], highest[2 * W][COLS];
 
     if (lane == 0) {
         for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1);
@@ -252,10 +249,14 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     // ---- the line of tiles: how many there are, and before each sequence. Up to 64 sequences are two a lane, in every warp for itself ----
     const int n_seq = a.batch.n_seq;
     long long all = 0, before0 = 0, before1 = 0;
-    auto count_tiles = [&](int s) {
+    int len0 = 0, len1 = 0, n0 = 0, n1 = 0, first0 = 0, first1 = 0;
+    auto loaded = [&](int s) {
         Walk<COLS> w;
-        w.seq = s;
-        w.load(a);
+        w.seq = s; w.n = 0; w.first = 0; w.len = 0;
+        if (s < n_seq) w.load(a);
+        return w;
+    };
+    auto count_tiles = [&](Walk<COLS> w) {
         if (w.n > 0 && w.len > a.batch.stride * a.kv.page_size && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
         return w.blocks(a) <= kAtFewBlocks ? w.tiles_of_sequence(a, 0, 1) : -1ll;
     };
@@ -274,8 +275,9 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         return k;
     };
     if (n_seq <= 64) {
-        const long long k0 = count_many(2 * lane < n_seq ? count_tiles(2 * lane) : 0ll, 2 * lane);
-        const long long k1 = count_many(2 * lane + 1 < n_seq ? count_tiles(2 * lane + 1) : 0ll, 2 * lane + 1);
+        const Walk<COLS> w0 = loaded(2 * lane), w1 = loaded(2 * lane + 1);
+        const long long k0 = count_many(count_tiles(w0), 2 * lane), k1 = count_many(count_tiles(w1), 2 * lane + 1);
+        len0 = w0.len; len1 = w1.len; n0 = w0.n; n1 = w1.n; first0 = w0.first; first1 = w1.first;
         long long upto = k0 + k1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         long long mine = 0;
         for (int i = 0; i < each; ++i) {
             const int s = tid * each + i;
-            const long long k = count_many(s < n_seq ? count_tiles(s) : 0ll, s);
+            const long long k = count_many(count_tiles(loaded(s)), s);
             if (s < n_seq) before[s] = mine;
             mine += k;
         }
@@ -327,14 +329,18 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             if (n_seq <= 64) {
                 const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
                 const long long b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
-                at.seek(a, s, lo - (s & 1 ? b1 : b0));
+                auto of = [&](int x0, int x1) { return __shfl_sync(0xffffffffu, s & 1 ? x1 : x0, s / 2); };
+                at.seq = s; at.len = of(len0, len1); at.n = of(n0, n1); at.first = of(first0, first1);
+                at.seek(a, lo - (s & 1 ? b1 : b0));
             } else {
                 int s = 0, end = n_seq;          // the last sequence with before[s] <= lo
                 while (end - s > 1) {
                     const int mid = (s + end) / 2;
                     if (before[mid] <= lo) s = mid; else end = mid;
                 }
-                at.seek(a, s, lo - before[s]);
+                at.seq = s;
+                at.load(a);
+                at.seek(a, lo - before[s]);
             }
             if (lane == 0) copied[warp] = used[warp] = at;
             __syncwarp();
@@ -714,72 +720,87 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     }
     __syncthreads();
 
-    // ---- parts of one item in this CTA meet: they stand one after another. Every warp sees which parts belong together (lane j: part j);
-    // first a warp takes a column of an item for the parts' weights, then threads take sums ----
+    // ---- parts of one item in this CTA meet: they stand one after another, and every warp sees which belong together (lane j: part j).
+    // A warp takes a column of an item, whatever the number of items: the parts' weights, a lane each, then their sums ----
     const long long id = lane < 2 * W ? meta[lane].id : -1;
     const uint32_t mates = __match_any_sync(0xffffffffu, id);
-    const uint32_t leaders = __ballot_sync(0xffffffffu, id >= 0 && (mates & ((1u << lane) - 1)) == 0);
+    const bool leads = id >= 0 && (mates & ((1u << lane) - 1)) == 0;
+    const uint32_t leaders = __ballot_sync(0xffffffffu, leads);
+    const int rank = __popc(leaders & ((1u << lane) - 1)), columns = __popc(leaders) * COLS;
     auto part_of = [&](int j) { return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes); };
-    {
-        int n = 0;
-        for (uint32_t left = leaders; left; left &= left - 1, ++n) {
-            const uint32_t group = __shfl_sync(0xffffffffu, mates, __ffs(left) - 1);
-            for (int col = (warp + W - n * COLS % W) % W; col < COLS; col += W) {
-                const bool in = group >> lane & 1;
-                const float v = in ? part_of(lane)[COLS * HD + col] : -INFINITY;
-                float top = v;
+    if (warp == 0) {                             // an item that begins here and goes on: up to the CTA of its last tile
+        const PartMeta first = meta[leads ? lane : 0];
+        const bool open = leads && first.from == 0 && meta[leads ? 31 - __clz(mates) : 0].to < first.nt;
+        const uint32_t any = __ballot_sync(0xffffffffu, open);
+        if (open || (any == 0 && lane == 0)) {
+            int4 join = make_int4(0, 0, 0, 0);
+            if (open) join = make_int4(int(((first.id + first.nt) * ctas - 1) / all) - cta + 1, first.ct, first.head, first.first);
+            *reinterpret_cast<int4*>(a.joins + 8 * cta) = join;
+            a.joins[8 * cta + 4] = open ? first.n : 0;
+        }
+    }
+    for (int x = warp; x < columns; x += W) {
+        const int col = x % COLS;
+        const int at = __ffs(__ballot_sync(0xffffffffu, leads && rank == x / COLS)) - 1;
+        const uint32_t group = __shfl_sync(0xffffffffu, mates, at);
+        const PartMeta& first = meta[at];
+        const bool in = group >> lane & 1;
+        const float v = in ? part_of(lane)[COLS * HD + col] : -INFINITY;
+        float top = v;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float by = top == -INFINITY ? 0.f : ex2(v - top);
-                const float sum = warp_sum(in ? by * part_of(lane)[COLS * HD + COLS + col] : 0.f);
-                if (in) weight[lane][col] = by;
-                if (lane == 0) { total[n][col] = sum; highest[n][col] = top; }
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float weight = top == -INFINITY ? 0.f : ex2(v - top);
+        const float total = warp_sum(in ? weight * part_of(lane)[COLS * HD + COLS + col] : 0.f);
+        constexpr int N = HD / 32 < 4 ? HD / 32 : 4, RUNS = HD / (32 * N);       // N numbers side by side
+        float o[RUNS][N] = {};
+        for (uint32_t left = group; left;) {     // four parts' loads at a time
+            float y4[4][RUNS][N], by[4];
+            bool one[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                one[i] = left != 0;
+                const int j = one[i] ? __ffs(left) - 1 : at;
+                left &= left - 1;
+                by[i] = __shfl_sync(0xffffffffu, weight, j);
+                const float* part = part_of(j) + col * HD + lane * N;
+#pragma unroll
+                for (int k = 0; k < RUNS; ++k)
+                    if constexpr (N == 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(part + k * 128);
+                        y4[i][k][0] = f.x; y4[i][k][1] = f.y; y4[i][k][2] = f.z; y4[i][k][3] = f.w;
+                    } else {
+                        const float2 f = *reinterpret_cast<const float2*>(part);
+                        y4[i][k][0] = f.x; y4[i][k][1] = f.y;
+                    }
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (one[i])
+#pragma unroll
+                    for (int k = 0; k < RUNS; ++k)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) o[k][e] += by[i] * y4[i][k][e];
         }
-    }
-    __syncthreads();
-    int4 join0 = make_int4(0, 0, 0, 0);
-    int join1 = 0;
-    {
-        int n = 0;
-        for (uint32_t left = leaders; left; left &= left - 1, ++n) {
-            const uint32_t group = __shfl_sync(0xffffffffu, mates, __ffs(left) - 1);
-            const PartMeta first = meta[__ffs(group) - 1];
-            const int to = meta[31 - __clz(group)].to;
-            const bool done = first.from == 0 && to == first.nt;
-            const int slot = first.from > 0 ? 0 : 1;
-            if (!done && slot == 1) {            // up to the CTA of the item's last tile
-                const long long last = first.id + first.nt - 1;
-                join0 = make_int4(int(((last + 1) * ctas - 1) / all) - cta + 1, first.ct, first.head, first.first);
-                join1 = first.n;
+        if (first.from == 0 && meta[31 - __clz(group)].to == first.nt) {
+            int g;
+            const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
+            const float by = total > 0.f ? S::unscale / total : 0.f;
+            if (row < 0) continue;
+            T* to = static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + lane * N;
+#pragma unroll
+            for (int k = 0; k < RUNS; ++k) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[k][e] *= by;
+                store_row<N>(to + k * 128, o[k]);
             }
-            float* out_part = a.parts + (size_t(cta) * 2 + slot) * S::part_floats;
-            for (int x = tid; x < COLS * (HD / 2); x += W * 32) {
-                const int col = x / (HD / 2), d = x % (HD / 2) * 2;
-                float2 o = make_float2(0.f, 0.f);
-#pragma unroll 4
-                for (int j = __ffs(group) - 1; j <= 31 - __clz(group); ++j) {
-                    if (!(group >> j & 1)) continue;
-                    const float by = weight[j][col];
-                    const float2 v = *reinterpret_cast<const float2*>(part_of(j) + col * HD + d);
-                    o.x += by * v.x; o.y += by * v.y;
-                }
-                if (done) {
-                    int g;
-                    const int row = row_of_column<COLS>(a, first.first, first.n, first.ct, col, g);
-                    const float by = total[n][col] > 0.f ? S::unscale / total[n][col] : 0.f;
-                    float res[2] = {o.x * by, o.y * by};
-                    if (row >= 0) store_row<2>(static_cast<T*>(a.out.p) + row * a.out.row + (first.head * a.group + g) * a.out.head + d, res);
-                } else {
-                    *reinterpret_cast<float2*>(out_part + col * HD + d) = o;
-                    if (d == 0) { out_part[COLS * HD + col] = highest[n][col]; out_part[COLS * HD + COLS + col] = total[n][col]; }
-                }
-            }
+        } else {                                 // slot 0: an item that began before this CTA
+            float* to = a.parts + (size_t(cta) * 2 + (first.from == 0)) * S::part_floats;
+#pragma unroll
+            for (int k = 0; k < RUNS; ++k)
+#pragma unroll
+                for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(to + col * HD + k * 128 + lane * N + e) = make_float2(o[k][e], o[k][e + 1]);
+            if (lane == 0) { to[COLS * HD + col] = top; to[COLS * HD + COLS + col] = total; }
         }
-    }
-    if (tid == 0) {
-        *reinterpret_cast<int4*>(a.joins + 8 * cta) = join0;
-        a.joins[8 * cta + 4] = join1;
     }
 }
 
