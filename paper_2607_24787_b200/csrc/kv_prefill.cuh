@@ -151,9 +151,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                     return max(0, own - int(unsigned(max(0, min(t - 1 - (len - m), m)) * a.group + kPfCols - 1) / kPfCols));
                 };
                 int low = 0, high = __reduce_max_sync(0xffffffffu, tokens) + 1;  // `low`: the most tokens that more than `block` items have
-                while (high - low > 1) {
-                    const int mid = low + (high - low) / 2;
-                    if (__reduce_add_sync(0xffffffffu, at_least(mid)) > block) low = mid; else high = mid;
+                while (high - low > 1) {         // (eight parts at a time: seven sums that do not wait for one another)
+                    const int step = (high - low + 7) / 8;
+                    int above = 0;
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) above += int(__reduce_add_sync(0xffffffffu, at_least(low + i * step))) > block;
+                    low += above * step;
+                    high = min(high, low + step);
                 }
                 skip = at_least(low + 1);
                 ours = at_least(low) - skip;
