@@ -26,29 +26,28 @@ Work work_of(const spm_model_cfg& m, const spm_attention& a) {
     return {up256((nb + 7) / 8 * 8 * k * 6), up256(nb * qkv_width(a) * 4), up256(nb * q_width(a) * 4), up256(attend)};
 }
 
-template <int NT, int MT>
-void launch_project(const __nv_bfloat16* W, const uint4* parts, int rows, int K, int N, float* y, int add, cudaStream_t st) {
-    project_kernel<NT, MT><<<N / (16 * MT), kPrWarps * 32, 0, st>>>(W, parts, rows, K, y, N, add);
+template <int NT, int MT, int U>
+cudaError_t launch_project(const __nv_bfloat16* W, const uint4* parts, int rows, int K, int N, float* y, int add, cudaStream_t st) {
+    return launch_early(project_kernel<NT, MT, U>, N / (16 * MT), kPrWarps * 32, 0, st, W, parts, rows, K, y, N, add);
 }
 
 // y [rows][N] (+)= W [N][K] x [rows][K] (normed with gamma)
 cudaError_t project(bool fp32, const void* W, const float* x, const float* gamma, float eps, int rows, int K, int N, void* work, float* y, int add, cudaStream_t st) {
     uint4* parts = fp32 ? nullptr : static_cast<uint4*>(work);
     float* plain = fp32 ? static_cast<float*>(work) : nullptr;
-    project_rows_kernel<<<fp32 ? rows : (rows + 7) / 8 * 8, 256, 0, st>>>(x, rows, K, gamma, eps, parts, plain);
-    cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_early(project_rows_kernel, rows, 256, 0, st, x, K, gamma, eps, parts, plain);
     if (e != cudaSuccess) return e;
-    if (fp32) {
-        project_fp32_kernel<<<dim3((N + kPrWarps - 1) / kPrWarps, (rows + 7) / 8), kPrWarps * 32, 0, st>>>(static_cast<const float*>(W), plain, rows, K, N, y, N, add);
-        return cudaGetLastError();
-    }
-    // with many rows a CTA takes 32 rows of W: what it reads of x from L2 is what it then waits for
+    if (fp32)
+        return launch_early(project_fp32_kernel, dim3((N + kPrWarps - 1) / kPrWarps, (rows + 7) / 8), kPrWarps * 32, 0, st, static_cast<const float*>(W), plain, rows, K, N, y, N, add);
+    // one round of CTAs: more of W in flight. With many rows a CTA takes 32 rows of W where that still makes a CTA an SM: what it reads of x
+    // from L2 is what it then waits for
     const auto* w = static_cast<const __nv_bfloat16*>(W);
-    if (rows <= 8) launch_project<1, 1>(w, parts, rows, K, N, y, add, st);
-    else if (rows <= 16) launch_project<2, 1>(w, parts, rows, K, N, y, add, st);
-    else if (rows <= 32) launch_project<4, 2>(w, parts, rows, K, N, y, add, st);
-    else launch_project<8, 2>(w, parts, rows, K, N, y, add, st);
-    return cudaGetLastError();
+    const bool few = N / 16 <= 148;
+    if (rows <= 8 && few) return launch_project<1, 1, 8>(w, parts, rows, K, N, y, add, st);
+    if (rows <= 8) return launch_project<1, 1, 4>(w, parts, rows, K, N, y, add, st);
+    if (rows <= 16) return launch_project<2, 1, 0>(w, parts, rows, K, N, y, add, st);
+    if (rows <= 32) return few ? launch_project<4, 1, 0>(w, parts, rows, K, N, y, add, st) : launch_project<4, 2, 0>(w, parts, rows, K, N, y, add, st);
+    return few ? launch_project<8, 1, 0>(w, parts, rows, K, N, y, add, st) : launch_project<8, 2, 0>(w, parts, rows, K, N, y, add, st);
 }
 
 }  // namespace

@@ -93,22 +93,6 @@ void by_type(int dtype, int hd, F f) {
     else size(static_cast<float*>(nullptr));
 }
 
-// Launched so that its CTAs may be in place before the stream's kernel before it has ended: every kernel here waits for that one before it
-// reads or writes anything, and lets its own successor do the same.
-template <typename... A, typename... B>
-cudaError_t launch_early(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const B&... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, A(args)...);
-}
 int launched(const char* call, cudaError_t e) {
     if (e != cudaSuccess) cudaGetLastError();
     return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));

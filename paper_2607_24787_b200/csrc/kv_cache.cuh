@@ -132,4 +132,21 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[E])
     else *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
+// Launched so that its CTAs may be in place before the stream's kernel before it has ended: every kernel launched so waits for that
+// one before it reads or writes anything but weights, and then lets its own successor do the same.
+template <typename... A, typename... B>
+cudaError_t launch_early(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const B&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, A(args)...);
+}
+
 }  // namespace spm
