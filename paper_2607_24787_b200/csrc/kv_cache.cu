@@ -136,9 +136,10 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
     return e == cudaSuccess ? launch_early(kv_attend_join_kernel<T, HD>, dim3(ctas, S::cols), kAtJoinThreads, 0, st, a) : e;
 }
 
-// Which of the two kernels a call's rows are for. Per token of context the tensor-core kernel takes 17 ns a round of CTAs (an SM does 256
-// columns of a head, and an item's tokens are not shared out), the other 4.3 ps a column of a head on all SMs together, whatever the rows
-// are (measured with 46592 columns of 4 heads: 245 and 1605 us; with 144 columns the rule leaves the other, 27 us). Lengths cancel.
+// Which of the two kernels a call's rows are for. Per token of context the tensor-core kernel takes 19 ns a round of CTAs (an SM does 256
+// columns of a head, and an item's tokens are not shared out), the other 4.5 ps a column of a head on all SMs together, whatever the rows
+// are; lengths cancel. Measured with 4 heads of 128 over 4096 tokens, columns times heads (tensor cores / other, us): 3200: 80 / 64,
+// 4096: 79 / 79, 8192: 79 / 140, 37888: 87 / 594; in two rounds, 10240: 159 / 177.
 bool prefill_pays(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
     if (dtype != SPM_DTYPE_BF16 || kv->head_dim > 128 || !b->row_start) return false;
     const long long columns = static_cast<long long>(b->n_rows) * (n_q_heads / kv->n_kv_heads), each = (columns + b->n_seq - 1) / b->n_seq;

@@ -8,10 +8,16 @@
 //
 // fp16 and not bf16 operands, since a bf16 rounding of probabilities and values would each cost as much as that of the result. Ranges are
 // kept by powers of two, which round nothing: a row's queries are brought to [2^9, 2^10) by its largest, keys of a tile in which one would
-// not fit are taken times 2^-4, a probability times 2^8 (it is at most 2^6 above the running maximum, see below), and values times 2^-E, E from the largest scale so
-// far (a tile whose values would not fit raises E, and the sums so far are scaled down).
+// not fit are taken times 2^-4, a probability times 2^8 (it is at most 2^6 above the running maximum, see below), and values times 2^-E, E
+// from the largest scale so far (a tile whose values would not fit raises E, and the sums so far are scaled down).
 //
 // A row's maximum is moved, and its sums scaled, only where a score is above it by more than 2^6.
+//
+// What bounds it, a CTA's tile of 128 tokens for 256 columns: 4017 cycles. The halves take turns, 2250 cycles of softmax and 1770 of products
+// with their hand-over; the exponentials (128 x 256 at 16 a cycle), the products and the shared memory that these read are 2050 each. Four
+// prompts of up to 2049 rows after up to 2048 tokens, 32 heads: 228 us, 0.81 PFLOP/s, of which an item's start and end (search 2 us, queries
+// 3, first scores 1.6, rows out 2.5) are a fifth. Slower: waits with a time hint (262 us for 245 then), steps of 64 tokens with two score
+// buffers a half (262), probabilities against the old maximum held in registers (311, spills).
 #pragma once
 
 #include "kv_attend.cuh"

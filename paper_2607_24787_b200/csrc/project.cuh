@@ -3,6 +3,8 @@
 // Bound by reading W once. Each row x is normed and split by a block of its own first (three bf16 parts, so that activations stay fp32 as
 // everywhere in a step), laid out as the B operand wants it; then a CTA takes 16 or 32 rows of W, its warps every eighth 32 columns, and
 // their sums meet in shared memory in a fixed order.
+// 5120 rows of 2048: 9.0 us for one row x (2.3 TB/s; launches, first words and the sums' joining are most of it), 37 for 64 rows, which read
+// x's parts from L2 once a CTA; 2048 rows of 4096: 12.7 and 27. (Each kernel alone and from a cold cache.)
 #pragma once
 
 #include <cstdint>

@@ -98,6 +98,25 @@ def test_block(name, nb, hd, gammas):
     m.close()
 
 
+@pytest.mark.parametrize("nb", [1, 8, 9, 31, 40])
+def test_block_of_many_heads(nb):
+    """w_qkv of 2816 rows and w_o of 512: more row tiles than SMs, and fewer."""
+    cfg = config("bf16", nb, n_layers=1)
+    m = build(cfg)
+    block = Block(m, cfg, nb, hq=40, seed=3)
+    g = torch.Generator().manual_seed(8)
+    block.step(g)
+    h = torch.randn(nb, cfg.hidden, generator=g).cuda()
+    start = h.double().cpu().numpy()
+    torch.cuda.synchronize()
+    m.attention_block(0, h)
+    m.synchronize()
+    want = block.want(0, start, nb)
+    for t in range(nb):
+        assert M.rel_linf(h[t].double().cpu().numpy(), want[t]) < 4e-5, t
+    m.close()
+
+
 @pytest.mark.parametrize("name,nb", [("tiny", 1), ("bf16", 1), ("bf16", 5), ("q4", 1), ("bf16", 64)])
 def test_steps_with_the_block(name, nb):
     """A decode step is the calls one after another; with every expert resident it is the same bits, also when replayed from a graph; and
