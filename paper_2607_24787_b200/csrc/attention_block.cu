@@ -32,13 +32,15 @@ cudaError_t launch_project(const __nv_bfloat16* W, const uint4* parts, int rows,
 }
 
 // y [rows][N] (+)= W [N][K] x [rows][K] (normed with gamma)
-cudaError_t project(bool fp32, const void* W, const float* x, const float* gamma, float eps, int rows, int K, int N, void* work, float* y, int add, cudaStream_t st) {
+cudaError_t project(bool fp32, const void* W, const float* x, const float* gamma, float eps, int rows, int K, int N, void* work, float* y, int add,
+                    cudaStream_t st) {
     uint4* parts = fp32 ? nullptr : static_cast<uint4*>(work);
     float* plain = fp32 ? static_cast<float*>(work) : nullptr;
     const cudaError_t e = launch_early(project_rows_kernel, rows, 256, 0, st, x, K, gamma, eps, parts, plain);
     if (e != cudaSuccess) return e;
     if (fp32)
-        return launch_early(project_fp32_kernel, dim3((N + kPrWarps - 1) / kPrWarps, (rows + 7) / 8), kPrWarps * 32, 0, st, static_cast<const float*>(W), plain, rows, K, N, y, N, add);
+        return launch_early(project_fp32_kernel, dim3((N + kPrWarps - 1) / kPrWarps, (rows + 7) / 8), kPrWarps * 32, 0, st, static_cast<const float*>(W),
+                            plain, rows, K, N, y, N, add);
     // one round of CTAs: more of W in flight. With many rows a CTA takes 32 rows of W where that still makes a CTA an SM: what it reads of x
     // from L2 is what it then waits for
     const auto* w = static_cast<const __nv_bfloat16*>(W);
@@ -90,7 +92,8 @@ int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int l
     float* out = reinterpret_cast<float*>(at + w.rows + w.qkv);
     void* attend = at + w.rows + w.qkv + w.out;
     auto cuda = [&](cudaError_t ce) { *why = std::string("attention: ") + cudaGetErrorString(ce); return SPM_ERR_CUDA; };
-    cudaError_t ce = project(fp32, static_cast<const char*>(a.w_qkv) + layer * N * D * e, h, a.rms_gamma + layer * D, m.rms_eps, nb, int(D), int(N), rows, qkv, 0, stream);
+    cudaError_t ce = project(fp32, static_cast<const char*>(a.w_qkv) + layer * N * D * e, h, a.rms_gamma + layer * D, m.rms_eps, nb, int(D), int(N), rows,
+                             qkv, 0, stream);
     if (ce != cudaSuccess) return cuda(ce);
     spm_kv_batch b = a.batch;
     b.row_start = nullptr;

@@ -40,7 +40,8 @@ struct AttendArgs {
     int page_shift;             // blocks a page are 1 << page_shift, or -1
     float scale;
     float* parts;               // [2 * CTAs][part floats]
-    int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns, head, first row, rows
+    int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns,
+                                // head, first row, rows
     int once;                   // every block is read by one warp alone
 };
 
@@ -67,7 +68,8 @@ struct AtShape {
     static constexpr int ring_bytes = stages * tile_bytes;
     static_assert(ring_bytes >= part_bytes, "a warp's last part takes the place of its ring");
     static constexpr int smem(int n_seq) { return warps * (ring_bytes + part_bytes + stages * 8) + (n_seq > 64 ? n_seq * 8 : 0); }
-    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 8 + (raw ? 9728 : 4608) <= 232448, "227 KB, the last of it for the kernel's own arrays");
+    static_assert(warps * (ring_bytes + part_bytes + stages * 8) + SPM_KV_MAX_SEQS * 8 + (raw ? 9728 : 4608) <= 232448,
+                  "227 KB, the last of it for the kernel's own arrays");
 };
 
 // A walk along the line of tiles. nk: tokens that the last of the item's columns sees, nt: tiles (one at least, so that rows that see
@@ -148,7 +150,8 @@ __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int
     return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
 }
 
-struct PartMeta { long long id; int ct, head, from, to, nt, first, n; };       // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
+// tiles [from, to) of nt; id: the item's first tile on the line, -1: none
+struct PartMeta { long long id; int ct, head, from, to, nt, first, n; };
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -161,9 +164,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     return r;
 }
 // D = A B + C
-__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float4& c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_k16_from(float (&d)[4], const float4& c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                             uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c.x), "f"(c.y), "f"(c.z), "f"(c.w));
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c.x), "f"(c.y), "f"(c.z), "f"(c.w));
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
 __device__ __forceinline__ uint32_t bits_of(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
@@ -320,7 +325,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         __syncthreads();
     }
 
-    const int ctas = all >= static_cast<long long>(gridDim.x) * kAtMinTiles ? int(gridDim.x) : max(1, (int(all) + kAtMinTiles - 1) / kAtMinTiles), cta = blockIdx.x;
+    const bool full = all >= static_cast<long long>(gridDim.x) * kAtMinTiles;
+    const int ctas = full ? int(gridDim.x) : max(1, (int(all) + kAtMinTiles - 1) / kAtMinTiles), cta = blockIdx.x;
     const long long cta_lo = cta < ctas ? all * cta / ctas : all, cta_hi = cta < ctas ? all * (cta + 1) / ctas : all;
     const long long lo = cta_lo + (cta_hi - cta_lo) * warp / W;
     const int count = int(cta_lo + (cta_hi - cta_lo) * (warp + 1) / W - lo);
@@ -332,7 +338,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         {
             Walk<COLS> at;
             if (n_seq <= 64) {
-                const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) + __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
+                const int s = __popc(__ballot_sync(0xffffffffu, 2 * lane < n_seq && before0 <= lo)) +
+                              __popc(__ballot_sync(0xffffffffu, 2 * lane + 1 < n_seq && before1 <= lo)) - 1;
                 const long long b0 = __shfl_sync(0xffffffffu, before0, s / 2), b1 = __shfl_sync(0xffffffffu, before1, s / 2);
                 auto of = [&](int x0, int x1) { return __shfl_sync(0xffffffffu, s & 1 ? x1 : x0, s / 2); };
                 at.seq = s; at.len = of(len0, len1); at.n = of(n0, n1); at.first = of(first0, first1);
@@ -496,7 +503,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                     const uint4 w = ldsm4(block + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const Nib4 u = RAW ? q4_unpack(h ? w.z : w.x) : q4_exact(h ? w.z : w.x), v = RAW ? q4_unpack(h ? w.w : w.y) : q4_exact(h ? w.w : w.y);
+                        const uint32_t low = h ? w.z : w.x, high = h ? w.w : w.y;
+                        const Nib4 u = RAW ? q4_unpack(low) : q4_exact(low), v = RAW ? q4_unpack(high) : q4_exact(high);
                         float d[4];
                         if constexpr (RAW) mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
                         else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
@@ -567,7 +575,10 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                         const float2 was = __half22float2(as_half2(wide[k])), is = __half22float2(as_half2(w));
                         const float by0 = was.x / is.x, by1 = was.y / is.y;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) { y[2 * k][0][j] *= by0; y[2 * k][1][j] *= by0; y[2 * k + 1][0][j] *= by1; y[2 * k + 1][1][j] *= by1; }
+                        for (int j = 0; j < 4; ++j) {
+                            y[2 * k][0][j] *= by0; y[2 * k][1][j] *= by0;
+                            y[2 * k + 1][0][j] *= by1; y[2 * k + 1][1][j] *= by1;
+                        }
                         wide[k] = w;
                     }
                 }
@@ -675,7 +686,10 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                     for (int k = 0; k < G / 2; ++k) {
                         const float2 by = __half22float2(as_half2(wide[k]));
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) { y[2 * k][0][j] *= by.x; y[2 * k][1][j] *= by.x; y[2 * k + 1][0][j] *= by.y; y[2 * k + 1][1][j] *= by.y; }
+                        for (int j = 0; j < 4; ++j) {
+                            y[2 * k][0][j] *= by.x; y[2 * k][1][j] *= by.x;
+                            y[2 * k + 1][0][j] *= by.y; y[2 * k + 1][1][j] *= by.y;
+                        }
                     }
                 }
                 if (ends && began == 0) {        // all of it is this warp's
@@ -701,8 +715,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                         const int col = 2 * c + e;
 #pragma unroll
                         for (int k = 0; k < G; ++k)
-                            *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) = make_float4(y[k][0][e], S::odd(y[k][0][2 + e], y[k][0][e]),
-                                                                                                       y[k][1][e], S::odd(y[k][1][2 + e], y[k][1][e]));
+                            *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) =
+                                make_float4(y[k][0][e], S::odd(y[k][0][2 + e], y[k][0][e]), y[k][1][e], S::odd(y[k][1][2 + e], y[k][1][e]));
                         if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f; part[COLS * HD + COLS + col] = l[e]; }
                     }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - t, use.ct, use.head, began, t + 1, use.nt, use.first, use.n};
@@ -732,7 +746,9 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     const bool leads = id >= 0 && (mates & ((1u << lane) - 1)) == 0;
     const uint32_t leaders = __ballot_sync(0xffffffffu, leads);
     const int rank = __popc(leaders & ((1u << lane) - 1)), columns = __popc(leaders) * COLS;
-    auto part_of = [&](int j) { return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes); };
+    auto part_of = [&](int j) {
+        return reinterpret_cast<const float*>(j & 1 ? smem + (j >> 1) * S::ring_bytes : smem + W * S::ring_bytes + (j >> 1) * S::part_bytes);
+    };
     if (warp == 0) {                             // an item that begins here and goes on: up to the CTA of its last tile
         const PartMeta first = meta[leads ? lane : 0];
         const bool open = leads && first.from == 0 && meta[leads ? 31 - __clz(mates) : 0].to < first.nt;

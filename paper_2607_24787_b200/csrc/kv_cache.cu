@@ -29,7 +29,8 @@ int check_dtype(const char* call, int dtype) {
     return dtype == SPM_DTYPE_FP32 || dtype == SPM_DTYPE_BF16 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "rows are fp32 or bf16");
 }
 int check_head_dim(const char* call, int hd) {
-    return hd == 64 || hd == 128 || hd == 256 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(hd) + " not supported: 64, 128 or 256");
+    if (hd == 64 || hd == 128 || hd == 256) return SPM_OK;
+    return fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(hd) + " not supported: 64, 128 or 256");
 }
 int check_cache_shape(const char* call, const spm_kv_cache* kv) {
     if (!kv) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
@@ -43,16 +44,21 @@ int check_cache_shape(const char* call, const spm_kv_cache* kv) {
 int check_cache(const char* call, const spm_kv_cache* kv) {
     if (int rc = check_cache_shape(call, kv)) return rc;
     if (!kv->pages && kv->n_pages > 0) return fail(call, SPM_ERR_INVALID_ARG, "pages is null");
-    if (!aligned(kv->pages, 16) || !aligned(kv->status, 4)) return fail(call, SPM_ERR_INVALID_ARG, "pages must be 16-byte aligned, status 4-byte aligned");
+    if (!aligned(kv->pages, 16) || !aligned(kv->status, 4))
+        return fail(call, SPM_ERR_INVALID_ARG, "pages must be 16-byte aligned, status 4-byte aligned");
     return SPM_OK;
 }
 int check_batch(const char* call, const spm_kv_cache* kv, const spm_kv_batch* b) {
     if (!b) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
-    if (b->n_seq < 0 || b->n_seq > SPM_KV_MAX_SEQS) return fail(call, SPM_ERR_INVALID_ARG, "n_seq " + std::to_string(b->n_seq) + " outside 0.." + std::to_string(SPM_KV_MAX_SEQS));
+    if (b->n_seq < 0 || b->n_seq > SPM_KV_MAX_SEQS)
+        return fail(call, SPM_ERR_INVALID_ARG, "n_seq " + std::to_string(b->n_seq) + " outside 0.." + std::to_string(SPM_KV_MAX_SEQS));
     if (b->n_rows < 0 || b->max_rows < 0 || b->table_stride < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
-    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX) return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 1 tokens");
-    if (b->n_seq > 0 && (!b->lengths || (!b->page_table && b->table_stride > 0))) return fail(call, SPM_ERR_INVALID_ARG, "page_table or lengths is null");
-    if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_start, 4)) return fail(call, SPM_ERR_INVALID_ARG, "page_table, lengths and row_start must be 4-byte aligned");
+    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX)
+        return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 1 tokens");
+    if (b->n_seq > 0 && (!b->lengths || (!b->page_table && b->table_stride > 0)))
+        return fail(call, SPM_ERR_INVALID_ARG, "page_table or lengths is null");
+    if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_start, 4))
+        return fail(call, SPM_ERR_INVALID_ARG, "page_table, lengths and row_start must be 4-byte aligned");
     if (!b->row_start && b->n_rows < b->n_seq) return fail(call, SPM_ERR_INVALID_ARG, "fewer rows than sequences, and no row_start");
     return SPM_OK;
 }
@@ -65,7 +71,8 @@ int check_rows(const char* call, const char* name, const spm_rows* r, int dtype)
 }
 int check_rope(const char* call, const spm_rope* r, const int32_t* positions, int64_t pos_stride, int n_rows, int hd) {
     if (!r) return fail(call, SPM_ERR_INVALID_ARG, "rope is null");
-    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % 16) return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of 16 up to head_dim");
+    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % 16)
+        return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of 16 up to head_dim");
     if (r->n_axes < 1 || r->n_axes > SPM_KV_MAX_AXES) return fail(call, SPM_ERR_INVALID_ARG, "n_axes outside 1.." + std::to_string(SPM_KV_MAX_AXES));
     if (r->rot_dim > 0 && (!r->inv_freq || !positions)) return fail(call, SPM_ERR_INVALID_ARG, "inv_freq or positions is null");
     if (r->rot_dim > 0 && r->n_axes > 1 && pos_stride < n_rows) return fail(call, SPM_ERR_INVALID_ARG, "pos_stride is less than the rows");
@@ -278,7 +285,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.joins = static_cast<int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
     if (prefill_pays(kv, batch, n_q_heads, dtype))
-        e = kv->head_dim == 64 ? launch_prefill<64>(a, dev, static_cast<cudaStream_t>(stream)) : launch_prefill<128>(a, dev, static_cast<cudaStream_t>(stream));
+        e = (kv->head_dim == 64 ? launch_prefill<64> : launch_prefill<128>)(a, dev, static_cast<cudaStream_t>(stream));
     else by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));

@@ -102,7 +102,10 @@ __device__ __forceinline__ void load_row(const float* p, float (&f)[E]) {
     if constexpr (E == 2) { const float2 v = *reinterpret_cast<const float2*>(p); f[0] = v.x; f[1] = v.y; }
     else
 #pragma unroll
-        for (int i = 0; i < E; i += 4) { const float4 v = *reinterpret_cast<const float4*>(p + i); f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w; }
+        for (int i = 0; i < E; i += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + i);
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
 }
 __device__ __forceinline__ void two_bf16(uint32_t v, float& a, float& b) { a = __uint_as_float(v << 16); b = __uint_as_float(v & 0xffff0000u); }
 template <int E>

@@ -91,7 +91,9 @@ __device__ __forceinline__ void st_shared16(uint32_t at, const uint4& v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 // 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
-__device__ __forceinline__ uint32_t pf_chunk(int row, int ch) { return uint32_t((ch >> 3) * (kPfTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)); }
+__device__ __forceinline__ uint32_t pf_chunk(int row, int ch) {
+    return uint32_t((ch >> 3) * (kPfTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+}
 
 struct PfShared {
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
@@ -235,8 +237,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         const uint32_t to = q_at + half * S::op_bytes;
 #pragma unroll 4
         for (int k = 0; k < LANES; ++k) {
-            const auto* from = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * AT_ONCE + lane / LANES));
-            copy16_or_zero(to + pf_chunk((row_in & ~31) + k * AT_ONCE + lane / LANES, lane % LANES), from ? from + lane % LANES * 8 : static_cast<const __nv_bfloat16*>(a.q.p), from != nullptr);
+            const int i = k * AT_ONCE + lane / LANES;
+            const auto* from = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i));
+            copy16_or_zero(to + pf_chunk((row_in & ~31) + i, lane % LANES), from ? from + lane % LANES * 8 : a.q.p, from != nullptr);
         }
         copies_arrived();
         __syncwarp();
@@ -258,7 +261,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
             const uint4 v = lds128(at);
             float q[8];
             two_bf16(v.x, q[0], q[1]); two_bf16(v.y, q[2], q[3]); two_bf16(v.z, q[4], q[5]); two_bf16(v.w, q[6], q[7]);
-            st_shared16(at, make_uint4(pack_half(q[0] * sign, q[4] * sign), pack_half(q[1] * sign, q[5] * sign), pack_half(q[2] * sign, q[6] * sign), pack_half(q[3] * sign, q[7] * sign)));
+            st_shared16(at, make_uint4(pack_half(q[0] * sign, q[4] * sign), pack_half(q[1] * sign, q[5] * sign),
+                                       pack_half(q[2] * sign, q[6] * sign), pack_half(q[3] * sign, q[7] * sign)));
         }
         fence_proxy_async();
     }
@@ -411,7 +415,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         uint4 kc[G], vc[G];
         uint32_t ks[G / 2], vs[G / 2], ks_then[G / 2], vs_then[G / 2];
         // where this thread's token of tile j is; its page has been loaded a tile before (-2: there is no such token)
-        auto slot_of = [&](int j) { const int block = (j * kPfTile + t) / kKvBlock; return a.page_shift >= 0 ? block >> a.page_shift : block / per_page; };
+        auto slot_of = [&](int j) {
+            const int block = (j * kPfTile + t) / kKvBlock;
+            return a.page_shift >= 0 ? block >> a.page_shift : block / per_page;
+        };
         auto page_of = [&](int j) { return j * kPfTile + t < nk ? table[slot_of(j)] : -2; };
         const unsigned char* at = nullptr;
         bool exists = false;
@@ -428,7 +435,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         };
         auto codes = [&](uint4 (&x)[G], int part) {
 #pragma unroll
-            for (int k = 0; k < G; ++k) x[k] = exists ? *reinterpret_cast<const uint4*>(at + part * kv_v_codes(HD) + k * (kKvBlock * 16)) : make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < G; ++k)
+                x[k] = exists ? *reinterpret_cast<const uint4*>(at + part * kv_v_codes(HD) + k * (kKvBlock * 16)) : make_uint4(0, 0, 0, 0);
         };
         auto expand = [&](uint32_t to, const uint4 (&x)[G], const uint32_t (&s)[G / 2], float by) {
             const uint32_t row_at = to + t * 128 + ((t & 7) << 4);               // (tiles start on 1024 bytes)
@@ -525,7 +533,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 #pragma unroll
                     for (int k = 0; k < HD / 16; ++k) {
                         const uint32_t off = (k / 4) * S::block_bytes + (k % 4) * 32;
-                        tc_mma_f16(t_s + h * 128, smem_desc_sw128(q_at + h * S::op_bytes + off, 16, 1024), smem_desc_sw128(k_at + st * S::op_bytes + off, 16, 1024), idesc_s, k > 0);
+                        tc_mma_f16(t_s + h * 128, smem_desc_sw128(q_at + h * S::op_bytes + off, 16, 1024),
+                                   smem_desc_sw128(k_at + st * S::op_bytes + off, 16, 1024), idesc_s, k > 0);
                     }
                     tc_commit(smem_u32(&sh.s_full[h]));
                 }
@@ -535,7 +544,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kPfTile / 16; ++k)
-                        pf_mma_ts(t_o + h * HD, t_s + h * 128 + 8 * k, smem_desc_sw128(v_at + st * S::op_bytes + k * 2048, S::block_bytes, 1024), idesc_o, more || k > 0);
+                        pf_mma_ts(t_o + h * HD, t_s + h * 128 + 8 * k, smem_desc_sw128(v_at + st * S::op_bytes + k * 2048, S::block_bytes, 1024),
+                                  idesc_o, more || k > 0);
                 }
                 __syncwarp();
             };

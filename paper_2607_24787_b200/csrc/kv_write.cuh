@@ -95,14 +95,16 @@ __device__ __forceinline__ void norm_and_turn(const RopeArgs& a, const Angles<HD
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
         const float4 v = at[e / 2 * (HD / 16)];
-        floats_of(add2(mul2(two_floats(x[e], x[e + 1]), two_floats(v.x, v.y)), mul2(two_floats(o[e], o[e + 1]), two_floats(v.z, v.w))), x[e], x[e + 1]);
+        const unsigned long long own = mul2(two_floats(x[e], x[e + 1]), two_floats(v.x, v.y)), theirs = mul2(two_floats(o[e], o[e + 1]), two_floats(v.z, v.w));
+        floats_of(add2(own, theirs), x[e], x[e + 1]);
     }
 }
 
 // A lane's eight elements into the cache (lanes with `write`): `at` is the head's block and part, tok the row's place there. Four lanes hold
 // a group.
 template <int HD>
-__device__ __forceinline__ void quantise_row(const KvPool& kv, unsigned char* codes_at, unsigned char* scales_at, int tok, bool write, int sub, float (&x)[8]) {
+__device__ __forceinline__ void quantise_row(const KvPool& kv, unsigned char* codes_at, unsigned char* scales_at, int tok, bool write, int sub,
+                                             float (&x)[8]) {
     bool odd = false;
     float m = 0.f;
 #pragma unroll
@@ -148,7 +150,7 @@ __device__ __forceinline__ void unpack8(const Raw8& r, float (&x)[8]) {
 // A warp takes a row, or one of `parts` of its heads: its angles first, then a few heads of one kind at a time (a turn), the next ones loaded
 // meanwhile. Warps share nothing, so that one's angles go along with another's heads.
 // Bound by instruction issue (74 % of the slots): some 240 a turn of two heads of 128, of which norm, rotation and finding the code are two
-// thirds, and a row's angles in 64 bits. 18124 prompt rows with 32 query heads: 121 us for 389 MB, 3.2 TB/s; a block of four warps a row
+// thirds, and a row's angles in 64 bits. 18124 prompt rows with 32 query heads: 121 us for 344 MB, 2.8 TB/s; a block of four warps a row
 // with barriers between angles and heads took 139. One row: 4 us, the chain from row number to page to codes.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kKvWarps * 32, 4) kv_write_kernel(const WriteArgs a, int parts) {

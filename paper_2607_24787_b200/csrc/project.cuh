@@ -66,7 +66,8 @@ __global__ void __launch_bounds__(256) project_rows_kernel(const float* x, int K
 // y[t * stride + n] (+)= sum over k of W[n][k] x[t][k]; N a multiple of 16 * MT, K of 32
 // U: turns of W that a warp has in registers ahead of their use (0: with many rows there are no registers for that)
 template <int NT, int MT, int U>
-__global__ void __launch_bounds__(kPrWarps * 32, U == 4 ? 4 : 1) project_kernel(const __nv_bfloat16* W, const uint4* parts, int rows, int K, float* y, long long stride, int add) {
+__global__ void __launch_bounds__(kPrWarps * 32, U == 4 ? 4 : 1) project_kernel(const __nv_bfloat16* W, const uint4* parts, int rows, int K, float* y,
+                                                                                long long stride, int add) {
     __shared__ float red[kPrWarps / 2][MT * 16][8 * NT + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int n0 = blockIdx.x * (16 * MT), KB = K / 32;
@@ -153,7 +154,8 @@ __global__ void __launch_bounds__(kPrWarps * 32, U == 4 ? 4 : 1) project_kernel(
 }
 
 // The same for fp32 weights (parity models): a warp takes a row of W and eight rows of x at a time
-__global__ void __launch_bounds__(kPrWarps * 32) project_fp32_kernel(const float* W, const float* x, int rows, int K, int N, float* y, long long stride, int add) {
+__global__ void __launch_bounds__(kPrWarps * 32) project_fp32_kernel(const float* W, const float* x, int rows, int K, int N, float* y,
+                                                                     long long stride, int add) {
     const int lane = threadIdx.x & 31, n = blockIdx.x * kPrWarps + (threadIdx.x >> 5), t0 = blockIdx.y * 8;
     grid_dep_wait();
     grid_dep_launch();
