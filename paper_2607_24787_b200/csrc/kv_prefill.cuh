@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     if (warp == 13) {
         int block = blockIdx.x / a.kv.heads;
         if (lane == 0) sh.n = 0;
+        __syncwarp();
         for (int s0 = 0; s0 < b.n_seq; s0 += 32) {
             const int s = s0 + lane;
             int f = s, m = s < b.n_seq ? 1 : 0;

@@ -336,6 +336,19 @@ def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     assert c.status.item() == 0
 
 
+@pytest.mark.parametrize("n_seq,most", [(31, 90), (32, 400), (40, 90), (70, 200)])
+def test_prompts_of_many_sequences(kv, n_seq, most):
+    """Items go by their tokens over up to 32 sequences and by sequence beyond: every row is somebody's, empty sequences and rows before
+    position 0 among them."""
+    g = torch.Generator().manual_seed(n_seq)
+    lengths = torch.randint(0, most, (n_seq,), generator=g).tolist()
+    rows = torch.randint(0, 50, (n_seq,), generator=g).tolist()
+    lengths[0], rows[0], lengths[1], rows[1], lengths[2], rows[2] = 0, 33, most, 0, most, 47
+    c = Case(kv, 25, lengths, rows, 1, 64, 16, BF16, 2, wide_table=1, fill=True)
+    check_attend(c, 16)
+    assert c.status.item() == 0
+
+
 @pytest.mark.parametrize("rows,heads", [([1, 1], 4), ([200, 64], 4), ([200, 64], 16)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_values_and_keys_of_any_size(kv, rows, heads, dtype):
