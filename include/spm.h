@@ -518,8 +518,9 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
 
 /* out = softmax(scale * q K^T) V for each new row and each of its n_q_heads heads (a multiple of n_kv_heads: query head h reads cache head
  * h / (n_q_heads / n_kv_heads)), over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's
- * statistics and all sums are fp32. bf16 calls round a probability, times its value's scale, once to bf16, or (calls of many rows) a
- * probability, a key and a value once each to fp16; fp32 calls round nothing but their sums. bf16 queries are below 2^63 in magnitude.
+ * statistics and all sums are fp32. bf16 calls round a probability and its product with its value's scale to fp16's 11 bits (fewer for
+ * probabilities below 2^-22 of the largest, scales below 2^-15 of their group's largest so far and products below 2^-23), or (calls of many
+ * rows) a probability, a key and a value once each; fp32 calls round nothing but their sums. bf16 queries are below 2^63 in magnitude.
  * out may not overlap q. Results do not depend on the order in which CTAs run, and are the same bits for the same call.
  * workspace: dev, 16-byte aligned, at least spm_kv_attend_workspace() bytes; what it held before does not matter, and calls that may run
  * at the same time need one each. */

@@ -8,10 +8,10 @@
 // Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
 // bf16 calls leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is what the group's sum starts
 // with. Values: the same words are fp16 subnormals, and probabilities times scales are fp16 numbers, of 11 bits and not bf16's 8: with bf16
-// the result's error was 1.5 times that of its own rounding, now it is 1.02 times that (64 sequences of up to 16001 tokens, 268 MB: 71 us
-// then, 73 now). For their range a group's scales are taken to 2^5 by a power of two that is above all of them so far, kept like the running
-// maximum; a probability and its product with the scale are each rounded to 11 bits while probability times scale is at least 2^-23 of the
-// most, to multiples of 2^-34 of the most below that. One more product with -8 in the codes' place goes into the
+// the result's error was 1.5 times that of its own rounding, now it is 1.02 times that, for 2 % of the time.
+// For their range a group's scales are taken to 2 by a power of two that is above all of them so far, kept like the running
+// maximum, and probabilities to 2^8: fp16's 11 bits hold for a probability down to 2^-22 of the largest, a scale down to 2^-15 of its
+// group's largest and their product down to 2^-23, and no product is above 65504. One more product with -8 in the codes' place goes into the
 // running sum before theirs, so that what is left to round is a tile's and not the whole context's sum of codes. fp32 calls subtract the 8
 // from each code, nine instructions for eight, and lose nothing to it.
 //
@@ -21,7 +21,7 @@
 // CTAs, in the workspace, where kv_attend_join_kernel adds them in order.
 //
 // What bounds it: instructions and their latencies, some 660 a tile for eight columns or one, 53 % of the issue slots with four warps a
-// scheduler (which is what 128 registers leave); memory waits. 64 sequences of up to 16001 tokens, 268 MB: 69 us, 3.9 TB/s, of it 2.2 us a
+// scheduler (which is what 128 registers leave); not memory. 64 sequences of up to 16001 tokens, 268 MB: 69 us, 3.9 TB/s, of it 2.2 us a
 // tile and warp, and 10 us at the ends (the kernel before, counting and finding the tiles 4, the parts' joining 4). More column tiles a warp
 // (16, 32 columns) were slower a column, and so were 12 warps with deeper rings, and loops rolled up against the size of the code.
 #pragma once
@@ -37,13 +37,16 @@ struct AttendArgs {
     KvBatch batch;
     HeadRows q, out;
     int group;                  // query heads a cache head
-    int page_shift;             // blocks a page are 1 << page_shift, or -1
+    int page_shift, group_shift;        // blocks a page, query heads a cache head are 1 << this, or -1
     float scale;
     float* parts;               // [2 * CTAs][part floats]
     int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns,
                                 // head, first row, rows
     int once;                   // every block is read by one warp alone
 };
+
+// Row of column x (eight sequences of five drafted rows, 8 heads a cache head: 26.1 us with the division alone, 24.9)
+__device__ __forceinline__ int column_row(const AttendArgs& a, int x) { return a.group_shift >= 0 ? x >> a.group_shift : x / a.group; }
 
 constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
@@ -61,8 +64,8 @@ struct AtShape {
     static constexpr int warps = HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
     static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : 3;
     static constexpr bool raw = sizeof(T) == 2;              // codes as they are masked out
-    static constexpr float up = raw ? 4.f : 0.f;                        // probabilities are taken to 2^4 then, so that none is above 2^10
-    static constexpr float unscale = raw ? 0x1p19f : kQ4ExactUnscale;   // of sums of codes times probabilities
+    static constexpr float up = raw ? 8.f : 0.f;                        // probabilities are taken to 2^8 then, so that none is above 2^14
+    static constexpr float unscale = raw ? 0x1p23f : kQ4ExactUnscale;   // of sums of codes times probabilities
     // a sum of an odd element, beside that of the even one before it
     __device__ static float odd(float both, float low) { return raw ? (both - low) * (1.f / 16.f) : both; }
     static constexpr int ring_bytes = stages * tile_bytes;
@@ -88,7 +91,7 @@ struct Walk {
     }
     __device__ __forceinline__ int blocks(const AttendArgs& a) const { return n > 0 ? (n * a.group + COLS - 1) / COLS : 0; }
     __device__ __forceinline__ void columns(const AttendArgs& a) {
-        const int last = n == 1 ? 0 : min(n - 1, ((ct + 1) * COLS - 1) / a.group);
+        const int last = n == 1 ? 0 : min(n - 1, column_row(a, (ct + 1) * COLS - 1));
         nk = max(0, min(len - n + last + 1, a.batch.stride * a.kv.page_size));
         nt = max(1, (nk + kAtTile - 1) / kAtTile);
     }
@@ -145,7 +148,7 @@ struct Walk {
 // Where a column's result goes: its row, -1 where the item has no such column
 template <int COLS>
 __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int n, int ct, int col, int& g) {
-    const int x = ct * COLS + col, i = n == 1 ? (x >= a.group) : x / a.group;
+    const int x = ct * COLS + col, i = n == 1 ? (x >= a.group) : column_row(a, x);
     g = x - i * a.group;
     return i < n && first + i >= 0 && first + i < a.batch.n_rows ? first + i : -1;
 }
@@ -201,7 +204,7 @@ __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
 // would leave the range of numbers).
 constexpr uint32_t kAtUp64 = 0x5f805f80u, kAtUp60 = 0x5d805d80u;
 constexpr float kAtUp69 = 0x1p69f;
-constexpr uint32_t kAtNarrowest = 0x18001800u, kAtWidest = 0x78007800u;     // 2^-9, 2^15
+constexpr uint32_t kAtNarrowest = 0x04000400u, kAtWidest = 0x78007800u;     // 2^-14, 2^15
 // A word's bytes as operands: the low nibble of bytes 0, 2 and both nibbles of them (low + 16 high, also linear), the same of bytes 1, 3:
 // four instructions. Values' elements are rows of the product, so the high nibble's sum is had from the two.
 constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus136 = 0x80888088u;      // -8 and -8 - 16 * 8 as codes
@@ -476,7 +479,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 __syncwarp();
             }
             began = t;
-            whole_tiles = min(use.nk, use.len - use.n + use.ct * COLS / a.group + 1) / kAtTile;
+            whole_tiles = min(use.nk, use.len - use.n + column_row(a, use.ct * COLS) + 1) / kAtTile;
         };
         begin();
         int stage = 0;
@@ -523,7 +526,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             if (!whole) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int i2 = (use.ct * COLS + 2 * c + e) / a.group;
+                    const int i2 = column_row(a, use.ct * COLS + 2 * c + e);
                     const int sees = min(use.nk, use.len - use.n + i2 + 1) - t * kAtTile;      // tokens of this tile
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
@@ -612,7 +615,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
 #pragma unroll
                     for (int k = 0; k < G; k += 2) {
                         const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
-                        const __half2 down = as_half2(0x8c008c00u - wide[k / 2]);          // 2^5 / wide
+                        const __half2 down = as_half2(0x7c007c00u - wide[k / 2]);          // 2 / wide
                         const __half2 s0 = __hmul2(as_half2(vs[b][0][k / 2]), down), s1 = __hmul2(as_half2(vs[b][1][k / 2]), down);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {

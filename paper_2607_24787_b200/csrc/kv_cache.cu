@@ -276,9 +276,11 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.q = rows_of(q); a.out = rows_of(out);
     a.group = n_q_heads / kv->n_kv_heads;
     const int per_page = kv->page_size / kKvBlock;
-    a.page_shift = -1;
-    for (int i = 0; i < 16; ++i)
+    a.page_shift = a.group_shift = -1;
+    for (int i = 0; i < 16; ++i) {
         if (per_page == 1 << i) a.page_shift = i;
+        if (a.group == 1 << i) a.group_shift = i;
+    }
     // (a guess where max_rows is one: it only says what to keep in L2)
     a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8);
     a.scale = scale;

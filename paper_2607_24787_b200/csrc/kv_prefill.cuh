@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     }
     if (len > cap && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
     // tiles of a half: up to the token that its last row sees
-    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x / a.group) + 1, cap)); };
+    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, column_row(a, x)) + 1, cap)); };
     const bool used1 = rb * kPfCols + kPfTile < n * a.group;
     const int tiles0 = (sees(rb * kPfCols + kPfTile - 1) + kPfTile - 1) / kPfTile;
     const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kPfTile - 1) / kPfTile : 0;
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     int row = -1, g = 0, limit = 0;
     float f = 1.f;
     if (warp < 8) {
-        const int x = rb * kPfCols + tid, i = x / a.group;
+        const int x = rb * kPfCols + tid, i = column_row(a, x);
         g = x - i * a.group;
         if (i < n && first + i >= 0 && first + i < b.n_rows) row = first + i;
         limit = sees(x);
