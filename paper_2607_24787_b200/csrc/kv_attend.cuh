@@ -3,8 +3,10 @@
 // For a cache head, the new rows' query heads that read it are columns: column x is head x % group of row x / group, and eight columns are
 // the N of an m16n8k16. Keys are its A operand (16 tokens by 16 elements) straight from their nibbles, and the scale of a group is put on
 // the sum of the group's 32 products. Values are the A operand of the second product, transposed by ldmatrix (32 elements by 16 tokens);
-// their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries and scaled probabilities are split
-// into three bf16 parts each.
+// their scale goes onto the probability, which is the B operand, so no value is ever rounded. fp32 queries and scaled probabilities are two
+// fp16 parts each, the number's rounding and the rounding of what that leaves: 23 bits at least, down to 2^-40 of a head's largest query
+// element and 2^-34 of the largest product (three bf16 parts, 24 bits and six products for four, took 72.7 us where these take 69.2: 64
+// sequences of 4096 tokens, 32 heads on 4).
 // Nibbles are exact operands as they are masked out of their word, as bf16 subnormals (q4_mma.cuh): five instructions for eight of them.
 // bf16 calls leave them so. Keys: the query is scaled up to them, and -8 times the sum of a group's queries is what the group's sum starts
 // with. Values: the same words are fp16 subnormals, and probabilities times scales are fp16 numbers, of 11 bits and not bf16's 8: with bf16
@@ -13,7 +15,8 @@
 // maximum, and probabilities to 2^8: fp16's 11 bits hold for a probability down to 2^-22 of the largest, a scale down to 2^-15 of its
 // group's largest and their product down to 2^-23, and no product is above 65504. One more product with -8 in the codes' place goes into the
 // running sum before theirs, so that what is left to round is a tile's and not the whole context's sum of codes. fp32 calls subtract the 8
-// from each code, nine instructions for eight, and lose nothing to it.
+// from each code, nine instructions for eight, and lose nothing to it; a tile's sums are added to the running ones outside of the products,
+// which cut sums off where they do not round them.
 //
 // All (sequence, columns, head) items together are a line of tiles of 32 tokens that is cut evenly between CTAs, and a CTA's piece
 // evenly between its warps, whatever the lengths are: a warp walks its tiles with the running maximum and sum of each column, fed by its
@@ -64,8 +67,8 @@ struct AtShape {
     static constexpr int warps = HD == 256 ? 8 : sizeof(T) == 4 ? 12 : 16;
     static constexpr int stages = HD == 64 ? 4 : HD == 256 || warps == 16 ? 2 : 3;
     static constexpr bool raw = sizeof(T) == 2;              // codes as they are masked out
-    static constexpr float up = raw ? 8.f : 0.f;                        // probabilities are taken to 2^8 then, so that none is above 2^14
-    static constexpr float unscale = raw ? 0x1p23f : kQ4ExactUnscale;   // of sums of codes times probabilities
+    static constexpr float up = 8.f;                       // probabilities are taken to 2^8 then, so that none is above 2^14
+    static constexpr float unscale = raw ? 0x1p23f : 0.5f;   // of sums of codes times probabilities
     // a sum of an odd element, beside that of the even one before it
     __device__ static float odd(float both, float low) { return raw ? (both - low) * (1.f / 16.f) : both; }
     static constexpr int ring_bytes = stages * tile_bytes;
@@ -181,6 +184,24 @@ __device__ __forceinline__ void mma_half_k16(float (&d)[4], uint32_t a0, uint32_
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_half_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// A word's codes less 8 as fp16, exact: 1024 + code and 1024 + 16 code are numbers
+__device__ __forceinline__ Nib4 q4_halves(uint32_t w) {
+    const __half2 off = as_half2(0xe408e408u), sixteenth = as_half2(0x2c002c00u), off72 = as_half2(0xd480d480u);       // -1032, 1 / 16, -72
+    const uint32_t v = w >> 8;
+    return Nib4{{bits_of(__hadd2(as_half2((w & 0x000f000fu) | 0x64006400u), off)), bits_of(__hfma2(as_half2((w & 0x00f000f0u) | 0x64006400u), sixteenth, off72)),
+                 bits_of(__hadd2(as_half2((v & 0x000f000fu) | 0x64006400u), off)), bits_of(__hfma2(as_half2((v & 0x00f000f0u) | 0x64006400u), sixteenth, off72))}};
+}
+// Two numbers as fp16, and what that leaves of them
+__device__ __forceinline__ void two_parts(float x0, float x1, uint32_t& high, uint32_t& low) {
+    const __half2 h = __floats2half2_rn(x0, x1);
+    const float2 f = __half22float2(h);
+    high = bits_of(h);
+    low = pack_half(x0 - f.x, x1 - f.y);
+}
 // HD / 32 scales of a token, two a word; as numbers
 template <int G>
 __device__ __forceinline__ void scale_words(uint32_t addr, uint32_t (&w)[G / 2]) {
@@ -212,24 +233,16 @@ __device__ __forceinline__ Nib4 q4_bytes(uint32_t w) {
     const uint32_t even = w & 0x00ff00ffu, odd = __byte_perm(w, 0u, 0x4341);
     return Nib4{{even & 0x000f000fu, even, odd & 0x000f000fu, odd}};
 }
-template <bool RAW>
 __device__ __forceinline__ void query_words(uint32_t (&w)[1][4], bool flip) {          // in: eight bf16 numbers as they were loaded
     const uint32_t x = w[0][0], y = w[0][1], z = w[0][2], u = w[0][3], sign = flip ? 0x80008000u : 0u;
     w[0][0] = __byte_perm(x, z, 0x5410) ^ sign; w[0][1] = __byte_perm(x, z, 0x7632) ^ sign;
     w[0][2] = __byte_perm(y, u, 0x5410) ^ sign; w[0][3] = __byte_perm(y, u, 0x7632) ^ sign;
-    if constexpr (RAW) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? kAtUp60 : kAtUp64)));
-    }
+    for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? kAtUp60 : kAtUp64)));
 }
-template <bool RAW>
-__device__ __forceinline__ void query_words(uint32_t (&w)[3][4], bool flip) {          // in: eight fp32 numbers in the first two parts
-    const uint32_t sign = flip ? 0x80000000u : 0u;
+__device__ __forceinline__ void query_parts(uint32_t (&w)[2][4], float by) {           // in: eight fp32 numbers
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const Split3 s = split3(__uint_as_float(w[0][i] ^ sign), __uint_as_float(w[1][i] ^ sign));
-        w[0][i] = s.part[0]; w[1][i] = s.part[1]; w[2][i] = s.part[2];
-    }
+    for (int i = 0; i < 4; ++i) two_parts(__uint_as_float(w[0][i]) * by, __uint_as_float(w[1][i]) * by, w[0][i], w[1][i]);
 }
 
 template <typename T, int HD>
@@ -237,7 +250,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     using S = AtShape<T, HD>;
     constexpr int G = HD / 32, COLS = S::cols, W = S::warps, STAGES = S::stages, BB = kv_block_bytes(HD);
     constexpr bool RAW = S::raw;
-    constexpr int QP = sizeof(T) == 4 ? 3 : 1;                 // parts of a query
+    constexpr int QP = sizeof(T) / 2;                          // parts of a query
     extern __shared__ __align__(128) unsigned char smem[];
     // pieces of a line go round the SM's four schedulers a quarter of the warps apart, so that a CTA of a few tiles uses all four
     const int tid = threadIdx.x, lane = tid & 31, place = tid >> 5, warp = (place & 3) * (W / 4) + (place >> 2), r = lane >> 2, c = lane & 3;
@@ -370,7 +383,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
 #pragma unroll
             for (int k = 0; k < G; ++k)
 #pragma unroll
-                for (int q = 0; q < (QP + 1) / 2; ++q) {
+                for (int q = 0; q < QP; ++q) {
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (row >= 0) v = *reinterpret_cast<const uint4*>(p + 32 * k + 4 * q);
                     qf[q][k][0] = v.x; qf[q][k][1] = v.y; qf[q][k][2] = v.z; qf[q][k][3] = v.w;
@@ -435,11 +448,32 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             if (i < count) issue(i);
         // scores are kept as the products give them; f > 0 takes them to powers of two (a negative scale turns the queries' signs, and
         // with a scale of 0 a masked score still counts as one)
-        const float f = fmaxf(fabsf(a.scale), 1e-30f) * ((RAW ? kAtUp69 : kQ4ExactUnscale) * 1.4426950408889634f), slack = 6.f / f;
+        constexpr int FS = RAW ? 1 : 2;          // (fp32 columns have a power of two each)
+        float f[FS], slack[FS];
+        f[0] = fmaxf(fabsf(a.scale), 1e-30f) * (kAtUp69 * 1.4426950408889634f);
+        slack[0] = 6.f / f[0];
         const bool flip = a.scale < 0.f;
         int whole_tiles = 0;
         int began = 0;                           // the item's tile with which this warp's part of it begins
         auto begin = [&] {
+            float by = 1.f;                      // fp32 queries: a column's largest to [2^14, 2^15)
+            if constexpr (!RAW) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int k = 0; k < G; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = max(top, max(qf[0][k][j] & 0x7fffffffu, qf[1][k][j] & 0x7fffffffu));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int e = top == 0 || top >= 0x7f800000u ? 0 : min(100, 14 - (int(top >> 23) - 127));
+                by = __int_as_float((127 + e) << 23);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {    // (so small a factor makes all scores alike)
+                    f[i] = fmaxf(fmaxf(fabsf(a.scale), 1e-30f) * 1.4426950408889634f / __shfl_sync(0xffffffffu, by, (2 * c + i) * 4), 1e-35f);
+                    slack[i] = 6.f / f[i];
+                }
+                if (flip) by = -by;
+            }
 #pragma unroll
             for (int k = 0; k < G; ++k) {
                 uint32_t w[QP][4];
@@ -447,7 +481,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 for (int q = 0; q < QP; ++q)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[q][j] = qf[q][k][j];
-                query_words<RAW>(w, flip);
+                if constexpr (RAW) query_words(w, flip);
+                else query_parts(w, by);
 #pragma unroll
                 for (int q = 0; q < QP; ++q)
 #pragma unroll
@@ -473,11 +508,9 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             }
             m[0] = m[1] = -INFINITY;
             l[0] = l[1] = 0.f;
-            if constexpr (RAW) {
 #pragma unroll
-                for (int k = 0; k < G / 2; ++k) wide[k] = kAtNarrowest;
-                __syncwarp();
-            }
+            for (int k = 0; k < G / 2; ++k) wide[k] = kAtNarrowest;
+            if constexpr (RAW) __syncwarp();
             began = t;
             whole_tiles = min(use.nk, use.len - use.n + column_row(a, use.ct * COLS) + 1) / kAtTile;
         };
@@ -507,14 +540,16 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t low = h ? w.z : w.x, high = h ? w.w : w.y;
-                        const Nib4 u = RAW ? q4_unpack(low) : q4_exact(low), v = RAW ? q4_unpack(high) : q4_exact(high);
+                        const Nib4 u = RAW ? q4_unpack(low) : q4_halves(low), v = RAW ? q4_unpack(high) : q4_halves(high);
                         float d[4];
-                        if constexpr (RAW) mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
-                        else mma_k16_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
-#pragma unroll
-                        for (int q = 0; q < QP; ++q) {
-                            if (q > 0) mma_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[q][k + h][0], qf[q][k + h][1]);
-                            mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[q][k + h][2], qf[q][k + h][3]);
+                        if constexpr (RAW) {
+                            mma_k16_from(d, starts[warp][k + h][c], u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
+                            mma_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[0][k + h][2], qf[0][k + h][3]);
+                        } else {
+                            mma_half_first(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[1][k + h][0], qf[1][k + h][1]);
+                            mma_half_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[1][k + h][2], qf[1][k + h][3]);
+                            mma_half_k16(d, u.p[0], v.p[0], u.p[1], v.p[1], qf[0][k + h][0], qf[0][k + h][1]);
+                            mma_half_k16(d, u.p[2], v.p[2], u.p[3], v.p[3], qf[0][k + h][2], qf[0][k + h][3]);
                         }
                         s[b][0] += s0[k + h] * d[0]; s[b][1] += s0[k + h] * d[1];
                         s[b][2] += s1[k + h] * d[2]; s[b][3] += s1[k + h] * d[3];
@@ -545,49 +580,45 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
                 top[e] = v;
-                raise |= v > m[e] + slack;         // (-infinity is not above -infinity)
+                raise |= v > m[e] + slack[e % FS];         // (-infinity is not above -infinity)
             }
-            // ---- bf16: the values' scales, and whether one is above its group's power of two (what has never been written may be anything) ----
+            // ---- the values' scales, and whether one is above its group's power of two (what has never been written may be anything) ----
             uint32_t vs[2][2][G / 2], widest[G / 2];
-            if constexpr (RAW) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        scale_words<G>(at + b * BB + kv_v_scales(HD) + (8 * j + r) * (2 * G), vs[b][j]);
-                        if (!whole && (!(have >> b & 1) || t * kAtTile + 16 * b + 8 * j + r >= use.nk))
+                for (int j = 0; j < 2; ++j) {
+                    scale_words<G>(at + b * BB + kv_v_scales(HD) + (8 * j + r) * (2 * G), vs[b][j]);
+                    if (!whole && (!(have >> b & 1) || t * kAtTile + 16 * b + 8 * j + r >= use.nk))
 #pragma unroll
-                            for (int k = 0; k < G / 2; ++k) vs[b][j][k] = 0;
-                    }
-#pragma unroll
-                for (int k = 0; k < G / 2; ++k) {
-                    auto of = [&](int b, int j) { return __habs2(as_half2(vs[b][j][k])); };
-                    widest[k] = bits_of(__hmax2(__hmax2(__hmax2(of(0, 0), of(0, 1)), __hmax2(of(1, 0), of(1, 1))), as_half2(wide[k])));
-                    raise |= widest[k] != wide[k];
+                        for (int k = 0; k < G / 2; ++k) vs[b][j][k] = 0;
                 }
+#pragma unroll
+            for (int k = 0; k < G / 2; ++k) {
+                auto of = [&](int b, int j) { return __habs2(as_half2(vs[b][j][k])); };
+                widest[k] = bits_of(__hmax2(__hmax2(__hmax2(of(0, 0), of(0, 1)), __hmax2(of(1, 0), of(1, 1))), as_half2(wide[k])));
+                raise |= widest[k] != wide[k];
             }
             if (__any_sync(0xffffffffu, raise)) {
-                if constexpr (RAW) {
 #pragma unroll
-                    for (int k = 0; k < G / 2; ++k) {
-                        uint32_t w = widest[k];
-                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 4));
-                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 8));
-                        w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 16));
-                        w = __vminu2(w, kAtWidest) + 0x03ff03ffu & 0x7c007c00u;
-                        const float2 was = __half22float2(as_half2(wide[k])), is = __half22float2(as_half2(w));
-                        const float by0 = was.x / is.x, by1 = was.y / is.y;
+                for (int k = 0; k < G / 2; ++k) {
+                    uint32_t w = widest[k];
+                    w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 4));
+                    w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 8));
+                    w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, 16));
+                    w = __vminu2(w, kAtWidest) + 0x03ff03ffu & 0x7c007c00u;
+                    const float2 was = __half22float2(as_half2(wide[k])), is = __half22float2(as_half2(w));
+                    const float by0 = was.x / is.x, by1 = was.y / is.y;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            y[2 * k][0][j] *= by0; y[2 * k][1][j] *= by0;
-                            y[2 * k + 1][0][j] *= by1; y[2 * k + 1][1][j] *= by1;
-                        }
-                        wide[k] = w;
+                    for (int j = 0; j < 4; ++j) {
+                        y[2 * k][0][j] *= by0; y[2 * k][1][j] *= by0;
+                        y[2 * k + 1][0][j] *= by1; y[2 * k + 1][1][j] *= by1;
                     }
+                    wide[k] = w;
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f);
+                    const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f[e % FS]);
                     m[e] = to;
                     l[e] *= by;
 #pragma unroll
@@ -596,12 +627,12 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f) + S::up;
+                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f[e % FS]) + S::up;
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float p = ex2(fmaf(s[b][2 * j + e], f, base));
+                        const float p = ex2(fmaf(s[b][2 * j + e], f[e % FS], base));
                         s[b][2 * j + e] = p;
                         l[e] += p;
                     }
@@ -630,39 +661,27 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                     }
                 } else {
                     float s0[G], s1[G];
-                    token_scales<G>(block + kv_v_scales(HD) + r * (2 * G), s0);
-                    token_scales<G>(block + kv_v_scales(HD) + (r + 8) * (2 * G), s1);
-                    if (!whole) {
 #pragma unroll
-                        for (int k = 0; k < G; ++k) {
-                            if (!(have >> b & 1) || t * kAtTile + 16 * b + r >= use.nk) s0[k] = 0.f;
-                            if (!(have >> b & 1) || t * kAtTile + 16 * b + 8 + r >= use.nk) s1[k] = 0.f;
-                        }
+                    for (int k = 0; k < G / 2; ++k) {
+                        const float2 down = __half22float2(as_half2(0x7c007c00u - wide[k]));     // 2 / wide
+                        const float2 f0 = __half22float2(as_half2(vs[b][0][k])), f1 = __half22float2(as_half2(vs[b][1][k]));
+                        s0[2 * k] = f0.x * down.x; s0[2 * k + 1] = f0.y * down.y; s1[2 * k] = f1.x * down.x; s1[2 * k + 1] = f1.y * down.y;
                     }
 #pragma unroll
                     for (int k = 0; k < G; k += 2) {
                         const uint4 w = ldsm4t(block + kv_v_codes(HD) + (k + (lane >> 4)) * (kKvBlock * 16) + (lane & 15) * 16);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const Nib4 u = q4_exact(h ? w.z : w.x), v = q4_exact(h ? w.w : w.y);
-                            float p0 = s[b][0] * s0[k + h], p1 = s[b][1] * s0[k + h], p2 = s[b][2] * s1[k + h], p3 = s[b][3] * s1[k + h];
-                            float d[2][4];       // (a product cuts its sum off where it does not round it: the running sum is added outside of it)
-#pragma unroll
-                            for (int q = 0; q < 3; ++q) {
-                                const uint32_t lo2 = pack_bf16(p0, p1), hi2 = pack_bf16(p2, p3), b0 = transpose8(lo2), b1 = transpose8(hi2);
-                                if (q < 2) {
-                                    float x0, x1;
-                                    two_bf16(lo2, x0, x1); p0 -= x0; p1 -= x1;
-                                    two_bf16(hi2, x0, x1); p2 -= x0; p3 -= x1;
-                                }
-                                if (q == 0) {
-                                    mma_k16_first(d[0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
-                                    mma_k16_first(d[1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
-                                } else {
-                                    mma_k16(d[0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
-                                    mma_k16(d[1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
-                                }
-                            }
+                            const Nib4 u = q4_halves(h ? w.z : w.x), v = q4_halves(h ? w.w : w.y);
+                            uint32_t b0, b1, low0, low1;
+                            two_parts(s[b][0] * s0[k + h], s[b][1] * s0[k + h], b0, low0);
+                            two_parts(s[b][2] * s1[k + h], s[b][3] * s1[k + h], b1, low1);
+                            b0 = transpose8(b0); b1 = transpose8(b1); low0 = transpose8(low0); low1 = transpose8(low1);
+                            float d[2][4];
+                            mma_half_first(d[0], u.p[0], u.p[1], v.p[0], v.p[1], low0, low1);
+                            mma_half_first(d[1], u.p[2], u.p[3], v.p[2], v.p[3], low0, low1);
+                            mma_half_k16(d[0], u.p[0], u.p[1], v.p[0], v.p[1], b0, b1);
+                            mma_half_k16(d[1], u.p[2], u.p[3], v.p[2], v.p[3], b0, b1);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) { y[k + h][0][j] += d[0][j]; y[k + h][1][j] += d[1][j]; }
                         }
@@ -684,15 +703,13 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                     v += __shfl_xor_sync(0xffffffffu, v, 16);
                     l[e] = v;
                 }
-                if constexpr (RAW) {
 #pragma unroll
-                    for (int k = 0; k < G / 2; ++k) {
-                        const float2 by = __half22float2(as_half2(wide[k]));
+                for (int k = 0; k < G / 2; ++k) {
+                    const float2 by = __half22float2(as_half2(wide[k]));
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            y[2 * k][0][j] *= by.x; y[2 * k][1][j] *= by.x;
-                            y[2 * k + 1][0][j] *= by.y; y[2 * k + 1][1][j] *= by.y;
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        y[2 * k][0][j] *= by.x; y[2 * k][1][j] *= by.x;
+                        y[2 * k + 1][0][j] *= by.y; y[2 * k + 1][1][j] *= by.y;
                     }
                 }
                 if (ends && began == 0) {        // all of it is this warp's
@@ -720,7 +737,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                         for (int k = 0; k < G; ++k)
                             *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) =
                                 make_float4(y[k][0][e], S::odd(y[k][0][2 + e], y[k][0][e]), y[k][1][e], S::odd(y[k][1][2 + e], y[k][1][e]));
-                        if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f; part[COLS * HD + COLS + col] = l[e]; }
+                        if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f[e % FS]; part[COLS * HD + COLS + col] = l[e]; }
                     }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - t, use.ct, use.head, began, t + 1, use.nt, use.first, use.n};
                 }
