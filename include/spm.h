@@ -520,8 +520,7 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
  * h / (n_q_heads / n_kv_heads)), over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's
  * statistics and all sums are fp32. bf16 calls round a probability and its product with its value's scale to fp16's 11 bits (fewer for
  * probabilities below 2^-22 of the largest, scales below 2^-15 of their group's largest so far and products below 2^-23), or (calls of many
- * rows) a probability, a key and a value once each; fp32 calls keep 23 bits of a query and of a probability times a scale. bf16 queries are
- * below 2^63 in magnitude.
+ * rows) a probability, a key and a value once each; fp32 calls keep 23 bits of a query and of a probability times a scale.
  * out may not overlap q. Results do not depend on the order in which CTAs run, and are the same bits for the same call.
  * workspace: dev, 16-byte aligned, at least spm_kv_attend_workspace() bytes; what it held before does not matter, and calls that may run
  * at the same time need one each. */

@@ -24,8 +24,8 @@
 // CTAs, in the workspace, where kv_attend_join_kernel adds them in order.
 //
 // What bounds it: instructions and their latencies, some 660 a tile for eight columns or one, 53 % of the issue slots with four warps a
-// scheduler (which is what 128 registers leave); not memory. 64 sequences of up to 16001 tokens, 268 MB: 69 us, 3.9 TB/s, of it 2.2 us a
-// tile and warp, and 10 us at the ends (the kernel before, counting and finding the tiles 4, the parts' joining 4). More column tiles a warp
+// scheduler (which is what 128 registers leave); not memory. 64 sequences of up to 16001 tokens, 268 MB: 70 us, 3.8 TB/s, of it 2.2 us a
+// tile and warp, and 11 us at the ends (the kernel before, counting and finding the tiles 4, the parts' joining 4). More column tiles a warp
 // (16, 32 columns) were slower a column, and so were 12 warps with deeper rings, and loops rolled up against the size of the code.
 #pragma once
 
@@ -220,12 +220,13 @@ __device__ __forceinline__ void token_scales(uint32_t addr, float (&s)[G]) {
     }
 }
 
-// One column's group of queries as the B operand: pairs (i, i + 4) of the eight elements 8 c .. 8 c + 7. bf16 queries are taken to the
-// nibbles' scale: 2^64 to codes of 2^-133, 2^60 to 16 times those; sums then stand at 2^-69 (queries of 2^63 and more, or below 2^-57,
-// would leave the range of numbers).
-constexpr uint32_t kAtUp64 = 0x5f805f80u, kAtUp60 = 0x5d805d80u;
+// One column's group of queries as the B operand: pairs (i, i + 4) of the eight elements 8 c .. 8 c + 7. bf16 columns are taken by a power of
+// two to a largest element in [1, 2), times 2^64 for codes of 2^-133 and 2^60 for 16 times those; sums then stand at 2^-69.
 constexpr float kAtUp69 = 0x1p69f;
 constexpr uint32_t kAtNarrowest = 0x04000400u, kAtWidest = 0x78007800u;     // 2^-14, 2^15
+// Of a column's factor of scores. So small a one makes all alike, and yet a masked score stays one; so large a one makes all differ.
+constexpr float kAtLeast = 1e-35f, kAtMost = 0x1p80f;
+__device__ __forceinline__ uint32_t bf16_power(int e) { return uint32_t(127 + e << 7) * 0x10001u; }
 // A word's bytes as operands: the low nibble of bytes 0, 2 and both nibbles of them (low + 16 high, also linear), the same of bytes 1, 3:
 // four instructions. Values' elements are rows of the product, so the high nibble's sum is had from the two.
 constexpr uint32_t kAtMinus8 = 0x80088008u, kAtMinus136 = 0x80888088u;      // -8 and -8 - 16 * 8 as codes
@@ -233,12 +234,12 @@ __device__ __forceinline__ Nib4 q4_bytes(uint32_t w) {
     const uint32_t even = w & 0x00ff00ffu, odd = __byte_perm(w, 0u, 0x4341);
     return Nib4{{even & 0x000f000fu, even, odd & 0x000f000fu, odd}};
 }
-__device__ __forceinline__ void query_words(uint32_t (&w)[1][4], bool flip) {          // in: eight bf16 numbers as they were loaded
+__device__ __forceinline__ void query_words(uint32_t (&w)[1][4], uint32_t up64, uint32_t up60, bool flip) {         // in: eight bf16 numbers as they were loaded
     const uint32_t x = w[0][0], y = w[0][1], z = w[0][2], u = w[0][3], sign = flip ? 0x80008000u : 0u;
     w[0][0] = __byte_perm(x, z, 0x5410) ^ sign; w[0][1] = __byte_perm(x, z, 0x7632) ^ sign;
     w[0][2] = __byte_perm(y, u, 0x5410) ^ sign; w[0][3] = __byte_perm(y, u, 0x7632) ^ sign;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? kAtUp60 : kAtUp64)));
+    for (int i = 0; i < 4; ++i) w[0][i] = bits2(__hmul2(bf2(w[0][i]), bf2(i & 1 ? up60 : up64)));
 }
 __device__ __forceinline__ void query_parts(uint32_t (&w)[2][4], float by) {           // in: eight fp32 numbers
 #pragma unroll
@@ -448,32 +449,38 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             if (i < count) issue(i);
         // scores are kept as the products give them; f > 0 takes them to powers of two (a negative scale turns the queries' signs, and
         // with a scale of 0 a masked score still counts as one)
-        constexpr int FS = RAW ? 1 : 2;          // (fp32 columns have a power of two each)
-        float f[FS], slack[FS];
-        f[0] = fmaxf(fabsf(a.scale), 1e-30f) * (kAtUp69 * 1.4426950408889634f);
-        slack[0] = 6.f / f[0];
+        float f[2], slack[2];                    // of columns 2 c, 2 c + 1
         const bool flip = a.scale < 0.f;
         int whole_tiles = 0;
         int began = 0;                           // the item's tile with which this warp's part of it begins
         auto begin = [&] {
-            float by = 1.f;                      // fp32 queries: a column's largest to [2^14, 2^15)
-            if constexpr (!RAW) {
-                uint32_t top = 0;
+            uint32_t tops[4] = {};               // a column's largest query element, of which the exponent counts
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (RAW) tops[j] = __vmaxu2(tops[j], qf[0][k][j] & 0x7fff7fffu);
+                    else tops[j] = max(tops[j], max(qf[0][k][j] & 0x7fffffffu, qf[1][k][j] & 0x7fffffffu));
+                }
+            uint32_t top = RAW ? __vmaxu2(__vmaxu2(tops[0], tops[1]), __vmaxu2(tops[2], tops[3])) : max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+            top = RAW ? max(top & 0xffffu, top >> 16) >> 7 : top >> 23;
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = top == 0 ? -126 : top == 255 ? 0 : int(top) - 127;
+            const int up = RAW ? -e : min(100, 14 - e);          // fp32 columns go to [2^14, 2^15)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float down = __int_as_float((127 - __shfl_sync(0xffffffffu, up, (2 * c + i) * 4)) << 23);
+                f[i] = fminf(fmaxf(fabsf(a.scale) * 1.4426950408889634f * down * (RAW ? kAtUp69 : 1.f), kAtLeast), RAW ? kAtMost * 0x1p40f : kAtMost);
+                slack[i] = __fdividef(6.f, f[i]);
+            }
+            const bool tiny = RAW && e < -60;    // 2^(64 - e) is no number then: in two steps
+            if (__any_sync(0xffffffffu, tiny))
 #pragma unroll
                 for (int k = 0; k < G; ++k)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) top = max(top, max(qf[0][k][j] & 0x7fffffffu, qf[1][k][j] & 0x7fffffffu));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const int e = top == 0 || top >= 0x7f800000u ? 0 : min(100, 14 - (int(top >> 23) - 127));
-                by = __int_as_float((127 + e) << 23);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {    // (so small a factor makes all scores alike)
-                    f[i] = fmaxf(fmaxf(fabsf(a.scale), 1e-30f) * 1.4426950408889634f / __shfl_sync(0xffffffffu, by, (2 * c + i) * 4), 1e-35f);
-                    slack[i] = 6.f / f[i];
-                }
-                if (flip) by = -by;
-            }
+                    for (int j = 0; j < 4; ++j) qf[0][k][j] = bits2(__hmul2(bf2(qf[0][k][j]), bf2(bf16_power(tiny ? 100 : 0))));
+            const uint32_t up64 = RAW ? bf16_power(64 - (tiny ? e + 100 : e)) : 0, up60 = up64 - 0x02000200u;      // 2^-4 of it
 #pragma unroll
             for (int k = 0; k < G; ++k) {
                 uint32_t w[QP][4];
@@ -481,8 +488,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 for (int q = 0; q < QP; ++q)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[q][j] = qf[q][k][j];
-                if constexpr (RAW) query_words(w, flip);
-                else query_parts(w, by);
+                if constexpr (RAW) query_words(w, up64, up60, flip);
+                else query_parts(w, __int_as_float((127 + up) << 23 | (flip ? int(0x80000000u) : 0)));
 #pragma unroll
                 for (int q = 0; q < QP; ++q)
 #pragma unroll
@@ -580,7 +587,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
                 top[e] = v;
-                raise |= v > m[e] + slack[e % FS];         // (-infinity is not above -infinity)
+                raise |= v > m[e] + slack[e];         // (-infinity is not above -infinity)
             }
             // ---- the values' scales, and whether one is above its group's power of two (what has never been written may be anything) ----
             uint32_t vs[2][2][G / 2], widest[G / 2];
@@ -618,7 +625,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f[e % FS]);
+                    const float to = fmaxf(m[e], top[e]), by = to == -INFINITY ? 1.f : ex2((m[e] - to) * f[e]);
                     m[e] = to;
                     l[e] *= by;
 #pragma unroll
@@ -627,12 +634,12 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f[e % FS]) + S::up;
+                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f[e]) + S::up;
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float p = ex2(fmaf(s[b][2 * j + e], f[e % FS], base));
+                        const float p = ex2(fmaf(s[b][2 * j + e], f[e], base));
                         s[b][2 * j + e] = p;
                         l[e] += p;
                     }
@@ -737,7 +744,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                         for (int k = 0; k < G; ++k)
                             *reinterpret_cast<float4*>(part + col * HD + 32 * k + 4 * r) =
                                 make_float4(y[k][0][e], S::odd(y[k][0][2 + e], y[k][0][e]), y[k][1][e], S::odd(y[k][1][2 + e], y[k][1][e]));
-                        if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f[e % FS]; part[COLS * HD + COLS + col] = l[e]; }
+                        if (r == 0) { part[COLS * HD + col] = m[e] == -INFINITY ? -INFINITY : m[e] * f[e]; part[COLS * HD + COLS + col] = l[e]; }
                     }
                     if (lane == 0) meta[2 * warp + !ends] = PartMeta{lo + i - t, use.ct, use.head, began, t + 1, use.nt, use.first, use.n};
                 }

@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         // to [2^9, 2^10); what is not a number stays as it is
         const int e = top == 0 || top >= 0x7f80u ? 0 : 9 - (int(top >> 7) - 127);
         const float up = top < 0x80u ? 0x1p100f : exp2f(float(min(e, 120))), sign = a.scale < 0.f ? -up : up;
-        f = fmaxf(fabsf(a.scale), 1e-30f) * 1.4426950408889634f / up;
+        f = fminf(fmaxf(fabsf(a.scale) * 1.4426950408889634f / up, kAtLeast), kAtMost);
 #pragma unroll 4
         for (int ch = 0; ch < LANES; ++ch) {
             const uint32_t at = to + pf_chunk(row_in, ch);

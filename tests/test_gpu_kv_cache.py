@@ -336,6 +336,24 @@ def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
     assert c.status.item() == 0
 
 
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("size,scale", [(1e-38, 1.0), (1e-30, 1e28), (1e30, 1e-31), (1e37, 0.0), (1.0, -0.3), (1e-3, 1e-35)])
+def test_queries_of_any_size(kv, hd, size, scale):
+    """fp32 queries from the smallest to the largest numbers, heads and elements of a head 2^20 apart."""
+    c = Case(kv, 26, [333, 40], [2, 1], 2, hd, 16, FP32, 1, fill=True)
+    q = c.randn(c.n_rows, 10, hd) * torch.logspace(-6, 0, 10, dtype=torch.float32, device="cuda")[None, :, None]
+    q[..., ::7] *= 1e-6
+    check_attend(c, 10, scale=scale, q=q * size)
+
+
+@pytest.mark.parametrize("rows", [2, 200, 300])
+@pytest.mark.parametrize("size,scale", [(1e-9, 1e8), (1e18, 1e-19), (1e15, 1e-31), (1e-30, 1e28), (1e36, 1e-37), (1e36, 0.0)])
+def test_bf16_queries_and_scales_of_any_size(kv, rows, size, scale):
+    c = Case(kv, 27, [333], [rows], 1, 128, 16, BF16, 1, fill=True)
+    q = (c.randn(c.n_rows, 16, 128).float() * size).bfloat16()
+    check_attend(c, 16, scale=scale, q=q)
+
+
 @pytest.mark.parametrize("n_seq,most", [(31, 90), (32, 400), (40, 90), (70, 200)])
 def test_prompts_of_many_sequences(kv, n_seq, most):
     """Items go by their tokens over up to 32 sequences and by sequence beyond: every row is somebody's, empty sequences and rows before
