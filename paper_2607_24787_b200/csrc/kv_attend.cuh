@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = top == 0 ? -126 : top == 255 ? 0 : int(top) - 127;
-            const int up = RAW ? -e : min(100, 14 - e);          // fp32 columns go to [2^14, 2^15)
+            const int up = RAW ? -e : min(126, 14 - e);          // fp32 columns go to [2^14, 2^15)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float down = __int_as_float((127 - __shfl_sync(0xffffffffu, up, (2 * c + i) * 4)) << 23);

@@ -337,7 +337,7 @@ def test_prompts(kv, lengths, rows, hq, hk, hd, page, pad, dtype):
 
 
 @pytest.mark.parametrize("hd", [64, 128, 256])
-@pytest.mark.parametrize("size,scale", [(1e-38, 1.0), (1e-30, 1e28), (1e30, 1e-31), (1e37, 0.0), (1.0, -0.3), (1e-3, 1e-35)])
+@pytest.mark.parametrize("size,scale", [(1e-38, 1.0), (1e-30, 1e28), (1e30, 1e-31), (1e37, 0.0), (1.0, -0.3), (1e-3, 1e-35), (1e-37, 1e36)])
 def test_queries_of_any_size(kv, hd, size, scale):
     """fp32 queries from the smallest to the largest numbers, heads and elements of a head 2^20 apart."""
     c = Case(kv, 26, [333, 40], [2, 1], 2, hd, 16, FP32, 1, fill=True)
