@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
                 top[e] = v;
-                raise |= v > m[e] + slack[e];         // (-infinity is not above -infinity)
+                raise |= v - m[e] > slack[e];         // (two of -infinity leave NaN, which is not above)
             }
             // ---- the values' scales, and whether one is above its group's power of two (what has never been written may be anything) ----
             uint32_t vs[2][2][G / 2], widest[G / 2];
@@ -634,12 +634,13 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float base = (m[e] == -INFINITY ? 0.f : m[e] * -f[e]) + S::up;
+                // (the difference first: of large scores times f the maximum's rounding alone is more than the range of fp16's exponents)
+                const float base = m[e] == -INFINITY ? 0.f : m[e];
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float p = ex2(fmaf(s[b][2 * j + e], f[e], base));
+                        const float p = ex2(fmaf(s[b][2 * j + e] - base, f[e], S::up));
                         s[b][2 * j + e] = p;
                         l[e] += p;
                     }

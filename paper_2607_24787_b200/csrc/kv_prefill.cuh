@@ -283,13 +283,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
         const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
         float m = -INFINITY, l = 0.f;
+        const float slack = 6.f / f;
         int e_now = 0;
         bool ok = true;
         for (int j = 0; j < own_tiles && ok; ++j) {
             if (!(ok = wait(sh.s_full[half], j & 1))) break;
             tc_fence_after();
             const int packed = *reinterpret_cast<volatile int*>(&sh.exps[j & 3]), e = int(short(packed & 0xffff));
-            const float ft = packed >> 16 & 1 ? f * 16.f : f;
+            const float units = packed >> 16 & 1 ? 16.f : 1.f;
             uint32_t there[4];
             bool whole = (j + 1) * kPfTile <= limit;
 #pragma unroll
@@ -322,9 +323,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 #pragma unroll
                 for (int i = 1; i < 32; ++i) tops[ch] = fmaxf(tops[ch], __uint_as_float(r[ch][i]));
             }
-            const float peak = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * ft;         // m is kept as a power of two's exponent
-            if (__any_sync(0xffffffffu, peak > m + 6.f || e != e_now)) {
-                const float to = fmaxf(m, peak), by = m == -INFINITY ? 0.f : ex2(m - to);
+            // m is in scores of whole keys
+            const float peak = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * units;
+            if (__any_sync(0xffffffffu, peak - m > slack || e != e_now)) {
+                const float to = fmaxf(m, peak), by = m == -INFINITY ? 0.f : ex2((m - to) * f);
                 m = to;
                 l *= by;
                 if (j > 0) {                     // (before that the sums hold nothing)
@@ -341,8 +343,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                 }
                 e_now = e;
             }
-            const float nb = 8.f - (m == -INFINITY ? 0.f : m);
-            const unsigned long long f2 = two_floats(ft, ft), nb2 = two_floats(nb, nb);
+            // the difference from the maximum first: of large scores times f the rounding alone is more than the range of fp16's exponents
+            const float base = m == -INFINITY ? 0.f : -m;
+            const unsigned long long units2 = two_floats(units, units), base2 = two_floats(base, base), f2 = two_floats(f, f), eight2 = two_floats(8.f, 8.f);
             unsigned long long sum0 = 0, sum1 = 0;
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) {
@@ -350,7 +353,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) {
                     float x0, x1;
-                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, nb2), x0, x1);
+                    floats_of(fma2(fma2(two_words(r[ch][i], r[ch][i + 1]), units2, base2), f2, eight2), x0, x1);
                     const float p0 = ex2(x0), p1 = ex2(x1);
                     unsigned long long& sum = i & 2 ? sum1 : sum0;
                     sum = add2(sum, two_floats(p0, p1));

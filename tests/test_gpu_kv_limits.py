@@ -1,0 +1,59 @@
+"""Attention over the 4-bit cache at the ends of what a call may hold: scores far beyond any model's, queries that are not numbers."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ref_cache as R
+from test_gpu_kv_cache import BF16, FP32, HALF, Case, kv  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def set_keys_and_values(c, key_codes, seed=0):
+    """Every key becomes (code - 8) in element 0 and 0 elsewhere, `key_codes` [n_seq][tokens]; values get random codes and scales."""
+    g = torch.Generator().manual_seed(seed)
+    hd = c.hd
+    pages = torch.randint(0, 256, c.start.shape, generator=g, dtype=torch.uint8)
+    pages[..., 17 * hd:] = (torch.rand(*pages.shape[:3], hd // 2, generator=g) + 0.5).half().view(torch.uint8)
+    pages[..., 16 * hd:17 * hd] = torch.ones(*pages.shape[:3], hd // 2).half().view(torch.uint8)
+    pages[..., :8 * hd] = 0x88
+    for s, codes in enumerate(key_codes):
+        for t, code in enumerate(codes):
+            page = int(c.table[s, t // c.page])
+            pages[page, :, t % c.page // 16, t % 16 * 16] = 0x80 | int(code)
+    c.start = pages.numpy().copy()
+    c.cache.pages.copy_(pages)
+
+
+# The best token's score is above every other one by at least the query's size times the scale, 2^18 and more: its probability is 1, all others
+# are 0, and the result is its value. That value is a code less 8 times an fp16 scale, which fp32 holds exactly; the sum of probabilities is one
+# power of two. What is left are the roundings of the quotient and the last product (fp32, two each, and the fast division's two), of the
+# value to fp16 where many bf16 rows meet, and of the result.
+@pytest.mark.parametrize("power", [19, 24, 27, 28, 30, 33, 40, 55, 90])
+@pytest.mark.parametrize("dtype,hd,lengths,rows,heads", [
+    (BF16, 128, [900, 40], [1, 1], 32), (FP32, 128, [900, 40], [1, 1], 32), (FP32, 256, [6000], [2], 8), (BF16, 64, [6000, 77], [3, 5], 16),
+    (BF16, 128, [600, 300], [300, 300], 16), (BF16, 64, [300, 1100], [130, 260], 16), (FP32, 64, [333], [50], 4),
+])
+def test_scores_of_any_size(kv, dtype, hd, lengths, rows, heads, power):  # noqa: F811
+    c = Case(kv, 41, lengths, rows, 1, hd, 32, dtype, 1, fill=True)
+    g = torch.Generator().manual_seed(power)
+    tops, codes = [], []
+    for n in lengths:                          # eight tokens, each above the ones before it
+        at = sorted([0] + (torch.randperm(n - 1, generator=g)[:7] + 1).tolist())
+        row = np.zeros(n, int)
+        row[at] = np.arange(8) + 8
+        tops.append(at)
+        codes.append(row)
+    set_keys_and_values(c, codes)
+    q = torch.zeros(c.n_rows, heads, hd, dtype=dtype)
+    q[..., 0] = torch.ldexp(1 + torch.randint(0, 128, (c.n_rows, heads), generator=g) / 128, torch.tensor(power)).to(dtype)
+    where = R.places(c.lengths, c.row_start, c.n_rows)
+    tol = HALF[dtype] * (1 + 2.0 ** -8) + 8 * HALF[FP32] + (2.0 ** -11 if dtype is BF16 and max(rows) > 64 else 0)
+    for scale in (0.7, -0.3):
+        out = c.cache.attend(c.batch, (q if scale > 0 else -q).cuda(), scale).double().cpu().numpy()
+        for i, at in enumerate(where):
+            if at is None:
+                continue
+            best = max(t for t in tops[at[0]] if t <= at[1])
+            want = R.get(c.start, int(c.table[at[0], best // c.page]), 0, best % c.page, 1)
+            assert (np.abs(out[i] - want) <= tol * np.abs(want)).all(), (scale, i, at, best)
