@@ -886,12 +886,12 @@ __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const At
         float to = top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) to = fmaxf(to, m[i]);
-        if (to == -INFINITY) continue;
-        const float keep = ex2(top - to);
+        // (parts of no token have no weight; a part whose scores are NaN has a maximum of -infinity too, and its sums make the rest NaN)
+        const float keep = top == to ? 1.f : ex2(top - to);
         sum *= keep; o *= keep; top = to;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float by = ex2(m[i] - to);
+            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - to);
             sum += by * l[i]; o += by * y[i];
         }
     }
@@ -904,14 +904,13 @@ __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const At
 #pragma unroll
         for (int i = 1; i < SETS; ++i) to = fmaxf(to, tops[i]);
         o = sum = 0.f;
-        if (to > -INFINITY)
 #pragma unroll
-            for (int i = 0; i < SETS; ++i) {
-                const float by = ex2(tops[i] - to);
-                sum += by * sums[i]; o += by * rows[i][d];
-            }
+        for (int i = 0; i < SETS; ++i) {
+            const float by = tops[i] == -INFINITY ? 0.f : ex2(tops[i] - to);
+            sum += by * sums[i]; o += by * rows[i][d];
+        }
     }
-    o = sum > 0.f ? o * (S::unscale / sum) : 0.f;
+    o = sum == 0.f ? 0.f : o * (S::unscale / sum);
     T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.z * a.group + g) * a.out.head + d;
     if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(o);
     else *to = o;

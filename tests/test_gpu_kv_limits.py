@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import ref_cache as R
-from test_gpu_kv_cache import BF16, FP32, HALF, Case, kv  # noqa: F401
+from test_gpu_kv_cache import BF16, FP32, HALF, Case, attend_tolerance, kv  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,33 @@ def test_scores_of_any_size(kv, dtype, hd, lengths, rows, heads, power):  # noqa
             best = max(t for t in tops[at[0]] if t <= at[1])
             want = R.get(c.start, int(c.table[at[0], best // c.page]), 0, best % c.page, 1)
             assert (np.abs(out[i] - want) <= tol * np.abs(want)).all(), (scale, i, at, best)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype,hd,lengths,rows,heads", [
+    (BF16, 128, [20], [1], 8), (FP32, 64, [1], [1], 2),                       # one tile, one token
+    (BF16, 128, [100], [1], 8), (FP32, 128, [100, 30], [1, 1], 8),            # cut between warps
+    (BF16, 128, [5000], [1], 8), (FP32, 128, [5000], [1], 3), (FP32, 256, [3000], [2], 4), (BF16, 256, [3000, 9], [1, 1], 4),   # and CTAs
+])
+def test_queries_that_are_not_finite(kv, dtype, hd, lengths, rows, heads, bad):  # noqa: F811
+    """A head whose query holds a NaN or an infinity gives NaN, however its tokens are shared out; the other heads give what they give."""
+    c = Case(kv, 42, lengths, rows, 1, hd, 16, dtype, 1, fill=True)
+    q = c.randn(c.n_rows, heads, hd)
+    clean, spread, reach, span = R.attend(q.double().cpu().numpy(), c.start, c.table.numpy(), c.lengths, c.row_start, hd ** -0.5)
+    n = c.row_start[-1]
+    hit = np.zeros((n, heads), bool)
+    for i, h in {(0, 0), (n - 1, heads - 1), (n // 2, heads // 2)}:
+        q[i, h, (5 * i + h) % hd] = bad
+        hit[i, h] = True
+    got = c.cache.attend(c.batch, q).double().cpu().numpy()[:n]
+    assert np.isnan(got[hit]).all()
+    tol = attend_tolerance(clean, spread, reach, span, dtype, max(lengths))[:n]
+    assert (np.abs(got - clean[:n]) <= tol)[~hit].all()
+
+
+def test_a_query_that_is_not_finite_and_sees_nothing(kv):  # noqa: F811
+    for dtype, rows, heads in ((BF16, [3], 4), (FP32, [3], 4)):
+        c = Case(kv, 43, [2], rows, 1, 128, 16, dtype, fill=True)
+        q = torch.full((c.n_rows, heads, 128), float("nan"), dtype=dtype, device="cuda")
+        out = c.cache.attend(c.batch, q)
+        assert (out[:-2] == 0).all() and out[-2:].isnan().all()
