@@ -848,7 +848,8 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
             for (int k = 0; k < RUNS; ++k)
 #pragma unroll
                 for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(to + col * HD + k * 128 + lane * N + e) = make_float2(o[k][e], o[k][e + 1]);
-            if (lane == 0) { to[COLS * HD + col] = top; to[COLS * HD + COLS + col] = total; }
+            // (a part whose scores are NaN is not to be taken for one that sees nothing: its maximum is above all, and the item becomes NaN)
+            if (lane == 0) { to[COLS * HD + col] = total == total ? top : INFINITY; to[COLS * HD + COLS + col] = total; }
         }
     }
 }
@@ -886,12 +887,12 @@ __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const At
         float to = top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) to = fmaxf(to, m[i]);
-        // (parts of no token have no weight; a part whose scores are NaN has a maximum of -infinity too, and its sums make the rest NaN)
-        const float keep = top == to ? 1.f : ex2(top - to);
+        if (to == -INFINITY) continue;
+        const float keep = ex2(top - to);
         sum *= keep; o *= keep; top = to;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - to);
+            const float by = ex2(m[i] - to);
             sum += by * l[i]; o += by * y[i];
         }
     }
@@ -904,11 +905,12 @@ __global__ void __launch_bounds__(kAtJoinThreads) kv_attend_join_kernel(const At
 #pragma unroll
         for (int i = 1; i < SETS; ++i) to = fmaxf(to, tops[i]);
         o = sum = 0.f;
+        if (to > -INFINITY)
 #pragma unroll
-        for (int i = 0; i < SETS; ++i) {
-            const float by = tops[i] == -INFINITY ? 0.f : ex2(tops[i] - to);
-            sum += by * sums[i]; o += by * rows[i][d];
-        }
+            for (int i = 0; i < SETS; ++i) {
+                const float by = ex2(tops[i] - to);
+                sum += by * sums[i]; o += by * rows[i][d];
+            }
     }
     o = sum == 0.f ? 0.f : o * (S::unscale / sum);
     T* to = static_cast<T*>(a.out.p) + row * a.out.row + (join.z * a.group + g) * a.out.head + d;
