@@ -252,9 +252,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, w[j] >> 16 & 0x7fffu));
         }
-        // to [2^9, 2^10); what is not a number stays as it is
+        // to [2^9, 2^10). A row with a NaN or an infinity becomes NaN as a whole: infinite scores could all be -infinity, as those of tokens
+        // that it does not see are
         const int e = top == 0 || top >= 0x7f80u ? 0 : 9 - (int(top >> 7) - 127);
-        const float up = top < 0x80u ? 0x1p100f : exp2f(float(min(e, 120))), sign = a.scale < 0.f ? -up : up;
+        const float up = top < 0x80u ? 0x1p100f : exp2f(float(min(e, 120))), sign = top >= 0x7f80u ? __int_as_float(0x7fffffff) : a.scale < 0.f ? -up : up;
         f = fminf(fmaxf(fabsf(a.scale) * 1.4426950408889634f / up, kAtLeast), kAtMost);
 #pragma unroll 4
         for (int ch = 0; ch < LANES; ++ch) {
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         tc_fence_after();
         if (ok) {
             // values stand at 2^-E, probabilities and their sum at 2^8. The rows go out by way of the half's queries' place, HD / 8 lanes a row
-            const float by = l > 0.f ? exp2f(float(e_now)) / l : 0.f;
+            const float by = l == 0.f ? 0.f : exp2f(float(e_now)) / l;
             const uint32_t rows_at = q_at + half * S::op_bytes + (row_in & ~31) * (HD * 2);
 #pragma unroll 1
             for (int ch = 0; ch < HD / 32; ++ch) {

@@ -64,6 +64,7 @@ def test_scores_of_any_size(kv, dtype, hd, lengths, rows, heads, power):  # noqa
     (BF16, 128, [20], [1], 8), (FP32, 64, [1], [1], 2),                       # one tile, one token
     (BF16, 128, [100], [1], 8), (FP32, 128, [100, 30], [1, 1], 8),            # cut between warps
     (BF16, 128, [5000], [1], 8), (FP32, 128, [5000], [1], 3), (FP32, 256, [3000], [2], 4), (BF16, 256, [3000, 9], [1, 1], 4),   # and CTAs
+    (BF16, 128, [300, 200], [300, 200], 16), (BF16, 64, [385, 1], [280, 1], 16),                                                 # prompts
 ])
 def test_queries_that_are_not_finite(kv, dtype, hd, lengths, rows, heads, bad):  # noqa: F811
     """A head whose query holds a NaN or an infinity gives NaN, however its tokens are shared out; the other heads give what they give."""
@@ -82,7 +83,7 @@ def test_queries_that_are_not_finite(kv, dtype, hd, lengths, rows, heads, bad): 
 
 
 def test_a_query_that_is_not_finite_and_sees_nothing(kv):  # noqa: F811
-    for dtype, rows, heads in ((BF16, [3], 4), (FP32, [3], 4)):
+    for dtype, rows, heads in ((BF16, [3], 4), (FP32, [3], 4), (BF16, [280], 16)):
         c = Case(kv, 43, [2], rows, 1, 128, 16, dtype, fill=True)
         q = torch.full((c.n_rows, heads, 128), float("nan"), dtype=dtype, device="cuda")
         out = c.cache.attend(c.batch, q)
