@@ -152,19 +152,22 @@ class OffloadedMoE:
             self._attention = None
             return
         dtype = torch.float32 if self.cfg.dtype == B.DTYPE_FP32 else torch.bfloat16
+        if len(caches) != self.L or any(c.device != self.device for c in caches):
+            raise ValueError(f"caches: {self.L}, one a layer, on {self.device}")
+        if w_o.dim() != 3 or page_table.dim() != 2:
+            raise ValueError("page_table: [n_seq, pages]" if w_o.dim() == 3 else "w_o: [L, D, q_heads * head_dim]")
         hd, n_q = caches[0].head_dim, w_o.shape[2] // caches[0].head_dim
         n = (n_q + 2 * caches[0].kv_heads) * hd
-        if len(caches) != self.L:
-            raise ValueError(f"{self.L} caches, one a layer")
         for name, x, shape, dt in (("w_qkv", w_qkv, (self.L, n, self.D), dtype), ("w_o", w_o, (self.L, self.D, n_q * hd), dtype),
                                    ("rms_gamma", rms_gamma, (self.L, self.D), torch.float32),
-                                   ("lengths", lengths, (page_table.shape[0],), torch.int32), ("page_table", page_table, tuple(page_table.shape), torch.int32)):
+                                   ("page_table", page_table, tuple(page_table.shape), torch.int32), ("lengths", lengths, (page_table.shape[0],), torch.int32)):
             if tuple(x.shape) != shape or x.dtype is not dt or x.device != self.device or not x.is_contiguous():
                 raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {self.device}")
-        if any(g not in (None, self.L * hd) for g in rope.gamma_sizes):
-            raise ValueError("the rope's gammas: [L * head_dim]")
-        if positions.dim() != 2 or positions.shape[1] != page_table.shape[0] or positions.dtype is not torch.int32 or not positions.is_contiguous():
-            raise ValueError("positions: a contiguous int32 tensor [axes, n_seq]")
+        if rope.device != self.device or any(g not in (None, self.L * hd) for g in rope.gamma_sizes):
+            raise ValueError(f"rope: on {self.device}, with gammas [L * head_dim]")
+        if (positions.dim() != 2 or not 1 <= positions.shape[0] <= 4 or positions.shape[1] != page_table.shape[0] or positions.dtype is not torch.int32
+                or positions.device != self.device or not positions.is_contiguous()):
+            raise ValueError(f"positions: a contiguous int32 tensor [1..4 axes, n_seq] on {self.device}")
         shapes = (B.KvCache * self.L)(*[c.c for c in caches])
         batch = B.KvBatch(page_table.data_ptr(), lengths.data_ptr(), None, page_table.shape[0], page_table.shape[1], page_table.shape[0], 1)
         a = B.Attention(shapes, batch, rope.for_axes(positions.shape[0]), positions.data_ptr(), positions.shape[1], rms_gamma.data_ptr(),

@@ -1,0 +1,51 @@
+"""Tensors that OffloadedMoE.set_attention refuses before it takes an address of any (no context and no GPU are needed for that)."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+L, D, HD, HK, HQ, N = 2, 512, 64, 2, 4, 3
+
+
+@pytest.fixture(scope="module")
+def model():
+    from paper_2607_24787_b200 import binding as B
+    from paper_2607_24787_b200.build import build
+    from paper_2607_24787_b200.model import OffloadedMoE
+    build()
+    here = torch.device("meta")                # of the context: a device that nothing reads from
+    ctx = SimpleNamespace(cfg=B.make_cfg(L, D, 8, 128, 2, 0, 4, B.DTYPE_BF16, max_batch=N), L=L, D=D, device=here, ctx=None)
+
+    def call(**kw):
+        on = lambda dt, *shape: torch.empty(*shape, dtype=dt, device=here)  # noqa: E731
+        cache = SimpleNamespace(head_dim=HD, kv_heads=HK, device=here, c=B.KvCache(1 << 20, None, 4, 16, HK, HD))
+        rope = SimpleNamespace(device=here, gamma_sizes=(None, None), for_axes=lambda n: B.Rope(1 << 20, None, None, None, n, HD, 0, 1e-6))
+        d = dict(caches=[cache] * L, page_table=on(torch.int32, N, 4), lengths=on(torch.int32, N), rope=rope, positions=on(torch.int32, 3, N),
+                 rms_gamma=on(torch.float32, L, D), w_qkv=on(torch.bfloat16, L, (HQ + 2 * HK) * HD, D), w_o=on(torch.bfloat16, L, D, HQ * HD))
+        d.update({k: v(d[k]) for k, v in kw.items()})
+        OffloadedMoE.set_attention(ctx, **d)
+    return call
+
+
+def elsewhere(x):
+    return SimpleNamespace(**{**vars(x), "device": torch.device("cuda", 7)})
+
+
+@pytest.mark.parametrize("name,change", [
+    ("positions", lambda x: torch.zeros(3, N, dtype=torch.int32)),             # in host memory
+    ("positions", lambda x: torch.empty(5, N, dtype=torch.int32, device="meta")),
+    ("page_table", lambda x: torch.zeros(N, 4, dtype=torch.int32)),
+    ("page_table", lambda x: x[0]),
+    ("lengths", lambda x: torch.zeros(N, dtype=torch.int32)),
+    ("rms_gamma", lambda x: torch.zeros(L, D)),
+    ("w_qkv", lambda x: torch.zeros(x.shape, dtype=x.dtype)),
+    ("w_o", lambda x: torch.zeros(x.shape, dtype=x.dtype)),
+    ("w_o", lambda x: x[0]),
+    ("rope", elsewhere),
+    ("caches", lambda x: [x[0], elsewhere(x[1])]),
+    ("caches", lambda x: x[:1]),
+    ("caches", lambda x: []),
+])
+def test_tensors_that_are_refused(model, name, change):
+    with pytest.raises(ValueError, match=name.rstrip("s")):
+        model(**{name: change})
