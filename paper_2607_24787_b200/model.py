@@ -180,6 +180,9 @@ class OffloadedMoE:
         self._attention = (caches, page_table, lengths, rope, positions, rms_gamma, w_qkv, w_o, work)
 
     def attention_block(self, layer, h_inout):
+        if (h_inout.dim() != 2 or h_inout.shape[1] != self.D or h_inout.dtype is not torch.float32 or h_inout.device != self.device
+                or not h_inout.is_contiguous()):
+            raise ValueError(f"h_inout: a contiguous fp32 tensor [rows, {self.D}] on {self.device}")
         B.spm_attention_block(self.ctx, layer, h_inout, h_inout.shape[0])
 
     # ---- control / accounting --------------------------------------------

@@ -49,3 +49,11 @@ def elsewhere(x):
 def test_tensors_that_are_refused(model, name, change):
     with pytest.raises(ValueError, match=name.rstrip("s")):
         model(**{name: change})
+
+
+@pytest.mark.parametrize("h", [torch.zeros(N, D), torch.empty(N, D, dtype=torch.bfloat16, device="meta"), torch.empty(N, D - 32, device="meta"),
+                               torch.empty(D, device="meta"), torch.empty(N, 2 * D, device="meta")[:, ::2], torch.empty(N, 2 * D, device="meta")[:, :D]])
+def test_rows_that_a_block_refuses(h):
+    from paper_2607_24787_b200.model import OffloadedMoE
+    with pytest.raises(ValueError, match="h_inout"):
+        OffloadedMoE.attention_block(SimpleNamespace(D=D, device=torch.device("meta"), ctx=None), 0, h)
