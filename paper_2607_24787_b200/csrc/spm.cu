@@ -1639,6 +1639,14 @@ int check_layer(spm_ctx* c, int layer, int nb) {
     return SPM_OK;
 }
 
+// Of a whole step: before it has changed anything
+int check_step(spm_ctx* c, int nb) {
+    if (int rc = check_layer(c, 0, nb)) return rc;
+    if (c->attention.on && nb > c->attention.a.batch.n_seq)
+        return fail(c, SPM_ERR_INVALID_ARG, "nb %d: the attention block has %d sequences", nb, c->attention.a.batch.n_seq);
+    return SPM_OK;
+}
+
 int check_status(spm_ctx* c) {
     int st = 0;
     CU(c, cudaMemcpy(&st, c->ws_status, sizeof st, cudaMemcpyDeviceToHost));
@@ -1932,7 +1940,7 @@ int spm_moe_ffn(spm_ctx* c, int layer, const float* x_norm, const int32_t* ids, 
 }
 
 int spm_decode_step(spm_ctx* c, const float* h_in, int nb, float* h_out) {
-    if (int rc = check_layer(c, 0, nb)) return rc;
+    if (int rc = check_step(c, nb)) return rc;
     if (!h_in || !h_out) return fail(c, SPM_ERR_INVALID_ARG, "null argument");
     if (!aligned16(h_out)) return fail(c, SPM_ERR_INVALID_ARG, "h_out must be 16-byte aligned");
     const spm_model_cfg& m = c->cfg;
@@ -1954,7 +1962,7 @@ int spm_decode_step(spm_ctx* c, const float* h_in, int nb, float* h_out) {
 }
 
 int spm_decode_step_host(spm_ctx* c, const float* h_in_host, int nb, float* h_out_host) {
-    if (int rc = check_layer(c, 0, nb)) return rc;
+    if (int rc = check_step(c, nb)) return rc;
     if (!h_in_host || !h_out_host) return fail(c, SPM_ERR_INVALID_ARG, "null argument");
     const size_t bytes = size_t(nb) * c->cfg.hidden * 4;
     CU(c, cudaMemcpyAsync(c->ws_h, h_in_host, bytes, cudaMemcpyHostToDevice, c->compute));

@@ -1,0 +1,48 @@
+"""Decode steps with the attention block: what a refused step leaves as it was."""
+import pytest
+import torch
+
+from test_gpu_attention_block import Block, build, config
+
+pytestmark = pytest.mark.gpu
+
+
+def resident(m, cfg):
+    for l in range(cfg.n_layers):
+        assert m.prefetch_async(l, list(range(cfg.n_experts))) == cfg.n_experts
+    m.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["offloaded", "resident"])
+def test_a_refused_step_changes_nothing(kind):
+    """Four rows for three sequences, before and after steps that are taken: outputs, caches and bookkeeping are as without that call."""
+    from paper_2607_24787_b200.binding import SpmError
+    runs = []
+    for refuse in (False, True):
+        cfg = config("bf16", 4, slots=8 if kind == "resident" else 4)
+        m = build(cfg)
+        if kind == "resident":
+            resident(m, cfg)
+        block = Block(m, cfg, 3)
+        g, outs = torch.Generator().manual_seed(4), []
+        wide, host = torch.randn(4, cfg.hidden, generator=g), torch.full((4, cfg.hidden), 5.0).pin_memory()
+        wide_in, wide_out = wide.cuda(), torch.full((4, cfg.hidden), 7.0, device="cuda")
+        torch.cuda.synchronize()
+        for step in range(12):
+            h = torch.randn(3, cfg.hidden, generator=g).cuda()
+            block.step(g)
+            if refuse:
+                with pytest.raises(SpmError):
+                    m.decode_step(wide_in, wide_out)
+                with pytest.raises(SpmError):
+                    m.decode_step_host(wide.pin_memory(), host)
+                m.synchronize()
+                assert (wide_out == 7).all() and (host == 5).all()
+            outs.append(m.decode_step(h))
+            m.synchronize()
+        st = m.stats()
+        assert (st["host_free_steps"] == 12) == (kind == "resident")
+        runs.append((outs, [c.pages.clone() for c in block.caches], m.events(), st["kernel_launches"], st["steps"]))
+        m.close()
+    assert runs[0][2:] == runs[1][2:]
+    assert all(torch.equal(a, b) for i in range(2) for a, b in zip(runs[0][i], runs[1][i]))
