@@ -334,8 +334,10 @@ int spm_test_grouped_q4(spm_ctx* ctx, int choice, uint64_t launches[2]);
 
 /* Profile the overlap window (Section 3.3): window_us = median device time of the expert FFN of
  * one layer at max_batch tokens with every needed expert resident (kernel(s) + combine, the same
- * path a decode step takes), t_xfer_us = median time of one expert copy from the pinned store,
- * *budget_raw = floor(window / t_xfer). Uses and then empties the cache. */
+ * path a decode step takes), and, after spm_set_attention, of the attention block of one layer too, at as many rows as it has
+ * sequences and over the lengths and positions as they stand (the key/value caches are only read; a run inside spm_init knows of no
+ * block); t_xfer_us = median time of one expert copy from the pinned store,
+ * *budget_raw = floor(window / t_xfer). Uses and then empties the cache of experts. */
 int spm_profile_window(spm_ctx* ctx, double* window_us, double* t_xfer_us, int* budget_raw);
 /* What the most recent spm_profile_window on this context measured, including the run inside
  * spm_init(budget = -1), whose budget is max(1, *budget_raw) (Section 3.3: the budget follows the

@@ -79,9 +79,14 @@ int check_attention(const spm_model_cfg& m, const spm_attention* a, std::string*
     return SPM_OK;
 }
 
-int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int layer, float* h, int nb, cudaStream_t stream, std::string* why) {
+int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int layer, float* h, int nb, cudaStream_t stream, std::string* why,
+                      bool timed) {
     const spm_attention& a = block.a;
-    const spm_kv_cache& kv = block.caches[layer];
+    spm_kv_cache kv = block.caches[layer], into = kv;
+    if (timed) {
+        kv.status = into.status = nullptr;
+        into.n_pages = 0;                        // (a page number outside the pool: not written)
+    }
     if (nb > a.batch.n_seq) { *why = "attention: more rows than sequences"; return SPM_ERR_INVALID_ARG; }
     const bool fp32 = fp32_model(m);
     const size_t e = fp32 ? 4 : 2, D = m.hidden, NQ = q_width(a), N = qkv_width(a), hd = kv.head_dim;
@@ -104,7 +109,7 @@ int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int l
     if (rope.k_gamma) rope.k_gamma += layer * hd;
     const int64_t row = int64_t(N), head = int64_t(hd);
     const spm_rows q{qkv, row, head}, k{qkv + NQ, row, head}, v{qkv + NQ + hd * kv.n_kv_heads, row, head}, o{out, int64_t(NQ), head};
-    int rc = spm_kv_write(&kv, &b, &rope, a.positions, a.pos_stride, &q, &q, a.n_q_heads, &k, &v, SPM_DTYPE_FP32, stream);
+    int rc = spm_kv_write(&into, &b, &rope, a.positions, a.pos_stride, &q, &q, a.n_q_heads, &k, &v, SPM_DTYPE_FP32, stream);
     if (rc == SPM_OK) rc = spm_kv_attend(&kv, &b, &q, a.n_q_heads, &o, a.scale, SPM_DTYPE_FP32, attend, w.attend, stream);
     if (rc != SPM_OK) { *why = spm_last_error(nullptr); return rc; }
     ce = project(fp32, static_cast<const char*>(a.w_o) + layer * D * NQ * e, out, nullptr, 0.f, nb, int(NQ), int(D), rows, h, 1, stream);

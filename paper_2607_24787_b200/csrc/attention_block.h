@@ -21,6 +21,8 @@ constexpr int kAttentionLaunches = 7;
 size_t attention_bytes(const spm_model_cfg& m, const spm_attention& a);
 // SPM_OK or the status of what is wrong, with a message
 int check_attention(const spm_model_cfg& m, const spm_attention* a, std::string* why);
-int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int layer, float* h, int nb, cudaStream_t stream, std::string* why);
+// `timed`: for its time alone. The cache and its status word stay as they are (k and v are cut to codes that go nowhere).
+int enqueue_attention(const AttentionBlock& block, const spm_model_cfg& m, int layer, float* h, int nb, cudaStream_t stream, std::string* why,
+                      bool timed = false);
 
 }  // namespace spm

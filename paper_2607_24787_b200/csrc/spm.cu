@@ -2315,12 +2315,26 @@ int spm_profile_window(spm_ctx* c, double* window_us, double* t_xfer_us, int* bu
         CU(c, cudaEventElapsedTime(&ms, e0, e1));
         if (it >= 5) wt.push_back(ms * 1e3f);
     }
+    // and the attention block of one layer, over what the caches hold now
+    std::vector<float> at;
+    for (int it = 0; c->attention.on && it < 14; ++it) {
+        std::string why;
+        CU(c, cudaEventRecord(e0, c->compute));
+        if (int rc = enqueue_attention(c->attention, m, it % m.n_layers, c->ws_h, std::min(nb, c->attention.a.batch.n_seq), c->compute, &why, true))
+            return fail(c, rc, "%s", why.c_str());
+        CU(c, cudaEventRecord(e1, c->compute));
+        CU(c, cudaEventSynchronize(e1));
+        float ms = 0;
+        CU(c, cudaEventElapsedTime(&ms, e0, e1));
+        if (it >= 5) at.push_back(ms * 1e3f);
+    }
     cudaEventDestroy(e0);
     cudaEventDestroy(e1);
     std::sort(tx.begin(), tx.end());
     std::sort(wt.begin(), wt.end());
+    std::sort(at.begin(), at.end());
     *t_xfer_us = tx[tx.size() / 2];
-    *window_us = wt[wt.size() / 2] + c->stub_us;
+    *window_us = wt[wt.size() / 2] + c->stub_us + (at.empty() ? 0.f : at[at.size() / 2]);
     *budget_raw = int(*window_us / *t_xfer_us);
     c->prof_window_us = *window_us;
     c->prof_xfer_us = *t_xfer_us;

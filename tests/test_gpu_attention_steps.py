@@ -1,7 +1,8 @@
-"""Decode steps with the attention block: what a refused step leaves as it was."""
+"""Decode steps with the attention block: what a refused step leaves as it was, the block's part of the overlap window."""
 import pytest
 import torch
 
+from oracle import ref_math as M
 from test_gpu_attention_block import Block, build, config
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +47,38 @@ def test_a_refused_step_changes_nothing(kind):
         m.close()
     assert runs[0][2:] == runs[1][2:]
     assert all(torch.equal(a, b) for i in range(2) for a, b in zip(runs[0][i], runs[1][i]))
+
+
+@pytest.mark.parametrize("name,nb,n_seq", [("bf16", 1, 1), ("q4", 16, 16), ("tiny", 4, 3)])
+def test_the_window_holds_the_block(name, nb, n_seq):
+    """The profiled window of a model with the block is longer by it, and profiling leaves the caches as they are."""
+    cfg = config(name, nb)
+    m = build(cfg)
+    for _ in range(2):                         # (the first profile of a process has kernels to load)
+        without = m.profile_window()[0]
+    block = Block(m, cfg, n_seq, pages_each=600)
+    block.lengths.fill_(9000)
+    block.table[-1, 7] = -1                    # (a page outside the pool is nobody's error here)
+    torch.cuda.synchronize()
+    state = [c.pages.clone() for c in block.caches] + [block.lengths.clone(), block.table.clone(), block.positions.clone()]
+    torch.cuda.synchronize()
+    W, t, raw = m.profile_window()
+    assert raw == M.window_budget(W, t) and m.get_profile() == (W, t, raw)
+    h = torch.randn(n_seq, cfg.hidden).cuda()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    times = []
+    now = [c.pages.clone() for c in block.caches] + [block.lengths.clone(), block.table.clone(), block.positions.clone()]
+    assert all(torch.equal(a, b) for a, b in zip(state, now))
+    torch.cuda.synchronize()
+    for i in range(9):
+        with torch.cuda.stream(m.compute):
+            begin.record()
+            m.attention_block(i % cfg.n_layers, h)
+            end.record()
+        m.compute.synchronize()
+        times.append(begin.elapsed_time(end) * 1e3)
+    took = sorted(times)[4]
+    assert W > without + 0.5 * took, (W, without, took)
+    m.set_attention(None, None, None, None, None, None, None, None)
+    assert m.profile_window()[0] < W - 0.4 * took
+    m.close()
