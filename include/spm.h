@@ -535,7 +535,9 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
  * for the step's nb rows, row s being the new token of sequence s. The synthetic configurations omit it (spm_set_attention_stub_us stands
  * in for its time); a model that has it hands it over once: */
 typedef struct {
-    const spm_kv_cache* caches;     /* HOST [L]: a cache a layer, all of one shape; copied                                        */
+    const spm_kv_cache* caches;     /* HOST [L]: a cache a layer, all of one shape; copied. Without a status word it gets the context's:
+                                       what a step leaves there, the next spm_synchronize / spm_get_stats reports once, as SPM_ERR_TIMEOUT,
+                                       SPM_ERR_NUMERIC (not finite) or SPM_ERR_INVALID_ARG (pages, lengths)                        */
     spm_kv_batch batch;             /* page_table, lengths, n_seq (>= every nb), table_stride; the rest is not read. Before a step
                                        the caller counts its new token in `lengths`, ahead of the step on the compute stream or
                                        synchronised with it (device memory, read by the step's kernels)                           */

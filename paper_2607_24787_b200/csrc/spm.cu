@@ -365,7 +365,7 @@ Layout layout_of(const spm_model_cfg* m, int S, bool with_multi = true) {
         l.tc_ready = c.take(size_t(l.max_units + 1) * sizeof(int));
     }
     l.counters = c.take(256);
-    l.status = c.take(4);
+    l.status = c.take(8);          // of the step's kernels, of the attention block's
     l.total = c.off;
     return l;
 }
@@ -1648,15 +1648,19 @@ int check_step(spm_ctx* c, int nb) {
 }
 
 int check_status(spm_ctx* c) {
-    int st = 0;
-    CU(c, cudaMemcpy(&st, c->ws_status, sizeof st, cudaMemcpyDeviceToHost));
-    if (st == 0) return SPM_OK;
-    CU(c, cudaMemset(c->ws_status, 0, sizeof st));      // reported once; the context stays usable
+    int both[2] = {};
+    CU(c, cudaMemcpy(both, c->ws_status, sizeof both, cudaMemcpyDeviceToHost));
+    const int st = both[0], kv = both[1];
+    if (st == 0 && kv == 0) return SPM_OK;
+    CU(c, cudaMemset(c->ws_status, 0, sizeof both));      // reported once; the context stays usable
     if (st & kStatusCopyTimeout) return fail(c, SPM_ERR_TIMEOUT, "expert FFN kernel gave up waiting for a weight copy");
     if (st & kStatusBadSlot) return fail(c, SPM_ERR_NOT_RESIDENT, "expert FFN kernel received a slot number outside the pool");
     if (st & kStatusGroupedTimeout) return fail(c, SPM_ERR_TIMEOUT, "grouped expert FFN kernel gave up waiting on a pipeline barrier");
     if (st & kStatusStepTimeout) return fail(c, SPM_ERR_TIMEOUT, "a step's kernel gave up waiting for a weight copy or for another of its CTAs");
     if (st & kStatusNonFinite) return fail(c, SPM_ERR_NUMERIC, "a routing kernel met a non-finite logit (NaN or Inf in the hidden rows or the weights)");
+    if (kv & SPM_KV_TIMEOUT) return fail(c, SPM_ERR_TIMEOUT, "attention block: a copy inside a kernel did not land");
+    if (kv & SPM_KV_NONFINITE) return fail(c, SPM_ERR_NUMERIC, "attention block: a NaN or infinity went into a key/value cache");
+    if (kv) return fail(c, SPM_ERR_INVALID_ARG, "attention block: %s", kv & SPM_KV_TOO_LONG ? "a length beyond its row of the page table" : "a page number outside the pool");
     return SPM_OK;
 }
 
@@ -2104,6 +2108,8 @@ int spm_set_attention(spm_ctx* c, const spm_attention* a) {
             return fail(c, SPM_ERR_INVALID_ARG, "attention: workspace must be 16-byte aligned and hold %zu bytes", attention_bytes(c->cfg, *a));
         block.a = *a;
         block.caches.assign(a->caches, a->caches + c->cfg.n_layers);
+        for (auto& kv : block.caches)
+            if (!kv.status) kv.status = c->ws_status + 1;
         block.on = true;
     }
     CU(c, cudaStreamSynchronize(c->compute));

@@ -144,7 +144,8 @@ class OffloadedMoE:
     # ---- the attention block, for models that have it ----
     def set_attention(self, caches, page_table, lengths, rope, positions, rms_gamma, w_qkv, w_o, scale=None):
         """Steps run spm_attention before each router. caches: a kv_cache.KVCache a layer; page_table [n_seq, pages], lengths [n_seq] and
-        positions [axes, n_seq] int32 on the device, which the caller moves on before each step; rope: a kv_cache.Rope whose gammas are
+        positions [axes, n_seq] int32 on the device, which the caller moves on before each step (a row of no sequence has length 0; a bad page
+        or length is an error of the next synchronize(), unless the cache has a status word of its own); rope: a kv_cache.Rope whose gammas are
         [L * head_dim]; rms_gamma [L, D] fp32; w_qkv [L, (q_heads + 2 kv_heads) * head_dim, D], w_o [L, D, q_heads * head_dim]. caches
         None: no block any more."""
         if caches is None:

@@ -69,6 +69,7 @@ def test_the_window_holds_the_block(name, nb, n_seq):
     times = []
     now = [c.pages.clone() for c in block.caches] + [block.lengths.clone(), block.table.clone(), block.positions.clone()]
     assert all(torch.equal(a, b) for a, b in zip(state, now))
+    block.table[-1, 7] = 0
     torch.cuda.synchronize()
     for i in range(9):
         with torch.cuda.stream(m.compute):
@@ -81,4 +82,59 @@ def test_the_window_holds_the_block(name, nb, n_seq):
     assert W > without + 0.5 * took, (W, without, took)
     m.set_attention(None, None, None, None, None, None, None, None)
     assert m.profile_window()[0] < W - 0.4 * took
+    m.close()
+
+
+@pytest.mark.parametrize("kind", ["offloaded", "resident", "block"])
+@pytest.mark.parametrize("fault,code", [("page", -1), ("length", -1), ("finite", -7), (None, 0)])
+def test_what_goes_wrong_in_a_step_is_reported(kind, fault, code):
+    """Caches without a status word: the next synchronize says it, once, and the context goes on. With one, it is there."""
+    from paper_2607_24787_b200 import binding as B
+    bits = dict(page=B.KV_BAD_PAGE, length=B.KV_TOO_LONG, finite=B.KV_NONFINITE)
+    cfg = config("bf16", 3, slots=8 if kind == "resident" else 4)
+    m = build(cfg)
+    if kind == "resident":
+        resident(m, cfg)
+    block = Block(m, cfg, 3)
+    g = torch.Generator().manual_seed(6)
+    words = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in block.caches]
+
+    def one():
+        h = torch.randn(3, cfg.hidden, generator=g).cuda()
+        block.step(g)
+        if kind == "block":
+            m.attention_block(1, h)
+        else:
+            m.decode_step(h)
+
+    def broken(on):
+        if fault == "page":
+            block.table[1, 0] = 10 ** 6 if on else keep[1, 0]
+        elif fault == "length":
+            block.lengths[2] = 97 if on else 5
+        elif fault == "finite":                # of one value's row of weights: infinite values, finite hidden rows
+            block.w_qkv[1, -1] = 3e38 if on else 0.01
+        torch.cuda.synchronize()
+
+    keep = block.table.clone()
+    block.lengths.clamp_(max=5)
+    one()
+    m.synchronize()
+    for own in (False, True):
+        if own:
+            for c, w in zip(block.caches, words):
+                c.c.status = w.data_ptr()
+            m.set_attention(block.caches, block.table, block.lengths, block.rope, block.positions, block.gamma, block.w_qkv, block.w_o)
+        for _ in range(2):
+            broken(True)
+            one()
+            if fault and not own:
+                with pytest.raises(B.SpmError) as e:
+                    m.synchronize()
+                assert e.value.code == code and "attention" in str(e.value)
+            m.synchronize()
+            broken(False)
+            one()
+            m.synchronize()
+    assert words[1].item() == (bits[fault] if fault else 0)
     m.close()
