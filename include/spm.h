@@ -530,6 +530,11 @@ int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, i
 int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_q_heads, const spm_rows* out, float scale,
                   int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
+/* For tests of SPM_KV_TIMEOUT: from here on the kernels of spm_kv_attend (of this process, as it enqueues or captures them) wait for an arrival
+ * that nobody makes, withhold 0: no more; every wait gives up after limit_us (1000 at least; 0: the 2 s that hold otherwise). Such a kernel sets the status
+ * bit, waits for what it has under way, releases its tensor memory and returns; rows of its output are left as they were or void. */
+int spm_test_kv_waits(int withhold, int limit_us);
+
 /* The attention block of a decode step: before each layer's router,
  *     x = RMSNorm(h); (q, k, v) = W_qkv x; spm_kv_write (norm, rotation, k and v into the layer's cache); o = spm_kv_attend; h += W_o o
  * for the step's nb rows, row s being the new token of sequence s. The synthetic configurations omit it (spm_set_attention_stub_us stands

@@ -143,6 +143,7 @@ _SIG = {
     "spm_kv_attend_workspace": [C.POINTER(KvCache), C.POINTER(KvBatch), C.c_int, C.c_int, C.POINTER(C.c_size_t)],
     "spm_kv_attend": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rows), C.c_int, C.POINTER(Rows), C.c_float, C.c_int, _P,
                       C.c_size_t, _P],
+    "spm_test_kv_waits": [C.c_int, C.c_int],
     "spm_host_alloc": [C.c_size_t, C.POINTER(_P)],
     "spm_host_free": [_P],
     "spm_sim_create": [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(_P)],
@@ -508,6 +509,10 @@ def spm_kv_attend_workspace(kv, batch, n_q_heads, dtype) -> int:
 
 def spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
     _check(load().spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream))
+
+
+def spm_test_kv_waits(withhold, limit_us):
+    _check(load().spm_test_kv_waits(int(withhold), limit_us))
 
 
 def spm_attention_workspace(cfg: ModelCfg, attention: Attention) -> int:

@@ -46,6 +46,8 @@ struct AttendArgs {
     int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns,
                                 // head, first row, rows
     int once;                   // every block is read by one warp alone
+    unsigned long long wait_ns; // a wait in a kernel gives up after this long
+    int withhold;               // (tests) arrivals that barriers wait for and nobody makes
 };
 
 // Row of column x (eight sequences of five drafted rows, 8 heads a cache head: 26.1 us with the division alone, 24.9)
@@ -55,7 +57,6 @@ constexpr int kAtTile = 32;     // tokens
 constexpr int kAtMaxCtas = 148;
 constexpr int kAtMinTiles = 4;  // of a CTA, before another one starts: a tile a scheduler (16, one a warp: 1025 tokens 11.8 us, 9.7 with 4)
 constexpr int kAtFewBlocks = 8; // column blocks of a sequence that a lane counts by itself
-constexpr unsigned long long kAtWaitNs = 2'000'000'000ull;
 
 template <typename T, int HD>
 struct AtShape {
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
     __shared__ long long warp_sum_of[W];
 
     if (lane == 0) {
-        for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1);
+        for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1 + a.withhold);
         fence_barrier_init();
         meta[2 * warp].id = meta[2 * warp + 1].id = -1;
     }
@@ -525,9 +526,9 @@ __global__ void __launch_bounds__(AtShape<T, HD>::warps * 32, 1) kv_attend_kerne
         int stage = 0;
         uint32_t phase = 0;
         for (int i = 0; i < count; ++i) {
-            if (!mbar_wait_bounded(bars + 8 * stage, phase, kAtWaitNs)) {       // give up, but not with copies in flight
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + 8 * stage, phase, a.wait_ns))) {       // give up, but not with copies in flight
                 if (lane == 0) kv_note(a.kv, SPM_KV_TIMEOUT);
-                for (int j = i; j < issued; ++j) mbar_wait_bounded(bars + 8 * (j % STAGES), j / STAGES & 1, kAtWaitNs);
+                for (int j = i; j < issued; ++j) mbar_wait_bounded(bars + 8 * (j % STAGES), j / STAGES & 1, a.wait_ns);
                 break;
             }
             const uint32_t at = ring_at + stage * S::tile_bytes, have = present >> (2 * stage) & 3;

@@ -120,6 +120,9 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
     return launched(call, e);
 }
 
+std::atomic<unsigned long long> g_wait_ns{2'000'000'000ull};
+std::atomic<int> g_withhold{0};
+
 size_t attend_bytes(int hd) { return kAtMaxCtas * (32 + 2 * size_t(8) * (hd + 2) * 4); }
 
 constexpr int kMaxDevices = 64;
@@ -284,6 +287,8 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     // (a guess where max_rows is one: it only says what to keep in L2)
     a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8);
     a.scale = scale;
+    a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    a.withhold = g_withhold.load(std::memory_order_relaxed);
     a.joins = static_cast<int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
     if (prefill_pays(kv, batch, n_q_heads, dtype))
@@ -293,6 +298,14 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));
     });
     return launched(call, e);
+}
+
+int spm_test_kv_waits(int withhold, int limit_us) {
+    // (copies that a kernel gives up on have to land within the limit again before it ends)
+    if (limit_us != 0 && limit_us < 1000) return fail("spm_test_kv_waits", SPM_ERR_INVALID_ARG, "limit_us is less than a millisecond");
+    g_withhold.store(withhold != 0, std::memory_order_relaxed);
+    g_wait_ns.store(limit_us ? static_cast<unsigned long long>(limit_us) * 1000ull : 2'000'000'000ull, std::memory_order_relaxed);
+    return SPM_OK;
 }
 
 }  // extern "C"

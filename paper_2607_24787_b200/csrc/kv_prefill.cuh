@@ -96,7 +96,7 @@ __device__ __forceinline__ uint32_t pf_chunk(int row, int ch) {
 }
 
 struct PfShared {
-    unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+    unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], drained;
     uint32_t tmem;
     int quit;                                    // a wait has run out: everybody leaves
     int rb, seq, first, n, len;                  // the item: its columns, its sequence's rows and tokens
@@ -184,8 +184,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 128); mbar_init(smem_u32(&sh.v_full[i]), 128);
             mbar_init(smem_u32(&sh.k_empty[i]), 1); mbar_init(smem_u32(&sh.v_empty[i]), 1);
-            mbar_init(smem_u32(&sh.s_full[i]), 1); mbar_init(smem_u32(&sh.p_full[i]), 128); mbar_init(smem_u32(&sh.o_full[i]), 1);
+            mbar_init(smem_u32(&sh.s_full[i]), 1); mbar_init(smem_u32(&sh.p_full[i]), 128 + a.withhold); mbar_init(smem_u32(&sh.o_full[i]), 1);
         }
+        mbar_init(smem_u32(&sh.drained), 1);
         sh.quit = 0;
         fence_barrier_init();
     }
@@ -205,20 +206,21 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kPfTile - 1) / kPfTile : 0;
     const int tiles = max(tiles0, tiles1);
 
+    // a warp goes on, or gives up, as one: what follows is for all of its lanes together
     auto wait = [&](const unsigned long long& bar, int parity) {
         const uint32_t at = smem_u32(&bar);
-        if (mbar_try_wait(at, parity)) return true;
+        if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
         const unsigned long long t0 = global_timer_ns();
         for (;;) {
 #pragma unroll 1
             for (int i = 0; i < 32; ++i)
-                if (mbar_try_wait(at, parity)) return true;
-            if (*reinterpret_cast<volatile int*>(&sh.quit)) return false;
-            if (global_timer_ns() - t0 > kAtWaitNs) {
+                if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
+            const bool late = global_timer_ns() - t0 > a.wait_ns;
+            if (late) {
                 *reinterpret_cast<volatile int*>(&sh.quit) = 1;
                 kv_note(a.kv, SPM_KV_TIMEOUT);
-                return false;
             }
+            if (__any_sync(0xffffffffu, late || *reinterpret_cast<volatile int*>(&sh.quit))) return false;
         }
     };
 
@@ -530,7 +532,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     } else {
         fewer_registers<kPfIssueRegs>();
         together();
-        // ---- products ----
+        // ---- products. The warp walks as one, so that the elected lane is one lane throughout, and what it commits at the end covers all that it
+        // has issued (a lane by itself, which computes its descriptors: 260 us for 236) ----
         if (warp == 12) {
             constexpr uint32_t idesc_s = pf_idesc(kPfTile, false), idesc_o = pf_idesc(HD, true);
             auto scores = [&](int h, int st) {
@@ -588,8 +591,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                 signal(sh.v_empty[st]);
                 if (j + 1 < tiles) signal(sh.k_empty[next]);
             }
+            if (tiles > 0) {                         // products under way end before tensor memory is given back, whoever has given up
+                signal(sh.drained);
+                mbar_wait_bounded(smem_u32(&sh.drained), 0, 2'000'000'000ull);
+                __syncwarp();
+            }
         }
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (warp == 12) tmem_dealloc(tmem, 512);

@@ -57,3 +57,12 @@ def test_rows_that_a_block_refuses(h):
     from paper_2607_24787_b200.model import OffloadedMoE
     with pytest.raises(ValueError, match="h_inout"):
         OffloadedMoE.attention_block(SimpleNamespace(D=D, device=torch.device("meta"), ctx=None), 0, h)
+
+
+def test_limits_that_are_refused():
+    from paper_2607_24787_b200 import binding as B
+    from paper_2607_24787_b200.build import build
+    build()
+    for us in (-1, 1, 999):
+        with pytest.raises(B.SpmError):
+            B.spm_test_kv_waits(0, us)

@@ -138,3 +138,24 @@ def test_what_goes_wrong_in_a_step_is_reported(kind, fault, code):
             m.synchronize()
     assert words[1].item() == (bits[fault] if fault else 0)
     m.close()
+
+
+def test_a_step_whose_copies_do_not_land_is_reported():
+    from paper_2607_24787_b200 import binding as B
+    cfg = config("bf16", 3, slots=4)
+    m = build(cfg)
+    block = Block(m, cfg, 3)
+    g = torch.Generator().manual_seed(7)
+    h = torch.randn(3, cfg.hidden, generator=g).cuda()
+    block.step(g)
+    try:
+        B.spm_test_kv_waits(1, 1000)
+        m.decode_step(h)
+    finally:
+        B.spm_test_kv_waits(0, 0)
+    with pytest.raises(B.SpmError) as e:
+        m.synchronize()
+    assert e.value.code == -4
+    m.decode_step(h)
+    m.synchronize()
+    m.close()

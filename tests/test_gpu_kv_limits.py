@@ -88,3 +88,25 @@ def test_a_query_that_is_not_finite_and_sees_nothing(kv):  # noqa: F811
         q = torch.full((c.n_rows, heads, 128), float("nan"), dtype=dtype, device="cuda")
         out = c.cache.attend(c.batch, q)
         assert (out[:-2] == 0).all() and out[-2:].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,hd,lengths,rows,heads", [
+    (BF16, 128, [900, 40], [1, 1], 8), (FP32, 64, [900], [4], 4), (BF16, 256, [20], [1], 2), (BF16, 128, [5000] * 70, [1] * 70, 8),
+    (BF16, 128, [600, 300], [300, 300], 16), (BF16, 64, [385, 1], [280, 1], 16), (BF16, 64, [20], [300], 16),
+])
+def test_a_wait_that_runs_out(kv, dtype, hd, lengths, rows, heads):  # noqa: F811
+    """An arrival that nobody makes: the kernels give up after the limit and say so, and the next call is what it was."""
+    from paper_2607_24787_b200 import binding as B
+    c = Case(kv, 44, lengths, rows, 1, hd, 16, dtype, fill=True)
+    q = c.randn(c.n_rows, heads, hd)
+    want = c.cache.attend(c.batch, q)
+    assert c.status.item() == 0
+    try:
+        B.spm_test_kv_waits(1, 1000)
+        c.cache.attend(c.batch, q)
+        torch.cuda.synchronize()
+    finally:
+        B.spm_test_kv_waits(0, 0)
+    assert c.status.item() == B.KV_TIMEOUT
+    c.status.zero_()
+    assert torch.equal(c.cache.attend(c.batch, q), want) and c.status.item() == 0
