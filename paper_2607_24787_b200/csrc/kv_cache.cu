@@ -284,8 +284,8 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
         if (per_page == 1 << i) a.page_shift = i;
         if (a.group == 1 << i) a.group_shift = i;
     }
-    // (a guess where max_rows is one: it only says what to keep in L2)
-    a.once = !batch->row_start || (static_cast<long long>(batch->max_rows ? batch->max_rows : 1) * a.group <= 8);
+    // one block of columns a sequence (a guess where max_rows is one: it only says what to keep in L2)
+    a.once = (batch->row_start ? std::max(batch->max_rows, 1) : 1ll) * a.group <= 8;
     a.scale = scale;
     a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     a.withhold = g_withhold.load(std::memory_order_relaxed);
