@@ -2,6 +2,7 @@
 #include "attention_block.h"
 
 #include <algorithm>
+#include <cmath>
 
 #include "project.cuh"
 
@@ -75,6 +76,7 @@ int check_attention(const spm_model_cfg& m, const spm_attention* a, std::string*
         if (!c.pages || reinterpret_cast<uintptr_t>(c.pages) % 16 || reinterpret_cast<uintptr_t>(c.status) % 4)
             return no(SPM_ERR_INVALID_ARG, "attention: pages must be 16-byte aligned, status 4-byte aligned");
     }
+    if (!std::isfinite(a->scale)) return no(SPM_ERR_INVALID_ARG, "attention: scale is not finite");
     if (b.n_seq < 1) return no(SPM_ERR_INVALID_ARG, "attention: no sequences");
     return SPM_OK;
 }

@@ -1,6 +1,7 @@
 // The entry points of the attention block: checks of arguments, launches.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <string>
 #include <type_traits>
@@ -262,6 +263,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     if (int rc = check_cache(call, kv)) return rc;
     if (int rc = check_batch(call, kv, batch)) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
+    if (!std::isfinite(scale)) return fail(call, SPM_ERR_INVALID_ARG, "scale is not finite");
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     if (int rc = check_rows(call, "q", q, dtype)) return rc;
     if (int rc = check_rows(call, "out", out, dtype)) return rc;

@@ -66,3 +66,26 @@ def test_limits_that_are_refused():
     for us in (-1, 1, 999):
         with pytest.raises(B.SpmError):
             B.spm_test_kv_waits(0, us)
+
+
+KV_AT = 1 << 20             # an address that is never read
+
+
+def kv_structs(B, **kw):
+    d = dict(page_table=KV_AT, lengths=KV_AT, row_start=None, n_seq=1, table_stride=2, n_rows=1, max_rows=1)
+    d.update(kw)
+    return B.KvCache(KV_AT, None, 4, 32, 2, 128), B.KvBatch(**d), B.Rows(KV_AT, 1024, 128)
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 1e39])
+def test_scales_that_are_refused(scale):
+    from paper_2607_24787_b200 import binding as B
+    kv, batch, rows = kv_structs(B)
+    with pytest.raises(B.SpmError) as e:
+        B.spm_kv_attend(kv, batch, rows, 8, rows, scale, B.DTYPE_BF16, KV_AT, 1 << 40)
+    assert e.value.code == -1 and "scale" in str(e.value)
+    cfg = B.make_cfg(L, D, 8, 128, 2, 0, 4, B.DTYPE_BF16, max_batch=N)
+    block = B.Attention((B.KvCache * L)(kv, kv), batch, B.Rope(KV_AT, None, None, None, 1, 128, 0, 1e-6), KV_AT, N, KV_AT, KV_AT, KV_AT, 8, scale, None, 0)
+    with pytest.raises(B.SpmError) as e:
+        B.spm_attention_workspace(cfg, block)
+    assert e.value.code == -1 and "scale" in str(e.value)
