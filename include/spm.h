@@ -478,7 +478,7 @@ typedef struct {
     const int32_t* lengths;       /* dev [n_seq]                                                                */
     const int32_t* row_start;     /* dev [n_seq + 1], not falling; NULL: row s is the one new row of sequence s */
     int32_t n_seq;                /* 0 .. SPM_KV_MAX_SEQS                                                       */
-    int32_t table_stride;         /* page numbers a sequence                                                    */
+    int32_t table_stride;         /* page numbers a sequence; times page_size at most 2^31 - 4096               */
     int32_t n_rows;               /* rows of the row arrays                                                     */
     int32_t max_rows;             /* about how many new rows a sequence has at most (0: not known): a hint for what to keep
                                      in L2; results hold for any value                                          */

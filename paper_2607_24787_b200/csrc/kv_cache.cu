@@ -54,8 +54,9 @@ int check_batch(const char* call, const spm_kv_cache* kv, const spm_kv_batch* b)
     if (b->n_seq < 0 || b->n_seq > SPM_KV_MAX_SEQS)
         return fail(call, SPM_ERR_INVALID_ARG, "n_seq " + std::to_string(b->n_seq) + " outside 0.." + std::to_string(SPM_KV_MAX_SEQS));
     if (b->n_rows < 0 || b->max_rows < 0 || b->table_stride < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
-    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX)
-        return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 1 tokens");
+    // (a tile's tokens more than a sequence's are still a number)
+    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX - 4095ll)
+        return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 4096 tokens");
     if (b->n_seq > 0 && (!b->lengths || (!b->page_table && b->table_stride > 0)))
         return fail(call, SPM_ERR_INVALID_ARG, "page_table or lengths is null");
     if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_start, 4))

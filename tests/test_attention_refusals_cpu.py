@@ -89,3 +89,16 @@ def test_scales_that_are_refused(scale):
     with pytest.raises(B.SpmError) as e:
         B.spm_attention_workspace(cfg, block)
     assert e.value.code == -1 and "scale" in str(e.value)
+
+
+def test_tables_whose_tokens_kernels_could_not_count():
+    """Tiles of 128 tokens are counted in 32 bits: 2^31 - 4096 tokens a sequence are taken, more are not."""
+    from paper_2607_24787_b200 import binding as B
+    for stride, ok in ((2 ** 26 - 128, True), (2 ** 26 - 127, False), (2 ** 26 - 1, False)):
+        kv, batch, rows = kv_structs(B, table_stride=stride)
+        if ok:
+            assert B.spm_kv_attend_workspace(kv, batch, 8, B.DTYPE_BF16) > 0
+            continue
+        with pytest.raises(B.SpmError) as e:
+            B.spm_kv_attend_workspace(kv, batch, 8, B.DTYPE_BF16)
+        assert e.value.code == -1
