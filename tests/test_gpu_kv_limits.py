@@ -110,3 +110,31 @@ def test_a_wait_that_runs_out(kv, dtype, hd, lengths, rows, heads):  # noqa: F81
     assert c.status.item() == B.KV_TIMEOUT
     c.status.zero_()
     assert torch.equal(c.cache.attend(c.batch, q), want) and c.status.item() == 0
+
+
+# Ordinary inputs, in the 2-norm, where independent roundings add up as squares. A bf16 result's own rounding is half a step at most, and the root
+# mean square of a rounding is its step over sqrt(12): 2^-8 / sqrt(3) = 0.00226 of a number just above a power of two and half of that below the
+# next, 0.00166 for normal numbers. What else bf16 calls round, probabilities and their products with scales (or probabilities, keys and values of
+# prompts), has fp16's 11 bits: 2^-11 / sqrt(3) = 0.00028 each at most, three of them 0.0005. Together 0.0018; one more rounding to bf16 on the way,
+# of probabilities say, would be 0.0023 and more. fp32 calls: two operands of 23 bits each a product, a score of some units, sums: ten halves of a
+# step of 2^-24, 6e-7; three of 2^-22 would be over it.
+@pytest.mark.parametrize("dtype,hd,lengths,rows,heads,page", [
+    (BF16, 128, [700, 333], [1, 1], 16, 64), (BF16, 64, [500, 90], [5, 3], 8, 16), (BF16, 256, [400], [2], 4, 32),
+    (BF16, 128, [600, 300], [280, 250], 16, 64), (BF16, 64, [300, 900], [300, 100], 24, 32),
+    (FP32, 128, [700, 333], [1, 1], 16, 64), (FP32, 64, [500, 90], [5, 3], 4, 16), (FP32, 256, [400], [30], 4, 32),
+])
+def test_errors_of_ordinary_calls(kv, dtype, hd, lengths, rows, heads, page):  # noqa: F811
+    c = Case(kv, 45, lengths, rows, 2, hd, page, dtype, fill=True)
+    q = c.randn(c.n_rows, heads, hd)
+    rows64, want, group = q.double().cpu().numpy(), np.zeros((c.n_rows, heads, hd)), heads // 2
+    for s, n in enumerate(rows):
+        at = slice(c.row_start[s], c.row_start[s + 1])
+        hidden = np.arange(lengths[s])[None] > np.arange(lengths[s] - n, lengths[s])[:, None]
+        for h in range(heads):
+            if h % group == 0:
+                k, v = R.context(c.start, c.table.numpy(), s, lengths[s], page, h // group)[:2]
+            z = np.where(hidden, -np.inf, rows64[at, h] @ k.T * hd ** -0.5)
+            p = np.exp(z - z.max(-1, keepdims=True))
+            want[at, h] = p @ v / p.sum(-1, keepdims=True)
+    got = c.cache.attend(c.batch, q).double().cpu().numpy()
+    assert np.linalg.norm(got - want) <= (2.1e-3 if dtype is BF16 else 6e-7) * np.linalg.norm(want)
