@@ -45,6 +45,7 @@ struct AttendArgs {
     float* parts;               // [2 * CTAs][part floats]
     int* joins;                 // [CTAs][8], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), columns,
                                 // head, first row, rows
+    const int* rows;            // new rows of each sequence that this kernel takes; NULL: all of them
     int once;                   // every block is read by one warp alone
     unsigned long long wait_ns; // a wait in a kernel gives up after this long
     int withhold;               // (tests) arrivals that barriers wait for and nobody makes
@@ -90,7 +91,7 @@ struct Walk {
         first = seq; n = 1;
         if (a.batch.row_start) {
             first = a.batch.row_start[seq];
-            n = min(a.batch.row_start[seq + 1] - first, a.batch.n_rows);
+            n = a.rows ? a.rows[seq] : min(a.batch.row_start[seq + 1] - first, a.batch.n_rows);
         }
     }
     __device__ __forceinline__ int blocks(const AttendArgs& a) const { return n > 0 ? (n * a.group + COLS - 1) / COLS : 0; }

@@ -125,7 +125,9 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
 std::atomic<unsigned long long> g_wait_ns{2'000'000'000ull};
 std::atomic<int> g_withhold{0};
 
-size_t attend_bytes(int hd) { return kAtMaxCtas * (32 + 2 * size_t(8) * (hd + 2) * 4); }
+// joins, the rows that each of two kernels takes, parts
+constexpr size_t kAtJoinBytes = kAtMaxCtas * 32, kAtRowsBytes = 2 * SPM_KV_MAX_SEQS * sizeof(int);
+size_t attend_bytes(int hd) { return kAtJoinBytes + kAtRowsBytes + kAtMaxCtas * 2 * size_t(8) * (hd + 2) * 4; }
 
 constexpr int kMaxDevices = 64;
 // Once a kernel and device: shared memory beyond 48 KB
@@ -150,18 +152,28 @@ cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st
 
 // Which of the two kernels a call's rows are for. Per token of context the tensor-core kernel takes 19 ns a round of CTAs (an SM does 256
 // columns of a head, and an item's tokens are not shared out), the other 4.5 ps a column of a head on all SMs together, whatever the rows
-// are; lengths cancel. Measured with 4 heads of 128 over 4096 tokens, columns times heads (tensor cores / other, us): 3200: 80 / 64,
-// 4096: 79 / 79, 8192: 79 / 140, 37888: 87 / 594; in two rounds, 10240: 159 / 177.
+// are; lengths cancel where sequences are alike, and long ones of few rows are taken out (kv_split_kernel). Measured with 4 heads of 128 over
+// 4096 tokens, columns times heads (tensor cores / other, us): 3200: 80 / 64, 4096: 79 / 79, 8192: 79 / 140, 37888: 87 / 594; in two rounds,
+// 10240: 159 / 177.
+constexpr int kPfColumns = 4000;                 // a round
 bool prefill_pays(const spm_kv_cache* kv, const spm_kv_batch* b, int n_q_heads, int dtype) {
     if (dtype != SPM_DTYPE_BF16 || kv->head_dim > 128 || !b->row_start) return false;
     const long long columns = static_cast<long long>(b->n_rows) * (n_q_heads / kv->n_kv_heads), each = (columns + b->n_seq - 1) / b->n_seq;
     const long long items = (each + kPfCols - 1) / kPfCols * b->n_seq * kv->n_kv_heads;
-    return columns * kv->n_kv_heads > 4000 * ((items + kAtMaxCtas - 1) / kAtMaxCtas);
+    return columns * kv->n_kv_heads > kPfColumns * ((items + kAtMaxCtas - 1) / kAtMaxCtas);
 }
 template <int HD>
-cudaError_t launch_prefill(const AttendArgs& a, int dev, cudaStream_t st) {
-    const cudaError_t e = allow_smem<kv_prefill_kernel<HD>>(dev, PfShape<HD>::smem);
+cudaError_t launch_prefill(AttendArgs a, void* workspace, int dev, int sms, cudaStream_t st) {
+    cudaError_t e = allow_smem<kv_prefill_kernel<HD>>(dev, PfShape<HD>::smem);
     if (e != cudaSuccess) return e;
+    if (a.batch.n_seq > 1 && a.batch.stride * a.kv.page_size > kPfLongTokens) {       // there may be sequences that are not for it
+        int* rows = reinterpret_cast<int*>(static_cast<char*>(workspace) + kAtJoinBytes);
+        e = launch_early(kv_split_kernel, 1, SPM_KV_MAX_SEQS, 0, st, a, kPfColumns, rows, rows + SPM_KV_MAX_SEQS);
+        a.rows = rows;
+        if (e == cudaSuccess) e = launch_attend<__nv_bfloat16, HD>(a, dev, sms, st);
+        if (e != cudaSuccess) return e;
+        a.rows = rows + SPM_KV_MAX_SEQS;
+    }
     // as many CTAs as there can be items: full ones of all rows, and one a sequence that is not full
     const long long items = (static_cast<long long>(a.batch.n_rows) * a.group / kPfCols + a.batch.n_seq) * a.kv.heads;
     if (items > INT32_MAX) return cudaErrorInvalidValue;
@@ -293,9 +305,9 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     a.withhold = g_withhold.load(std::memory_order_relaxed);
     a.joins = static_cast<int*>(workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtMaxCtas * 32);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAtJoinBytes + kAtRowsBytes);
     if (prefill_pays(kv, batch, n_q_heads, dtype))
-        e = (kv->head_dim == 64 ? launch_prefill<64> : launch_prefill<128>)(a, dev, static_cast<cudaStream_t>(stream));
+        e = (kv->head_dim == 64 ? launch_prefill<64> : launch_prefill<128>)(a, workspace, dev, sms, static_cast<cudaStream_t>(stream));
     else by_type(dtype, kv->head_dim, [&](auto* t, auto size) {
         using T = std::remove_pointer_t<decltype(t)>;
         e = launch_attend<T, size.value>(a, dev, sms, static_cast<cudaStream_t>(stream));

@@ -138,3 +138,74 @@ def test_errors_of_ordinary_calls(kv, dtype, hd, lengths, rows, heads, page):  #
             want[at, h] = p @ v / p.sum(-1, keepdims=True)
     got = c.cache.attend(c.batch, q).double().cpu().numpy()
     assert np.linalg.norm(got - want) <= (2.1e-3 if dtype is BF16 else 6e-7) * np.linalg.norm(want)
+
+
+def want_of(c, q, heads, lengths, rows):
+    """Results of a whole batch in 64 bits (rows and heads of a sequence at a time)."""
+    rows64, want, group = q.double().cpu().numpy(), np.zeros((c.n_rows, heads, c.hd)), heads // c.hk
+    for s, n in enumerate(rows):
+        at = slice(c.row_start[s], c.row_start[s + 1])
+        for h in range(heads):
+            if h % group == 0:
+                k, v, there = R.context(c.start, c.table.numpy(), s, min(lengths[s], c.table.shape[1] * c.page), c.page, h // group)[:3]
+            hidden = (np.arange(len(k))[None] > np.arange(lengths[s] - n, lengths[s])[:, None]) | ~there
+            z = np.where(hidden, -np.inf, rows64[at, h] @ k.T * c.hd ** -0.5)
+            p = np.exp(z - np.maximum(z.max(-1, keepdims=True, initial=-np.inf), -1e30))
+            want[at, h] = p @ v / np.maximum(p.sum(-1, keepdims=True), 1e-30)
+    return want
+
+
+@pytest.mark.parametrize("hd,lengths,rows,heads,hk", [
+    (128, [300, 9000, 9, 8600, 0, 9500], [300, 1, 1, 3, 1, 0], 16, 1),       # a prompt beside decoded and drafted tokens of long contexts
+    (64, [9000, 260, 270, 40], [2, 260, 200, 1], 24, 2),
+    (128, [700] * 40, [10] * 40, 16, 1),                                     # none is longer than the others
+    (64, [30] * 99 + [8800], [5] * 99 + [5], 16, 1),
+])
+def test_batches_of_prompts_and_long_contexts(kv, hd, lengths, rows, heads, hk):  # noqa: F811
+    c = Case(kv, 46, lengths, rows, hk, hd, 16, BF16, 2, wide_table=600, fill=True)
+    q = c.randn(c.n_rows, heads, hd)
+    out = torch.full_like(q, 9.0)
+    c.cache.attend(c.batch, q, out=out)
+    n = c.row_start[-1]
+    want = want_of(c, q, heads, lengths, rows)[:n]
+    got = out.double().cpu().numpy()
+    assert (got[n:] == 9).all() and c.status.item() == 0
+    for i in range(n):                         # the norm of a row: twice what all of it may be off by (see above), a row being few numbers
+        assert np.linalg.norm(got[i] - want[i]) <= 4.2e-3 * np.linalg.norm(want[i]), i
+    assert torch.equal(c.cache.attend(c.batch, q)[:n], out[:n])
+
+
+def test_a_prompt_does_not_slow_long_contexts_down(kv):  # noqa: F811
+    """One prompt and seven sequences of 100 000 tokens, together and in two calls. One after another's tokens in one place would be 14 times."""
+    lengths, rows = [2048] + [100_000] * 7, [2048] + [1] * 7
+    need = [-(-n // 64) for n in lengths]
+    table = torch.full((8, max(need)), -1, dtype=torch.int32)
+    at = 0
+    for i, n in enumerate(need):
+        table[i, :n] = torch.arange(at, at + n)
+        at += n
+    pages = torch.randint(0, 256, (at, 4, 4, 18 * 128), dtype=torch.uint8, device="cuda")
+    pages[..., 16 * 128:] = torch.rand(at, 4, 4, 128, device="cuda").half().view(torch.uint8)
+    cache = kv.KVCache(pages)
+    q = torch.randn(sum(rows), 32, 128, device="cuda").bfloat16()
+
+    def batch(a, b):
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        starts = np.cumsum([0] + rows[a:b]).tolist()
+        return kv.KVBatch(table[a:b].cuda(), ints(lengths[a:b]), ints(starts), n_rows=starts[-1], max_rows=max(rows[a:b]))
+
+    def took(*calls):
+        best = 1e9
+        for _ in range(6):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            for b, x in calls:
+                cache.attend(b, x)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        return best
+
+    whole, prompt, rest = batch(0, 8), batch(0, 1), batch(1, 8)
+    together, apart = took((whole, q)), took((prompt, q[:2048]), (rest, q[2048:]))
+    assert together < 3 * apart, (together, apart)
