@@ -510,7 +510,7 @@ int spm_rotate_heads(const spm_rope* rope, const int32_t* positions, int64_t pos
                      int n_rows, int n_heads, int head_dim, int dtype, void* stream);
 
 /* The batch's new rows of k and v go into the cache (k normed with k_gamma and rotated first), and q_out = norm and rotation of q
- * (n_q_heads heads; q NULL: none). rope NULL: neither norm nor rotation, and q must be NULL. */
+ * (n_q_heads heads; q NULL: none; q_out may be q itself, with the same strides). rope NULL: neither norm nor rotation, and q must be NULL. */
 int spm_kv_write(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
                  const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* k, const spm_rows* v, int dtype, void* stream);
 

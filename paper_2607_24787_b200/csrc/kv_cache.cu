@@ -71,6 +71,7 @@ int check_rows(const char* call, const char* name, const spm_rows* r, int dtype)
         return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + ": rows of heads must start on 16-byte boundaries");
     return SPM_OK;
 }
+bool other_strides(const spm_rows* x, const spm_rows* y) { return x->row_stride != y->row_stride || x->head_stride != y->head_stride; }
 int check_rope(const char* call, const spm_rope* r, const int32_t* positions, int64_t pos_stride, int n_rows, int hd) {
     if (!r) return fail(call, SPM_ERR_INVALID_ARG, "rope is null");
     if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % 16)
@@ -201,6 +202,7 @@ int spm_rotate_heads(const spm_rope* rope, const int32_t* positions, int64_t pos
     if (int rc = check_rope(call, rope, positions, pos_stride, n_rows, head_dim)) return rc;
     if (int rc = check_rows(call, "x", x, dtype)) return rc;
     if (int rc = check_rows(call, "y", y, dtype)) return rc;
+    if (x->p == y->p && other_strides(x, y)) return fail(call, SPM_ERR_INVALID_ARG, "y in x's place has other strides");
     WriteArgs a{};
     a.kv.page_size = kKvBlock;
     a.batch.n_seq = -1;
@@ -226,6 +228,7 @@ int spm_kv_write(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_ro
     if (q) {
         if (int rc = check_rows(call, "q", q, dtype)) return rc;
         if (int rc = check_rows(call, "q_out", q_out, dtype)) return rc;
+        if (q->p == q_out->p && other_strides(q, q_out)) return fail(call, SPM_ERR_INVALID_ARG, "q_out in q's place has other strides");
     }
     WriteArgs a{};
     a.kv = pool_of(kv);
@@ -280,6 +283,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     if (int rc = check_rows(call, "q", q, dtype)) return rc;
     if (int rc = check_rows(call, "out", out, dtype)) return rc;
+    if (q->p == out->p) return fail(call, SPM_ERR_INVALID_ARG, "out is in the place of q, which is read until the end");
     if (static_cast<long long>(batch->n_rows) * n_q_heads > INT32_MAX) return fail(call, SPM_ERR_INVALID_ARG, "n_rows * n_q_heads is over 2^31 - 1");
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < attend_bytes(kv->head_dim))
         return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(attend_bytes(kv->head_dim)) + " bytes");

@@ -102,3 +102,20 @@ def test_tables_whose_tokens_kernels_could_not_count():
         with pytest.raises(B.SpmError) as e:
             B.spm_kv_attend_workspace(kv, batch, 8, B.DTYPE_BF16)
         assert e.value.code == -1
+
+
+def test_results_on_top_of_what_other_rows_still_read():
+    """Attention's results in its queries' place, and turned heads in their own place with other strides."""
+    from paper_2607_24787_b200 import binding as B
+    kv, batch, rows = kv_structs(B)
+    other = B.Rows(KV_AT, 2048, 256)
+    for out in (rows, other):
+        with pytest.raises(B.SpmError) as e:
+            B.spm_kv_attend(kv, batch, rows, 8, out, 0.1, B.DTYPE_BF16, KV_AT, 1 << 40)
+        assert e.value.code == -1 and "place" in str(e.value)
+    rope = B.Rope(KV_AT, None, None, None, 1, 128, 0, 1e-6)
+    for call in (lambda: B.spm_rotate_heads(rope, KV_AT, 1, rows, other, 1, 8, 128, B.DTYPE_BF16),
+                 lambda: B.spm_kv_write(kv, batch, rope, KV_AT, 1, rows, other, 8, B.Rows(2 * KV_AT, 256, 128), B.Rows(3 * KV_AT, 256, 128), B.DTYPE_BF16)):
+        with pytest.raises(B.SpmError) as e:
+            call()
+        assert e.value.code == -1 and "place" in str(e.value)
