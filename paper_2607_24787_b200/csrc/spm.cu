@@ -2103,6 +2103,8 @@ int spm_set_attention(spm_ctx* c, const spm_attention* a) {
             return fail(c, SPM_ERR_CONFIG, "attention: rot_dim or n_axes unsupported");
         if (a->rope.rot_dim > 0 && (!a->rope.inv_freq || !a->positions || (a->rope.n_axes > 1 && a->pos_stride < a->batch.n_seq)))
             return fail(c, SPM_ERR_INVALID_ARG, "attention: inv_freq or positions is null, or pos_stride less than the sequences");
+        if (reinterpret_cast<uintptr_t>(a->rope.inv_freq) % 4 || reinterpret_cast<uintptr_t>(a->positions) % 4)
+            return fail(c, SPM_ERR_INVALID_ARG, "attention: inv_freq and positions must be 4-byte aligned");
         if (!aligned16(a->rope.q_gamma) || !aligned16(a->rope.k_gamma)) return fail(c, SPM_ERR_INVALID_ARG, "attention: gammas must be 16-byte aligned");
         if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < attention_bytes(c->cfg, *a))
             return fail(c, SPM_ERR_INVALID_ARG, "attention: workspace must be 16-byte aligned and hold %zu bytes", attention_bytes(c->cfg, *a));

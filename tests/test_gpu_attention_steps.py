@@ -159,3 +159,34 @@ def test_a_step_whose_copies_do_not_land_is_reported():
     m.decode_step(h)
     m.synchronize()
     m.close()
+
+
+def test_addresses_that_a_step_would_refuse():
+    """What the calls of a step refuse is refused when the block is set, and what was set before stays."""
+    from paper_2607_24787_b200 import binding as B
+    cfg = config("bf16", 3)
+    m = build(cfg)
+    block = Block(m, cfg, 3)
+    work = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    caches = (B.KvCache * cfg.n_layers)(*[c.c for c in block.caches])
+
+    def attention(rope_kw={}, **kw):
+        r = block.rope.for_axes(3)
+        rope = B.Rope(*(rope_kw.get(f, getattr(r, f)) for f, _ in B.Rope._fields_))
+        batch = B.KvBatch(block.table.data_ptr(), block.lengths.data_ptr(), None, 3, block.table.shape[1], 3, 1)
+        d = dict(caches=caches, batch=batch, rope=rope, positions=block.positions.data_ptr(), pos_stride=3, rms_gamma=block.gamma.data_ptr(),
+                 w_qkv=block.w_qkv.data_ptr(), w_o=block.w_o.data_ptr(), n_q_heads=block.hq, scale=0.1, workspace=work.data_ptr(),
+                 workspace_bytes=work.numel())
+        d.update(kw)
+        return B.Attention(**d)
+
+    at = block.positions.data_ptr()
+    for bad in (dict(positions=at + 2), dict(positions=None), dict(pos_stride=2), dict(rope_kw=dict(inv_freq=block.inv.data_ptr() + 2)),
+                dict(rope_kw=dict(inv_freq=None)), dict(rope_kw=dict(rot_dim=8)), dict(rope_kw=dict(n_axes=5)), dict(rope_kw=dict(q_gamma=at + 4))):
+        with pytest.raises(B.SpmError):
+            B.spm_set_attention(m.ctx, attention(**bad))
+    B.spm_set_attention(m.ctx, attention())
+    block.step(torch.Generator().manual_seed(1))
+    m.decode_step(torch.randn(3, cfg.hidden).cuda())
+    m.synchronize()
+    m.close()
