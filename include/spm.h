@@ -476,7 +476,7 @@ typedef struct {
 typedef struct {
     const int32_t* page_table;    /* dev [n_seq][table_stride]                                                  */
     const int32_t* lengths;       /* dev [n_seq]                                                                */
-    const int32_t* row_start;     /* dev [n_seq + 1], not falling; NULL: row s is the one new row of sequence s */
+    const int32_t* row_start;     /* dev [n_seq + 1], not falling, at most n_rows; NULL: row s is the one new row of sequence s */
     int32_t n_seq;                /* 0 .. SPM_KV_MAX_SEQS                                                       */
     int32_t table_stride;         /* page numbers a sequence; times page_size at most 2^31 - 4096               */
     int32_t n_rows;               /* rows of the row arrays                                                     */
@@ -522,8 +522,9 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
  * h / (n_q_heads / n_kv_heads)), over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's
  * statistics and all sums are fp32. bf16 calls round a probability and its product with its value's scale to fp16's 11 bits (fewer for
  * probabilities below 2^-22 of the largest, scales below 2^-15 of their group's largest so far and products below 2^-23), or (calls of many
- * rows) a probability, a key and a value once each; fp32 calls keep 23 bits of a query and of a probability times a scale.
- * out may not overlap q. Results do not depend on the order in which CTAs run, and are the same bits for the same call.
+ * rows) a probability, a key and a value once each (a value under 2^-21 of the largest of its head so far keeps fewer bits); fp32 calls keep
+ * 23 bits of a query and of a probability times a scale. A query with a NaN or an infinity gives NaN for its head, unless it sees no token.
+ * scale is finite; out may not overlap q. Results do not depend on the order in which CTAs run, and are the same bits for the same call.
  * workspace: dev, 16-byte aligned, at least spm_kv_attend_workspace() bytes; what it held before does not matter, and calls that may run
  * at the same time need one each. */
 int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, int n_q_heads, int dtype, size_t* bytes);

@@ -23,8 +23,8 @@
 // own ring of bulk copies. Where a cut falls into an item the parts meet in shared memory (cuts between warps) or, for cuts between
 // CTAs, in the workspace, where kv_attend_join_kernel adds them in order.
 //
-// What bounds it: instructions and their latencies, some 660 a tile for eight columns or one, 53 % of the issue slots with four warps a
-// scheduler (which is what 128 registers leave); not memory. 64 sequences of up to 16001 tokens, 268 MB: 70 us, 3.8 TB/s, of it 2.2 us a
+// What bounds it: instructions and their latencies, some 670 a tile for eight columns or one, 49 % of the issue slots with four warps a
+// scheduler (which is what 128 registers leave); not memory. 64 sequences of up to 16001 tokens, 268 MB: 72 us, 3.7 TB/s, of it 2.2 us a
 // tile and warp, and 11 us at the ends (the kernel before, counting and finding the tiles 4, the parts' joining 4). More column tiles a warp
 // (16, 32 columns) were slower a column, and so were 12 warps with deeper rings, and loops rolled up against the size of the code.
 #pragma once

@@ -15,9 +15,10 @@
 //
 // What bounds it, a CTA's tile of 128 tokens for 256 columns: 4017 cycles. The halves take turns, 2250 cycles of softmax and 1770 of products
 // with their hand-over; the exponentials (128 x 256 at 16 a cycle), the products and the shared memory that these read are 2050 each. Four
-// prompts of up to 2049 rows after up to 2048 tokens, 32 heads: 228 us, 0.81 PFLOP/s, of which an item's start and end (search 2 us, queries
-// 3, first scores 1.6, rows out 2.5) are a fifth. Slower: waits with a time hint (262 us for 245 then), steps of 64 tokens with two score
-// buffers a half (262), probabilities against the old maximum held in registers (311, spills).
+// prompts of up to 2049 rows after up to 2048 tokens, 32 heads: 236 us, 0.78 PFLOP/s (the cycles are of 228 us, before exponents were taken from
+// differences and waits by whole warps), of which an item's start and end (search 2 us, queries 3, first scores 1.6, rows out 2.5) are a fifth.
+// Slower: waits with a time hint (262 us for 245 then), steps of 64 tokens with two score buffers a half (262), probabilities against the old
+// maximum held in registers (311, spills).
 #pragma once
 
 #include "kv_attend.cuh"
