@@ -565,6 +565,50 @@ int spm_set_attention(spm_ctx* ctx, const spm_attention* attention);
 /* The block of one layer by itself, as spm_decode_step runs it: h_inout dev [nb][D]. Asynchronous, on the compute stream. */
 int spm_attention_block(spm_ctx* ctx, int layer, float* h_inout, int nb);
 
+/* ---- attention over latent rows: keys and values from one vector a token, which all heads share ----------------------------------
+ * A token's row in the cache is [latent | key]: latent_dim elements, normed as they go in, and a key of rope_dim elements, turned by the
+ * token's position. A head has two matrices: W_k [head][latent_dim] makes the first part of its key from the latent vector, W_v
+ * [head][latent_dim] its value. The absorbed form makes neither: with q' = [q W_k | q_turned] (spm_head_product),
+ *     o'_t = softmax(scale q' . row) latent   (spm_latent_attend),   o = o' W_v^T   (spm_head_product, transposed).
+ *
+ * rows is [n_pages][page_size][latent_dim + rope_dim] in bf16. Batches, pages, new rows and their positions, padded rows, the status word
+ * and its bits, streams and captured calls are as those of the 4-bit cache above; n_pages * page_size is at most 2^31 - 1. */
+typedef struct {
+    void*    rows;          /* dev, 16-byte aligned                                                             */
+    int32_t* status;        /* dev: one word that SPM_KV_* bits are or-ed into; NULL: not recorded              */
+    int32_t  n_pages;
+    int32_t  page_size;     /* tokens, a multiple of 16, at most 65536                                          */
+    int32_t  latent_dim;    /* 128, 256, 384 or 512                                                             */
+    int32_t  rope_dim;      /* 16, 32, 48 or 64                                                                 */
+} spm_latent_cache;
+
+/* The batch's new rows go into the cache: latent (rows of latent_dim elements; head strides are not read) normed with rope's k_gamma
+ * [latent_dim] (NULL: no norm) and key (rows of rope_dim elements) turned, both rounded to bf16; and q_out = the last rope_dim elements of
+ * n_q_heads query heads, q, turned (q NULL: none; q_out may be q itself, with the same strides). rope's rot_dim is at most rope_dim, its
+ * q_gamma NULL. rope NULL: neither norm nor rotation, and q must be NULL. An element that is not finite in bf16 is written as it is, and
+ * SPM_KV_NONFINITE recorded. */
+int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
+                     const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* latent, const spm_rows* key, int dtype, void* stream);
+
+/* out (n_heads heads of latent_dim elements) = softmax(scale q . row) latent for each new row and each of its n_heads heads, q of latent_dim +
+ * rope_dim elements, over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's statistics and all
+ * sums are fp32; bf16 calls round a probability once, to bf16's 8 bits, fp32 calls keep 24 bits of queries and probabilities. A query with
+ * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN (an infinity: in its own
+ * elements at least) for the rows that see it, and changes no other. scale times log2(e) is finite; out may not overlap q. Results do not
+ * depend on the order in which CTAs run, and are the same bits for the same call. Any number of new rows is right; prompts in bf16 are
+ * faster in the expanded form.
+ * workspace: dev, 16-byte aligned, at least spm_latent_attend_workspace() bytes; what it held before does not matter, and calls that may run
+ * at the same time need one each. */
+int spm_latent_attend_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int dtype, size_t* bytes);
+int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_heads, const spm_rows* out, float scale,
+                      int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y_h = x_h W_h (transposed 0: W_h is [in_dim][out_dim]) or x_h W_h^T (else: [out_dim][in_dim]) for each head h of each of n_rows rows. w: dev,
+ * bf16, element (h, i, j) at h * w_head_stride + i * w_row_stride + j; 16-byte aligned, strides multiples of 8. in_dim and out_dim: multiples
+ * of 64, at most 8192. Products of fp32 rows are exact, sums fp32. y may not overlap x. dtype: of x and y. */
+int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, int64_t w_row_stride, int transposed, const spm_rows* y, int n_rows,
+                     int n_heads, int in_dim, int out_dim, int dtype, void* stream);
+
 /* Pinned host memory for the expert store (thin wrappers over cudaHostAlloc / cudaFreeHost). */
 int spm_host_alloc(size_t bytes, void** out);
 int spm_host_free(void* p);

@@ -67,6 +67,11 @@ class KvCache(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("status", C.c_void_p)] + [(k, C.c_int32) for k in ("n_pages", "page_size", "n_kv_heads", "head_dim")]
 
 
+class LatentRows(C.Structure):
+    """spm_latent_cache."""
+    _fields_ = [("rows", C.c_void_p), ("status", C.c_void_p)] + [(k, C.c_int32) for k in ("n_pages", "page_size", "latent_dim", "rope_dim")]
+
+
 class KvBatch(C.Structure):
     _fields_ = ([(k, C.c_void_p) for k in ("page_table", "lengths", "row_start")]
                 + [(k, C.c_int32) for k in ("n_seq", "table_stride", "n_rows", "max_rows")])
@@ -144,6 +149,12 @@ _SIG = {
     "spm_kv_attend": [C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(Rows), C.c_int, C.POINTER(Rows), C.c_float, C.c_int, _P,
                       C.c_size_t, _P],
     "spm_test_kv_waits": [C.c_int, C.c_int],
+    "spm_latent_write": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.POINTER(Rope), _P, C.c_int64, C.POINTER(Rows), C.POINTER(Rows), C.c_int,
+                         C.POINTER(Rows), C.POINTER(Rows), C.c_int, _P],
+    "spm_latent_attend_workspace": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "spm_latent_attend": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.POINTER(Rows), C.c_int, C.POINTER(Rows), C.c_float, C.c_int, _P,
+                          C.c_size_t, _P],
+    "spm_head_product": [C.POINTER(Rows), _P, C.c_int64, C.c_int64, C.c_int, C.POINTER(Rows), C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, _P],
     "spm_host_alloc": [C.c_size_t, C.POINTER(_P)],
     "spm_host_free": [_P],
     "spm_sim_create": [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(_P)],
@@ -509,6 +520,24 @@ def spm_kv_attend_workspace(kv, batch, n_q_heads, dtype) -> int:
 
 def spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
     _check(load().spm_kv_attend(kv, batch, q, n_q_heads, out, scale, dtype, workspace, workspace_bytes, stream))
+
+
+def spm_latent_write(kv, batch, rope, positions, pos_stride, q, q_out, n_q_heads, latent, key, dtype, stream=None):
+    _check(load().spm_latent_write(kv, batch, rope, positions, pos_stride, q, q_out, n_q_heads, latent, key, dtype, stream))
+
+
+def spm_latent_attend_workspace(kv, batch, n_heads, dtype) -> int:
+    out = C.c_size_t()
+    _check(load().spm_latent_attend_workspace(kv, batch, n_heads, dtype, C.byref(out)))
+    return out.value
+
+
+def spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
+    _check(load().spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, workspace_bytes, stream))
+
+
+def spm_head_product(x, w, w_head_stride, w_row_stride, transposed, y, n_rows, n_heads, in_dim, out_dim, dtype, stream=None):
+    _check(load().spm_head_product(x, w, w_head_stride, w_row_stride, int(transposed), y, n_rows, n_heads, in_dim, out_dim, dtype, stream))
 
 
 def spm_test_kv_waits(withhold, limit_us):

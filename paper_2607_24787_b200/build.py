@@ -4,11 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspm.so")
-SOURCES = ["spm.cu", "ffn_noalloc.cu", "kv_cache.cu", "attention_block.cu"]
+SOURCES = ["spm.cu", "ffn_noalloc.cu", "kv_cache.cu", "attention_block.cu", "latent_cache.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC,-O3,-Wall", "--expt-relaxed-constexpr",
@@ -35,7 +37,17 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, *NVCC_FLAGS, *extra, "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+    flags = [f for f in NVCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        cmds = [[nvcc, *flags, *extra, "-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)]
+        with ThreadPoolExecutor(len(cmds)) as pool:      # a process a source
+            list(pool.map(lambda c: _run(c, verbose), cmds))
+        _run([nvcc, *NVCC_FLAGS, *extra, "-o", LIB, *objects], verbose)
+    return LIB
+
+
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), file=sys.stderr)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -43,7 +55,6 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
         raise RuntimeError("nvcc failed:\n" + r.stdout + r.stderr)
     if verbose and (r.stdout or r.stderr):
         print(r.stdout + r.stderr, file=sys.stderr)
-    return LIB
 
 
 if __name__ == "__main__":

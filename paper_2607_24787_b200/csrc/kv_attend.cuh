@@ -161,11 +161,6 @@ __device__ __forceinline__ int row_of_column(const AttendArgs& a, int first, int
 // tiles [from, to) of nt; id: the item's first tile on the line, -1: none
 struct PartMeta { long long id; int ct, head, from, to, nt, first, n; };
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));

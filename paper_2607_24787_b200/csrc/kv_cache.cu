@@ -1,6 +1,5 @@
 // The entry points of the attention block: checks of arguments, launches.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -9,26 +8,14 @@
 #include <cuda_runtime.h>
 
 #include "kv_attend.cuh"
+#include "kv_checks.h"
 #include "kv_prefill.cuh"
 #include "kv_write.cuh"
-
-namespace spm {
-void set_thread_error(const std::string& msg);   // defined next to spm_last_error
-}
 
 using namespace spm;
 
 namespace {
 
-int fail(const char* call, int code, const std::string& msg) {
-    set_thread_error(std::string(call) + ": " + msg);
-    return code;
-}
-bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-
-int check_dtype(const char* call, int dtype) {
-    return dtype == SPM_DTYPE_FP32 || dtype == SPM_DTYPE_BF16 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "rows are fp32 or bf16");
-}
 int check_head_dim(const char* call, int hd) {
     if (hd == 64 || hd == 128 || hd == 256) return SPM_OK;
     return fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(hd) + " not supported: 64, 128 or 256");
@@ -49,47 +36,7 @@ int check_cache(const char* call, const spm_kv_cache* kv) {
         return fail(call, SPM_ERR_INVALID_ARG, "pages must be 16-byte aligned, status 4-byte aligned");
     return SPM_OK;
 }
-int check_batch(const char* call, const spm_kv_cache* kv, const spm_kv_batch* b) {
-    if (!b) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
-    if (b->n_seq < 0 || b->n_seq > SPM_KV_MAX_SEQS)
-        return fail(call, SPM_ERR_INVALID_ARG, "n_seq " + std::to_string(b->n_seq) + " outside 0.." + std::to_string(SPM_KV_MAX_SEQS));
-    if (b->n_rows < 0 || b->max_rows < 0 || b->table_stride < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
-    // (a tile's tokens more than a sequence's are still a number)
-    if (static_cast<long long>(b->table_stride) * kv->page_size > INT32_MAX - 4095ll)
-        return fail(call, SPM_ERR_INVALID_ARG, "table_stride * page_size is over 2^31 - 4096 tokens");
-    if (b->n_seq > 0 && (!b->lengths || (!b->page_table && b->table_stride > 0)))
-        return fail(call, SPM_ERR_INVALID_ARG, "page_table or lengths is null");
-    if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_start, 4))
-        return fail(call, SPM_ERR_INVALID_ARG, "page_table, lengths and row_start must be 4-byte aligned");
-    if (!b->row_start && b->n_rows < b->n_seq) return fail(call, SPM_ERR_INVALID_ARG, "fewer rows than sequences, and no row_start");
-    return SPM_OK;
-}
-int check_rows(const char* call, const char* name, const spm_rows* r, int dtype) {
-    const long long e = dtype == SPM_DTYPE_BF16 ? 2 : 4;
-    if (!r || !r->p) return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + " is null");
-    if (!aligned(r->p, 16) || r->row_stride * e % 16 || r->head_stride * e % 16)
-        return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + ": rows of heads must start on 16-byte boundaries");
-    return SPM_OK;
-}
-bool other_strides(const spm_rows* x, const spm_rows* y) { return x->row_stride != y->row_stride || x->head_stride != y->head_stride; }
-int check_rope(const char* call, const spm_rope* r, const int32_t* positions, int64_t pos_stride, int n_rows, int hd) {
-    if (!r) return fail(call, SPM_ERR_INVALID_ARG, "rope is null");
-    if (r->rot_dim < 0 || r->rot_dim > hd || r->rot_dim % 16)
-        return fail(call, SPM_ERR_CONFIG, "rot_dim " + std::to_string(r->rot_dim) + " is not a multiple of 16 up to head_dim");
-    if (r->n_axes < 1 || r->n_axes > SPM_KV_MAX_AXES) return fail(call, SPM_ERR_INVALID_ARG, "n_axes outside 1.." + std::to_string(SPM_KV_MAX_AXES));
-    if (r->rot_dim > 0 && (!r->inv_freq || !positions)) return fail(call, SPM_ERR_INVALID_ARG, "inv_freq or positions is null");
-    if (r->rot_dim > 0 && r->n_axes > 1 && pos_stride < n_rows) return fail(call, SPM_ERR_INVALID_ARG, "pos_stride is less than the rows");
-    if (!aligned(r->inv_freq, 4) || !aligned(positions, 4) || !aligned(r->q_gamma, 16) || !aligned(r->k_gamma, 16))
-        return fail(call, SPM_ERR_INVALID_ARG, "gammas must be 16-byte aligned, inv_freq and positions 4-byte aligned");
-    return SPM_OK;
-}
-
 KvPool pool_of(const spm_kv_cache* kv) { return {static_cast<unsigned char*>(kv->pages), kv->status, kv->n_pages, kv->page_size, kv->n_kv_heads}; }
-KvBatch batch_of(const spm_kv_batch* b) { return {b->page_table, b->lengths, b->row_start, b->n_seq, b->table_stride, b->n_rows}; }
-HeadRows rows_of(const spm_rows* r) { return {r->p, r->row_stride, r->head_stride}; }
-RopeArgs rope_of(const spm_rope* r, const int32_t* positions, int64_t pos_stride) {
-    return {r->inv_freq, r->axis_of, r->q_gamma, r->k_gamma, positions, pos_stride, r->n_axes, r->rot_dim, r->neighbours, r->eps};
-}
 
 // calls f with a null pointer of the row type and the head size as a constant
 template <typename F>
@@ -101,11 +48,6 @@ void by_type(int dtype, int hd, F f) {
     };
     if (dtype == SPM_DTYPE_BF16) size(static_cast<__nv_bfloat16*>(nullptr));
     else size(static_cast<float*>(nullptr));
-}
-
-int launched(const char* call, cudaError_t e) {
-    if (e != cudaSuccess) cudaGetLastError();
-    return e == cudaSuccess ? SPM_OK : fail(call, SPM_ERR_CUDA, std::string("launch: ") + cudaGetErrorString(e));
 }
 
 int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaStream_t st) {
@@ -123,23 +65,9 @@ int launch_write(const char* call, const WriteArgs& a, int hd, int dtype, cudaSt
     return launched(call, e);
 }
 
-std::atomic<unsigned long long> g_wait_ns{2'000'000'000ull};
-std::atomic<int> g_withhold{0};
-
 // joins, the rows that each of two kernels takes, parts
 constexpr size_t kAtJoinBytes = kAtMaxCtas * 32, kAtRowsBytes = 2 * SPM_KV_MAX_SEQS * sizeof(int);
 size_t attend_bytes(int hd) { return kAtJoinBytes + kAtRowsBytes + kAtMaxCtas * 2 * size_t(8) * (hd + 2) * 4; }
-
-constexpr int kMaxDevices = 64;
-// Once a kernel and device: shared memory beyond 48 KB
-template <auto KERNEL>
-cudaError_t allow_smem(int dev, int bytes) {
-    static std::atomic<bool> done[kMaxDevices];
-    if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) done[dev].store(true, std::memory_order_release);
-    return e;
-}
 
 template <typename T, int HD>
 cudaError_t launch_attend(const AttendArgs& a, int dev, int sms, cudaStream_t st) {
@@ -217,7 +145,7 @@ int spm_kv_write(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_ro
     const char* call = "spm_kv_write";
     if (int rc = check_dtype(call, dtype)) return rc;
     if (int rc = check_cache(call, kv)) return rc;
-    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
     if (n_q_heads < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
     if (q && !rope) return fail(call, SPM_ERR_INVALID_ARG, "q without rope: there is nothing to do to it");
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
@@ -244,7 +172,7 @@ int spm_kv_read(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_row
     const char* call = "spm_kv_read";
     if (int rc = check_dtype(call, dtype)) return rc;
     if (int rc = check_cache(call, kv)) return rc;
-    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
     if (!k_out && !v_out) return fail(call, SPM_ERR_INVALID_ARG, "neither k_out nor v_out");
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
     ReadArgs a{};
@@ -266,7 +194,7 @@ int spm_kv_attend_workspace(const spm_kv_cache* kv, const spm_kv_batch* batch, i
     if (!bytes) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
     if (int rc = check_dtype(call, dtype)) return rc;
     if (int rc = check_cache_shape(call, kv)) return rc;
-    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
     *bytes = attend_bytes(kv->head_dim);
     return SPM_OK;
@@ -277,7 +205,7 @@ int spm_kv_attend(const spm_kv_cache* kv, const spm_kv_batch* batch, const spm_r
     const char* call = "spm_kv_attend";
     if (int rc = check_dtype(call, dtype)) return rc;
     if (int rc = check_cache(call, kv)) return rc;
-    if (int rc = check_batch(call, kv, batch)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return fail(call, SPM_ERR_CONFIG, "n_q_heads is not a multiple of n_kv_heads");
     if (!std::isfinite(scale)) return fail(call, SPM_ERR_INVALID_ARG, "scale is not finite");
     if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;

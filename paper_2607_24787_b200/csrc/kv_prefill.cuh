@@ -33,8 +33,6 @@ constexpr int kPfCols = 256;
 constexpr int kPfThreads = 16 * 32;
 constexpr int kPfSoftmaxRegs = 176, kPfOperandRegs = 104, kPfIssueRegs = 56;
 static_assert(2 * kPfSoftmaxRegs + kPfOperandRegs + kPfIssueRegs == 4 * 128, "the split is what the launch has");
-template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int HD>
 struct PfShape {
     static constexpr int block_bytes = kPfTile * 128;                    // 64 elements of 128 rows
@@ -42,42 +40,10 @@ struct PfShape {
     static constexpr int smem = 6 * op_bytes + 1024;                     // queries of two halves, two stages of keys and values
 };
 
-// A in tensor memory
-__device__ __forceinline__ void pf_mma_ts(uint32_t d, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
-        "}\n"
-        ::"r"(d), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
 // fp16 x fp16 -> fp32, M = 128
 __host__ __device__ constexpr uint32_t pf_idesc(int n, bool b_mn_major) {
     return (1u << 4) | (uint32_t(b_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
 }
-#define PF_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
-#define PF_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
-__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
-        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : PF_R8(r, 0), PF_R8(r, 8), PF_R8(r, 16), PF_R8(r, 24) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void tmem_ld16_raw(uint32_t at, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : PF_R8(r, 0), PF_R8(r, 8) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-        ::PF_W8(r, 0), PF_W8(r, 8), "r"(at) : "memory");
-}
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-
 // Eight codes of a word as fp16 elements times a scale, in the order (0, 4, 1, 5, 2, 6, 3, 7): 1024 + q (low nibbles of the masked halves)
 // less 1032, 1024 + 16 q over 16 less 72, both exact, then one rounding
 __device__ __forceinline__ uint4 pf_expand(uint32_t w, __half2 s) {
@@ -87,9 +53,6 @@ __device__ __forceinline__ uint4 pf_expand(uint32_t w, __half2 s) {
                       bits_of(__hmul2(__hfma2(as_half2((w & 0x00f000f0u) | 0x64006400u), sixteenth, off72), s)),
                       bits_of(__hmul2(__hadd2(as_half2((h & 0x000f000fu) | 0x64006400u), off), s)),
                       bits_of(__hmul2(__hfma2(as_half2((h & 0x00f000f0u) | 0x64006400u), sixteenth, off72), s)));
-}
-__device__ __forceinline__ void st_shared16(uint32_t at, const uint4& v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 // 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
 __device__ __forceinline__ uint32_t pf_chunk(int row, int ch) {
@@ -105,12 +68,6 @@ struct PfShared {
     int widest[4], widest_key[4];                // an operand warp's largest scale of a tile's values and keys, as fp32 bits
     uint32_t there[4][4];                        // which tokens of a tile exist
 };
-
-// 16 bytes to shared memory, or zeros, without a register on the way; then: this thread's have arrived.
-__device__ __forceinline__ void copy16_or_zero(uint32_t at, const void* from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Sequences of a batch of prompts that are not for the kernel below: it walks an item's tokens one after another, so a few of few columns over
 // many tokens are better shared out between all SMs. They are those of over twice the tokens that the batch's columns see in the mean, if
@@ -597,7 +554,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kPfTile / 16; ++k)
-                        pf_mma_ts(t_o + h * HD, t_s + h * 128 + 8 * k, smem_desc_sw128(v_at + st * S::op_bytes + k * 2048, S::block_bytes, 1024),
+                        tc_mma_f16_ts(t_o + h * HD, t_s + h * 128 + 8 * k, smem_desc_sw128(v_at + st * S::op_bytes + k * 2048, S::block_bytes, 1024),
                                   idesc_o, more || k > 0);
                 }
                 __syncwarp();

@@ -1,0 +1,691 @@
+// Attention of new rows over latent rows, which are keys and values of all heads at once (the absorbed form), on tcgen05.
+//
+// A column is a head of a new row: column x of a sequence is head x % heads of row x / heads. A CTA takes COLS columns and walks their
+// tokens 64 at a time. Both products have the cache's rows as their A operand, where they lie, and columns as N, so that few columns cost
+// few cycles: scores S^T [64 tokens][columns] = C q^T, the rows K-major, and sums O^T [latent][columns] += C^T P^T, the same bytes M-major.
+// S^T, in two buffers, and O^T, latent / 128 tiles, are in tensor memory. Every byte of a row comes to the SM once, for both.
+//
+// A warp brings tiles by TMA (64 elements of a page's rows a copy, swizzled) into a ring of as many stages as there is room for; one issues
+// the products, of a tile's scores as soon as it has landed, of its sums as soon as its probabilities are there; four turn scores into
+// probabilities, 16 tokens each, and write results. A probability is 2^(s - m), m not the running maximum but one that was it: it is moved
+// only when a score is above it by more than 64, where it has lost nothing yet (P is bf16, which has fp32's range, and sums stay below
+// 2^(64 + 31)). So a tile needs no maximum over its tokens, only a vote that none is that far above.
+//
+// fp32 queries and probabilities are three bf16 parts each, cut off and not rounded: three columns side by side in one product, added up
+// as scores and results are read. bf16 calls round a probability to bf16's 8 bits once.
+//
+// All (sequence, columns) items together are a line of tiles that is cut evenly between CTAs, whatever the lengths are. An item's parts
+// in several CTAs go to the workspace and latent_join_kernel adds them in order. (Items count with all of a sequence's tokens; columns that
+// see fewer, as a prompt's do, leave their CTA idle for the others. Such calls are few: prompts have the expanded form.)
+#pragma once
+
+#include <cuda.h>
+
+#include "kv_cache.cuh"
+#include "latent_cache.cuh"
+#include "mma_ops.cuh"
+#include "ptx.cuh"
+#include "tc_ops.cuh"
+
+namespace spm {
+
+struct LatentAttendArgs {
+    LatentPool kv;
+    KvBatch batch;
+    HeadRows q, out;
+    int heads;
+    int chunks, stages;         // 64-element chunks of a row, tiles of the ring
+    int box;                    // tokens of a copy: 16, 32 or 64, all of one page
+    float factor;               // of scores: scale times log2(e)
+    float* parts;               // [2 * CTAs][LaPart floats]
+    int4* joins;                // [CTAs], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), sequence, block of columns
+    unsigned long long wait_ns; // a wait in a kernel gives up after this long
+    int withhold;               // (tests) arrivals that barriers wait for and nobody makes
+};
+
+constexpr int kLaTile = 64, kLaMaxCtas = 148, kLaMaxStages = 8, kLaThreads = 192;
+constexpr int kLaChunkBytes = kLaTile * 128;
+constexpr float kLaSlack = 64.f;
+
+template <typename T, int COLS>
+struct LaShape {
+    static constexpr int parts = sizeof(T) == 4 ? 3 : 1;     // of a number
+    static constexpr int n = COLS * parts;                   // N of the products
+    static_assert(n <= 64 && n % 16 == 0, "O^T of 512 elements, and two buffers of S^T, fit tensor memory");
+    static constexpr int q_bytes(int chunks) { return chunks * n * 128; }
+    static constexpr int p_bytes = n * 128;
+    static constexpr int fixed(int chunks) { return 1024 + q_bytes(chunks) + p_bytes; }
+    static constexpr int part_floats(int latent) { return COLS * (latent + 2); }     // sums, then maxima, then sums of probabilities
+};
+constexpr int kLaOwnBytes = 2048;                            // LaShared below
+constexpr int la_smem(int fixed, int chunks, int stages) { return fixed + chunks * stages * kLaChunkBytes; }
+
+struct LaShared {
+    unsigned long long full[kLaMaxStages], empty[kLaMaxStages], s_full[2], p_full, q_full, drained;
+    uint32_t tmem;
+    int quit;                                                // a wait has run out: everybody leaves
+    int ctas;                                                // that have a piece
+    int seq, group, tile;                                    // where this CTA's piece of the line begins
+    long long left, all, at;                                 // its tiles, all tiles, its first one
+    int absent[kLaMaxStages];                                // a tile's copies (`box` tokens each) that there are not
+    int limit[2][64];                                        // tokens that a column sees; of one item and the next
+};
+static_assert(sizeof(LaShared) <= kLaOwnBytes, "what shared memory has beside the ring");
+
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int element, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(element), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        " .reg .pred p;\n"
+        " mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// bf16 x bf16 -> fp32
+__host__ __device__ constexpr uint32_t la_idesc(int m, int n, bool a_mn_major) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(a_mn_major) << 15) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
+}
+// 16 lanes, 16 columns, in the layout of mma.sync's accumulators: r[4 i + 2 h + e] is row lane / 4 + 8 h, column 8 i + 2 (lane % 4) + e
+__device__ __forceinline__ void tmem_ld_frag(uint32_t at, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : SPM_R8(r, 0) : "r"(at) : "memory");
+}
+// four 8 x 8 matrices, each stored by columns
+__device__ __forceinline__ void st_matrix_trans(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// A sequence's items on the line: blocks of columns, tiles of each (one at least, so that rows that see nothing are written too)
+struct LaSequence { int first, n, len, cap_len, blocks, tiles; };
+template <int COLS>
+__device__ __forceinline__ LaSequence la_sequence(const LatentAttendArgs& a, int s) {
+    LaSequence q;
+    q.first = s;
+    q.n = 1;
+    if (a.batch.row_start) {
+        q.first = a.batch.row_start[s];
+        q.n = max(0, min(a.batch.row_start[s + 1] - q.first, a.batch.n_rows));
+    }
+    q.len = a.batch.lengths[s];
+    q.cap_len = max(0, min(q.len, a.batch.stride * a.kv.page_size));
+    q.blocks = (q.n * a.heads + COLS - 1) / COLS;
+    q.tiles = max(1, (q.cap_len + kLaTile - 1) / kLaTile);
+    return q;
+}
+
+// A CTA's walk over its items. `tiles`: those of [from, to) in which the item's columns see a token.
+template <int COLS>
+struct LaWalk {
+    LaSequence s;
+    int seq, group, from, to, sees, tiles;
+    long long left;
+    __device__ __forceinline__ void start(const LatentAttendArgs& a, const LaShared& sh) {
+        seq = sh.seq; group = sh.group; from = sh.tile; left = sh.left;
+        if (left > 0) { s = la_sequence<COLS>(a, seq); piece(a); }
+    }
+    __device__ __forceinline__ void piece(const LatentAttendArgs& a) {
+        to = int(min(static_cast<long long>(s.tiles), from + left));
+        const int last = min(s.n - 1, ((group + 1) * COLS - 1) / a.heads);
+        sees = max(0, min(s.len - s.n + last + 1, s.cap_len));
+        tiles = max(0, min(to, (sees + kLaTile - 1) / kLaTile) - from);
+    }
+    __device__ __forceinline__ void next(const LatentAttendArgs& a) {
+        left -= to - from;
+        if (left <= 0) return;
+        from = 0;
+        if (++group >= s.blocks) {
+            group = 0;
+            do {
+                if (++seq >= a.batch.n_seq) { left = 0; return; }
+                s = la_sequence<COLS>(a, seq);
+            } while (s.n <= 0);
+        }
+        piece(a);
+    }
+};
+
+template <typename T, int COLS>
+__global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const LatentAttendArgs a, const __grid_constant__ CUtensorMap rows_map) {
+    using S = LaShape<T, COLS>;
+    constexpr int N = S::n, PARTS = S::parts, BLOCKS = COLS / 8;
+    extern __shared__ __align__(16) unsigned char raw_smem[];
+    // (the kernel's own arrays first: they take the room that aligning the rest would)
+    LaShared& sh = *reinterpret_cast<LaShared*>(raw_smem);
+    const uint32_t base = (smem_u32(raw_smem) + kLaOwnBytes + 1023) & ~1023u;
+    const int chunks = a.chunks, stages = a.stages, latent = a.kv.latent;
+    const uint32_t stage_bytes = chunks * kLaChunkBytes, q_at = base + stages * stage_bytes, p_at = q_at + S::q_bytes(chunks);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    grid_dep_wait();
+    grid_dep_launch();
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) { mbar_init(smem_u32(&sh.full[i]), 1 + a.withhold); mbar_init(smem_u32(&sh.empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.s_full[i]), 1);
+        mbar_init(smem_u32(&sh.p_full), 128);
+        mbar_init(smem_u32(&sh.q_full), 128);
+        mbar_init(smem_u32(&sh.drained), 1);
+        sh.quit = 0;
+        fence_barrier_init();
+    }
+    if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), 512);
+    if (warp == 4) {
+        // ---- this CTA's piece of the line: a lane counts sequences side by side ----
+        const int each = (a.batch.n_seq + 31) / 32, s0 = lane * each, s1 = min(s0 + each, a.batch.n_seq);
+        long long mine = 0;
+        for (int s = s0; s < s1; ++s) {
+            const LaSequence q = la_sequence<COLS>(a, s);
+            mine += static_cast<long long>(q.blocks) * q.tiles;
+            if (q.n > 0 && q.len > q.cap_len && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+        }
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const long long all = __shfl_sync(0xffffffffu, upto, 31);
+        // (no more CTAs than tiles: those that share an item are neighbours)
+        const long long ctas = max(1ll, min(all, static_cast<long long>(gridDim.x))), cta = min(static_cast<long long>(blockIdx.x), ctas);
+        const long long at = all * cta / ctas, end = cta < ctas ? all * (cta + 1) / ctas : at;
+        if (lane == 0) { sh.left = end - at; sh.all = all; sh.at = at; sh.ctas = int(ctas); }
+        long long rest = at - (upto - mine);
+        if (end > at && rest >= 0 && rest < mine)
+            for (int s = s0; s < s1; ++s) {
+                const LaSequence q = la_sequence<COLS>(a, s);
+                const long long own = static_cast<long long>(q.blocks) * q.tiles;
+                if (rest < own) {
+                    sh.seq = s;
+                    sh.group = int(rest / q.tiles);
+                    sh.tile = int(rest % q.tiles);
+                    break;
+                }
+                rest -= own;
+            }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t t_s = sh.tmem, t_o = t_s + 2 * N;
+
+    // a warp goes on, or gives up, as one
+    auto wait = [&](const unsigned long long& bar, int parity) {
+        const uint32_t at = smem_u32(&bar);
+        if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
+        const unsigned long long t0 = global_timer_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 32; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
+            const bool late = global_timer_ns() - t0 > a.wait_ns;
+            if (late) {
+                *reinterpret_cast<volatile int*>(&sh.quit) = 1;
+                kv_note(a.kv, SPM_KV_TIMEOUT);
+            }
+            if (__any_sync(0xffffffffu, late || *reinterpret_cast<volatile int*>(&sh.quit))) return false;
+        }
+    };
+
+    LaWalk<COLS> w;
+    w.start(a, sh);
+    bool ok = true;
+    if (warp < 4) {
+        // ---- queries, softmax, results ----
+        int item = 0, st = 0, turn = 0;          // items with a token in them; stage of the tile, and its barriers' phase
+        unsigned it = 0;                         // tiles
+        const int r0 = lane >> 2, c2 = (lane & 3) * 2;
+        auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+        auto vote = [](bool yes) {
+            int any;
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                         : "=r"(any) : "r"(int(yes)) : "memory");
+            return any != 0;
+        };
+        float* red = reinterpret_cast<float*>(raw_smem + (p_at - smem_u32(raw_smem)));       // [4 warps][COLS], in the probabilities' place
+        while (w.left > 0 && ok) {
+            const int half = item & 1;
+            // ---- this item's columns: a warp brings every fourth ----
+            if (w.tiles > 0) {
+#pragma unroll 4
+                for (int col = warp; col < COLS; col += 4) {
+                    const int x = w.group * COLS + col, i = x / a.heads, h = x - i * a.heads, row = w.s.first + i;
+                    const bool is = i < w.s.n && row >= 0 && row < a.batch.n_rows;
+                    const T* from = static_cast<const T*>(a.q.p) + row * a.q.row + h * a.q.head;
+                    const int vectors = (latent + a.kv.rope) / 8;
+                    Raw8 v[3] = {};
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (is && k * 32 + lane < vectors) v[k] = raw8(from + (k * 32 + lane) * 8);
+                    bool odd = false;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        float f[8];
+                        unpack8<T>(v[k], f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) odd |= !(fabsf(f[e]) < INFINITY);
+                    }
+                    // (infinite scores could all be -infinity, as those of tokens that it does not see are: NaN as a whole)
+                    const uint32_t nan = __any_sync(0xffffffffu, odd) ? 0x7fff7fffu : 0u;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        const int e = k * 32 + lane;
+                        if (e >= vectors) continue;
+                        const uint32_t to = q_at + (e >> 3) * (N * 128) + col * 128 + (((e & 7) ^ (col & 7)) << 4);
+                        if constexpr (PARTS == 1) st_shared16(to, make_uint4(v[k].a.x | nan, v[k].a.y | nan, v[k].a.z | nan, v[k].a.w | nan));
+                        else {
+                            float f[8];
+                            unpack8<T>(v[k], f);
+                            uint32_t p[4][3];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) cut_parts(f[2 * u], f[2 * u + 1], p[u]);
+#pragma unroll
+                            for (int u = 0; u < 3; ++u) st_shared16(to + u * (COLS * 128), make_uint4(p[0][u] | nan, p[1][u] | nan, p[2][u] | nan, p[3][u] | nan));
+                        }
+                    }
+                    if (lane == 0) sh.limit[half][col] = is ? max(0, min(w.s.len - w.s.n + i + 1, w.s.cap_len)) : 0;
+                }
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&sh.q_full));
+            }
+            float m[BLOCKS][2], l[BLOCKS][2] = {};
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) m[i][0] = m[i][1] = 0.f;
+            // tokens that all columns see: behind them are masks to look at
+            const int all_see = w.s.n == 1 ? w.sees : max(0, min(w.s.len - w.s.n + w.group * COLS / a.heads + 1, w.s.cap_len));
+            for (int j = 0; j < w.tiles; ++j, ++it) {
+                const int t0 = (w.from + j) * kLaTile;
+                // (a warp that gives up still comes to the others' barriers; they leave together)
+                ok = ok && wait(sh.s_full[it & 1], (it >> 1) & 1) && wait(sh.full[st], turn);
+                tc_fence_after();
+                uint32_t r[N / 16][8];
+#pragma unroll
+                for (int i = 0; i < N / 16; ++i) tmem_ld_frag(t_s + (it & 1) * N + 16 * i + (uint32_t(warp) << 21), r[i]);
+                tmem_wait_ld();
+                const int absent = *reinterpret_cast<volatile int*>(&sh.absent[st]);
+                const bool masks = t0 + kLaTile > all_see || absent != 0;
+                float s[BLOCKS][4];              // (s - m): [8-wide block][row half * 2 + column]
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = __uint_as_float(r[i / 2][(i & 1) * 4 + e]);
+                        if constexpr (PARTS == 3) v = v + __uint_as_float(r[i / 2 + 1][(i & 1) * 4 + e]) + __uint_as_float(r[i / 2 + 2][(i & 1) * 4 + e]);
+                        s[i][e] = fmaf(v, a.factor, -m[i][e & 1]);
+                    }
+                auto highest = [&] {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+                    return top;
+                };
+                // the sums of the tile before are done (and the item before's, at its end): P and O may be touched
+                auto sums_done = [&] { ok = ok && (j == 0 || wait(sh.empty[(st == 0 ? stages : st) - 1], st == 0 ? turn ^ 1 : turn)); };
+                if (vote(highest() > kLaSlack || j == 0 || masks || !ok)) {
+                    if (vote(!ok)) { ok = false; break; }
+                    sums_done();
+                    if (masks) {
+                        // a thread looks at half of a token's row. What no column may see becomes zeros, so that 0 * NaN does not come up, and so
+                        // does a row that is not finite where some columns see it and some do not
+                        uint32_t* odd = reinterpret_cast<uint32_t*>(red);
+                        if (tid < 2) odd[tid] = 0;
+                        together();
+                        const int t = tid >> 1, token = t0 + t;
+                        const bool there = token < w.sees && !(absent >> (t / a.box) & 1);
+                        const uint32_t at = base + st * stage_bytes + t * 128;
+                        const int units = latent / 8;
+                        bool bad = false;
+                        if (there && token >= all_see)
+                            for (int u = tid & 1; u < units; u += 2) {
+                                const uint4 v = lds128(at + (u >> 3) * kLaChunkBytes + (((u & 7) ^ (t & 7)) << 4));
+                                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) bad |= (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
+                            }
+                        const bool either = __shfl_xor_sync(0xffffffffu, bad, 1) | bad;
+                        if (!there || either)
+                            for (int u = tid & 1; u < units; u += 2)
+                                st_shared16(at + (u >> 3) * kLaChunkBytes + (((u & 7) ^ (t & 7)) << 4), make_uint4(0, 0, 0, 0));
+                        if (either) atomicOr(&odd[t >> 5], 1u << (t & 31));
+                        together();
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int mine = warp * 16 + r0 + 8 * k;
+                            const bool gone = absent >> (mine / a.box) & 1, poison = odd[mine >> 5] >> (mine & 31) & 1;
+#pragma unroll
+                            for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    if (gone || t0 + mine >= sh.limit[half][8 * i + c2 + e]) s[i][2 * k + e] = -INFINITY;
+                                    else if (poison) s[i][2 * k + e] = __int_as_float(0x7fffffff);
+                                }
+                        }
+                    }
+                    if (vote(highest() > kLaSlack || j == 0)) {
+                        tc_fence_after();
+#pragma unroll
+                        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float top = fmaxf(s[i][e], s[i][e + 2]);
+#pragma unroll
+                                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                                if (lane < 4) red[warp * COLS + 8 * i + c2 + e] = top;
+                            }
+                        together();
+                        float by[BLOCKS][2];
+#pragma unroll
+                        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int col = 8 * i + c2 + e;
+                                float top = fmaxf(fmaxf(red[col], red[COLS + col]), fmaxf(red[2 * COLS + col], red[3 * COLS + col]));
+                                // (nothing seen: stays. Only the first tile's may be below zero)
+                                if (top == -INFINITY || (j > 0 && top < 0.f)) top = 0.f;
+                                m[i][e] += top;
+                                by[i][e] = j > 0 ? ex2(-top) : 0.f;
+                                l[i][e] *= by[i][e];
+                                s[i][e] -= top;
+                                s[i][e + 2] -= top;
+                            }
+                        together();
+                        if (j > 0) {                 // seldom: the sums so far go down
+                            if (warp == 0 && lane < 4)
+#pragma unroll
+                                for (int i = 0; i < BLOCKS; ++i) { red[8 * i + c2] = by[i][0]; red[8 * i + c2 + 1] = by[i][1]; }
+                            together();
+#pragma unroll 1
+                            for (int mt = 0; mt < latent / 128; ++mt)
+#pragma unroll 1
+                                for (int ch = 0; ch < N / 16; ++ch) {
+                                    uint32_t o[16];
+                                    const uint32_t at = t_o + mt * N + ch * 16 + (uint32_t(warp) << 21);
+                                    tmem_ld16_raw(at, o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * red[(ch * 16 + i) % COLS]);
+                                    tmem_st16(at, o);
+                                }
+                            tmem_wait_st();
+                            together();
+                        }
+                    }
+                } else sums_done();
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[i][e] = ex2(s[i][e]);
+                        l[i][e & 1] += s[i][e];
+                    }
+                // [column][token]: 16-byte unit 2 warp + (row half) of a column's 128 bytes
+                const uint32_t to = p_at + ((lane >> 4) * 8 + (lane & 7)) * 128 + ((2 * warp + (lane >> 3 & 1) ^ (lane & 7)) << 4);
+#pragma unroll
+                for (int i = 0; i < BLOCKS; i += 2) {
+                    uint32_t p[4][3];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float x = s[i + k / 2][(k & 1) * 2], y = s[i + k / 2][(k & 1) * 2 + 1];
+                        if constexpr (PARTS == 3) cut_parts(x, y, p[k]);
+                        else p[k][0] = pack_bf16(x, y);
+                    }
+#pragma unroll
+                    for (int u = 0; u < PARTS; ++u) st_matrix_trans(to + (u * COLS + 8 * i) * 128, p[0][u], p[1][u], p[2][u], p[3][u]);
+                }
+                fence_proxy_async();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&sh.p_full));
+                if (++st == stages) { st = 0; turn ^= 1; }
+            }
+            // ---- the item's result, or this CTA's part of it ----
+            const bool whole = w.from == 0 && w.to == w.s.tiles;
+            if (w.tiles > 0) {
+                ok = ok && wait(sh.empty[(st == 0 ? stages : st) - 1], st == 0 ? turn ^ 1 : turn);
+                if (vote(!ok)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) l[i][e] += __shfl_xor_sync(0xffffffffu, l[i][e], o);
+                        if (lane < 4) red[warp * COLS + 8 * i + c2 + e] = l[i][e];
+                    }
+                together();
+            }
+            float* part = a.parts + (size_t(blockIdx.x) * 2 + (w.from == 0)) * S::part_floats(latent);       // slot 0: an item that began before this CTA
+            float total = 0.f;
+            if (w.tiles > 0 && tid < COLS) total = red[tid] + red[COLS + tid] + red[2 * COLS + tid] + red[3 * COLS + tid];
+            together();
+            if (!whole) {
+                // (NaN is no part that sees nothing: its maximum is above all, and the item becomes NaN)
+                if (warp == 0 && lane < 4)
+#pragma unroll
+                    for (int i = 0; i < BLOCKS; ++i) { red[8 * i + c2] = m[i][0]; red[8 * i + c2 + 1] = m[i][1]; }
+                together();
+                if (tid < COLS) {
+                    part[COLS * latent + tid] = total == 0.f ? -INFINITY : total == total ? red[tid] : INFINITY;
+                    part[COLS * latent + COLS + tid] = total;
+                }
+            } else if (tid < COLS) red[tid] = total == 0.f ? 0.f : 1.f / total;
+            together();
+            if (w.tiles > 0 || whole) {
+#pragma unroll 1
+                for (int ch = 0; ch < COLS / 16; ++ch)
+#pragma unroll 1
+                    for (int mt = 0; mt < latent / 128; ++mt) {
+                        const int d = mt * 128 + tid;
+                        uint32_t o[PARTS][16] = {};
+                        if (w.tiles > 0) {
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + ch * 16 + (uint32_t(warp) << 21), o[u]);
+                            tmem_wait_ld();
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int col = ch * 16 + i;
+                            float v = __uint_as_float(o[0][i]);
+                            if constexpr (PARTS == 3) v = v + __uint_as_float(o[1][i]) + __uint_as_float(o[2][i]);
+                            if (whole) {
+                                const int x = w.group * COLS + col, row_in = x / a.heads, h = x - row_in * a.heads, row = w.s.first + row_in;
+                                if (row_in >= w.s.n || row < 0 || row >= a.batch.n_rows) continue;
+                                T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d;
+                                v *= red[col];
+                                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(v);
+                                else *to = v;
+                            } else part[col * latent + d] = v;
+                        }
+                    }
+            }
+            tc_fence_before();
+            together();                          // (`red` has been read)
+            item += w.tiles > 0;
+            w.next(a);
+        }
+    } else if (warp == 4) {
+        // ---- tiles on their way in ----
+        int st = 0, turn = 0;
+        unsigned it = 0;
+        int4 join = make_int4(0, 0, 0, 0);
+        while (w.left > 0 && ok) {
+            if (w.from == 0 && w.to < w.s.tiles) {           // begins here and goes on: up to the CTA that has its last tile
+                const long long end = sh.at + (sh.left - w.left) + w.s.tiles;
+                join = make_int4(int((end * sh.ctas - 1) / sh.all) - int(blockIdx.x) + 1, w.seq, w.group, 0);
+            }
+            const int copies = kLaTile / a.box;
+            auto row_of = [&](int j) {           // of this lane's copy in the pool; -1: there is none, -2: nobody sees it
+                const int token = (w.from + j) * kLaTile + lane * a.box;
+                return lane < copies && j < w.tiles && token < w.sees ? latent_row_at(a.kv, a.batch, w.seq, token, true) : -2ll;
+            };
+            long long row = row_of(0);
+            for (int j = 0; j < w.tiles; ++j, ++it) {
+                const long long row_then = row_of(j + 1);
+                if (it >= unsigned(stages) && !(ok = wait(sh.empty[st], turn ^ 1))) break;
+                const uint32_t there = __ballot_sync(0xffffffffu, row >= 0);
+                const uint32_t bar = smem_u32(&sh.full[st]);
+                if (lane == 0) {
+                    sh.absent[st] = int(~there & ((1u << copies) - 1));
+                    mbar_arrive_expect_tx(bar, __popc(there) * a.box * 128 * chunks);
+                }
+                __syncwarp();
+                if (row >= 0)
+                    for (int c = 0; c < chunks; ++c)
+                        tma_rows(base + st * stage_bytes + c * kLaChunkBytes + lane * a.box * 128, &rows_map, c * 64, int(row), bar);
+                __syncwarp();
+                row = row_then;
+                if (++st == stages) { st = 0; turn ^= 1; }
+            }
+            if (ok) w.next(a);
+        }
+        // copies under way end before shared memory is given back, whoever has given up
+        for (unsigned k = it > unsigned(stages) ? it - stages : 0; k < it; ++k) mbar_wait_bounded(smem_u32(&sh.full[k % stages]), (k / stages) & 1, a.wait_ns);
+        if (lane == 0) a.joins[blockIdx.x] = join;
+        __syncwarp();
+    } else {
+        // ---- products. The warp walks as one, so that the elected lane is one lane throughout ----
+        const uint32_t idesc_s = la_idesc(kLaTile, N, false), idesc_o = la_idesc(128, N, true);
+        const int rope_steps = a.kv.rope / 16, m_tiles = latent / 128;
+        int st = 0, turn = 0, item = 0;
+        unsigned it = 0;
+        bool any = false;
+        auto scores = [&](unsigned tile, int stage) {
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t d = t_s + (tile & 1) * N, from = base + stage * stage_bytes;
+                for (int c = 0; c < chunks; ++c) {
+                    const int steps = c + 1 < chunks ? 4 : rope_steps;
+                    for (int k = 0; k < steps; ++k)
+                        tc_mma_f16(d, smem_desc_sw128(from + c * kLaChunkBytes + k * 32, 16, 1024), smem_desc_sw128(q_at + c * (N * 128) + k * 32, 16, 1024),
+                                   idesc_s, c + k > 0);
+                }
+                tc_commit(smem_u32(&sh.s_full[tile & 1]));
+            }
+            any = true;
+            __syncwarp();
+        };
+        while (w.left > 0 && ok) {
+            if (w.tiles > 0) {
+                if (!(ok = wait(sh.q_full, item & 1))) break;
+                if (!(ok = wait(sh.full[st], turn))) break;
+                scores(it, st);
+                for (int j = 0; j < w.tiles; ++j, ++it) {
+                    const int next = st + 1 == stages ? 0 : st + 1, next_turn = next == 0 ? turn ^ 1 : turn;
+                    bool more = j + 1 < w.tiles;
+                    // the next tile's scores, should it land before this one's probabilities are there
+                    const unsigned long long t0 = global_timer_ns();
+                    for (int i = 1;; ++i) {
+                        if (more && __all_sync(0xffffffffu, mbar_test(smem_u32(&sh.full[next]), next_turn))) { scores(it + 1, next); more = false; }
+                        if (!more) { ok = wait(sh.p_full, it & 1); break; }
+                        if (__all_sync(0xffffffffu, mbar_test(smem_u32(&sh.p_full), it & 1))) break;
+                        if (i % 64 == 0 && __any_sync(0xffffffffu, global_timer_ns() - t0 > a.wait_ns)) { ok = wait(sh.p_full, it & 1); break; }
+                    }
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t from = base + st * stage_bytes;
+                        for (int mt = 0; mt < m_tiles; ++mt)
+#pragma unroll
+                            for (int k = 0; k < kLaTile / 16; ++k)
+                                tc_mma_f16(t_o + mt * N, smem_desc_sw128(from + mt * 2 * kLaChunkBytes + k * 2048, kLaChunkBytes, 1024),
+                                           smem_desc_sw128(p_at + k * 32, 16, 1024), idesc_o, j > 0 || k > 0);
+                        tc_commit(smem_u32(&sh.empty[st]));
+                    }
+                    __syncwarp();
+                    if (more) {
+                        if (!(ok = wait(sh.full[next], next_turn))) break;
+                        scores(it + 1, next);
+                    }
+                    st = next; turn = next_turn;
+                }
+                ++item;
+            }
+            if (ok) w.next(a);
+        }
+        if (any) {                               // products under way end before tensor memory is given back, whoever has given up
+            if (elect_one()) tc_commit(smem_u32(&sh.drained));
+            __syncwarp();
+            mbar_wait_bounded(smem_u32(&sh.drained), 0, 2'000'000'000ull);
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 5) tmem_dealloc(t_s, 512);
+}
+
+// Adds the parts of items that were cut between CTAs. A task is a column's 128 elements of one such item; its eight warps take the parts in
+// turn, all of one warp's in flight together, and add up in order.
+constexpr int kLaJoinThreads = 256, kLaJoinBlocks = 592;
+template <typename T, int COLS>
+__global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const LatentAttendArgs a, int ctas) {
+    using S = LaShape<T, COLS>;
+    __shared__ int owners[kLaMaxCtas], n_owners;
+    __shared__ float weight[kLaMaxCtas], norm;
+    __shared__ float4 sums[8][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    grid_dep_wait();
+    grid_dep_launch();
+    if (warp == 0) {
+        int count = 0;
+        for (int i = 0; i < ctas; i += 32) {
+            const bool is = i + lane < ctas && a.joins[i + lane].x > 0;
+            const uint32_t who = __ballot_sync(0xffffffffu, is);
+            if (is) owners[count + __popc(who & ((1u << lane) - 1))] = i + lane;
+            count += __popc(who);
+        }
+        if (lane == 0) n_owners = count;
+    }
+    __syncthreads();
+    const int latent = a.kv.latent, wide = latent / 128;
+    for (int task = blockIdx.x; task < n_owners * COLS * wide; task += gridDim.x) {
+        const int owner = owners[task / (COLS * wide)], col = task / wide % COLS, d0 = task % wide * 128;
+        const int4 join = a.joins[owner];
+        const LaSequence s = la_sequence<COLS>(a, join.y);
+        const int x = join.z * COLS + col, row_in = x / a.heads, h = x - row_in * a.heads, row = s.first + row_in;
+        if (row_in >= s.n || row < 0 || row >= a.batch.n_rows) continue;
+        // part 0 is the second slot of its CTA, the others are the first slots of theirs
+        const size_t each = S::part_floats(latent);
+        const float* parts = a.parts + size_t(owner) * 2 * each;
+        auto part = [&](int j) { return parts + (j == 0 ? 1 : 2 * j) * each; };
+        if (warp == 0) {
+            float top = -INFINITY, sum = 0.f;
+            for (int j = lane; j < join.x; j += 32) top = fmaxf(top, part(j)[COLS * latent + col]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            for (int j = lane; j < join.x; j += 32) {
+                const float m = part(j)[COLS * latent + col], by = m == -INFINITY ? 0.f : ex2(m - top);
+                weight[j] = by;
+                if (by != 0.f) sum += by * part(j)[COLS * latent + COLS + col];
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) norm = sum == 0.f ? 0.f : 1.f / sum;
+        }
+        __syncthreads();
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int j = warp; j < join.x; j += 8) {
+            const float by = weight[j];
+            if (by == 0.f) continue;             // (a part that saw nothing has written no sums)
+            const float4 v = *reinterpret_cast<const float4*>(part(j) + col * latent + d0 + lane * 4);
+            o.x += by * v.x; o.y += by * v.y; o.z += by * v.z; o.w += by * v.w;
+        }
+        sums[warp][lane] = o;
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+            for (int k = 1; k < 8; ++k) { const float4 v = sums[k][lane]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+            const float y[4] = {o.x * norm, o.y * norm, o.z * norm, o.w * norm};
+            store_row<4>(static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d0 + lane * 4, y);
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace spm

@@ -1,0 +1,201 @@
+// The entry points of attention over latent rows: checks of arguments, launches.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <string>
+
+#include <cuda_runtime.h>
+
+#include "head_product.cuh"
+#include "kv_checks.h"
+#include "latent_attend.cuh"
+#include "latent_write.cuh"
+#include "tma_maps.h"
+
+using namespace spm;
+
+namespace {
+
+constexpr int kMaxSmem = 232448;
+
+int check_latent_shape(const char* call, const spm_latent_cache* kv) {
+    if (!kv) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (kv->latent_dim < 128 || kv->latent_dim > 512 || kv->latent_dim % 128)
+        return fail(call, SPM_ERR_CONFIG, "latent_dim " + std::to_string(kv->latent_dim) + " not supported: 128, 256, 384 or 512");
+    if (kv->rope_dim < 16 || kv->rope_dim > 64 || kv->rope_dim % 16)
+        return fail(call, SPM_ERR_CONFIG, "rope_dim " + std::to_string(kv->rope_dim) + " not supported: 16, 32, 48 or 64");
+    if (kv->page_size < 16 || kv->page_size % 16 || kv->page_size > 65536)
+        return fail(call, SPM_ERR_CONFIG, "page_size " + std::to_string(kv->page_size) + " is not a multiple of 16 up to 65536");
+    if (kv->n_pages < 0) return fail(call, SPM_ERR_INVALID_ARG, "n_pages is negative");
+    if (static_cast<long long>(kv->n_pages) * kv->page_size > INT32_MAX) return fail(call, SPM_ERR_CONFIG, "n_pages * page_size is over 2^31 - 1 tokens");
+    return SPM_OK;
+}
+int check_latent_cache(const char* call, const spm_latent_cache* kv) {
+    if (int rc = check_latent_shape(call, kv)) return rc;
+    if (!kv->rows && kv->n_pages > 0) return fail(call, SPM_ERR_INVALID_ARG, "rows is null");
+    if (!aligned(kv->rows, 16) || !aligned(kv->status, 4))
+        return fail(call, SPM_ERR_INVALID_ARG, "rows must be 16-byte aligned, status 4-byte aligned");
+    return SPM_OK;
+}
+int check_heads(const char* call, int n) { return n >= 1 && n <= 1024 ? SPM_OK : fail(call, SPM_ERR_CONFIG, "heads outside 1..1024"); }
+
+LatentPool pool_of(const spm_latent_cache* kv) {
+    return {static_cast<__nv_bfloat16*>(kv->rows), kv->status, kv->n_pages, kv->page_size, kv->latent_dim, kv->rope_dim};
+}
+
+// ---- absorbed attention ----
+// Columns of a CTA: what a sequence has, in equal blocks of at most 64 (fp32, three parts each: 16). max_rows may be a guess: any choice is right.
+int columns_of(const spm_kv_batch* b, int n_heads, int dtype) {
+    if (dtype == SPM_DTYPE_FP32) return 16;
+    long long rows = 1;
+    if (b->row_start && b->n_seq > 0) rows = b->max_rows > 0 ? b->max_rows : (b->n_rows + b->n_seq - 1) / b->n_seq;
+    const long long columns = std::max(1ll, std::min<long long>(rows, b->n_rows) * n_heads), blocks = (columns + 63) / 64;
+    return int(((columns + blocks - 1) / blocks + 15) / 16 * 16);
+}
+constexpr size_t kLaJoinBytes = (kLaMaxCtas * sizeof(int4) + 255) / 256 * 256;
+size_t attend_bytes(int cols, int latent) { return kLaJoinBytes + kLaMaxCtas * 2 * size_t(cols) * (latent + 2) * sizeof(float); }
+
+template <typename T, int COLS>
+cudaError_t launch_attend(LatentAttendArgs a, const CUtensorMap& map, int dev, int sms, cudaStream_t st) {
+    using S = LaShape<T, COLS>;
+    cudaError_t e = allow_smem<latent_attend_kernel<T, COLS>>(dev, kMaxSmem);
+    if (e != cudaSuccess) return e;
+    const int fixed = kLaOwnBytes + S::fixed(a.chunks);
+    a.stages = std::min(kLaMaxStages, (kMaxSmem - fixed) / (a.chunks * kLaChunkBytes));
+    const int ctas = std::min(sms, kLaMaxCtas);
+    e = launch_early(latent_attend_kernel<T, COLS>, ctas, kLaThreads, la_smem(fixed, a.chunks, a.stages), st, a, map);
+    return e == cudaSuccess ? launch_early(latent_join_kernel<T, COLS>, kLaJoinBlocks, kLaJoinThreads, 0, st, a, ctas) : e;
+}
+
+template <typename T, bool TRANSPOSED>
+cudaError_t launch_product(const HeadProductArgs& a, int n_heads, cudaStream_t st) {
+    const auto grid = [&](int rows) { return dim3(unsigned((a.n_rows + rows - 1) / rows) * a.out_tiles, n_heads); };
+    if (a.n_rows <= 16) return launch_early(head_product_kernel<T, TRANSPOSED, 1>, grid(16), kHpWarps * 32, 0, st, a);
+    return launch_early(head_product_kernel<T, TRANSPOSED, 2>, grid(32), kHpWarps * 32, 0, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
+                     const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* latent, const spm_rows* key, int dtype, void* stream) {
+    const char* call = "spm_latent_write";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_latent_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
+    if (n_q_heads < 0 || n_q_heads > 1024) return fail(call, SPM_ERR_INVALID_ARG, "n_q_heads outside 0..1024");
+    if (q && !rope) return fail(call, SPM_ERR_INVALID_ARG, "q without rope: there is nothing to do to it");
+    if (rope && rope->q_gamma) return fail(call, SPM_ERR_INVALID_ARG, "q_gamma: queries have no norm here");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    if (rope)
+        if (int rc = check_rope(call, rope, positions, pos_stride, batch->n_rows, kv->rope_dim)) return rc;
+    if (int rc = check_rows(call, "latent", latent, dtype)) return rc;
+    if (int rc = check_rows(call, "key", key, dtype)) return rc;
+    if (q) {
+        if (int rc = check_rows(call, "q", q, dtype)) return rc;
+        if (int rc = check_rows(call, "q_out", q_out, dtype)) return rc;
+        if (q->p == q_out->p && other_strides(q, q_out)) return fail(call, SPM_ERR_INVALID_ARG, "q_out in q's place has other strides");
+    }
+    LatentWriteArgs a{};
+    a.kv = pool_of(kv);
+    a.batch = batch_of(batch);
+    if (rope) { a.rope = rope_of(rope, positions, pos_stride); a.turn = 1; }
+    if (q) { a.q = rows_of(q); a.q_out = rows_of(q_out); a.q_heads = n_q_heads; }
+    a.latent = rows_of(latent); a.key = rows_of(key);
+    a.n_rows = batch->n_rows;
+    // a row a warp, or where these are few its query heads shared out
+    constexpr int kWarps = 592 * kKvWarps;       // that the GPU has room for
+    const int parts = std::max(1, std::min((a.q_heads + 7) / 8, kWarps / a.n_rows));
+    const unsigned grid = unsigned((static_cast<long long>(a.n_rows) * parts + kKvWarps - 1) / kKvWarps);
+    const auto st = static_cast<cudaStream_t>(stream);
+    return launched(call, dtype == SPM_DTYPE_BF16 ? launch_early(latent_write_kernel<__nv_bfloat16>, grid, kKvWarps * 32, 0, st, a, parts)
+                                                  : launch_early(latent_write_kernel<float>, grid, kKvWarps * 32, 0, st, a, parts));
+}
+
+int spm_latent_attend_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int dtype, size_t* bytes) {
+    const char* call = "spm_latent_attend_workspace";
+    if (!bytes) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_latent_shape(call, kv)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
+    if (int rc = check_heads(call, n_heads)) return rc;
+    *bytes = attend_bytes(columns_of(batch, n_heads, dtype), kv->latent_dim);
+    return SPM_OK;
+}
+
+int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_heads, const spm_rows* out, float scale,
+                      int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* call = "spm_latent_attend";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_latent_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
+    if (int rc = check_heads(call, n_heads)) return rc;
+    const float factor = scale * 1.4426950408889634f;
+    if (!std::isfinite(factor)) return fail(call, SPM_ERR_INVALID_ARG, "scale is not finite, or not below 2^127");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    if (int rc = check_rows(call, "q", q, dtype)) return rc;
+    if (int rc = check_rows(call, "out", out, dtype)) return rc;
+    if (q->p == out->p) return fail(call, SPM_ERR_INVALID_ARG, "out is in the place of q, which is read until the end");
+    if (static_cast<long long>(batch->n_rows) * n_heads > INT32_MAX - 64) return fail(call, SPM_ERR_INVALID_ARG, "n_rows * n_heads is over 2^31 - 65");
+    const int cols = columns_of(batch, n_heads, dtype);
+    const size_t need = attend_bytes(cols, kv->latent_dim);
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
+        return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 16-byte aligned and hold " + std::to_string(need) + " bytes");
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return fail(call, SPM_ERR_CUDA, cudaGetErrorString(e));
+    if (dev < 0 || dev >= kMaxDevices) return fail(call, SPM_ERR_CONFIG, "device ordinal out of range");
+    LatentAttendArgs a{};
+    a.kv = pool_of(kv);
+    a.batch = batch_of(batch);
+    a.q = rows_of(q); a.out = rows_of(out);
+    a.heads = n_heads;
+    a.chunks = kv->latent_dim / 64 + 1;
+    a.box = kv->page_size % 64 == 0 ? 64 : kv->page_size % 32 == 0 ? 32 : 16;
+    a.factor = factor;
+    a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    a.withhold = g_withhold.load(std::memory_order_relaxed);
+    a.joins = static_cast<int4*>(workspace);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kLaJoinBytes);
+    CUtensorMap map{};                           // (a pool without pages: no copy is made)
+    if (kv->n_pages > 0 && !make_token_map(&map, kv->rows, kv->latent_dim + kv->rope_dim, uint64_t(kv->n_pages) * kv->page_size, a.box))
+        return fail(call, SPM_ERR_CUDA, "no tensor map of the cache's rows");
+    const auto st = static_cast<cudaStream_t>(stream);
+    if (dtype == SPM_DTYPE_FP32) e = launch_attend<float, 16>(a, map, dev, sms, st);
+    else if (cols == 16) e = launch_attend<__nv_bfloat16, 16>(a, map, dev, sms, st);
+    else if (cols == 32) e = launch_attend<__nv_bfloat16, 32>(a, map, dev, sms, st);
+    else if (cols == 48) e = launch_attend<__nv_bfloat16, 48>(a, map, dev, sms, st);
+    else e = launch_attend<__nv_bfloat16, 64>(a, map, dev, sms, st);
+    return launched(call, e);
+}
+
+int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, int64_t w_row_stride, int transposed, const spm_rows* y, int n_rows,
+                     int n_heads, int in_dim, int out_dim, int dtype, void* stream) {
+    const char* call = "spm_head_product";
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (int rc = check_heads(call, n_heads)) return rc;
+    if (in_dim < 64 || in_dim > 8192 || in_dim % 64 || out_dim < 64 || out_dim > 8192 || out_dim % 64)
+        return fail(call, SPM_ERR_CONFIG, "in_dim and out_dim are multiples of 64 up to 8192");
+    if (n_rows < 0) return fail(call, SPM_ERR_INVALID_ARG, "a negative size");
+    if (n_rows > INT32_MAX / 128 - 32) return fail(call, SPM_ERR_INVALID_ARG, "too many rows");          // (tiles of rows times tiles of outputs are a number)
+    if (n_rows == 0) return SPM_OK;
+    if (int rc = check_rows(call, "x", x, dtype)) return rc;
+    if (int rc = check_rows(call, "y", y, dtype)) return rc;
+    if (x->p == y->p) return fail(call, SPM_ERR_INVALID_ARG, "y is in the place of x, which is read until the end");
+    if (!w || !aligned(w, 16) || w_head_stride % 8 || w_row_stride % 8)
+        return fail(call, SPM_ERR_INVALID_ARG, "w: rows of weights must start on 16-byte boundaries");
+    HeadProductArgs a{};
+    a.x = rows_of(x); a.y = rows_of(y);
+    a.w = static_cast<const __nv_bfloat16*>(w);
+    a.w_head = w_head_stride; a.w_row = w_row_stride;
+    a.n_rows = n_rows; a.in = in_dim; a.out_tiles = out_dim / kHpOut;
+    const auto st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (dtype == SPM_DTYPE_BF16) e = transposed ? launch_product<__nv_bfloat16, true>(a, n_heads, st) : launch_product<__nv_bfloat16, false>(a, n_heads, st);
+    else e = transposed ? launch_product<float, true>(a, n_heads, st) : launch_product<float, false>(a, n_heads, st);
+    return launched(call, e);
+}
+
+}  // extern "C"
