@@ -53,7 +53,7 @@ __device__ __forceinline__ void pairs_of(const __nv_bfloat16* p, bool there, uin
 
 // TRANSPOSED: W is [out][in], else [in][out]
 template <typename T, bool TRANSPOSED, int MT>
-__global__ void __launch_bounds__(kHpWarps * 32) head_product_kernel(const HeadProductArgs a) {
+__global__ void __launch_bounds__(kHpWarps * 32, MT == 1 ? 2 : 1) head_product_kernel(const HeadProductArgs a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     constexpr int STEP = TRANSPOSED ? 32 : 16;               // contracted elements of a step
     __shared__ float sums[kHpWarps / 2][MT * 16][kHpOut];

@@ -33,15 +33,20 @@ struct LatentAttendArgs {
     LatentPool kv;
     KvBatch batch;
     HeadRows q, out;
-    int heads;
+    int heads, heads_shift;     // x / heads is x * heads_times >> heads_shift for x below 2^31
+    uint32_t heads_times;
     int chunks, stages;         // 64-element chunks of a row, tiles of the ring
     int box;                    // tokens of a copy: 16, 32 or 64, all of one page
     float factor;               // of scores: scale times log2(e)
     float* parts;               // [2 * CTAs][LaPart floats]
-    int4* joins;                // [CTAs], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), sequence, block of columns
+    int4* joins;                // [CTAs], of the item that begins in this CTA and goes on behind it: CTAs that share it (0: none), its
+                                // sequence's first row and rows, block of columns
     unsigned long long wait_ns; // a wait in a kernel gives up after this long
     int withhold;               // (tests) arrivals that barriers wait for and nobody makes
 };
+
+// Row of column x
+__device__ __forceinline__ int la_row(const LatentAttendArgs& a, int x) { return int(static_cast<unsigned long long>(uint32_t(x)) * a.heads_times >> a.heads_shift); }
 
 constexpr int kLaTile = 64, kLaMaxCtas = 148, kLaMaxStages = 8, kLaThreads = 192;
 constexpr int kLaChunkBytes = kLaTile * 128;
@@ -60,17 +65,6 @@ struct LaShape {
 constexpr int kLaOwnBytes = 2048;                            // LaShared below
 constexpr int la_smem(int fixed, int chunks, int stages) { return fixed + chunks * stages * kLaChunkBytes; }
 
-struct LaShared {
-    unsigned long long full[kLaMaxStages], empty[kLaMaxStages], s_full[2], p_full, q_full, drained;
-    uint32_t tmem;
-    int quit;                                                // a wait has run out: everybody leaves
-    int ctas;                                                // that have a piece
-    int seq, group, tile;                                    // where this CTA's piece of the line begins
-    long long left, all, at;                                 // its tiles, all tiles, its first one
-    int absent[kLaMaxStages];                                // a tile's copies (`box` tokens each) that there are not
-    int limit[2][64];                                        // tokens that a column sees; of one item and the next
-};
-static_assert(sizeof(LaShared) <= kLaOwnBytes, "what shared memory has beside the ring");
 
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int element, int row, uint32_t bar) {
     asm volatile(
@@ -92,10 +86,26 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
 __host__ __device__ constexpr uint32_t la_idesc(int m, int n, bool a_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(a_mn_major) << 15) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
 }
+// D[tmem] (+)= A * B by the descriptors' words
+template <bool MORE>
+__device__ __forceinline__ void tc_mma_lo(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        ".reg .b64 x, y;\n\t"
+        "mov.b64 x, {%1, %2};\n\t"
+        "mov.b64 y, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %5, p;\n\t"
+        "}\n"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "n"(int(MORE)) : "memory");
+}
 // 16 lanes, 16 columns, in the layout of mma.sync's accumulators: r[4 i + 2 h + e] is row lane / 4 + 8 h, column 8 i + 2 (lane % 4) + e
 __device__ __forceinline__ void tmem_ld_frag(uint32_t at, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : SPM_R8(r, 0) : "r"(at) : "memory");
 }
+// a word of two bf16 numbers, one of them not finite
+__device__ __forceinline__ bool odd_word(uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; }
 // four 8 x 8 matrices, each stored by columns
 __device__ __forceinline__ void st_matrix_trans(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -103,6 +113,21 @@ __device__ __forceinline__ void st_matrix_trans(uint32_t at, uint32_t a, uint32_
 
 // A sequence's items on the line: blocks of columns, tiles of each (one at least, so that rows that see nothing are written too)
 struct LaSequence { int first, n, len, cap_len, blocks, tiles; };
+// An item counts so many tiles more than it has: what its queries and its result cost beside them
+template <int COLS> constexpr int kLaItemCost = 1 + COLS / 16;
+struct LaShared {
+    unsigned long long full[kLaMaxStages], empty[kLaMaxStages], s_full[2], p_full, q_full, drained;
+    uint32_t tmem;
+    int quit;                                                // a wait has run out: everybody leaves
+    int ctas;                                                // that have a piece
+    int seq, group, tile;                                    // where this CTA's piece of the line begins
+    LaSequence first;                                        // that sequence
+    long long left, all, at;                                 // its tiles, all tiles, its first one
+    int absent[kLaMaxStages];                                // a tile's copies (`box` tokens each) that there are not
+    int limit[2][64];                                        // tokens that a column sees; of one item and the next
+};
+static_assert(sizeof(LaShared) <= kLaOwnBytes, "what shared memory has beside the ring");
+
 template <int COLS>
 __device__ __forceinline__ LaSequence la_sequence(const LatentAttendArgs& a, int s) {
     LaSequence q;
@@ -119,26 +144,31 @@ __device__ __forceinline__ LaSequence la_sequence(const LatentAttendArgs& a, int
     return q;
 }
 
-// A CTA's walk over its items. `tiles`: those of [from, to) in which the item's columns see a token.
+// A CTA's walk over its items. [begin, end): its units of the item's cost; from: its first tile; tiles: how many of its tiles the item's
+// columns see a token in.
 template <int COLS>
 struct LaWalk {
+    static constexpr int kCost = kLaItemCost<COLS>;
     LaSequence s;
-    int seq, group, from, to, sees, tiles;
+    int seq, group, begin, end, from, sees, tiles;
     long long left;
     __device__ __forceinline__ void start(const LatentAttendArgs& a, const LaShared& sh) {
-        seq = sh.seq; group = sh.group; from = sh.tile; left = sh.left;
-        if (left > 0) { s = la_sequence<COLS>(a, seq); piece(a); }
+        seq = sh.seq; group = sh.group; begin = sh.tile; left = sh.left;
+        if (left > 0) { s = sh.first; piece(a); }
     }
     __device__ __forceinline__ void piece(const LatentAttendArgs& a) {
-        to = int(min(static_cast<long long>(s.tiles), from + left));
-        const int last = min(s.n - 1, ((group + 1) * COLS - 1) / a.heads);
+        end = int(min(static_cast<long long>(s.tiles + kCost), begin + left));
+        from = max(0, begin - kCost);
+        const int last = min(s.n - 1, la_row(a, (group + 1) * COLS - 1));
         sees = max(0, min(s.len - s.n + last + 1, s.cap_len));
-        tiles = max(0, min(to, (sees + kLaTile - 1) / kLaTile) - from);
+        tiles = max(0, min(end - kCost, (sees + kLaTile - 1) / kLaTile) - from);
     }
+    __device__ __forceinline__ bool begins() const { return begin == 0; }
+    __device__ __forceinline__ bool ends() const { return end == s.tiles + kCost; }
     __device__ __forceinline__ void next(const LatentAttendArgs& a) {
-        left -= to - from;
+        left -= end - begin;
         if (left <= 0) return;
-        from = 0;
+        begin = 0;
         if (++group >= s.blocks) {
             group = 0;
             do {
@@ -162,6 +192,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     const uint32_t stage_bytes = chunks * kLaChunkBytes, q_at = base + stages * stage_bytes, p_at = q_at + S::q_bytes(chunks);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
+    if (tid == 128) asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
     grid_dep_wait();
     grid_dep_launch();
     if (tid == 0) {
@@ -178,9 +209,10 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         // ---- this CTA's piece of the line: a lane counts sequences side by side ----
         const int each = (a.batch.n_seq + 31) / 32, s0 = lane * each, s1 = min(s0 + each, a.batch.n_seq);
         long long mine = 0;
+        LaSequence q{};                          // (up to 32 sequences: loaded once)
         for (int s = s0; s < s1; ++s) {
-            const LaSequence q = la_sequence<COLS>(a, s);
-            mine += static_cast<long long>(q.blocks) * q.tiles;
+            q = la_sequence<COLS>(a, s);
+            mine += static_cast<long long>(q.blocks) * (q.tiles + kLaItemCost<COLS>);
             if (q.n > 0 && q.len > q.cap_len && blockIdx.x == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
         }
         long long upto = mine;
@@ -192,17 +224,21 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         const long long all = __shfl_sync(0xffffffffu, upto, 31);
         // (no more CTAs than tiles: those that share an item are neighbours)
         const long long ctas = max(1ll, min(all, static_cast<long long>(gridDim.x))), cta = min(static_cast<long long>(blockIdx.x), ctas);
-        const long long at = all * cta / ctas, end = cta < ctas ? all * (cta + 1) / ctas : at;
+        const bool narrow = all < 1 << 24;       // (divisions of 64 bits are slow)
+        const long long at = narrow ? uint32_t(all * cta) / uint32_t(ctas) : all * cta / ctas;
+        const long long end = cta == ctas ? at : narrow ? uint32_t(all * (cta + 1)) / uint32_t(ctas) : all * (cta + 1) / ctas;
         if (lane == 0) { sh.left = end - at; sh.all = all; sh.at = at; sh.ctas = int(ctas); }
         long long rest = at - (upto - mine);
         if (end > at && rest >= 0 && rest < mine)
             for (int s = s0; s < s1; ++s) {
-                const LaSequence q = la_sequence<COLS>(a, s);
-                const long long own = static_cast<long long>(q.blocks) * q.tiles;
+                if (each > 1) q = la_sequence<COLS>(a, s);
+                const int cost = q.tiles + kLaItemCost<COLS>;
+                const long long own = static_cast<long long>(q.blocks) * cost;
                 if (rest < own) {
                     sh.seq = s;
-                    sh.group = int(rest / q.tiles);
-                    sh.tile = int(rest % q.tiles);
+                    sh.first = q;
+                    sh.group = narrow ? int(uint32_t(rest) / uint32_t(cost)) : int(rest / cost);
+                    sh.tile = int(rest - static_cast<long long>(sh.group) * cost);
                     break;
                 }
                 rest -= own;
@@ -246,57 +282,69 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                          : "=r"(any) : "r"(int(yes)) : "memory");
             return any != 0;
         };
+        // This item's queries, a warp every fourth column, all of a warp's loads in flight together
+        const int vectors = (latent + a.kv.rope) / 8;
+        auto bring_queries = [&](int half) {
+            auto column = [&](int col, const T*& from) {
+                const int x = w.group * COLS + col, i = la_row(a, x), row = w.s.first + i;
+                const bool is = i < w.s.n && row >= 0 && row < a.batch.n_rows;
+                from = static_cast<const T*>(a.q.p) + (is ? row * a.q.row + (x - i * a.heads) * a.q.head : 0);
+                if (lane == 0) sh.limit[half][col] = is ? max(0, min(w.s.len - w.s.n + i + 1, w.s.cap_len)) : 0;
+                return is;
+            };
+            // unit lane + 32 k of column `col`
+            auto place = [&](int col, int k) { return (q_at + (4 * k + (lane >> 3)) * (N * 128) + col * 128) ^ (((lane ^ col) & 7) << 4); };
+            if constexpr (PARTS == 1) {
+#pragma unroll 4
+                for (int col = warp; col < COLS; col += 4) {
+                    const T* from;
+                    const bool is = column(col, from);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (k * 32 + lane < vectors) copy16_or_zero(place(col, k), from + (is ? (k * 32 + lane) * 8 : 0), is);
+                }
+                copies_arrived();
+            } else {
+                Raw8 v[COLS / 4][3];
+#pragma unroll
+                for (int c = 0; c < COLS / 4; ++c) {
+                    const T* from;
+                    const bool is = column(4 * c + warp, from);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) v[c][k] = is && k * 32 + lane < vectors ? raw8(from + (k * 32 + lane) * 8) : Raw8{};
+                }
+#pragma unroll
+                for (int c = 0; c < COLS / 4; ++c) {
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        if (k * 32 + lane >= vectors) continue;
+                        float f[8];
+                        unpack8<T>(v[c][k], f);
+                        uint32_t p[4][3];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) cut_parts(f[2 * u], f[2 * u + 1], p[u]);
+#pragma unroll
+                        for (int u = 0; u < 3; ++u)
+                            st_shared16(place(4 * c + warp, k) + u * (COLS * 128), make_uint4(p[0][u], p[1][u], p[2][u], p[3][u]));
+                    }
+                }
+            }
+        };
         float* red = reinterpret_cast<float*>(raw_smem + (p_at - smem_u32(raw_smem)));       // [4 warps][COLS], in the probabilities' place
         while (w.left > 0 && ok) {
             const int half = item & 1;
             // ---- this item's columns: a warp brings every fourth ----
             if (w.tiles > 0) {
-#pragma unroll 4
-                for (int col = warp; col < COLS; col += 4) {
-                    const int x = w.group * COLS + col, i = x / a.heads, h = x - i * a.heads, row = w.s.first + i;
-                    const bool is = i < w.s.n && row >= 0 && row < a.batch.n_rows;
-                    const T* from = static_cast<const T*>(a.q.p) + row * a.q.row + h * a.q.head;
-                    const int vectors = (latent + a.kv.rope) / 8;
-                    Raw8 v[3] = {};
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (is && k * 32 + lane < vectors) v[k] = raw8(from + (k * 32 + lane) * 8);
-                    bool odd = false;
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        float f[8];
-                        unpack8<T>(v[k], f);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) odd |= !(fabsf(f[e]) < INFINITY);
-                    }
-                    // (infinite scores could all be -infinity, as those of tokens that it does not see are: NaN as a whole)
-                    const uint32_t nan = __any_sync(0xffffffffu, odd) ? 0x7fff7fffu : 0u;
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        const int e = k * 32 + lane;
-                        if (e >= vectors) continue;
-                        const uint32_t to = q_at + (e >> 3) * (N * 128) + col * 128 + (((e & 7) ^ (col & 7)) << 4);
-                        if constexpr (PARTS == 1) st_shared16(to, make_uint4(v[k].a.x | nan, v[k].a.y | nan, v[k].a.z | nan, v[k].a.w | nan));
-                        else {
-                            float f[8];
-                            unpack8<T>(v[k], f);
-                            uint32_t p[4][3];
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) cut_parts(f[2 * u], f[2 * u + 1], p[u]);
-#pragma unroll
-                            for (int u = 0; u < 3; ++u) st_shared16(to + u * (COLS * 128), make_uint4(p[0][u] | nan, p[1][u] | nan, p[2][u] | nan, p[3][u] | nan));
-                        }
-                    }
-                    if (lane == 0) sh.limit[half][col] = is ? max(0, min(w.s.len - w.s.n + i + 1, w.s.cap_len)) : 0;
-                }
+                bring_queries(half);
                 fence_proxy_async();
                 mbar_arrive(smem_u32(&sh.q_full));
             }
+            bool first = true;                   // no token so far
             float m[BLOCKS][2], l[BLOCKS][2] = {};
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) m[i][0] = m[i][1] = 0.f;
             // tokens that all columns see: behind them are masks to look at
-            const int all_see = w.s.n == 1 ? w.sees : max(0, min(w.s.len - w.s.n + w.group * COLS / a.heads + 1, w.s.cap_len));
+            const int all_see = w.s.n == 1 ? w.sees : max(0, min(w.s.len - w.s.n + la_row(a, w.group * COLS) + 1, w.s.cap_len));
             for (int j = 0; j < w.tiles; ++j, ++it) {
                 const int t0 = (w.from + j) * kLaTile;
                 // (a warp that gives up still comes to the others' barriers; they leave together)
@@ -327,7 +375,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                 };
                 // the sums of the tile before are done (and the item before's, at its end): P and O may be touched
                 auto sums_done = [&] { ok = ok && (j == 0 || wait(sh.empty[(st == 0 ? stages : st) - 1], st == 0 ? turn ^ 1 : turn)); };
-                if (vote(highest() > kLaSlack || j == 0 || masks || !ok)) {
+                if (vote(highest() > kLaSlack || first || masks || !ok)) {
                     if (vote(!ok)) { ok = false; break; }
                     sums_done();
                     if (masks) {
@@ -346,7 +394,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                                 const uint4 v = lds128(at + (u >> 3) * kLaChunkBytes + (((u & 7) ^ (t & 7)) << 4));
                                 const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) bad |= (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
+                                for (int k = 0; k < 4; ++k) bad |= odd_word(x[k]);
                             }
                         const bool either = __shfl_xor_sync(0xffffffffu, bad, 1) | bad;
                         if (!there || either)
@@ -367,7 +415,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                                 }
                         }
                     }
-                    if (vote(highest() > kLaSlack || j == 0)) {
+                    if (vote(highest() > kLaSlack || first)) {
                         tc_fence_after();
 #pragma unroll
                         for (int i = 0; i < BLOCKS; ++i)
@@ -386,16 +434,18 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             for (int e = 0; e < 2; ++e) {
                                 const int col = 8 * i + c2 + e;
                                 float top = fmaxf(fmaxf(red[col], red[COLS + col]), fmaxf(red[2 * COLS + col], red[3 * COLS + col]));
+                                // (a query with an infinity may have no other scores than -infinity, as of tokens that it does not see: NaN)
+                                if (first && top == -INFINITY && t0 + (__ffs(~absent) - 1) * a.box < sh.limit[half][col]) l[i][e] = __int_as_float(0x7fffffff);
                                 // (nothing seen: stays. Only the first tile's may be below zero)
-                                if (top == -INFINITY || (j > 0 && top < 0.f)) top = 0.f;
+                                if (top == -INFINITY || (!first && top < 0.f)) top = 0.f;
                                 m[i][e] += top;
-                                by[i][e] = j > 0 ? ex2(-top) : 0.f;
+                                by[i][e] = first ? 1.f : ex2(-top);
                                 l[i][e] *= by[i][e];
                                 s[i][e] -= top;
                                 s[i][e + 2] -= top;
                             }
                         together();
-                        if (j > 0) {                 // seldom: the sums so far go down
+                        if (!first) {                // seldom: the sums so far go down
                             if (warp == 0 && lane < 4)
 #pragma unroll
                                 for (int i = 0; i < BLOCKS; ++i) { red[8 * i + c2] = by[i][0]; red[8 * i + c2 + 1] = by[i][1]; }
@@ -415,6 +465,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             tmem_wait_st();
                             together();
                         }
+                        first &= absent == (1 << kLaTile / a.box) - 1;
                     }
                 } else sums_done();
 #pragma unroll
@@ -444,7 +495,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                 if (++st == stages) { st = 0; turn ^= 1; }
             }
             // ---- the item's result, or this CTA's part of it ----
-            const bool whole = w.from == 0 && w.to == w.s.tiles;
+            const bool whole = w.begins() && w.ends();
             if (w.tiles > 0) {
                 ok = ok && wait(sh.empty[(st == 0 ? stages : st) - 1], st == 0 ? turn ^ 1 : turn);
                 if (vote(!ok)) { ok = false; break; }
@@ -459,7 +510,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     }
                 together();
             }
-            float* part = a.parts + (size_t(blockIdx.x) * 2 + (w.from == 0)) * S::part_floats(latent);       // slot 0: an item that began before this CTA
+            float* part = a.parts + (size_t(blockIdx.x) * 2 + w.begins()) * S::part_floats(latent);       // slot 0: an item that began before this CTA
             float total = 0.f;
             if (w.tiles > 0 && tid < COLS) total = red[tid] + red[COLS + tid] + red[2 * COLS + tid] + red[3 * COLS + tid];
             together();
@@ -475,6 +526,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                 }
             } else if (tid < COLS) red[tid] = total == 0.f ? 0.f : 1.f / total;
             together();
+            // a part: four columns of an element side by side, elements behind each other
             if (w.tiles > 0 || whole) {
 #pragma unroll 1
                 for (int ch = 0; ch < COLS / 16; ++ch)
@@ -488,18 +540,26 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             tmem_wait_ld();
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int col = ch * 16 + i;
-                            float v = __uint_as_float(o[0][i]);
-                            if constexpr (PARTS == 3) v = v + __uint_as_float(o[1][i]) + __uint_as_float(o[2][i]);
-                            if (whole) {
-                                const int x = w.group * COLS + col, row_in = x / a.heads, h = x - row_in * a.heads, row = w.s.first + row_in;
+                        for (int i = 0; i < 16; i += 4) {
+                            float v[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                v[k] = __uint_as_float(o[0][i + k]);
+                                if constexpr (PARTS == 3) v[k] = v[k] + __uint_as_float(o[1][i + k]) + __uint_as_float(o[2][i + k]);
+                            }
+                            if (!whole) {
+                                *reinterpret_cast<float4*>(part + ((mt * (COLS / 4) + ch * 4 + i / 4) * 128 + tid) * 4) = make_float4(v[0], v[1], v[2], v[3]);
+                                continue;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int col = ch * 16 + i + k, x = w.group * COLS + col, row_in = la_row(a, x), h = x - row_in * a.heads, row = w.s.first + row_in;
                                 if (row_in >= w.s.n || row < 0 || row >= a.batch.n_rows) continue;
                                 T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d;
-                                v *= red[col];
-                                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(v);
-                                else *to = v;
-                            } else part[col * latent + d] = v;
+                                const float y = v[k] * red[col];
+                                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(y);
+                                else *to = y;
+                            }
                         }
                     }
             }
@@ -513,38 +573,47 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         int st = 0, turn = 0;
         unsigned it = 0;
         int4 join = make_int4(0, 0, 0, 0);
+        long long joined = 0;
         while (w.left > 0 && ok) {
-            if (w.from == 0 && w.to < w.s.tiles) {           // begins here and goes on: up to the CTA that has its last tile
-                const long long end = sh.at + (sh.left - w.left) + w.s.tiles;
-                join = make_int4(int((end * sh.ctas - 1) / sh.all) - int(blockIdx.x) + 1, w.seq, w.group, 0);
+            if (w.begins() && !w.ends()) {       // goes on behind this CTA, up to there
+                joined = sh.at + (sh.left - w.left) + w.s.tiles + w.kCost;
+                join = make_int4(0, w.s.first, w.s.n, w.group);
             }
-            const int copies = kLaTile / a.box;
-            auto row_of = [&](int j) {           // of this lane's copy in the pool; -1: there is none, -2: nobody sees it
-                const int token = (w.from + j) * kLaTile + lane * a.box;
-                return lane < copies && j < w.tiles && token < w.sees ? latent_row_at(a.kv, a.batch, w.seq, token, true) : -2ll;
+            // pages are asked for two tiles ahead, and looked at one tile ahead
+            const int copies = kLaTile / a.box, copy = lane & (copies - 1);
+            const int* table = a.batch.table + size_t(w.seq) * a.batch.stride;
+            auto token_of = [&](int j) { return (w.from + j) * kLaTile + copy * a.box; };
+            auto page_of = [&](int j) { return j < w.tiles && token_of(j) < w.sees ? table[token_of(j) / a.kv.page_size] : -1; };
+            auto row_of = [&](int j, int page) { // of this lane's copy in the pool; -1: there is none, or nobody sees it
+                if (page >= 0 && page < a.kv.n_pages) return page * a.kv.page_size + token_of(j) % a.kv.page_size;
+                if (j < w.tiles && token_of(j) < w.sees) kv_note(a.kv, SPM_KV_BAD_PAGE);
+                return -1;
             };
-            long long row = row_of(0);
+            const int first_page = page_of(0);
+            int page = page_of(1), row = row_of(0, first_page);
             for (int j = 0; j < w.tiles; ++j, ++it) {
-                const long long row_then = row_of(j + 1);
+                const int page_then = page_of(j + 2);
                 if (it >= unsigned(stages) && !(ok = wait(sh.empty[st], turn ^ 1))) break;
-                const uint32_t there = __ballot_sync(0xffffffffu, row >= 0);
-                const uint32_t bar = smem_u32(&sh.full[st]);
+                const uint32_t there = __ballot_sync(0xffffffffu, row >= 0) & ((1u << copies) - 1);
+                const uint32_t bar = smem_u32(&sh.full[st]), to = base + st * stage_bytes;
                 if (lane == 0) {
                     sh.absent[st] = int(~there & ((1u << copies) - 1));
                     mbar_arrive_expect_tx(bar, __popc(there) * a.box * 128 * chunks);
                 }
                 __syncwarp();
-                if (row >= 0)
-                    for (int c = 0; c < chunks; ++c)
-                        tma_rows(base + st * stage_bytes + c * kLaChunkBytes + lane * a.box * 128, &rows_map, c * 64, int(row), bar);
+                if (row >= 0)                    // (a lane's copy is the same in each round)
+                    for (int k = lane; k < copies * chunks; k += 32)
+                        tma_rows(to + k / copies * kLaChunkBytes + copy * a.box * 128, &rows_map, k / copies * 64, row, bar);
                 __syncwarp();
-                row = row_then;
+                row = row_of(j + 1, page);
+                page = page_then;
                 if (++st == stages) { st = 0; turn ^= 1; }
             }
             if (ok) w.next(a);
         }
         // copies under way end before shared memory is given back, whoever has given up
         for (unsigned k = it > unsigned(stages) ? it - stages : 0; k < it; ++k) mbar_wait_bounded(smem_u32(&sh.full[k % stages]), (k / stages) & 1, a.wait_ns);
+        if (joined > 0) join.x = int((joined * sh.ctas - 1) / sh.all) - int(blockIdx.x) + 1;             // up to the CTA that has its last tile
         if (lane == 0) a.joins[blockIdx.x] = join;
         __syncwarp();
     } else {
@@ -554,19 +623,50 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         int st = 0, turn = 0, item = 0;
         unsigned it = 0;
         bool any = false;
+        // Descriptors differ in their address alone, the low word. One instruction or two a product, or the issuing thread is slower than they are
+        const uint64_t rows_k = smem_desc_sw128(base, 16, 1024), rows_m = smem_desc_sw128(base, kLaChunkBytes, 1024);
+        const uint64_t q_k = smem_desc_sw128(q_at, 16, 1024), p_k = smem_desc_sw128(p_at, 16, 1024);
+        const uint32_t hi_k = uint32_t(rows_k >> 32), hi_m = uint32_t(rows_m >> 32), lo_p = uint32_t(p_k);
         auto scores = [&](unsigned tile, int stage) {
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t d = t_s + (tile & 1) * N, from = base + stage * stage_bytes;
-                for (int c = 0; c < chunks; ++c) {
-                    const int steps = c + 1 < chunks ? 4 : rope_steps;
-                    for (int k = 0; k < steps; ++k)
-                        tc_mma_f16(d, smem_desc_sw128(from + c * kLaChunkBytes + k * 32, 16, 1024), smem_desc_sw128(q_at + c * (N * 128) + k * 32, 16, 1024),
-                                   idesc_s, c + k > 0);
+                const uint32_t d = t_s + (tile & 1) * N;
+                uint32_t lo_a = uint32_t(rows_k) + stage * (stage_bytes >> 4), lo_b = uint32_t(q_k);
+                tc_mma_lo<false>(d, lo_a, hi_k, lo_b, hi_k, idesc_s);
+                tc_mma_lo<true>(d, lo_a + 2, hi_k, lo_b + 2, hi_k, idesc_s);
+                tc_mma_lo<true>(d, lo_a + 4, hi_k, lo_b + 4, hi_k, idesc_s);
+                tc_mma_lo<true>(d, lo_a + 6, hi_k, lo_b + 6, hi_k, idesc_s);
+#pragma unroll 2
+                for (int c = 2; c < chunks; ++c) {
+                    lo_a += kLaChunkBytes >> 4;
+                    lo_b += N * 8;
+                    tc_mma_lo<true>(d, lo_a, hi_k, lo_b, hi_k, idesc_s);
+                    tc_mma_lo<true>(d, lo_a + 2, hi_k, lo_b + 2, hi_k, idesc_s);
+                    tc_mma_lo<true>(d, lo_a + 4, hi_k, lo_b + 4, hi_k, idesc_s);
+                    tc_mma_lo<true>(d, lo_a + 6, hi_k, lo_b + 6, hi_k, idesc_s);
                 }
+                lo_a += kLaChunkBytes >> 4;
+                lo_b += N * 8;
+                for (int k = 0; k < rope_steps; ++k) tc_mma_lo<true>(d, lo_a + 2 * k, hi_k, lo_b + 2 * k, hi_k, idesc_s);
                 tc_commit(smem_u32(&sh.s_full[tile & 1]));
             }
             any = true;
+            __syncwarp();
+        };
+        auto sums = [&](int stage, bool more) {
+            if (elect_one()) {
+                uint32_t lo_a = uint32_t(rows_m) + stage * (stage_bytes >> 4), d = t_o;
+                for (int mt = 0; mt < m_tiles; ++mt) {
+                    if (more) tc_mma_lo<true>(d, lo_a, hi_m, lo_p, hi_k, idesc_o);
+                    else tc_mma_lo<false>(d, lo_a, hi_m, lo_p, hi_k, idesc_o);
+                    tc_mma_lo<true>(d, lo_a + 128, hi_m, lo_p + 2, hi_k, idesc_o);
+                    tc_mma_lo<true>(d, lo_a + 256, hi_m, lo_p + 4, hi_k, idesc_o);
+                    tc_mma_lo<true>(d, lo_a + 384, hi_m, lo_p + 6, hi_k, idesc_o);
+                    lo_a += 2 * kLaChunkBytes >> 4;
+                    d += N;
+                }
+                tc_commit(smem_u32(&sh.empty[stage]));
+            }
             __syncwarp();
         };
         while (w.left > 0 && ok) {
@@ -587,16 +687,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     }
                     if (!ok) break;
                     tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t from = base + st * stage_bytes;
-                        for (int mt = 0; mt < m_tiles; ++mt)
-#pragma unroll
-                            for (int k = 0; k < kLaTile / 16; ++k)
-                                tc_mma_f16(t_o + mt * N, smem_desc_sw128(from + mt * 2 * kLaChunkBytes + k * 2048, kLaChunkBytes, 1024),
-                                           smem_desc_sw128(p_at + k * 32, 16, 1024), idesc_o, j > 0 || k > 0);
-                        tc_commit(smem_u32(&sh.empty[st]));
-                    }
-                    __syncwarp();
+                    sums(st, j > 0);
                     if (more) {
                         if (!(ok = wait(sh.full[next], next_turn))) break;
                         scores(it + 1, next);
@@ -620,21 +711,23 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     if (warp == 5) tmem_dealloc(t_s, 512);
 }
 
-// Adds the parts of items that were cut between CTAs. A task is a column's 128 elements of one such item; its eight warps take the parts in
-// turn, all of one warp's in flight together, and add up in order.
+// Adds the parts of items that were cut between CTAs. A task is four columns' 32 elements of one such item, a warp's; where these are so few
+// that the parts of each are many, a block's, whose eight warps take the parts in turn. Parts are added in the same order each time.
 constexpr int kLaJoinThreads = 256, kLaJoinBlocks = 592;
 template <typename T, int COLS>
 __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const LatentAttendArgs a, int ctas) {
     using S = LaShape<T, COLS>;
+    constexpr int WARPS = kLaJoinThreads / 32;
     __shared__ int owners[kLaMaxCtas], n_owners;
-    __shared__ float weight[kLaMaxCtas], norm;
-    __shared__ float4 sums[8][32];
+    __shared__ __align__(16) float weights[WARPS][kLaMaxCtas][4];
+    __shared__ float4 sums[WARPS][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dep_wait();
     grid_dep_launch();
     if (warp == 0) {
         int count = 0;
-        for (int i = 0; i < ctas; i += 32) {
+#pragma unroll
+        for (int i = 0; i < kLaMaxCtas; i += 32) {
             const bool is = i + lane < ctas && a.joins[i + lane].x > 0;
             const uint32_t who = __ballot_sync(0xffffffffu, is);
             if (is) owners[count + __popc(who & ((1u << lane) - 1))] = i + lane;
@@ -643,48 +736,70 @@ __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const Laten
         if (lane == 0) n_owners = count;
     }
     __syncthreads();
-    const int latent = a.kv.latent, wide = latent / 128;
-    for (int task = blockIdx.x; task < n_owners * COLS * wide; task += gridDim.x) {
-        const int owner = owners[task / (COLS * wide)], col = task / wide % COLS, d0 = task % wide * 128;
+    const int latent = a.kv.latent, each_item = COLS / 4 * (latent / 32), tasks = n_owners * each_item;
+    const bool together = tasks <= int(gridDim.x);           // a block a task
+    const int step = together ? WARPS : 1;
+    for (int task = together ? blockIdx.x : blockIdx.x * WARPS + warp; task < tasks; task += gridDim.x * (WARPS / step)) {
+        const int owner = owners[task / each_item], in = task % each_item, quad = in / (latent / 32), d = in % (latent / 32) * 32 + lane;
         const int4 join = a.joins[owner];
-        const LaSequence s = la_sequence<COLS>(a, join.y);
-        const int x = join.z * COLS + col, row_in = x / a.heads, h = x - row_in * a.heads, row = s.first + row_in;
-        if (row_in >= s.n || row < 0 || row >= a.batch.n_rows) continue;
         // part 0 is the second slot of its CTA, the others are the first slots of theirs
         const size_t each = S::part_floats(latent);
         const float* parts = a.parts + size_t(owner) * 2 * each;
         auto part = [&](int j) { return parts + (j == 0 ? 1 : 2 * j) * each; };
-        if (warp == 0) {
-            float top = -INFINITY, sum = 0.f;
-            for (int j = lane; j < join.x; j += 32) top = fmaxf(top, part(j)[COLS * latent + col]);
+        // lane (j, k): maxima and sums of every eighth part's column k
+        constexpr int EACH = (kLaMaxCtas + 7) / 8;
+        const int k = lane & 3, end_at = COLS * latent + quad * 4 + k;
+        float m[EACH], l[EACH], top = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            for (int j = lane; j < join.x; j += 32) {
-                const float m = part(j)[COLS * latent + col], by = m == -INFINITY ? 0.f : ex2(m - top);
-                weight[j] = by;
-                if (by != 0.f) sum += by * part(j)[COLS * latent + COLS + col];
+        for (int i = 0; i < EACH; ++i) {
+            const int j = i * 8 + (lane >> 2);
+            m[i] = j < join.x ? part(j)[end_at] : -INFINITY;
+            l[i] = j < join.x ? part(j)[end_at + COLS] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) top = fmaxf(top, m[i]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int j = i * 8 + (lane >> 2);
+            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - top);
+            if (by != 0.f) sum += by * l[i];
+            if (j < join.x) weights[warp][j][k] = by;
+        }
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        __syncwarp();
+        float o[4] = {};
+#pragma unroll 8
+        for (int j = together ? warp : 0; j < join.x; j += step) {
+            const float4 v = *reinterpret_cast<const float4*>(part(j) + ((d / 128 * (COLS / 4) + quad) * 128 + d % 128) * 4);
+            const float4 by = *reinterpret_cast<const float4*>(weights[warp][j]);
+            // (a part that saw nothing has written no sums)
+            o[0] += by.x == 0.f ? 0.f : by.x * v.x; o[1] += by.y == 0.f ? 0.f : by.y * v.y;
+            o[2] += by.z == 0.f ? 0.f : by.z * v.z; o[3] += by.w == 0.f ? 0.f : by.w * v.w;
+        }
+        if (together) {
+            sums[warp][lane] = make_float4(o[0], o[1], o[2], o[3]);
+            __syncthreads();
+            if (warp == 0) {
+#pragma unroll
+                for (int u = 1; u < WARPS; ++u) { const float4 v = sums[u][lane]; o[0] += v.x; o[1] += v.y; o[2] += v.z; o[3] += v.w; }
             }
-            sum = warp_sum(sum);
-            if (lane == 0) norm = sum == 0.f ? 0.f : 1.f / sum;
+            __syncthreads();
         }
-        __syncthreads();
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int j = warp; j < join.x; j += 8) {
-            const float by = weight[j];
-            if (by == 0.f) continue;             // (a part that saw nothing has written no sums)
-            const float4 v = *reinterpret_cast<const float4*>(part(j) + col * latent + d0 + lane * 4);
-            o.x += by * v.x; o.y += by * v.y; o.z += by * v.z; o.w += by * v.w;
-        }
-        sums[warp][lane] = o;
-        __syncthreads();
-        if (warp == 0) {
+        const float norm = sum == 0.f ? 0.f : 1.f / sum;
+        if (!together || warp == 0)
 #pragma unroll
-            for (int k = 1; k < 8; ++k) { const float4 v = sums[k][lane]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
-            const float y[4] = {o.x * norm, o.y * norm, o.z * norm, o.w * norm};
-            store_row<4>(static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d0 + lane * 4, y);
-        }
-        __syncthreads();
+            for (int i = 0; i < 4; ++i) {
+                const int x = join.w * COLS + quad * 4 + i, row_in = la_row(a, x), h = x - row_in * a.heads, row = join.y + row_in;
+                const float y = o[i] * __shfl_sync(0xffffffffu, norm, i);
+                if (row_in >= join.z || row < 0 || row >= a.batch.n_rows) continue;
+                T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d;
+                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(y);
+                else *to = y;
+            }
+        __syncwarp();
     }
 }
 

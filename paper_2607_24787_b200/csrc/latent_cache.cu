@@ -70,8 +70,9 @@ cudaError_t launch_attend(LatentAttendArgs a, const CUtensorMap& map, int dev, i
 template <typename T, bool TRANSPOSED>
 cudaError_t launch_product(const HeadProductArgs& a, int n_heads, cudaStream_t st) {
     const auto grid = [&](int rows) { return dim3(unsigned((a.n_rows + rows - 1) / rows) * a.out_tiles, n_heads); };
-    if (a.n_rows <= 16) return launch_early(head_product_kernel<T, TRANSPOSED, 1>, grid(16), kHpWarps * 32, 0, st, a);
-    return launch_early(head_product_kernel<T, TRANSPOSED, 2>, grid(32), kHpWarps * 32, 0, st, a);
+    if constexpr (sizeof(T) == 2)
+        if (a.n_rows > 16) return launch_early(head_product_kernel<T, TRANSPOSED, 2>, grid(32), kHpWarps * 32, 0, st, a);
+    return launch_early(head_product_kernel<T, TRANSPOSED, 1>, grid(16), kHpWarps * 32, 0, st, a);
 }
 
 }  // namespace
@@ -107,10 +108,10 @@ int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, cons
     // a row a warp, or where these are few its query heads shared out
     constexpr int kWarps = 592 * kKvWarps;       // that the GPU has room for
     const int parts = std::max(1, std::min((a.q_heads + 7) / 8, kWarps / a.n_rows));
-    const unsigned grid = unsigned((static_cast<long long>(a.n_rows) * parts + kKvWarps - 1) / kKvWarps);
+    const dim3 grid(unsigned((a.n_rows + kKvWarps - 1ll) / kKvWarps), parts);
     const auto st = static_cast<cudaStream_t>(stream);
-    return launched(call, dtype == SPM_DTYPE_BF16 ? launch_early(latent_write_kernel<__nv_bfloat16>, grid, kKvWarps * 32, 0, st, a, parts)
-                                                  : launch_early(latent_write_kernel<float>, grid, kKvWarps * 32, 0, st, a, parts));
+    return launched(call, dtype == SPM_DTYPE_BF16 ? launch_early(latent_write_kernel<__nv_bfloat16>, grid, kKvWarps * 32, 0, st, a)
+                                                  : launch_early(latent_write_kernel<float>, grid, kKvWarps * 32, 0, st, a));
 }
 
 int spm_latent_attend_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int dtype, size_t* bytes) {
@@ -152,6 +153,10 @@ int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, con
     a.batch = batch_of(batch);
     a.q = rows_of(q); a.out = rows_of(out);
     a.heads = n_heads;
+    int bits = 0;                                // x / d = x * ceil(2^(31 + bits) / d) >> (31 + bits), 2^bits >= d, for x below 2^31
+    while (1 << bits < n_heads) ++bits;
+    a.heads_shift = 31 + bits;
+    a.heads_times = uint32_t(((1ull << a.heads_shift) + n_heads - 1) / n_heads);
     a.chunks = kv->latent_dim / 64 + 1;
     a.box = kv->page_size % 64 == 0 ? 64 : kv->page_size % 32 == 0 ? 32 : 16;
     a.factor = factor;

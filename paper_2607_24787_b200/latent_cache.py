@@ -15,7 +15,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .kv_cache import _dtype, _enqueue, _need, _rows, _vector
+from .kv_cache import DTYPES, _dtype, _enqueue, _need, _rows, _vector
 
 
 class LatentCache:
@@ -47,25 +47,34 @@ class LatentCache:
 
     def _vectors(self, x, n, size, dtype, what):
         """spm_rows of a tensor [n, size] whose elements are contiguous."""
-        _need(x.dim() == 2, f"{what}: [rows, {size}], not {list(x.shape)}")
-        return _rows(x.unsqueeze(1), n, 1, size, dtype, self.device, what)
+        if x.shape != (n, size):
+            raise ValueError(f"{what}: shape [{n}, {size}], not {list(x.shape)}")
+        if x.dtype is not dtype or x.device != self.device:
+            raise ValueError(f"{what}: {dtype} on {self.device}, not {x.dtype} on {x.device}")
+        row, one = x.stride()
+        if one != 1:
+            raise ValueError(f"{what}: the elements of a row must be contiguous")
+        return B.Rows(x.data_ptr(), row, 0)
 
     def write(self, batch, latent, key, q=None, positions=None, rope=None, q_out=None):
         """latent [rows, latent_dim] and key [rows, rope_dim] of the batch's new rows go into the cache, normed by `rope`'s k_gamma and turned;
         returns q [rows, heads, rope_dim], the parts of the queries that turn, turned (None without q)."""
         self._on(batch, "batch")
         n, size, device, dtype = batch.n_rows, self.rope_dim, self.device, latent.dtype
-        dt = _dtype(latent.unsqueeze(1), "latent")
+        dt = DTYPES.get(dtype)
+        if dt is None:
+            raise ValueError(f"latent: fp32 or bf16, not {dtype}")
         cl, ck = self._vectors(latent, n, self.latent_dim, dtype, "latent"), self._vectors(key, n, size, dtype, "key")
         cq = co = cr = pos = None
         stride = heads = 0
         if rope is not None:
             self._on(rope, "rope")
-            _need(rope.gamma_sizes[0] is None, "rope: queries have no norm here, q_gamma is to be None")
+            if rope.gamma_sizes[0] is not None:
+                raise ValueError("rope: queries have no norm here, q_gamma is to be None")
             cr, pos, stride = rope._with(positions, n, self.latent_dim, False, True)
         if q is not None:
-            _need(rope is not None, "q without rope: there is nothing to do to it")
-            _need(q.dim() == 3, "q: [rows, heads, rope_dim]")
+            if rope is None or q.dim() != 3:
+                raise ValueError("q without rope: there is nothing to do to it" if rope is None else "q: [rows, heads, rope_dim]")
             heads = q.shape[1]
             cq = _rows(q, n, heads, size, dtype, device, "q")
             if q_out is None:
@@ -104,14 +113,16 @@ def head_product(x, w, transposed=False, out=None):
     dt = _dtype(x, "x")
     n, heads, size = x.shape
     device = x.device
-    _need(w.dim() == 3 and w.dtype is torch.bfloat16 and w.device == device and w.shape[0] == heads and w.shape[1 + bool(transposed)] == size
-          and w.stride(2) == 1, f"w: bf16 [{heads}, {'out, ' if transposed else ''}{size}{'' if transposed else ', out'}] on {device}, rows contiguous")
-    to = w.shape[1 if transposed else 2]
+    shape, strides = w.shape, w.stride()
+    if (len(shape) != 3 or w.dtype is not torch.bfloat16 or w.device != device or shape[0] != heads or shape[2 if transposed else 1] != size
+            or strides[2] != 1):
+        raise ValueError(f"w: bf16 [{heads}, {'out, ' if transposed else ''}{size}{'' if transposed else ', out'}] on {device}, rows contiguous")
+    to = shape[1 if transposed else 2]
     cx = _rows(x, n, heads, size, x.dtype, device, "x")
     if out is None:
         out = x.new_empty(n, heads, to)
         cy = B.Rows(out.data_ptr(), heads * to, to)
     else:
         cy = _rows(out, n, heads, to, x.dtype, device, "out")
-    _enqueue(device, B.load().spm_head_product, cx, w.data_ptr(), w.stride(0), w.stride(1), int(transposed), cy, n, heads, size, to, dt)
+    _enqueue(device, B.load().spm_head_product, cx, w.data_ptr(), strides[0], strides[1], int(transposed), cy, n, heads, size, to, dt)
     return out
