@@ -603,6 +603,24 @@ int spm_latent_attend_workspace(const spm_latent_cache* kv, const spm_kv_batch* 
 int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rows* q, int n_heads, const spm_rows* out, float scale,
                       int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Matrices of heads, bf16: element (h, i, j) is p[h * head_stride + i * row_stride + j]. p is 16-byte aligned, strides are multiples of 8 elements. */
+typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
+
+/* The expanded form, for prompts: out (n_heads heads of head_dim elements) = softmax(scale q . key) value for each new row and each of its
+ * heads, over the tokens up to the row's own position, with key = [W_k latent | key of the row] and value = W_v latent made from the cache for
+ * all tokens of the batch's sequences, a round of heads at a time. q: heads of head_dim + rope_dim elements. head_dim: 64 or 128.
+ * n_tokens: at least the tokens of all sequences that have rows in this batch (the sum of their lengths), which is what the workspace has
+ * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. dtype: bf16 (fp32 rows have the absorbed form). Keys' first
+ * parts, values, probabilities and results are rounded to bf16 once each; statistics and sums are fp32. What is said above of queries and
+ * rows that are not finite holds, but that any element of a row that is not finite makes all elements of the result NaN.
+ * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * head_dim * 4 and a little more, but
+ * not much over 512 MB where a head takes less); one for each of calls that may run at the same time. */
+int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,
+                                         size_t* bytes);
+int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rows* q, const spm_matrices* w_k, const spm_matrices* w_v,
+                               int n_heads, int head_dim, const spm_rows* out, float scale, int n_tokens, int dtype, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
 /* y_h = x_h W_h (transposed 0: W_h is [in_dim][out_dim]) or x_h W_h^T (else: [out_dim][in_dim]) for each head h of each of n_rows rows. w: dev,
  * bf16, element (h, i, j) at h * w_head_stride + i * w_row_stride + j; 16-byte aligned, strides multiples of 8. in_dim and out_dim: multiples
  * of 64, at most 8192. Products of fp32 rows are exact, sums fp32. y may not overlap x. dtype: of x and y. */

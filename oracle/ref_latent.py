@@ -46,11 +46,12 @@ def _softmax(z):
 
 def attend(q, pages, table, lengths, row_start, scale, latent, w_k=None, w_v=None):
     """q [rows, heads, ...] float64 -> (out, sum of p |value|, largest |scale| sum |q key| of a seen token), rows of no sequence NaN. Without w_k
-    and w_v the absorbed form: keys are whole rows, values their latent part. With them (float64 [heads, head, latent]) the expanded one."""
+    and w_v the absorbed form: keys are whole rows, values their latent part. With them (float64 [heads, head, latent]) the expanded one, and then
+    also the sum of p |w_v| |latent| and the largest |scale| |q| |w_k| |latent|: what sums made of latent vectors may be off by a part of."""
     n_rows, heads = q.shape[:2]
     size = latent if w_v is None else w_v.shape[1]
-    out, spread = np.full((n_rows, heads, size), np.nan), np.zeros((n_rows, heads, size))
-    reach = np.zeros((n_rows, heads, 1))
+    out, spread, made = np.full((n_rows, heads, size), np.nan), np.zeros((n_rows, heads, size)), np.zeros((n_rows, heads, size))
+    reach, reach_made = np.zeros((n_rows, heads, 1)), np.zeros((n_rows, heads, 1))
     kept = {}
     for i, at in enumerate(places(lengths, row_start, n_rows)):
         if at is None:
@@ -62,7 +63,9 @@ def attend(q, pages, table, lengths, row_start, scale, latent, w_k=None, w_v=Non
             if w_k is None:
                 kept[seq] = there, [(rows, rows[:, :latent])] * heads
             else:
-                kept[seq] = there, [(np.concatenate((rows[:, :latent] @ w_k[h].T, rows[:, latent:]), 1), rows[:, :latent] @ w_v[h].T) for h in range(heads)]
+                c, r = rows[:, :latent], rows[:, latent:]
+                kept[seq] = there, [(np.concatenate((c @ w_k[h].T, r), 1), c @ w_v[h].T, np.abs(c) @ np.abs(w_k[h]).T, np.abs(c) @ np.abs(w_v[h]).T)
+                                    for h in range(heads)]
         there, kv = kept[seq]
         see = np.flatnonzero(there & (np.arange(len(there)) <= pos))
         for h in range(heads):
@@ -73,4 +76,7 @@ def attend(q, pages, table, lengths, row_start, scale, latent, w_k=None, w_v=Non
             p = _softmax(k @ q[i, h] * scale)
             out[i, h], spread[i, h] = p @ v, p @ np.abs(v)
             reach[i, h] = (np.abs(k) @ np.abs(q[i, h])).max() * abs(scale)
-    return out, spread, reach
+            if w_k is not None:
+                made[i, h] = p @ kv[h][3][see]
+                reach_made[i, h] = (kv[h][2][see] @ np.abs(q[i, h, :w_k.shape[1]])).max() * abs(scale)
+    return (out, spread, reach) if w_k is None else (out, spread, reach, made, reach_made)

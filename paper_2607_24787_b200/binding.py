@@ -81,6 +81,10 @@ class Rows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class Matrices(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("head_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
 class Rope(C.Structure):
     _fields_ = ([(k, C.c_void_p) for k in ("inv_freq", "axis_of", "q_gamma", "k_gamma")]
                 + [(k, C.c_int32) for k in ("n_axes", "rot_dim", "neighbours")] + [("eps", C.c_float)])
@@ -154,6 +158,9 @@ _SIG = {
     "spm_latent_attend_workspace": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.c_int, C.c_int, C.POINTER(C.c_size_t)],
     "spm_latent_attend": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.POINTER(Rows), C.c_int, C.POINTER(Rows), C.c_float, C.c_int, _P,
                           C.c_size_t, _P],
+    "spm_latent_attend_expanded_workspace": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "spm_latent_attend_expanded": [C.POINTER(LatentRows), C.POINTER(KvBatch), C.POINTER(Rows), C.POINTER(Matrices), C.POINTER(Matrices), C.c_int, C.c_int,
+                                   C.POINTER(Rows), C.c_float, C.c_int, C.c_int, _P, C.c_size_t, _P],
     "spm_head_product": [C.POINTER(Rows), _P, C.c_int64, C.c_int64, C.c_int, C.POINTER(Rows), C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, _P],
     "spm_host_alloc": [C.c_size_t, C.POINTER(_P)],
     "spm_host_free": [_P],
@@ -534,6 +541,16 @@ def spm_latent_attend_workspace(kv, batch, n_heads, dtype) -> int:
 
 def spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, workspace_bytes, stream=None):
     _check(load().spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, workspace_bytes, stream))
+
+
+def spm_latent_attend_expanded_workspace(kv, batch, n_heads, head_dim, n_tokens, dtype) -> int:
+    out = C.c_size_t()
+    _check(load().spm_latent_attend_expanded_workspace(kv, batch, n_heads, head_dim, n_tokens, dtype, C.byref(out)))
+    return out.value
+
+
+def spm_latent_attend_expanded(kv, batch, q, w_k, w_v, n_heads, head_dim, out, scale, n_tokens, dtype, workspace, workspace_bytes, stream=None):
+    _check(load().spm_latent_attend_expanded(kv, batch, q, w_k, w_v, n_heads, head_dim, out, scale, n_tokens, dtype, workspace, workspace_bytes, stream))
 
 
 def spm_head_product(x, w, w_head_stride, w_row_stride, transposed, y, n_rows, n_heads, in_dim, out_dim, dtype, stream=None):

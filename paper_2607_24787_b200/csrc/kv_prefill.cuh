@@ -22,12 +22,12 @@
 #pragma once
 
 #include "kv_attend.cuh"
+#include "prompt_items.cuh"
 #include "tc_ops.cuh"
 
 namespace spm {
 
 constexpr int kPfTile = 128;                     // tokens of a tile, rows of a half
-constexpr int kPfCols = 256;
 // two halves' softmax warps, operand warps, the issuing warp and three that only make its four whole. Registers a thread: 128 at the launch,
 // of which the last two fours give some to the softmax warps (2 x 176 + 104 + 56 = 4 x 128).
 constexpr int kPfThreads = 16 * 32;
@@ -63,7 +63,7 @@ struct PfShared {
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], drained;
     uint32_t tmem;
     int quit;                                    // a wait has run out: everybody leaves
-    int rb, seq, first, n, len;                  // the item: its columns, its sequence's rows and tokens
+    PfItem item;
     int exps[4];                                 // E of a tile, and whether its keys are times 2^-4 (bit 16)
     int widest[4], widest_key[4];                // an operand warp's largest scale of a tile's values and keys, as fp32 bits
     uint32_t there[4][4];                        // which tokens of a tile exist
@@ -126,62 +126,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
 
     grid_dep_wait();
     grid_dep_launch();
-    // ---- which item, heads together. Up to 32 sequences: those of the most tokens first, so that what is left at the end is short; more:
-    // one sequence after another, its last (longest) columns first. A warp searches, others prepare what all items need ----
+    // ---- which item, heads together. A warp searches, others prepare what all items need ----
     const int head = blockIdx.x % a.kv.heads, cap = b.stride * a.kv.page_size;
-    if (warp == 13) {
-        int block = blockIdx.x / a.kv.heads;
-        if (lane == 0) sh.n = 0;
-        __syncwarp();
-        for (int s0 = 0; s0 < b.n_seq; s0 += 32) {
-            const int s = s0 + lane;
-            int f = s, m = s < b.n_seq ? 1 : 0;
-            if (b.row_start && s < b.n_seq) {
-                f = b.row_start[s];
-                m = a.rows ? a.rows[s] : max(0, min(b.row_start[s + 1] - f, b.n_rows));
-            }
-            const int len = s < b.n_seq ? b.lengths[s] : 0, tokens = max(0, min(len, cap));
-            const int own = (m * a.group + kPfCols - 1) / kPfCols;               // (a call's rows times heads fit)
-            auto running = [&](int v) {
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int w = __shfl_up_sync(0xffffffffu, v, o);
-                    if (lane >= o) v += w;
-                }
-                return v;
-            };
-            int before = running(own) - own;
-            const int all = __shfl_sync(0xffffffffu, before + own, 31);
-            if (block >= all) { block -= all; continue; }
-            int ours = own, skip = 0;            // of this sequence's items, longest first: `ours` after `skip`
-            if (b.n_seq <= 32) {
-                // items whose first row sees `t` tokens and more
-                auto at_least = [&](int t) {
-                    if (t <= 0) return own;
-                    if (t > tokens) return 0;
-                    return max(0, own - int(unsigned(max(0, min(t - 1 - (len - m), m)) * a.group + kPfCols - 1) / kPfCols));
-                };
-                int low = 0, high = __reduce_max_sync(0xffffffffu, tokens) + 1;  // `low`: the most tokens that more than `block` items have
-                while (high - low > 1) {         // (eight parts at a time: seven sums that do not wait for one another)
-                    const int step = (high - low + 7) / 8;
-                    int above = 0;
-#pragma unroll
-                    for (int i = 1; i < 8; ++i) above += int(__reduce_add_sync(0xffffffffu, at_least(low + i * step))) > block;
-                    low += above * step;
-                    high = min(high, low + step);
-                }
-                skip = at_least(low + 1);
-                ours = at_least(low) - skip;
-                block -= __reduce_add_sync(0xffffffffu, skip);
-                before = running(ours) - ours;
-            }
-            if (before <= block && block < before + ours) {
-                sh.rb = own - 1 - skip - (block - before);
-                sh.seq = s; sh.first = f; sh.n = m; sh.len = len;
-            }
-            break;
-        }
-    }
+    if (warp == 13) pf_find(b, a.rows, a.group, cap, blockIdx.x / a.kv.heads, sh.item);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 128); mbar_init(smem_u32(&sh.v_full[i]), 128);
@@ -194,7 +141,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv_prefill_kernel(const AttendA
     }
     if (warp == 12) tmem_alloc(smem_u32(&sh.tmem), 512);
     __syncthreads();
-    const int rb = sh.rb, seq = sh.seq, first = sh.first, n = sh.n, len = sh.len;
+    const int rb = sh.item.rb, seq = sh.item.seq, first = sh.item.first, n = sh.item.n, len = sh.item.len;
     if (n == 0) {                                // more CTAs than items
         tc_fence_before();
         if (warp == 12) tmem_dealloc(sh.tmem, 512);

@@ -9,6 +9,8 @@
 #include "head_product.cuh"
 #include "kv_checks.h"
 #include "latent_attend.cuh"
+#include "latent_expand.cuh"
+#include "latent_prompts.cuh"
 #include "latent_write.cuh"
 #include "tma_maps.h"
 
@@ -65,6 +67,66 @@ cudaError_t launch_attend(LatentAttendArgs a, const CUtensorMap& map, int dev, i
     const int ctas = std::min(sms, kLaMaxCtas);
     e = launch_early(latent_attend_kernel<T, COLS>, ctas, kLaThreads, la_smem(fixed, a.chunks, a.stages), st, a, map);
     return e == cudaSuccess ? launch_early(latent_join_kernel<T, COLS>, kLaJoinBlocks, kLaJoinThreads, 0, st, a, ctas) : e;
+}
+
+// ---- expanded attention ----
+// The workspace: keys and values of a round's heads, [heads][tokens][head_dim] each, [tokens][64] shared parts of keys, a bit a token
+struct Expanded { int tokens, heads, rounds; size_t values, ropes, there, bytes; };
+constexpr size_t kLxMost = size_t(512) << 20;    // of keys and values together, where more than one head is more
+Expanded expanded_of(const spm_kv_batch* b, int n_heads, int head_dim, int n_tokens) {
+    Expanded e{};
+    e.tokens = int(std::max(1ll, (n_tokens + 127ll * b->n_seq) / 128) * 128);
+    const size_t head = size_t(e.tokens) * head_dim * 4;
+    e.rounds = int((n_heads + std::max<size_t>(1, kLxMost / head) - 1) / std::max<size_t>(1, kLxMost / head));
+    e.heads = (n_heads + e.rounds - 1) / e.rounds;
+    e.rounds = (n_heads + e.heads - 1) / e.heads;
+    e.values = e.heads * head / 2;
+    e.ropes = e.heads * head;
+    e.there = e.ropes + size_t(e.tokens) * 128;
+    e.bytes = e.there + size_t(e.tokens) / 8;
+    return e;
+}
+int check_expanded(const char* call, const spm_kv_batch* b, int n_heads, int head_dim, int n_tokens, int dtype) {
+    if (int rc = check_dtype(call, dtype)) return rc;
+    if (dtype != SPM_DTYPE_BF16) return fail(call, SPM_ERR_CONFIG, "the expanded form is for bf16 rows; fp32 rows have the absorbed form");
+    if (int rc = check_heads(call, n_heads)) return rc;
+    if (head_dim != 64 && head_dim != 128) return fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(head_dim) + " not supported: 64 or 128");
+    if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(call, SPM_ERR_INVALID_ARG, "n_tokens outside 0..2^30");
+    if (static_cast<long long>(b->n_rows) * n_heads > INT32_MAX - 64) return fail(call, SPM_ERR_INVALID_ARG, "n_rows * n_heads is over 2^31 - 65");
+    return SPM_OK;
+}
+int check_matrices(const char* call, const char* name, const spm_matrices* w, int rows) {
+    if (!w || !w->p) return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + " is null");
+    if (!aligned(w->p, 16) || w->row_stride % 8 || w->head_stride % 8 || w->row_stride < rows || w->head_stride < rows)
+        return fail(call, SPM_ERR_INVALID_ARG, std::string(name) + ": rows of weights must start on 16-byte boundaries and not overlap");
+    return SPM_OK;
+}
+
+template <int HD>
+cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expanded& e, int n_heads, const CUtensorMap& rows, const CUtensorMap& wk, const CUtensorMap& wv,
+                            const CUtensorMap& keys, const CUtensorMap& ropes, const CUtensorMap& values, int dev, int sms, cudaStream_t st) {
+    cudaError_t err = allow_smem<latent_expand_kernel<HD>>(dev, kMaxSmem);
+    if (err == cudaSuccess) err = allow_smem<latent_prompt_kernel<HD>>(dev, LpShape<HD>::smem);
+    const int fixed = kLxOwnBytes + 1024 + x.kv.latent / 64 * kLxChunkBytes, stage = 2 * HD * 128;
+    x.stages = std::min(8, (kMaxSmem - fixed) / stage);
+    const int tiles = e.tokens / kLxTile;
+    for (int h0 = 0; err == cudaSuccess && h0 < n_heads; h0 += e.heads) {
+        x.h0 = a.h0 = h0;
+        x.heads = a.heads = std::min(e.heads, n_heads - h0);
+        // parts of the heads: the fewest rounds of CTAs, of which each begins with what takes as long as a head and a half
+        int parts = 1;
+        double best = 1e30;
+        for (int p = 1; p <= x.heads; ++p) {
+            const double t = double((static_cast<long long>(tiles) * p + sms - 1) / sms) * ((x.heads + p - 1) / p + 1.5);
+            if (t < best) { best = t; parts = p; }
+        }
+        err = launch_early(latent_expand_kernel<HD>, dim3(tiles, parts), kLxThreads, fixed + x.stages * stage, st, x, rows, wk, wv);
+        if (err != cudaSuccess) break;
+        const long long items = (a.batch.n_rows / kPfCols + a.batch.n_seq) * static_cast<long long>(a.heads);
+        if (items > INT32_MAX) return cudaErrorInvalidValue;
+        err = launch_early(latent_prompt_kernel<HD>, unsigned(items), kLpThreads, LpShape<HD>::smem, st, a, keys, ropes, values);
+    }
+    return err;
 }
 
 template <typename T, bool TRANSPOSED>
@@ -174,6 +236,75 @@ int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, con
     else if (cols == 48) e = launch_attend<__nv_bfloat16, 48>(a, map, dev, sms, st);
     else e = launch_attend<__nv_bfloat16, 64>(a, map, dev, sms, st);
     return launched(call, e);
+}
+
+int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,
+                                         size_t* bytes) {
+    const char* call = "spm_latent_attend_expanded_workspace";
+    if (!bytes) return fail(call, SPM_ERR_INVALID_ARG, "null argument");
+    if (int rc = check_latent_shape(call, kv)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
+    if (int rc = check_expanded(call, batch, n_heads, head_dim, n_tokens, dtype)) return rc;
+    *bytes = expanded_of(batch, n_heads, head_dim, n_tokens).bytes;
+    return SPM_OK;
+}
+
+int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rows* q, const spm_matrices* w_k, const spm_matrices* w_v,
+                               int n_heads, int head_dim, const spm_rows* out, float scale, int n_tokens, int dtype, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    const char* call = "spm_latent_attend_expanded";
+    if (int rc = check_latent_cache(call, kv)) return rc;
+    if (int rc = check_batch(call, kv->page_size, batch)) return rc;
+    if (int rc = check_expanded(call, batch, n_heads, head_dim, n_tokens, dtype)) return rc;
+    const float factor = scale * 1.4426950408889634f;
+    if (!std::isfinite(factor)) return fail(call, SPM_ERR_INVALID_ARG, "scale is not finite, or not below 2^127");
+    if (batch->n_rows == 0 || batch->n_seq == 0) return SPM_OK;
+    if (int rc = check_rows(call, "q", q, dtype)) return rc;
+    if (int rc = check_rows(call, "out", out, dtype)) return rc;
+    if (q->p == out->p) return fail(call, SPM_ERR_INVALID_ARG, "out is in the place of q, which is read until the end");
+    if (int rc = check_matrices(call, "w_k", w_k, kv->latent_dim)) return rc;
+    if (int rc = check_matrices(call, "w_v", w_v, kv->latent_dim)) return rc;
+    const Expanded e = expanded_of(batch, n_heads, head_dim, n_tokens);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < e.bytes)
+        return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold " + std::to_string(e.bytes) + " bytes");
+    if (static_cast<long long>(e.tokens) * e.heads > INT32_MAX) return fail(call, SPM_ERR_CONFIG, "n_tokens times heads is over 2^31 - 1");
+    int dev = 0, sms = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (err != cudaSuccess) return fail(call, SPM_ERR_CUDA, cudaGetErrorString(err));
+    if (dev < 0 || dev >= kMaxDevices) return fail(call, SPM_ERR_CONFIG, "device ordinal out of range");
+    char* work = static_cast<char*>(workspace);
+    LatentExpandArgs x{};
+    x.kv = pool_of(kv);
+    x.batch = batch_of(batch);
+    x.box = kv->page_size % 128 == 0 ? 128 : kv->page_size % 64 == 0 ? 64 : kv->page_size % 32 == 0 ? 32 : 16;
+    x.tokens = e.tokens;
+    x.keys = reinterpret_cast<__nv_bfloat16*>(work);
+    x.values = reinterpret_cast<__nv_bfloat16*>(work + e.values);
+    x.ropes = reinterpret_cast<__nv_bfloat16*>(work + e.ropes);
+    x.there = reinterpret_cast<uint32_t*>(work + e.there);
+    x.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    x.withhold = g_withhold.load(std::memory_order_relaxed);
+    LatentPromptArgs a{};
+    a.kv = x.kv;
+    a.batch = x.batch;
+    a.q = rows_of(q); a.out = rows_of(out);
+    a.tokens = e.tokens;
+    a.there = x.there;
+    a.factor = factor;
+    a.wait_ns = x.wait_ns;
+    a.withhold = x.withhold;
+    CUtensorMap rows{}, wk, wv, keys, ropes, values;         // (a pool without pages: no copy is made of it)
+    const uint64_t made = uint64_t(e.heads) * e.tokens;
+    if ((kv->n_pages > 0 && !make_token_map(&rows, kv->rows, kv->latent_dim + kv->rope_dim, uint64_t(kv->n_pages) * kv->page_size, x.box)) ||
+        !make_matrix_map(&wk, w_k->p, kv->latent_dim, head_dim, n_heads, w_k->row_stride, w_k->head_stride) ||
+        !make_matrix_map(&wv, w_v->p, kv->latent_dim, head_dim, n_heads, w_v->row_stride, w_v->head_stride) ||
+        !make_token_map(&keys, x.keys, head_dim, made, kLpTile) || !make_token_map(&values, x.values, head_dim, made, kLpTile) ||
+        !make_token_map(&ropes, x.ropes, 64, e.tokens, kLpTile))
+        return fail(call, SPM_ERR_CUDA, "no tensor map of the cache's rows, the matrices or the workspace");
+    const auto st = static_cast<cudaStream_t>(stream);
+    return launched(call, head_dim == 64 ? launch_expanded<64>(x, a, e, n_heads, rows, wk, wv, keys, ropes, values, dev, sms, st)
+                                         : launch_expanded<128>(x, a, e, n_heads, rows, wk, wv, keys, ropes, values, dev, sms, st));
 }
 
 int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, int64_t w_row_stride, int transposed, const spm_rows* y, int n_rows,

@@ -1,0 +1,277 @@
+// Keys and values of a batch's tokens, made from their latent vectors for one head after another, on tcgen05.
+//
+// [key | value] of a head = C [W_k ; W_v]^T: 128 tokens of one sequence, all of their latent vectors in shared memory, against the head's
+// matrices, whose rows come by in chunks of 64 elements. Sums of two heads are in tensor memory, so that one is rounded to bf16 and
+// written while the next is made. Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
+//
+// A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
+// element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
+#pragma once
+
+#include <cuda.h>
+
+#include "kv_cache.cuh"
+#include "latent_attend.cuh"
+#include "latent_cache.cuh"
+#include "ptx.cuh"
+#include "tc_ops.cuh"
+
+namespace spm {
+
+constexpr int kLxTile = 128, kLxThreads = 192, kLxChunkBytes = kLxTile * 128;
+
+struct LatentExpandArgs {
+    LatentPool kv;
+    KvBatch batch;
+    int heads, h0;              // of this round, the first one's number
+    int box;                    // tokens of a copy, all of one page
+    int stages;                 // of the matrices' ring
+    int tokens;                 // that the workspace has room for, a multiple of 128
+    __nv_bfloat16 *keys, *values, *ropes;       // [heads][tokens][HD] twice, [tokens][64]
+    uint32_t* there;            // [tokens / 32]
+    unsigned long long wait_ns;
+    int withhold;
+};
+
+// Where a sequence's tokens stand in the workspace, and how many of them
+struct LxPlace { int seq, at, tokens, tile; };
+
+// Of a sequence (all lanes of a warp together): tokens that count, and rows
+__device__ __forceinline__ int lx_tokens(const KvBatch& b, int cap, int s) {
+    if (s >= b.n_seq) return 0;
+    if (b.row_start && min(b.row_start[s + 1] - b.row_start[s], b.n_rows) <= 0) return 0;     // (no rows look at them)
+    return max(0, min(b.lengths[s], cap));
+}
+// Tile `tile` of the workspace (tile < 0: sequence `seq`'s first), by a warp
+__device__ __forceinline__ LxPlace lx_find(const KvBatch& b, int cap, int room, int seq, int tile) {
+    const int lane = threadIdx.x & 31;
+    LxPlace p{-1, 0, 0, 0};
+    long long before = 0;                        // tiles
+    for (int s0 = 0; s0 < b.n_seq; s0 += 32) {
+        const int tokens = lx_tokens(b, cap, s0 + lane);
+        const long long own = (tokens + kLxTile - 1) / kLxTile;
+        long long upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const long long first = before + upto - own;
+        const bool here = tile >= 0 ? first <= tile && tile < first + own : s0 + lane == seq;
+        const uint32_t who = __ballot_sync(0xffffffffu, here);
+        if (who) {
+            const int from = __ffs(who) - 1;
+            const long long at = min(__shfl_sync(0xffffffffu, first, from) * kLxTile, static_cast<long long>(room));
+            p.seq = s0 + from;
+            p.at = int(at);
+            p.tokens = min(__shfl_sync(0xffffffffu, tokens, from), room - p.at);
+            p.tile = tile - p.at / kLxTile;
+            return p;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return p;
+}
+
+struct LxShared {
+    unsigned long long a_full, b_full[8], b_empty[8], d_full[2], d_empty[2], drained;
+    uint32_t tmem;
+    int quit;
+    LxPlace place;
+    int rows[kLxTile / 16];     // of the tile's copies in the pool, -1: there is none
+};
+constexpr int kLxOwnBytes = 1024;
+static_assert(sizeof(LxShared) <= kLxOwnBytes, "what shared memory has beside the operands");
+
+__device__ __forceinline__ void tma_matrix(uint32_t dst, const CUtensorMap* map, int element, int row, int head, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(element), "r"(row), "r"(head), "r"(bar) : "memory");
+}
+// a sector of 32 bytes a thread
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), SPM_W8(v, 0) : "memory");
+}
+__device__ __forceinline__ bool not_finite(uint32_t bits) { return (bits & 0x7f800000u) == 0x7f800000u; }
+
+// blockIdx.x: a tile of the workspace, blockIdx.y: one of gridDim.y parts of the heads
+template <int HD>
+__global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const LatentExpandArgs a, const __grid_constant__ CUtensorMap rows_map,
+                                                                      const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    constexpr int N = 2 * HD, STAGE = N * 128;
+    extern __shared__ __align__(16) unsigned char raw_smem[];
+    LxShared& sh = *reinterpret_cast<LxShared*>(raw_smem);
+    const uint32_t a_at = (smem_u32(raw_smem) + kLxOwnBytes + 1023) & ~1023u;
+    const int chunks = a.kv.latent / 64, cap = a.batch.stride * a.kv.page_size;
+    const uint32_t b_at = a_at + chunks * kLxChunkBytes;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    grid_dep_wait();
+    grid_dep_launch();
+    if (tid == 0) {
+        mbar_init(smem_u32(&sh.a_full), 1 + a.withhold);
+        for (int i = 0; i < a.stages; ++i) { mbar_init(smem_u32(&sh.b_full[i]), 1); mbar_init(smem_u32(&sh.b_empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.d_full[i]), 1); mbar_init(smem_u32(&sh.d_empty[i]), 128); }
+        mbar_init(smem_u32(&sh.drained), 1);
+        sh.quit = 0;
+        fence_barrier_init();
+    }
+    if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), 2 * N);
+    const int copies = kLxTile / a.box;
+    if (warp == 4) {
+        const LxPlace p = lx_find(a.batch, cap, a.tokens, 0, blockIdx.x);
+        int row = -1;
+        const int token = p.tile * kLxTile + lane * a.box;
+        if (p.seq >= 0 && lane < copies && token < p.tokens) {
+            const int page = a.batch.table[size_t(p.seq) * a.batch.stride + token / a.kv.page_size];
+            if (page >= 0 && page < a.kv.n_pages) row = page * a.kv.page_size + token % a.kv.page_size;
+            else kv_note(a.kv, SPM_KV_BAD_PAGE);
+        }
+        if (lane == 0) sh.place = p;
+        if (lane < copies) sh.rows[lane] = row;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    const LxPlace place = sh.place;
+    if (place.seq < 0) {                         // more tiles in the workspace than there are
+        tc_fence_before();
+        __syncthreads();
+        if (warp == 5) tmem_dealloc(tmem, 2 * N);
+        return;
+    }
+    const int head0 = a.heads * int(blockIdx.y) / int(gridDim.y), head1 = a.heads * int(blockIdx.y + 1) / int(gridDim.y);
+
+    auto wait = [&](const unsigned long long& bar, int parity) {
+        const uint32_t at = smem_u32(&bar);
+        if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
+        const unsigned long long t0 = global_timer_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 32; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(at, parity))) return true;
+            const bool late = global_timer_ns() - t0 > a.wait_ns;
+            if (late) {
+                *reinterpret_cast<volatile int*>(&sh.quit) = 1;
+                kv_note(a.kv, SPM_KV_TIMEOUT);
+            }
+            if (__any_sync(0xffffffffu, late || *reinterpret_cast<volatile int*>(&sh.quit))) return false;
+        }
+    };
+    bool ok = true;
+
+    if (warp < 4) {
+        // ---- rows out: a token a thread ----
+        const int t = place.tile * kLxTile + tid, row = sh.rows[tid / a.box];
+        const bool there = t < place.tokens && row >= 0;
+        const size_t to = size_t(place.at) + t;
+        if (blockIdx.y == 0) {
+            const uint32_t bits = __ballot_sync(0xffffffffu, there);
+            if (lane == 0) a.there[to / 32] = bits;
+            const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + (there ? static_cast<long long>(row) + tid % a.box : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
+            uint4* rope = reinterpret_cast<uint4*>(a.ropes + to * 64);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rope[i] = there && i < a.kv.rope / 8 ? from[i] : make_uint4(0, 0, 0, 0);
+        }
+        for (int h = head0; h < head1; ++h) {
+            const int buf = (h - head0) & 1, turn = (h - head0) >> 1 & 1;
+            if (!(ok = wait(sh.d_full[buf], turn))) break;
+            tc_fence_after();
+            bool odd = false;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                uint32_t w[HD / 2];
+#pragma unroll
+                for (int ch = 0; ch < HD / 32; ++ch) {
+                    uint32_t r[32];
+                    tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        if (part == 0) odd |= not_finite(r[i]) || not_finite(r[i + 1]);
+                        else if (odd) {
+                            if (not_finite(r[i])) r[i] = 0;
+                            if (not_finite(r[i + 1])) r[i + 1] = 0;
+                        }
+                        w[ch * 16 + i / 2] = there ? pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1])) : 0u;
+                    }
+                }
+                if (part == 0 && odd && there) w[0] = 0x7fff7fffu;
+                if (part == 1) {
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&sh.d_empty[buf]));
+                }
+                __nv_bfloat16* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
+#pragma unroll
+                for (int i = 0; i < HD / 2; i += 8) st_global32(out + 2 * i, w + i);
+            }
+        }
+    } else if (warp == 4) {
+        // ---- latent vectors, then matrices, on their way in ----
+        const int row = lane < copies ? sh.rows[lane] : -1, n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        const uint32_t a_bar = smem_u32(&sh.a_full);
+        if (lane == 0) mbar_arrive_expect_tx(a_bar, n * a.box * 128 * chunks);
+        __syncwarp();
+        if (row >= 0)
+            for (int c = 0; c < chunks; ++c) tma_rows(a_at + c * kLxChunkBytes + lane * a.box * 128, &rows_map, c * 64, row, a_bar);
+        __syncwarp();
+        int st = 0, turn = 0, it = 0;
+        for (int h = head0; h < head1 && ok; ++h)
+            for (int c = 0; c < chunks; ++c, ++it) {
+                if (it >= a.stages && !(ok = wait(sh.b_empty[st], turn ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&sh.b_full[st]), at = b_at + st * STAGE;
+                    mbar_arrive_expect_tx(bar, STAGE);
+                    tma_matrix(at, &k_map, c * 64, 0, a.h0 + h, bar);
+                    tma_matrix(at + HD * 128, &v_map, c * 64, 0, a.h0 + h, bar);
+                }
+                __syncwarp();
+                if (++st == a.stages) { st = 0; turn ^= 1; }
+            }
+        // copies under way end before shared memory is given back, whoever has given up
+        mbar_wait_bounded(a_bar, 0, a.wait_ns);
+        for (int k = it > a.stages ? it - a.stages : 0; k < it; ++k) mbar_wait_bounded(smem_u32(&sh.b_full[k % a.stages]), (k / a.stages) & 1, a.wait_ns);
+        __syncwarp();
+    } else {
+        // ---- products ----
+        const uint32_t idesc = la_idesc(kLxTile, N, false);
+        const uint64_t a_desc = smem_desc_sw128(a_at, 16, 1024), b_desc = smem_desc_sw128(b_at, 16, 1024);
+        const uint32_t hi = uint32_t(a_desc >> 32);
+        int st = 0, turn = 0;
+        bool any = false;
+        ok = wait(sh.a_full, 0);
+        for (int h = head0; h < head1 && ok; ++h) {
+            const int i = h - head0, buf = i & 1;
+            if (i >= 2 && !(ok = wait(sh.d_empty[buf], (i / 2 - 1) & 1))) break;
+            for (int c = 0; c < chunks; ++c) {
+                if (!(ok = wait(sh.b_full[st], turn))) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t d = tmem + buf * N, lo_a = uint32_t(a_desc) + c * (kLxChunkBytes >> 4), lo_b = uint32_t(b_desc) + st * (STAGE >> 4);
+                    if (c == 0) tc_mma_lo<false>(d, lo_a, hi, lo_b, hi, idesc);
+                    else tc_mma_lo<true>(d, lo_a, hi, lo_b, hi, idesc);
+                    tc_mma_lo<true>(d, lo_a + 2, hi, lo_b + 2, hi, idesc);
+                    tc_mma_lo<true>(d, lo_a + 4, hi, lo_b + 4, hi, idesc);
+                    tc_mma_lo<true>(d, lo_a + 6, hi, lo_b + 6, hi, idesc);
+                    tc_commit(smem_u32(&sh.b_empty[st]));
+                    if (c + 1 == chunks) tc_commit(smem_u32(&sh.d_full[buf]));
+                }
+                any = true;
+                __syncwarp();
+                if (++st == a.stages) { st = 0; turn ^= 1; }
+            }
+        }
+        if (any) {                               // products under way end before tensor memory is given back, whoever has given up
+            if (elect_one()) tc_commit(smem_u32(&sh.drained));
+            __syncwarp();
+            mbar_wait_bounded(smem_u32(&sh.drained), 0, 2'000'000'000ull);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 5) tmem_dealloc(tmem, 2 * N);
+}
+
+}  // namespace spm

@@ -1,0 +1,396 @@
+// Attention of prompts over keys and values that latent_expand_kernel has made, on tcgen05.
+//
+// A CTA takes 256 rows of a head of one sequence, two M = 128 halves, and walks the tokens in tiles of 128. A key is HD elements of its
+// head and a chunk of up to 64 that all heads share; keys and values come by TMA. One warp issues the products; four warps a half turn scores
+// into probabilities, one row a thread, while the tensor cores are at the other half: S(j) of one half, then P V(j) and S(j + 1) of the
+// other. Scores, probabilities (bf16, in the scores' place, as the A operand of the second product) and sums stay in tensor memory.
+//
+// A row's maximum is moved, and its sums scaled, only where a score is above it by more than 64 in powers of two: probabilities are
+// bf16, which has fp32's range, so nothing is lost before that. A probability, a key's first part and a value are rounded to bf16 once.
+#pragma once
+
+#include <cuda.h>
+
+#include "latent_expand.cuh"
+#include "mma_ops.cuh"
+#include "prompt_items.cuh"
+
+namespace spm {
+
+struct LatentPromptArgs {
+    LatentPool kv;              // (its status, sizes)
+    KvBatch batch;
+    HeadRows q, out;
+    int heads, h0;              // of this round, the first one's number
+    int tokens;                 // of the workspace
+    const uint32_t* there;
+    float factor;               // of scores: scale times log2(e)
+    unsigned long long wait_ns;
+    int withhold;
+};
+
+constexpr int kLpTile = 128;
+// two halves' softmax warps, then the copying warp, the issuing warp and two that only make its four whole. Registers a thread: 168 at the launch,
+// of which the last four give some to the softmax warps
+constexpr int kLpThreads = 12 * 32, kLpSoftmaxRegs = 216, kLpOtherRegs = 72;
+static_assert(2 * kLpSoftmaxRegs + kLpOtherRegs <= 3 * 168, "the split is what the launch has");
+template <int HD>
+struct LpShape {
+    static constexpr int chunk = kLpTile * 128;                          // 64 elements of 128 rows
+    static constexpr int k_chunks = HD / 64 + 1, v_chunks = HD / 64;
+    static constexpr int k_bytes = k_chunks * chunk, v_bytes = v_chunks * chunk;
+    static constexpr int v_stages = HD == 64 ? 2 : 1;                    // (what shared memory has room for)
+    static constexpr int smem = 1024 + 2 * k_bytes + 2 * k_bytes + v_stages * v_bytes;       // queries of two halves, two stages of keys, values
+};
+
+struct LpShared {
+    unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], drained;
+    uint32_t tmem;
+    int quit;
+    PfItem item;
+    LxPlace place;
+};
+
+// 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
+__device__ __forceinline__ uint32_t lp_chunk(int row, int ch) { return uint32_t((ch >> 3) * (kLpTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)); }
+
+template <int HD>
+__global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const LatentPromptArgs a, const __grid_constant__ CUtensorMap k_map,
+                                                                      const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap v_map) {
+    using S = LpShape<HD>;
+    extern __shared__ __align__(16) unsigned char raw_smem[];
+    const uint32_t q_at = (smem_u32(raw_smem) + 1023) & ~1023u, k_at = q_at + 2 * S::k_bytes, v_at = k_at + 2 * S::k_bytes;
+    __shared__ LpShared sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const KvBatch& b = a.batch;
+
+    grid_dep_wait();
+    grid_dep_launch();
+    const int head = blockIdx.x % a.heads, cap = b.stride * a.kv.page_size;
+    if (warp == 9) {
+        pf_find(b, nullptr, 1, cap, blockIdx.x / a.heads, sh.item);
+        __syncwarp();
+        const LxPlace p = lx_find(b, cap, a.tokens, sh.item.n > 0 ? sh.item.seq : 0, -1);
+        if (lane == 0) sh.place = p;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.k_full[i]), 1 + a.withhold); mbar_init(smem_u32(&sh.v_full[i]), 1);
+            mbar_init(smem_u32(&sh.k_empty[i]), 1); mbar_init(smem_u32(&sh.v_empty[i]), 1);
+            mbar_init(smem_u32(&sh.s_full[i]), 1); mbar_init(smem_u32(&sh.p_full[i]), 128); mbar_init(smem_u32(&sh.o_full[i]), 1);
+        }
+        mbar_init(smem_u32(&sh.drained), 1);
+        sh.quit = 0;
+        fence_barrier_init();
+    }
+    if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
+    __syncthreads();
+    const int rb = sh.item.rb, first = sh.item.first, n = sh.item.n, len = sh.item.len;
+    const int at = sh.place.at, there_are = n > 0 ? max(0, min(min(len, cap), sh.place.tokens)) : 0;     // tokens in the workspace
+    if (n == 0) {                                // more CTAs than items
+        tc_fence_before();
+        if (warp == 8) tmem_dealloc(sh.tmem, 512);
+        return;
+    }
+    if (len > there_are && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
+    // tiles of a half: up to the token that its last row sees
+    auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x) + 1, there_are)); };
+    const bool used1 = rb * kPfCols + kLpTile < n;
+    const int tiles0 = (sees(rb * kPfCols + kLpTile - 1) + kLpTile - 1) / kLpTile;
+    const int tiles1 = used1 ? (sees(rb * kPfCols + kPfCols - 1) + kLpTile - 1) / kLpTile : 0;
+    const int tiles = max(tiles0, tiles1);
+
+    // a warp goes on, or gives up, as one
+    auto wait = [&](const unsigned long long& bar, int parity) {
+        const uint32_t w = smem_u32(&bar);
+        if (__all_sync(0xffffffffu, mbar_try_wait(w, parity))) return true;
+        const unsigned long long t0 = global_timer_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 32; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(w, parity))) return true;
+            const bool late = global_timer_ns() - t0 > a.wait_ns;
+            if (late) {
+                *reinterpret_cast<volatile int*>(&sh.quit) = 1;
+                kv_note(a.kv, SPM_KV_TIMEOUT);
+            }
+            if (__any_sync(0xffffffffu, late || *reinterpret_cast<volatile int*>(&sh.quit))) return false;
+        }
+    };
+    uint32_t tmem = 0, t_s = 0, t_o = 0;
+    auto together = [&] {                        // queries, barriers and tensor memory are there
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        tmem = t_s = sh.tmem;
+        t_o = tmem + 256;
+    };
+
+    if (warp < 8) {
+        more_registers<kLpSoftmaxRegs>();
+        // ---- queries: a warp brings its 32 rows, a row at a time; then a lane has a row ----
+        const int half = warp >> 2, row_in = tid & 127, i_row = rb * kPfCols + tid;
+        const int row = i_row < n && first + i_row >= 0 && first + i_row < b.n_rows ? first + i_row : -1;
+        const int limit = i_row < n ? sees(i_row) : 0;
+        const __nv_bfloat16* src = row < 0 ? nullptr : static_cast<const __nv_bfloat16*>(a.q.p) + row * a.q.row + (a.h0 + head) * a.q.head;
+        const int vectors = (HD + a.kv.rope) / 8;
+#pragma unroll 4
+        for (int i = 0; i < 32; ++i) {
+            const auto* from = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i));
+            if (lane < vectors) copy16_or_zero(q_at + half * S::k_bytes + lp_chunk((row_in & ~31) + i, lane), from ? from + lane * 8 : static_cast<const __nv_bfloat16*>(a.q.p), from != nullptr);
+        }
+        copies_arrived();
+        fence_proxy_async();
+        together();
+        // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
+        const int own_tiles = half == 0 ? tiles0 : tiles1;
+        const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
+        const float f = fmaxf(fabsf(a.factor), 0x1p-126f);        // (not zero: masked scores are -infinity)
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = 0; j < own_tiles && ok; ++j) {
+            uint32_t there[4];
+            bool whole = (j + 1) * kLpTile <= limit;
+            {
+                const uint4 w = *reinterpret_cast<const uint4*>(a.there + (at + j * kLpTile) / 32);
+                there[0] = w.x; there[1] = w.y; there[2] = w.z; there[3] = w.w;
+            }
+            whole &= (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu;
+            whole = __all_sync(0xffffffffu, whole);
+            if (!(ok = wait(sh.s_full[half], j & 1))) break;
+            tc_fence_after();
+            if (!whole)                          // tokens that this row sees
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int left = limit - j * kLpTile - 32 * i;
+                    if (left < 32) there[i] &= left <= 0 ? 0u : (1u << left) - 1;
+                }
+            uint32_t r[4][32];
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_at + 32 * ch, r[ch]);
+            tmem_wait_ld();
+            if (a.factor < 0.f)
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[ch][i] ^= 0x80000000u;
+            if (!whole)
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!(there[ch] >> i & 1)) r[ch][i] = 0xff800000u;
+            float tops[4];
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) {
+                tops[ch] = __uint_as_float(r[ch][0]);
+#pragma unroll
+                for (int i = 1; i < 32; ++i) tops[ch] = fmaxf(tops[ch], __uint_as_float(r[ch][i]));
+            }
+            const float peak = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            if (__any_sync(0xffffffffu, m == -INFINITY || (peak - m) * f > kLaSlack)) {
+                // (scores of a query with an infinity may all be -infinity, as those of tokens that it does not see are: NaN)
+                if (m == -INFINITY && peak == -INFINITY && (there[0] | there[1] | there[2] | there[3])) l = __int_as_float(0x7fffffff);
+                const float to = fmaxf(m, peak), by = m == -INFINITY ? 1.f : ex2((m - to) * f);
+                m = to;
+                l *= by;
+                if (j > 0) {                     // (before that the sums hold nothing)
+#pragma unroll 1
+                    for (int ch = 0; ch < HD / 16; ++ch) {
+                        uint32_t o[16];
+                        tmem_ld16_raw(o_at + 16 * ch, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
+                        tmem_st16(o_at + 16 * ch, o);
+                    }
+                }
+            }
+            const float base = m == -INFINITY ? 0.f : -m * f;
+            const unsigned long long base2 = two_floats(base, base), f2 = two_floats(f, f);
+            unsigned long long sum0 = 0, sum1 = 0;
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) {
+                uint32_t p[16];
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    float x0, x1;
+                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, base2), x0, x1);
+                    const float p0 = ex2(x0), p1 = ex2(x1);
+                    unsigned long long& sum = i & 2 ? sum1 : sum0;
+                    sum = add2(sum, two_floats(p0, p1));
+                    p[i / 2] = pack_bf16(p0, p1);
+                }
+                tmem_st16(s_at + 16 * ch, p);
+            }
+            {
+                float x0, x1;
+                floats_of(add2(sum0, sum1), x0, x1);
+                l += x0 + x1;
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&sh.p_full[half]));
+        }
+        if (own_tiles > 0 && ok) ok = wait(sh.o_full[half], 0);
+        tc_fence_after();
+        if (ok) {
+            // the rows go out by way of the half's queries' place, HD / 8 lanes a row
+            constexpr int LANES = HD / 8, AT_ONCE = 32 / LANES;
+            const float by = l == 0.f ? 0.f : 1.f / l;
+            const uint32_t rows_at = q_at + half * S::k_bytes + (row_in & ~31) * (HD * 2);
+#pragma unroll 1
+            for (int ch = 0; ch < HD / 32; ++ch) {
+                uint32_t r[32];
+                if (own_tiles > 0) {
+                    tmem_ld32(o_at + 32 * ch, r);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(r[i + k]) * by;
+                    st_shared16(rows_at + lane * (HD * 2) + ((ch * 4 + i / 8 ^ lane & LANES - 1) << 4),
+                                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
+                }
+            }
+            __syncwarp();
+            __nv_bfloat16* to = row < 0 ? nullptr : static_cast<__nv_bfloat16*>(a.out.p) + row * a.out.row + (a.h0 + head) * a.out.head;
+#pragma unroll 4
+            for (int k = 0; k < LANES; ++k) {
+                const int i = k * AT_ONCE + lane / LANES;
+                auto* dst = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), i));
+                const uint4 v = lds128(rows_at + i * (HD * 2) + ((lane % LANES ^ i & LANES - 1) << 4));
+                if (dst) *reinterpret_cast<uint4*>(dst + lane % LANES * 8) = v;
+            }
+        }
+    } else {
+        fewer_registers<kLpOtherRegs>();
+        bool ok = true;
+        if (warp == 9) {
+            // ---- keys and values on their way in (they need no queries: begun before the others are ready) ----
+            const int row0 = head * a.tokens + at;
+            auto keys = [&](int j) {
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&sh.k_full[j & 1]), to = k_at + (j & 1) * S::k_bytes;
+                    mbar_arrive_expect_tx(bar, S::k_bytes);
+                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, row0 + j * kLpTile, bar);
+                    tma_rows(to + HD / 64 * S::chunk, &rope_map, 0, at + j * kLpTile, bar);
+                }
+                __syncwarp();
+            };
+            auto values = [&](int j) {
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&sh.v_full[j % S::v_stages]), to = v_at + j % S::v_stages * S::v_bytes;
+                    mbar_arrive_expect_tx(bar, S::v_bytes);
+                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &v_map, c * 64, row0 + j * kLpTile, bar);
+                }
+                __syncwarp();
+            };
+            int k_sent = 0, v_sent = 0;
+            if (tiles > 0) { keys(0); values(0); k_sent = v_sent = 1; }
+            together();
+            for (int j = 0; j < tiles; ++j) {
+                if (j + 1 < tiles) {             // (their place is free before that of the values is)
+                    if (j + 1 >= 2 && !(ok = wait(sh.k_empty[(j + 1) & 1], ((j + 1) / 2 - 1) & 1))) break;
+                    keys(j + 1);
+                    ++k_sent;
+                }
+                if (j > 0) {
+                    if (j >= S::v_stages && !(ok = wait(sh.v_empty[j % S::v_stages], (j / S::v_stages - 1) & 1))) break;
+                    values(j);
+                    ++v_sent;
+                }
+            }
+            // copies under way end before shared memory is given back, whoever has given up
+            for (int j = max(0, k_sent - 2); j < k_sent; ++j) mbar_wait_bounded(smem_u32(&sh.k_full[j & 1]), j / 2 & 1, a.wait_ns);
+            for (int j = max(0, v_sent - S::v_stages); j < v_sent; ++j) mbar_wait_bounded(smem_u32(&sh.v_full[j % S::v_stages]), j / S::v_stages & 1, a.wait_ns);
+        } else {
+            together();
+            // ---- products. The warp walks as one, so that the elected lane is one lane throughout ----
+            if (warp == 8) {
+                constexpr uint32_t idesc_s = la_idesc(kLpTile, kLpTile, false);
+                constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (uint32_t(HD >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+                const int rope_steps = a.kv.rope / 16;
+                const uint64_t q_desc = smem_desc_sw128(q_at, 16, 1024), k_desc = smem_desc_sw128(k_at, 16, 1024), v_desc = smem_desc_sw128(v_at, S::chunk, 1024);
+                const uint32_t hi = uint32_t(q_desc >> 32);
+                auto scores = [&](int h, int j) {
+                    if (elect_one()) {
+                        const uint32_t d = t_s + h * 128, lo_q = uint32_t(q_desc) + h * (S::k_bytes >> 4), lo_k = uint32_t(k_desc) + (j & 1) * (S::k_bytes >> 4);
+#pragma unroll
+                        for (int k = 0; k < HD / 16; ++k) {
+                            const uint32_t off = (k / 4) * (S::chunk >> 4) + (k % 4) * 2;
+                            if (k == 0) tc_mma_lo<false>(d, lo_q, hi, lo_k, hi, idesc_s);
+                            else tc_mma_lo<true>(d, lo_q + off, hi, lo_k + off, hi, idesc_s);
+                        }
+                        for (int k = 0; k < rope_steps; ++k) {
+                            const uint32_t off = HD / 64 * (S::chunk >> 4) + k * 2;
+                            tc_mma_lo<true>(d, lo_q + off, hi, lo_k + off, hi, idesc_s);
+                        }
+                        tc_commit(smem_u32(&sh.s_full[h]));
+                    }
+                    __syncwarp();
+                };
+                auto sums = [&](int h, int j) {
+                    if (elect_one()) {
+                        const uint64_t v = v_desc + uint64_t(j % S::v_stages * (S::v_bytes >> 4));
+#pragma unroll
+                        for (int k = 0; k < kLpTile / 16; ++k) tc_mma_f16_ts(t_o + h * HD, t_s + h * 128 + 8 * k, v + uint64_t(k * 128), idesc_o, j > 0 || k > 0);
+                    }
+                    __syncwarp();
+                };
+                auto signal = [&](unsigned long long& bar) {
+                    if (elect_one()) tc_commit(smem_u32(&bar));
+                    __syncwarp();
+                };
+                const int count[2] = {tiles0, tiles1};
+                bool any = false;
+                ok = tiles == 0 || wait(sh.k_full[0], 0);
+                tc_fence_after();
+                if (ok && tiles > 0) {
+                    any = true;
+                    for (int h = 0; h < 2; ++h)
+                        if (count[h] > 0) scores(h, 0);
+                    signal(sh.k_empty[0]);
+                }
+                for (int j = 0; ok && j < tiles; ++j) {
+                    const int vs = j % S::v_stages;
+                    bool keys = false;           // of the next tile have been waited for
+                    if (!(ok = wait(sh.v_full[vs], j / S::v_stages & 1))) break;
+                    for (int h = 0; h < 2; ++h) {
+                        if (j < count[h]) {
+                            if (!(ok = wait(sh.p_full[h], j & 1))) break;
+                            tc_fence_after();
+                            sums(h, j);
+                            if (j + 1 == count[h]) signal(sh.o_full[h]);
+                        }
+                        if (h == 1) signal(sh.v_empty[vs]);      // (ahead of the next scores)
+                        if (j + 1 < count[h]) {
+                            if (!keys && !(ok = wait(sh.k_full[(j + 1) & 1], (j + 1) / 2 & 1))) break;
+                            keys = true;
+                            tc_fence_after();
+                            scores(h, j + 1);
+                        }
+                    }
+                    if (!ok) break;
+                    if (j + 1 < tiles) signal(sh.k_empty[(j + 1) & 1]);
+                }
+                if (any) {                       // products under way end before tensor memory is given back, whoever has given up
+                    signal(sh.drained);
+                    mbar_wait_bounded(smem_u32(&sh.drained), 0, 2'000'000'000ull);
+                    __syncwarp();
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace spm

@@ -68,6 +68,19 @@ inline bool make_token_map(CUtensorMap* map, const void* base, int D, uint64_t r
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// bf16 matrices [n][rows][D], rows and matrices apart; a box is 64 elements x all rows of a matrix, 128-byte swizzle.
+inline bool make_matrix_map(CUtensorMap* map, const void* base, int D, int rows, int n, uint64_t row_stride, uint64_t stride) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {cuuint64_t(D), cuuint64_t(rows), cuuint64_t(n)};
+    const cuuint64_t strides[2] = {row_stride * 2, stride * 2};
+    const cuuint32_t box[3] = {64, cuuint32_t(rows), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Packed 4-bit expert blobs [n_slots][I][3][RB bytes] (RB = D/2 nibble bytes + D/16 scale bytes per
 // row) viewed as a 4-D byte tensor (RB, 3, I, n_slots). Two box shapes over the same memory:
 // 64 nibble bytes (128 weights) x 128 rows with the 64-byte swizzle, and 16 scale bytes x 128 rows.

@@ -1,7 +1,7 @@
 """Attention with keys and values from one latent vector a token, on torch tensors: a paged bf16 cache of latent rows, the products of
 every head around it, attention over it.
 
-Marshals to spm_latent_write, spm_head_product and spm_latent_attend (include/spm.h says what they compute). Batches, rotations, streams,
+Marshals to spm_latent_write, spm_head_product, spm_latent_attend and spm_latent_attend_expanded (include/spm.h says what they compute). Batches, rotations, streams,
 graphs, outputs and workspaces are as in kv_cache.py. A decode step's attention, with w [heads, 2 * head, latent] the matrix that makes keys
 and values from latent vectors, w_k = w[:, :head] and w_v = w[:, head:]:
 
@@ -9,6 +9,8 @@ and values from latent vectors, w_k = w[:, :head] and w_v = w[:, head:]:
     head_product(q_plain, w_k, out=q[..., :latent])
     cache.write(batch, latents, keys, q=q_turning, positions=positions, rope=rope, q_out=q[..., latent:])
     out = head_product(cache.attend(batch, q, scale), w_v, transposed=True)
+
+A prompt's: cache.write, with q turned in place, then cache.attend_expanded(batch, q, w_k, w_v, scale, n_tokens).
 """
 from __future__ import annotations
 
@@ -104,6 +106,31 @@ class LatentCache:
             work_size = self._workspace[key] = B.spm_latent_attend_workspace(self.c, batch.c, heads, dt)
         work = torch.empty(work_size, dtype=torch.uint8, device=device)
         _enqueue(device, self._lib.spm_latent_attend, self.c, batch.c, cq, heads, co, scale, dt, work.data_ptr(), work_size)
+        return out
+
+    def attend_expanded(self, batch, q, w_k, w_v, scale, n_tokens, out=None):
+        """The same attention for prompts, in bf16, of whole queries q [rows, heads, head + rope_dim]: keys and values are made from the cache by w_k and
+        w_v [heads, head, latent_dim]; returns [rows, heads, head]. n_tokens: at least the tokens of all sequences together (the sum of
+        their lengths, their new rows included), which the host knows: room for their keys and values."""
+        self._on(batch, "batch")
+        n, device = batch.n_rows, self.device
+        dt, dtype = _dtype(q, "q"), q.dtype
+        heads, size = q.shape[1], q.shape[2] - self.rope_dim
+        cq = _rows(q, n, heads, size + self.rope_dim, dtype, device, "q")
+        matrices = []
+        for w, what in ((w_k, "w_k"), (w_v, "w_v")):
+            if w.shape != (heads, size, self.latent_dim) or w.dtype is not torch.bfloat16 or w.device != device or w.stride(2) != 1:
+                raise ValueError(f"{what}: bf16 [{heads}, {size}, {self.latent_dim}] on {device}, rows contiguous")
+            matrices.append(B.Matrices(w.data_ptr(), w.stride(0), w.stride(1)))
+        if out is None:
+            out = q.new_empty(n, heads, size)
+            co = B.Rows(out.data_ptr(), heads * size, size)
+        else:
+            co = _rows(out, n, heads, size, dtype, device, "out")
+        work_size = B.spm_latent_attend_expanded_workspace(self.c, batch.c, heads, size, n_tokens, dt)
+        work = torch.empty(work_size, dtype=torch.uint8, device=device)
+        _enqueue(device, self._lib.spm_latent_attend_expanded, self.c, batch.c, cq, *matrices, heads, size, co, scale, n_tokens, dt,
+                 work.data_ptr(), work_size)
         return out
 
 

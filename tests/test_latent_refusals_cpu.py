@@ -114,6 +114,40 @@ def test_write_ropes(B):
     refused(B, call(B.Rope(*good), positions=None), -1, "positions")
 
 
+def expanded(B, kv=None, b=None, heads=16, head=128, n_tokens=100, dtype=1, scale=0.1, q=None, out=None, w_k=None, w_v=None, work=AT, size=1 << 50):
+    q, out = q or B.Rows(AT, 16 * 192, 192), out or B.Rows(2 * AT, 16 * 128, 128)
+    w_k, w_v = w_k or B.Matrices(AT, 256 * 512, 512), w_v or B.Matrices(AT, 256 * 512, 512)
+    return lambda: B.spm_latent_attend_expanded(kv or cache(B), b or batch(B), q, w_k, w_v, heads, head, out, scale, n_tokens, dtype, work, size)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(dtype=0), -2, "absorbed"), (dict(dtype=2), -2, "fp32 or bf16"), (dict(heads=0), -2, "heads"), (dict(head=96), -2, "head_dim"), (dict(head=256), -2, "head_dim"),
+    (dict(n_tokens=-1), -1, "n_tokens"), (dict(n_tokens=2 ** 30 + 1), -1, "n_tokens"), (dict(scale=float("inf")), -1, "scale"),
+    (dict(work=None), -1, "workspace"), (dict(work=AT + 128), -1, "workspace"), (dict(size=1000), -1, "workspace"),
+])
+def test_expanded(B, kw, code, word):
+    refused(B, expanded(B, **kw), code, word)
+
+
+def test_expanded_structs(B):
+    for change, code, word in SHAPES + POINTERS:
+        refused(B, expanded(B, kv=cache(B, **change)), code, word)
+    for change, word in BATCHES:
+        refused(B, expanded(B, b=batch(B, **change)), -1, word)
+    for bad in (B.Rows(None, 9216, 576), B.Rows(AT + 8, 9216, 576), B.Rows(AT, 9217, 576)):
+        refused(B, expanded(B, q=bad), -1, "null" if bad.p is None else "boundaries")
+        refused(B, expanded(B, out=bad), -1, "null" if bad.p is None else "boundaries")
+    refused(B, expanded(B, out=B.Rows(AT, 16 * 192, 192)), -1, "place")
+    for bad in (B.Matrices(None, 65536, 512), B.Matrices(AT + 8, 65536, 512), B.Matrices(AT, 65540, 512), B.Matrices(AT, 65536, 516), B.Matrices(AT, 65536, 0),
+                B.Matrices(AT, -65536, 512)):
+        refused(B, expanded(B, w_k=bad), -1, "w_k")
+        refused(B, expanded(B, w_v=bad), -1, "w_v")
+    expanded(B, b=batch(B, n_rows=0))()
+    with pytest.raises(B.SpmError):
+        B.spm_latent_attend_expanded_workspace(cache(B), batch(B), 16, 100, 10, 1)
+    assert B.spm_latent_attend_expanded_workspace(cache(B), batch(B), 16, 128, 1000, 1) >= 1000 * 16 * 128 * 4
+
+
 @pytest.mark.parametrize("size,to,code,word", [(0, 64, -2, "in_dim"), (96, 64, -2, "in_dim"), (64, 96, -2, "out_dim"), (64, 8256, -2, "out_dim")])
 def test_product_sizes(B, size, to, code, word):
     x, y = B.Rows(AT, 9216, 576), B.Rows(2 * AT, 9216, 576)
