@@ -2,7 +2,7 @@
 //
 // A column is a head of a new row: column x of a sequence is head x % heads of row x / heads. A CTA takes COLS columns and walks their
 // tokens 64 at a time. Both products have the cache's rows as their A operand, where they lie, and columns as N, so that few columns cost
-// few cycles: scores S^T [64 tokens][columns] = C q^T, the rows K-major, and sums O^T [latent][columns] += C^T P^T, the same bytes M-major.
+// few cycles: scores S^T [tokens][columns] = C q^T, the rows K-major, and sums O^T [latent][columns] += C^T P^T, the same bytes M-major.
 // S^T, in two buffers, and O^T, latent / 128 tiles, are in tensor memory. Every byte of a row comes to the SM once, for both.
 //
 // A warp brings tiles by TMA (64 elements of a page's rows a copy, swizzled) into a ring of as many stages as there is room for; one issues
@@ -63,13 +63,18 @@ struct LaShape {
     static constexpr int part_floats(int latent) { return COLS * (latent + 2); }     // sums, then maxima, then sums of probabilities
 };
 constexpr int kLaOwnBytes = 2048;                            // LaShared below
-constexpr int la_smem(int fixed, int chunks, int stages) { return fixed + chunks * stages * kLaChunkBytes; }
 
 
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int element, int row, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(map), "r"(element), "r"(row), "r"(bar) : "memory");
+}
+// the same for rows that nobody else reads
+__device__ __forceinline__ void tma_rows_once(uint32_t dst, const CUtensorMap* map, int element, int row, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+        ::"r"(dst), "l"(map), "r"(element), "r"(row), "r"(bar), "l"(policy) : "memory");
 }
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -331,6 +336,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
             }
         };
         float* red = reinterpret_cast<float*>(raw_smem + (p_at - smem_u32(raw_smem)));       // [4 warps][COLS], in the probabilities' place
+        long long* to_of = reinterpret_cast<long long*>(red + 4 * COLS);         // [COLS]
         while (w.left > 0 && ok) {
             const int half = item & 1;
             // ---- this item's columns: a warp brings every fourth ----
@@ -524,9 +530,15 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     part[COLS * latent + tid] = total == 0.f ? -INFINITY : total == total ? red[tid] : INFINITY;
                     part[COLS * latent + COLS + tid] = total;
                 }
-            } else if (tid < COLS) red[tid] = total == 0.f ? 0.f : 1.f / total;
+            } else if (tid < COLS) {             // where the column's result goes (-1: nowhere), and what it is scaled by
+                const int x = w.group * COLS + tid, row_in = la_row(a, x), row = w.s.first + row_in;
+                const bool is = row_in < w.s.n && row >= 0 && row < a.batch.n_rows;
+                red[tid] = total == 0.f ? 0.f : 1.f / total;
+                to_of[tid] = is ? row * a.out.row + (x - row_in * a.heads) * a.out.head : -1;
+            }
             together();
-            // a part: four columns of an element side by side, elements behind each other
+            // a part: four columns of an element side by side, elements behind each other. A result: an element a thread, in bf16 two of one column of
+            // each two
             if (w.tiles > 0 || whole) {
 #pragma unroll 1
                 for (int ch = 0; ch < COLS / 16; ++ch)
@@ -552,13 +564,18 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                                 continue;
                             }
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const int col = ch * 16 + i + k, x = w.group * COLS + col, row_in = la_row(a, x), h = x - row_in * a.heads, row = w.s.first + row_in;
-                                if (row_in >= w.s.n || row < 0 || row >= a.batch.n_rows) continue;
-                                T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d;
-                                const float y = v[k] * red[col];
-                                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(y);
-                                else *to = y;
+                            for (int k = 0; k < 4; k += sizeof(T) == 2 ? 2 : 1) {
+                                const int col = ch * 16 + i + k;
+                                if constexpr (sizeof(T) == 2) {
+                                    const float x = v[k] * red[col], y = v[k + 1] * red[col + 1];
+                                    const bool odd = lane & 1;
+                                    const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+                                    const long long at = to_of[col + odd];
+                                    if (at >= 0) *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out.p) + at + (d & ~1)) = odd ? pack_bf16(got, y) : pack_bf16(x, got);
+                                } else {
+                                    const long long at = to_of[col];
+                                    if (at >= 0) static_cast<T*>(a.out.p)[at + d] = v[k] * red[col];
+                                }
                             }
                         }
                     }
@@ -572,6 +589,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         // ---- tiles on their way in ----
         int st = 0, turn = 0;
         unsigned it = 0;
+        const uint64_t once = policy_evict_first();          // (262145 tokens of 16 heads: TODO us without)
         int4 join = make_int4(0, 0, 0, 0);
         long long joined = 0;
         while (w.left > 0 && ok) {
@@ -601,9 +619,12 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     mbar_arrive_expect_tx(bar, __popc(there) * a.box * 128 * chunks);
                 }
                 __syncwarp();
-                if (row >= 0)                    // (a lane's copy is the same in each round)
-                    for (int k = lane; k < copies * chunks; k += 32)
-                        tma_rows(to + k / copies * kLaChunkBytes + copy * a.box * 128, &rows_map, k / copies * 64, row, bar);
+                if (row >= 0)                    // (a lane's copy is the same for each of its chunks)
+                    for (int c = lane / copies; c < chunks; c += 32 / copies) {
+                        const uint32_t at = to + c * kLaChunkBytes + copy * a.box * 128;
+                        if (w.s.blocks == 1) tma_rows_once(at, &rows_map, c * 64, row, bar, once);
+                        else tma_rows(at, &rows_map, c * 64, row, bar);
+                    }
                 __syncwarp();
                 row = row_of(j + 1, page);
                 page = page_then;
@@ -721,6 +742,7 @@ __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const Laten
     __shared__ int owners[kLaMaxCtas], n_owners;
     __shared__ __align__(16) float weights[WARPS][kLaMaxCtas][4];
     __shared__ float4 sums[WARPS][32];
+    __shared__ float tops[WARPS][4], totals[WARPS][4];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dep_wait();
     grid_dep_launch();
@@ -747,44 +769,68 @@ __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const Laten
         const float* parts = a.parts + size_t(owner) * 2 * each;
         auto part = [&](int j) { return parts + (j == 0 ? 1 : 2 * j) * each; };
         // lane (j, k): maxima and sums of every eighth part's column k
-        constexpr int EACH = (kLaMaxCtas + 7) / 8;
+        // this warp's parts: every one, or every eighth. Lane (i, k): maxima and sums of column k
+        const int from = together ? warp : 0, mine = from < join.x ? (join.x - from + step - 1) / step : 0;
         const int k = lane & 3, end_at = COLS * latent + quad * 4 + k;
-        float m[EACH], l[EACH], top = -INFINITY, sum = 0.f;
+        float top = -INFINITY, sum = 0.f;
+        for (int i0 = lane >> 2; i0 < mine; i0 += 32) {
+            float m[4], l[4];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int j = i * 8 + (lane >> 2);
-            m[i] = j < join.x ? part(j)[end_at] : -INFINITY;
-            l[i] = j < join.x ? part(j)[end_at + COLS] : 0.f;
+            for (int u = 0; u < 4; ++u) {
+                const bool is = i0 + 8 * u < mine;
+                const float* at = part(from + (is ? i0 + 8 * u : 0) * step) + end_at;
+                m[u] = is ? at[0] : -INFINITY;
+                l[u] = is ? at[COLS] : 0.f;
+            }
+            float to = top;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) to = fmaxf(to, m[u]);
+            if (sum != 0.f) sum *= ex2(top - to);
+            top = to;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (m[u] != -INFINITY) sum += l[u] * ex2(m[u] - to);
+                if (i0 + 8 * u < mine) weights[warp][i0 + 8 * u][k] = m[u];
+            }
         }
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) top = fmaxf(top, m[i]);
+        const float own = top;
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int j = i * 8 + (lane >> 2);
-            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - top);
-            if (by != 0.f) sum += by * l[i];
-            if (j < join.x) weights[warp][j][k] = by;
-        }
+        if (sum != 0.f) sum *= ex2(own - top);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        for (int i = lane >> 2; i < mine; i += 8) {
+            const float m = weights[warp][i][k];
+            weights[warp][i][k] = m == -INFINITY ? 0.f : ex2(m - top);
+        }
         __syncwarp();
         float o[4] = {};
 #pragma unroll 8
-        for (int j = together ? warp : 0; j < join.x; j += step) {
-            const float4 v = *reinterpret_cast<const float4*>(part(j) + ((d / 128 * (COLS / 4) + quad) * 128 + d % 128) * 4);
-            const float4 by = *reinterpret_cast<const float4*>(weights[warp][j]);
+        for (int i = 0; i < mine; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(part(from + i * step) + ((d / 128 * (COLS / 4) + quad) * 128 + d % 128) * 4);
+            const float4 by = *reinterpret_cast<const float4*>(weights[warp][i]);
             // (a part that saw nothing has written no sums)
             o[0] += by.x == 0.f ? 0.f : by.x * v.x; o[1] += by.y == 0.f ? 0.f : by.y * v.y;
             o[2] += by.z == 0.f ? 0.f : by.z * v.z; o[3] += by.w == 0.f ? 0.f : by.w * v.w;
         }
-        if (together) {
+        if (together) {                          // the warps' sums, by their maxima
+            if (lane < 4) { tops[warp][lane] = top; totals[warp][lane] = sum; }
             sums[warp][lane] = make_float4(o[0], o[1], o[2], o[3]);
             __syncthreads();
             if (warp == 0) {
 #pragma unroll
-                for (int u = 1; u < WARPS; ++u) { const float4 v = sums[u][lane]; o[0] += v.x; o[1] += v.y; o[2] += v.z; o[3] += v.w; }
+                for (int i = 0; i < 4; ++i) {
+                    float most = -INFINITY, total = 0.f, y = 0.f;
+#pragma unroll
+                    for (int u = 0; u < WARPS; ++u) most = fmaxf(most, tops[u][i]);
+#pragma unroll
+                    for (int u = 0; u < WARPS; ++u) {
+                        const float by = tops[u][i] == -INFINITY ? 0.f : ex2(tops[u][i] - most);
+                        if (by != 0.f) { total += by * totals[u][i]; y += by * reinterpret_cast<const float*>(&sums[u][lane])[i]; }
+                    }
+                    o[i] = y;
+                    if (k == i) sum = total;
+                }
             }
             __syncthreads();
         }

@@ -58,14 +58,18 @@ constexpr size_t kLaJoinBytes = (kLaMaxCtas * sizeof(int4) + 255) / 256 * 256;
 size_t attend_bytes(int cols, int latent) { return kLaJoinBytes + kLaMaxCtas * 2 * size_t(cols) * (latent + 2) * sizeof(float); }
 
 template <typename T, int COLS>
-cudaError_t launch_attend(LatentAttendArgs a, const CUtensorMap& map, int dev, int sms, cudaStream_t st) {
+cudaError_t launch_attend(LatentAttendArgs a, int dev, int sms, cudaStream_t st) {
+    const int page_size = a.kv.page_size;
     using S = LaShape<T, COLS>;
     cudaError_t e = allow_smem<latent_attend_kernel<T, COLS>>(dev, kMaxSmem);
     if (e != cudaSuccess) return e;
-    const int fixed = kLaOwnBytes + S::fixed(a.chunks);
-    a.stages = std::min(kLaMaxStages, (kMaxSmem - fixed) / (a.chunks * kLaChunkBytes));
+    const int fixed = kLaOwnBytes + S::fixed(a.chunks), stage = a.chunks * kLaChunkBytes;
+    a.stages = std::min(kLaMaxStages, (kMaxSmem - fixed) / stage);
+    a.box = page_size % 64 == 0 ? 64 : page_size % 32 == 0 ? 32 : 16;
+    CUtensorMap map{};                           // (a pool without pages: no copy is made)
+    if (a.kv.n_pages > 0 && !make_token_map(&map, a.kv.rows, a.kv.latent + a.kv.rope, uint64_t(a.kv.n_pages) * page_size, a.box)) return cudaErrorInvalidValue;
     const int ctas = std::min(sms, kLaMaxCtas);
-    e = launch_early(latent_attend_kernel<T, COLS>, ctas, kLaThreads, la_smem(fixed, a.chunks, a.stages), st, a, map);
+    e = launch_early(latent_attend_kernel<T, COLS>, ctas, kLaThreads, fixed + a.stages * stage, st, a, map);
     return e == cudaSuccess ? launch_early(latent_join_kernel<T, COLS>, kLaJoinBlocks, kLaJoinThreads, 0, st, a, ctas) : e;
 }
 
@@ -220,21 +224,17 @@ int spm_latent_attend(const spm_latent_cache* kv, const spm_kv_batch* batch, con
     a.heads_shift = 31 + bits;
     a.heads_times = uint32_t(((1ull << a.heads_shift) + n_heads - 1) / n_heads);
     a.chunks = kv->latent_dim / 64 + 1;
-    a.box = kv->page_size % 64 == 0 ? 64 : kv->page_size % 32 == 0 ? 32 : 16;
     a.factor = factor;
     a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     a.withhold = g_withhold.load(std::memory_order_relaxed);
     a.joins = static_cast<int4*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kLaJoinBytes);
-    CUtensorMap map{};                           // (a pool without pages: no copy is made)
-    if (kv->n_pages > 0 && !make_token_map(&map, kv->rows, kv->latent_dim + kv->rope_dim, uint64_t(kv->n_pages) * kv->page_size, a.box))
-        return fail(call, SPM_ERR_CUDA, "no tensor map of the cache's rows");
     const auto st = static_cast<cudaStream_t>(stream);
-    if (dtype == SPM_DTYPE_FP32) e = launch_attend<float, 16>(a, map, dev, sms, st);
-    else if (cols == 16) e = launch_attend<__nv_bfloat16, 16>(a, map, dev, sms, st);
-    else if (cols == 32) e = launch_attend<__nv_bfloat16, 32>(a, map, dev, sms, st);
-    else if (cols == 48) e = launch_attend<__nv_bfloat16, 48>(a, map, dev, sms, st);
-    else e = launch_attend<__nv_bfloat16, 64>(a, map, dev, sms, st);
+    if (dtype == SPM_DTYPE_FP32) e = launch_attend<float, 16>(a, dev, sms, st);
+    else if (cols == 16) e = launch_attend<__nv_bfloat16, 16>(a, dev, sms, st);
+    else if (cols == 32) e = launch_attend<__nv_bfloat16, 32>(a, dev, sms, st);
+    else if (cols == 48) e = launch_attend<__nv_bfloat16, 48>(a, dev, sms, st);
+    else e = launch_attend<__nv_bfloat16, 64>(a, dev, sms, st);
     return launched(call, e);
 }
 

@@ -32,7 +32,7 @@ struct LatentPromptArgs {
 constexpr int kLpTile = 128;
 // two halves' softmax warps, then the copying warp, the issuing warp and two that only make its four whole. Registers a thread: 168 at the launch,
 // of which the last four give some to the softmax warps
-constexpr int kLpThreads = 12 * 32, kLpSoftmaxRegs = 216, kLpOtherRegs = 72;
+constexpr int kLpThreads = 12 * 32, kLpSoftmaxRegs = 208, kLpOtherRegs = 88;
 static_assert(2 * kLpSoftmaxRegs + kLpOtherRegs <= 3 * 168, "the split is what the launch has");
 template <int HD>
 struct LpShape {
@@ -148,14 +148,12 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         const float f = fmaxf(fabsf(a.factor), 0x1p-126f);        // (not zero: masked scores are -infinity)
         float m = -INFINITY, l = 0.f;
         bool ok = true;
+        const uint4* bits = reinterpret_cast<const uint4*>(a.there + at / 32);
+        uint4 bits_then = own_tiles > 0 ? bits[0] : make_uint4(0, 0, 0, 0);
         for (int j = 0; j < own_tiles && ok; ++j) {
-            uint32_t there[4];
-            bool whole = (j + 1) * kLpTile <= limit;
-            {
-                const uint4 w = *reinterpret_cast<const uint4*>(a.there + (at + j * kLpTile) / 32);
-                there[0] = w.x; there[1] = w.y; there[2] = w.z; there[3] = w.w;
-            }
-            whole &= (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu;
+            uint32_t there[4] = {bits_then.x, bits_then.y, bits_then.z, bits_then.w};
+            if (j + 1 < own_tiles) bits_then = bits[j + 1];
+            bool whole = (j + 1) * kLpTile <= limit && (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu;
             whole = __all_sync(0xffffffffu, whole);
             if (!(ok = wait(sh.s_full[half], j & 1))) break;
             tc_fence_after();
