@@ -1,6 +1,6 @@
 // y_h = x_h W_h or x_h W_h^T for every head h of every row: what stands before and behind attention over latent rows.
 //
-// A CTA takes 64 outputs of a head for 16 MT rows; its eight warps share the contracted axis out and add up in shared memory. Weights go
+// A CTA takes 64 outputs of a head for 16 MT rows; its warps share the contracted axis out and add up in shared memory. Weights go
 // from global memory into mma.sync's B fragments without a stop: the contracted elements and the outputs may be numbered as one likes as
 // long as both operands and the result agree. Output g * 8 + j is column g of the j-th 8-wide product, so a thread reads eight neighbouring
 // weights of a row and writes sixteen neighbouring outputs; contracted element 4 c + i (or 8 c + i, where these are the neighbours) is
@@ -23,63 +23,84 @@ struct HeadProductArgs {
     int n_rows, in, out_tiles;
 };
 
-constexpr int kHpOut = 64, kHpWarps = 8;
+constexpr int kHpOut = 64;
 
 __device__ __forceinline__ void hp_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// N pairs of neighbouring elements of a row of x, as PARTS bf16 words each
+// N pairs of neighbouring elements of a row of x: as they are in memory, and as PARTS bf16 words each
+template <typename T, int N> struct Pairs;
 template <int N>
-__device__ __forceinline__ void pairs_of(const float* p, bool there, uint32_t (&w)[N][3]) {
+struct Pairs<float, N> {
+    float4 v[N / 2];
+    __device__ __forceinline__ void load(const float* p, bool there) {
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-        const float4 v = there ? *reinterpret_cast<const float4*>(p + 2 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
-        cut_parts(v.x, v.y, w[i]);
-        cut_parts(v.z, v.w, w[i + 1]);
+        for (int i = 0; i < N / 2; ++i) v[i] = there ? reinterpret_cast<const float4*>(p)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-}
+    __device__ __forceinline__ void parts(uint32_t (&w)[N][3]) const {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) { cut_parts(v[i].x, v[i].y, w[2 * i]); cut_parts(v[i].z, v[i].w, w[2 * i + 1]); }
+    }
+};
 template <int N>
-__device__ __forceinline__ void pairs_of(const __nv_bfloat16* p, bool there, uint32_t (&w)[N][1]) {
-    if constexpr (N == 2) {
-        const uint2 v = there ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
-        w[0][0] = v.x; w[1][0] = v.y;
-    } else {
-        const uint4 v = there ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
-        w[0][0] = v.x; w[1][0] = v.y; w[2][0] = v.z; w[3][0] = v.w;
+struct Pairs<__nv_bfloat16, N> {
+    uint32_t v[N];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool there) {
+        if constexpr (N == 2) {
+            const uint2 u = there ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
+            v[0] = u.x; v[1] = u.y;
+        } else {
+            const uint4 u = there ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+        }
     }
-}
+    __device__ __forceinline__ void parts(uint32_t (&w)[N][1]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i][0] = v[i];
+    }
+};
 
 // TRANSPOSED: W is [out][in], else [in][out]
-template <typename T, bool TRANSPOSED, int MT>
-__global__ void __launch_bounds__(kHpWarps * 32, MT == 1 ? 2 : 1) head_product_kernel(const HeadProductArgs a) {
+template <typename T, bool TRANSPOSED, int MT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) head_product_kernel(const HeadProductArgs a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    constexpr int STEP = TRANSPOSED ? 32 : 16;               // contracted elements of a step
-    __shared__ float sums[kHpWarps / 2][MT * 16][kHpOut];
+    constexpr int STEP = TRANSPOSED ? 32 : 16, PAIRS = TRANSPOSED ? 4 : 2;       // contracted elements of a step, of them pairs of a thread
+    __shared__ float sums[WARPS / 2][MT * 16][kHpOut];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int head = blockIdx.y, o0 = blockIdx.x % a.out_tiles * kHpOut, row0 = blockIdx.x / a.out_tiles * (16 * MT);
     const __nv_bfloat16* w = a.w + head * a.w_head;
     const T* x = static_cast<const T*>(a.x.p) + head * a.x.head;
-    const int steps = a.in / STEP, from = steps * warp / kHpWarps, to = steps * (warp + 1) / kHpWarps;
+    const int steps = a.in / STEP, from = steps * warp / WARPS, to = steps * (warp + 1) / WARPS;
     float acc[MT][8][4] = {};
     grid_dep_wait();
     grid_dep_launch();
+    // a step's weights and rows as they are in memory, one step ahead
+    uint4 w_raw[TRANSPOSED ? 8 : 4];
+    Pairs<T, PAIRS> x_raw[MT][2];
+    auto load = [&](int s) {
+        if (s >= to) return;
+#pragma unroll
+        for (int j = 0; j < (TRANSPOSED ? 8 : 4); ++j)
+            w_raw[j] = *reinterpret_cast<const uint4*>(TRANSPOSED ? w + (o0 + g * 8 + j) * a.w_row + s * 32 + c * 8 : w + (s * 16 + c * 4 + j) * a.w_row + o0 + g * 8);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = row0 + t * 16 + i * 8 + g;
+                x_raw[t][i].load(x + r * a.x.row + s * STEP + c * 2 * PAIRS, r < a.n_rows);
+            }
+    };
+    load(from);
     for (int s = from; s < to; ++s) {
-        uint32_t b[8][TRANSPOSED ? 4 : 2];
+        uint32_t b[8][TRANSPOSED ? 4 : 2], rows[MT][2][PAIRS][PARTS];
         if constexpr (TRANSPOSED) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint4 v = *reinterpret_cast<const uint4*>(w + (o0 + g * 8 + j) * a.w_row + s * 32 + c * 8);
-                b[j][0] = v.x; b[j][1] = v.y; b[j][2] = v.z; b[j][3] = v.w;
-            }
+            for (int j = 0; j < 8; ++j) { b[j][0] = w_raw[j].x; b[j][1] = w_raw[j].y; b[j][2] = w_raw[j].z; b[j][3] = w_raw[j].w; }
         } else {
-            uint32_t v[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 u = *reinterpret_cast<const uint4*>(w + (s * 16 + c * 4 + i) * a.w_row + o0 + g * 8);
-                v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
-            }
+            const uint32_t v[4][4] = {{w_raw[0].x, w_raw[0].y, w_raw[0].z, w_raw[0].w}, {w_raw[1].x, w_raw[1].y, w_raw[1].z, w_raw[1].w},
+                                      {w_raw[2].x, w_raw[2].y, w_raw[2].z, w_raw[2].w}, {w_raw[3].x, w_raw[3].y, w_raw[3].z, w_raw[3].w}};
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t pick = j & 1 ? 0x7632 : 0x5410;
@@ -87,27 +108,26 @@ __global__ void __launch_bounds__(kHpWarps * 32, MT == 1 ? 2 : 1) head_product_k
                 b[j][1] = __byte_perm(v[2][j / 2], v[3][j / 2], pick);
             }
         }
-        constexpr int PAIRS = TRANSPOSED ? 4 : 2;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            uint32_t top[PAIRS][PARTS], low[PAIRS][PARTS];
-            const int r0 = row0 + t * 16 + g, r1 = r0 + 8, k0 = s * STEP + c * 2 * PAIRS;
-            pairs_of<PAIRS>(x + r0 * a.x.row + k0, r0 < a.n_rows, top);
-            pairs_of<PAIRS>(x + r1 * a.x.row + k0, r1 < a.n_rows, low);
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x_raw[t][i].parts(rows[t][i]);
+        load(s + 1);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int k = 0; k < PAIRS; k += 2)
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
-                    const uint32_t frag[4] = {top[k][p], low[k][p], top[k + 1][p], low[k + 1][p]};
+                    const uint32_t frag[4] = {rows[t][0][k][p], rows[t][1][k][p], rows[t][0][k + 1][p], rows[t][1][k + 1][p]};
 #pragma unroll
                     for (int j = 0; j < 8; ++j) hp_mma(acc[t][j], frag, b[j][k], b[j][k + 1]);
                 }
-        }
     }
     // ---- the warps' sums: the upper half hands over, the lower half adds, twice in turn; always in the same order ----
 #pragma unroll
-    for (int n = kHpWarps / 2; n > 0; n /= 2) {
-        if (n < kHpWarps / 2) __syncthreads();
+    for (int n = WARPS / 2; n > 0; n /= 2) {
+        if (n < WARPS / 2) __syncthreads();
         if (warp >= n && warp < 2 * n)
 #pragma unroll
             for (int t = 0; t < MT; ++t)

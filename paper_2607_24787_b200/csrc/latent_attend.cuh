@@ -287,53 +287,38 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                          : "=r"(any) : "r"(int(yes)) : "memory");
             return any != 0;
         };
-        // This item's queries, a warp every fourth column, all of a warp's loads in flight together
-        const int vectors = (latent + a.kv.rope) / 8;
+        // This item's queries, eight lanes a column, all of a warp's loads in flight together
         auto bring_queries = [&](int half) {
-            auto column = [&](int col, const T*& from) {
-                const int x = w.group * COLS + col, i = la_row(a, x), row = w.s.first + i;
+            const int unit = lane & 7, last_units = a.kv.rope / 8;
+#pragma unroll
+            for (int c0 = 0; c0 < COLS; c0 += 16) {
+                const int col = c0 + warp * 4 + (lane >> 3), x = w.group * COLS + col, i = la_row(a, x), row = w.s.first + i;
                 const bool is = i < w.s.n && row >= 0 && row < a.batch.n_rows;
-                from = static_cast<const T*>(a.q.p) + (is ? row * a.q.row + (x - i * a.heads) * a.q.head : 0);
-                if (lane == 0) sh.limit[half][col] = is ? max(0, min(w.s.len - w.s.n + i + 1, w.s.cap_len)) : 0;
-                return is;
-            };
-            // unit lane + 32 k of column `col`
-            auto place = [&](int col, int k) { return (q_at + (4 * k + (lane >> 3)) * (N * 128) + col * 128) ^ (((lane ^ col) & 7) << 4); };
-            if constexpr (PARTS == 1) {
-#pragma unroll 4
-                for (int col = warp; col < COLS; col += 4) {
-                    const T* from;
-                    const bool is = column(col, from);
+                const T* from = static_cast<const T*>(a.q.p) + (is ? row * a.q.row + (x - i * a.heads) * a.q.head + unit * 8 : 0);
+                if (unit == 0) sh.limit[half][col] = is ? max(0, min(w.s.len - w.s.n + i + 1, w.s.cap_len)) : 0;
+                const uint32_t to = q_at + col * 128 + ((unit ^ col & 7) << 4);
+                if constexpr (PARTS == 1) {
+#pragma unroll 3
+                    for (int k = 0; k + 1 < chunks; ++k) copy16_or_zero(to + k * (N * 128), from + (is ? k * 64 : 0), is);
+                    if (unit < last_units) copy16_or_zero(to + (chunks - 1) * (N * 128), from + (is ? (chunks - 1) * 64 : 0), is);
+                } else {
+                    Raw8 v[9];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (k * 32 + lane < vectors) copy16_or_zero(place(col, k), from + (is ? (k * 32 + lane) * 8 : 0), is);
-                }
-                copies_arrived();
-            } else {
-                Raw8 v[COLS / 4][3];
+                    for (int k = 0; k < 9; ++k) v[k] = is && (k + 1 < chunks || (k + 1 == chunks && unit < last_units)) ? raw8(from + k * 64) : Raw8{};
 #pragma unroll
-                for (int c = 0; c < COLS / 4; ++c) {
-                    const T* from;
-                    const bool is = column(4 * c + warp, from);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) v[c][k] = is && k * 32 + lane < vectors ? raw8(from + (k * 32 + lane) * 8) : Raw8{};
-                }
-#pragma unroll
-                for (int c = 0; c < COLS / 4; ++c) {
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        if (k * 32 + lane >= vectors) continue;
+                    for (int k = 0; k < 9; ++k) {
+                        if (k >= chunks) continue;
                         float f[8];
-                        unpack8<T>(v[c][k], f);
+                        unpack8<T>(v[k], f);
                         uint32_t p[4][3];
 #pragma unroll
                         for (int u = 0; u < 4; ++u) cut_parts(f[2 * u], f[2 * u + 1], p[u]);
 #pragma unroll
-                        for (int u = 0; u < 3; ++u)
-                            st_shared16(place(4 * c + warp, k) + u * (COLS * 128), make_uint4(p[0][u], p[1][u], p[2][u], p[3][u]));
+                        for (int u = 0; u < 3; ++u) st_shared16(to + k * (N * 128) + u * (COLS * 128), make_uint4(p[0][u], p[1][u], p[2][u], p[3][u]));
                     }
                 }
             }
+            if constexpr (PARTS == 1) copies_arrived();
         };
         float* red = reinterpret_cast<float*>(raw_smem + (p_at - smem_u32(raw_smem)));       // [4 warps][COLS], in the probabilities' place
         long long* to_of = reinterpret_cast<long long*>(red + 4 * COLS);         // [COLS]
@@ -541,7 +526,15 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
             // each two
             if (w.tiles > 0 || whole) {
 #pragma unroll 1
-                for (int ch = 0; ch < COLS / 16; ++ch)
+                for (int ch = 0; ch < COLS / 16; ++ch) {
+                    float by[16];
+                    long long at[16];            // of the column in bf16 of every other one: of this lane's
+                    if (whole)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            by[i] = red[ch * 16 + i];
+                            at[i] = to_of[ch * 16 + (sizeof(T) == 2 ? i / 2 * 2 + (lane & 1) : i)];
+                        }
 #pragma unroll 1
                     for (int mt = 0; mt < latent / 128; ++mt) {
                         const int d = mt * 128 + tid;
@@ -551,34 +544,30 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + ch * 16 + (uint32_t(warp) << 21), o[u]);
                             tmem_wait_ld();
                         }
+                        float v[16];
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            float v[4];
+                        for (int i = 0; i < 16; ++i) {
+                            v[i] = __uint_as_float(o[0][i]);
+                            if constexpr (PARTS == 3) v[i] = v[i] + __uint_as_float(o[1][i]) + __uint_as_float(o[2][i]);
+                        }
+                        if (!whole) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                v[k] = __uint_as_float(o[0][i + k]);
-                                if constexpr (PARTS == 3) v[k] = v[k] + __uint_as_float(o[1][i + k]) + __uint_as_float(o[2][i + k]);
-                            }
-                            if (!whole) {
-                                *reinterpret_cast<float4*>(part + ((mt * (COLS / 4) + ch * 4 + i / 4) * 128 + tid) * 4) = make_float4(v[0], v[1], v[2], v[3]);
-                                continue;
-                            }
+                            for (int i = 0; i < 16; i += 4)
+                                *reinterpret_cast<float4*>(part + ((mt * (COLS / 4) + ch * 4 + i / 4) * 128 + tid) * 4) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        } else if constexpr (sizeof(T) == 2) {
+                            const bool odd = lane & 1;
 #pragma unroll
-                            for (int k = 0; k < 4; k += sizeof(T) == 2 ? 2 : 1) {
-                                const int col = ch * 16 + i + k;
-                                if constexpr (sizeof(T) == 2) {
-                                    const float x = v[k] * red[col], y = v[k + 1] * red[col + 1];
-                                    const bool odd = lane & 1;
-                                    const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
-                                    const long long at = to_of[col + odd];
-                                    if (at >= 0) *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out.p) + at + (d & ~1)) = odd ? pack_bf16(got, y) : pack_bf16(x, got);
-                                } else {
-                                    const long long at = to_of[col];
-                                    if (at >= 0) static_cast<T*>(a.out.p)[at + d] = v[k] * red[col];
-                                }
+                            for (int i = 0; i < 16; i += 2) {
+                                const float x = v[i] * by[i], y = v[i + 1] * by[i + 1], got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+                                if (at[i] >= 0) *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out.p) + at[i] + (d & ~1)) = odd ? pack_bf16(got, y) : pack_bf16(x, got);
                             }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (at[i] >= 0) static_cast<T*>(a.out.p)[at[i] + d] = v[i] * by[i];
                         }
                     }
+                }
             }
             tc_fence_before();
             together();                          // (`red` has been read)
@@ -589,7 +578,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         // ---- tiles on their way in ----
         int st = 0, turn = 0;
         unsigned it = 0;
-        const uint64_t once = policy_evict_first();          // (262145 tokens of 16 heads: TODO us without)
+        const uint64_t once = policy_evict_first();          // (262145 tokens of 16 heads: 72 us without, 64)
         int4 join = make_int4(0, 0, 0, 0);
         long long joined = 0;
         while (w.left > 0 && ok) {

@@ -135,10 +135,14 @@ cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expand
 
 template <typename T, bool TRANSPOSED>
 cudaError_t launch_product(const HeadProductArgs& a, int n_heads, cudaStream_t st) {
-    const auto grid = [&](int rows) { return dim3(unsigned((a.n_rows + rows - 1) / rows) * a.out_tiles, n_heads); };
+    const auto ctas = [&](int rows) { return unsigned((a.n_rows + rows - 1) / rows) * a.out_tiles; };
+    // fp32 rows take registers threefold: 16 of them a CTA. Enough CTAs for several on an SM have four warps, fewer eight, which wait less long.
+    const bool one = a.n_rows <= 16 || sizeof(T) == 4;
+    const dim3 grid(ctas(one ? 16 : 32), n_heads);
+    const bool many = static_cast<long long>(grid.x) * n_heads >= 2 * 148;
     if constexpr (sizeof(T) == 2)
-        if (a.n_rows > 16) return launch_early(head_product_kernel<T, TRANSPOSED, 2>, grid(32), kHpWarps * 32, 0, st, a);
-    return launch_early(head_product_kernel<T, TRANSPOSED, 1>, grid(16), kHpWarps * 32, 0, st, a);
+        if (!one) return many ? launch_early(head_product_kernel<T, TRANSPOSED, 2, 4>, grid, 128, 0, st, a) : launch_early(head_product_kernel<T, TRANSPOSED, 2, 8>, grid, 256, 0, st, a);
+    return many ? launch_early(head_product_kernel<T, TRANSPOSED, 1, 4>, grid, 128, 0, st, a) : launch_early(head_product_kernel<T, TRANSPOSED, 1, 8>, grid, 256, 0, st, a);
 }
 
 }  // namespace

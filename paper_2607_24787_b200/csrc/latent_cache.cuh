@@ -2,6 +2,7 @@
 #pragma once
 
 #include "kv_cache.cuh"
+#include "mma_ops.cuh"
 
 namespace spm {
 
@@ -22,15 +23,11 @@ __device__ __forceinline__ long long latent_row_at(const LatentPool& kv, const K
     return -1;
 }
 
-// bf16 parts of two numbers: cut off, so that the sum is exact
+// bf16 parts of two numbers: cut off, so that the sum is exact (an infinity's are itself and zeros, a NaN's first is one whatever its bits)
 __device__ __forceinline__ void cut_parts(float a, float b, uint32_t (&p)[3]) {
+    const Split3 s = split3(a + 0.f, b + 0.f);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        const uint32_t ha = __float_as_uint(a) & 0xffff0000u, hb = __float_as_uint(b) & 0xffff0000u;
-        p[i] = ha >> 16 | hb;
-        a -= __uint_as_float(ha);
-        b -= __uint_as_float(hb);
-    }
+    for (int i = 0; i < 3; ++i) p[i] = s.part[i];
 }
 __device__ __forceinline__ void cut_parts(uint32_t v, uint32_t (&p)[1]) { p[0] = v; }
 
