@@ -19,6 +19,8 @@
 // see fewer, as a prompt's do, leave their CTA idle for the others. Such calls are few: prompts have the expanded form.)
 #pragma once
 
+#include <type_traits>
+
 #include <cuda.h>
 
 #include "kv_cache.cuh"
@@ -721,18 +723,117 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     if (warp == 5) tmem_dealloc(t_s, 512);
 }
 
-// Adds the parts of items that were cut between CTAs. A task is four columns' 32 elements of one such item, a warp's; where these are so few
-// that the parts of each are many, a block's, whose eight warps take the parts in turn. Parts are added in the same order each time.
-constexpr int kLaJoinThreads = 256, kLaJoinBlocks = 592;
+// Adds the parts of items that were cut between CTAs. A task is four columns of one such item and 128 of their elements, a warp's; where these
+// are fewer than warps, 32 elements; where these are no more than blocks, a block's, whose eight warps take the parts in turn. Parts are
+// added in the same order each time.
+constexpr int kLaJoinThreads = 256, kLaJoinBlocks = 592, kLaJoinWarps = kLaJoinThreads / 32;
+struct LaJoinShared {
+    float weights[kLaJoinWarps][kLaMaxCtas][4];
+    float4 sums[kLaJoinWarps][32];
+    float tops[kLaJoinWarps][4], totals[kLaJoinWarps][4];
+};
+// WIDE: runs of 32 elements a lane has four columns of. BLOCK: all warps of a block together
+template <typename T, int COLS, int WIDE, bool BLOCK>
+__device__ __forceinline__ void la_join(const LatentAttendArgs& a, LaJoinShared& sh, int owner, int quad, int d0) {
+    using S = LaShape<T, COLS>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, latent = a.kv.latent, from = BLOCK ? warp : 0, step = BLOCK ? kLaJoinWarps : 1;
+    const int4 join = a.joins[owner];
+    // part 0 is the second slot of its CTA, the others are the first slots of theirs
+    const size_t each = S::part_floats(latent);
+    const float* parts = a.parts + size_t(owner) * 2 * each;
+    auto part = [&](int j) { return parts + (j == 0 ? 1 : 2 * j) * each; };
+    const int mine = from < join.x ? (join.x - from + step - 1) / step : 0;
+    // lane (i, k): maxima and sums of column k
+    const int k = lane & 3, end_at = COLS * latent + quad * 4 + k;
+    float top = -INFINITY, sum = 0.f;
+    for (int i0 = lane >> 2; i0 < mine; i0 += 32) {
+        float m[4], l[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool is = i0 + 8 * u < mine;
+            const float* at = part(from + (is ? i0 + 8 * u : 0) * step) + end_at;
+            m[u] = is ? at[0] : -INFINITY;
+            l[u] = is ? at[COLS] : 0.f;
+        }
+        float to = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) to = fmaxf(to, m[u]);
+        if (sum != 0.f) sum *= ex2(top - to);
+        top = to;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (m[u] != -INFINITY) sum += l[u] * ex2(m[u] - to);
+            if (i0 + 8 * u < mine) sh.weights[warp][i0 + 8 * u][k] = m[u];
+        }
+    }
+    const float own = top;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (sum != 0.f) sum *= ex2(own - top);
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int i = lane >> 2; i < mine; i += 8) {
+        const float m = sh.weights[warp][i][k];
+        sh.weights[warp][i][k] = m == -INFINITY ? 0.f : ex2(m - top);
+    }
+    __syncwarp();
+    float o[WIDE][4] = {};
+    const size_t at = ((d0 / 128 * (COLS / 4) + quad) * 128 + d0 % 128 + lane) * 4;
+#pragma unroll 8 / WIDE
+    for (int i = 0; i < mine; ++i) {
+        const float4 by = *reinterpret_cast<const float4*>(sh.weights[warp][i]);
+        float4 v[WIDE];
+#pragma unroll
+        for (int u = 0; u < WIDE; ++u) v[u] = *reinterpret_cast<const float4*>(part(from + i * step) + at + u * 128);
+        // (a part that saw nothing has written no sums)
+#pragma unroll
+        for (int u = 0; u < WIDE; ++u) {
+            o[u][0] += by.x == 0.f ? 0.f : by.x * v[u].x; o[u][1] += by.y == 0.f ? 0.f : by.y * v[u].y;
+            o[u][2] += by.z == 0.f ? 0.f : by.z * v[u].z; o[u][3] += by.w == 0.f ? 0.f : by.w * v[u].w;
+        }
+    }
+    if constexpr (BLOCK) {                       // the warps' sums, by their maxima
+        if (lane < 4) { sh.tops[warp][lane] = top; sh.totals[warp][lane] = sum; }
+        sh.sums[warp][lane] = make_float4(o[0][0], o[0][1], o[0][2], o[0][3]);
+        __syncthreads();
+        if (warp == 0)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float most = -INFINITY, total = 0.f, y = 0.f;
+#pragma unroll
+                for (int u = 0; u < kLaJoinWarps; ++u) most = fmaxf(most, sh.tops[u][i]);
+#pragma unroll
+                for (int u = 0; u < kLaJoinWarps; ++u) {
+                    const float by = sh.tops[u][i] == -INFINITY ? 0.f : ex2(sh.tops[u][i] - most);
+                    if (by != 0.f) { total += by * sh.totals[u][i]; y += by * reinterpret_cast<const float*>(&sh.sums[u][lane])[i]; }
+                }
+                o[0][i] = y;
+                if (k == i) sum = total;
+            }
+        __syncthreads();
+        if (warp > 0) return;
+    }
+    const float norm = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int x = join.w * COLS + quad * 4 + i, row_in = la_row(a, x), h = x - row_in * a.heads, row = join.y + row_in;
+        const float by = __shfl_sync(0xffffffffu, norm, i);
+        if (row_in >= join.z || row < 0 || row >= a.batch.n_rows) continue;
+        T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d0 + lane;
+#pragma unroll
+        for (int u = 0; u < WIDE; ++u) {
+            const float y = o[u][i] * by;
+            if constexpr (sizeof(T) == 2) to[u * 32] = __float2bfloat16_rn(y);
+            else to[u * 32] = y;
+        }
+    }
+    __syncwarp();
+}
 template <typename T, int COLS>
 __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const LatentAttendArgs a, int ctas) {
-    using S = LaShape<T, COLS>;
-    constexpr int WARPS = kLaJoinThreads / 32;
     __shared__ int owners[kLaMaxCtas], n_owners;
-    __shared__ __align__(16) float weights[WARPS][kLaMaxCtas][4];
-    __shared__ float4 sums[WARPS][32];
-    __shared__ float tops[WARPS][4], totals[WARPS][4];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ __align__(16) LaJoinShared sh;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dep_wait();
     grid_dep_launch();
     if (warp == 0) {
@@ -747,95 +848,21 @@ __global__ void __launch_bounds__(kLaJoinThreads) latent_join_kernel(const Laten
         if (lane == 0) n_owners = count;
     }
     __syncthreads();
-    const int latent = a.kv.latent, each_item = COLS / 4 * (latent / 32), tasks = n_owners * each_item;
-    const bool together = tasks <= int(gridDim.x);           // a block a task
-    const int step = together ? WARPS : 1;
-    for (int task = together ? blockIdx.x : blockIdx.x * WARPS + warp; task < tasks; task += gridDim.x * (WARPS / step)) {
-        const int owner = owners[task / each_item], in = task % each_item, quad = in / (latent / 32), d = in % (latent / 32) * 32 + lane;
-        const int4 join = a.joins[owner];
-        // part 0 is the second slot of its CTA, the others are the first slots of theirs
-        const size_t each = S::part_floats(latent);
-        const float* parts = a.parts + size_t(owner) * 2 * each;
-        auto part = [&](int j) { return parts + (j == 0 ? 1 : 2 * j) * each; };
-        // lane (j, k): maxima and sums of every eighth part's column k
-        // this warp's parts: every one, or every eighth. Lane (i, k): maxima and sums of column k
-        const int from = together ? warp : 0, mine = from < join.x ? (join.x - from + step - 1) / step : 0;
-        const int k = lane & 3, end_at = COLS * latent + quad * 4 + k;
-        float top = -INFINITY, sum = 0.f;
-        for (int i0 = lane >> 2; i0 < mine; i0 += 32) {
-            float m[4], l[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const bool is = i0 + 8 * u < mine;
-                const float* at = part(from + (is ? i0 + 8 * u : 0) * step) + end_at;
-                m[u] = is ? at[0] : -INFINITY;
-                l[u] = is ? at[COLS] : 0.f;
-            }
-            float to = top;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) to = fmaxf(to, m[u]);
-            if (sum != 0.f) sum *= ex2(top - to);
-            top = to;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (m[u] != -INFINITY) sum += l[u] * ex2(m[u] - to);
-                if (i0 + 8 * u < mine) weights[warp][i0 + 8 * u][k] = m[u];
-            }
+    constexpr int QUADS = COLS / 4;
+    const int runs = a.kv.latent / 32, narrow = n_owners * QUADS * runs, wide = narrow / 4;
+    const auto narrow_task = [&](int task, auto block) {
+        const int item = task / (QUADS * runs), in = task % (QUADS * runs);
+        la_join<T, COLS, 1, block.value>(a, sh, owners[item], in / runs, in % runs * 32);
+    };
+    if (narrow <= int(gridDim.x)) {
+        if (int(blockIdx.x) < narrow) narrow_task(blockIdx.x, std::integral_constant<bool, true>{});
+    } else if (wide < int(gridDim.x) * kLaJoinWarps / 2)
+        for (int task = blockIdx.x * kLaJoinWarps + warp; task < narrow; task += gridDim.x * kLaJoinWarps) narrow_task(task, std::integral_constant<bool, false>{});
+    else
+        for (int task = blockIdx.x * kLaJoinWarps + warp; task < wide; task += gridDim.x * kLaJoinWarps) {
+            const int item = task / (QUADS * runs / 4), in = task % (QUADS * runs / 4);
+            la_join<T, COLS, 4, false>(a, sh, owners[item], in / (runs / 4), in % (runs / 4) * 128);
         }
-        const float own = top;
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (sum != 0.f) sum *= ex2(own - top);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        for (int i = lane >> 2; i < mine; i += 8) {
-            const float m = weights[warp][i][k];
-            weights[warp][i][k] = m == -INFINITY ? 0.f : ex2(m - top);
-        }
-        __syncwarp();
-        float o[4] = {};
-#pragma unroll 8
-        for (int i = 0; i < mine; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(part(from + i * step) + ((d / 128 * (COLS / 4) + quad) * 128 + d % 128) * 4);
-            const float4 by = *reinterpret_cast<const float4*>(weights[warp][i]);
-            // (a part that saw nothing has written no sums)
-            o[0] += by.x == 0.f ? 0.f : by.x * v.x; o[1] += by.y == 0.f ? 0.f : by.y * v.y;
-            o[2] += by.z == 0.f ? 0.f : by.z * v.z; o[3] += by.w == 0.f ? 0.f : by.w * v.w;
-        }
-        if (together) {                          // the warps' sums, by their maxima
-            if (lane < 4) { tops[warp][lane] = top; totals[warp][lane] = sum; }
-            sums[warp][lane] = make_float4(o[0], o[1], o[2], o[3]);
-            __syncthreads();
-            if (warp == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float most = -INFINITY, total = 0.f, y = 0.f;
-#pragma unroll
-                    for (int u = 0; u < WARPS; ++u) most = fmaxf(most, tops[u][i]);
-#pragma unroll
-                    for (int u = 0; u < WARPS; ++u) {
-                        const float by = tops[u][i] == -INFINITY ? 0.f : ex2(tops[u][i] - most);
-                        if (by != 0.f) { total += by * totals[u][i]; y += by * reinterpret_cast<const float*>(&sums[u][lane])[i]; }
-                    }
-                    o[i] = y;
-                    if (k == i) sum = total;
-                }
-            }
-            __syncthreads();
-        }
-        const float norm = sum == 0.f ? 0.f : 1.f / sum;
-        if (!together || warp == 0)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int x = join.w * COLS + quad * 4 + i, row_in = la_row(a, x), h = x - row_in * a.heads, row = join.y + row_in;
-                const float y = o[i] * __shfl_sync(0xffffffffu, norm, i);
-                if (row_in >= join.z || row < 0 || row >= a.batch.n_rows) continue;
-                T* to = static_cast<T*>(a.out.p) + row * a.out.row + h * a.out.head + d;
-                if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(y);
-                else *to = y;
-            }
-        __syncwarp();
-    }
 }
 
 }  // namespace spm
