@@ -13,6 +13,7 @@
 #include "latent_cache.cuh"
 #include "mma_ops.cuh"
 #include "ptx.cuh"
+#include "tc_ops.cuh"
 
 namespace spm {
 
@@ -161,6 +162,138 @@ __global__ void __launch_bounds__(WARPS * 32) head_product_kernel(const HeadProd
                 store_row<8>(y + r * a.y.row + 8 * k, v);
             }
         }
+}
+
+// The same for more rows: a CTA takes 128 outputs of a head for 64 rows, four warps' rows by two warps' outputs, and chunks of 64 contracted
+// elements come into shared memory by asynchronous copies, several ahead, so that every weight and every element comes from memory once.
+// Elements and outputs are numbered as above. 16-byte units of a row are moved by the row's number so that what eight (or, of 8 bytes, 16)
+// threads read together lies in different banks.
+constexpr int kHtRows = 64, kHtOut = 128, kHtChunk = 64, kHtStages = 5, kHtThreads = 256;
+template <typename T>
+struct HtShape {
+    static constexpr int w_bytes = kHtOut * kHtChunk * 2, x_bytes = kHtRows * kHtChunk * int(sizeof(T)), stage = w_bytes + x_bytes;
+    static constexpr int smem = kHtStages * stage;
+};
+template <typename T, bool TRANSPOSED>
+__global__ void __launch_bounds__(kHtThreads) head_product_tile_kernel(const HeadProductArgs a, int out) {
+    using S = HtShape<T>;
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, STEP = TRANSPOSED ? 32 : 16, PAIRS = TRANSPOSED ? 4 : 2;
+    extern __shared__ __align__(128) unsigned char ht_smem[];
+    const uint32_t base = smem_u32(ht_smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3, wr = warp & 3, wn = warp >> 2;
+    const int head = blockIdx.y, o0 = blockIdx.x % a.out_tiles * kHtOut, row0 = blockIdx.x / a.out_tiles * kHtRows;
+    const __nv_bfloat16* w = a.w + head * a.w_head;
+    const T* x = static_cast<const T*>(a.x.p) + head * a.x.head;
+    grid_dep_wait();
+    grid_dep_launch();
+    // where unit u of a row lies: W by rows of outputs (transposed) or of contracted elements, x by rows
+    auto w_unit = [](int r, int u) { return TRANSPOSED ? uint32_t(r * 128 + ((u ^ ((r >> 3 & 1) << 2)) << 4)) : uint32_t(r * 256 + ((u ^ ((r >> 2 & 3) << 1)) << 4)); };
+    auto x_unit = [](int r, int u) {
+        const int by = sizeof(T) == 4 ? (TRANSPOSED ? r & 1 : (r & 1) << 2) : (TRANSPOSED ? (r & 1) << 2 : (r & 3) << 1);
+        return uint32_t(r * (kHtChunk * int(sizeof(T))) + ((u ^ by) << 4));
+    };
+    const int chunks = a.in / kHtChunk;
+    auto copy = [&](int k) {
+        if (k < chunks) {
+            const uint32_t to = base + k % kHtStages * S::stage;
+#pragma unroll
+            for (int i = tid; i < S::w_bytes / 16; i += kHtThreads) {
+                constexpr int UNITS = TRANSPOSED ? kHtChunk / 8 : kHtOut / 8;
+                const int r = i / UNITS, u = i % UNITS, o = o0 + (TRANSPOSED ? r : u * 8);
+                const bool is = o < out;
+                copy16_or_zero(to + w_unit(r, u), is ? (TRANSPOSED ? w + o * a.w_row + k * kHtChunk + u * 8 : w + (k * kHtChunk + r) * a.w_row + o) : w, is);
+            }
+#pragma unroll
+            for (int i = tid; i < S::x_bytes / 16; i += kHtThreads) {
+                constexpr int EACH = 16 / int(sizeof(T)), UNITS = kHtChunk / EACH;
+                const int r = i / UNITS, u = i % UNITS;
+                const bool is = row0 + r < a.n_rows;
+                copy16_or_zero(to + S::w_bytes + x_unit(r, u), is ? x + (row0 + r) * a.x.row + k * kHtChunk + u * EACH : x, is);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < kHtStages - 1; ++k) copy(k);
+    float acc[8][4] = {};
+    const bool idle = o0 + wn * 64 >= out;       // (the last 64 of an odd number of them)
+    for (int k = 0; k < chunks; ++k) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kHtStages - 2) : "memory");
+        __syncthreads();
+        copy(k + kHtStages - 1);
+        if (idle) continue;
+        const uint32_t w_at = base + k % kHtStages * S::stage, x_at = w_at + S::w_bytes;
+        float part[8][4] = {};                   // fp32: a chunk's sums, added up outside of the products, which cut sums off where they do not round them
+        float (&sum)[8][4] = sizeof(T) == 4 ? part : acc;
+#pragma unroll
+        for (int s = 0; s < kHtChunk / STEP; ++s) {
+            uint32_t rows[2][PAIRS][PARTS], b[8][TRANSPOSED ? 4 : 2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = wr * 16 + i * 8 + g;
+                if constexpr (sizeof(T) == 4) {
+                    Pairs<float, PAIRS> p;
+#pragma unroll
+                    for (int u = 0; u < PAIRS / 2; ++u) {
+                        const uint4 v = lds128(x_at + x_unit(r, s * (STEP / 4) + c * (PAIRS / 2) + u));
+                        p.v[u] = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+                    }
+                    p.parts(rows[i]);
+                } else if constexpr (TRANSPOSED) {
+                    const uint4 v = lds128(x_at + x_unit(r, s * 4 + c));
+                    rows[i][0][0] = v.x; rows[i][1][0] = v.y; rows[i][2][0] = v.z; rows[i][3][0] = v.w;
+                } else
+                    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(rows[i][0][0]), "=r"(rows[i][1][0]) : "r"(x_at + x_unit(r, s * 2 + (c >> 1)) + (c & 1) * 8));
+            }
+            if constexpr (TRANSPOSED) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint4 v = lds128(w_at + w_unit(wn * 64 + g * 8 + j, s * 4 + c));
+                    b[j][0] = v.x; b[j][1] = v.y; b[j][2] = v.z; b[j][3] = v.w;
+                }
+            } else {
+                uint32_t v[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 u = lds128(w_at + w_unit(s * 16 + c * 4 + i, wn * 8 + g));
+                    v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t pick = j & 1 ? 0x7632 : 0x5410;
+                    b[j][0] = __byte_perm(v[0][j / 2], v[1][j / 2], pick);
+                    b[j][1] = __byte_perm(v[2][j / 2], v[3][j / 2], pick);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < PAIRS; e += 2)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    const uint32_t frag[4] = {rows[0][e][p], rows[1][e][p], rows[0][e + 1][p], rows[1][e + 1][p]};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) hp_mma(sum[j], frag, b[j][e], b[j][e + 1]);
+                }
+        }
+        if constexpr (sizeof(T) == 4)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] += part[j][e];
+    }
+    if (idle) return;
+    T* y = static_cast<T*>(a.y.p) + head * a.y.head + o0 + wn * 64 + 16 * c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = row0 + wr * 16 + i * 8 + g;
+        if (r >= a.n_rows) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = acc[j][i * 2 + k];
+            store_row<8>(y + r * a.y.row + 8 * k, v);
+        }
+    }
 }
 
 }  // namespace spm

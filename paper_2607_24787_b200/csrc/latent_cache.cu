@@ -134,11 +134,19 @@ cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expand
 }
 
 template <typename T, bool TRANSPOSED>
-cudaError_t launch_product(const HeadProductArgs& a, int n_heads, cudaStream_t st) {
-    const auto ctas = [&](int rows) { return unsigned((a.n_rows + rows - 1) / rows) * a.out_tiles; };
+cudaError_t launch_product(HeadProductArgs a, int n_heads, int out, int dev, cudaStream_t st) {
+    // Enough work for CTAs of 64 rows and 128 outputs on most SMs, and more than a few rows: these read everything once (TODO)
+    const long long tiles = (a.n_rows + kHtRows - 1ll) / kHtRows * ((out + kHtOut - 1) / kHtOut);
+    if (a.n_rows > 16 && tiles * n_heads >= 96) {
+        const cudaError_t e = allow_smem<head_product_tile_kernel<T, TRANSPOSED>>(dev, HtShape<T>::smem);
+        if (e != cudaSuccess) return e;
+        a.out_tiles = (out + kHtOut - 1) / kHtOut;
+        return launch_early(head_product_tile_kernel<T, TRANSPOSED>, dim3(unsigned(tiles), n_heads), kHtThreads, HtShape<T>::smem, st, a, out);
+    }
     // fp32 rows take registers threefold: 16 of them a CTA. Enough CTAs for several on an SM have four warps, fewer eight, which wait less long.
     const bool one = a.n_rows <= 16 || sizeof(T) == 4;
-    const dim3 grid(ctas(one ? 16 : 32), n_heads);
+    a.out_tiles = out / kHpOut;
+    const dim3 grid(unsigned((a.n_rows + (one ? 15 : 31)) / (one ? 16 : 32)) * a.out_tiles, n_heads);
     const bool many = static_cast<long long>(grid.x) * n_heads >= 2 * 148;
     if constexpr (sizeof(T) == 2)
         if (!one) return many ? launch_early(head_product_kernel<T, TRANSPOSED, 2, 4>, grid, 128, 0, st, a) : launch_early(head_product_kernel<T, TRANSPOSED, 2, 8>, grid, 256, 0, st, a);
@@ -330,11 +338,15 @@ int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, in
     a.x = rows_of(x); a.y = rows_of(y);
     a.w = static_cast<const __nv_bfloat16*>(w);
     a.w_head = w_head_stride; a.w_row = w_row_stride;
-    a.n_rows = n_rows; a.in = in_dim; a.out_tiles = out_dim / kHpOut;
+    a.n_rows = n_rows; a.in = in_dim;
     const auto st = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (dtype == SPM_DTYPE_BF16) e = transposed ? launch_product<__nv_bfloat16, true>(a, n_heads, st) : launch_product<__nv_bfloat16, false>(a, n_heads, st);
-    else e = transposed ? launch_product<float, true>(a, n_heads, st) : launch_product<float, false>(a, n_heads, st);
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return fail(call, SPM_ERR_CUDA, cudaGetErrorString(e));
+    if (dev < 0 || dev >= kMaxDevices) return fail(call, SPM_ERR_CONFIG, "device ordinal out of range");
+    if (dtype == SPM_DTYPE_BF16)
+        e = transposed ? launch_product<__nv_bfloat16, true>(a, n_heads, out_dim, dev, st) : launch_product<__nv_bfloat16, false>(a, n_heads, out_dim, dev, st);
+    else e = transposed ? launch_product<float, true>(a, n_heads, out_dim, dev, st) : launch_product<float, false>(a, n_heads, out_dim, dev, st);
     return launched(call, e);
 }
 

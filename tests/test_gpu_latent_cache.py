@@ -166,7 +166,7 @@ def test_write_notes_what_it_cannot_place(lib):
 
 # ---- products of heads -------------------------------------------------------
 PRODUCTS = [(1, 16, 128, 512), (3, 1, 64, 64), (16, 5, 512, 128), (17, 10, 64, 256), (32, 2, 384, 128), (33, 33, 128, 128), (200, 3, 512, 64), (64, 128, 512, 128),
-            (7, 2, 1024, 320)]
+            (7, 2, 1024, 320), (70, 60, 64, 320), (130, 40, 320, 64)]
 
 
 @pytest.mark.parametrize("transposed", [False, True])
