@@ -2,7 +2,9 @@
 //
 // [key | value] of a head = C [W_k ; W_v]^T: 128 tokens of one sequence, all of their latent vectors in shared memory, against the head's
 // matrices, whose rows come by in chunks of 64 elements. Sums of two heads are in tensor memory, so that one is rounded to bf16 and
-// written while the next is made. Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
+// written while the next is made. All (tile of tokens, head) pairs are a line that is cut evenly between CTAs, so that a CTA brings the latent
+// vectors of two or three tiles and not of many (with a CTA for each tile and a third of the heads four prompts' 10563 tokens of 16 heads took
+// 59 us, TODO now). Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
 //
 // A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
 // element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
@@ -42,6 +44,14 @@ __device__ __forceinline__ int lx_tokens(const KvBatch& b, int cap, int s) {
     if (b.row_start && min(b.row_start[s + 1] - b.row_start[s], b.n_rows) <= 0) return 0;     // (no rows look at them)
     return max(0, min(b.lengths[s], cap));
 }
+// Tiles of all sequences, as far as there is room, by a warp
+__device__ __forceinline__ int lx_tiles(const KvBatch& b, int cap, int room) {
+    long long sum = 0;
+    for (int s0 = 0; s0 < b.n_seq; s0 += 32) sum += (lx_tokens(b, cap, s0 + (threadIdx.x & 31)) + kLxTile - 1) / kLxTile;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return int(min(sum, static_cast<long long>(room / kLxTile)));
+}
 // Tile `tile` of the workspace (tile < 0: sequence `seq`'s first), by a warp
 __device__ __forceinline__ LxPlace lx_find(const KvBatch& b, int cap, int room, int seq, int tile) {
     const int lane = threadIdx.x & 31;
@@ -74,11 +84,27 @@ __device__ __forceinline__ LxPlace lx_find(const KvBatch& b, int cap, int room, 
 }
 
 struct LxShared {
-    unsigned long long a_full, b_full[8], b_empty[8], d_full[2], d_empty[2], drained;
+    unsigned long long a_full, a_empty, b_full[8], b_empty[8], d_full[2], d_empty[2], drained;
     uint32_t tmem;
-    int quit;
-    LxPlace place;
-    int rows[kLxTile / 16];     // of the tile's copies in the pool, -1: there is none
+    int quit, tiles;
+};
+// A CTA's piece of the line, tile by tile
+struct LxWalk {
+    long long at, end;
+    int heads, tile, h0, h1;
+    __device__ __forceinline__ LxWalk(int tiles, int n) : heads(n) {
+        const long long all = static_cast<long long>(tiles) * n;
+        at = all * blockIdx.x / gridDim.x;
+        end = all * (blockIdx.x + 1) / gridDim.x;
+        piece();
+    }
+    __device__ __forceinline__ void piece() {
+        tile = int(at / heads);
+        h0 = int(at - static_cast<long long>(tile) * heads);
+        h1 = int(min(static_cast<long long>(heads), h0 + end - at));
+    }
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ void next() { at += h1 - h0; if (more()) piece(); }
 };
 constexpr int kLxOwnBytes = 1024;
 static_assert(sizeof(LxShared) <= kLxOwnBytes, "what shared memory has beside the operands");
@@ -94,7 +120,6 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t* v) {
 }
 __device__ __forceinline__ bool not_finite(uint32_t bits) { return (bits & 0x7f800000u) == 0x7f800000u; }
 
-// blockIdx.x: a tile of the workspace, blockIdx.y: one of gridDim.y parts of the heads
 template <int HD>
 __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const LatentExpandArgs a, const __grid_constant__ CUtensorMap rows_map,
                                                                       const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -110,6 +135,7 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
     grid_dep_launch();
     if (tid == 0) {
         mbar_init(smem_u32(&sh.a_full), 1 + a.withhold);
+        mbar_init(smem_u32(&sh.a_empty), 1);
         for (int i = 0; i < a.stages; ++i) { mbar_init(smem_u32(&sh.b_full[i]), 1); mbar_init(smem_u32(&sh.b_empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.d_full[i]), 1); mbar_init(smem_u32(&sh.d_empty[i]), 128); }
         mbar_init(smem_u32(&sh.drained), 1);
@@ -117,31 +143,24 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
         fence_barrier_init();
     }
     if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), 2 * N);
-    const int copies = kLxTile / a.box;
     if (warp == 4) {
-        const LxPlace p = lx_find(a.batch, cap, a.tokens, 0, blockIdx.x);
-        int row = -1;
-        const int token = p.tile * kLxTile + lane * a.box;
-        if (p.seq >= 0 && lane < copies && token < p.tokens) {
-            const int page = a.batch.table[size_t(p.seq) * a.batch.stride + token / a.kv.page_size];
-            if (page >= 0 && page < a.kv.n_pages) row = page * a.kv.page_size + token % a.kv.page_size;
-            else kv_note(a.kv, SPM_KV_BAD_PAGE);
-        }
-        if (lane == 0) sh.place = p;
-        if (lane < copies) sh.rows[lane] = row;
+        const int tiles = lx_tiles(a.batch, cap, a.tokens);
+        if (lane == 0) sh.tiles = tiles;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
-    const LxPlace place = sh.place;
-    if (place.seq < 0) {                         // more tiles in the workspace than there are
-        tc_fence_before();
-        __syncthreads();
-        if (warp == 5) tmem_dealloc(tmem, 2 * N);
-        return;
-    }
-    const int head0 = a.heads * int(blockIdx.y) / int(gridDim.y), head1 = a.heads * int(blockIdx.y + 1) / int(gridDim.y);
+    LxWalk w(sh.tiles, a.heads);
+    // where a token of the place's tile stands in the pool, -1: nowhere
+    auto row_of = [&](const LxPlace& place, int in, bool note) {
+        const int token = place.tile * kLxTile + in;
+        if (place.seq < 0 || token >= place.tokens) return -1;
+        const int page = a.batch.table[size_t(place.seq) * a.batch.stride + token / a.kv.page_size];
+        if (page >= 0 && page < a.kv.n_pages) return page * a.kv.page_size + token % a.kv.page_size;
+        if (note) kv_note(a.kv, SPM_KV_BAD_PAGE);
+        return -1;
+    };
 
     auto wait = [&](const unsigned long long& bar, int parity) {
         const uint32_t at = smem_u32(&bar);
@@ -163,74 +182,83 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
 
     if (warp < 4) {
         // ---- rows out: a token a thread ----
-        const int t = place.tile * kLxTile + tid, row = sh.rows[tid / a.box];
-        const bool there = t < place.tokens && row >= 0;
-        const size_t to = size_t(place.at) + t;
-        if (blockIdx.y == 0) {
-            const uint32_t bits = __ballot_sync(0xffffffffu, there);
-            if (lane == 0) a.there[to / 32] = bits;
-            const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + (there ? static_cast<long long>(row) + tid % a.box : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
-            uint4* rope = reinterpret_cast<uint4*>(a.ropes + to * 64);
+        int i = 0;                               // heads so far
+        for (; w.more() && ok; w.next()) {
+            const LxPlace place = lx_find(a.batch, cap, a.tokens, 0, w.tile);
+            const int row = row_of(place, tid, false);
+            const bool there = row >= 0;
+            const size_t to = size_t(w.tile) * kLxTile + tid;
+            if (w.h0 == 0) {
+                const uint32_t bits = __ballot_sync(0xffffffffu, there);
+                if (lane == 0) a.there[to / 32] = bits;
+                const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + static_cast<long long>(there ? row : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
+                uint4* rope = reinterpret_cast<uint4*>(a.ropes + to * 64);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rope[i] = there && i < a.kv.rope / 8 ? from[i] : make_uint4(0, 0, 0, 0);
-        }
-        for (int h = head0; h < head1; ++h) {
-            const int buf = (h - head0) & 1, turn = (h - head0) >> 1 & 1;
-            if (!(ok = wait(sh.d_full[buf], turn))) break;
-            tc_fence_after();
-            bool odd = false;
+                for (int k = 0; k < 8; ++k) rope[k] = there && k < a.kv.rope / 8 ? from[k] : make_uint4(0, 0, 0, 0);
+            }
+            for (int h = w.h0; h < w.h1; ++h, ++i) {
+                const int buf = i & 1, turn = i >> 1 & 1;
+                if (!(ok = wait(sh.d_full[buf], turn))) break;
+                tc_fence_after();
+                bool odd = false;
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                uint32_t w[HD / 2];
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t word[HD / 2];
 #pragma unroll
-                for (int ch = 0; ch < HD / 32; ++ch) {
-                    uint32_t r[32];
-                    tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), r);
-                    tmem_wait_ld();
+                    for (int ch = 0; ch < HD / 32; ++ch) {
+                        uint32_t r[32];
+                        tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), r);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        if (part == 0) odd |= not_finite(r[i]) || not_finite(r[i + 1]);
-                        else if (odd) {
-                            if (not_finite(r[i])) r[i] = 0;
-                            if (not_finite(r[i + 1])) r[i + 1] = 0;
+                        for (int i = 0; i < 32; i += 2) {
+                            if (part == 0) odd |= not_finite(r[i]) || not_finite(r[i + 1]);
+                            else if (odd) {
+                                if (not_finite(r[i])) r[i] = 0;
+                                if (not_finite(r[i + 1])) r[i + 1] = 0;
+                            }
+                            word[ch * 16 + i / 2] = there ? pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1])) : 0u;
                         }
-                        w[ch * 16 + i / 2] = there ? pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1])) : 0u;
                     }
-                }
-                if (part == 0 && odd && there) w[0] = 0x7fff7fffu;
-                if (part == 1) {
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&sh.d_empty[buf]));
-                }
-                __nv_bfloat16* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
+                    if (part == 0 && odd && there) word[0] = 0x7fff7fffu;
+                    if (part == 1) {
+                        tc_fence_before();
+                        mbar_arrive(smem_u32(&sh.d_empty[buf]));
+                    }
+                    __nv_bfloat16* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
 #pragma unroll
-                for (int i = 0; i < HD / 2; i += 8) st_global32(out + 2 * i, w + i);
+                    for (int i = 0; i < HD / 2; i += 8) st_global32(out + 2 * i, word + i);
+                }
             }
         }
     } else if (warp == 4) {
         // ---- latent vectors, then matrices, on their way in ----
-        const int row = lane < copies ? sh.rows[lane] : -1, n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        const int copies = kLxTile / a.box;
         const uint32_t a_bar = smem_u32(&sh.a_full);
-        if (lane == 0) mbar_arrive_expect_tx(a_bar, n * a.box * 128 * chunks);
-        __syncwarp();
-        if (row >= 0)
-            for (int c = 0; c < chunks; ++c) tma_rows(a_at + c * kLxChunkBytes + lane * a.box * 128, &rows_map, c * 64, row, a_bar);
-        __syncwarp();
-        int st = 0, turn = 0, it = 0;
-        for (int h = head0; h < head1 && ok; ++h)
-            for (int c = 0; c < chunks; ++c, ++it) {
-                if (it >= a.stages && !(ok = wait(sh.b_empty[st], turn ^ 1))) break;
-                if (elect_one()) {
-                    const uint32_t bar = smem_u32(&sh.b_full[st]), at = b_at + st * STAGE;
-                    mbar_arrive_expect_tx(bar, STAGE);
-                    tma_matrix(at, &k_map, c * 64, 0, a.h0 + h, bar);
-                    tma_matrix(at + HD * 128, &v_map, c * 64, 0, a.h0 + h, bar);
+        int st = 0, turn = 0, it = 0, tile = 0;
+        for (; w.more() && ok; w.next(), ++tile) {
+            const LxPlace place = lx_find(a.batch, cap, a.tokens, 0, w.tile);
+            const int row = lane < copies ? row_of(place, lane * a.box, true) : -1, n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+            if (tile > 0 && !(ok = wait(sh.a_empty, (tile - 1) & 1))) break;
+            if (lane == 0) mbar_arrive_expect_tx(a_bar, n * a.box * 128 * chunks);
+            __syncwarp();
+            if (row >= 0)
+                for (int c = 0; c < chunks; ++c) tma_rows(a_at + c * kLxChunkBytes + lane * a.box * 128, &rows_map, c * 64, row, a_bar);
+            __syncwarp();
+            for (int h = w.h0; h < w.h1 && ok; ++h)
+                for (int c = 0; c < chunks; ++c, ++it) {
+                    if (it >= a.stages && !(ok = wait(sh.b_empty[st], turn ^ 1))) break;
+                    if (elect_one()) {
+                        const uint32_t bar = smem_u32(&sh.b_full[st]), to = b_at + st * STAGE;
+                        mbar_arrive_expect_tx(bar, STAGE);
+                        tma_matrix(to, &k_map, c * 64, 0, a.h0 + h, bar);
+                        tma_matrix(to + HD * 128, &v_map, c * 64, 0, a.h0 + h, bar);
+                    }
+                    __syncwarp();
+                    if (++st == a.stages) { st = 0; turn ^= 1; }
                 }
-                __syncwarp();
-                if (++st == a.stages) { st = 0; turn ^= 1; }
-            }
+        }
         // copies under way end before shared memory is given back, whoever has given up
-        mbar_wait_bounded(a_bar, 0, a.wait_ns);
+        if (tile > 0 || !ok) mbar_wait_bounded(a_bar, (max(tile, 1) - 1) & 1, a.wait_ns);
         for (int k = it > a.stages ? it - a.stages : 0; k < it; ++k) mbar_wait_bounded(smem_u32(&sh.b_full[k % a.stages]), (k / a.stages) & 1, a.wait_ns);
         __syncwarp();
     } else {
@@ -240,26 +268,32 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
         const uint32_t hi = uint32_t(a_desc >> 32);
         int st = 0, turn = 0;
         bool any = false;
-        ok = wait(sh.a_full, 0);
-        for (int h = head0; h < head1 && ok; ++h) {
-            const int i = h - head0, buf = i & 1;
-            if (i >= 2 && !(ok = wait(sh.d_empty[buf], (i / 2 - 1) & 1))) break;
-            for (int c = 0; c < chunks; ++c) {
-                if (!(ok = wait(sh.b_full[st], turn))) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t d = tmem + buf * N, lo_a = uint32_t(a_desc) + c * (kLxChunkBytes >> 4), lo_b = uint32_t(b_desc) + st * (STAGE >> 4);
-                    if (c == 0) tc_mma_lo<false>(d, lo_a, hi, lo_b, hi, idesc);
-                    else tc_mma_lo<true>(d, lo_a, hi, lo_b, hi, idesc);
-                    tc_mma_lo<true>(d, lo_a + 2, hi, lo_b + 2, hi, idesc);
-                    tc_mma_lo<true>(d, lo_a + 4, hi, lo_b + 4, hi, idesc);
-                    tc_mma_lo<true>(d, lo_a + 6, hi, lo_b + 6, hi, idesc);
-                    tc_commit(smem_u32(&sh.b_empty[st]));
-                    if (c + 1 == chunks) tc_commit(smem_u32(&sh.d_full[buf]));
+        int i = 0, tile = 0;
+        for (; w.more() && ok; w.next(), ++tile) {
+            ok = wait(sh.a_full, tile & 1);
+            for (int h = w.h0; h < w.h1 && ok; ++h, ++i) {
+                const int buf = i & 1;
+                if (i >= 2 && !(ok = wait(sh.d_empty[buf], (i / 2 - 1) & 1))) break;
+                for (int c = 0; c < chunks; ++c) {
+                    if (!(ok = wait(sh.b_full[st], turn))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t d = tmem + buf * N, lo_a = uint32_t(a_desc) + c * (kLxChunkBytes >> 4), lo_b = uint32_t(b_desc) + st * (STAGE >> 4);
+                        if (c == 0) tc_mma_lo<false>(d, lo_a, hi, lo_b, hi, idesc);
+                        else tc_mma_lo<true>(d, lo_a, hi, lo_b, hi, idesc);
+                        tc_mma_lo<true>(d, lo_a + 2, hi, lo_b + 2, hi, idesc);
+                        tc_mma_lo<true>(d, lo_a + 4, hi, lo_b + 4, hi, idesc);
+                        tc_mma_lo<true>(d, lo_a + 6, hi, lo_b + 6, hi, idesc);
+                        tc_commit(smem_u32(&sh.b_empty[st]));
+                        if (c + 1 == chunks) {
+                            tc_commit(smem_u32(&sh.d_full[buf]));
+                            if (h + 1 == w.h1) tc_commit(smem_u32(&sh.a_empty));
+                        }
+                    }
+                    any = true;
+                    __syncwarp();
+                    if (++st == a.stages) { st = 0; turn ^= 1; }
                 }
-                any = true;
-                __syncwarp();
-                if (++st == a.stages) { st = 0; turn ^= 1; }
             }
         }
         if (any) {                               // products under way end before tensor memory is given back, whoever has given up
