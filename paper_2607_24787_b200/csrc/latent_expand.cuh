@@ -4,7 +4,7 @@
 // matrices, whose rows come by in chunks of 64 elements. Sums of two heads are in tensor memory, so that one is rounded to bf16 and
 // written while the next is made. All (tile of tokens, head) pairs are a line that is cut evenly between CTAs, so that a CTA brings the latent
 // vectors of two or three tiles and not of many (with a CTA for each tile and a third of the heads four prompts' 10563 tokens of 16 heads took
-// 59 us, TODO now). Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
+// 59 us, 54 now). Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
 //
 // A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
 // element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
@@ -201,29 +201,30 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
                 if (!(ok = wait(sh.d_full[buf], turn))) break;
                 tc_fence_after();
                 bool odd = false;
-#pragma unroll
+#pragma unroll 1
                 for (int part = 0; part < 2; ++part) {
-                    uint32_t word[HD / 2];
+                    uint32_t r[HD], word[HD / 2];
 #pragma unroll
-                    for (int ch = 0; ch < HD / 32; ++ch) {
-                        uint32_t r[32];
-                        tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), r);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            if (part == 0) odd |= not_finite(r[i]) || not_finite(r[i + 1]);
-                            else if (odd) {
-                                if (not_finite(r[i])) r[i] = 0;
-                                if (not_finite(r[i + 1])) r[i + 1] = 0;
-                            }
-                            word[ch * 16 + i / 2] = there ? pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1])) : 0u;
-                        }
-                    }
-                    if (part == 0 && odd && there) word[0] = 0x7fff7fffu;
+                    for (int ch = 0; ch < HD / 32; ++ch)
+                        tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), *reinterpret_cast<uint32_t(*)[32]>(r + ch * 32));
+                    tmem_wait_ld();
                     if (part == 1) {
                         tc_fence_before();
                         mbar_arrive(smem_u32(&sh.d_empty[buf]));
                     }
+                    unsigned long long zero = 0; // 0 times what is not finite is NaN
+#pragma unroll
+                    for (int e = 0; e < HD; e += 2) zero = fma2(two_words(r[e], r[e + 1]), 0ull, zero);
+                    float z0, z1;
+                    floats_of(zero, z0, z1);
+                    const bool bad = z0 != z0 || z1 != z1;
+                    if (part == 0) odd = bad;
+                    else if (odd && bad)
+#pragma unroll
+                        for (int e = 0; e < HD; ++e) r[e] = not_finite(r[e]) ? 0u : r[e];
+#pragma unroll
+                    for (int e = 0; e < HD; e += 2) word[e / 2] = there ? pack_bf16(__uint_as_float(r[e]), __uint_as_float(r[e + 1])) : 0u;
+                    if (part == 0 && odd && there) word[0] = 0x7fff7fffu;
                     __nv_bfloat16* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
 #pragma unroll
                     for (int i = 0; i < HD / 2; i += 8) st_global32(out + 2 * i, word + i);
