@@ -610,10 +610,12 @@ typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
  * heads, over the tokens up to the row's own position, with key = [W_k latent | key of the row] and value = W_v latent made from the cache for
  * all tokens of the batch's sequences, a round of heads at a time. q: heads of head_dim + rope_dim elements. head_dim: 64 or 128.
  * n_tokens: at least the tokens of all sequences that have rows in this batch (the sum of their lengths), which is what the workspace has
- * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. dtype: bf16 (fp32 rows have the absorbed form). Keys' first
- * parts, values, probabilities and results are rounded to bf16 once each; statistics and sums are fp32. What is said above of queries and
+ * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. dtype: bf16 (fp32 rows have the absorbed form). Results are
+ * rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two: a query's element keeps fewer bits below
+ * 2^-23 of its head's largest, a key's below 2^-23 of the largest of its 32 tokens and head, a value below 2^-18 of its head's largest so far, a
+ * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and
  * rows that are not finite holds, but that any element of a row that is not finite makes all elements of the result NaN.
- * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * head_dim * 4 and a little more, but
+ * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * (head_dim + 32) * 4 and a little more, but
  * not much over 512 MB where a head takes less); one for each of calls that may run at the same time. */
 int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,
                                          size_t* bytes);

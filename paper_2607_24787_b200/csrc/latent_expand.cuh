@@ -6,6 +6,9 @@
 // vectors of two or three tiles and not of many (with a CTA for each tile and a third of the heads four prompts' 10563 tokens of 16 heads took
 // 59 us, 54 now). Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
 //
+// Both are fp16, times a power of two for each 32 tokens of a head: bf16's roundings of keys, values and probabilities were together 1.4 times that
+// of the result. The key that all heads share stands behind each head's own, times the same power of two.
+//
 // A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
 // element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
 #pragma once
@@ -20,6 +23,11 @@
 
 namespace spm {
 
+constexpr int kLxLeast = -110;                   // E of values that are all zero, or nearly
+__device__ __forceinline__ uint32_t pack_fp16(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
 constexpr int kLxTile = 128, kLxThreads = 192, kLxChunkBytes = kLxTile * 128;
 
 struct LatentExpandArgs {
@@ -29,7 +37,8 @@ struct LatentExpandArgs {
     int box;                    // tokens of a copy, all of one page
     int stages;                 // of the matrices' ring
     int tokens;                 // that the workspace has room for, a multiple of 128
-    __nv_bfloat16 *keys, *values, *ropes;       // [heads][tokens][HD] twice, [tokens][64]
+    __half *keys, *values;                      // [heads][tokens][HD + 64], [heads][tokens][HD], times 2^-E
+    short *key_exps, *value_exps;               // [heads][tokens / 32]: E
     uint32_t* there;            // [tokens / 32]
     unsigned long long wait_ns;
     int withhold;
@@ -191,10 +200,17 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
             if (w.h0 == 0) {
                 const uint32_t bits = __ballot_sync(0xffffffffu, there);
                 if (lane == 0) a.there[to / 32] = bits;
-                const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + static_cast<long long>(there ? row : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
-                uint4* rope = reinterpret_cast<uint4*>(a.ropes + to * 64);
+            }
+            // the shared key, as it is in the cache, and its largest magnitude
+            const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + static_cast<long long>(there ? row : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
+            auto rope = [&](int k) { return there && k < a.kv.rope / 8 ? from[k] : make_uint4(0, 0, 0, 0); };
+            uint32_t rope_top = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) rope[k] = there && k < a.kv.rope / 8 ? from[k] : make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < 8; ++k) {
+                const uint4 v = rope(k);
+                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rope_top = max(rope_top, max(x[e] << 16 & 0x7fffffffu, x[e] & 0x7fff0000u));
             }
             for (int h = w.h0; h < w.h1; ++h, ++i) {
                 const int buf = i & 1, turn = i >> 1 & 1;
@@ -218,16 +234,46 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
                     float z0, z1;
                     floats_of(zero, z0, z1);
                     const bool bad = z0 != z0 || z1 != z1;
-                    if (part == 0) odd = bad;
+                    if (!there)
+#pragma unroll
+                        for (int e = 0; e < HD; ++e) r[e] = 0u;
+                    if (part == 0) odd = there && (bad || rope_top >= 0x7f800000u);
                     else if (odd && bad)
 #pragma unroll
                         for (int e = 0; e < HD; ++e) r[e] = not_finite(r[e]) ? 0u : r[e];
+                    // the largest of a warp's tokens is brought to [2^9, 2^10)
+                    uint32_t top = part == 0 ? rope_top : 0;
 #pragma unroll
-                    for (int e = 0; e < HD; e += 2) word[e / 2] = there ? pack_bf16(__uint_as_float(r[e]), __uint_as_float(r[e + 1])) : 0u;
-                    if (part == 0 && odd && there) word[0] = 0x7fff7fffu;
-                    __nv_bfloat16* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
+                    for (int e = 0; e < HD; ++e) top = max(top, r[e] & 0x7fffffffu);
+                    top = __reduce_max_sync(0xffffffffu, part == 0 && odd ? 0u : top);
+                    const int power = top == 0 ? kLxLeast : max(kLxLeast, min(int(top >> 23) - 127 - 9, 118));
+                    const float by = __int_as_float((127 - power) << 23);
 #pragma unroll
-                    for (int i = 0; i < HD / 2; i += 8) st_global32(out + 2 * i, word + i);
+                    for (int e = 0; e < HD; e += 2) word[e / 2] = pack_fp16(__uint_as_float(r[e]) * by, __uint_as_float(r[e + 1]) * by);
+                    if (lane == 0) (part == 0 ? a.key_exps : a.value_exps)[(size_t(h) * a.tokens + to) / 32] = short(power);
+                    if (part == 1) {
+                        __half* out = a.values + (size_t(h) * a.tokens + to) * HD;
+#pragma unroll
+                        for (int e = 0; e < HD / 2; e += 8) st_global32(out + 2 * e, word + e);
+                        continue;
+                    }
+                    if (odd) word[0] = 0x7fff7fffu;
+                    __half* out = a.keys + (size_t(h) * a.tokens + to) * (HD + 64);
+#pragma unroll
+                    for (int e = 0; e < HD / 2; e += 8) st_global32(out + 2 * e, word + e);
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+                        const uint4 u = rope(k), v = rope(k + 1);
+                        const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                        uint32_t y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float lo, hi;
+                            two_bf16(x[e], lo, hi);
+                            y[e] = pack_fp16(lo * by, hi * by);
+                        }
+                        st_global32(out + HD + k * 8, y);
+                    }
                 }
             }
         }

@@ -3,10 +3,12 @@
 // A CTA takes 256 rows of a head of one sequence, two M = 128 halves, and walks the tokens in tiles of 128. A key is HD elements of its
 // head and a chunk of up to 64 that all heads share; keys and values come by TMA. One warp issues the products; four warps a half turn scores
 // into probabilities, one row a thread, while the tensor cores are at the other half: S(j) of one half, then P V(j) and S(j + 1) of the
-// other. Scores, probabilities (bf16, in the scores' place, as the A operand of the second product) and sums stay in tensor memory.
+// other. Scores, probabilities (fp16, in the scores' place, as the A operand of the second product) and sums stay in tensor memory.
 //
-// A row's maximum is moved, and its sums scaled, only where a score is above it by more than 64 in powers of two: probabilities are
-// bf16, which has fp32's range, so nothing is lost before that. A probability, a key's first part and a value are rounded to bf16 once.
+// Keys and values stand at 2^-E, E for each 32 tokens, and a row's queries are brought to [2^9, 2^10) by its largest, all in fp16. A row's maximum is
+// moved, and its sums scaled, only where a score is above it by more than 2^6. Probabilities are fp16, times 2^4 and 2^(E - R), R the largest
+// E of values so far but for 5, which moves, and the sums with it, where an E is above that. So no probability is above 2^15, and 11 bits
+// hold for those down to 2^-18 of the largest and values down to 2^-18 of their head's largest.
 #pragma once
 
 #include <cuda.h>
@@ -24,16 +26,20 @@ struct LatentPromptArgs {
     int heads, h0;              // of this round, the first one's number
     int tokens;                 // of the workspace
     const uint32_t* there;
+    const short *key_exps, *value_exps;
     float factor;               // of scores: scale times log2(e)
     unsigned long long wait_ns;
     int withhold;
 };
 
 constexpr int kLpTile = 128;
+constexpr float kLpSlack = 6.f, kLpUp = 4.f;     // scores above the maximum that was, and probabilities' scale, as powers of two
+constexpr int kLpRoom = 5;                       // of E above R
 // two halves' softmax warps, then the copying warp, the issuing warp and two that only make its four whole. Registers a thread: 168 at the launch,
 // of which the last four give some to the softmax warps
 constexpr int kLpThreads = 12 * 32, kLpSoftmaxRegs = 208, kLpOtherRegs = 88;
 static_assert(2 * kLpSoftmaxRegs + kLpOtherRegs <= 3 * 168, "the split is what the launch has");
+__device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
 template <int HD>
 struct LpShape {
     static constexpr int chunk = kLpTile * 128;                          // 64 elements of 128 rows
@@ -56,7 +62,7 @@ __device__ __forceinline__ uint32_t lp_chunk(int row, int ch) { return uint32_t(
 
 template <int HD>
 __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const LatentPromptArgs a, const __grid_constant__ CUtensorMap k_map,
-                                                                      const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap v_map) {
+                                                                      const __grid_constant__ CUtensorMap v_map) {
     using S = LpShape<HD>;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     const uint32_t q_at = (smem_u32(raw_smem) + 1023) & ~1023u, k_at = q_at + 2 * S::k_bytes, v_at = k_at + 2 * S::k_bytes;
@@ -140,19 +146,46 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
             if (lane < vectors) copy16_or_zero(q_at + half * S::k_bytes + lp_chunk((row_in & ~31) + i, lane), from ? from + lane * 8 : static_cast<const __nv_bfloat16*>(a.q.p), from != nullptr);
         }
         copies_arrived();
+        __syncwarp();
+        uint32_t top = 0;                        // this lane's row: its largest magnitude, as bf16 bits
+        const uint32_t row_at = q_at + half * S::k_bytes;
+#pragma unroll 4
+        for (int ch = 0; ch < vectors; ++ch) {
+            const uint4 v = lds128(row_at + lp_chunk(row_in, ch));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7fffu, w[k] >> 16 & 0x7fffu));
+        }
+        const int e = top == 0 || top >= 0x7f80u ? 0 : min(9 - (int(top >> 7) - 127), 120);
+        const float up = exp2f(float(e)), sign = a.factor < 0.f ? -up : up;
+#pragma unroll 4
+        for (int ch = 0; ch < vectors; ++ch) {
+            const uint32_t where = row_at + lp_chunk(row_in, ch);
+            const uint4 v = lds128(where);
+            float x[8];
+            two_bf16(v.x, x[0], x[1]); two_bf16(v.y, x[2], x[3]); two_bf16(v.z, x[4], x[5]); two_bf16(v.w, x[6], x[7]);
+            st_shared16(where, make_uint4(pack_fp16(x[0] * sign, x[1] * sign), pack_fp16(x[2] * sign, x[3] * sign), pack_fp16(x[4] * sign, x[5] * sign),
+                                          pack_fp16(x[6] * sign, x[7] * sign)));
+        }
         fence_proxy_async();
         together();
         // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
         const int own_tiles = half == 0 ? tiles0 : tiles1;
         const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
-        const float f = fmaxf(fabsf(a.factor), 0x1p-126f);        // (not zero: masked scores are -infinity)
+        const float f = fabsf(a.factor) / up;
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         const uint4* bits = reinterpret_cast<const uint4*>(a.there + at / 32);
+        const size_t first_32 = (size_t(head) * a.tokens + at) / 32;
+        const short4 *powers_of = reinterpret_cast<const short4*>(a.value_exps + first_32), *units_of = reinterpret_cast<const short4*>(a.key_exps + first_32);
         uint4 bits_then = own_tiles > 0 ? bits[0] : make_uint4(0, 0, 0, 0);
+        short4 powers_then = own_tiles > 0 ? powers_of[0] : make_short4(0, 0, 0, 0), units_then = own_tiles > 0 ? units_of[0] : powers_then;
+        int run = -1000;                         // R
         for (int j = 0; j < own_tiles && ok; ++j) {
             uint32_t there[4] = {bits_then.x, bits_then.y, bits_then.z, bits_then.w};
-            if (j + 1 < own_tiles) bits_then = bits[j + 1];
+            const int power[4] = {powers_then.x, powers_then.y, powers_then.z, powers_then.w};
+            const float unit[4] = {two_to(units_then.x), two_to(units_then.y), two_to(units_then.z), two_to(units_then.w)};
+            if (j + 1 < own_tiles) { bits_then = bits[j + 1]; powers_then = powers_of[j + 1]; units_then = units_of[j + 1]; }
             bool whole = (j + 1) * kLpTile <= limit && (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu;
             whole = __all_sync(0xffffffffu, whole);
             if (!(ok = wait(sh.s_full[half], j & 1))) break;
@@ -167,11 +200,6 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_at + 32 * ch, r[ch]);
             tmem_wait_ld();
-            if (a.factor < 0.f)
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) r[ch][i] ^= 0x80000000u;
             if (!whole)
 #pragma unroll
                 for (int ch = 0; ch < 4; ++ch)
@@ -185,13 +213,20 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
 #pragma unroll
                 for (int i = 1; i < 32; ++i) tops[ch] = fmaxf(tops[ch], __uint_as_float(r[ch][i]));
             }
-            const float peak = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-            if (__any_sync(0xffffffffu, m == -INFINITY || (peak - m) * f > kLaSlack)) {
+            const float peak = fmaxf(fmaxf(tops[0] * unit[0], tops[1] * unit[1]), fmaxf(tops[2] * unit[2], tops[3] * unit[3]));
+            int power_top = -1000;               // of values that this row sees
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch)
+                if (whole || there[ch] != 0) power_top = max(power_top, power[ch]);
+            if (__any_sync(0xffffffffu, m == -INFINITY || (peak - m) * f > kLpSlack || power_top > run + kLpRoom)) {
                 // (scores of a query with an infinity may all be -infinity, as those of tokens that it does not see are: NaN)
                 if (m == -INFINITY && peak == -INFINITY && (there[0] | there[1] | there[2] | there[3])) l = __int_as_float(0x7fffffff);
                 const float to = fmaxf(m, peak), by = m == -INFINITY ? 1.f : ex2((m - to) * f);
                 m = to;
                 l *= by;
+                const int run_then = power_top > run + kLpRoom ? power_top : run;
+                const float down = by * exp2f(float(max(run - run_then, -200)));
+                run = run_then;
                 if (j > 0) {                     // (before that the sums hold nothing)
 #pragma unroll 1
                     for (int ch = 0; ch < HD / 16; ++ch) {
@@ -199,32 +234,33 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                         tmem_ld16_raw(o_at + 16 * ch, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * down);
                         tmem_st16(o_at + 16 * ch, o);
                     }
                 }
             }
             const float base = m == -INFINITY ? 0.f : -m * f;
-            const unsigned long long base2 = two_floats(base, base), f2 = two_floats(f, f);
-            unsigned long long sum0 = 0, sum1 = 0;
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) {
+                // (values 2^60 below the largest are as good as zero, and yet their tokens' probabilities count)
+                const float f_of = fmaxf(f * unit[ch], 0x1p-126f);             // (not zero: masked scores are -infinity)
+                const float shift = float(max(power[ch] - run, -60)), from = base + (kLpUp + shift);
+                const unsigned long long from2 = two_floats(from, from), f2 = two_floats(f_of, f_of);
+                unsigned long long sum0 = 0, sum1 = 0;
                 uint32_t p[16];
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) {
                     float x0, x1;
-                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, base2), x0, x1);
+                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, from2), x0, x1);
                     const float p0 = ex2(x0), p1 = ex2(x1);
                     unsigned long long& sum = i & 2 ? sum1 : sum0;
                     sum = add2(sum, two_floats(p0, p1));
-                    p[i / 2] = pack_bf16(p0, p1);
+                    p[i / 2] = pack_fp16(p0, p1);
                 }
                 tmem_st16(s_at + 16 * ch, p);
-            }
-            {
                 float x0, x1;
                 floats_of(add2(sum0, sum1), x0, x1);
-                l += x0 + x1;
+                l = fmaf(x0 + x1, ex2(-shift), l);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -235,7 +271,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         if (ok) {
             // the rows go out by way of the half's queries' place, HD / 8 lanes a row
             constexpr int LANES = HD / 8, AT_ONCE = 32 / LANES;
-            const float by = l == 0.f ? 0.f : 1.f / l;
+            const float by = l == 0.f ? 0.f : exp2f(float(run)) / l;
             const uint32_t rows_at = q_at + half * S::k_bytes + (row_in & ~31) * (HD * 2);
 #pragma unroll 1
             for (int ch = 0; ch < HD / 32; ++ch) {
@@ -276,8 +312,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                 if (elect_one()) {
                     const uint32_t bar = smem_u32(&sh.k_full[j & 1]), to = k_at + (j & 1) * S::k_bytes;
                     mbar_arrive_expect_tx(bar, S::k_bytes);
-                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, row0 + j * kLpTile, bar);
-                    tma_rows(to + HD / 64 * S::chunk, &rope_map, 0, at + j * kLpTile, bar);
+                    for (int c = 0; c < S::k_chunks; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, row0 + j * kLpTile, bar);
                 }
                 __syncwarp();
             };
@@ -311,8 +346,8 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
             together();
             // ---- products. The warp walks as one, so that the elected lane is one lane throughout ----
             if (warp == 8) {
-                constexpr uint32_t idesc_s = la_idesc(kLpTile, kLpTile, false);
-                constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (uint32_t(HD >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+                constexpr uint32_t idesc_s = (1u << 4) | (uint32_t(kLpTile >> 3) << 17) | (uint32_t(kLpTile >> 4) << 24);        // fp16 x fp16 -> fp32
+                constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(HD >> 3) << 17) | (uint32_t(128 >> 4) << 24);
                 const int rope_steps = a.kv.rope / 16;
                 const uint64_t q_desc = smem_desc_sw128(q_at, 16, 1024), k_desc = smem_desc_sw128(k_at, 16, 1024), v_desc = smem_desc_sw128(v_at, S::chunk, 1024);
                 const uint32_t hi = uint32_t(q_desc >> 32);
