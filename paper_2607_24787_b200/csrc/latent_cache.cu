@@ -74,9 +74,9 @@ cudaError_t launch_attend(LatentAttendArgs a, int dev, int sms, cudaStream_t st)
 }
 
 // ---- expanded attention ----
-// The workspace: keys and values of a round's heads, [heads][tokens][head_dim + 64] and [heads][tokens][head_dim], a bit a token, and powers of two
-// of keys and of values for each 32 tokens
-struct Expanded { int tokens, heads, rounds; size_t values, there, key_exps, value_exps, bytes; };
+// The workspace: keys and values of a round's heads, [heads][tokens][head_dim] each, the shared parts of keys, [heads][tokens][64] (written where a
+// head's differ) and [tokens][64], a bit a token, and powers of two of keys and of values for each 32 tokens
+struct Expanded { int tokens, heads, rounds; size_t values, own, shared, there, key_exps, value_exps, bytes; };
 constexpr size_t kLxMost = size_t(512) << 20;    // of keys and values together, where more than one head is more
 Expanded expanded_of(const spm_kv_batch* b, int n_heads, int head_dim, int n_tokens) {
     Expanded e{};
@@ -85,8 +85,11 @@ Expanded expanded_of(const spm_kv_batch* b, int n_heads, int head_dim, int n_tok
     e.rounds = int((n_heads + std::max<size_t>(1, kLxMost / head) - 1) / std::max<size_t>(1, kLxMost / head));
     e.heads = (n_heads + e.rounds - 1) / e.rounds;
     e.rounds = (n_heads + e.heads - 1) / e.heads;
-    e.values = size_t(e.heads) * e.tokens * (head_dim + 64) * 2;
-    e.there = e.heads * head;
+    const size_t rows = size_t(e.heads) * e.tokens;
+    e.values = rows * head_dim * 2;
+    e.own = 2 * e.values;
+    e.shared = e.own + rows * 128;
+    e.there = e.shared + size_t(e.tokens) * 128;
     e.key_exps = e.there + size_t(e.tokens) / 8;
     e.value_exps = e.key_exps + size_t(e.heads) * e.tokens / 16;
     e.bytes = e.value_exps + size_t(e.heads) * e.tokens / 16;
@@ -110,7 +113,7 @@ int check_matrices(const char* call, const char* name, const spm_matrices* w, in
 
 template <int HD>
 cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expanded& e, int n_heads, const CUtensorMap& rows, const CUtensorMap& wk, const CUtensorMap& wv,
-                            const CUtensorMap& keys, const CUtensorMap& values, int dev, int sms, cudaStream_t st) {
+                            const CUtensorMap& keys, const CUtensorMap& ropes, const CUtensorMap& ropes32, const CUtensorMap& values, int dev, int sms, cudaStream_t st) {
     cudaError_t err = allow_smem<latent_expand_kernel<HD>>(dev, kMaxSmem);
     if (err == cudaSuccess) err = allow_smem<latent_prompt_kernel<HD>>(dev, LpShape<HD>::smem);
     const int fixed = kLxOwnBytes + 1024 + x.kv.latent / 64 * kLxChunkBytes, stage = 2 * HD * 128;
@@ -124,7 +127,7 @@ cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expand
         if (err != cudaSuccess) break;
         const long long items = (a.batch.n_rows / kPfCols + a.batch.n_seq) * static_cast<long long>(a.heads);
         if (items > INT32_MAX) return cudaErrorInvalidValue;
-        err = launch_early(latent_prompt_kernel<HD>, unsigned(items), kLpThreads, LpShape<HD>::smem, st, a, keys, values);
+        err = launch_early(latent_prompt_kernel<HD>, unsigned(items), kLpThreads, LpShape<HD>::smem, st, a, keys, ropes, ropes32, values);
     }
     return err;
 }
@@ -276,7 +279,7 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     const Expanded e = expanded_of(batch, n_heads, head_dim, n_tokens);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < e.bytes)
         return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold " + std::to_string(e.bytes) + " bytes");
-    if (static_cast<long long>(e.tokens) * e.heads > INT32_MAX) return fail(call, SPM_ERR_CONFIG, "n_tokens times heads is over 2^31 - 1");
+    if (static_cast<long long>(e.tokens) * (e.heads + 1) > INT32_MAX) return fail(call, SPM_ERR_CONFIG, "n_tokens times heads is over 2^31 - 1");
     int dev = 0, sms = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -290,6 +293,8 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     x.tokens = e.tokens;
     x.keys = reinterpret_cast<__half*>(work);
     x.values = reinterpret_cast<__half*>(work + e.values);
+    x.own = reinterpret_cast<__half*>(work + e.own);
+    x.shared = reinterpret_cast<__half*>(work + e.shared);
     x.key_exps = reinterpret_cast<short*>(work + e.key_exps);
     x.value_exps = reinterpret_cast<short*>(work + e.value_exps);
     x.there = reinterpret_cast<uint32_t*>(work + e.there);
@@ -300,22 +305,24 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     a.batch = x.batch;
     a.q = rows_of(q); a.out = rows_of(out);
     a.tokens = e.tokens;
+    a.shared_row = e.heads * e.tokens;
     a.there = x.there;
     a.key_exps = x.key_exps;
     a.value_exps = x.value_exps;
     a.factor = factor;
     a.wait_ns = x.wait_ns;
     a.withhold = x.withhold;
-    CUtensorMap rows{}, wk, wv, keys, values;         // (a pool without pages: no copy is made of it)
+    CUtensorMap rows{}, wk, wv, keys, ropes, ropes32, values;         // (a pool without pages: no copy is made of it)
     const uint64_t made = uint64_t(e.heads) * e.tokens;
     if ((kv->n_pages > 0 && !make_token_map(&rows, kv->rows, kv->latent_dim + kv->rope_dim, uint64_t(kv->n_pages) * kv->page_size, x.box)) ||
         !make_matrix_map(&wk, w_k->p, kv->latent_dim, head_dim, n_heads, w_k->row_stride, w_k->head_stride) ||
         !make_matrix_map(&wv, w_v->p, kv->latent_dim, head_dim, n_heads, w_v->row_stride, w_v->head_stride) ||
-        !make_token_map(&keys, x.keys, head_dim + 64, made, kLpTile) || !make_token_map(&values, x.values, head_dim, made, kLpTile))
+        !make_token_map(&keys, x.keys, head_dim, made, kLpTile) || !make_token_map(&values, x.values, head_dim, made, kLpTile) ||
+        !make_token_map(&ropes, x.own, 64, made + e.tokens, kLpTile) || !make_token_map(&ropes32, x.own, 64, made + e.tokens, 32))
         return fail(call, SPM_ERR_CUDA, "no tensor map of the cache's rows, the matrices or the workspace");
     const auto st = static_cast<cudaStream_t>(stream);
-    return launched(call, head_dim == 64 ? launch_expanded<64>(x, a, e, n_heads, rows, wk, wv, keys, values, dev, sms, st)
-                                         : launch_expanded<128>(x, a, e, n_heads, rows, wk, wv, keys, values, dev, sms, st));
+    return launched(call, head_dim == 64 ? launch_expanded<64>(x, a, e, n_heads, rows, wk, wv, keys, ropes, ropes32, values, dev, sms, st)
+                                         : launch_expanded<128>(x, a, e, n_heads, rows, wk, wv, keys, ropes, ropes32, values, dev, sms, st));
 }
 
 int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, int64_t w_row_stride, int transposed, const spm_rows* y, int n_rows,

@@ -7,7 +7,8 @@
 // 59 us, 54 now). Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
 //
 // Both are fp16, times a power of two for each 32 tokens of a head: bf16's roundings of keys, values and probabilities were together 1.4 times that
-// of the result. The key that all heads share stands behind each head's own, times the same power of two.
+// of the result. A key's power is 1 where the largest of its 32 tokens is in fp16's range as it is, which it is but for odd models, and the part
+// that all heads share is there once; elsewhere each head has a copy of that too, times its own power of two.
 //
 // A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
 // element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
@@ -28,7 +29,7 @@ __device__ __forceinline__ uint32_t pack_fp16(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-constexpr int kLxTile = 128, kLxThreads = 192, kLxChunkBytes = kLxTile * 128;
+constexpr int kLxTile = 128, kLxThreads = 320, kLxChunkBytes = kLxTile * 128;
 
 struct LatentExpandArgs {
     LatentPool kv;
@@ -37,7 +38,8 @@ struct LatentExpandArgs {
     int box;                    // tokens of a copy, all of one page
     int stages;                 // of the matrices' ring
     int tokens;                 // that the workspace has room for, a multiple of 128
-    __half *keys, *values;                      // [heads][tokens][HD + 64], [heads][tokens][HD], times 2^-E
+    __half *keys, *values;                      // [heads][tokens][HD] twice, times 2^-E
+    __half *shared, *own;                       // the shared parts of keys: [tokens][64], and [heads][tokens][64] times 2^-E, where that is not 1
     short *key_exps, *value_exps;               // [heads][tokens / 32]: E
     uint32_t* there;            // [tokens / 32]
     unsigned long long wait_ns;
@@ -146,13 +148,13 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
         mbar_init(smem_u32(&sh.a_full), 1 + a.withhold);
         mbar_init(smem_u32(&sh.a_empty), 1);
         for (int i = 0; i < a.stages; ++i) { mbar_init(smem_u32(&sh.b_full[i]), 1); mbar_init(smem_u32(&sh.b_empty[i]), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.d_full[i]), 1); mbar_init(smem_u32(&sh.d_empty[i]), 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.d_full[i]), 1); mbar_init(smem_u32(&sh.d_empty[i]), 256); }
         mbar_init(smem_u32(&sh.drained), 1);
         sh.quit = 0;
         fence_barrier_init();
     }
-    if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), 2 * N);
-    if (warp == 4) {
+    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 2 * N);
+    if (warp == 8) {
         const int tiles = lx_tiles(a.batch, cap, a.tokens);
         if (lane == 0) sh.tiles = tiles;
     }
@@ -189,21 +191,39 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
     };
     bool ok = true;
 
-    if (warp < 4) {
-        // ---- rows out: a token a thread ----
+    if (warp < 8) {
+        // ---- rows out: a token a thread, four warps its keys and four its values ----
+        const int part = warp >> 2, in = tid & 127;
+        const uint32_t lanes = uint32_t(warp & 3) << 21;
         int i = 0;                               // heads so far
         for (; w.more() && ok; w.next()) {
             const LxPlace place = lx_find(a.batch, cap, a.tokens, 0, w.tile);
-            const int row = row_of(place, tid, false);
+            const int row = row_of(place, in, false);
             const bool there = row >= 0;
-            const size_t to = size_t(w.tile) * kLxTile + tid;
-            if (w.h0 == 0) {
-                const uint32_t bits = __ballot_sync(0xffffffffu, there);
-                if (lane == 0) a.there[to / 32] = bits;
-            }
-            // the shared key, as it is in the cache, and its largest magnitude
+            const size_t to = size_t(w.tile) * kLxTile + in;
+            // the shared key, as it is in the cache
             const uint4* from = reinterpret_cast<const uint4*>(a.kv.rows + static_cast<long long>(there ? row : 0) * (a.kv.latent + a.kv.rope) + a.kv.latent);
             auto rope = [&](int k) { return there && k < a.kv.rope / 8 ? from[k] : make_uint4(0, 0, 0, 0); };
+            auto shared_key = [&](__half* out, float by) {
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) {
+                    const uint4 u = rope(k), v = rope(k + 1);
+                    const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                    uint32_t y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float lo, hi;
+                        two_bf16(x[e], lo, hi);
+                        y[e] = pack_fp16(lo * by, hi * by);
+                    }
+                    st_global32(out + k * 8, y);
+                }
+            };
+            if (w.h0 == 0 && part == 0) {
+                const uint32_t bits = __ballot_sync(0xffffffffu, there);
+                if (lane == 0) a.there[to / 32] = bits;
+                shared_key(a.shared + to * 64, 1.f);
+            }
             uint32_t rope_top = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -216,68 +236,54 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
                 const int buf = i & 1, turn = i >> 1 & 1;
                 if (!(ok = wait(sh.d_full[buf], turn))) break;
                 tc_fence_after();
-                bool odd = false;
-#pragma unroll 1
-                for (int part = 0; part < 2; ++part) {
-                    uint32_t r[HD], word[HD / 2];
+                uint32_t r[HD], word[HD / 2];
+                auto take = [&](int which) {
 #pragma unroll
                     for (int ch = 0; ch < HD / 32; ++ch)
-                        tmem_ld32(tmem + buf * N + part * HD + ch * 32 + (uint32_t(warp) << 21), *reinterpret_cast<uint32_t(*)[32]>(r + ch * 32));
+                        tmem_ld32(tmem + buf * N + which * HD + ch * 32 + lanes, *reinterpret_cast<uint32_t(*)[32]>(r + ch * 32));
                     tmem_wait_ld();
-                    if (part == 1) {
-                        tc_fence_before();
-                        mbar_arrive(smem_u32(&sh.d_empty[buf]));
-                    }
+                };
+                auto not_all_finite = [&] {
                     unsigned long long zero = 0; // 0 times what is not finite is NaN
 #pragma unroll
                     for (int e = 0; e < HD; e += 2) zero = fma2(two_words(r[e], r[e + 1]), 0ull, zero);
                     float z0, z1;
                     floats_of(zero, z0, z1);
-                    const bool bad = z0 != z0 || z1 != z1;
-                    if (!there)
-#pragma unroll
-                        for (int e = 0; e < HD; ++e) r[e] = 0u;
-                    if (part == 0) odd = there && (bad || rope_top >= 0x7f800000u);
-                    else if (odd && bad)
+                    return there && (z0 != z0 || z1 != z1);
+                };
+                take(part);
+                bool odd = not_all_finite() || (there && part == 0 && rope_top >= 0x7f800000u);
+                if (part == 1 && __any_sync(0xffffffffu, odd)) {             // values: is it the token, or the matrix?
+                    take(0);
+                    const bool token = not_all_finite() || (there && rope_top >= 0x7f800000u);
+                    take(1);
+                    if (token)
 #pragma unroll
                         for (int e = 0; e < HD; ++e) r[e] = not_finite(r[e]) ? 0u : r[e];
-                    // the largest of a warp's tokens is brought to [2^9, 2^10)
-                    uint32_t top = part == 0 ? rope_top : 0;
-#pragma unroll
-                    for (int e = 0; e < HD; ++e) top = max(top, r[e] & 0x7fffffffu);
-                    top = __reduce_max_sync(0xffffffffu, part == 0 && odd ? 0u : top);
-                    const int power = top == 0 ? kLxLeast : max(kLxLeast, min(int(top >> 23) - 127 - 9, 118));
-                    const float by = __int_as_float((127 - power) << 23);
-#pragma unroll
-                    for (int e = 0; e < HD; e += 2) word[e / 2] = pack_fp16(__uint_as_float(r[e]) * by, __uint_as_float(r[e + 1]) * by);
-                    if (lane == 0) (part == 0 ? a.key_exps : a.value_exps)[(size_t(h) * a.tokens + to) / 32] = short(power);
-                    if (part == 1) {
-                        __half* out = a.values + (size_t(h) * a.tokens + to) * HD;
-#pragma unroll
-                        for (int e = 0; e < HD / 2; e += 8) st_global32(out + 2 * e, word + e);
-                        continue;
-                    }
-                    if (odd) word[0] = 0x7fff7fffu;
-                    __half* out = a.keys + (size_t(h) * a.tokens + to) * (HD + 64);
-#pragma unroll
-                    for (int e = 0; e < HD / 2; e += 8) st_global32(out + 2 * e, word + e);
-#pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
-                        const uint4 u = rope(k), v = rope(k + 1);
-                        const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-                        uint32_t y[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float lo, hi;
-                            two_bf16(x[e], lo, hi);
-                            y[e] = pack_fp16(lo * by, hi * by);
-                        }
-                        st_global32(out + HD + k * 8, y);
-                    }
                 }
+                tc_fence_before();
+                mbar_arrive(smem_u32(&sh.d_empty[buf]));
+                if (!there)
+#pragma unroll
+                    for (int e = 0; e < HD; ++e) r[e] = 0u;
+                // the largest of a warp's tokens is brought to [2^9, 2^10); of keys if it is below 2^-4 or not below 2^15
+                uint32_t top = part == 0 ? rope_top : 0;
+#pragma unroll
+                for (int e = 0; e < HD; ++e) top = max(top, r[e] & 0x7fffffffu);
+                top = __reduce_max_sync(0xffffffffu, part == 0 && odd ? 0u : top);
+                const int power = part == 0 && (top == 0 || (top >= 0x3d800000u && top < 0x47000000u)) ? 0 : top == 0 ? kLxLeast : max(kLxLeast, min(int(top >> 23) - 127 - 9, 118));
+                const float by = __int_as_float((127 - power) << 23);
+#pragma unroll
+                for (int e = 0; e < HD; e += 2) word[e / 2] = pack_fp16(__uint_as_float(r[e]) * by, __uint_as_float(r[e + 1]) * by);
+                if (lane == 0) (part == 0 ? a.key_exps : a.value_exps)[(size_t(h) * a.tokens + to) / 32] = short(power);
+                if (part == 0 && odd) word[0] = 0x7fff7fffu;
+                __half* out = (part == 0 ? a.keys : a.values) + (size_t(h) * a.tokens + to) * HD;
+#pragma unroll
+                for (int e = 0; e < HD / 2; e += 8) st_global32(out + 2 * e, word + e);
+                if (part == 0 && power != 0) shared_key(a.own + (size_t(h) * a.tokens + to) * 64, by);
             }
         }
-    } else if (warp == 4) {
+    } else if (warp == 8) {
         // ---- latent vectors, then matrices, on their way in ----
         const int copies = kLxTile / a.box;
         const uint32_t a_bar = smem_u32(&sh.a_full);
@@ -352,7 +358,7 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 5) tmem_dealloc(tmem, 2 * N);
+    if (warp == 9) tmem_dealloc(tmem, 2 * N);
 }
 
 }  // namespace spm

@@ -24,7 +24,7 @@ struct LatentPromptArgs {
     KvBatch batch;
     HeadRows q, out;
     int heads, h0;              // of this round, the first one's number
-    int tokens;                 // of the workspace
+    int tokens, shared_row;     // of the workspace; where, behind the heads' copies, the shared parts of keys begin
     const uint32_t* there;
     const short *key_exps, *value_exps;
     float factor;               // of scores: scale times log2(e)
@@ -62,6 +62,7 @@ __device__ __forceinline__ uint32_t lp_chunk(int row, int ch) { return uint32_t(
 
 template <int HD>
 __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const LatentPromptArgs a, const __grid_constant__ CUtensorMap k_map,
+                                                                      const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap rope32_map,
                                                                       const __grid_constant__ CUtensorMap v_map) {
     using S = LpShape<HD>;
     extern __shared__ __align__(16) unsigned char raw_smem[];
@@ -308,11 +309,20 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         if (warp == 9) {
             // ---- keys and values on their way in (they need no queries: begun before the others are ready) ----
             const int row0 = head * a.tokens + at;
+            const short4* units_of = reinterpret_cast<const short4*>(a.key_exps + (size_t(head) * a.tokens + at) / 32);
+            short4 units = tiles > 0 ? units_of[0] : make_short4(0, 0, 0, 0);      // of the next tile's keys
             auto keys = [&](int j) {
+                const int own[4] = {units.x, units.y, units.z, units.w};
+                if (j + 1 < tiles) units = units_of[j + 1];
                 if (elect_one()) {
-                    const uint32_t bar = smem_u32(&sh.k_full[j & 1]), to = k_at + (j & 1) * S::k_bytes;
+                    const uint32_t bar = smem_u32(&sh.k_full[j & 1]), to = k_at + (j & 1) * S::k_bytes, rope_to = to + HD / 64 * S::chunk;
+                    const int mine = row0 + j * kLpTile, shared = a.shared_row + at + j * kLpTile;
                     mbar_arrive_expect_tx(bar, S::k_bytes);
-                    for (int c = 0; c < S::k_chunks; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, row0 + j * kLpTile, bar);
+                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, mine, bar);
+                    if ((own[0] | own[1] | own[2] | own[3]) == 0) tma_rows(rope_to, &rope_map, 0, shared, bar);
+                    else                         // this head's copy where there is one
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) tma_rows(rope_to + k * 32 * 128, &rope32_map, 0, (own[k] != 0 ? mine : shared) + k * 32, bar);
                 }
                 __syncwarp();
             };

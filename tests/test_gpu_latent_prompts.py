@@ -117,6 +117,25 @@ def test_values_of_any_size(lib, order):  # noqa: F811
     assert (np.abs(got - want) <= tol).all()
 
 
+@pytest.mark.parametrize("small,large", [(-40, 0), (0, 40), (-30, 30)])
+def test_keys_of_any_size(lib, small, large):  # noqa: F811
+    """Some tokens' keys are far from fp16's range, in tiles with ordinary ones beside them: scores are of one size by the queries, or zero."""
+    c = Case(lib, 33, [500, 130], [500, 30], 128, 32, 16, BF16, fill=True)
+    for seq in range(2):
+        for t in range(c.lengths[seq]):
+            size = [0, small, 0, large, 0, 0, large][t // 32 % 7]
+            c.start[c.table[seq, t // 16], t % 16] *= 2.0 ** size
+    c.cache.pages.copy_(c.start)
+    q, w = c.randn(c.n_rows, 3, 96), matrices(c, 3, 64)
+    w[1].mul_(2.0 ** -large if large else 1.0)
+    for scale in (0.1 * 2.0 ** -large, 0.0):
+        out = f64(c.cache.attend_expanded(c.batch, q, *w, scale, 630))
+        want, spread, reach, made, reach_made = R.attend(f64(q), f64(c.start), c.table.numpy(), c.lengths, c.row_start, scale, 128, f64(w[0]), f64(w[1]))
+        largest = np.nanmax(np.abs(f64(c.start)[..., :128])) * np.abs(f64(w[1])).sum(-1).max()
+        tol = tolerance(want, spread, reach, made, reach_made, 128, 96, 500) + 500 * 2.0 ** -28 * largest
+        assert (np.abs(out - want) <= tol)[:c.n].all()
+
+
 def test_bad_queries_stay_by_themselves(lib):  # noqa: F811
     c = Case(lib, 24, [200, 0, 70], [150, 1, 3], 256, 32, 16, BF16, fill=True)
     w = matrices(c, 3, 64)
