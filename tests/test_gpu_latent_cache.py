@@ -415,6 +415,24 @@ def test_a_step_and_its_replay(lib):
         assert torch.equal(o, want)
 
 
+def test_pools_beyond_4_gigabytes(lib):
+    """Rows whose byte offsets do not fit into 32 bits, signed or not: written, attended to and expanded as in a small pool."""
+    heads, head, page, n = 4, 64, 256, 16_500
+    small = Case(lib, 34, [700], [3], 512, 64, page, BF16)
+    rows = small.randn(700, 576)
+    table = torch.tensor([[2, 0, 1]], dtype=torch.int32)
+    big = lib.LatentCache(torch.empty(n, page, 576, dtype=BF16, device="cuda"), 512)      # 4.9 GB
+    outs = []
+    q, qe, w = small.randn(700, heads, 576), small.randn(700, heads, head + 64), torch.randn(heads, 2 * head, 512, generator=small.g).mul(0.05).to(BF16).cuda()
+    for cache, first in ((lib.LatentCache(torch.empty(3, page, 576, dtype=BF16, device="cuda"), 512), 0), (big, n - 3)):
+        start = torch.tensor([0, 700], dtype=torch.int32, device="cuda")
+        batch = lib.kv.KVBatch((table + first).int().cuda(), torch.tensor([700], dtype=torch.int32, device="cuda"), start, n_rows=700, max_rows=700)
+        cache.write(batch, rows[:, :512], rows[:, 512:])
+        outs.append((cache.attend(batch, q, 0.05), cache.attend_expanded(batch, qe, w[:, :head], w[:, head:], 0.1, 700), cache.pages[first:first + 3].clone()))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
 def test_waits_that_run_out(lib):
     """Copies that never count as landed: the call ends with the status bit, and the next one is right."""
     from paper_2607_24787_b200 import binding as B
