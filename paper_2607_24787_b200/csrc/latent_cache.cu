@@ -75,8 +75,8 @@ cudaError_t launch_attend(LatentAttendArgs a, int dev, int sms, cudaStream_t st)
 
 // ---- expanded attention ----
 // The workspace: keys and values of a round's heads, [heads][tokens][head_dim] each, the shared parts of keys, [heads][tokens][64] (written where a
-// head's differ) and [tokens][64], a bit a token, and powers of two of keys and of values for each 32 tokens
-struct Expanded { int tokens, heads, rounds; size_t values, own, shared, there, key_exps, value_exps, bytes; };
+// head's differ) and [tokens][64], a bit a token, powers of two of keys and of values for each 32 tokens, and the attention's items
+struct Expanded { int tokens, heads, rounds; size_t values, own, shared, there, key_exps, value_exps, items, bytes; int n_items; };
 constexpr size_t kLxMost = size_t(512) << 20;    // of keys and values together, where more than one head is more
 Expanded expanded_of(const spm_kv_batch* b, int n_heads, int head_dim, int n_tokens) {
     Expanded e{};
@@ -92,7 +92,9 @@ Expanded expanded_of(const spm_kv_batch* b, int n_heads, int head_dim, int n_tok
     e.there = e.shared + size_t(e.tokens) * 128;
     e.key_exps = e.there + size_t(e.tokens) / 8;
     e.value_exps = e.key_exps + size_t(e.heads) * e.tokens / 16;
-    e.bytes = e.value_exps + size_t(e.heads) * e.tokens / 16;
+    e.items = (e.value_exps + size_t(e.heads) * e.tokens / 16 + 15) / 16 * 16;
+    e.n_items = b->n_rows / kPfCols + b->n_seq;
+    e.bytes = e.items + size_t(e.n_items) * sizeof(LxItem);
     return e;
 }
 int check_expanded(const char* call, const spm_kv_batch* b, int n_heads, int head_dim, int n_tokens, int dtype) {
@@ -125,7 +127,7 @@ cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expand
         const long long units = static_cast<long long>(tiles) * x.heads;
         err = launch_early(latent_expand_kernel<HD>, unsigned(std::min<long long>(units, sms)), kLxThreads, fixed + x.stages * stage, st, x, rows, wk, wv);
         if (err != cudaSuccess) break;
-        const long long items = (a.batch.n_rows / kPfCols + a.batch.n_seq) * static_cast<long long>(a.heads);
+        const long long items = static_cast<long long>(e.n_items) * a.heads;
         if (items > INT32_MAX) return cudaErrorInvalidValue;
         err = launch_early(latent_prompt_kernel<HD>, unsigned(items), kLpThreads, LpShape<HD>::smem, st, a, keys, ropes, ropes32, values);
     }
@@ -298,6 +300,8 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     x.key_exps = reinterpret_cast<short*>(work + e.key_exps);
     x.value_exps = reinterpret_cast<short*>(work + e.value_exps);
     x.there = reinterpret_cast<uint32_t*>(work + e.there);
+    x.items = reinterpret_cast<LxItem*>(work + e.items);
+    x.n_items = e.n_items;
     x.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     x.withhold = g_withhold.load(std::memory_order_relaxed);
     LatentPromptArgs a{};
@@ -307,6 +311,7 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     a.tokens = e.tokens;
     a.shared_row = e.heads * e.tokens;
     a.there = x.there;
+    a.items = x.items;
     a.key_exps = x.key_exps;
     a.value_exps = x.value_exps;
     a.factor = factor;

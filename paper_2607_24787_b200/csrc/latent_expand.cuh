@@ -20,6 +20,7 @@
 #include "kv_cache.cuh"
 #include "latent_attend.cuh"
 #include "latent_cache.cuh"
+#include "prompt_items.cuh"
 #include "ptx.cuh"
 #include "tc_ops.cuh"
 
@@ -32,6 +33,10 @@ __device__ __forceinline__ uint32_t pack_fp16(float a, float b) {
 }
 constexpr int kLxTile = 128, kLxThreads = 320, kLxChunkBytes = kLxTile * 128;
 
+// What a CTA of the attention takes (its rows, and where their tokens stand in the workspace), found here, where it is beside other work
+struct alignas(16) LxItem { PfItem item; int at, tokens, unused; };
+static_assert(sizeof(LxItem) == 32, "two 16-byte words");
+
 struct LatentExpandArgs {
     LatentPool kv;
     KvBatch batch;
@@ -43,6 +48,8 @@ struct LatentExpandArgs {
     __half *shared, *own;                       // the shared parts of keys: [tokens][64], and [heads][tokens][64] times 2^-E, where that is not 1
     short *key_exps, *value_exps;               // [heads][tokens / 32]: E
     uint32_t* there;            // [tokens / 32]
+    LxItem* items;              // [n_items]
+    int n_items;
     unsigned long long wait_ns;
     int withhold;
 };
@@ -99,6 +106,7 @@ struct LxShared {
     unsigned long long a_full, a_empty, b_full[8], b_empty[8], d_full[2], d_empty[2], drained;
     uint32_t tmem;
     int quit, tiles;
+    PfItem items[8];                             // a warp's
 };
 // A CTA's piece of the line, tile by tile
 struct LxWalk {
@@ -196,6 +204,14 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
         // ---- rows out: a token a thread, four warps its keys and four its values ----
         const int part = warp >> 2, in = tid & 127;
         const uint32_t lanes = uint32_t(warp & 3) << 21;
+        for (int x = blockIdx.x * 8 + warp; x < a.n_items; x += gridDim.x * 8) {
+            PfItem& item = sh.items[warp];
+            pf_find(a.batch, nullptr, 1, cap, x, item);
+            __syncwarp();
+            const LxPlace p = lx_find(a.batch, cap, a.tokens, item.n > 0 ? item.seq : 0, -1);
+            if (lane == 0) a.items[x] = LxItem{item, p.at, p.tokens, 0};
+            __syncwarp();
+        }
         int i = 0;                               // heads so far
         for (; w.more() && ok; w.next()) {
             const LxPlace place = lx_find(a.batch, cap, a.tokens, 0, w.tile);

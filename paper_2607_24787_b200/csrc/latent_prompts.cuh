@@ -30,6 +30,7 @@ struct LatentPromptArgs {
     int heads, h0;              // of this round, the first one's number
     int tokens, shared_row;     // of the workspace; where, behind the heads' copies, the shared parts of keys begin
     const uint32_t* there;
+    const LxItem* items;
     const short *key_exps, *value_exps;
     float factor;               // of scores: scale times log2(e)
     unsigned long long wait_ns;
@@ -37,6 +38,7 @@ struct LatentPromptArgs {
 };
 
 constexpr int kLpTile = 128;
+constexpr int kLpAtOnce = 4;                      // times four rows of queries, that a warp has under way
 constexpr float kLpSlack = 6.f, kLpUp = 4.f;     // scores above the maximum that was, and probabilities' scale, as powers of two
 constexpr int kLpRoom = 5;                       // of E above R
 // two halves' softmax warps, then the copying warp, the issuing warp and two that only make its four whole. Registers a thread: 168 at the launch,
@@ -57,8 +59,6 @@ struct LpShared {
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][2], o_full[2], drained;
     uint32_t tmem;
     int quit;
-    PfItem item;
-    LxPlace place;
 };
 
 // 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
@@ -78,13 +78,9 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
     grid_dep_wait();
     grid_dep_launch();
     const int head = blockIdx.x % a.heads, cap = b.stride * a.kv.page_size;
-    if (warp == 9) {
-        pf_find(b, nullptr, 1, cap, blockIdx.x / a.heads, sh.item);
-        __syncwarp();
-        const LxPlace p = lx_find(b, cap, a.tokens, sh.item.n > 0 ? sh.item.seq : 0, -1);
-        if (lane == 0) sh.place = p;
-    }
-    if (tid == 0) {
+    const LxItem mine = a.items[blockIdx.x / a.heads];
+    if (mine.item.n == 0) return;                // more CTAs than items
+    if (warp == 9 && lane == 0) {                // (the warp that copies, which need not wait for others then)
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 1 + a.withhold); mbar_init(smem_u32(&sh.v_full[i]), 1);
             mbar_init(smem_u32(&sh.k_empty[i]), 1); mbar_init(smem_u32(&sh.v_empty[i]), 1);
@@ -94,15 +90,10 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         sh.quit = 0;
         fence_barrier_init();
     }
+    __syncwarp();
     if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
-    __syncthreads();
-    const int rb = sh.item.rb, first = sh.item.first, n = sh.item.n, len = sh.item.len;
-    const int at = sh.place.at, there_are = n > 0 ? max(0, min(min(len, cap), sh.place.tokens)) : 0;     // tokens in the workspace
-    if (n == 0) {                                // more CTAs than items
-        tc_fence_before();
-        if (warp == 8) tmem_dealloc(sh.tmem, 512);
-        return;
-    }
+    const int rb = mine.item.rb, first = mine.item.first, n = mine.item.n, len = mine.item.len;
+    const int at = mine.at, there_are = max(0, min(min(len, cap), mine.tokens));     // tokens in the workspace
     if (len > there_are && rb == 0 && head == 0 && tid == 0) kv_note(a.kv, SPM_KV_TOO_LONG);
     // tiles of a half: up to the token that its last row sees
     auto sees = [&](int x) { return max(0, min(len - n + min(n - 1, x) + 1, there_are)); };
@@ -143,34 +134,48 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         const int half = warp >> 2, row_in = tid & 127, i_row = rb * kPfCols + tid;
         const int row = i_row < n && first + i_row >= 0 && first + i_row < b.n_rows ? first + i_row : -1;
         const int limit = i_row < n ? sees(i_row) : 0;
-        const __nv_bfloat16* src = row < 0 ? nullptr : static_cast<const __nv_bfloat16*>(a.q.p) + row * a.q.row + (a.h0 + head) * a.q.head;
-        const int vectors = (HD + a.kv.rope) / 8;
-#pragma unroll 4
-        for (int i = 0; i < 32; ++i) {
-            const auto* from = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i));
-            if (lane < vectors) copy16_or_zero(q_at + half * S::k_bytes + lp_chunk((row_in & ~31) + i, lane), from ? from + lane * 8 : static_cast<const __nv_bfloat16*>(a.q.p), from != nullptr);
-        }
-        copies_arrived();
-        __syncwarp();
-        uint32_t top = 0;                        // this lane's row: its largest magnitude, as bf16 bits
-        const uint32_t row_at = q_at + half * S::k_bytes;
-#pragma unroll 4
-        for (int ch = 0; ch < vectors; ++ch) {
-            const uint4 v = lds128(row_at + lp_chunk(row_in, ch));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        // (eight lanes a row, so that a row's largest magnitude is three exchanges away and nothing but the result goes through shared memory)
+        const int oct = lane >> 3, unit = lane & 7, i0 = i_row - lane, there_to = min(n, b.n_rows - first);
+        const bool tail = unit < a.kv.rope / 8;  // of the last chunk's units
+        const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q.p) + (first + static_cast<long long>(i0 + oct)) * a.q.row + (a.h0 + head) * a.q.head + unit * 8;
+        const uint32_t to_at = q_at + half * S::k_bytes + ((row_in & ~31) + oct) * 128;
+        float up = 1.f;                          // 2^e of this lane's row
+#pragma unroll 1
+        for (int g = 0; g < 8; g += kLpAtOnce) {
+            uint4 v[kLpAtOnce][S::k_chunks];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7fffu, w[k] >> 16 & 0x7fffu));
-        }
-        const int e = top == 0 || top >= 0x7f80u ? 0 : min(9 - (int(top >> 7) - 127), 120);
-        const float up = exp2f(float(e)), sign = a.factor < 0.f ? -up : up;
-#pragma unroll 4
-        for (int ch = 0; ch < vectors; ++ch) {
-            const uint32_t where = row_at + lp_chunk(row_in, ch);
-            const uint4 v = lds128(where);
-            float x[8];
-            two_bf16(v.x, x[0], x[1]); two_bf16(v.y, x[2], x[3]); two_bf16(v.z, x[4], x[5]); two_bf16(v.w, x[6], x[7]);
-            st_shared16(where, make_uint4(pack_fp16(x[0] * sign, x[1] * sign), pack_fp16(x[2] * sign, x[3] * sign), pack_fp16(x[4] * sign, x[5] * sign),
-                                          pack_fp16(x[6] * sign, x[7] * sign)));
+            for (int k = 0; k < kLpAtOnce; ++k) {
+                const int i = i0 + (g + k) * 4 + oct;
+                const bool is = i < there_to && first + i >= 0;
+#pragma unroll
+                for (int c = 0; c < S::k_chunks; ++c) {
+                    v[k][c] = make_uint4(0, 0, 0, 0);
+                    if (is && (c + 1 < S::k_chunks || tail)) v[k][c] = *reinterpret_cast<const uint4*>(from + (g + k) * 4 * a.q.row + c * 64);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kLpAtOnce; ++k) {
+                uint32_t top = 0;                // as bf16 bits
+#pragma unroll
+                for (int c = 0; c < S::k_chunks; ++c) {
+                    const uint32_t w[4] = {v[k][c].x, v[k][c].y, v[k][c].z, v[k][c].w};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) top = max(top, max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
+                }
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float by = two_to(top == 0 || top >= 0x7f80u ? 0 : min(9 - (int(top >> 7) - 127), 120)), signed_by = a.factor < 0.f ? -by : by;
+                const float of_row = __shfl_sync(0xffffffffu, by, (lane & 3) * 8);
+                if (lane >> 2 == g + k) up = of_row;
+#pragma unroll
+                for (int c = 0; c < S::k_chunks; ++c) {
+                    float x[8];
+                    two_bf16(v[k][c].x, x[0], x[1]); two_bf16(v[k][c].y, x[2], x[3]); two_bf16(v[k][c].z, x[4], x[5]); two_bf16(v[k][c].w, x[6], x[7]);
+                    st_shared16(to_at + c * S::chunk + (g + k) * 512 + ((unit ^ ((g + k) * 4 + oct & 7)) << 4),
+                                make_uint4(pack_fp16(x[0] * signed_by, x[1] * signed_by), pack_fp16(x[2] * signed_by, x[3] * signed_by),
+                                           pack_fp16(x[4] * signed_by, x[5] * signed_by), pack_fp16(x[6] * signed_by, x[7] * signed_by)));
+                }
+            }
         }
         fence_proxy_async();
         together();
@@ -323,13 +328,13 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                 if (j + 1 < tiles) units = units_of[j + 1];
                 if (elect_one()) {
                     const uint32_t bar = smem_u32(&sh.k_full[j & 1]), to = k_at + (j & 1) * S::k_bytes, rope_to = to + HD / 64 * S::chunk;
-                    const int mine = row0 + j * kLpTile, shared = a.shared_row + at + j * kLpTile;
+                    const int own_row = row0 + j * kLpTile, shared = a.shared_row + at + j * kLpTile;
                     mbar_arrive_expect_tx(bar, S::k_bytes);
-                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, mine, bar);
+                    for (int c = 0; c < HD / 64; ++c) tma_rows(to + c * S::chunk, &k_map, c * 64, own_row, bar);
                     if ((own[0] | own[1] | own[2] | own[3]) == 0) tma_rows(rope_to, &rope_map, 0, shared, bar);
                     else                         // this head's copy where there is one
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) tma_rows(rope_to + k * 32 * 128, &rope32_map, 0, (own[k] != 0 ? mine : shared) + k * 32, bar);
+                        for (int k = 0; k < 4; ++k) tma_rows(rope_to + k * 32 * 128, &rope32_map, 0, (own[k] != 0 ? own_row : shared) + k * 32, bar);
                 }
                 __syncwarp();
             };
@@ -342,8 +347,9 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                 __syncwarp();
             };
             int k_sent = 0, v_sent = 0;
-            if (tiles > 0) { keys(0); values(0); k_sent = v_sent = 1; }
-            together();
+            if (tiles > 0) { keys(0); k_sent = 1; }
+            together();                          // (values are not wanted before, and would be in the queries' way)
+            if (tiles > 0) { values(0); v_sent = 1; }
             for (int j = 0; j < tiles; ++j) {
                 if (j + 1 < tiles) {             // (their place is free before that of the values is)
                     if (j + 1 >= 2 && !(ok = wait(sh.k_empty[(j + 1) & 1], ((j + 1) / 2 - 1) & 1))) break;
