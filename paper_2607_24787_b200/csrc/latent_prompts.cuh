@@ -10,9 +10,11 @@
 // E of values so far but for 5, which moves, and the sums with it, where an E is above that. So no probability is above 2^15, and 11 bits
 // hold for those down to 2^-18 of the largest and values down to 2^-18 of their head's largest.
 //
-// What bounds it: halves take turns, and a turn is the longer of 1880 cycles of softmax (maxima 370, exponentials 1350) and 1790 of products with
-// their hand-over, the scores' at the 128 bytes a cycle that shared memory gives them. Four prompts of up to 2049 rows over up to 4097 tokens, 16 heads of
-// 128 + 64: 148 us, 0.85 PFLOP/s.
+// What bounds it: a half's chain, 3300 cycles a tile, while the other's runs beside it: scores out of tensor memory and maxima 550, exponentials 1300 (the
+// special function units' 16 a cycle, so that a quarter of them are a polynomial: 148 us without, 144), products and their hand-over 1400, of which 20
+// products at 60 cycles are all but 200. With two threads a row it took 161 us: registers for 512 threads spill, and the units are the same. Values in two
+// stages of 64 tokens: 152. Four prompts of up to 2049 rows over up to 4097 tokens, 16 heads of 128 + 64: 144 us, 0.87 PFLOP/s at 1.72 GHz; a CTA's
+// queries and first keys are 5 us of that, its results 2, three times.
 #pragma once
 
 #include <cuda.h>
@@ -64,6 +66,25 @@ struct LpShared {
 // 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
 __device__ __forceinline__ uint32_t lp_chunk(int row, int ch) { return uint32_t((ch >> 3) * (kLpTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)); }
 
+// 2^x of two numbers below 2^7 by the pipes that ex2 leaves idle: 2^n (1 + f (c1 + f (c2 + f c3))), n the next integer, |f| <= 1/2, where the cubic of least
+// relative error that is 1 at 0 is off by 1.02e-4, less than half of fp16's rounding. Below -127 it is 0; NaN stays.
+__device__ __forceinline__ unsigned long long two_to2(unsigned long long x) {
+    float x0, x1;
+    floats_of(x, x0, x1);
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x0));             // -127
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x1));
+    x = two_floats(x0, x1);
+    const float round = 12582912.f;              // 1.5 * 2^23: the sum's lowest bits are n
+    const unsigned long long t = add2(x, two_floats(round, round)), n = add2(t, two_floats(-round, -round)), f = fma2(n, two_floats(-1.f, -1.f), x);
+    unsigned long long y = fma2(f, two_floats(0.05500893f, 0.05500893f), two_floats(0.24221096f, 0.24221096f));
+    y = fma2(y, f, two_floats(0.69328293f, 0.69328293f));
+    y = fma2(y, f, two_floats(1.f, 1.f));
+    float t0, t1;
+    floats_of(t, t0, t1);
+    const unsigned long long by = two_words((__float_as_uint(t0) << 23) + 0x3f800000u, (__float_as_uint(t1) << 23) + 0x3f800000u);
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(y) : "l"(by));
+    return y;
+}
 template <int HD>
 __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const LatentPromptArgs a, const __grid_constant__ CUtensorMap k_map,
                                                                       const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap rope32_map,
@@ -261,9 +282,13 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                 uint32_t p[16];
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) {
-                    float x0, x1;
-                    floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), f2, from2), x0, x1);
-                    const float p0 = ex2(x0), p1 = ex2(x1);
+                    const unsigned long long x = fma2(two_words(r[ch][i], r[ch][i + 1]), f2, from2);
+                    float p0, p1;
+                    if (i % 8 == 2) floats_of(two_to2(x), p0, p1);             // two of eight
+                    else {
+                        floats_of(x, p0, p1);
+                        p0 = ex2(p0); p1 = ex2(p1);
+                    }
                     unsigned long long& sum = i & 2 ? sum1 : sum0;
                     sum = add2(sum, two_floats(p0, p1));
                     p[i / 2] = pack_fp16(p0, p1);
@@ -418,8 +443,10 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                 }
                 for (int j = 0; ok && j < tiles; ++j) {
                     const int vs = j % S::v_stages;
-                    bool keys = false;           // of the next tile have been waited for
+                    // (ahead of the probabilities, which come last)
+                    if (j + 1 < tiles && !(ok = wait(sh.k_full[(j + 1) & 1], (j + 1) / 2 & 1))) break;
                     if (!(ok = wait(sh.v_full[vs], j / S::v_stages & 1))) break;
+                    tc_fence_after();
                     for (int h = 0; h < 2; ++h) {
                         if (j < count[h]) {
                             for (int part = 0; part < 2 && ok; ++part) {
@@ -432,9 +459,6 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                         }
                         if (h == 1) signal(sh.v_empty[vs]);      // (ahead of the next scores)
                         if (j + 1 < count[h]) {
-                            if (!keys && !(ok = wait(sh.k_full[(j + 1) & 1], (j + 1) / 2 & 1))) break;
-                            keys = true;
-                            tc_fence_after();
                             scores(h, j + 1);
                         }
                     }
