@@ -73,6 +73,16 @@ def test_many_sequences(lib):  # noqa: F811
     check(c, 2, 64)
 
 
+def test_more_blocks_of_rows_than_warps_that_look_for_them(lib):  # noqa: F811
+    """As many sequences as a batch has, and 60000 rows of one, most of them before position 0."""
+    r = np.random.default_rng(4)
+    lengths = [int(x) for x in r.integers(0, 20, 1024)]
+    rows = [int(r.integers(0, n + 1)) for n in lengths]
+    lengths[900], rows[900] = 700, 60000
+    c = Case(lib, 34, lengths, rows, 128, 16, 16, BF16, fill=True)
+    check(c, 1, 64)
+
+
 @pytest.mark.parametrize("size,scale", [(1.0, -0.2), (1.0, 0.0), (30.0, 0.3), (1e-20, 1e18)])
 def test_scores_of_any_size(lib, size, scale):  # noqa: F811
     c = Case(lib, 22, [400, 90], [130, 60], 128, 32, 16, BF16, fill=True)
@@ -164,6 +174,18 @@ def test_bad_tokens_reach_only_rows_that_see_them(lib, what, whole):  # noqa: F8
     out = c.cache.attend_expanded(c.batch, q, *w, 0.1, 330)
     assert out[30:60].isnan().all()
     assert torch.equal(out[:30], good[:30]) and torch.equal(out[60], good[60])
+
+
+def test_a_bad_token_at_any_place_of_a_tile(lib):  # noqa: F811
+    """Token i of sequence i, whose rows all see the whole tile that it is in."""
+    c = Case(lib, 33, [200] * 33, [40] * 33, 128, 16, 16, BF16, fill=True)
+    w = matrices(c, 2, 64)
+    q = c.randn(c.n_rows, 2, 80)
+    good = c.cache.attend_expanded(c.batch, q, *w, 0.1, 200 * 33)
+    for i in range(32):
+        c.cache.pages[c.table[i, i // 16], i % 16] = float("nan")
+    out = c.cache.attend_expanded(c.batch, q, *w, 0.1, 200 * 33)
+    assert out[:32 * 40].isnan().all() and torch.equal(out[32 * 40:], good[32 * 40:])
 
 
 def test_pages_that_are_not_there(lib):  # noqa: F811
