@@ -63,9 +63,6 @@ struct LpShared {
     int quit;
 };
 
-// 16-byte chunk `ch` (eight elements) of a row of an operand tile: 128-byte rows of 64 elements, swizzled
-__device__ __forceinline__ uint32_t lp_chunk(int row, int ch) { return uint32_t((ch >> 3) * (kLpTile * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)); }
-
 // 2^x of two numbers below 2^7 by the pipes that ex2 leaves idle: 2^n (1 + f (c1 + f (c2 + f c3))), n the next integer, |f| <= 1/2, where the cubic of least
 // relative error that is 1 at 0 is off by 1.02e-4, less than half of fp16's rounding. Below -127 it is 0; NaN stays.
 __device__ __forceinline__ unsigned long long two_to2(unsigned long long x) {
@@ -151,7 +148,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
 
     if (warp < 8) {
         more_registers<kLpSoftmaxRegs>();
-        // ---- queries: a warp brings its 32 rows, a row at a time; then a lane has a row ----
+        // ---- queries: a warp brings its 32 rows ----
         const int half = warp >> 2, row_in = tid & 127, i_row = rb * kPfCols + tid;
         const int row = i_row < n && first + i_row >= 0 && first + i_row < b.n_rows ? first + i_row : -1;
         const int limit = i_row < n ? sees(i_row) : 0;
