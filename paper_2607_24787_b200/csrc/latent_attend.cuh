@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                                 const int col = 8 * i + c2 + e;
                                 float top = fmaxf(fmaxf(red[col], red[COLS + col]), fmaxf(red[2 * COLS + col], red[3 * COLS + col]));
                                 // (a query with an infinity may have no other scores than -infinity, as of tokens that it does not see: NaN)
-                                if (first && top == -INFINITY && t0 + (__ffs(~absent) - 1) * a.box < sh.limit[half][col]) l[i][e] = __int_as_float(0x7fffffff);
+                                const int there = __ffs(~absent & ((1 << kLaTile / a.box) - 1));       // its first copy that there is, 0: none
+                                if (first && top == -INFINITY && there > 0 && t0 + (there - 1) * a.box < sh.limit[half][col]) l[i][e] = __int_as_float(0x7fffffff);
                                 // (nothing seen: stays. Only the first tile's may be below zero)
                                 if (top == -INFINITY || (!first && top < 0.f)) top = 0.f;
                                 m[i][e] += top;
