@@ -593,8 +593,8 @@ int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, cons
 /* out (n_heads heads of latent_dim elements) = softmax(scale q . row) latent for each new row and each of its n_heads heads, q of latent_dim +
  * rope_dim elements, over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's statistics and all
  * sums are fp32; bf16 calls round a probability once, to bf16's 8 bits, fp32 calls keep 24 bits of queries and probabilities. A query with
- * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN (an infinity: in its own
- * elements at least) for the rows that see it, and changes no other. scale times log2(e) is finite; out may not overlap q. Results do not
+ * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN for the rows that see it, and
+ * changes no other; a score times log2(e) beyond fp32's range gives NaN too. scale times log2(e) is finite; out may not overlap q. Results do not
  * depend on the order in which CTAs run, and are the same bits for the same call. Any number of new rows is right; prompts in bf16 are
  * faster in the expanded form.
  * workspace: dev, 16-byte aligned, at least spm_latent_attend_workspace() bytes; what it held before does not matter, and calls that may run
@@ -613,8 +613,7 @@ typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
  * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. dtype: bf16 (fp32 rows have the absorbed form). Results are
  * rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two: a query's element keeps fewer bits below
  * 2^-23 of its head's largest, a key's below 2^-23 of the largest of its 32 tokens and head, a value below 2^-18 of its head's largest so far, a
- * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and
- * rows that are not finite holds, but that any element of a row that is not finite makes all elements of the result NaN.
+ * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and rows that are not finite holds.
  * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * (head_dim + 32) * 4 and a little more, but
  * not much over 512 MB where a head takes less); one for each of calls that may run at the same time. */
 int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,

@@ -370,11 +370,26 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                         for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
                     return top;
                 };
+                auto lowest = [&] {
+                    float low = INFINITY;
+#pragma unroll
+                    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) low = fminf(low, s[i][e]);
+                    return low;
+                };
                 // the sums of the tile before are done (and the item before's, at its end): P and O may be touched
                 auto sums_done = [&] { ok = ok && (j == 0 || wait(sh.empty[(st == 0 ? stages : st) - 1], st == 0 ? turn ^ 1 : turn)); };
-                if (vote(highest() > kLaSlack || first || masks || !ok)) {
+                if (vote(highest() > kLaSlack || lowest() == -INFINITY || first || masks || !ok)) {
                     if (vote(!ok)) { ok = false; break; }
                     sums_done();
+                    // A score of -infinity comes of an infinity in the query or the row, as one of +infinity does, which becomes NaN by itself. From
+                    // here on it is what masks put in place of a score
+#pragma unroll
+                    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (s[i][e] == -INFINITY) s[i][e] = __int_as_float(0x7fffffff);
                     if (masks) {
                         // a thread looks at half of a token's row. What no column may see becomes zeros, so that 0 * NaN does not come up, and so
                         // does a row that is not finite where some columns see it and some do not
@@ -431,9 +446,6 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             for (int e = 0; e < 2; ++e) {
                                 const int col = 8 * i + c2 + e;
                                 float top = fmaxf(fmaxf(red[col], red[COLS + col]), fmaxf(red[2 * COLS + col], red[3 * COLS + col]));
-                                // (a query with an infinity may have no other scores than -infinity, as of tokens that it does not see: NaN)
-                                const int there = __ffs(~absent & ((1 << kLaTile / a.box) - 1));       // its first copy that there is, 0: none
-                                if (first && top == -INFINITY && there > 0 && t0 + (there - 1) * a.box < sh.limit[half][col]) l[i][e] = __int_as_float(0x7fffffff);
                                 // (nothing seen: stays. Only the first tile's may be below zero)
                                 if (top == -INFINITY || (!first && top < 0.f)) top = 0.f;
                                 m[i][e] += top;
