@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         // ---- softmax: this thread's row is lane 32 (warp % 4) + lane of tensor memory ----
         const int own_tiles = half == 0 ? tiles0 : tiles1;
         const uint32_t lanes = uint32_t(warp & 3) << 21, s_at = t_s + half * 128 + lanes, o_at = t_o + half * HD + lanes;
-        const float f = fabsf(a.factor) / up;
+        const float f = fmaxf(fabsf(a.factor) / up, 0x1p-149f);                // (not zero: masked scores are -infinity)
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         const uint4* bits = reinterpret_cast<const uint4*>(a.there + at / 32);
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
         for (int j = 0; j < own_tiles && ok; ++j) {
             uint32_t there[4] = {bits_then.x, bits_then.y, bits_then.z, bits_then.w};
             const int power[4] = {powers_then.x, powers_then.y, powers_then.z, powers_then.w};
-            const float unit[4] = {two_to(units_then.x), two_to(units_then.y), two_to(units_then.z), two_to(units_then.w)};
+            float unit[4] = {two_to(units_then.x), two_to(units_then.y), two_to(units_then.z), two_to(units_then.w)};
             if (j + 1 < own_tiles) { bits_then = bits[j + 1]; powers_then = powers_of[j + 1]; units_then = units_of[j + 1]; }
             bool whole = (j + 1) * kLpTile <= limit && (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu;
             whole = __all_sync(0xffffffffu, whole);
@@ -268,11 +268,31 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
                     }
                 }
             }
-            const float base = m == -INFINITY ? 0.f : -m * f;
+            float base = m == -INFINITY ? 0.f : -m * f;
+            // Of large scores the rounding of this and of their own products is more than the range of fp16's exponents: rows that have such take the
+            // differences from the maximum first, in its unit (below 2^8 the rounding is 2^-16 at most)
+            const bool far = !(fabsf(base) < 256.f);
+            if (__any_sync(0xffffffffu, far)) {
+                const float from = far ? -m : 0.f;
+                const unsigned long long from2 = two_floats(from, from);
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) {
+                    const float by = far ? unit[ch] : 1.f;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float x0, x1;
+                        floats_of(fma2(two_words(r[ch][i], r[ch][i + 1]), two_floats(by, by), from2), x0, x1);
+                        r[ch][i] = __float_as_uint(x0);
+                        r[ch][i + 1] = __float_as_uint(x1);
+                    }
+                    if (far) unit[ch] = 1.f;
+                }
+                if (far) base = 0.f;
+            }
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) {
                 // (values 2^60 below the largest are as good as zero, and yet their tokens' probabilities count)
-                const float f_of = fmaxf(f * unit[ch], 0x1p-126f);             // (not zero: masked scores are -infinity)
+                const float f_of = fmaxf(f * unit[ch], 0x1p-149f);
                 const float shift = float(max(power[ch] - run, -60)), from = base + (kLpUp + shift);
                 const unsigned long long from2 = two_floats(from, from), f2 = two_floats(f_of, f_of);
                 unsigned long long sum0 = 0, sum1 = 0;

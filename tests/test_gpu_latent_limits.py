@@ -4,7 +4,8 @@ import pytest
 import torch
 
 from oracle import ref_latent as R
-from test_gpu_latent_cache import BF16, FP32, Case, attend_tolerance, check_attend, f64, lib  # noqa: F401 (lib is a fixture)
+from oracle.ref_cache import places
+from test_gpu_latent_cache import BF16, FP32, HALF, Case, attend_tolerance, check_attend, f64, lib  # noqa: F401 (lib is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +87,43 @@ def test_an_infinity_in_a_key_of_a_long_context(lib, token, dtype):  # noqa: F81
         c.cache.pages[c.table[0, token // 64], token % 64, 140] = what
         out = c.cache.attend(c.batch, q, 0.1)
         assert out[0].isnan().all() and torch.equal(out[1], good[1])
+
+
+# ---- scores of any size, expanded ----------------------------------------------
+# The best token's score is above every other one by at least the query's size times the scale, 2^18 and more: its probability is 1, all others
+# are 0, and the result is its value: a sum of 128 fp32 products (each addition off by 2^-23 at most), rounded to fp16 (2^-11; 2^-25 where the
+# largest value of its 32 tokens is 2^9 or more: 2^-34 of the largest) and to bf16, with a handful of fp32 roundings between.
+@pytest.mark.parametrize("power", [8, 13, 19, 24, 27, 28, 30, 33, 40, 55, 90])
+@pytest.mark.parametrize("lengths,rows,heads,head,rope,unit", [
+    ([600, 300], [300, 300], 3, 128, 64, 0), ([300, 1100], [130, 260], 2, 64, 16, 0), ([20, 40], [20, 1], 2, 64, 16, 0), ([700], [200], 2, 128, 16, -30),
+    ([700], [200], 2, 64, 32, 100),
+])
+def test_expanded_scores_of_any_size(lib, lengths, rows, heads, head, rope, unit, power):  # noqa: F811
+    c = Case(lib, 53, lengths, rows, 128, rope, 32, BF16, 1, fill=True)
+    g = torch.Generator().manual_seed(power)
+    tops = []
+    c.start[..., 128:] = c.start[..., 128:] * 0                    # (what is not a number behind a sequence's end stays)
+    for s, n in enumerate(lengths):                # eight tokens, each above the ones before it; others far below, some of them small by themselves
+        at = sorted([0] + (torch.randperm(n - 1, generator=g)[:7] + 1).tolist())
+        tops.append(at)
+        for t in range(n):
+            key = at.index(t) + 1.0 if t in at else -8.0 if t // 32 % 2 else -2.0 ** -10
+            c.start[c.table[s, t // 32], t % 32, 128] = key * 2.0 ** unit
+    c.cache.pages.copy_(c.start)
+    q = torch.zeros(c.n_rows, heads, head + rope, dtype=BF16)
+    q[..., head] = torch.ldexp(1 + torch.randint(0, 128, (c.n_rows, heads), generator=g) / 128, torch.tensor(power - unit)).to(BF16)
+    w_k = torch.zeros(heads, head, 128, dtype=BF16, device="cuda")
+    w_v = torch.randn(heads, head, 128, generator=g).mul(0.1).to(BF16)
+    values = [np.einsum("tc,hdc->thd", R.context(f64(c.start), c.table.numpy(), s, n)[0][:, :128], f64(w_v)) for s, n in enumerate(lengths)]
+    made = [np.einsum("tc,hdc->thd", np.abs(R.context(f64(c.start), c.table.numpy(), s, n)[0][:, :128]), np.abs(f64(w_v))) for s, n in enumerate(lengths)]
+    # (below 2^13 the others are not all zero: only that it is near)
+    others = {8: 2.0 ** -8, 13: 0.0}.get(power, 0.0)
+    for scale in (0.7, -0.3):
+        got = f64(c.cache.attend_expanded(c.batch, (q if scale > 0 else -q).cuda(), w_k, w_v.cuda(), scale, sum(lengths)))
+        for i, at in enumerate(places(lengths, c.row_start, c.n_rows)):
+            if at is None:
+                continue
+            best = max(t for t in tops[at[0]] if t <= at[1])
+            want, largest = values[at[0]][best], np.abs(values[at[0]]).max()
+            tol = (2.0 ** -11 + HALF[BF16] * (1 + 2.0 ** -8) + 16 * HALF[FP32]) * np.abs(want) + 128 * 2.0 ** -23 * made[at[0]][best] + (2.0 ** -34 + others) * largest
+            assert (np.abs(got[i] - want) <= tol).all(), (scale, i, at, best)
