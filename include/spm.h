@@ -614,6 +614,7 @@ typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
  * rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two: a query's element keeps fewer bits below
  * 2^-23 of its head's largest, a key's below 2^-23 of the largest of its 32 tokens and head, a value below 2^-18 of its head's largest so far, a
  * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and rows that are not finite holds.
+ * An element of a key of 2^109 or more counts as one that is not finite.
  * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * (head_dim + 32) * 4 and a little more, but
  * not much over 512 MB where a head takes less); one for each of calls that may run at the same time. */
 int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,

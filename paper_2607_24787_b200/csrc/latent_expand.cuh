@@ -11,8 +11,8 @@
 // of the result. A key's power is 1 where the largest of its 32 tokens is in fp16's range as it is, which it is but for odd models, and the part
 // that all heads share is there once; elsewhere each head has a copy of that too, times its own power of two.
 //
-// A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite gets NaN as its key's first
-// element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
+// A token that does not exist becomes zeros, and its bit in `there` too. A token whose keys are not finite, or have an element of 2^109 or more, gets
+// NaN as its key's first element and finite values: scores of rows that see it are NaN, and 0 * NaN does not come up for those that do not.
 #pragma once
 
 #include <cuda.h>
@@ -27,6 +27,8 @@
 namespace spm {
 
 constexpr int kLxLeast = -110;                   // E of values that are all zero, or nearly
+// Where keys end, as fp32 bits: 2^109. A score is less than 192 products of 2^10 by 2^10, times 2^E, E at most 108 - 9: 2^127, and so is a difference of two
+constexpr uint32_t kLxKeyEnd = (127 + 109) << 23;
 __device__ __forceinline__ uint32_t pack_fp16(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -260,23 +262,23 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
                         tmem_ld32(tmem + buf * N + which * HD + ch * 32 + lanes, *reinterpret_cast<uint32_t(*)[32]>(r + ch * 32));
                     tmem_wait_ld();
                 };
-                auto not_all_finite = [&] {
-                    unsigned long long zero = 0; // 0 times what is not finite is NaN
+                auto largest = [&] {             // as fp32 bits; what is not finite is above all else
+                    uint32_t v = 0;
 #pragma unroll
-                    for (int e = 0; e < HD; e += 2) zero = fma2(two_words(r[e], r[e + 1]), 0ull, zero);
-                    float z0, z1;
-                    floats_of(zero, z0, z1);
-                    return there && (z0 != z0 || z1 != z1);
+                    for (int e = 0; e < HD; ++e) v = max(v, r[e] & 0x7fffffffu);
+                    return there ? v : 0u;
                 };
                 take(part);
-                bool odd = not_all_finite() || (there && part == 0 && rope_top >= 0x7f800000u);
+                uint32_t top = part == 0 ? max(rope_top, largest()) : largest();
+                const bool odd = top >= (part == 0 ? kLxKeyEnd : 0x7f800000u);
                 if (part == 1 && __any_sync(0xffffffffu, odd)) {             // values: is it the token, or the matrix?
                     take(0);
-                    const bool token = not_all_finite() || (there && rope_top >= 0x7f800000u);
+                    const bool token = max(rope_top, largest()) >= kLxKeyEnd;
                     take(1);
                     if (token)
 #pragma unroll
                         for (int e = 0; e < HD; ++e) r[e] = not_finite(r[e]) ? 0u : r[e];
+                    top = largest();
                 }
                 tc_fence_before();
                 mbar_arrive(smem_u32(&sh.d_empty[buf]));
@@ -284,9 +286,6 @@ __global__ void __launch_bounds__(kLxThreads, 1) latent_expand_kernel(const Late
 #pragma unroll
                     for (int e = 0; e < HD; ++e) r[e] = 0u;
                 // the largest of a warp's tokens is brought to [2^9, 2^10); of keys if it is below 2^-4 or not below 2^15
-                uint32_t top = part == 0 ? rope_top : 0;
-#pragma unroll
-                for (int e = 0; e < HD; ++e) top = max(top, r[e] & 0x7fffffffu);
                 top = __reduce_max_sync(0xffffffffu, part == 0 && odd ? 0u : top);
                 const int power = part == 0 && (top == 0 || (top >= 0x3d800000u && top < 0x47000000u)) ? 0 : top == 0 ? kLxLeast : max(kLxLeast, min(int(top >> 23) - 127 - 9, 118));
                 const float by = __int_as_float((127 - power) << 23);

@@ -127,3 +127,22 @@ def test_expanded_scores_of_any_size(lib, lengths, rows, heads, head, rope, unit
             want, largest = values[at[0]][best], np.abs(values[at[0]]).max()
             tol = (2.0 ** -11 + HALF[BF16] * (1 + 2.0 ** -8) + 16 * HALF[FP32]) * np.abs(want) + 128 * 2.0 ** -23 * made[at[0]][best] + (2.0 ** -34 + others) * largest
             assert (np.abs(got[i] - want) <= tol).all(), (scale, i, at, best)
+
+
+@pytest.mark.parametrize("part", ["key", "made"])
+@pytest.mark.parametrize("power,finite", [(100, True), (113, False), (120, False)])
+def test_expanded_keys_too_large_for_a_call(lib, part, power, finite):  # noqa: F811
+    """An element of a key of 2^109 and more counts as one that is not finite: NaN for the rows that see it, and for no other."""
+    c = Case(lib, 54, [200, 130], [60, 1], 128, 32, 16, BF16, fill=True)
+    q = c.randn(c.n_rows, 2, 96).mul(2.0 ** -20)
+    w = torch.randn(2, 128, 128, generator=c.g).mul(0.1).to(BF16).cuda()
+    w_k, w_v = w[:, :64], w[:, 64:]
+    w_v[..., 5], w_k[..., 5] = 0, 1
+    good = c.cache.attend_expanded(c.batch, q, w_k, w_v, 2.0 ** -90, 330)
+    c.cache.pages[c.table[0, 170 // 16], 170 % 16, 128 + 7 if part == "key" else 5] = 2.0 ** power
+    out = c.cache.attend_expanded(c.batch, q, w_k, w_v, 2.0 ** -90, 330)
+    assert torch.equal(out[:30], good[:30]) and torch.equal(out[60], good[60])
+    if finite:                                                     # scores are all but zero
+        assert (out[30:60] - good[30:60]).abs().max() <= 2.0 ** -5 * good.abs().max()
+    else:
+        assert out[30:60].isnan().all()
