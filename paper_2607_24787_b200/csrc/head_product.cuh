@@ -7,7 +7,9 @@
 // thread c's i-th of a step.
 //
 // Rows in fp32 are three bf16 parts, cut off and not rounded (their sum is the number, 24 bits, and none overflows), so that products are
-// exact and sums fp32.
+// exact and sums fp32. mma.sync cuts sums off where it does not round them, some 2^-23 of a sum a product, which adds up where terms are of one sign (8192
+// elements in one sum: 343 * 2^-24 too small). So fp32 calls' sums leave the products every few elements and are added up outside: here a step's, the
+// lower parts first, so that the first parts' bits are all there and only the lower ones' last are cut off.
 #pragma once
 
 #include "latent_cache.cuh"
@@ -115,15 +117,29 @@ __global__ void __launch_bounds__(WARPS * 32) head_product_kernel(const HeadProd
             for (int i = 0; i < 2; ++i) x_raw[t][i].parts(rows[t][i]);
         load(s + 1);
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int t = 0; t < MT; ++t) {
+            auto product = [&](float (&d)[4], int j, int k, int p) {
+                const uint32_t frag[4] = {rows[t][0][k][p], rows[t][1][k][p], rows[t][0][k + 1][p], rows[t][1][k + 1][p]};
+                hp_mma(d, frag, b[j][k], b[j][k + 1]);
+            };
+            if constexpr (PARTS == 3) {
+                float step[8][4] = {};
 #pragma unroll
-            for (int k = 0; k < PAIRS; k += 2)
+                for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    const uint32_t frag[4] = {rows[t][0][k][p], rows[t][1][k][p], rows[t][0][k + 1][p], rows[t][1][k + 1][p]};
+                    for (int k = 0; k < PAIRS; k += 2)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) hp_mma(acc[t][j], frag, b[j][k], b[j][k + 1]);
-                }
+                        for (int j = 0; j < 8; ++j) product(step[j], j, k, p);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][j][e] += step[j][e];
+            } else
+#pragma unroll
+                for (int k = 0; k < PAIRS; k += 2)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) product(acc[t][j], j, k, 0);
+        }
     }
     // ---- the warps' sums: the upper half hands over, the lower half adds, twice in turn; always in the same order ----
 #pragma unroll
@@ -216,7 +232,7 @@ __global__ void __launch_bounds__(kHtThreads) head_product_tile_kernel(const Hea
     };
 #pragma unroll
     for (int k = 0; k < kHtStages - 1; ++k) copy(k);
-    float acc[8][4] = {};
+    float acc[8][4] = {}, low[8][4] = {};
     const bool idle = o0 + wn * 64 >= out;       // (the last 64 of an odd number of them)
     for (int k = 0; k < chunks; ++k) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kHtStages - 2) : "memory");
@@ -224,7 +240,7 @@ __global__ void __launch_bounds__(kHtThreads) head_product_tile_kernel(const Hea
         copy(k + kHtStages - 1);
         if (idle) continue;
         const uint32_t w_at = base + k % kHtStages * S::stage, x_at = w_at + S::w_bytes;
-        float part[8][4] = {};                   // fp32: a chunk's sums, added up outside of the products, which cut sums off where they do not round them
+        float part[8][4] = {};                   // fp32: the first parts' sums of a chunk; the others' are 2^-7 of them at most and stay in the products
         float (&sum)[8][4] = sizeof(T) == 4 ? part : acc;
 #pragma unroll
         for (int s = 0; s < kHtChunk / STEP; ++s) {
@@ -272,7 +288,7 @@ __global__ void __launch_bounds__(kHtThreads) head_product_tile_kernel(const Hea
                 for (int p = 0; p < PARTS; ++p) {
                     const uint32_t frag[4] = {rows[0][e][p], rows[1][e][p], rows[0][e + 1][p], rows[1][e + 1][p]};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) hp_mma(sum[j], frag, b[j][e], b[j][e + 1]);
+                    for (int j = 0; j < 8; ++j) hp_mma(p == 0 ? sum[j] : low[j], frag, b[j][e], b[j][e + 1]);
                 }
         }
         if constexpr (sizeof(T) == 4)
@@ -282,6 +298,11 @@ __global__ void __launch_bounds__(kHtThreads) head_product_tile_kernel(const Hea
                 for (int e = 0; e < 4; ++e) acc[j][e] += part[j][e];
     }
     if (idle) return;
+    if constexpr (sizeof(T) == 4)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] += low[j][e];
     T* y = static_cast<T*>(a.y.p) + head * a.y.head + o0 + wn * 64 + 16 * c;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

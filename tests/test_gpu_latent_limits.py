@@ -146,3 +146,25 @@ def test_expanded_keys_too_large_for_a_call(lib, part, power, finite):  # noqa: 
         assert (out[30:60] - good[30:60]).abs().max() <= 2.0 ** -5 * good.abs().max()
     else:
         assert out[30:60].isnan().all()
+
+
+# ---- products of heads ---------------------------------------------------------
+# Terms of one sign, 1/4 to 9/4 each, so that what is cut off a sum adds up. Of the first parts a product has its last bit at 2^-16 and 64 of them are below
+# 2^8: exact in 24 bits. The other parts are 2^-7 of the result at most; a product of 16 elements is off by 17 steps of 2^-23 at most of what
+# is there (16 terms and the sum, cut off at one place). In units of 2^-24 of the result:
+# few rows: sums of 16 elements (transposed 32) begin with the other parts (two to four products, half a unit), which the first parts cut off at most twice (four units),
+# and are added up in fp32, half a step each of what is there so far; the warps' sums by three additions more. `warps`: a CTA's, which share them out;
+# 64 rows (warps 1): first parts' sums of 64 elements are added up in fp32; the other parts' products stay in one sum, two for each 16 elements.
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("n,heads,size,to,warps", [(3, 2, 8192, 128, 8), (3, 150, 8192, 128, 4), (40, 3, 8192, 64, 8), (17, 2, 4096, 192, 8), (1, 5, 576, 64, 8),
+                                                   (64, 100, 2048, 128, 1)])
+def test_fp32_products_of_one_sign(lib, n, heads, size, to, warps, transposed):  # noqa: F811
+    g = torch.Generator().manual_seed(57)
+    x = torch.rand(n, heads, size, generator=g).add(0.5).cuda()
+    w = torch.rand(heads, to, size, generator=g).add(0.5).to(BF16).cuda()
+    y = lib.head_product(x, w if transposed else w.transpose(1, 2).contiguous(), transposed=transposed)
+    want = torch.stack([x[:, h].double() @ w[h].double().T for h in range(heads)], 1)
+    added = size // 64 if warps == 1 else -(-size // (32 if transposed else 16) // warps)
+    other = 17 * 2 * 2.0 ** -7 * (2 * size // 16 + 1) / 2 if warps == 1 else 4.5
+    bound = (added + 1) / 2 + other + 3
+    assert ((y.double() - want).abs() <= bound * 2.0 ** -24 * want).all()
