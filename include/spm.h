@@ -610,7 +610,7 @@ typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
  * heads, over the tokens up to the row's own position, with key = [W_k latent | key of the row] and value = W_v latent made from the cache for
  * all tokens of the batch's sequences, a round of heads at a time. q: heads of head_dim + rope_dim elements. head_dim: 64 or 128.
  * n_tokens: at least the tokens of all sequences that have rows in this batch (the sum of their lengths), which is what the workspace has
- * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. dtype: bf16 (fp32 rows have the absorbed form). Results are
+ * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. n_tokens + 127 n_seq is below 2^30. dtype: bf16 (fp32 rows have the absorbed form). Results are
  * rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two: a query's element keeps fewer bits below
  * 2^-23 of its head's largest, a key's below 2^-23 of the largest of its 32 tokens and head, a value below 2^-18 of its head's largest so far, a
  * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and rows that are not finite holds.

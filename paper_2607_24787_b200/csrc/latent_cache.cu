@@ -102,7 +102,8 @@ int check_expanded(const char* call, const spm_kv_batch* b, int n_heads, int hea
     if (dtype != SPM_DTYPE_BF16) return fail(call, SPM_ERR_CONFIG, "the expanded form is for bf16 rows; fp32 rows have the absorbed form");
     if (int rc = check_heads(call, n_heads)) return rc;
     if (head_dim != 64 && head_dim != 128) return fail(call, SPM_ERR_CONFIG, "head_dim " + std::to_string(head_dim) + " not supported: 64 or 128");
-    if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(call, SPM_ERR_INVALID_ARG, "n_tokens outside 0..2^30");
+    // (rows of the workspace are counted in 32 bits, the shared parts of keys behind one head's; more heads a round are 512 MB at most)
+    if (n_tokens < 0 || n_tokens + 127ll * b->n_seq >= 1ll << 30) return fail(call, SPM_ERR_INVALID_ARG, "n_tokens outside 0..2^30 - 127 n_seq - 1");
     if (static_cast<long long>(b->n_rows) * n_heads > INT32_MAX - 64) return fail(call, SPM_ERR_INVALID_ARG, "n_rows * n_heads is over 2^31 - 65");
     return SPM_OK;
 }
@@ -281,7 +282,6 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
     const Expanded e = expanded_of(batch, n_heads, head_dim, n_tokens);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < e.bytes)
         return fail(call, SPM_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold " + std::to_string(e.bytes) + " bytes");
-    if (static_cast<long long>(e.tokens) * (e.heads + 1) > INT32_MAX) return fail(call, SPM_ERR_CONFIG, "n_tokens times heads is over 2^31 - 1");
     int dev = 0, sms = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
