@@ -543,14 +543,21 @@ def spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, works
     _check(load().spm_latent_attend(kv, batch, q, n_heads, out, scale, dtype, workspace, workspace_bytes, stream))
 
 
+def _int32(n):
+    """n, which a c_int argument would cut to its low 32 bits."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{n} is not a number of 32 bits")
+    return n
+
+
 def spm_latent_attend_expanded_workspace(kv, batch, n_heads, head_dim, n_tokens, dtype) -> int:
     out = C.c_size_t()
-    _check(load().spm_latent_attend_expanded_workspace(kv, batch, n_heads, head_dim, n_tokens, dtype, C.byref(out)))
+    _check(load().spm_latent_attend_expanded_workspace(kv, batch, n_heads, head_dim, _int32(n_tokens), dtype, C.byref(out)))
     return out.value
 
 
 def spm_latent_attend_expanded(kv, batch, q, w_k, w_v, n_heads, head_dim, out, scale, n_tokens, dtype, workspace, workspace_bytes, stream=None):
-    _check(load().spm_latent_attend_expanded(kv, batch, q, w_k, w_v, n_heads, head_dim, out, scale, n_tokens, dtype, workspace, workspace_bytes, stream))
+    _check(load().spm_latent_attend_expanded(kv, batch, q, w_k, w_v, n_heads, head_dim, out, scale, _int32(n_tokens), dtype, workspace, workspace_bytes, stream))
 
 
 def spm_head_product(x, w, w_head_stride, w_row_stride, transposed, y, n_rows, n_heads, in_dim, out_dim, dtype, stream=None):

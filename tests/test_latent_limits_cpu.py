@@ -18,3 +18,10 @@ def test_the_workspace_query_and_the_call_take_the_same_sizes(B, heads, head, n_
         else:
             refused(B, query, -1, "n_tokens")
             refused(B, expanded(B, b=b, heads=heads, head=head, n_tokens=n), -1, "n_tokens")
+
+
+@pytest.mark.parametrize("n_tokens", [2 ** 31, 2 ** 32 + 100, -2 ** 31 - 1])
+def test_a_number_of_tokens_is_not_cut_to_32_bits(B, n_tokens):  # noqa: F811
+    for call in (lambda: B.spm_latent_attend_expanded_workspace(cache(B), batch(B), 16, 128, n_tokens, 1), expanded(B, n_tokens=n_tokens)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
