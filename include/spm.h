@@ -585,7 +585,7 @@ typedef struct {
 /* The batch's new rows go into the cache: latent (rows of latent_dim elements; head strides are not read) normed with rope's k_gamma
  * [latent_dim] (NULL: no norm) and key (rows of rope_dim elements) turned, both rounded to bf16; and q_out = the last rope_dim elements of
  * n_q_heads query heads, q, turned (q NULL: none; q_out may be q itself, with the same strides). rope's rot_dim is at most rope_dim, its
- * q_gamma NULL. rope NULL: neither norm nor rotation, and q must be NULL. An element that is not finite in bf16 is written as it is, and
+ * q_gamma NULL; the norm's sum is fp32 here. rope NULL: neither norm nor rotation, and q must be NULL. An element that is not finite in bf16 is written as it is, and
  * SPM_KV_NONFINITE recorded. */
 int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
                      const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* latent, const spm_rows* key, int dtype, void* stream);

@@ -20,7 +20,7 @@ struct LatentWriteArgs {
 
 // A warp takes a row, or one of gridDim.y parts of its query heads (the first part the cache's row too). A lane holds eight elements of a head,
 // rope / 8 lanes a head, so a warp takes several heads at once. A row's angles, taken in 64 bits (far positions), are one a lane (at most 64
-// elements turn) and pass through shared memory to the lanes that need them. The norm's sum is fp32: what it scales is rounded to bf16's 8 bits.
+// elements turn) and pass through shared memory to the lanes that need them. The norm's sum is fp32, what it scales being rounded to bf16's 8 bits.
 // With a head at a time, an element pair a lane, 18124 prompt rows of 16 heads took 76 us, 33 now (135 MB); what bounds it is issue, two thirds of the slots.
 template <typename T>
 __global__ void __launch_bounds__(kKvWarps * 32, 4) latent_write_kernel(const LatentWriteArgs a) {
@@ -89,14 +89,27 @@ __global__ void __launch_bounds__(kKvWarps * 32, 4) latent_write_kernel(const La
         const long long at = latent_row_at(a.kv, a.batch, r.seq, r.pos, lane == 0);
         __nv_bfloat16* to = a.kv.rows + (at >= 0 ? at : 0) * (a.kv.latent + a.kv.rope);
         bool odd = false;
-        float x[2][8], sum = 0.f;
+        float x[2][8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            unpack8<T>(latent[i], x[i]);
+        for (int i = 0; i < 2; ++i) unpack8<T>(latent[i], x[i]);
+        auto mean_of_squares = [&] {
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
+            return warp_sum(sum) / float(a.kv.latent);
+        };
+        float mean = mean_of_squares() + a.rope.eps;
+        if (a.rope.k_gamma && !(mean > 0x1p-80f && mean < 0x1p110f)) {         // squares that fp32 does not hold, or not all of: of the row times a power of two
+            const float by = mean < 1.f ? 0x1p100f : 0x1p-70f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] *= by;
+            mean = mean_of_squares() + a.rope.eps * by * by;
         }
-        const float inv = rsqrtf(warp_sum(sum) / float(a.kv.latent) + a.rope.eps);
+        const float inv = rsqrtf(mean);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = i * 256 + lane * 8;

@@ -168,3 +168,20 @@ def test_fp32_products_of_one_sign(lib, n, heads, size, to, warps, transposed): 
     other = 17 * 2 * 2.0 ** -7 * (2 * size // 16 + 1) / 2 if warps == 1 else 4.5
     bound = (added + 1) / 2 + other + 3
     assert ((y.double() - want).abs() <= bound * 2.0 ** -24 * want).all()
+
+
+# ---- rows on their way into the cache --------------------------------------------
+# fp32 roundings of a sum of 256 squares, a root and two products, then the one to bf16 (of the smallest numbers: half a step of 2^-133)
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("size,eps", [(1.0, 1e-6), (1e17, 1e-6), (1e19, 1e-6), (1e30, 0.0), (1e38, 1e-6), (1e-18, 0.0), (1e-25, 0.0), (1e-37, 0.0), (1e-25, 1e-6), (0.0, 1e-6)])
+def test_norms_of_rows_of_any_size(lib, size, eps, dtype):  # noqa: F811
+    c = Case(lib, 58, [40, 9], [11, 3], 256, 32, 16, dtype)
+    x, key = torch.randn(c.n_rows, 256, generator=c.g).clamp(-3, 3).mul(size).to(dtype).cuda(), c.randn(c.n_rows, 32)
+    x[3] = c.randn(256)                                            # one row is an ordinary one
+    gamma = 1 + 0.2 * torch.randn(256, generator=c.g)
+    rope = lib.kv.Rope(torch.ones(16).cuda(), k_gamma=gamma.cuda(), eps=eps)
+    c.cache.write(c.batch, x, key, positions=torch.zeros(c.n_rows, dtype=torch.int32, device="cuda"), rope=rope)
+    want = R.norm(f64(x), gamma.numpy(), float(np.float32(eps))) if size else np.where(np.arange(c.n_rows)[:, None] == 3, R.norm(f64(x), gamma.numpy(), eps), 0)
+    got = np.stack([f64(c.cache.pages[int(c.table[s, p // 16]), p % 16, :256]) for s, p in places(c.lengths, c.row_start, c.n_rows)])
+    assert (np.abs(got - want) <= (256 + 8) * HALF[FP32] * np.abs(want) + HALF[BF16] * np.abs(want) + 2.0 ** -134).all()
+    assert c.status.item() == 0
