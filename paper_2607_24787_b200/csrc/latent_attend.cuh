@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     const uint32_t stage_bytes = chunks * kLaChunkBytes, q_at = base + stages * stage_bytes, p_at = q_at + S::q_bytes(chunks);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-    if (tid == 128) asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
+    if (tid == 128 && a.kv.n_pages > 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
     grid_dep_wait();
     grid_dep_launch();
     if (tid == 0) {

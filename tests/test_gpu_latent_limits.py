@@ -185,3 +185,31 @@ def test_norms_of_rows_of_any_size(lib, size, eps, dtype):  # noqa: F811
     got = np.stack([f64(c.cache.pages[int(c.table[s, p // 16]), p % 16, :256]) for s, p in places(c.lengths, c.row_start, c.n_rows)])
     assert (np.abs(got - want) <= (256 + 8) * HALF[FP32] * np.abs(want) + HALF[BF16] * np.abs(want) + 2.0 ** -134).all()
     assert c.status.item() == 0
+
+
+# ---- pools without pages ---------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_a_pool_without_pages(lib, dtype):  # noqa: F811
+    """No token exists: nothing is written, rows that see only such tokens give zeros, and the status says why."""
+    from paper_2607_24787_b200 import binding as B
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cache = lib.LatentCache(torch.zeros(0, 32, 144, dtype=BF16, device="cuda"), 128, status)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = lib.kv.KVBatch(torch.zeros(2, 9, dtype=torch.int32, device="cuda"), ints(200, 30), ints(0, 5, 6), n_rows=7, max_rows=5)
+    g = torch.Generator().manual_seed(59)
+    rows = torch.randn(7, 144, generator=g).to(dtype).cuda()
+    cache.write(batch, rows[:, :128], rows[:, 128:])
+    assert status.item() == B.KV_BAD_PAGE
+    out = cache.attend(batch, torch.randn(7, 5, 144, generator=g).to(dtype).cuda(), 0.1, out=torch.full((7, 5, 128), 9.0, dtype=dtype, device="cuda"))
+    assert (out[:6] == 0).all() and (out[6] == 9).all()
+    if dtype is BF16:
+        w = torch.randn(5, 128, 128, generator=g).to(BF16).cuda()
+        out = cache.attend_expanded(batch, torch.randn(7, 5, 80, generator=g).to(BF16).cuda(), w[:, :64], w[:, 64:], 0.1, 230,
+                                    out=torch.full((7, 5, 64), 9.0, dtype=BF16, device="cuda"))
+        assert (out[:6] == 0).all() and (out[6] == 9).all()
+    # and a table without pages
+    status.zero_()
+    batch = lib.kv.KVBatch(torch.zeros(2, 0, dtype=torch.int32, device="cuda"), ints(200, 30), ints(0, 5, 6), n_rows=7, max_rows=5)
+    cache.write(batch, rows[:, :128], rows[:, 128:])
+    out = cache.attend(batch, torch.randn(7, 5, 144, generator=g).to(dtype).cuda(), 0.1)
+    assert (out[:6] == 0).all() and status.item() == B.KV_TOO_LONG
