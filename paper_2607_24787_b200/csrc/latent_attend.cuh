@@ -12,7 +12,8 @@
 // 2^(64 + 31)). So a tile needs no maximum over its tokens, only a vote that none is that far above.
 //
 // fp32 queries and probabilities are three bf16 parts each, cut off and not rounded: three columns side by side in one product, added up
-// as scores and results are read. bf16 calls round a probability to bf16's 8 bits once.
+// as scores and results are read. Their sums leave the products every kLaAside tiles, which cut sums off where they do not round them: with 63 tiles of
+// one sign in them results were 1.1e-5 too small, now they are as near as plain fp32 ones. bf16 calls round a probability to bf16's 8 bits once.
 //
 // All (sequence, columns) items together are a line of tiles that is cut evenly between CTAs, whatever the lengths are. An item's parts
 // in several CTAs go to the workspace and latent_join_kernel adds them in order. (Items count with all of a sequence's tokens; columns that
@@ -57,12 +58,13 @@ __device__ __forceinline__ int la_row(const LatentAttendArgs& a, int x) { return
 constexpr int kLaTile = 64, kLaMaxCtas = 148, kLaMaxStages = 8, kLaThreads = 192;
 constexpr int kLaChunkBytes = kLaTile * 128;
 constexpr float kLaSlack = 64.f;
+constexpr int kLaAside = 4;                      // tiles whose sums an fp32 call's products hold, the others' stand behind O
 
 template <typename T, int COLS>
 struct LaShape {
     static constexpr int parts = sizeof(T) == 4 ? 3 : 1;     // of a number
     static constexpr int n = COLS * parts;                   // N of the products
-    static_assert(n <= 64 && n % 16 == 0, "O^T of 512 elements, and two buffers of S^T, fit tensor memory");
+    static_assert((2 + 4) * n + (parts == 3 ? 4 * COLS : 0) <= 512 && n % 16 == 0, "O^T of 512 elements, two buffers of S^T, and sums aside fit tensor memory");
     static constexpr int q_bytes(int chunks) { return chunks * n * 128; }
     static constexpr int p_bytes = n * 128;
     static constexpr int fixed(int chunks) { return 1024 + q_bytes(chunks) + p_bytes; }
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t t_s = sh.tmem, t_o = t_s + 2 * N;
+    const uint32_t t_s = sh.tmem, t_o = t_s + 2 * N, aside_at = t_o + latent / 128 * N;
 
     // a warp goes on, or gives up, as one
     auto wait = [&](const unsigned long long& bar, int parity) {
@@ -338,6 +340,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
             }
             bool first = true;                   // no token so far
             float m[BLOCKS][2], l[BLOCKS][2] = {};
+            bool aside = false;                  // fp32 calls: there are sums of tiles before, behind O
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) m[i][0] = m[i][1] = 0.f;
             // tokens that all columns see: behind them are masks to look at
@@ -463,9 +466,9 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
 #pragma unroll 1
                             for (int mt = 0; mt < latent / 128; ++mt)
 #pragma unroll 1
-                                for (int ch = 0; ch < N / 16; ++ch) {
+                                for (int ch = 0; ch < N / 16 + aside; ++ch) {
                                     uint32_t o[16];
-                                    const uint32_t at = t_o + mt * N + ch * 16 + (uint32_t(warp) << 21);
+                                    const uint32_t at = (ch < N / 16 ? t_o + mt * N + ch * 16 : aside_at + mt * 16) + (uint32_t(warp) << 21);
                                     tmem_ld16_raw(at, o);
                                     tmem_wait_ld();
 #pragma unroll
@@ -478,6 +481,25 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                         first &= absent == (1 << kLaTile / a.box) - 1;
                     }
                 } else sums_done();
+                if constexpr (PARTS == 3)
+                    if (j > 0 && j % kLaAside == 0) {        // the products begin anew
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int mt = 0; mt < latent / 128; ++mt) {
+                            const uint32_t to = aside_at + mt * 16 + (uint32_t(warp) << 21);
+                            uint32_t o[PARTS][16], v[16] = {};
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + (uint32_t(warp) << 21), o[u]);
+                            if (aside) tmem_ld16_raw(to, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                v[i] = __float_as_uint(__uint_as_float(o[2][i]) + __uint_as_float(o[1][i]) + __uint_as_float(o[0][i]) + __uint_as_float(v[i]));
+                            tmem_st16(to, v);
+                        }
+                        tmem_wait_st();
+                        aside = true;
+                    }
 #pragma unroll
                 for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
@@ -557,8 +579,9 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
 #pragma unroll 1
                     for (int mt = 0; mt < latent / 128; ++mt) {
                         const int d = mt * 128 + tid;
-                        uint32_t o[PARTS][16] = {};
+                        uint32_t o[PARTS][16] = {}, before[16] = {};
                         if (w.tiles > 0) {
+                            if (PARTS == 3 && aside) tmem_ld16_raw(aside_at + mt * 16 + (uint32_t(warp) << 21), before);
 #pragma unroll
                             for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + ch * 16 + (uint32_t(warp) << 21), o[u]);
                             tmem_wait_ld();
@@ -567,7 +590,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             v[i] = __uint_as_float(o[0][i]);
-                            if constexpr (PARTS == 3) v[i] = v[i] + __uint_as_float(o[1][i]) + __uint_as_float(o[2][i]);
+                            if constexpr (PARTS == 3) v[i] = __uint_as_float(o[2][i]) + __uint_as_float(o[1][i]) + v[i] + __uint_as_float(before[i]);
                         }
                         if (!whole) {
 #pragma unroll
@@ -716,7 +739,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     }
                     if (!ok) break;
                     tc_fence_after();
-                    sums(st, j > 0);
+                    sums(st, PARTS == 3 ? j % kLaAside != 0 : j > 0);
                     if (more) {
                         if (!(ok = wait(sh.full[next], next_turn))) break;
                         scores(it + 1, next);

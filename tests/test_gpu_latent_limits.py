@@ -213,3 +213,19 @@ def test_a_pool_without_pages(lib, dtype):  # noqa: F811
     cache.write(batch, rows[:, :128], rows[:, 128:])
     out = cache.attend(batch, torch.randn(7, 5, 144, generator=g).to(dtype).cuda(), 0.1)
     assert (out[:6] == 0).all() and status.item() == B.KV_TOO_LONG
+
+
+# ---- long sums of fp32 calls -------------------------------------------------------
+def test_long_sums_of_one_sign(lib):  # noqa: F811
+    """8000 tokens in one CTA, all of the same probability, 1: results are means. Values of 8 bits from 2^-8 to 1 end at 2^-15, and 256 of them are below 2^8: exact
+    in 24 bits. Up to 32 such sums are added up in fp32, half a step of 2^-24 each of what is there so far (half as many, and a half), then up to two parts
+    joined, divided by their sum: six roundings more."""
+    n, heads, latent, rope, page = 8000, 1024, 128, 16, 64
+    g = torch.Generator(device="cuda").manual_seed(60)
+    pages = torch.rand(3 * n // page, page, latent + rope, device="cuda", generator=g).mul(-8).exp2().to(BF16)
+    cache = lib.LatentCache(pages, latent)
+    table = torch.randperm(3 * n // page, device="cuda", generator=g).to(torch.int32).view(3, -1)
+    batch = lib.kv.KVBatch(table, torch.full((3,), n, dtype=torch.int32, device="cuda"))
+    out = cache.attend(batch, torch.zeros(3, heads, latent + rope, device="cuda"), 0.1).double()
+    want = pages[table.long()].flatten(1, 2)[..., :latent].double().mean(1)[:, None]
+    assert ((out - want).abs() <= ((32 + 1) / 2 + 6) * 2.0 ** -24 * want).all()
