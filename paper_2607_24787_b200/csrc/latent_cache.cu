@@ -137,20 +137,27 @@ cudaError_t launch_expanded(LatentExpandArgs x, LatentPromptArgs a, const Expand
 
 template <typename T, bool TRANSPOSED>
 cudaError_t launch_product(HeadProductArgs a, int n_heads, int out, int dev, cudaStream_t st) {
-    // Enough work for CTAs of 64 rows and 128 outputs on most SMs, and rows that fill them: these read everything once. 64 rows, 128 heads, 512 to 128
-    // (us, of it 8 of a call, these / the others): bf16 14.4 / 18.5, fp32 23.5 / 25.5; 32 rows: bf16 14.4 / 16.5, fp32 22.5 / 18.5.
+    // CTAs of 64 rows and 128 outputs read everything once, and pay where there are rows that fill them and enough of them for most SMs. Kernel times in us,
+    // these / the others, heads x in to out, transposed (T) or not:
+    //   bf16  128 x 512 to 128 T: 32 rows 10.1 / 9.3, 48 10.6 / 13.3, 64 10.6 / 13.8, 128 18.4 / 22.5;  128 x 128 to 512: 32 rows 13.9 / 10.9, 48 14.3 / 17.5, 128 24.9 / 30.8
+    //   fp32  128 x 512 to 128 T: 32 rows 17.0 / 14.7, 48 17.7 / 17.1, 49 17.5 / 20.8, 64 18.1 / 21.4;  128 x 128 to 512: 32 rows 21.3 / 16.7, 48 22.6 / 22.9, 128 40.3 / 51.6
+    //   few tiles, bf16 / fp32  16 x 128 to 512, 64 rows, 64 tiles: 5.6 / 5.7, 7.3 / 6.3;  16 x 512 to 128 T, 400 rows, 112 tiles: 10.2 / 11.9, 17.4 / 16.9;
+    //   20 x 384 to 128 T, 400 rows, 140 tiles: 8.6 / 11.0, 14.2 / 17.6;  33 x 64 to 128, 128 rows, 66 tiles: 4.9 / 4.9, 6.2 / 5.5
     const long long tiles = (a.n_rows + kHtRows - 1ll) / kHtRows * ((out + kHtOut - 1) / kHtOut);
-    if (a.n_rows > (sizeof(T) == 4 ? 48 : 16) && tiles * n_heads >= 96) {
+    if (a.n_rows > (sizeof(T) == 4 ? 48 : 32) && tiles * n_heads >= 96) {
         const cudaError_t e = allow_smem<head_product_tile_kernel<T, TRANSPOSED>>(dev, HtShape<T>::smem);
         if (e != cudaSuccess) return e;
         a.out_tiles = (out + kHtOut - 1) / kHtOut;
         return launch_early(head_product_tile_kernel<T, TRANSPOSED>, dim3(unsigned(tiles), n_heads), kHtThreads, HtShape<T>::smem, st, a, out);
     }
-    // fp32 rows take registers threefold: 16 of them a CTA. Enough CTAs for several on an SM have four warps, fewer eight, which wait less long.
+    // fp32 rows take registers threefold: 16 of them a CTA. Eight warps wait less long for one another than four, but where these are more CTAs than the
+    // SMs hold of them (two of 16 bf16 rows, else one) four are better. Kernel times in us, four warps / eight: bf16 16 x 512 to 128 T, 16 rows, 32 CTAs 6.1 / 5.1;
+    // 128 x 512 to 128 T, 256 CTAs: 8 rows 7.9 / 7.5, 16 rows 7.9 / 8.1, 32 rows 9.3 / 11.9; 20 x 384 to 128 T, 128 rows, 160 CTAs 6.7 / 9.8;
+    // fp32 16 x 512 to 128 T: 64 rows, 128 CTAs 7.7 / 6.5, 128 rows, 256 CTAs 8.4 / 11.0; 128 x 512 to 128 T, 16 rows, 256 CTAs 9.9 / 12.2
     const bool one = a.n_rows <= 16 || sizeof(T) == 4;
     a.out_tiles = out / kHpOut;
     const dim3 grid(unsigned((a.n_rows + (one ? 15 : 31)) / (one ? 16 : 32)) * a.out_tiles, n_heads);
-    const bool many = static_cast<long long>(grid.x) * n_heads >= 2 * 148;
+    const bool many = static_cast<long long>(grid.x) * n_heads > (one && sizeof(T) == 2 ? 2 : 1) * 148;
     if constexpr (sizeof(T) == 2)
         if (!one) return many ? launch_early(head_product_kernel<T, TRANSPOSED, 2, 4>, grid, 128, 0, st, a) : launch_early(head_product_kernel<T, TRANSPOSED, 2, 8>, grid, 256, 0, st, a);
     return many ? launch_early(head_product_kernel<T, TRANSPOSED, 1, 4>, grid, 128, 0, st, a) : launch_early(head_product_kernel<T, TRANSPOSED, 1, 8>, grid, 256, 0, st, a);
