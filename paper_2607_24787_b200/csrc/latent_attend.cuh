@@ -8,8 +8,8 @@
 // A warp brings tiles by TMA (64 elements of a page's rows a copy, swizzled) into a ring of as many stages as there is room for; one issues
 // the products, of a tile's scores as soon as it has landed, of its sums as soon as its probabilities are there; four turn scores into
 // probabilities, 16 tokens each, and write results. A probability is 2^(s - m), m not the running maximum but one that was it: it is moved
-// only when a score is above it by more than 64, where it has lost nothing yet (P is bf16, which has fp32's range, and sums stay below
-// 2^(64 + 31)). So a tile needs no maximum over its tokens, only a vote that none is that far above.
+// only when a score is above it by more than 8, which it seldom is after a tile (P is bf16, which has fp32's range, and loses nothing above 1; sums of
+// values up to 2^100 stay in fp32's range over 2^18 tokens of a CTA). So a tile needs no maximum over its tokens, only a vote that none is that far above.
 //
 // fp32 queries and probabilities are three bf16 parts each, cut off and not rounded: three columns side by side in one product, added up
 // as scores and results are read. Their sums leave the products every kLaAside tiles, which cut sums off where they do not round them: with 63 tiles of
@@ -57,7 +57,7 @@ __device__ __forceinline__ int la_row(const LatentAttendArgs& a, int x) { return
 
 constexpr int kLaTile = 64, kLaMaxCtas = 148, kLaMaxStages = 8, kLaThreads = 192;
 constexpr int kLaChunkBytes = kLaTile * 128;
-constexpr float kLaSlack = 64.f;
+constexpr float kLaSlack = 8.f;
 constexpr int kLaAside = 4;                      // tiles whose sums an fp32 call's products hold, the others' stand behind O
 
 template <typename T, int COLS>

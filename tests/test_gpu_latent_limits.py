@@ -229,3 +229,21 @@ def test_long_sums_of_one_sign(lib):  # noqa: F811
     out = cache.attend(batch, torch.zeros(3, heads, latent + rope, device="cuda"), 0.1).double()
     want = pages[table.long()].flatten(1, 2)[..., :latent].double().mean(1)[:, None]
     assert ((out - want).abs() <= ((32 + 1) / 2 + 6) * 2.0 ** -24 * want).all()
+
+
+# ---- values of any size, absorbed --------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("size", [-100, 40, 70, 99])
+def test_latent_vectors_of_any_size(lib, size, dtype):  # noqa: F811
+    """As many sequences as CTAs. Scores come from the shared keys alone and go up by some 50 powers of two from tile to tile."""
+    lengths = [320] * 160
+    c = Case(lib, 61, lengths, [1] * 160, 128, 16, 64, dtype, fill=True)
+    ramp = torch.arange(320).div(64, rounding_mode="floor") * 12.0 * 0.693 + torch.arange(320) % 3
+    for s in range(160):
+        for p in range(5):
+            c.start[c.table[s, p], :, 128:] = ramp[64 * p:64 * p + 64, None].to(BF16)
+    c.start[..., :128] *= 2.0 ** size
+    c.cache.pages.copy_(c.start)
+    q = torch.zeros(c.n_rows, 6, 144, dtype=dtype)
+    q[..., 130] = torch.linspace(-1, 1, 6).to(dtype)
+    check_attend(c, 6, 1.0, q.cuda())
