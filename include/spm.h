@@ -585,14 +585,15 @@ typedef struct {
 /* The batch's new rows go into the cache: latent (rows of latent_dim elements; head strides are not read) normed with rope's k_gamma
  * [latent_dim] (NULL: no norm) and key (rows of rope_dim elements) turned, both rounded to bf16; and q_out = the last rope_dim elements of
  * n_q_heads query heads, q, turned (q NULL: none; q_out may be q itself, with the same strides). rope's rot_dim is at most rope_dim, its
- * q_gamma NULL; the norm's sum is fp32 here. rope NULL: neither norm nor rotation, and q must be NULL. An element that is not finite in bf16 is written as it is, and
- * SPM_KV_NONFINITE recorded. */
+ * q_gamma NULL; the norm's sum is fp32 here. rope NULL: neither norm nor rotation, and q must be NULL. An element that is not finite in
+ * bf16 is written as it is, and SPM_KV_NONFINITE recorded. */
 int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, const spm_rope* rope, const int32_t* positions, int64_t pos_stride,
                      const spm_rows* q, const spm_rows* q_out, int n_q_heads, const spm_rows* latent, const spm_rows* key, int dtype, void* stream);
 
 /* out (n_heads heads of latent_dim elements) = softmax(scale q . row) latent for each new row and each of its n_heads heads, q of latent_dim +
  * rope_dim elements, over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's statistics and all
- * sums are fp32; bf16 calls round a probability once, to bf16's 8 bits, fp32 calls keep 24 bits of queries and probabilities. A query with
+ * sums are fp32; bf16 calls round a probability once, to bf16's 8 bits, fp32 calls keep 24 bits of probabilities and of queries' elements (of 2^-100
+ * and more: below that the lowest bits go). A query with
  * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN for the rows that see it, and
  * changes no other; a score times log2(e) beyond fp32's range gives NaN too. Latent elements are up to 2^100, or their sums may leave that range. scale times log2(e) is finite; out may not overlap q. Results do not
  * depend on the order in which CTAs run, and are the same bits for the same call. Any number of new rows is right; prompts in bf16 are
@@ -610,11 +611,12 @@ typedef struct { const void* p; int64_t head_stride, row_stride; } spm_matrices;
  * heads, over the tokens up to the row's own position, with key = [W_k latent | key of the row] and value = W_v latent made from the cache for
  * all tokens of the batch's sequences, a round of heads at a time. q: heads of head_dim + rope_dim elements. head_dim: 64 or 128.
  * n_tokens: at least the tokens of all sequences that have rows in this batch (the sum of their lengths), which is what the workspace has
- * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. n_tokens + 127 n_seq is below 2^30. dtype: bf16 (fp32 rows have the absorbed form). Results are
- * rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two: a query's element keeps fewer bits below
- * 2^-23 of its head's largest, a key's below 2^-23 of the largest of its 32 tokens and head, a value below 2^-18 of its head's largest so far, a
- * probability below 2^-18 of its row's largest; statistics and sums are fp32. What is said above of queries and rows that are not finite holds.
- * An element of a key of 2^109 or more counts as one that is not finite.
+ * room for; tokens beyond that do not exist, and SPM_KV_TOO_LONG is recorded. n_tokens + 127 n_seq is below 2^30. dtype: bf16 (fp32 rows have
+ * the absorbed form). Results are rounded to bf16; keys, queries, values and probabilities are fp16 numbers, of 11 bits, times powers of two. A query's
+ * element keeps fewer bits below 2^-23 of its head's largest, a value below 2^-18 of its head's largest so far, a probability below 2^-18 of its row's
+ * largest. A key's element keeps fewer below 2^-14 (it is off by 2^-25 at most there) where the largest of its 32 tokens and head is from 2^-4 up to
+ * 2^15, and elsewhere below 2^-23 of that largest. Statistics and sums are fp32. What is said above of queries and rows that are not finite holds. An
+ * element of a key of 2^109 or more counts as one that is not finite.
  * workspace: dev, 256-byte aligned, at least spm_latent_attend_expanded_workspace() bytes (n_tokens * n_heads * (head_dim + 32) * 4 and a little more, but
  * not much over 512 MB where a head takes less); one for each of calls that may run at the same time. */
 int spm_latent_attend_expanded_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int head_dim, int n_tokens, int dtype,
@@ -625,7 +627,8 @@ int spm_latent_attend_expanded(const spm_latent_cache* kv, const spm_kv_batch* b
 
 /* y_h = x_h W_h (transposed 0: W_h is [in_dim][out_dim]) or x_h W_h^T (else: [out_dim][in_dim]) for each head h of each of n_rows rows. w: dev,
  * bf16, element (h, i, j) at h * w_head_stride + i * w_row_stride + j; 16-byte aligned, strides multiples of 8. in_dim and out_dim: multiples
- * of 64, at most 8192. Products of fp32 rows are exact, sums fp32. y may not overlap x. dtype: of x and y. */
+ * of 64, at most 8192. Products of fp32 rows are exact (of elements of 2^-100 and more: below that the lowest bits go), sums fp32. y may not overlap
+ * x. dtype: of x and y. */
 int spm_head_product(const spm_rows* x, const void* w, int64_t w_head_stride, int64_t w_row_stride, int transposed, const spm_rows* y, int n_rows,
                      int n_heads, int in_dim, int out_dim, int dtype, void* stream);
 

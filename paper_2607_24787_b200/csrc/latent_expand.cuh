@@ -1,11 +1,12 @@
 // Keys and values of a batch's tokens, made from their latent vectors for one head after another, on tcgen05.
 //
 // [key | value] of a head = C [W_k ; W_v]^T: 128 tokens of one sequence, all of their latent vectors in shared memory, against the head's
-// matrices, whose rows come by in chunks of 64 elements. Sums of two heads are in tensor memory, so that one is rounded to bf16 and
+// matrices, whose rows come by in chunks of 64 elements. Sums of two heads are in tensor memory, so that one is rounded to fp16 and
 // written while the next is made. All (tile of tokens, head) pairs are a line that is cut evenly between CTAs, so that a CTA brings the latent
-// vectors of two or three tiles and not of many (with a CTA for each tile and a third of the heads four prompts' 10563 tokens of 16 heads took
-// 59 us, with the cut 54; 56 since keys and values have powers of two: 0.80 PFLOP/s). What bounds it: the products of a tile and head, some 4500 cycles, and the results' way out of
-// tensor memory and the SM, which is longer than these and only partly beside them. Sequences stand behind each other in the workspace, each from a multiple of 128 tokens on.
+// vectors of two or three tiles and not of many: four prompts' 10563 tokens of 16 heads take 56 us, 0.80 PFLOP/s (54 with the cut before there were powers of
+// two, 59 with a CTA for each tile and a third of the heads). What bounds it: the products of a tile and head, some 4500 cycles, and the results' way
+// out of tensor memory and the SM, which is longer than these and only partly beside them. Sequences stand behind each other in the workspace, each
+// from a multiple of 128 tokens on.
 //
 // Both are fp16, times a power of two for each 32 tokens of a head: bf16's roundings of keys, values and probabilities were together 1.4 times that
 // of the result. A key's power is 1 where the largest of its 32 tokens is in fp16's range as it is, which it is but for odd models, and the part
