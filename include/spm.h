@@ -592,7 +592,8 @@ int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, cons
 
 /* out (n_heads heads of latent_dim elements) = softmax(scale q . row) latent for each new row and each of its n_heads heads, q of latent_dim +
  * rope_dim elements, over the tokens up to the row's own position. A row that sees no token gives zeros. The softmax's statistics and all
- * sums are fp32; bf16 calls round a probability once, to bf16's 8 bits, fp32 calls keep 24 bits of probabilities and of queries' elements (of 2^-100
+ * sums are fp32; bf16 calls keep 16 bits of a probability, but 8 where a block of columns (a sequence's new rows times heads, in equal blocks of
+ * 64 at most) is over 48, fp32 calls 24 bits of probabilities and of queries' elements (of 2^-100
  * and more: below that the lowest bits go). A query with
  * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN for the rows that see it, and
  * changes no other; a score times log2(e) beyond fp32's range gives NaN too. Latent elements are up to 2^100, or their sums may leave that range. scale times log2(e) is finite; out may not overlap q. Results do not

@@ -13,7 +13,9 @@
 //
 // fp32 queries and probabilities are three bf16 parts each, cut off and not rounded: three columns side by side in one product, added up
 // as scores and results are read. Their sums leave the products every kLaAside tiles, which cut sums off where they do not round them: with 63 tiles of
-// one sign in them results were 1.1e-5 too small, now they are as near as plain fp32 ones. bf16 calls round a probability to bf16's 8 bits once.
+// one sign in them results were 1.1e-5 too small, now they are as near as plain fp32 ones. bf16 calls' probabilities are two such parts (results then differ
+// from plain fp32 arithmetic's by their own rounding alone; 64 sequences 103 -> 107 us), but with 64 columns, whose second parts neither shared memory nor
+// tensor memory has room for: one, of 8 bits (0.0020 of a result where its own rounding is 0.0017).
 //
 // All (sequence, columns) items together are a line of tiles that is cut evenly between CTAs, whatever the lengths are. An item's parts
 // in several CTAs go to the workspace and latent_join_kernel adds them in order. (Items count with all of a sequence's tokens; columns that
@@ -62,11 +64,12 @@ constexpr int kLaAside = 4;                      // tiles whose sums an fp32 cal
 
 template <typename T, int COLS>
 struct LaShape {
-    static constexpr int parts = sizeof(T) == 4 ? 3 : 1;     // of a number
-    static constexpr int n = COLS * parts;                   // N of the products
-    static_assert((2 + 4) * n + (parts == 3 ? 4 * COLS : 0) <= 512 && n % 16 == 0, "O^T of 512 elements, two buffers of S^T, and sums aside fit tensor memory");
+    static constexpr int parts = sizeof(T) == 4 ? 3 : 1;                             // of a query's number
+    static constexpr int p_parts = sizeof(T) == 4 ? 3 : COLS <= 48 ? 2 : 1;          // of a probability (64 columns: shared memory has room for one)
+    static constexpr int n = COLS * parts, n_o = COLS * p_parts;                     // N of the products
+    static_assert(2 * n + 4 * n_o + (parts == 3 ? 4 * COLS : 0) <= 512 && n % 16 == 0, "O^T of 512 elements, two buffers of S^T, and sums aside fit tensor memory");
     static constexpr int q_bytes(int chunks) { return chunks * n * 128; }
-    static constexpr int p_bytes = n * 128;
+    static constexpr int p_bytes = n_o * 128;
     static constexpr int fixed(int chunks) { return 1024 + q_bytes(chunks) + p_bytes; }
     static constexpr int part_floats(int latent) { return COLS * (latent + 2); }     // sums, then maxima, then sums of probabilities
 };
@@ -199,7 +202,7 @@ struct LaWalk {
 template <typename T, int COLS>
 __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const LatentAttendArgs a, const __grid_constant__ CUtensorMap rows_map) {
     using S = LaShape<T, COLS>;
-    constexpr int N = S::n, PARTS = S::parts, BLOCKS = COLS / 8;
+    constexpr int N = S::n, NO = S::n_o, PARTS = S::parts, P_PARTS = S::p_parts, BLOCKS = COLS / 8;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     // (the kernel's own arrays first: they take the room that aligning the rest would)
     LaShared& sh = *reinterpret_cast<LaShared*>(raw_smem);
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t t_s = sh.tmem, t_o = t_s + 2 * N, aside_at = t_o + latent / 128 * N;
+    const uint32_t t_s = sh.tmem, t_o = t_s + 2 * N, aside_at = t_o + latent / 128 * NO;
 
     // a warp goes on, or gives up, as one
     auto wait = [&](const unsigned long long& bar, int parity) {
@@ -469,9 +472,9 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
 #pragma unroll 1
                             for (int mt = 0; mt < latent / 128; ++mt)
 #pragma unroll 1
-                                for (int ch = 0; ch < N / 16 + aside; ++ch) {
+                                for (int ch = 0; ch < NO / 16 + aside; ++ch) {
                                     uint32_t o[16];
-                                    const uint32_t at = (ch < N / 16 ? t_o + mt * N + ch * 16 : aside_at + mt * 16) + (uint32_t(warp) << 21);
+                                    const uint32_t at = (ch < NO / 16 ? t_o + mt * NO + ch * 16 : aside_at + mt * 16) + (uint32_t(warp) << 21);
                                     tmem_ld16_raw(at, o);
                                     tmem_wait_ld();
 #pragma unroll
@@ -492,7 +495,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             const uint32_t to = aside_at + mt * 16 + (uint32_t(warp) << 21);
                             uint32_t o[PARTS][16], v[16] = {};
 #pragma unroll
-                            for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + (uint32_t(warp) << 21), o[u]);
+                            for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * NO + u * COLS + (uint32_t(warp) << 21), o[u]);
                             if (aside) tmem_ld16_raw(to, v);
                             tmem_wait_ld();
 #pragma unroll
@@ -520,9 +523,14 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                         const float x = s[i + k / 2][(k & 1) * 2], y = s[i + k / 2][(k & 1) * 2 + 1];
                         if constexpr (PARTS == 3) cut_parts(x, y, p[k]);
                         else p[k][0] = pack_bf16(x, y);
+                        if constexpr (P_PARTS == 2) {
+                            float x0, y0;
+                            two_bf16(p[k][0], x0, y0);
+                            p[k][1] = pack_bf16(x - x0, y - y0);
+                        }
                     }
 #pragma unroll
-                    for (int u = 0; u < PARTS; ++u) st_matrix_trans(to + (u * COLS + 8 * i) * 128, p[0][u], p[1][u], p[2][u], p[3][u]);
+                    for (int u = 0; u < P_PARTS; ++u) st_matrix_trans(to + (u * COLS + 8 * i) * 128, p[0][u], p[1][u], p[2][u], p[3][u]);
                 }
                 fence_proxy_async();
                 tc_fence_before();
@@ -582,17 +590,18 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
 #pragma unroll 1
                     for (int mt = 0; mt < latent / 128; ++mt) {
                         const int d = mt * 128 + tid;
-                        uint32_t o[PARTS][16] = {}, before[16] = {};
+                        uint32_t o[P_PARTS][16] = {}, before[16] = {};
                         if (w.tiles > 0) {
                             if (PARTS == 3 && aside) tmem_ld16_raw(aside_at + mt * 16 + (uint32_t(warp) << 21), before);
 #pragma unroll
-                            for (int u = 0; u < PARTS; ++u) tmem_ld16_raw(t_o + mt * N + u * COLS + ch * 16 + (uint32_t(warp) << 21), o[u]);
+                            for (int u = 0; u < P_PARTS; ++u) tmem_ld16_raw(t_o + mt * NO + u * COLS + ch * 16 + (uint32_t(warp) << 21), o[u]);
                             tmem_wait_ld();
                         }
                         float v[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             v[i] = __uint_as_float(o[0][i]);
+                            if constexpr (P_PARTS == 2) v[i] += __uint_as_float(o[1][i]);
                             if constexpr (PARTS == 3) v[i] = __uint_as_float(o[2][i]) + __uint_as_float(o[1][i]) + v[i] + __uint_as_float(before[i]);
                         }
                         if (!whole) {
@@ -673,7 +682,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
         __syncwarp();
     } else {
         // ---- products. The warp walks as one, so that the elected lane is one lane throughout ----
-        const uint32_t idesc_s = la_idesc(kLaTile, N, false), idesc_o = la_idesc(128, N, true);
+        const uint32_t idesc_s = la_idesc(kLaTile, N, false), idesc_o = la_idesc(128, NO, true);
         const int rope_steps = a.kv.rope / 16, m_tiles = latent / 128;
         int st = 0, turn = 0, item = 0;
         unsigned it = 0;
@@ -718,7 +727,7 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                     tc_mma_lo<true>(d, lo_a + 256, hi_m, lo_p + 4, hi_k, idesc_o);
                     tc_mma_lo<true>(d, lo_a + 384, hi_m, lo_p + 6, hi_k, idesc_o);
                     lo_a += 2 * kLaChunkBytes >> 4;
-                    d += N;
+                    d += NO;
                 }
                 tc_commit(smem_u32(&sh.empty[stage]));
             }
