@@ -597,8 +597,8 @@ int spm_latent_write(const spm_latent_cache* kv, const spm_kv_batch* batch, cons
  * and more: below that the lowest bits go). A query with
  * a NaN or an infinity gives NaN for its head, unless it sees no token. A cache row that is not finite gives NaN for the rows that see it, and
  * changes no other; a score times log2(e) beyond fp32's range gives NaN too. Latent elements are up to 2^100, or their sums may leave that range. scale times log2(e) is finite; out may not overlap q. Results do not
- * depend on the order in which CTAs run, and are the same bits for the same call. Any number of new rows is right; prompts in bf16 are
- * faster in the expanded form.
+ * depend on the order in which CTAs run, and are the same bits for the same call. Any number of new rows is right; prompts in bf16 of some
+ * hundred rows are faster in the expanded form.
  * workspace: dev, 16-byte aligned, at least spm_latent_attend_workspace() bytes; what it held before does not matter, and calls that may run
  * at the same time need one each. */
 int spm_latent_attend_workspace(const spm_latent_cache* kv, const spm_kv_batch* batch, int n_heads, int dtype, size_t* bytes);

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(WARPS * 32) head_product_kernel(const HeadProd
 // elements come into shared memory by asynchronous copies, several ahead, so that every weight and every element comes from memory once.
 // Elements and outputs are numbered as above. 16-byte units of a row are moved by the row's number so that what eight (or, of 8 bytes, 16)
 // threads read together lies in different banks. What bounds it with fp32 rows, whose parts make three products of one, is mma.sync, some 16 cycles
-// a product and scheduler (64 rows, 128 heads from 512 to 128: 16 us, the kernel above 19).
+// a product and scheduler (64 rows, 128 heads from 512 to 128: 18 us, the kernel above 21, both with cold caches).
 constexpr int kHtRows = 64, kHtOut = 128, kHtChunk = 64, kHtStages = 5, kHtThreads = 256;
 template <typename T>
 struct HtShape {

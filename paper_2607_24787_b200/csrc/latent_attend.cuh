@@ -21,7 +21,7 @@
 // in several CTAs go to the workspace and latent_join_kernel adds them in order. (Items count with all of a sequence's tokens; columns that
 // see fewer, as a prompt's do, leave their CTA idle for the others. Such calls are few: prompts have the expanded form.)
 //
-// What bounds it: DRAM, with 16 columns (64 sequences, 536 MB of rows of 512 + 64: 97.5 us, 5.5 TB/s); with 64, of whose queries beside shared memory
+// What bounds it: DRAM, with 16 columns (64 sequences, 536 MB of rows of 512 + 64: 100.5 us, 5.4 TB/s); with 64, of whose queries beside shared memory
 // has room for two tiles only, a tile's copy, scores, softmax and sums waiting for one another (3700 cycles a tile, 2300 of them products; 32 sequences, 145 MB,
 // 128 heads: 80 us). A few tiles a CTA: the way to the first scores and from the last sums.
 #pragma once

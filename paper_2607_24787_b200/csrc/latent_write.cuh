@@ -21,7 +21,8 @@ struct LatentWriteArgs {
 // A warp takes a row, or one of gridDim.y parts of its query heads (the first part the cache's row too). A lane holds eight elements of a head,
 // rope / 8 lanes a head, so a warp takes several heads at once. A row's angles, taken in 64 bits (far positions), are one a lane (at most 64
 // elements turn) and pass through shared memory to the lanes that need them. The norm's sum is fp32, what it scales being rounded to bf16's 8 bits.
-// With a head at a time, an element pair a lane, 18124 prompt rows of 16 heads took 76 us, 33 now (135 MB); what bounds it is issue, two thirds of the slots.
+// With a head at a time, an element pair a lane, 18124 prompt rows of 16 heads took 76 us, 33.5 now (135 MB); 1271
+// instructions a row fill two thirds of the issue slots, the rest waits for loads, with 44 % of the warps that an SM holds.
 template <typename T>
 __global__ void __launch_bounds__(kKvWarps * 32, 4) latent_write_kernel(const LatentWriteArgs a) {
     constexpr int AHEAD = 2;           // vectors in flight (four: registers spill, 41 us for 38 with nothing in L2)
