@@ -247,10 +247,12 @@ __global__ void __launch_bounds__(kLpThreads, 1) latent_prompt_kernel(const Late
             for (int ch = 0; ch < 4; ++ch)
                 if (whole || there[ch] != 0) power_top = max(power_top, power[ch]);
             const bool any = (there[0] | there[1] | there[2] | there[3]) != 0;      // (rows that there are not would scale sums at every tile)
-            if (__any_sync(0xffffffffu, (any && m == -INFINITY) || (peak - m) * f > kLpSlack || power_top > run + kLpRoom)) {
+            // (a row moves its maximum when it has to and not with the warp's others, so that its bits are its own; one that is NaN already need not)
+            const bool moves = (any && m == -INFINITY && l == l) || (peak - m) * f > kLpSlack;
+            if (__any_sync(0xffffffffu, moves || power_top > run + kLpRoom)) {
                 // (scores of a query with an infinity may all be -infinity, as those of tokens that it does not see are: NaN)
                 if (any && m == -INFINITY && peak == -INFINITY) l = __int_as_float(0x7fffffff);
-                const float to = fmaxf(m, peak), by = m == -INFINITY ? 1.f : ex2((m - to) * f);
+                const float to = moves ? fmaxf(m, peak) : m, by = m == -INFINITY ? 1.f : ex2((m - to) * f);
                 m = to;
                 l *= by;
                 const int run_then = power_top > run + kLpRoom ? power_top : run;

@@ -264,3 +264,60 @@ def test_errors_of_ordinary_calls(lib, lengths, rows, heads, latent, rope, limit
     got = f64(c.cache.attend(c.batch, q, (128 + rope) ** -0.5))
     want = R.attend(f64(q), f64(c.start), c.table.numpy(), lengths, c.row_start, (128 + rope) ** -0.5, latent)[0]
     assert np.linalg.norm(got - want) <= limit * np.linalg.norm(want)
+
+
+# ---- queries that are not finite, waits that run out ---------------------------------
+SHARED = [  # form, lengths, new rows, heads: one tile; several; cut between CTAs; columns of 16, 32, 48 and 64; prompts
+    ("bf16", [20], [1], 8), ("fp32", [1], [1], 2), ("bf16", [300, 40], [2, 1], 16), ("fp32", [300, 40], [2, 1], 16), ("bf16", [5000], [1], 8), ("fp32", [9000], [1], 3),
+    ("bf16", [3000, 9], [5, 1], 16), ("bf16", [3000, 200], [1, 1], 64), ("fp32", [700], [3], 20), ("expanded", [300, 200], [300, 200], 3), ("expanded", [20], [20], 2),
+    ("expanded", [500, 1], [280, 1], 2),
+]
+
+
+def form_of(form, lengths, rows, heads):
+    c = Case(form_of.lib, 63, lengths, rows, 256, 32, 16, FP32 if form == "fp32" else BF16, 1, fill=True)
+    w = torch.randn(heads, 128, 256, generator=c.g).mul(0.1).to(BF16).cuda()
+    q = c.randn(c.n_rows, heads, 96 if form == "expanded" else 288)
+
+    def run():
+        if form == "expanded":
+            return c.cache.attend_expanded(c.batch, q, w[:, :64], w[:, 64:], 0.1, sum(lengths))[:c.n]
+        return c.cache.attend(c.batch, q, 0.1)[:c.n]
+    return c, q, run
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("form,lengths,rows,heads", SHARED)
+def test_queries_that_are_not_finite(lib, form, lengths, rows, heads, bad):  # noqa: F811
+    """A head whose query holds a NaN or an infinity gives NaN, however its tokens are shared out; the other heads give the same bits."""
+    form_of.lib = lib
+    c, q, run = form_of(form, lengths, rows, heads)
+    good = run()
+    assert good.isfinite().all()
+    hit = {(0, 0), (c.n - 1, heads - 1), (c.n // 2, heads // 2)}
+    for i, h in hit:
+        q[i, h, (5 * i + 37 * h) % q.shape[2]] = bad
+    out = run()
+    for i, h in hit:
+        assert out[i, h].isnan().all()
+        out[i, h] = good[i, h]
+    assert torch.equal(out, good)
+
+
+@pytest.mark.parametrize("form,lengths,rows,heads", SHARED)
+def test_a_wait_that_runs_out(lib, form, lengths, rows, heads):  # noqa: F811
+    """An arrival that nobody makes: the kernels give up after the limit and say so, and the next call is what it was."""
+    from paper_2607_24787_b200 import binding as B
+    form_of.lib = lib
+    c, q, run = form_of(form, lengths, rows, heads)
+    want = run()
+    assert c.status.item() == 0
+    try:
+        B.spm_test_kv_waits(1, 1000)
+        run()
+        torch.cuda.synchronize()
+    finally:
+        B.spm_test_kv_waits(0, 0)
+    assert c.status.item() == B.KV_TIMEOUT
+    c.status.zero_()
+    assert torch.equal(run(), want) and c.status.item() == 0
