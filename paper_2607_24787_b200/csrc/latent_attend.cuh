@@ -455,8 +455,8 @@ __global__ void __launch_bounds__(kLaThreads, 1) latent_attend_kernel(const Late
                             for (int e = 0; e < 2; ++e) {
                                 const int col = 8 * i + c2 + e;
                                 float top = fmaxf(fmaxf(red[col], red[COLS + col]), fmaxf(red[2 * COLS + col], red[3 * COLS + col]));
-                                // (nothing seen: stays. Only the first tile's may be below zero)
-                                if (top == -INFINITY || (!first && top < 0.f)) top = 0.f;
+                                // (nothing seen, or no reason to move but that another column has one: stays. The first tile's may be below zero)
+                                if (top == -INFINITY || (!first && top <= kLaSlack)) top = 0.f;
                                 m[i][e] += top;
                                 by[i][e] = first ? 1.f : ex2(-top);
                                 l[i][e] *= by[i][e];

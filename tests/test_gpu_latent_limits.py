@@ -321,3 +321,20 @@ def test_a_wait_that_runs_out(lib, form, lengths, rows, heads):  # noqa: F811
     assert c.status.item() == B.KV_TIMEOUT
     c.status.zero_()
     assert torch.equal(run(), want) and c.status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_a_score_that_is_not_finite_behind_others(lib, dtype):  # noqa: F811
+    """An infinity in a query meets keys of one sign first and of the other later: its head gives NaN, the heads beside it the same bits."""
+    c = Case(lib, 64, [320] * 160, [1] * 160, 128, 16, 64, dtype, fill=True)
+    for s in range(160):
+        c.start[c.table[s, 0], :, 130] = -1.0
+        c.start[c.table[s, 1:5].long(), :, 130] = 1.0
+    c.cache.pages.copy_(c.start)
+    q = c.randn(160, 6, 144)
+    good = c.cache.attend(c.batch, q, 0.3)
+    q[:, 2, 130] = float("inf")
+    out = c.cache.attend(c.batch, q, 0.3)
+    assert out[:, 2].isnan().all()
+    out[:, 2] = good[:, 2]
+    assert torch.equal(out, good)
